@@ -253,6 +253,97 @@ int tlq_apply_layer(const void* X, int64_t N, int64_t C1, const void* W, int64_t
                     const void* bias, const tlq_config* cfg, void* workspace, size_t workspace_bytes,
                     uint8_t* codes, float* steps, int32_t* zeros, void* Yq, void* stream);
 
+/*
+ * ------------------------------------------------------------------------------------------------------------------
+ * Serving a calibrated layer (symmetric mode).  What runs the layer that the calls above have calibrated, from the codes
+ * that they returned: the 8-bit product, the write of keys and values into an 8-bit cache, and attention over it.  The
+ * calls were added without a change to any earlier one.
+ *  - Workspaces of these calls are ZEROED ONCE by their owner and then kept: the calls leave their counters at zero.  One
+ *    workspace serves any number of calls on one stream; streams that run at the same time need one each.  The status
+ *    word (byte 0, tlq_read_status) is not reset by these calls: it keeps the last error until its owner zeroes the
+ *    workspace again.
+ *  - Lengths and block tables are read on the device, so a call never synchronises.  An entry that does not fit (a length
+ *    beyond the table, a block outside of the cache, a position outside of the angle table) sets the status word to
+ *    TLQ_ERR_SHAPE; what it concerns is left out, and nothing is accessed out of bounds.
+ *  - T = 0 or N = 0 (nothing to do in this step) is TLQ_OK and launches nothing.
+ */
+
+/*
+ * The product of kept codes: Y[n,o] = t[n] u[o] sum_c Xq[n,c] Wq[o,c] + bias[o], rounded to bf16 once (the sum is an exact
+ * 32-bit integer).
+ *   Xq [N,C1] int8 and t [N] fp32 as tlq_quantize_activations returns them (steps of tokens),
+ *   Wq [C2,C1] int8 and u [C2] fp32 as tlq_quantize_weights returns them (steps of output channels; w_bits up to 8),
+ *   bias [C2] bf16 or NULL, Y [N,C2] bf16.  C1 a multiple of 16 up to 131056 (the integer sum stays below 2^31); any C2.
+ */
+size_t tlq_linear_i8_workspace_bytes(int64_t N, int64_t C1, int64_t C2);
+int tlq_linear_i8(const int8_t* Xq, const float* t, int64_t N, int64_t C1, const int8_t* Wq, const float* u, int64_t C2,
+                  const void* bias, void* workspace, size_t workspace_bytes, void* Y, void* stream);
+
+/*
+ * The 8-bit cache of one layer.  A block holds TLQ_KV_BLOCK tokens of one request.  Keys and values are int8 codes with
+ * one step per block and kv head (the quantizer of Sec. 2.2 with n = 8: step = max|.| / 127, floor 1e-5 on the maximum).
+ * Keys lie token by channel, values channel by token.
+ */
+#define TLQ_KV_BLOCK 64
+typedef struct {
+  uint32_t struct_size; /* sizeof(tlq_kv_cache); checked */
+  int32_t n_kv_heads;
+  int32_t head_dim;     /* 64 or 128 */
+  int32_t n_blocks;
+  int8_t* k_codes;      /* [n_blocks, n_kv_heads, 64, head_dim] */
+  int8_t* v_codes;      /* [n_blocks, n_kv_heads, head_dim, 64] */
+  float* k_steps;       /* [n_blocks, n_kv_heads] */
+  float* v_steps;       /* [n_blocks, n_kv_heads] */
+} tlq_kv_cache;
+
+/* The requests of one step.  Request b owns rows [cu_q[b], cu_q[b+1]) of the call's token tensors (none is allowed); they
+ * are the last ones of its kv_len[b] cached tokens, the new ones included.  Token j of its context lies in block
+ * block_table[b, j / 64]. */
+typedef struct {
+  uint32_t struct_size; /* sizeof(tlq_kv_batch); checked */
+  int32_t n_requests;   /* 1 .. 65535 */
+  int32_t max_q_len;    /* upper bound of cu_q[b+1] - cu_q[b] (host) */
+  int32_t max_blocks;   /* columns of block_table */
+  const int32_t* cu_q;        /* [n_requests + 1] */
+  const int32_t* kv_len;      /* [n_requests] */
+  const int32_t* block_table; /* [n_requests, max_blocks] */
+} tlq_kv_batch;
+
+/* Workspace of the two calls below, for steps of up to T tokens (zeroed once by its owner, see above). */
+size_t tlq_kv_workspace_bytes(const tlq_kv_cache* cache, const tlq_kv_batch* batch, int32_t n_heads, int64_t T);
+
+/*
+ * Norm and rotate the queries and keys of a step's tokens, and write keys and values into the cache, in one pass.
+ *   qkv [T, >= (n_heads + 2 n_kv_heads) * head_dim] bf16, rows ld elements apart (a multiple of 8): the queries of all
+ *     heads, then the keys, then the values of the kv heads (what a projection by the row-concatenated weights returns).
+ *   q_norm, k_norm [head_dim] bf16 or NULL: y = x * rsqrt(mean over the head's channels of x^2 + eps) * w.
+ *   positions [n_axes, T] int32 or NULL (no rotation), cos_sin [n_positions, head_dim] fp32: the cosines of the
+ *     head_dim / 2 pairs, then the sines.  Pair (i, i + head_dim/2) turns by the angle of its axis' position; the first
+ *     sections[0] pairs take axis 0, the next sections[1] axis 1, the rest axis 2 (sections: host, n_axes entries that add
+ *     up to head_dim / 2; may be NULL for one axis).  n_axes is 1 or 3.
+ *   q_out [T, n_heads, head_dim] bf16.
+ *   k_values, v_values [T, n_kv_heads, head_dim] bf16 or NULL: the values that the new codes stand for, code * step (what
+ *     later steps see; PassAct2 calibration propagates them).
+ * A block that already holds tokens of its request keeps the larger of its step and the new tokens' one; when it grows, the
+ * older codes follow: c <- rint(c * old / new).  Codes saturate at +-127.  Values that are not finite take no part in a
+ * step: an infinity saturates, a NaN becomes 0, and the status word is set to TLQ_ERR_NONFINITE.
+ */
+int tlq_kv_store(const void* qkv, int64_t T, int64_t ld, int32_t n_heads, const tlq_kv_cache* cache,
+                 const tlq_kv_batch* batch, const int32_t* positions, int32_t n_axes, const int32_t* sections /* host */,
+                 const float* cos_sin, int64_t n_positions, const void* q_norm, const void* k_norm, float eps,
+                 void* q_out, void* k_values, void* v_values, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention over the cache: out = sum_j softmax_j(scale * q . k_j) v_j over the cached tokens j of the row's request; with
+ * causal != 0 over those up to the row's own place only.  Query head i reads kv head i / (n_heads / n_kv_heads).
+ *   q [T, n_heads, head_dim] bf16, rows ldq elements apart (a multiple of 8); out [T, n_heads, head_dim] bf16;
+ *   lse [T, n_heads] fp32 or NULL: ln sum_j exp(scale * q . k_j).  scale > 0 and finite.
+ * A row that sees nothing (no cached token, or a place before the first) gets zeros and lse = -infinity.
+ */
+int tlq_kv_attention(const void* q, int64_t T, int64_t ldq, int32_t n_heads, const tlq_kv_cache* cache,
+                     const tlq_kv_batch* batch, float scale, int32_t causal, void* workspace, size_t workspace_bytes,
+                     void* out, float* lse, void* stream);
+
 /* Synchronise `stream` and return the device status word of `workspace` (TLQ_OK, TLQ_ERR_TIMEOUT,
  * TLQ_ERR_NONFINITE) or TLQ_ERR_CUDA if the stream reports an error. */
 int tlq_read_status(const void* workspace, void* stream);

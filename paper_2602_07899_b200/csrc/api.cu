@@ -25,8 +25,6 @@ int device_sm_count() {
 
 namespace {
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 int check_cfg(const tlq_config* cfg, int64_t C1, bool need_quantizer = true) {
   if (cfg == nullptr || cfg->struct_size != sizeof(tlq_config)) return TLQ_ERR_INVALID_ARG;
   if ((cfg->flags & ~(uint32_t)(TLQ_FLAG_SKIP_ZERO_WEIGHT_TOKENS | TLQ_FLAG_GEMM_CTA_PAIRS | TLQ_FLAG_GEMM_NARROW_TILES |
@@ -46,15 +44,6 @@ int check_cfg(const tlq_config* cfg, int64_t C1, bool need_quantizer = true) {
     if ((C1 % 16) != 0) return TLQ_ERR_SHAPE;
   } else {
     return TLQ_ERR_INVALID_ARG;
-  }
-  return TLQ_OK;
-}
-
-int have_device() {
-  int n = 0;
-  if (cudaGetDeviceCount(&n) != cudaSuccess || n < 1) {
-    cudaGetLastError();
-    return TLQ_ERR_CUDA;
   }
   return TLQ_OK;
 }

@@ -1,0 +1,314 @@
+// Norms of queries and keys, position rotation and the write of keys and values into the 8-bit cache, in one pass over
+// the rows of the fused projection.
+//
+// Per head h of a token with place p:  y = x * rsqrt(mean_c x_c^2 + eps) * w  (queries and keys, when w is given),
+// (y_i, y_{i+D/2}) <- (y_i cos - y_{i+D/2} sin, y_{i+D/2} cos + y_i sin) with the angle of pair i, queries rounded to
+// bf16 once.  Keys and values are quantized as the layer's activations are (paper Sec. 2.2, symmetric, n = 8), with one
+// step for the 64 tokens of a cache block and one head: step = max|.| / 127.  A block that already holds tokens of its
+// request keeps the larger of its old step and the new tokens' one; when it grows, the older codes follow it,
+// c <- rint(c * old / new).
+//
+// All statistics and products are in 32 bits; the quantizer's division is the IEEE one, so that codes of values (which
+// see no norm) are those of the definition.
+//
+// Bound: bytes.  The rows are read once and everything is kept in registers between the maximum and the codes.  One CTA
+// owns a cache block of one head (its tokens lie in one request), because its step needs all of them; the remaining CTAs
+// stream query rows, 64 per CTA.  Values lie channel by token in the cache (what a matrix instruction over tokens
+// reads), so a CTA turns its 64 x D bytes in shared memory and writes rows of 64 bytes.
+#include "serve.cuh"
+
+namespace tlq {
+namespace {
+
+constexpr int kStoreThreads = 256;
+
+struct StoreArgs {
+  const uint16_t* qkv;
+  int64_t ld;
+  RopeArgs rope;
+  const uint16_t* q_norm;
+  const uint16_t* k_norm;
+  float eps;
+  uint16_t* q_out;
+  uint16_t* k_values;
+  uint16_t* v_values;
+  unsigned kv_ctas;           // CTAs of the cache part; the rest stream query rows
+};
+
+// Channels of one lane: [4 l, 4 l + 4) and the same of the upper half, so that both members of its four rotation pairs
+// are its own.  A row takes D / 8 lanes.
+template <int D>
+struct Row {
+  float lo[4], hi[4];
+};
+
+template <int D>
+__device__ __forceinline__ void load_row(Row<D>& r, const uint16_t* p, int l) {
+  const uint2 a = *reinterpret_cast<const uint2*>(p + 4 * l);
+  const uint2 b = *reinterpret_cast<const uint2*>(p + D / 2 + 4 * l);
+  r.lo[0] = __uint_as_float(a.x << 16); r.lo[1] = __uint_as_float(a.x & 0xFFFF0000u);
+  r.lo[2] = __uint_as_float(a.y << 16); r.lo[3] = __uint_as_float(a.y & 0xFFFF0000u);
+  r.hi[0] = __uint_as_float(b.x << 16); r.hi[1] = __uint_as_float(b.x & 0xFFFF0000u);
+  r.hi[2] = __uint_as_float(b.y << 16); r.hi[3] = __uint_as_float(b.y & 0xFFFF0000u);
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+template <int D>
+__device__ __forceinline__ void store_row(uint16_t* p, const float (&lo)[4], const float (&hi)[4], int l) {
+  *reinterpret_cast<uint2*>(p + 4 * l) = make_uint2(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]));
+  *reinterpret_cast<uint2*>(p + D / 2 + 4 * l) = make_uint2(pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]));
+}
+
+template <int D>
+__device__ __forceinline__ void norm_row(Row<D>& r, const Row<D>& w, float eps) {
+  float s = 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) s = fmaf(r.lo[j], r.lo[j], fmaf(r.hi[j], r.hi[j], s));
+#pragma unroll
+  for (int o = D / 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+  const float k = rsqrtf(s * (1.0f / D) + eps);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    r.lo[j] = r.lo[j] * k * w.lo[j];
+    r.hi[j] = r.hi[j] * k * w.hi[j];
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void rotate_row(Row<D>& r, const RopeArgs& rope, int64_t T, int64_t token, int l,
+                                           WorkspaceHeader* hdr) {
+  float c[4], s[4];
+  if (rope.n_axes == 1) {
+    int64_t pos = rope.positions[token];
+    if (pos < 0 || pos >= rope.n_positions) {
+      report_status(hdr, TLQ_ERR_SHAPE, 201);
+      pos = 0;
+    }
+    const float4 cc = *reinterpret_cast<const float4*>(rope.cos_sin + pos * D + 4 * l);
+    const float4 ss = *reinterpret_cast<const float4*>(rope.cos_sin + pos * D + D / 2 + 4 * l);
+    c[0] = cc.x; c[1] = cc.y; c[2] = cc.z; c[3] = cc.w;
+    s[0] = ss.x; s[1] = ss.y; s[2] = ss.z; s[3] = ss.w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int pair = 4 * l + j;
+      const int axis = (pair >= rope.pairs_end[0] ? 1 : 0) + (pair >= rope.pairs_end[1] ? 1 : 0);
+      int64_t pos = rope.positions[axis * T + token];
+      if (pos < 0 || pos >= rope.n_positions) {
+        report_status(hdr, TLQ_ERR_SHAPE, 201);
+        pos = 0;
+      }
+      c[j] = rope.cos_sin[pos * D + pair];
+      s[j] = rope.cos_sin[pos * D + D / 2 + pair];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float a = r.lo[j], b = r.hi[j];
+    r.lo[j] = a * c[j] - b * s[j];
+    r.hi[j] = b * c[j] + a * s[j];
+  }
+}
+
+// Largest finite magnitude; anything not finite is reported by the caller and kept out of the step.
+__device__ __forceinline__ void take_max(float x, float& top, bool& odd) {
+  const float m = fabsf(x);
+  if (m <= 3.402823466e38f) top = fmaxf(top, m); else odd = true;
+}
+
+// rint(x / step) in [-127, 127]; a NaN becomes 0.
+__device__ __forceinline__ int to_code(float x, float step) {
+  const float q = rintf(__fdiv_rn(x, step));
+  return (int)fminf(fmaxf(q, -127.f), 127.f) * (q == q ? 1 : 0);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kStoreThreads)
+kv_store_kernel(const KvArgs a, const StoreArgs g) {
+  constexpr int kLanes = D / 8;                      // lanes of a row
+  constexpr int kRows = kStoreThreads / kLanes;      // rows of one sweep
+  constexpr int kSweeps = kKvBlock / kRows;
+  const int l = threadIdx.x % kLanes, row = threadIdx.x / kLanes;
+  const bool turn = g.rope.positions != nullptr;
+
+  if (blockIdx.x >= g.kv_ctas) {
+    // ------------------------------------------------------------------ queries: 64 rows of (token, head)
+    const int64_t first = (int64_t)(blockIdx.x - g.kv_ctas) * kKvBlock;
+    const int64_t rows = a.T * a.n_heads;
+    Row<D> w{};
+    if (g.q_norm != nullptr) load_row(w, g.q_norm, l);
+    Row<D> x[kSweeps];
+#pragma unroll
+    for (int i = 0; i < kSweeps; ++i) {
+      const int64_t r = first + i * kRows + row;
+      if (r < rows) load_row(x[i], g.qkv + (r / a.n_heads) * g.ld + (r % a.n_heads) * D, l);
+      else x[i] = Row<D>{};
+    }
+#pragma unroll
+    for (int i = 0; i < kSweeps; ++i) {
+      const int64_t r = first + i * kRows + row;
+      if (g.q_norm != nullptr) norm_row(x[i], w, g.eps);
+      if (r >= rows) continue;
+      if (turn) rotate_row(x[i], g.rope, a.T, r / a.n_heads, l, a.hdr);
+      store_row<D>(g.q_out + r * D, x[i].lo, x[i].hi, l);
+    }
+    return;
+  }
+
+  // -------------------------------------------------------------------- one cache block of one head
+  __shared__ long long sums[kStoreThreads / 32];
+  __shared__ Found found;
+  __shared__ float tops[2][kStoreThreads / 32];
+  __shared__ __align__(16) int8_t turned[D][kKvBlock];
+  const int h = blockIdx.x % a.n_kv;
+  auto blocks_of = [&](int b) -> long long {
+    const Request r = load_request(a, b);
+    return r.q_len > 0 ? (r.kv - 1) / kKvBlock - max(r.kv - r.q_len, 0) / kKvBlock + 1 : 0;
+  };
+  if (!locate_item<kStoreThreads>(a.B, blockIdx.x / a.n_kv, blocks_of, sums, &found)) return;
+  const Request req = load_request(a, found.request);
+  const int begin = req.kv - req.q_len;              // place of the request's first new token
+  if (begin < 0 && threadIdx.x == 0) report_status(a.hdr, TLQ_ERR_SHAPE, 202);
+  if (req.kv < 1) return;
+  const int blk = max(begin, 0) / kKvBlock + (int)found.rest;
+  const int p0 = max(max(begin, 0), blk * kKvBlock); // places [p0, p1) of the new tokens in this block
+  const int p1 = min(req.kv, (blk + 1) * kKvBlock);
+  const int phys = a.block_table[(int64_t)found.request * a.max_blocks + blk];
+  if (phys < 0 || phys >= a.n_blocks) {
+    if (threadIdx.x == 0) report_status(a.hdr, TLQ_ERR_SHAPE, 203);
+    return;
+  }
+  const int off0 = p0 - blk * kKvBlock, n_new = p1 - p0;
+  const int64_t tok0 = (int64_t)req.q0 + (p0 - begin);
+
+  Row<D> w{};
+  if (g.k_norm != nullptr) load_row(w, g.k_norm, l);
+  Row<D> kx[kSweeps], vx[kSweeps];
+  float ktop = 0.f, vtop = 0.f;
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < kSweeps; ++i) {
+    const int n = i * kRows + row;
+    if (n < n_new) {
+      const uint16_t* p = g.qkv + (tok0 + n) * g.ld + (int64_t)(a.n_heads + h) * D;
+      load_row(kx[i], p, l);
+      load_row(vx[i], p + (int64_t)a.n_kv * D, l);
+    } else {
+      kx[i] = Row<D>{};
+      vx[i] = Row<D>{};
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kSweeps; ++i) {
+    const int n = i * kRows + row;
+    if (g.k_norm != nullptr) norm_row(kx[i], w, g.eps);
+    if (n < n_new) {
+      if (turn) rotate_row(kx[i], g.rope, a.T, tok0 + n, l, a.hdr);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        take_max(kx[i].lo[j], ktop, odd); take_max(kx[i].hi[j], ktop, odd);
+        take_max(vx[i].lo[j], vtop, odd); take_max(vx[i].hi[j], vtop, odd);
+      }
+    }
+  }
+  if (odd) report_status(a.hdr, TLQ_ERR_NONFINITE, 204);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    ktop = fmaxf(ktop, __shfl_xor_sync(0xFFFFFFFFu, ktop, o));
+    vtop = fmaxf(vtop, __shfl_xor_sync(0xFFFFFFFFu, vtop, o));
+  }
+  if ((threadIdx.x & 31) == 0) {
+    tops[0][threadIdx.x >> 5] = ktop;
+    tops[1][threadIdx.x >> 5] = vtop;
+  }
+  const int64_t at = (int64_t)phys * a.n_kv + h;
+  const float kold = off0 > 0 ? a.k_steps[at] : 0.f, vold = off0 > 0 ? a.v_steps[at] : 0.f;
+  __syncthreads();                                   // also: every thread has read the old steps
+#pragma unroll
+  for (int i = 0; i < kStoreThreads / 32; ++i) {
+    ktop = fmaxf(ktop, tops[0][i]);
+    vtop = fmaxf(vtop, tops[1][i]);
+  }
+  const float kstep = fmaxf(kold, __fdiv_rn(fmaxf(ktop, TLQ_RANGE_FLOOR), 127.f));
+  const float vstep = fmaxf(vold, __fdiv_rn(fmaxf(vtop, TLQ_RANGE_FLOOR), 127.f));
+  if (threadIdx.x == 0) {
+    a.k_steps[at] = kstep;
+    a.v_steps[at] = vstep;
+  }
+  int8_t* kc = a.k_codes + at * kKvBlock * D;
+  int8_t* vc = a.v_codes + at * kKvBlock * D;
+  // older codes follow a step that grew
+  if (kold > 0.f && kstep > kold) {
+    const float f = __fdiv_rn(kold, kstep);
+    for (int i = threadIdx.x; i < off0 * D / 4; i += kStoreThreads) {
+      char4 c = reinterpret_cast<char4*>(kc)[i];
+      c.x = (signed char)(int)rintf((float)c.x * f); c.y = (signed char)(int)rintf((float)c.y * f);
+      c.z = (signed char)(int)rintf((float)c.z * f); c.w = (signed char)(int)rintf((float)c.w * f);
+      reinterpret_cast<char4*>(kc)[i] = c;
+    }
+  }
+  if (vold > 0.f && vstep > vold) {
+    const float f = __fdiv_rn(vold, vstep);
+    for (int i = threadIdx.x; i < D * kKvBlock; i += kStoreThreads)
+      if (i % kKvBlock < off0) vc[i] = (int8_t)(int)rintf((float)vc[i] * f);
+  }
+#pragma unroll
+  for (int i = 0; i < kSweeps; ++i) {
+    const int n = i * kRows + row;
+    if (n >= n_new) break;
+    uint32_t lo = 0, hi = 0;
+    float klo[4], khi[4], vlo[4], vhi[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int a0 = to_code(kx[i].lo[j], kstep), a1 = to_code(kx[i].hi[j], kstep);
+      const int b0 = to_code(vx[i].lo[j], vstep), b1 = to_code(vx[i].hi[j], vstep);
+      lo |= (uint32_t)(a0 & 255) << (8 * j);
+      hi |= (uint32_t)(a1 & 255) << (8 * j);
+      turned[4 * l + j][n] = (int8_t)b0;
+      turned[D / 2 + 4 * l + j][n] = (int8_t)b1;
+      klo[j] = (float)a0 * kstep; khi[j] = (float)a1 * kstep;
+      vlo[j] = (float)b0 * vstep; vhi[j] = (float)b1 * vstep;
+    }
+    *reinterpret_cast<uint32_t*>(kc + (off0 + n) * D + 4 * l) = lo;
+    *reinterpret_cast<uint32_t*>(kc + (off0 + n) * D + D / 2 + 4 * l) = hi;
+    const int64_t to = ((tok0 + n) * a.n_kv + h) * D;
+    if (g.k_values != nullptr) store_row<D>(g.k_values + to, klo, khi, l);
+    if (g.v_values != nullptr) store_row<D>(g.v_values + to, vlo, vhi, l);
+  }
+  __syncthreads();
+  if (n_new == kKvBlock) {
+    for (int i = threadIdx.x; i < D * kKvBlock / 16; i += kStoreThreads)
+      reinterpret_cast<uint4*>(vc)[i] = reinterpret_cast<const uint4*>(&turned[0][0])[i];
+  } else {
+    for (int i = threadIdx.x; i < D * n_new; i += kStoreThreads) {
+      const int c = i / n_new, n = i % n_new;
+      vc[c * kKvBlock + off0 + n] = turned[c][n];
+    }
+  }
+}
+
+}  // namespace
+
+int launch_kv_store(const uint16_t* qkv, int64_t ld, int head_dim, const KvArgs& a, const RopeArgs& rope,
+                    const uint16_t* q_norm, const uint16_t* k_norm, float eps, uint16_t* q_out, uint16_t* k_values,
+                    uint16_t* v_values, cudaStream_t st) {
+  StoreArgs g{};
+  g.qkv = qkv; g.ld = ld; g.rope = rope; g.q_norm = q_norm; g.k_norm = k_norm; g.eps = eps;
+  g.q_out = q_out; g.k_values = k_values; g.v_values = v_values;
+  // n tokens of one request touch at most (n - 1) / 64 + 2 blocks and at most n
+  int64_t blocks = a.T / kKvBlock + 2 * (int64_t)a.B;
+  if (blocks > a.T) blocks = a.T;
+  const int64_t q_ctas = ceil_div(a.T * a.n_heads, kKvBlock);
+  if (blocks * a.n_kv + q_ctas > 0x7FFFFFFFLL) return TLQ_ERR_SHAPE;
+  g.kv_ctas = (unsigned)(blocks * a.n_kv);
+  const unsigned grid = g.kv_ctas + (unsigned)q_ctas;
+  if (head_dim == 128) kv_store_kernel<128><<<grid, kStoreThreads, 0, st>>>(a, g);
+  else kv_store_kernel<64><<<grid, kStoreThreads, 0, st>>>(a, g);
+  return after_launch();
+}
+
+}  // namespace tlq

@@ -1,0 +1,128 @@
+// Shared declarations of the serving operators: the 8-bit product, the key-value store and attention over the cache.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace tlq {
+
+constexpr int kKvBlock = TLQ_KV_BLOCK;   // tokens of one cache block
+
+// What the kernels need of a batch and of the cache (device pointers).
+struct KvArgs {
+  int8_t* k_codes;            // [n_blocks][Hkv][64][D]
+  int8_t* v_codes;            // [n_blocks][Hkv][D][64]
+  float* k_steps;             // [n_blocks][Hkv]
+  float* v_steps;
+  const int32_t* cu_q;        // [B + 1]
+  const int32_t* kv_len;      // [B]
+  const int32_t* block_table; // [B][max_blocks]
+  int64_t T;                  // rows of q / qkv
+  int n_blocks, max_blocks, B, max_q_len;
+  int n_heads, n_kv, group;   // group = n_heads / n_kv
+  WorkspaceHeader* hdr;
+};
+
+__device__ __forceinline__ void report_status(WorkspaceHeader* hdr, int status, int where) {
+  hdr->where = where;
+  hdr->status = status;
+}
+
+// Lengths of one request, forced into what the call's buffers hold (anything else is reported, and what does not fit
+// is left out), so that no metadata can move an access out of bounds.
+struct Request {
+  int q0, q_len, kv;          // first row of q, new tokens, cached tokens with the new ones
+};
+__device__ __forceinline__ Request load_request(const KvArgs& a, int b) {
+  const int c0 = a.cu_q[b], c1 = a.cu_q[b + 1], kv = a.kv_len[b];
+  Request r;
+  r.q0 = max(0, min(c0, (int)a.T));
+  const int end = max(r.q0, min(c1, (int)a.T));
+  r.q_len = min(end - r.q0, a.max_q_len);
+  const long long room = (long long)a.max_blocks * kKvBlock;
+  r.kv = kv < 0 ? 0 : ((long long)kv > room ? (int)room : kv);
+  if (r.q0 != c0 || r.q_len != c1 - c0 || r.kv != kv) report_status(a.hdr, TLQ_ERR_SHAPE, 200);
+  return r;
+}
+
+// Inclusive scan of one value per thread of a block of kThreads; `sums` is kThreads / 32 words of shared memory.
+template <int kThreads>
+__device__ __forceinline__ long long block_scan(long long v, long long* sums, long long& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long n = __shfl_up_sync(0xFFFFFFFFu, v, o);
+    if (lane >= o) v += n;
+  }
+  __syncthreads();               // earlier readers of `sums` are done
+  if (lane == 31) sums[warp] = v;
+  __syncthreads();
+  long long before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) {
+    const long long s = sums[w];
+    if (w < warp) before += s;
+    total += s;
+  }
+  return v + before;
+}
+
+// The request that holds item number `target` when request b owns count(b) items, and the item's number in it.
+// All threads of the block call it; `found` (shared) receives {request, number in it}.  False when there is none.
+struct Found {
+  long long rest;
+  int request;
+};
+template <int kThreads, typename F>
+__device__ __forceinline__ bool locate_item(int B, long long target, F count, long long* sums, Found* found) {
+  long long base = 0;
+  if (threadIdx.x == 0) found->request = -1;
+  for (int b0 = 0; b0 < B; b0 += kThreads) {
+    const int b = b0 + (int)threadIdx.x;
+    const long long n = b < B ? count(b) : 0;
+    long long total;
+    const long long upto = block_scan<kThreads>(n, sums, total);
+    if (n > 0 && target - base >= upto - n && target - base < upto) {
+      found->request = b;
+      found->rest = target - base - (upto - n);
+    }
+    base += total;
+    if (target < base) break;
+  }
+  __syncthreads();
+  return found->request >= 0;
+}
+
+// ---------------------------------------------------------------------------------------------- launchers
+// kv_store.cu
+struct RopeArgs {
+  const int32_t* positions;   // [axes][T] or null (no rotation)
+  const float* cos_sin;       // [n_positions][D]: cosines of the D/2 pairs, then sines
+  int64_t n_positions;
+  int n_axes;
+  int pairs_end[3];           // pairs [pairs_end[a-1], pairs_end[a]) turn by position axis a
+};
+int launch_kv_store(const uint16_t* qkv, int64_t ld, int head_dim, const KvArgs& a, const RopeArgs& rope,
+                    const uint16_t* q_norm, const uint16_t* k_norm, float eps, uint16_t* q_out, uint16_t* k_values,
+                    uint16_t* v_values, cudaStream_t st);
+
+// kv_attention.cu: workspace of the split over the cache (counters are zero between calls)
+constexpr int kMaxWorkers = 512;          // CTAs that share one call's work
+constexpr int kMaxRowTile = 16;           // query rows of one work item
+inline size_t kv_split_floats(int head_dim) {
+  return (size_t)kMaxWorkers * 2 * kMaxRowTile * ((size_t)head_dim + 2);
+}
+struct KvSplit {
+  int32_t* counters;          // [kMaxWorkers]
+  float* partials;            // kv_split_floats()
+};
+int launch_kv_attention(const uint16_t* q, int64_t ldq, int head_dim, const KvArgs& a, float scale, int causal,
+                        uint16_t* out, float* lse, const KvSplit& split, cudaStream_t st);
+
+// linear_i8.cu
+int launch_linear_i8(const int8_t* Xq, const float* t, const int8_t* Wq, const float* u, const uint16_t* bias, int64_t N,
+                     int64_t C1, int64_t C2, uint16_t* Y, WorkspaceHeader* hdr, cudaStream_t st);
+
+}  // namespace tlq

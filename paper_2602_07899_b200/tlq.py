@@ -32,7 +32,8 @@ EXPORTS = (
     "tlq_scale_candidates", "tlq_scale_candidates_noalloc", "tlq_quantize_weights", "tlq_pack_codes4", "tlq_quantize_activations", "tlq_scale_search_workspace_bytes", "tlq_scale_search_layer", "tlq_scale_search_layer_two_stream",
     "tlq_apply_layer_workspace_bytes", "tlq_apply_layer", "tlq_read_status", "tlq_stage_timing_enable",
     "tlq_stage_timing_drain", "tlq_kernel_launch_count", "tlq_selftest_bounded_wait", "tlq_debug_tile_walk", "tlq_debug_resident_walk", "tlq_l2_partition_info", "tlq_debug_canary_offsets",
-    "tlq_debug_check_canaries",
+    "tlq_debug_check_canaries", "tlq_linear_i8_workspace_bytes", "tlq_linear_i8", "tlq_kv_workspace_bytes", "tlq_kv_store",
+    "tlq_kv_attention",
 )
 
 
@@ -47,6 +48,20 @@ class Config(ctypes.Structure):
                 ("a_bits", ctypes.c_int32), ("group_size", ctypes.c_int32), ("n_grid", ctypes.c_int32),
                 ("stat_mode", ctypes.c_int32), ("flags", ctypes.c_uint32)]
 
+
+class _KvCacheStruct(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("n_blocks", ctypes.c_int32), ("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("k_steps", ctypes.c_void_p), ("v_steps", ctypes.c_void_p)]
+
+
+class _KvBatchStruct(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("n_requests", ctypes.c_int32), ("max_q_len", ctypes.c_int32),
+                ("max_blocks", ctypes.c_int32), ("cu_q", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("block_table", ctypes.c_void_p)]
+
+
+KV_BLOCK = 64                 # tokens of one cache block
 
 FLAG_SKIP_ZERO_WEIGHT_TOKENS = 1
 FLAG_GEMM_CTA_PAIRS = 2
@@ -109,6 +124,18 @@ def _load() -> ctypes.CDLL:
     lib.tlq_debug_resident_walk.restype = i32
     lib.tlq_stage_timing_enable.argtypes = [i32]
     lib.tlq_stage_timing_drain.argtypes = [ctypes.POINTER(ctypes.c_float), i32]
+    kvp, kbp = ctypes.POINTER(_KvCacheStruct), ctypes.POINTER(_KvBatchStruct)
+    lib.tlq_linear_i8_workspace_bytes.restype = sz
+    lib.tlq_linear_i8_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.tlq_linear_i8.restype = i32
+    lib.tlq_linear_i8.argtypes = [vp, vp, i64, i64, vp, vp, i64, vp, vp, sz, vp, vp]
+    lib.tlq_kv_workspace_bytes.restype = sz
+    lib.tlq_kv_workspace_bytes.argtypes = [kvp, kbp, i32, i64]
+    lib.tlq_kv_store.restype = i32
+    lib.tlq_kv_store.argtypes = [vp, i64, i64, i32, kvp, kbp, vp, i32, ctypes.POINTER(ctypes.c_int32), vp, i64, vp, vp,
+                                 ctypes.c_float, vp, vp, vp, vp, sz, vp]
+    lib.tlq_kv_attention.restype = i32
+    lib.tlq_kv_attention.argtypes = [vp, i64, i64, i32, kvp, kbp, ctypes.c_float, i32, vp, sz, vp, vp, vp]
     for fn in ("tlq_token_importance", "tlq_scale_candidates", "tlq_scale_candidates_noalloc", "tlq_quantize_weights", "tlq_pack_codes4", "tlq_quantize_activations", "tlq_scale_search_layer",
                "tlq_apply_layer", "tlq_read_status", "tlq_stage_timing_enable", "tlq_stage_timing_drain"):
         getattr(lib, fn).restype = i32
@@ -292,6 +319,167 @@ def tlq_apply_layer(X: torch.Tensor, W: torch.Tensor, s: Optional[torch.Tensor],
     if check:
         _check(lib.tlq_read_status(_ptr(ws), st), "tlq_apply_layer (device)")
     return dict(Yq=Yq, codes=codes, steps=steps, zeros=zeros)
+
+
+# ----------------------------------------------------------------------------------------------- serving
+# What runs a calibrated layer: see the serving part of include/tlq.h.  These calls never synchronise; read the status
+# word of their workspace with tlq_read_status when a step's results are fetched.
+
+
+def _typed(t: torch.Tensor, dtype: torch.dtype, shape, what: str) -> torch.Tensor:
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return t
+
+
+def _rows(t: torch.Tensor, what: str) -> int:
+    """Row pitch in elements of a bf16 tensor whose rows are contiguous."""
+    if t.dtype != torch.bfloat16:
+        raise ValueError(f"{what} must be torch.bfloat16, got {t.dtype}")
+    inner = t.shape[-1]
+    if t.stride(-1) != 1 or (t.dim() == 3 and t.shape[1] > 1 and t.stride(1) != inner):
+        raise ValueError(f"{what}: the heads and channels of a token must be contiguous")
+    width = t.shape[1:].numel()
+    return t.stride(0) if t.shape[0] > 1 else width
+
+
+class KvCache:
+    """The 8-bit cache of one layer: k_codes int8 [blocks, kv heads, 64, head_dim] (token by channel), v_codes int8
+    [blocks, kv heads, head_dim, 64] (channel by token), k_steps and v_steps float32 [blocks, kv heads]."""
+
+    def __init__(self, k_codes: torch.Tensor, v_codes: torch.Tensor, k_steps: torch.Tensor, v_steps: torch.Tensor):
+        blocks, heads, _, dim = k_codes.shape
+        _typed(k_codes, torch.int8, (blocks, heads, KV_BLOCK, dim), "k_codes")
+        _typed(v_codes, torch.int8, (blocks, heads, dim, KV_BLOCK), "v_codes")
+        _typed(k_steps, torch.float32, (blocks, heads), "k_steps")
+        _typed(v_steps, torch.float32, (blocks, heads), "v_steps")
+        self.k_codes, self.v_codes, self.k_steps, self.v_steps = k_codes, v_codes, k_steps, v_steps
+        self.n_blocks, self.n_kv_heads, self.head_dim, self.device = blocks, heads, dim, k_codes.device
+        self._c = _KvCacheStruct(ctypes.sizeof(_KvCacheStruct), heads, dim, blocks, k_codes.data_ptr(), v_codes.data_ptr(),
+                                 k_steps.data_ptr(), v_steps.data_ptr())
+
+    @classmethod
+    def empty(cls, n_blocks: int, n_kv_heads: int, head_dim: int, device) -> "KvCache":
+        return cls(torch.zeros((n_blocks, n_kv_heads, KV_BLOCK, head_dim), dtype=torch.int8, device=device),
+                   torch.zeros((n_blocks, n_kv_heads, head_dim, KV_BLOCK), dtype=torch.int8, device=device),
+                   torch.zeros((n_blocks, n_kv_heads), dtype=torch.float32, device=device),
+                   torch.zeros((n_blocks, n_kv_heads), dtype=torch.float32, device=device))
+
+
+class KvBatch:
+    """The requests of one step, on the device: cu_q int32 [n + 1], kv_len int32 [n] (with the step's tokens),
+    block_table int32 [n, max_blocks]; max_q_len bounds the new tokens of a request (host)."""
+
+    def __init__(self, cu_q: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, max_q_len: int):
+        n = kv_len.shape[0]
+        _typed(cu_q, torch.int32, (n + 1,), "cu_q")
+        _typed(kv_len, torch.int32, (n,), "kv_len")
+        _typed(block_table, torch.int32, (n, block_table.shape[-1]), "block_table")
+        self.cu_q, self.kv_len, self.block_table, self.max_q_len = cu_q, kv_len, block_table, int(max_q_len)
+        self._c = _KvBatchStruct(ctypes.sizeof(_KvBatchStruct), n, self.max_q_len, block_table.shape[1], cu_q.data_ptr(),
+                                 kv_len.data_ptr(), block_table.data_ptr())
+
+
+def linear_workspace(N: int, C1: int, C2: int, device) -> torch.Tensor:
+    """A zeroed workspace for tlq_linear_i8 of up to N tokens (kept by the caller, one per stream)."""
+    n = int(lib.tlq_linear_i8_workspace_bytes(N, C1, C2))
+    if n == 0:
+        raise TlqError(ERR_SHAPE, "tlq_linear_i8_workspace_bytes")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def kv_workspace(cache: KvCache, n_heads: int, T: int, batch: KvBatch) -> torch.Tensor:
+    """A zeroed workspace for tlq_kv_store and tlq_kv_attention of up to T tokens (kept by the caller, one per stream)."""
+    n = int(lib.tlq_kv_workspace_bytes(cache._c, batch._c, n_heads, T))
+    if n == 0:
+        raise TlqError(ERR_SHAPE, "tlq_kv_workspace_bytes")
+    return torch.zeros(n, dtype=torch.uint8, device=cache.device)
+
+
+def tlq_linear_i8(Xq: torch.Tensor, t: torch.Tensor, Wq: torch.Tensor, u: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Xq int8 [N,C1] with steps t [N], Wq int8 [C2,C1] with steps u [C2], bias bf16 [C2] or None -> bf16 [N,C2]."""
+    N, C1 = Xq.shape
+    C2 = Wq.shape[0]
+    _typed(Xq, torch.int8, (N, C1), "Xq")
+    _typed(Wq, torch.int8, (C2, C1), "Wq")
+    _typed(t, torch.float32, (N,), "t")
+    _typed(u, torch.float32, (C2,), "u")
+    if bias is not None:
+        _typed(bias, torch.bfloat16, (C2,), "bias")
+    if workspace is None:
+        workspace = linear_workspace(N, C1, C2, Xq.device)
+    if out is None:
+        out = torch.empty((N, C2), dtype=torch.bfloat16, device=Xq.device)
+    else:
+        _typed(out, torch.bfloat16, (N, C2), "out")
+    _check(lib.tlq_linear_i8(Xq.data_ptr(), t.data_ptr(), N, C1, Wq.data_ptr(), u.data_ptr(), C2,
+                             None if bias is None else bias.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                             out.data_ptr(), _stream(stream)), "tlq_linear_i8")
+    return out
+
+
+def tlq_kv_store(qkv: torch.Tensor, n_heads: int, cache: KvCache, batch: KvBatch, positions: Optional[torch.Tensor] = None,
+                 cos_sin: Optional[torch.Tensor] = None, sections=None, q_norm: Optional[torch.Tensor] = None,
+                 k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6, want_values: bool = False,
+                 workspace: Optional[torch.Tensor] = None, stream=None):
+    """qkv bf16 [T, >= (n_heads + 2 kv heads) * head_dim] (rows may be strided) -> (q bf16 [T, n_heads, head_dim], k values,
+    v values): normed (q_norm, k_norm bf16 [head_dim]) and rotated (positions int32 [T], [1,T] or [3,T]; cos_sin float32
+    [positions, head_dim]; sections: pairs of each axis) queries; keys and values go into the cache, and come back as the
+    values their codes stand for (bf16 [T, kv heads, head_dim]) with want_values."""
+    T, d = qkv.shape[0], cache.head_dim
+    ld = _rows(qkv, "qkv")
+    if qkv.dim() != 2 or qkv.shape[1] < (n_heads + 2 * cache.n_kv_heads) * d:
+        raise ValueError("qkv must be [T, (n_heads + 2 * n_kv_heads) * head_dim]")
+    axes, sec, limit = 1, None, 0
+    if positions is not None:
+        axes = 1 if positions.dim() == 1 else positions.shape[0]
+        _typed(positions, torch.int32, (T,) if positions.dim() == 1 else (axes, T), "positions")
+        if cos_sin is None:
+            raise ValueError("positions need cos_sin")
+        limit = cos_sin.shape[0]
+        _typed(cos_sin, torch.float32, (limit, d), "cos_sin")
+        if sections is not None:
+            if len(sections) != axes:
+                raise ValueError("one section for each position axis")
+            sec = (ctypes.c_int32 * axes)(*sections)
+    for w, what in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+        if w is not None:
+            _typed(w, torch.bfloat16, (d,), what)
+    if workspace is None:
+        workspace = kv_workspace(cache, n_heads, T, batch)
+    q = torch.empty((T, n_heads, d), dtype=torch.bfloat16, device=qkv.device)
+    k = v = None
+    if want_values:
+        k = torch.empty((T, cache.n_kv_heads, d), dtype=torch.bfloat16, device=qkv.device)
+        v = torch.empty_like(k)
+    _check(lib.tlq_kv_store(qkv.data_ptr(), T, ld, n_heads, cache._c, batch._c,
+                            None if positions is None else positions.data_ptr(), axes, sec,
+                            None if cos_sin is None else cos_sin.data_ptr(), limit,
+                            None if q_norm is None else q_norm.data_ptr(), None if k_norm is None else k_norm.data_ptr(),
+                            eps, q.data_ptr(), None if k is None else k.data_ptr(), None if v is None else v.data_ptr(),
+                            workspace.data_ptr(), workspace.numel(), _stream(stream)), "tlq_kv_store")
+    return q, k, v
+
+
+def tlq_kv_attention(q: torch.Tensor, cache: KvCache, batch: KvBatch, scale: float, causal: bool = True,
+                     want_lse: bool = False, workspace: Optional[torch.Tensor] = None, stream=None):
+    """q bf16 [T, n_heads, head_dim] (rows may be strided) -> (out bf16 [T, n_heads, head_dim], lse float32 [T, n_heads] or
+    None): attention of a step's rows over the cached tokens of their requests."""
+    T, n_heads, d = q.shape
+    if d != cache.head_dim:
+        raise ValueError("q and the cache differ in head_dim")
+    ldq = _rows(q, "q")
+    if workspace is None:
+        workspace = kv_workspace(cache, n_heads, T, batch)
+    out = torch.empty((T, n_heads, d), dtype=torch.bfloat16, device=q.device)
+    lse = torch.empty((T, n_heads), dtype=torch.float32, device=q.device) if want_lse else None
+    _check(lib.tlq_kv_attention(q.data_ptr(), T, ldq, n_heads, cache._c, batch._c, scale, 1 if causal else 0,
+                                workspace.data_ptr(), workspace.numel(), out.data_ptr(),
+                                None if lse is None else lse.data_ptr(), _stream(stream)), "tlq_kv_attention")
+    return out, lse
 
 
 def tlq_read_status(workspace: torch.Tensor, stream=None) -> int:
