@@ -5,28 +5,33 @@
 // The steps never touch an element of the cache: with a = scale * log2(e) * kstep and b = log2(vstep) the kernel works on
 // t_j = a (q . kc_j) + b and p_j = 2^(t_j - m), so that o = sum p_j vc_j / sum p_j / vstep, where the running maximum m
 // is taken over t.  8-bit codes are exact in 16-bit floats, so both products run on the matrix instruction m16n8k16 in
-// f16 with 32-bit sums.  q enters as f16 after a power of two per row that brings its largest element to [1, 2) (exact
+// f16 with 32-bit sums.  For the scores it is cheaper to multiply by kc + 128 (three byte operations make four operands):
+// the 128 sum(q) that this adds is a constant of a column and becomes part of b.
+// q enters as f16 after a power of two per row that brings its largest element to [1, 2) (exact
 // for all but elements 2^-14 below it); p enters as f16 scaled by 2^15, which keeps 11 bits for every p_j >= 2^-29 of the
 // largest.  Maximum, sums and the output sum are 32-bit.
 //
 // Layout.  All query heads of a kv head (and the tokens of a short draft) are the 8 or 16 columns of the products
 // S^T = K q^T (m = 16 tokens) and O^T = V^T P^T (m = 16 channels): with the cache on the m side no lane is idle when there
 // are only 8 rows.  Which token or channel a matrix index means is free as long as both operands agree, so every lane
-// reads its operands from global memory as whole 16-byte pieces, straight into registers: no shared memory, no barrier.
-// The probabilities change from result layout to operand layout by movmatrix.
+// reads its operands as whole 16-byte pieces of a row.  The probabilities change from result layout to operand layout by
+// movmatrix.
 //
 // Split.  A unit is one block of 64 tokens of one (request, kv head, row tile).  All units form one line that is cut into
-// equal parts, one per CTA, whatever the requests' lengths; a CTA's eight warps take its blocks in turn, each with its own
-// running softmax, joined through shared memory at the end of an item.  An item that several CTAs share is joined by the
-// one that finishes last (partials in the workspace; its counter goes back to zero), in a fixed order.
+// equal parts, one per warp, whatever the requests' lengths.  A warp walks its part alone, with a ring of asynchronous
+// copies of its own that runs ahead over item boundaries; it writes the items that lie inside its part, and leaves
+// partial sums of at most two that do not.  Then the warps of a CTA join what they share, and of the items that several
+// CTAs share the one that finishes last joins the rest (its counter goes back to zero), all in a fixed order.
 //
-// Bound: the cache's bytes.  16 KB per block and kv head at 128 channels.
+// Bound: the cache's bytes, 16 KB per block and kv head at 128 channels.  The ring holds 24 KB per warp, 192 KB per SM:
+// at 44 GB/s and about 2 us per SM some 90 KB have to be under way all the time.
 #include "serve.cuh"
+#include "umma.cuh"
 
 namespace tlq {
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kWarps = kSplitWarps;
 constexpr int kThreads = kWarps * 32;
 constexpr float kShift = 15.f;            // p is kept as 2^kShift * p in 16 bits
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -41,15 +46,27 @@ struct AttnArgs {
   KvSplit split;
 };
 
-__device__ __forceinline__ uint4 ld_cache(const int8_t* p) {
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
   uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
   return v;
 }
+// Copy of `bytes` (a multiple of 16) that counts on the barrier.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 
-// Four 8-bit codes to two pairs of f16: 1024 + (code + 128) by byte placement, minus 1152.
-__device__ __forceinline__ void codes_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+// Four 8-bit codes to two pairs of f16.  Keys: code + 128 in the lowest byte of a 16-bit float is the (subnormal, exact)
+// number (code + 128) 2^-24.  Values: exactly the code, as 1024 + (code + 128) by byte placement, minus 1152; a sum of
+// p (code + 128) less 128 sum(p) would leave a rounding of 2^-23 x 128 in channels whose own values are small.
+constexpr float kUnit = 16777216.f;       // 2^24
+__device__ __forceinline__ void keys_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  const uint32_t x = w ^ 0x80808080u;
+  lo = __byte_perm(x, 0u, 0x4140);
+  hi = __byte_perm(x, 0u, 0x4342);
+}
+__device__ __forceinline__ void values_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
   const uint32_t x = w ^ 0x80808080u;
   const uint32_t a = __byte_perm(x, 0x64646464u, 0x4140), b = __byte_perm(x, 0x64646464u, 0x4342);
   const __half2 off = __floats2half2_rn(1152.f, 1152.f);
@@ -82,48 +99,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // Steps below this have a smaller logarithm than the running maximum can carry; values that small count as zero.
 constexpr float kStepFloor = 7.8886090522101181e-31f;      // 2^-100
 
-template <int D, int NT>
-struct Block {                 // one block of one kv head, in this lane's registers
-  uint4 k[4][D / 64][2];       // [16 tokens][64 channels][row g or g + 8]
-  uint4 v[D / 16][2];          // [16 channels][row g or g + 8]
-  float kstep, vstep;
-  int base;                    // place of its first token, or a place beyond every mask
-};
-
-template <int D, int NT>
-__device__ __forceinline__ void load_k(Block<D, NT>& s, const KvArgs& a, int phys, int h, int blk, int g, int t) {
-  const bool bad = phys < 0 || phys >= a.n_blocks;
-  if (bad) {
-    report_status(a.hdr, TLQ_ERR_SHAPE, 210);
-    phys = 0;
-  }
-  const int64_t at = (int64_t)phys * a.n_kv + h;
-  s.base = bad ? 0x7FFFFFFF - kKvBlock : blk * kKvBlock;
-  s.kstep = __ldg(a.k_steps + at);
-  s.vstep = __ldg(a.v_steps + at);
-  const int8_t* p = a.k_codes + at * (kKvBlock * D) + (16 * (g >> 1) + (g & 1)) * D + 16 * t;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c) {
-      s.k[i][c][0] = ld_cache(p + 4 * i * D + 64 * c);
-      s.k[i][c][1] = ld_cache(p + (4 * i + 2) * D + 64 * c);
-    }
-}
-template <int D, int NT>
-__device__ __forceinline__ void load_v(Block<D, NT>& s, const KvArgs& a, int phys, int h, int g, int t) {
-  if (phys < 0 || phys >= a.n_blocks) phys = 0;
-  const int8_t* p = a.v_codes + ((int64_t)phys * a.n_kv + h) * (kKvBlock * D) + g * kKvBlock + 16 * t;
-#pragma unroll
-  for (int i = 0; i < D / 16; ++i) {
-    s.v[i][0] = ld_cache(p + 16 * i * kKvBlock);
-    s.v[i][1] = ld_cache(p + (16 * i + 8) * kKvBlock);
-  }
-}
-
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// Units of a request: row tiles x kv heads x blocks (one for a request without cached tokens, whose rows are empty).
+// Units of a request: row tiles x kv heads x (blocks + kItemUnits); blocks is one for a request without cached tokens, whose
+// rows are empty.  What an item costs beside its blocks (its queries, its result) takes as long as kItemUnits blocks.
+constexpr int kItemUnits = 1;
 struct Units {
   int row_tiles, blocks;
   long long total;
@@ -132,31 +112,211 @@ __device__ __forceinline__ Units units_of(const KvArgs& a, const Request& r, int
   Units u;
   u.row_tiles = (int)(((long long)r.q_len * a.group + row_tile - 1) / row_tile);
   u.blocks = r.kv > 0 ? (r.kv + kKvBlock - 1) / kKvBlock : 1;
-  u.total = (long long)u.row_tiles * a.n_kv * u.blocks;
+  u.total = (long long)u.row_tiles * a.n_kv * (u.blocks + kItemUnits);
   return u;
 }
+
+
+// A place on the line of units: block `blk` of an item (request b, kv head h, row tile), or one of the units before it (blk < 0).
+struct Walker {
+  int b, h, tile, blk;
+  Request req;
+  Units un;
+
+  __device__ __forceinline__ void enter(const KvArgs& a, int request, int row_tile) {
+    b = request;
+    req = load_request(a, b);
+    un = units_of(a, req, row_tile);
+  }
+  // `rest` units into request `request`
+  __device__ __forceinline__ void start(const KvArgs& a, int request, long long rest, int row_tile) {
+    enter(a, request, row_tile);
+    const long long item = rest / (un.blocks + kItemUnits);
+    blk = (int)(rest - item * (un.blocks + kItemUnits)) - kItemUnits;
+    h = (int)(item / un.row_tiles);
+    tile = (int)(item - (long long)h * un.row_tiles);
+  }
+  // to the first unit of the next item
+  __device__ __forceinline__ void next_item(const KvArgs& a, int row_tile) {
+    blk = -kItemUnits;
+    if (++tile < un.row_tiles) return;
+    tile = 0;
+    if (++h < a.n_kv) return;
+    h = 0;
+    do {
+      if (b + 1 >= a.B) return;                            // past the end: nobody looks further
+      enter(a, b + 1, row_tile);
+    } while (un.total == 0);
+  }
+};
+
+// An item of which a worker has only a part.
+struct Shared {
+  long long begin, end;        // units of its blocks; begin = end: nothing here
+  int b, h, tile;
+};
+
+// Row of the output that column c of an item belongs to.
+__device__ __forceinline__ int64_t out_row(const KvArgs& a, const Request& r, int h, int row) {
+  return (int64_t)(r.q0 + row / a.group) * a.n_heads + h * a.group + row % a.group;
+}
+
+// Writes four channels of one column of a joined item: to the output, or with `to` into another partial.
+template <int D, int NT>
+__device__ __forceinline__ void leave(const KvArgs& a, const AttnArgs& g, const Shared& it, const Request& req, float* to, int e,
+                                      float mm, float den, const float4& sum) {
+  constexpr int kRows = 8 * NT;
+  const int c = e / (D / 4), d = (e % (D / 4)) * 4;
+  if (to != nullptr) {
+    reinterpret_cast<float4*>(to + 2 * kRows)[e] = sum;
+    if (d == 0) {
+      to[c] = mm;
+      to[kRows + c] = den;
+    }
+    return;
+  }
+  const int64_t at = out_row(a, req, it.h, it.tile * kRows + c);
+  const bool none = mm == -INFINITY && den == 0.f;         // a row that sees nothing (a NaN row has den = NaN)
+  const float inv = none ? 0.f : 1.0f / den;
+  const __nv_bfloat162 y0 = __floats2bfloat162_rn(none ? 0.f : sum.x * inv, none ? 0.f : sum.y * inv);
+  const __nv_bfloat162 y1 = __floats2bfloat162_rn(none ? 0.f : sum.z * inv, none ? 0.f : sum.w * inv);
+  *reinterpret_cast<uint2*>(g.out + at * D + d) =
+      make_uint2(*reinterpret_cast<const uint32_t*>(&y0), *reinterpret_cast<const uint32_t*>(&y1));
+  if (d == 0 && g.lse != nullptr) g.lse[at] = none ? -INFINITY : kLn2 * (log2f(den) + mm - kShift);
+}
+
+__device__ __forceinline__ void add_scaled(float4& sum, const float4& v, float f) {
+  sum.x = fmaf(v.x, f, sum.x); sum.y = fmaf(v.y, f, sum.y); sum.z = fmaf(v.z, f, sum.z); sum.w = fmaf(v.w, f, sum.w);
+}
+
+// Joins the partials of up to kWarps warps of this CTA (kRows maxima, kRows sums, kRows x D output sums each; first_part,
+// then `pitch` floats apart from second_part on).  `lanes` threads share the work; all loads of a column are under way at once.
+template <int D, int NT>
+__device__ __forceinline__ void join_warps(const KvArgs& a, const AttnArgs& g, const Shared& it, int count, const float* first_part,
+                                           const float* second_part, size_t pitch, float* to, int lane, int lanes) {
+  constexpr int kRows = 8 * NT;
+  const Request req = load_request(a, it.b);
+  const int n_rows = min(kRows, req.q_len * a.group - it.tile * kRows);
+  for (int e = lane; e < n_rows * (D / 4); e += lanes) {
+    const int c = e / (D / 4);
+    float m[kWarps], l[kWarps];
+    float4 v[kWarps];
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      const float* p = i == 0 ? first_part : second_part + (i - 1) * pitch;
+      const bool in = i < count;
+      m[i] = in ? __ldcg(p + c) : -INFINITY;
+      l[i] = in ? __ldcg(p + kRows + c) : 0.f;
+      v[i] = in ? __ldcg(reinterpret_cast<const float4*>(p + 2 * kRows) + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    float mm = -INFINITY, den = 0.f;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) mm = fmaxf(mm, m[i]);
+    const float mu = mm == -INFINITY ? 0.f : mm;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      const float f = exp2_fast(m[i] - mu);
+      add_scaled(sum, v[i], f);
+      den = fmaf(l[i], f, den);
+    }
+    leave<D, NT>(a, g, it, req, to, e, mm, den, sum);
+  }
+}
+
+// Joins the partials of `count` CTAs (first_part, then `pitch` floats apart from second_part on) into the output.  All
+// threads of the CTA; `weights` holds kMaxWorkers x kRows floats of shared memory.
+template <int D, int NT>
+__device__ __forceinline__ void join_ctas(const KvArgs& a, const AttnArgs& g, const Shared& it, int count, const float* first_part,
+                                          const float* second_part, size_t pitch, float* weights) {
+  constexpr int kRows = 8 * NT;
+  const Request req = load_request(a, it.b);
+  const int n_rows = min(kRows, req.q_len * a.group - it.tile * kRows);
+  auto part = [&](int i) { return i == 0 ? first_part : second_part + (size_t)(i - 1) * pitch; };
+  constexpr int kBatch = 20;                               // parts whose loads are under way at once
+  __shared__ float s_max[kRows], s_den[kRows];
+  const int lane = threadIdx.x & 31;
+  for (int c = threadIdx.x >> 5; c < kRows; c += kWarps) {
+    float m[kMaxWorkers / 32], l[kMaxWorkers / 32], mm = -INFINITY, den = 0.f;
+#pragma unroll
+    for (int i = 0; i < kMaxWorkers / 32; ++i) {
+      const int k = i * 32 + lane;
+      m[i] = k < count ? __ldcg(part(k) + c) : -INFINITY;
+      l[i] = k < count ? __ldcg(part(k) + kRows + c) : 0.f;
+      mm = fmaxf(mm, m[i]);
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xFFFFFFFFu, mm, d));
+    const float mu = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+    for (int i = 0; i < kMaxWorkers / 32; ++i) {
+      const int k = i * 32 + lane;
+      const float f = exp2_fast(m[i] - mu);
+      if (k < count) weights[k * kRows + c] = f;
+      den = fmaf(l[i], f, den);
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) den += __shfl_xor_sync(0xFFFFFFFFu, den, d);
+    if (lane == 0) {
+      s_max[c] = mm;
+      s_den[c] = den;
+    }
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < n_rows * (D / 4); e += kThreads) {
+    const int c = e / (D / 4);
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = 0; i0 < count; i0 += kBatch) {
+      float4 v[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        v[i] = i0 + i < count ? __ldcg(reinterpret_cast<const float4*>(part(i0 + i) + 2 * kRows) + e)
+                              : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) add_scaled(sum, v[i], i0 + i < count ? weights[(i0 + i) * kRows + c] : 0.f);
+    }
+    leave<D, NT>(a, g, it, req, nullptr, e, s_max[c], s_den[c], sum);
+  }
+  __syncthreads();                                         // the next item's join may overwrite the weights
+}
+
+template <int D>
+constexpr int kAhead = D == 128 ? 2 : 3;                   // blocks that the ring runs ahead
+template <int D>
+constexpr int kChunks = 2 * kAhead<D> - 1;                 // a chunk is the keys, or the values, of one block
+template <int D>
+constexpr size_t kRingBytes = (size_t)kWarps * kChunks<D> * kKvBlock * D;
 
 template <int D, int NT>
 __global__ void __launch_bounds__(kThreads, 1)
 kv_attention_kernel(const KvArgs a, const AttnArgs g) {
   constexpr int kRows = 8 * NT;
-  extern __shared__ float smem[];
-  float* s_o = smem;                               // [kWarps][kRows][D + 1]
-  float* s_m = s_o + kWarps * kRows * (D + 1);     // [kWarps][kRows]
-  float* s_l = s_m + kWarps * kRows;
+  constexpr int kRing = kChunks<D>, kDeep = kAhead<D>;
+  constexpr uint32_t kBytes = kKvBlock * D;
+  constexpr size_t kPitch = (size_t)kRows * (D + 2);       // floats of a partial
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ __align__(8) uint64_t s_bars[kWarps * kRing];
   __shared__ long long sums[kWarps];
   __shared__ Found found;
-  __shared__ int s_last;
+  __shared__ Shared s_first[kWarps], s_last[kWarps], s_cta[2];
+  __shared__ int s_join[2], s_abort, s_has[kWarps];         // s_has: 1 a first part, 2 a last part, 4 the first part does not end here
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int gr = lane >> 2, tq = lane & 3;
 
   // ---------------------------------------------------------------- this CTA's part of the line of units
+  if (threadIdx.x == 0) s_abort = 0;
+  if (lane == 0) {
+    for (int i = 0; i < kRing; ++i) ptx::mbar_init(ptx::smem_u32(&s_bars[warp * kRing + i]), 1);
+    ptx::fence_barrier_init();
+  }
+  if (threadIdx.x < 2) s_cta[threadIdx.x].begin = s_cta[threadIdx.x].end = 0;
+  if (lane == 0) s_has[warp] = 0;
+  auto count_units = [&](int b) { return units_of(a, load_request(a, b), kRows).total; };
   long long total = 0;
   for (int b0 = 0; b0 < a.B; b0 += kThreads) {
     const int b = b0 + (int)threadIdx.x;
-    const long long n = b < a.B ? units_of(a, load_request(a, b), kRows).total : 0;
     long long part;
-    block_scan<kThreads>(n, sums, part);
+    block_scan<kThreads>(b < a.B ? count_units(b) : 0, sums, part);
     total += part;
   }
   if (total == 0) return;
@@ -166,103 +326,183 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
   if ((long long)blockIdx.x >= workers) return;
   const long long u_begin = total * blockIdx.x / workers, u_end = total * (blockIdx.x + 1) / workers;
   auto worker_of = [&](long long unit) { return ((unit + 1) * workers - 1) / total; };
-  if (!locate_item<kThreads>(a.B, u_begin, [&](int b) { return units_of(a, load_request(a, b), kRows).total; }, sums,
-                             &found))
-    return;
-  int b = found.request;
-  Request req = load_request(a, b);
-  Units un = units_of(a, req, kRows);
-  long long unit = u_begin;
-  long long rest = found.rest;                     // units of request b before `unit`
+  if (!locate_item<kThreads>(a.B, u_begin, count_units, sums, &found)) return;
 
-  while (unit < u_end) {
-    if (rest >= un.total) {                        // next request with any work
-      rest -= un.total;
-      do {
-        if (++b >= a.B) return;
-        req = load_request(a, b);
-        un = units_of(a, req, kRows);
-      } while (un.total == 0);
-      continue;
+  // ---------------------------------------------------------------- this warp's part of it
+  // (with fewer units than warps the first ones get one each: warps with nothing to do are the last ones)
+  const long long n_units = u_end - u_begin;
+  auto bound_of = [&](int w) { return u_begin + (n_units < kWarps ? min((long long)w, n_units) : n_units * w / kWarps); };
+  const long long w_begin = bound_of(warp), w_end = bound_of(warp + 1);
+  const uint32_t ring = ptx::smem_u32(smem) + warp * (kRing * kBytes);
+  const uint32_t bars = ptx::smem_u32(&s_bars[warp * kRing]);
+  float* const partials = g.split.partials;
+  auto warp_slot = [&](int w, int i) { return partials + (((size_t)blockIdx.x * kWarps + w) * 2 + i) * kPitch; };
+  auto cta_slot = [&](long long c, int i) { return partials + ((size_t)kMaxWorkers * kWarps * 2 + (size_t)c * 2 + i) * kPitch; };
+
+  if (w_begin < w_end) {
+    Walker con;                                            // what is computed now
+    {
+      int b = found.request;
+      long long rest = found.rest + (w_begin - u_begin);
+      con.enter(a, b, kRows);
+      while (rest >= con.un.total) {                       // the part may begin some requests after the CTA's
+        rest -= con.un.total;
+        con.enter(a, ++b, kRows);
+      }
+      con.start(a, b, rest, kRows);
     }
-    const int item = (int)(rest / un.blocks), blk0 = (int)(rest % un.blocks);
-    const int h = item / un.row_tiles, tile = item % un.row_tiles;
-    const long long item_begin = unit - blk0, item_end = item_begin + un.blocks;
-    const int blk1 = item_end <= u_end ? un.blocks : blk0 + (int)(u_end - unit);
-    const int n_rows = min(kRows, req.q_len * a.group - tile * kRows);
-    const int past = req.kv - req.q_len;
+    Walker pro = con;                                      // what is copied next
+    long long pro_left = w_end - w_begin;
+    // steps and first places of the blocks under way
+    float q_k[kDeep], q_v[kDeep];
+    int q_base[kDeep];
+    int phys = 0;                                          // of the block at `pro`
+    const int8_t* v_src = nullptr;                         // values of the block whose keys were copied last
+    // leaves the units before an item's blocks (and items of requests without cached tokens) and looks the block up
+    auto look_up = [&]() {
+      while (pro_left > 0) {
+        if (pro.blk < 0) {
+          pro_left += pro.blk;
+          pro.blk = 0;
+        } else if (pro.req.kv > 0) {
+          phys = __ldg(a.block_table + (int64_t)pro.b * a.max_blocks + pro.blk);
+          return;
+        } else {
+          --pro_left;
+          pro.next_item(a, kRows);
+        }
+      }
+    };
+    int put = 0;                                           // chunk that is copied next
+    auto copy = [&](const int8_t* src) {
+      __syncwarp();                                        // every lane has read what the chunk held
+      if (lane == 0) {
+        ptx::mbar_expect_tx(bars + 8 * put, kBytes);
+        bulk_load(ring + put * kBytes, src, kBytes, bars + 8 * put);
+      }
+      put = put + 1 == kRing ? 0 : put + 1;
+    };
+    // copies the keys of the next block into the ring and notes its steps at place i of the queue
+    auto copy_keys = [&](int i) {
+      if (pro_left <= 0) { v_src = nullptr; return; }
+      const bool bad = phys < 0 || phys >= a.n_blocks;
+      if (bad) report_status(a.hdr, TLQ_ERR_SHAPE, 210);
+      const int64_t at = (int64_t)(bad ? 0 : phys) * a.n_kv + pro.h;
+      q_base[i] = bad ? 0x7FFFFFFF - kKvBlock : pro.blk * kKvBlock;
+      q_k[i] = __ldg(a.k_steps + at);
+      q_v[i] = __ldg(a.v_steps + at);
+      copy(a.k_codes + at * kBytes);
+      v_src = a.v_codes + at * kBytes;
+      --pro_left;
+      if (++pro.blk >= pro.un.blocks) pro.next_item(a, kRows);
+      look_up();
+    };
+    auto copy_values = [&]() {
+      if (v_src != nullptr) copy(v_src);
+    };
+    look_up();
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) {
+      copy_keys(i);
+      if (i + 1 < kDeep) copy_values();                    // the last block's values follow when a chunk is free
+    }
+    int take = 0;                                          // chunk that is read next
+    uint32_t phase = 0;
+    bool ok = true;
+    auto arrive = [&]() {
+      ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bars + 8 * take, phase, &s_abort));
+      return ring + take * kBytes;
+    };
+    auto taken = [&]() {
+      if (++take == kRing) { take = 0; phase ^= 1u; }
+    };
 
-    // -------------------------------------------------------------- query rows, as the n side of the products
-    uint32_t qf[NT][D / 16][2];
-    float fac[NT][2];                              // of columns 2 tq, 2 tq + 1: scale * log2(e) * 2^exponent
-    int last[NT][2];                               // last place that the column sees
+    long long unit = w_begin;
+    while (true) {
+      if (con.blk < 0) {
+        unit -= con.blk;
+        con.blk = 0;
+      }
+      if (unit >= w_end || !ok) break;
+      const int blk0 = con.blk;
+      const long long left = w_end - unit;
+      const int blk1 = con.un.blocks - blk0 <= left ? con.un.blocks : blk0 + (int)left;
+      const Request req = con.req;
+      const int n_rows = min(kRows, req.q_len * a.group - con.tile * kRows);
+      const int past = req.kv - req.q_len, row0 = con.tile * kRows;
+
+      // ------------------------------------------------------------ query rows, as the n side of the products
+      uint32_t qf[NT][D / 16][2];
+      float fac[NT][2];                                    // of columns 2 tq, 2 tq + 1: scale * log2(e) * 2^(24 + exponent)
+      float off[NT][2];                                    // and 128 2^-24 sum(q)
+      int last[NT][2];                                     // last place that the column sees
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int r = n * 8 + gr;
-      float f = 0.f;
-      float x[D / 4];
-      float top = 0.f;
-      const bool live = r < n_rows;
-      const int row = tile * kRows + r;
-      if (live) {
-        const uint16_t* p = g.q + (int64_t)(req.q0 + row / a.group) * g.ldq + (int64_t)(h * a.group + row % a.group) * D;
+      for (int n = 0; n < NT; ++n) {
+        const int r = n * 8 + gr;
+        float x[D / 4];
+        float top = 0.f;
+        if (r < n_rows) {
+          const int row = row0 + r;
+          const uint16_t* p = g.q + (int64_t)(req.q0 + row / a.group) * g.ldq + (int64_t)(con.h * a.group + row % a.group) * D;
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c)
+          for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              float e[8];
+              unpack8(__ldg(reinterpret_cast<const uint4*>(p + 64 * c + 16 * tq + 8 * i)), e);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) x[c * 16 + i * 8 + j] = e[j];
+            }
+        } else {
+#pragma unroll
+          for (int j = 0; j < D / 4; ++j) x[j] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < D / 4; ++j) top = fmaxf(top, fabsf(x[j]));
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+        const int ex = top > 0.f && top <= 3.4e38f ? ilogbf(top) : 0;
+        const float f = ldexpf(g.scale_log2, ex + 24);
+        float qs = 0.f;
+        // 2^-ex in two factors, either of which is a normal number
+        const float d0 = ldexpf(1.0f, -(ex / 2)), d1 = ldexpf(1.0f, -(ex - ex / 2));
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+          qf[n][s][0] = pack_f16(x[4 * s] * d0 * d1, x[4 * s + 1] * d0 * d1);
+          qf[n][s][1] = pack_f16(x[4 * s + 2] * d0 * d1, x[4 * s + 3] * d0 * d1);
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            float e[8];
-            unpack8(*reinterpret_cast<const uint4*>(p + 64 * c + 16 * tq + 8 * i), e);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[c * 16 + i * 8 + j] = e[j];
+            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&qf[n][s][i]));
+            qs += y.x + y.y;
           }
-      } else {
+        }
+        qs += __shfl_xor_sync(0xFFFFFFFFu, qs, 1);
+        qs += __shfl_xor_sync(0xFFFFFFFFu, qs, 2);
 #pragma unroll
-        for (int j = 0; j < D / 4; ++j) x[j] = 0.f;
+        for (int j = 0; j < 2; ++j) {
+          fac[n][j] = __shfl_sync(0xFFFFFFFFu, f, (2 * tq + j) * 4);
+          off[n][j] = __shfl_sync(0xFFFFFFFFu, qs, (2 * tq + j) * 4) * (128.f / kUnit);
+          const int c = n * 8 + 2 * tq + j;
+          last[n][j] = c >= n_rows ? -1 : g.causal ? min(past + (row0 + c) / a.group, req.kv - 1) : req.kv - 1;
+        }
       }
-#pragma unroll
-      for (int j = 0; j < D / 4; ++j) top = fmaxf(top, fabsf(x[j]));
-      top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-      top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-      const int ex = top > 0.f && top <= 3.4e38f ? ilogbf(top) : 0;
-      f = ldexpf(g.scale_log2, ex);
-#pragma unroll
-      for (int s = 0; s < D / 16; ++s) {
-        qf[n][s][0] = pack_f16(ldexpf(x[4 * s], -ex), ldexpf(x[4 * s + 1], -ex));
-        qf[n][s][1] = pack_f16(ldexpf(x[4 * s + 2], -ex), ldexpf(x[4 * s + 3], -ex));
-      }
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        fac[n][j] = __shfl_sync(0xFFFFFFFFu, f, (2 * tq + j) * 4);
-        const int c = n * 8 + 2 * tq + j;
-        last[n][j] = c >= n_rows ? -1 : g.causal ? min(past + (tile * kRows + c) / a.group, req.kv - 1) : req.kv - 1;
-      }
-    }
-    // a block that ends at or before this place needs no mask
-    const int row0 = tile * kRows;
-    const int sure = g.causal ? min(past + row0 / a.group, req.kv - 1) : req.kv - 1;
+      // a block that ends at or before this place needs no mask
+      const int sure = g.causal ? min(past + row0 / a.group, req.kv - 1) : req.kv - 1;
 
-    float o[NT][D / 16][4];
-    float m[NT][2], l[NT][2];
+      float o[NT][D / 16][4];
+      float m[NT][2], l[NT][2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      m[n][0] = m[n][1] = -INFINITY;
-      l[n][0] = l[n][1] = 0.f;
+      for (int n = 0; n < NT; ++n) {
+        m[n][0] = m[n][1] = -INFINITY;
+        l[n][0] = l[n][1] = 0.f;
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i)
+        for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[n][i][j] = 0.f;
-    }
+          for (int j = 0; j < 4; ++j) o[n][i][j] = 0.f;
+      }
 
-    const int32_t* table = a.block_table + (int64_t)b * a.max_blocks;
-    const int stop = req.kv > 0 ? blk1 : 0;
-    int blk = blk0 + warp;
-    if (blk < stop) {
-      Block<D, NT> s;
-      int phys = __ldg(table + blk);
-      load_k(s, a, phys, h, blk, gr, tq);
-      load_v(s, a, phys, h, gr, tq);
-      int phys_next = blk + kWarps < stop ? __ldg(table + blk + kWarps) : 0;
-      while (true) {
+      const int n_blk = req.kv > 0 ? blk1 - blk0 : 0;
+      for (int it = 0; it < n_blk; ++it) {
         // ---------------------------------------------------------- S^T = K q^T
         float sc[NT][4][4];
 #pragma unroll
@@ -271,22 +511,26 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
           for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) sc[n][i][j] = 0.f;
+        const uint32_t ka = arrive() + (16 * (gr >> 1) + (gr & 1)) * D + 16 * tq;
+        if (!ok) break;
 #pragma unroll
         for (int c = 0; c < D / 64; ++c)
 #pragma unroll
-          for (int w = 0; w < 4; ++w)
+          for (int i = 0; i < 4; ++i) {
+            const uint4 k0 = lds128(ka + 4 * i * D + 64 * c), k1 = lds128(ka + (4 * i + 2) * D + 64 * c);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int w = 0; w < 4; ++w) {
               uint32_t a0, a1, a2, a3;
-              codes_to_f16(word(s.k[i][c][0], w), a0, a2);
-              codes_to_f16(word(s.k[i][c][1], w), a1, a3);
+              keys_to_f16(word(k0, w), a0, a2);
+              keys_to_f16(word(k1, w), a1, a3);
 #pragma unroll
               for (int n = 0; n < NT; ++n) mma_f16(sc[n][i], a0, a1, a2, a3, qf[n][4 * c + w][0], qf[n][4 * c + w][1]);
             }
-        const float kstep = s.kstep, vstep = s.vstep < kStepFloor ? kStepFloor : s.vstep, vinv = 1.0f / vstep, vlog = log2f(vstep);
-        const int base = s.base, next = blk + kWarps;
-        const bool more = next < stop;
-        if (more) load_k(s, a, phys_next, h, next, gr, tq);
+          }
+        taken();
+        copy_values();
+        const float kstep = q_k[0], vstep = q_v[0] < kStepFloor ? kStepFloor : q_v[0], vinv = 1.0f / vstep, vlog = log2f(vstep);
+        const int base = q_base[0];
 
         // ---------------------------------------------------------- running softmax of each column
         const bool masked = base + kKvBlock - 1 > sure;
@@ -295,13 +539,13 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const float f = fac[n][j] * kstep;
+            const float f = fac[n][j] * kstep, add = fmaf(-off[n][j], f, vlog);
             float top = -INFINITY;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
-                float x = fmaf(sc[n][i][2 * e + j], f, vlog);
+                float x = fmaf(sc[n][i][2 * e + j], f, add);
                 if (masked && base + 16 * (gr >> 1) + (gr & 1) + 4 * i + 2 * e > last[n][j]) x = -INFINITY;
                 sc[n][i][2 * e + j] = x;
                 top = fmaxf(top, x);
@@ -335,134 +579,154 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
           }
         }
         // ---------------------------------------------------------- O^T += V^T P^T
+        const uint32_t va = arrive() + gr * kKvBlock + 16 * tq;
+        if (!ok) break;
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i)
+        for (int i = 0; i < D / 16; ++i) {
+          const uint4 v0 = lds128(va + 16 * i * kKvBlock), v1 = lds128(va + (16 * i + 8) * kKvBlock);
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
             uint32_t a0, a1, a2, a3;
-            codes_to_f16(word(s.v[i][0], w), a0, a2);
-            codes_to_f16(word(s.v[i][1], w), a1, a3);
+            values_to_f16(word(v0, w), a0, a2);
+            values_to_f16(word(v1, w), a1, a3);
 #pragma unroll
             for (int n = 0; n < NT; ++n) mma_f16(o[n][i], a0, a1, a2, a3, pf[n][w][0], pf[n][w][1]);
           }
-        if (!more) break;
-        load_v(s, a, phys_next, h, gr, tq);
-        blk = next;
-        phys_next = blk + kWarps < stop ? __ldg(table + blk + kWarps) : 0;
-      }
-    }
-    // ---------------------------------------------------------------- join the warps
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) l[n][j] += __shfl_xor_sync(0xFFFFFFFFu, l[n][j], d);
-    __syncthreads();                               // the previous item's readers are done
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int c = n * 8 + 2 * tq + j;
-        if (gr == 0) {
-          s_m[warp * kRows + c] = m[n][j];
-          s_l[warp * kRows + c] = l[n][j];
         }
-        float* to = s_o + (warp * kRows + c) * (D + 1);
+        taken();
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-          to[16 * i + gr] = o[n][i][j];
-          to[16 * i + 8 + gr] = o[n][i][2 + j];
+        for (int i = 0; i + 1 < kDeep; ++i) {
+          q_k[i] = q_k[i + 1];
+          q_v[i] = q_v[i + 1];
+          q_base[i] = q_base[i + 1];
         }
+        copy_keys(kDeep - 1);
       }
-    __syncthreads();
-    const bool whole = item_begin >= u_begin && item_end <= u_end;
-    const int slot = blockIdx.x * 2 + (item_begin >= u_begin ? 1 : 0);
-    float* part = g.split.partials + (size_t)slot * kRows * (D + 2);
-    for (int e = threadIdx.x; e < kRows * D; e += kThreads) {
-      const int c = e / D, d = e % D;
-      float mm = -INFINITY;
+      if (!ok) break;
+      // -------------------------------------------------------------- leave the item
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) mm = fmaxf(mm, s_m[w * kRows + c]);
-      const float mu = mm == -INFINITY ? 0.f : mm;
-      float sum = 0.f, den = 0.f;
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float f = exp2_fast(s_m[w * kRows + c] - mu);
-        sum = fmaf(s_o[(w * kRows + c) * (D + 1) + d], f, sum);
-        den = fmaf(s_l[w * kRows + c], f, den);
-      }
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) l[n][j] += __shfl_xor_sync(0xFFFFFFFFu, l[n][j], d);
+      const bool whole = blk0 == 0 && blk1 == con.un.blocks;
       if (whole) {
-        if (c < n_rows) {
-          const int row = tile * kRows + c;
-          const int64_t at = (int64_t)(req.q0 + row / a.group) * a.n_heads + h * a.group + row % a.group;
-          const bool none = mm == -INFINITY && den == 0.f;       // a row that sees nothing (a NaN row has den = NaN)
-          const __nv_bfloat16 y = __float2bfloat16_rn(none ? 0.f : sum / den);
-          g.out[at * D + d] = *reinterpret_cast<const uint16_t*>(&y);
-          if (d == 0 && g.lse != nullptr) g.lse[at] = none ? -INFINITY : kLn2 * (log2f(den) + mm - kShift);
-        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int c = n * 8 + 2 * tq + j;
+            if (c >= n_rows) continue;
+            const int64_t at = out_row(a, req, con.h, row0 + c);
+            const bool none = m[n][j] == -INFINITY && l[n][j] == 0.f;    // a row that sees nothing (a NaN row has a NaN sum)
+            const float inv = none ? 0.f : 1.0f / l[n][j];
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const __nv_bfloat16 y = __float2bfloat16_rn(none ? 0.f : o[n][i][2 * e + j] * inv);
+                g.out[at * D + 16 * i + 8 * e + gr] = *reinterpret_cast<const uint16_t*>(&y);
+              }
+            if (gr == 0 && g.lse != nullptr) g.lse[at] = none ? -INFINITY : kLn2 * (log2f(l[n][j]) + m[n][j] - kShift);
+          }
       } else {
-        part[2 * kRows + e] = sum;
-        if (d == 0) {
-          part[c] = mm;
-          part[kRows + c] = den;
+        float* to = warp_slot(warp, blk0 == 0 ? 1 : 0);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int c = n * 8 + 2 * tq + j;
+            if (gr == 0) {
+              to[c] = m[n][j];
+              to[kRows + c] = l[n][j];
+            }
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+              to[2 * kRows + c * D + 16 * i + gr] = o[n][i][j];
+              to[2 * kRows + c * D + 16 * i + 8 + gr] = o[n][i][2 + j];
+            }
+          }
+        if (lane == 0) {
+          Shared* d = blk0 == 0 ? &s_last[warp] : &s_first[warp];
+          d->begin = unit - blk0;
+          d->end = d->begin + con.un.blocks;
+          d->b = con.b; d->h = con.h; d->tile = con.tile;
+          s_has[warp] |= blk0 == 0 ? 2 : blk1 < con.un.blocks ? 5 : 1;
         }
       }
+      unit += blk1 - blk0;
+      con.blk = blk1;
+      if (unit < w_end) con.next_item(a, kRows);
     }
-    if (!whole) {
-      // ---------------------------------------------------------------- join the CTAs that share the item
-      const long long first = worker_of(item_begin), final = worker_of(item_end - 1);
+    if (!ok && lane == 0) report_status(a.hdr, TLQ_ERR_TIMEOUT, 211);
+  }
+  __syncthreads();
+  if (*(volatile int*)&s_abort != 0) {                     // a copy that never came: give those under way time to land
+    for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+    return;
+  }
+
+  // ---------------------------------------------------------------- join the warps of this CTA
+  // An item that is cut starts with the last item of some warp, or began before the CTA (the first of warp 0), and goes on
+  // in the first items of the warps after it.
+  const int has = lane < kWarps ? s_has[lane] : 0;
+  const uint32_t firsts = __ballot_sync(0xFFFFFFFFu, has & 1), lasts = __ballot_sync(0xFFFFFFFFu, has & 2),
+                 thrus = __ballot_sync(0xFFFFFFFFu, has & 4);
+  // one chain: all threads; several: the warp that it begins in (what began before the CTA: warp 0)
+  const int n_chains = __popc(lasts) + (int)(firsts & 1u);
+  for (int i = 0; i < 2; ++i) {
+    const int w = n_chains > 1 ? warp : i == 0 ? 0 : __ffs(lasts) - 1;
+    if (i == 0 ? (w != 0 || !(firsts & 1u)) : (w < 0 || !(lasts >> w & 1u))) continue;
+    int parts = 1;
+    bool on = i != 0 || (thrus & 1u);
+    while (on && w + parts < kWarps && (firsts >> (w + parts) & 1u)) {
+      on = thrus >> (w + parts) & 1u;
+      ++parts;
+    }
+    const Shared it = i ? s_last[w] : s_first[w];
+    const bool inside = it.begin >= u_begin && it.end <= u_end;
+    float* to = inside ? nullptr : cta_slot(blockIdx.x, it.begin >= u_begin ? 1 : 0);
+    const int id = n_chains > 1 ? lane : (int)threadIdx.x;
+    join_warps<D, NT>(a, g, it, parts, warp_slot(w, i), warp_slot(w, 0) + 2 * kPitch, 2 * kPitch, to, id,
+                      n_chains > 1 ? 32 : kThreads);
+    if (!inside && id == 0) s_cta[it.begin >= u_begin ? 1 : 0] = it;
+  }
+  // ---------------------------------------------------------------- join the CTAs that share an item
+  __syncthreads();
+  if (s_cta[0].begin == s_cta[0].end && s_cta[1].begin == s_cta[1].end) return;
+  if (threadIdx.x < 2) {
+    const Shared it = s_cta[threadIdx.x];
+    s_join[threadIdx.x] = 0;
+    if (it.begin < it.end) {
+      const long long first = worker_of(it.begin), final = worker_of(it.end - 1);
+      __threadfence();                                     // the CTA's partials, which the barrier has ordered before this
+      s_join[threadIdx.x] = atomicAdd(g.split.counters + first, 1) == (int)(final - first);
+      if (s_join[threadIdx.x]) g.split.counters[first] = 0;
       __threadfence();
-      __syncthreads();
-      if (threadIdx.x == 0) s_last = atomicAdd(g.split.counters + first, 1) == (int)(final - first);
-      __syncthreads();
-      if (s_last) {
-        __threadfence();
-        if (threadIdx.x == 0) g.split.counters[first] = 0;
-        const float* base = g.split.partials;
-        const size_t pitch = (size_t)kRows * (D + 2);
-        for (int e = threadIdx.x; e < kRows * D; e += kThreads) {
-          const int c = e / D, d = e % D;
-          if (c >= n_rows) break;
-          float mm = -INFINITY, sum = 0.f, den = 0.f;
-          for (long long w = first; w <= final; ++w) {
-            const float* p = base + (size_t)(2 * w + (w == first ? 1 : 0)) * pitch;
-            mm = fmaxf(mm, __ldcg(p + c));
-          }
-          const float mu = mm == -INFINITY ? 0.f : mm;
-#pragma unroll 4
-          for (long long w = first; w <= final; ++w) {
-            const float* p = base + (size_t)(2 * w + (w == first ? 1 : 0)) * pitch;
-            const float f = exp2_fast(__ldcg(p + c) - mu);
-            sum = fmaf(__ldcg(p + 2 * kRows + e), f, sum);
-            den = fmaf(__ldcg(p + kRows + c), f, den);
-          }
-          const int row = tile * kRows + c;
-          const int64_t at = (int64_t)(req.q0 + row / a.group) * a.n_heads + h * a.group + row % a.group;
-          const bool none = mm == -INFINITY && den == 0.f;
-          const __nv_bfloat16 y = __float2bfloat16_rn(none ? 0.f : sum / den);
-          g.out[at * D + d] = *reinterpret_cast<const uint16_t*>(&y);
-          if (d == 0 && g.lse != nullptr) g.lse[at] = none ? -INFINITY : kLn2 * (log2f(den) + mm - kShift);
-        }
-      }
     }
-    unit += blk1 - blk0;
-    rest += blk1 - blk0;
+  }
+  __syncthreads();
+  for (int i = 0; i < 2; ++i) {
+    if (!s_join[i]) continue;
+    const Shared it = s_cta[i];
+    const long long first = worker_of(it.begin), final = worker_of(it.end - 1);
+    join_ctas<D, NT>(a, g, it, (int)(final - first) + 1, cta_slot(first, 1), cta_slot(first, 0) + 2 * kPitch, 2 * kPitch,
+                     reinterpret_cast<float*>(smem));
   }
 }
 
 template <int D, int NT>
 int launch(const KvArgs& a, const AttnArgs& g, cudaStream_t st) {
-  constexpr size_t smem = (size_t)kWarps * 8 * NT * (D + 3) * sizeof(float);
   static OncePerDevice once;
   const int rc = once_per_device(once, [] {
-    return cudaFuncSetAttribute(kv_attention_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    return cudaFuncSetAttribute(kv_attention_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes<D>);
   });
   if (rc != TLQ_OK) return rc;
   const int sms = device_sm_count();
   if (sms <= 0) return TLQ_ERR_CUDA;
   const int grid = sms < kMaxWorkers ? sms : kMaxWorkers;
-  kv_attention_kernel<D, NT><<<grid, kThreads, smem, st>>>(a, g);
+  kv_attention_kernel<D, NT><<<grid, kThreads, kRingBytes<D>, st>>>(a, g);
   return after_launch();
 }
 

@@ -109,10 +109,11 @@ int launch_kv_store(const uint16_t* qkv, int64_t ld, int head_dim, const KvArgs&
                     uint16_t* v_values, cudaStream_t st);
 
 // kv_attention.cu: workspace of the split over the cache (counters are zero between calls)
-constexpr int kMaxWorkers = 512;          // CTAs that share one call's work
+constexpr int kMaxWorkers = 160;          // CTAs that share one call's work (one per SM)
+constexpr int kSplitWarps = 8;            // warps of one of them
 constexpr int kMaxRowTile = 16;           // query rows of one work item
-inline size_t kv_split_floats(int head_dim) {
-  return (size_t)kMaxWorkers * 2 * kMaxRowTile * ((size_t)head_dim + 2);
+inline size_t kv_split_floats(int head_dim) {          // two partials of every warp and of every CTA
+  return (size_t)kMaxWorkers * 2 * (kSplitWarps + 1) * kMaxRowTile * ((size_t)head_dim + 2);
 }
 struct KvSplit {
   int32_t* counters;          // [kMaxWorkers]
