@@ -309,6 +309,7 @@ gemm_w8a8_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
           if (lane == 0)
             args.partials[(int64_t)k * args.otiles * args.mtiles * 8 + ((int64_t)ot * args.mtiles + mt) * 8 + ew] = v;
         } else {
+          const bool even = (args.C2 & 7) == 0;
 #pragma unroll 1
           for (int c = 0; c < 8; ++c) {
             uint32_t r[16];
@@ -318,7 +319,13 @@ gemm_w8a8_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
 #pragma unroll
               for (int p = 0; p < 2; ++p) {
                 const int64_t col = col_base + c * 16 + p * 8;
-                if (col < args.C2) {
+                if (col < args.C2 && !even) {            // rows of Y at any alignment: one element at a time
+                  for (int j = 0; j < 8 && col + j < args.C2; ++j) {
+                    float v = (float)(int)r[p * 8 + j] * (tn * __ldg(u_row + col + j));
+                    if (args.bias != nullptr) v += bf16_bits_to_float(args.bias[col + j]);
+                    args.yq[n * args.C2 + col + j] = (uint16_t)float_to_bf16_bits(v);
+                  }
+                } else if (col < args.C2) {
                   uint32_t o[4];
 #pragma unroll
                   for (int j = 0; j < 8; ++j) {
