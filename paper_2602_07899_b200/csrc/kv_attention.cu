@@ -42,7 +42,7 @@ struct AttnArgs {
   uint16_t* out;
   float* lse;
   float scale_log2;          // scale * log2(e)
-  int causal;
+  int causal, max_rows;      // requests with max_rows query rows or more belong to the prompt kernel
   KvSplit split;
 };
 
@@ -108,9 +108,10 @@ struct Units {
   int row_tiles, blocks;
   long long total;
 };
-__device__ __forceinline__ Units units_of(const KvArgs& a, const Request& r, int row_tile) {
+__device__ __forceinline__ Units units_of(const KvArgs& a, const Request& r, int row_tile, int max_rows) {
   Units u;
-  u.row_tiles = (int)(((long long)r.q_len * a.group + row_tile - 1) / row_tile);
+  const long long rows = (long long)r.q_len * a.group;
+  u.row_tiles = rows < max_rows ? (int)((rows + row_tile - 1) / row_tile) : 0;
   u.blocks = r.kv > 0 ? (r.kv + kKvBlock - 1) / kKvBlock : 1;
   u.total = (long long)u.row_tiles * a.n_kv * (u.blocks + kItemUnits);
   return u;
@@ -119,14 +120,14 @@ __device__ __forceinline__ Units units_of(const KvArgs& a, const Request& r, int
 
 // A place on the line of units: block `blk` of an item (request b, kv head h, row tile), or one of the units before it (blk < 0).
 struct Walker {
-  int b, h, tile, blk;
+  int b, h, tile, blk, max_rows;
   Request req;
   Units un;
 
   __device__ __forceinline__ void enter(const KvArgs& a, int request, int row_tile) {
     b = request;
     req = load_request(a, b);
-    un = units_of(a, req, row_tile);
+    un = units_of(a, req, row_tile, max_rows);
   }
   // `rest` units into request `request`
   __device__ __forceinline__ void start(const KvArgs& a, int request, long long rest, int row_tile) {
@@ -311,7 +312,7 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
   }
   if (threadIdx.x < 2) s_cta[threadIdx.x].begin = s_cta[threadIdx.x].end = 0;
   if (lane == 0) s_has[warp] = 0;
-  auto count_units = [&](int b) { return units_of(a, load_request(a, b), kRows).total; };
+  auto count_units = [&](int b) { return units_of(a, load_request(a, b), kRows, g.max_rows).total; };
   long long total = 0;
   for (int b0 = 0; b0 < a.B; b0 += kThreads) {
     const int b = b0 + (int)threadIdx.x;
@@ -341,6 +342,7 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
 
   if (w_begin < w_end) {
     Walker con;                                            // what is computed now
+    con.max_rows = g.max_rows;
     {
       int b = found.request;
       long long rest = found.rest + (w_begin - u_begin);
@@ -739,7 +741,13 @@ int launch_kv_attention(const uint16_t* q, int64_t ldq, int head_dim, const KvAr
   g.scale_log2 = scale * kLog2e;
   g.causal = causal;
   g.split = split;
-  const bool narrow = (int64_t)a.group * a.max_q_len <= 8;
+  const int64_t rows = (int64_t)a.group * (a.T < a.max_q_len ? a.T : a.max_q_len);     // of one request, at most
+  g.max_rows = kPromptRows;
+  if (rows >= kPromptRows) {
+    const int rc = launch_kv_prompt(q, ldq, head_dim, a, scale, causal, kPromptRows, out, lse, split, st);
+    if (rc != TLQ_OK) return rc;
+  }
+  const bool narrow = rows <= 8;
   if (head_dim == 128) return narrow ? launch<128, 1>(a, g, st) : launch<128, 2>(a, g, st);
   return narrow ? launch<64, 1>(a, g, st) : launch<64, 2>(a, g, st);
 }

@@ -1,0 +1,738 @@
+// Attention of many query rows over the 8-bit cache (prompts and chunks of prompts) on the tensor-memory path.
+//
+// The formulas are those of kv_attention.cu: scores from (kc + 128) with the 128 sum(q) taken out by a constant of the row,
+// p_j = 2^(t_j - m) with t_j = a (q . kc_j) + log2(vstep), output sums of p vc and sums of p / vstep.
+//
+// A CTA works on 256 rows of one (request, kv head), a row being one query head of one token: two tiles of 128 rows, so
+// that the exponentials of one run while the tensor core works on the other.  Per tile and 128 cached tokens: S = q K^T
+// (tcgen05, f16 x f16 -> f32, tensor memory), one thread per row takes the maximum and the exponentials of its row straight
+// from tensor memory and writes P over S as f16, O += P V with P from tensor memory.  The output sum is rescaled only when
+// the maximum of a row has grown by more than 4 (a factor of 16 in p): p is kept as 2^11 p, so that it fits 16 bits either way.
+//   warps 0..3, 4..7  softmax of tile 0, 1: a thread is a row (and its accumulator lane)
+//   warps 8..11       bring the codes of keys and values from the cache into registers, turn them into f16 and lay them
+//                     out for the tensor core (128-byte swizzle); two stages each
+//   warp 12           issues the products
+// Work is cut as in the few-row kernel: items (row tiles of a kv head) lie on one line, weighted by their cached tokens,
+// every CTA takes an equal part of it; an item that is cut leaves partial sums, and the CTA that completes it joins them.
+//
+// Bound: the tensor core (4 D flops per visible pair) and, next to it, the exponential unit: 256 x 128 exponentials at 16
+// per cycle take as long as the products of the same tile.
+#include "serve.cuh"
+#include "umma.cuh"
+
+namespace tlq {
+namespace {
+
+constexpr int kTile = 128, kItemRows = 256, kKeys = 128;
+constexpr int kSoftWarps = 8, kLoadWarps = 4;
+constexpr int kThreads = (kSoftWarps + kLoadWarps + 1) * 32;
+constexpr float kShift = 11.f, kGrow = 4.f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kStepFloor = 7.8886090522101181e-31f;      // 2^-100, as in kv_attention.cu
+constexpr float kUnit = 16777216.f;                        // 2^24
+constexpr int kMinTiles = 6;                               // key tiles of a CTA's part, at least
+constexpr int kItemCost = 2;                               // what an item costs beside its key tiles, in key tiles
+
+struct PromptArgs {
+  const uint16_t* q;
+  int64_t ldq;
+  uint16_t* out;
+  float* lse;
+  float scale_log2;
+  int causal, min_rows;         // requests with fewer rows than this belong to the few-row kernel
+  KvSplit split;
+};
+
+template <int D>
+constexpr uint32_t kPanels = D / 64;                       // 64 channels of f16 are one row of the swizzle
+template <int D>
+constexpr uint32_t kQBytes = kTile * D * 2;                // of one tile of queries
+template <int D>
+constexpr uint32_t kKBytes = kKeys * D * 2;                // of one stage of keys
+template <int D>
+constexpr uint32_t kVBytes = kKeys * D * 2;                // of one stage of values
+template <int D>
+constexpr size_t kSmem = 1024 + 2 * kQBytes<D> + 2 * kKBytes<D> + 2 * kVBytes<D>;
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint4 ld_cache(const int8_t* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+// (code + 128) 2^-24 as f16, and exactly the code: see kv_attention.cu
+__device__ __forceinline__ void keys_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  const uint32_t x = w ^ 0x80808080u;
+  lo = __byte_perm(x, 0u, 0x4140);
+  hi = __byte_perm(x, 0u, 0x4342);
+}
+__device__ __forceinline__ void values_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  const uint32_t x = w ^ 0x80808080u;
+  const uint32_t a = __byte_perm(x, 0x64646464u, 0x4140), b = __byte_perm(x, 0x64646464u, 0x4342);
+  const __half2 off = __floats2half2_rn(1152.f, 1152.f);
+  const __half2 ra = __hsub2(*reinterpret_cast<const __half2*>(&a), off);
+  const __half2 rb = __hsub2(*reinterpret_cast<const __half2*>(&b), off);
+  lo = *reinterpret_cast<const uint32_t*>(&ra);
+  hi = *reinterpret_cast<const uint32_t*>(&rb);
+}
+
+__device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  ptx::mma_bf16_ss(d, a, b, idesc, accumulate);            // kind::f16 covers both types; the descriptor names f16
+}
+// A from tensor memory
+__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// ---------------------------------------------------------------------------------------------- the line of work
+// Item `tile` of a request costs first + tile * more; the first n cost sum(n).
+struct Costs {
+  int tiles;
+  long long first, more;
+  __device__ __forceinline__ long long sum(long long n) const { return first * n + more * (n * (n - 1) / 2); }
+};
+__device__ __forceinline__ Costs costs_of(const KvArgs& a, const PromptArgs& g, const Request& r) {
+  Costs c;
+  const long long rows = (long long)r.q_len * a.group;
+  c.tiles = rows >= g.min_rows ? (int)((rows + kItemRows - 1) / kItemRows) : 0;
+  const int seen = g.causal ? min(max(r.kv - r.q_len, 0) + kItemRows / a.group, r.kv) : r.kv;
+  c.first = 64LL * (kItemCost + 1) + 64LL * seen / kKeys;
+  c.more = g.causal ? 64LL * kItemRows / kKeys / a.group : 0;
+  return c;
+}
+
+// A part of an item: key tiles [k0, k1) of n.
+struct Segment {
+  int b, h, tile, k0, k1, n;
+  long long at, len;            // the item on the line
+  Request req;
+};
+
+// Walks the items that overlap [x0, x1) of the line.
+struct Walk {
+  long long x0, x1, base;       // base: where (request b, head h) starts on the line
+  int b, h, tile;
+  Request req;
+  Costs costs;
+
+  __device__ __forceinline__ int key_tiles(const KvArgs& a, const PromptArgs& g) const {
+    const long long rows = (long long)req.q_len * a.group;
+    const int row = (int)(min((long long)(tile + 1) * kItemRows, rows) - 1);
+    const int last = g.causal ? min(req.kv - req.q_len + row / a.group, req.kv - 1) : req.kv - 1;
+    return last < 0 ? 0 : last / kKeys + 1;
+  }
+  __device__ __forceinline__ void start(const KvArgs& a, const PromptArgs& g, int request, long long rest, long long from, long long to) {
+    x0 = from; x1 = to;
+    b = request;
+    req = load_request(a, b);
+    costs = costs_of(a, g, req);
+    const long long one = costs.sum(costs.tiles);
+    h = (int)(rest / one);
+    const long long in = rest - h * one;
+    base = from - in;
+    int lo = 0, hi = costs.tiles - 1;                      // the last tile that starts at or before `in`
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (costs.sum(mid) <= in) lo = mid; else hi = mid - 1;
+    }
+    tile = lo;
+  }
+  // the part of the current item in [from, to)
+  __device__ __forceinline__ void cut(long long from, long long to, long long at, long long len, int n, int& k0, int& k1) const {
+    k0 = from <= at ? 0 : from >= at + len ? n : (int)((long long)n * (from - at) / len);
+    k1 = to >= at + len ? n : to <= at ? 0 : (int)((long long)n * (to - at) / len);
+  }
+  // next part with something to do; false at the end
+  __device__ __forceinline__ bool next(const KvArgs& a, const PromptArgs& g, Segment& s) {
+    while (true) {
+      while (tile >= costs.tiles) {
+        base += costs.sum(costs.tiles);
+        tile = 0;
+        if (costs.tiles > 0 && ++h < a.n_kv) break;
+        h = 0;
+        if (++b >= a.B) return false;
+        req = load_request(a, b);
+        costs = costs_of(a, g, req);
+      }
+      s.at = base + costs.sum(tile);
+      if (s.at >= x1) return false;
+      s.len = costs.sum(tile + 1) - costs.sum(tile);
+      s.n = key_tiles(a, g);
+      cut(x0, x1, s.at, s.len, s.n, s.k0, s.k1);
+      s.b = b; s.h = h; s.tile = tile; s.req = req;
+      const bool here = s.n == 0 ? s.at >= x0 : s.k0 < s.k1;   // an item without visible keys belongs to whoever has its start
+      ++tile;
+      if (here) return true;
+    }
+  }
+};
+
+struct Cut {                    // an item of which this CTA has only a part
+  long long at, len;
+  int b, h, tile, n;
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t q_at = base, k_at = q_at + 2 * kQBytes<D>, v_at = k_at + 2 * kKBytes<D>;
+  __shared__ __align__(8) uint64_t bars[16];
+  __shared__ __align__(16) float4 s_steps[4][2];           // of the two blocks of a key tile: kstep, log2 vstep, 1 / vstep, usable
+  __shared__ long long sums[kThreads / 32];
+  __shared__ Found found;
+  __shared__ Cut s_cut[2];
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_abort, s_join[2];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto bar = [&](int i) { return ptx::smem_u32(&bars[i]); };
+  // [0,2) q ready, [2,4) k ready, [4,6) k free, [6,8) v ready, [8,10) v free, [10,12) S ready, [12,14) P ready, [14,16) O ready
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(bar(i), 4);
+      ptx::mbar_init(bar(2 + i), kLoadWarps);
+      ptx::mbar_init(bar(4 + i), 1);
+      ptx::mbar_init(bar(6 + i), kLoadWarps);
+      ptx::mbar_init(bar(8 + i), 1);
+      ptx::mbar_init(bar(10 + i), 1);
+      ptx::mbar_init(bar(12 + i), 4);
+      ptx::mbar_init(bar(14 + i), 1);
+      s_cut[i].len = 0;
+    }
+    s_abort = 0;
+    ptx::fence_barrier_init();
+  }
+  volatile int* abort_flag = &s_abort;
+
+  // ---------------------------------------------------------------- this CTA's part of the line
+  auto cost_of = [&](int b) {
+    const Costs c = costs_of(a, g, load_request(a, b));
+    return c.sum(c.tiles) * a.n_kv;
+  };
+  long long total = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+    const int b = b0 + (int)threadIdx.x;
+    long long part;
+    block_scan<kThreads>(b < a.B ? cost_of(b) : 0, sums, part);
+    total += part;
+  }
+  if (total == 0) return;
+  // a part is worth joining from some key tiles on
+  const long long workers = max(1LL, min((long long)gridDim.x, total / (64 * kMinTiles)));
+  if (blockIdx.x >= workers) return;
+  auto edge = [&](long long w) { return total * w / workers; };
+  auto worker_of = [&](long long x) { return ((x + 1) * workers - 1) / total; };
+  const long long x0 = edge(blockIdx.x), x1 = edge(blockIdx.x + 1);
+  if (x0 >= x1) return;
+  if (!locate_item<kThreads>(a.B, x0, cost_of, sums, &found)) return;
+  Walk walk;
+  walk.start(a, g, found.request, found.rest, x0, x1);
+  if (warp == 12) ptx::tmem_alloc(ptx::smem_u32(&s_tmem), 512);
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = s_tmem;                            // S of tile 0, 1 at columns 0, 128; O at 256, 384
+  float* const partials = g.split.partials;
+  constexpr size_t kPitch = (size_t)kItemRows * (D + 2);   // floats of a partial: maxima, sums, output sums
+  auto slot = [&](long long w, int i) { return partials + ((size_t)w * 2 + i) * kPitch; };
+  Segment s;
+
+  if (warp < kSoftWarps) {
+    // ------------------------------------------------------------------ softmax: a thread is a row
+    const int t = warp >> 2, row_in_tile = (warp & 3) * 32 + lane;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t s_col = tmem + lanes + t * kTile, o_col = tmem + lanes + 256 + t * kTile;
+    const uint32_t q_row = q_at + t * kQBytes<D> + row_in_tile * 128;
+    uint32_t s_phase = 0, o_phase = 0;
+    int step = 0;                                          // key tiles so far, of all segments
+    bool ok = true;
+    while (ok && walk.next(a, g, s)) {
+      const int row = s.tile * kItemRows + t * kTile + row_in_tile;
+      const long long rows = (long long)s.req.q_len * a.group;
+      const bool live = row < rows;
+      const int limit = !live ? -1 : g.causal ? min(s.req.kv - s.req.q_len + row / a.group, s.req.kv - 1) : s.req.kv - 1;
+      const int64_t at = live ? (int64_t)(s.req.q0 + row / a.group) * a.n_heads + s.h * a.group + row % a.group : 0;
+      // the row of q: a power of two brings it into the range of f16
+      float fac = 0.f, off = 0.f;
+      if (s.k0 < s.k1) {
+        const uint16_t* p = g.q + (live ? (int64_t)(s.req.q0 + row / a.group) * g.ldq + (int64_t)(s.h * a.group + row % a.group) * D : 0);
+        uint4 v[D / 8];
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) v[i] = live ? __ldg(reinterpret_cast<const uint4*>(p) + i) : make_uint4(0, 0, 0, 0);
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          float e[8];
+          unpack8(v[i], e);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(e[j]));
+        }
+        const int ex = top > 0.f && top <= 3.4e38f ? ilogbf(top) : 0;
+        const float d0 = ldexpf(1.0f, -(ex / 2)), d1 = ldexpf(1.0f, -(ex - ex / 2));
+        float qs = 0.f;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          float e[8];
+          unpack8(v[i], e);
+          uint32_t w[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            w[j] = pack_f16(e[2 * j] * d0 * d1, e[2 * j + 1] * d0 * d1);
+            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+            qs += y.x + y.y;
+          }
+          sts128(q_row + (i >> 3) * (kTile * 128) + (((i & 7) ^ (row_in_tile & 7)) << 4), w[0], w[1], w[2], w[3]);
+        }
+        fac = ldexpf(g.scale_log2, ex + 24);
+        off = qs * (128.f / kUnit);
+        ptx::fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(bar(t));
+      }
+
+      float m = -INFINITY, l = 0.f;
+      for (int k = s.k0; k < s.k1; ++k, ++step) {
+        ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(10 + t), s_phase, abort_flag));
+        if (!ok) break;
+        s_phase ^= 1u;
+        ptx::tc_fence_after();
+        const float4 w0 = s_steps[step & 3][0], w1 = s_steps[step & 3][1];
+        const float a0 = fac * w0.x, a1 = fac * w1.x;
+        const float b0 = fmaf(-off, a0, w0.y), b1 = fmaf(-off, a1, w1.y);
+        const int first = k * kKeys;                       // place of the tile's first key
+        const bool masked = __any_sync(0xFFFFFFFFu, first + kKeys - 1 > limit) || w0.w == 0.f || w1.w == 0.f;
+        float top = -INFINITY;
+        if (!masked) {
+          float r0 = -INFINITY, r1 = -INFINITY;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t v[32];
+            ptx::tmem_ld32(s_col + 32 * c, v);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              if (c < 2) r0 = fmaxf(r0, __uint_as_float(v[j])); else r1 = fmaxf(r1, __uint_as_float(v[j]));
+            }
+          }
+          top = fmaxf(fmaf(r0, a0, b0), fmaf(r1, a1, b1));
+        } else {
+          const int see0 = w0.w == 0.f ? -1 : min(limit - first, kKeys - 1), see1 = w1.w == 0.f ? -1 : min(limit - first, kKeys - 1);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t v[32];
+            ptx::tmem_ld32(s_col + 32 * c, v);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              const float x = fmaf(__uint_as_float(v[j]), c < 2 ? a0 : a1, c < 2 ? b0 : b1);
+              top = 32 * c + j <= (c < 2 ? see0 : see1) ? fmaxf(top, x) : top;
+            }
+          }
+        }
+        // a maximum that has grown by more than kGrow: the output sum follows
+        const bool grow = top > m + kGrow || (m == -INFINITY && top > -INFINITY);
+        if (__any_sync(0xFFFFFFFFu, grow)) {
+          const float mn = fmaxf(m, top);
+          const float corr = mn == -INFINITY ? 1.f : exp2_fast(m - mn);
+          m = mn;
+          l *= corr;
+          if (k > s.k0) {
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t v[32];
+              ptx::tmem_ld32(o_col + 32 * c, v);
+              ptx::tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * corr);
+              tmem_st32(o_col + 32 * c, v);
+            }
+          }
+        }
+        const float mu = m == -INFINITY ? 0.f : m;
+        const float c0 = b0 - mu + kShift, c1 = b1 - mu + kShift;
+        float sum0 = 0.f, sum1 = 0.f;
+        const int see0 = !masked ? kKeys : w0.w == 0.f ? -1 : limit - first, see1 = !masked ? kKeys : w1.w == 0.f ? -1 : limit - first;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t v[32], p[16];
+          ptx::tmem_ld32(s_col + 32 * c, v);
+          ptx::tmem_ld_wait();
+          if (!masked) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              const float x = exp2_fast(fmaf(__uint_as_float(v[j]), c < 2 ? a0 : a1, c < 2 ? c0 : c1));
+              const float y = exp2_fast(fmaf(__uint_as_float(v[j + 1]), c < 2 ? a0 : a1, c < 2 ? c0 : c1));
+              if (c < 2) sum0 += x + y; else sum1 += x + y;
+              p[j / 2] = pack_f16(x, y);
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              float x = exp2_fast(fmaf(__uint_as_float(v[j]), c < 2 ? a0 : a1, c < 2 ? c0 : c1));
+              float y = exp2_fast(fmaf(__uint_as_float(v[j + 1]), c < 2 ? a0 : a1, c < 2 ? c0 : c1));
+              x = 32 * c + j <= (c < 2 ? see0 : see1) ? x : 0.f;
+              y = 32 * c + j + 1 <= (c < 2 ? see0 : see1) ? y : 0.f;
+              if (c < 2) sum0 += x + y; else sum1 += x + y;
+              p[j / 2] = pack_f16(x, y);
+            }
+          }
+          tmem_st16(s_col + 16 * c, p);                    // over columns that have been read
+        }
+        l += (sum0 > 0.f ? sum0 * w0.z : sum0) + (sum1 > 0.f ? sum1 * w1.z : sum1);
+        tmem_st_wait();
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(bar(12 + t));
+      }
+      if (!ok) break;
+
+      // ---------------------------------------------------------------- leave the item
+      const bool none = m == -INFINITY && l == 0.f;        // a row that sees nothing (a NaN row has a NaN sum)
+      const bool whole = s.k0 == 0 && s.k1 == s.n;
+      if (s.k0 < s.k1) {
+        ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(14 + t), o_phase, abort_flag));
+        if (!ok) break;
+        o_phase ^= 1u;
+        ptx::tc_fence_after();
+      }
+      const float inv = none ? 0.f : 1.0f / l;
+      const int r = t * kTile + row_in_tile;
+      float* part = slot(blockIdx.x, s.at >= x0 ? 1 : 0);
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t v[32];
+        if (s.k0 < s.k1) {
+          ptx::tmem_ld32(o_col + 32 * c, v);
+          ptx::tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = 0u;
+        }
+        if (live && whole) {
+          uint4* to = reinterpret_cast<uint4*>(g.out + at * D + 32 * c);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t y[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const __nv_bfloat162 z = __floats2bfloat162_rn(none ? 0.f : __uint_as_float(v[8 * i + 2 * j]) * inv,
+                                                             none ? 0.f : __uint_as_float(v[8 * i + 2 * j + 1]) * inv);
+              y[j] = *reinterpret_cast<const uint32_t*>(&z);
+            }
+            to[i] = make_uint4(y[0], y[1], y[2], y[3]);
+          }
+        } else if (live) {
+          uint4* to = reinterpret_cast<uint4*>(part + 2 * kItemRows + (size_t)r * D + 32 * c);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) to[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        }
+        __syncwarp();
+      }
+      if (live && whole && g.lse != nullptr) g.lse[at] = none ? -INFINITY : kLn2 * (log2f(l) + m - kShift);
+      if (live && !whole) {
+        part[r] = m;
+        part[kItemRows + r] = l;
+      }
+      if (!whole && threadIdx.x == 0) {
+        Cut* c = &s_cut[s.at >= x0 ? 1 : 0];
+        c->at = s.at; c->len = s.len; c->b = s.b; c->h = s.h; c->tile = s.tile; c->n = s.n;
+      }
+      ptx::tc_fence_before();
+    }
+    if (!ok && lane == 0) report_status(a.hdr, TLQ_ERR_TIMEOUT, 230);
+  } else if (warp < kSoftWarps + kLoadWarps) {
+    // ------------------------------------------------------------------ codes of keys and values to f16 operands
+    const int lw = warp - kSoftWarps, lr = lane & 7, piece = lane >> 3;      // a warp takes 8 rows x 64 bytes at a time
+    constexpr int kNum = D / 16;                           // such pieces per warp of a key (or value) tile
+    int step = 0;
+    bool ok = true;
+    int64_t block[2];
+    uint4 kr[kNum], vr[kNum];
+    bool more = walk.next(a, g, s);
+    while (more && s.k0 >= s.k1) more = walk.next(a, g, s);
+    int k = more ? s.k0 : 0;
+    // the blocks of key tile k, and their steps (by two threads)
+    int phys[2];
+    auto look_up = [&]() {
+      const int n_blocks = (s.req.kv + kKvBlock - 1) / kKvBlock;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        phys[i] = 2 * k + i < n_blocks ? __ldg(a.block_table + (int64_t)s.b * a.max_blocks + 2 * k + i) : -1;
+    };
+    auto enter = [&](int at_step) {
+      const int n_blocks = (s.req.kv + kKvBlock - 1) / kKvBlock;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const bool in = 2 * k + i < n_blocks, bad = phys[i] < 0 || phys[i] >= a.n_blocks;
+        if (in && bad) report_status(a.hdr, TLQ_ERR_SHAPE, 231);
+        block[i] = (int64_t)(bad ? 0 : phys[i]) * a.n_kv + s.h;
+        if (lw == 0 && lane == i) {
+          const float vs = __ldg(a.v_steps + block[i]), v = vs < kStepFloor ? kStepFloor : vs;
+          s_steps[at_step & 3][i] = make_float4(__ldg(a.k_steps + block[i]), log2f(v), 1.0f / v, bad ? 0.f : 1.f);
+        }
+      }
+    };
+    // rows of a key tile: 16 groups of 8 tokens, D / 64 halves; of a value tile: 2 blocks of D / 8 groups of 8 channels
+    auto load_keys = [&]() {
+#pragma unroll
+      for (int i = 0; i < kNum; ++i) {
+        const int idx = lw + 4 * i, r = (idx / kPanels<D>) * 8 + lr, half = idx % kPanels<D>;
+        kr[i] = ld_cache(a.k_codes + block[r >> 6] * (kKvBlock * D) + (r & 63) * D + half * 64 + piece * 16);
+      }
+    };
+    auto load_values = [&]() {
+#pragma unroll
+      for (int i = 0; i < kNum; ++i) {
+        const int idx = lw + 4 * i, which = idx / (D / 8), r = (idx % (D / 8)) * 8 + lr;
+        vr[i] = ld_cache(a.v_codes + block[which] * (kKvBlock * D) + r * kKvBlock + piece * 16);
+      }
+    };
+    if (more) {
+      look_up();
+      enter(0);
+      load_keys();
+      load_values();
+    }
+    while (more && ok) {
+      // the tile after this one
+      int kn = k + 1;
+      bool after = true;
+      if (kn >= s.k1) {
+        do after = walk.next(a, g, s); while (after && s.k0 >= s.k1);
+        kn = s.k0;
+      }
+      k = kn;
+      if (after) look_up();
+      const int stage = step & 1;
+      const uint32_t parity = ((uint32_t)(step >> 1) & 1u) ^ 1u;
+      ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(4 + stage), parity, abort_flag));
+      if (!ok) break;
+#pragma unroll
+      for (int i = 0; i < kNum; ++i) {
+        const int idx = lw + 4 * i, r = (idx / kPanels<D>) * 8 + lr, half = idx % kPanels<D>;
+        const uint32_t to = k_at + stage * kKBytes<D> + half * (kKeys * 128) + r * 128;
+        uint32_t x[8];
+        keys_to_f16(kr[i].x, x[0], x[1]); keys_to_f16(kr[i].y, x[2], x[3]);
+        keys_to_f16(kr[i].z, x[4], x[5]); keys_to_f16(kr[i].w, x[6], x[7]);
+        sts128(to + (((2 * piece) ^ lr) << 4), x[0], x[1], x[2], x[3]);
+        sts128(to + (((2 * piece + 1) ^ lr) << 4), x[4], x[5], x[6], x[7]);
+      }
+      ptx::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(bar(2 + stage));
+      ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(8 + stage), parity, abort_flag));
+      if (!ok) break;
+#pragma unroll
+      for (int i = 0; i < kNum; ++i) {
+        const int idx = lw + 4 * i, which = idx / (D / 8), r = (idx % (D / 8)) * 8 + lr;
+        const uint32_t to = v_at + stage * kVBytes<D> + which * (D * 128) + r * 128;
+        uint32_t x[8];
+        values_to_f16(vr[i].x, x[0], x[1]); values_to_f16(vr[i].y, x[2], x[3]);
+        values_to_f16(vr[i].z, x[4], x[5]); values_to_f16(vr[i].w, x[6], x[7]);
+        sts128(to + (((2 * piece) ^ lr) << 4), x[0], x[1], x[2], x[3]);
+        sts128(to + (((2 * piece + 1) ^ lr) << 4), x[4], x[5], x[6], x[7]);
+      }
+      ptx::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(bar(6 + stage));
+      ++step;
+      more = after;
+      if (more) {
+        enter(step);
+        load_keys();
+        load_values();
+      }
+    }
+    if (!ok && lane == 0) report_status(a.hdr, TLQ_ERR_TIMEOUT, 232);
+  } else if (lane == 0) {
+    // ------------------------------------------------------------------ products
+    constexpr uint32_t kIdescS = ptx::make_idesc(1, 0, kTile, kKeys, false);   // f16 x f16 -> f32
+    constexpr uint32_t kIdescO = ptx::make_idesc(1, 0, kTile, D, false);
+    int step = 0;
+    uint32_t q_phase = 0, p_phase = 0;
+    bool ok = true;
+    auto wait = [&](int i, uint32_t parity) {
+      ok = ok && ptx::mbar_wait(bar(i), parity, abort_flag);
+      ptx::tc_fence_after();
+    };
+    auto scores = [&](int t, int st) {
+#pragma unroll
+      for (uint32_t c = 0; c < kPanels<D>; ++c) {
+        const uint64_t x = ptx::smem_desc_sw128(q_at + t * kQBytes<D> + c * (kTile * 128));
+        const uint64_t y = ptx::smem_desc_sw128(k_at + (st & 1) * kKBytes<D> + c * (kKeys * 128));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mma_f16_ss(tmem + t * kTile, x + 2 * i, y + 2 * i, kIdescS, c > 0 || i > 0);
+      }
+      ptx::mma_commit(bar(10 + t));
+    };
+    while (ok && walk.next(a, g, s)) {
+      if (s.k0 >= s.k1) continue;
+      for (int t = 0; t < 2; ++t) wait(t, q_phase);
+      q_phase ^= 1u;
+      wait(2 + (step & 1), (uint32_t)(step >> 1) & 1u);
+      if (!ok) break;
+      scores(0, step);
+      scores(1, step);
+      ptx::mma_commit(bar(4 + (step & 1)));
+      for (int k = s.k0; k < s.k1 && ok; ++k, ++step) {
+        const int stage = step & 1;
+        wait(6 + stage, (uint32_t)(step >> 1) & 1u);
+        const bool next = k + 1 < s.k1;
+        for (int t = 0; t < 2 && ok; ++t) {
+          wait(12 + t, p_phase);
+          if (!ok) break;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const uint64_t y = ptx::smem_desc_sw128(v_at + stage * kVBytes<D> + c * (D * 128));
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              mma_f16_ts(tmem + 256 + t * kTile, tmem + t * kTile + 32 * c + 8 * i, y + 2 * i, kIdescO, k > s.k0 || c > 0 || i > 0);
+          }
+          if (next) {
+            if (t == 0) wait(2 + ((step + 1) & 1), (uint32_t)((step + 1) >> 1) & 1u);
+            if (!ok) break;
+            scores(t, step + 1);
+          } else {
+            ptx::mma_commit(bar(14 + t));
+          }
+        }
+        if (!ok) break;
+        ptx::mma_commit(bar(8 + stage));
+        if (next) ptx::mma_commit(bar(4 + ((step + 1) & 1)));
+        p_phase ^= 1u;
+      }
+    }
+    if (!ok) report_status(a.hdr, TLQ_ERR_TIMEOUT, 233);
+  }
+  __syncwarp();
+  if (*abort_flag != 0)
+    for (int i = 0; i < 1000; ++i) __nanosleep(1000);      // products under way end before their memory is given back
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (warp == 12) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc(tmem, 512);
+  }
+  if (*abort_flag != 0) return;
+
+  // ------------------------------------------------------------------ join the CTAs that share an item
+  if (threadIdx.x < 2) {
+    const Cut c = s_cut[threadIdx.x];
+    s_join[threadIdx.x] = 0;
+    if (c.len > 0) {
+      int k0, k1;
+      walk.cut(x0, x1, c.at, c.len, c.n, k0, k1);
+      int32_t* counter = g.split.counters + worker_of(c.at);
+      __threadfence();                                     // the CTA's partials, which the barrier has ordered before this
+      const int before = atomicAdd(counter, k1 - k0);      // key tiles of the item that are done
+      if (before + (k1 - k0) == c.n) {
+        *counter = 0;
+        s_join[threadIdx.x] = 1;
+      }
+      __threadfence();
+    }
+  }
+  __syncthreads();
+  for (int i = 0; i < 2; ++i) {
+    if (!s_join[i]) continue;
+    const Cut c = s_cut[i];
+    const Request req = load_request(a, c.b);
+    const long long rows = (long long)req.q_len * a.group;
+    const long long first = worker_of(c.at), final = worker_of(c.at + c.len - 1);
+    for (int e = threadIdx.x; e < kItemRows * (D / 4); e += kThreads) {
+      const int r = e / (D / 4), d = (e % (D / 4)) * 4;
+      const int row = c.tile * kItemRows + r;
+      if (row >= rows) break;
+      float mm = -INFINITY, den = 0.f;
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (long long w = first; w <= final; ++w) {
+        int k0, k1;
+        walk.cut(edge(w), edge(w + 1), c.at, c.len, c.n, k0, k1);
+        if (k0 >= k1) continue;
+        const float* p = slot(w, c.at >= edge(w) ? 1 : 0);
+        const float m = __ldcg(p + r), l = __ldcg(p + kItemRows + r);
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(p + 2 * kItemRows) + e);
+        const float mn = fmaxf(mm, m), mu = mn == -INFINITY ? 0.f : mn;
+        const float f = exp2_fast(mm - mu), h = exp2_fast(m - mu);
+        mm = mn;
+        den = den * f + l * h;
+        sum.x = sum.x * f + v.x * h; sum.y = sum.y * f + v.y * h;
+        sum.z = sum.z * f + v.z * h; sum.w = sum.w * f + v.w * h;
+      }
+      const int64_t at = (int64_t)(req.q0 + row / a.group) * a.n_heads + c.h * a.group + row % a.group;
+      const bool none = mm == -INFINITY && den == 0.f;
+      const float inv = none ? 0.f : 1.0f / den;
+      const __nv_bfloat162 y0 = __floats2bfloat162_rn(none ? 0.f : sum.x * inv, none ? 0.f : sum.y * inv);
+      const __nv_bfloat162 y1 = __floats2bfloat162_rn(none ? 0.f : sum.z * inv, none ? 0.f : sum.w * inv);
+      *reinterpret_cast<uint2*>(g.out + at * D + d) =
+          make_uint2(*reinterpret_cast<const uint32_t*>(&y0), *reinterpret_cast<const uint32_t*>(&y1));
+      if (d == 0 && g.lse != nullptr) g.lse[at] = none ? -INFINITY : kLn2 * (log2f(den) + mm - kShift);
+    }
+  }
+}
+
+template <int D>
+int launch(const KvArgs& a, const PromptArgs& g, cudaStream_t st) {
+  static OncePerDevice once;
+  const int rc = once_per_device(once, [] {
+    return cudaFuncSetAttribute(kv_prompt_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem<D>);
+  });
+  if (rc != TLQ_OK) return rc;
+  const int sms = device_sm_count();
+  if (sms <= 0) return TLQ_ERR_CUDA;
+  kv_prompt_kernel<D><<<sms < kMaxWorkers ? sms : kMaxWorkers, kThreads, kSmem<D>, st>>>(a, g);
+  return after_launch();
+}
+
+}  // namespace
+
+int launch_kv_prompt(const uint16_t* q, int64_t ldq, int head_dim, const KvArgs& a, float scale, int causal, int min_rows,
+                     uint16_t* out, float* lse, const KvSplit& split, cudaStream_t st) {
+  PromptArgs g{};
+  g.q = q; g.ldq = ldq; g.out = out; g.lse = lse;
+  g.scale_log2 = scale * kLog2e;
+  g.causal = causal;
+  g.min_rows = min_rows;
+  g.split = split;
+  return head_dim == 128 ? launch<128>(a, g, st) : launch<64>(a, g, st);
+}
+
+}  // namespace tlq

@@ -112,13 +112,19 @@ int launch_kv_store(const uint16_t* qkv, int64_t ld, int head_dim, const KvArgs&
 constexpr int kMaxWorkers = 160;          // CTAs that share one call's work (one per SM)
 constexpr int kSplitWarps = 8;            // warps of one of them
 constexpr int kMaxRowTile = 16;           // query rows of one work item
-inline size_t kv_split_floats(int head_dim) {          // two partials of every warp and of every CTA
-  return (size_t)kMaxWorkers * 2 * (kSplitWarps + 1) * kMaxRowTile * ((size_t)head_dim + 2);
+constexpr int kPromptItemRows = 256;      // query rows of one item of the prompt kernel (kv_prompt.cu)
+constexpr int kPromptRows = 64;           // requests with at least this many query rows per kv head go to it
+inline size_t kv_split_floats(int head_dim, int64_t rows) {   // two partials of every warp and of every CTA
+  const size_t few = (size_t)kMaxWorkers * 2 * (kSplitWarps + 1) * kMaxRowTile * ((size_t)head_dim + 2);
+  const size_t many = (size_t)kMaxWorkers * 2 * kPromptItemRows * ((size_t)head_dim + 2);
+  return rows >= kPromptRows && many > few ? many : few;
 }
 struct KvSplit {
   int32_t* counters;          // [kMaxWorkers]
   float* partials;            // kv_split_floats()
 };
+int launch_kv_prompt(const uint16_t* q, int64_t ldq, int head_dim, const KvArgs& a, float scale, int causal, int min_rows,
+                     uint16_t* out, float* lse, const KvSplit& split, cudaStream_t st);
 int launch_kv_attention(const uint16_t* q, int64_t ldq, int head_dim, const KvArgs& a, float scale, int causal,
                         uint16_t* out, float* lse, const KvSplit& split, cudaStream_t st);
 

@@ -31,6 +31,12 @@ int check_heads(int32_t n_heads, const tlq_kv_cache* c) {
   return n_heads >= 1 && n_heads <= 65536 && n_heads % c->n_kv_heads == 0 ? TLQ_OK : TLQ_ERR_SHAPE;
 }
 
+// Query rows of one request and kv head, at most.
+int64_t query_rows(const tlq_kv_cache* c, const tlq_kv_batch* b, int32_t n_heads, int64_t T) {
+  const int64_t n = T < b->max_q_len ? T : b->max_q_len;
+  return n * (n_heads / c->n_kv_heads);
+}
+
 KvArgs make_args(const tlq_kv_cache* c, const tlq_kv_batch* b, int32_t n_heads, int64_t T, void* workspace) {
   KvArgs a{};
   a.k_codes = c->k_codes; a.v_codes = c->v_codes; a.k_steps = c->k_steps; a.v_steps = c->v_steps;
@@ -70,7 +76,7 @@ int tlq_linear_i8(const int8_t* Xq, const float* t, int64_t N, int64_t C1, const
 
 size_t tlq_kv_workspace_bytes(const tlq_kv_cache* cache, const tlq_kv_batch* batch, int32_t n_heads, int64_t T) {
   if (check_cache(cache) != TLQ_OK || check_batch(batch) != TLQ_OK || check_heads(n_heads, cache) != TLQ_OK || T < 0) return 0;
-  return align_up(kHeaderBytes + kCounterBytes + kv_split_floats(cache->head_dim) * sizeof(float), 256);
+  return align_up(kHeaderBytes + kCounterBytes + kv_split_floats(cache->head_dim, query_rows(cache, batch, n_heads, T)) * sizeof(float), 256);
 }
 
 int tlq_kv_store(const void* qkv, int64_t T, int64_t ld, int32_t n_heads, const tlq_kv_cache* cache,
@@ -126,7 +132,7 @@ int tlq_kv_attention(const void* q, int64_t T, int64_t ldq, int32_t n_heads, con
   if (rc == TLQ_OK) rc = check_batch(batch);
   if (rc == TLQ_OK) rc = check_heads(n_heads, cache);
   if (rc != TLQ_OK) return rc;
-  if (T < 0 || T > 0x7FFFFF00LL) return TLQ_ERR_SHAPE;
+  if (T < 0 || T > 0x7FFFFF00LL || T * (n_heads / cache->n_kv_heads) > 0x7FFFFF00LL) return TLQ_ERR_SHAPE;
   if (workspace == nullptr) return TLQ_ERR_INVALID_ARG;
   if (T > 0 && (q == nullptr || out == nullptr)) return TLQ_ERR_INVALID_ARG;
   if (ldq < (int64_t)n_heads * cache->head_dim || (ldq % 8) != 0) return TLQ_ERR_SHAPE;

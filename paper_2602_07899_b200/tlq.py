@@ -8,6 +8,7 @@ raises if it has not been built: there is no fallback implementation.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -157,8 +158,15 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
+# the raw handle of the current stream, without a Stream object (a microsecond per call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
+        if _raw_stream is not None and _raw_device is not None:
+            return _raw_stream(_raw_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
@@ -326,8 +334,11 @@ def tlq_apply_layer(X: torch.Tensor, W: torch.Tensor, s: Optional[torch.Tensor],
 # word of their workspace with tlq_read_status when a step's results are fetched.
 
 
+_I8, _I32, _F32, _BF16 = torch.int8, torch.int32, torch.float32, torch.bfloat16
+
+
 def _typed(t: torch.Tensor, dtype: torch.dtype, shape, what: str) -> torch.Tensor:
-    if t.dtype != dtype or t.shape != shape:
+    if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous")
@@ -336,13 +347,14 @@ def _typed(t: torch.Tensor, dtype: torch.dtype, shape, what: str) -> torch.Tenso
 
 def _rows(t: torch.Tensor, what: str) -> int:
     """Row pitch in elements of a bf16 tensor whose rows are contiguous."""
-    if t.dtype != torch.bfloat16:
+    if t.dtype is not _BF16:
         raise ValueError(f"{what} must be torch.bfloat16, got {t.dtype}")
+    if t.is_contiguous():
+        return t.shape[1] if t.ndim == 2 else t.shape[1] * t.shape[2]
     inner = t.shape[-1]
-    if t.stride(-1) != 1 or (t.dim() == 3 and t.shape[1] > 1 and t.stride(1) != inner):
+    if t.stride(-1) != 1 or (t.ndim == 3 and t.shape[1] > 1 and t.stride(1) != inner):
         raise ValueError(f"{what}: the heads and channels of a token must be contiguous")
-    width = t.shape[1:].numel()
-    return t.stride(0) if t.shape[0] > 1 else width
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1:].numel()
 
 
 class KvCache:
@@ -359,6 +371,7 @@ class KvCache:
         self.n_blocks, self.n_kv_heads, self.head_dim, self.device = blocks, heads, dim, k_codes.device
         self._c = _KvCacheStruct(ctypes.sizeof(_KvCacheStruct), heads, dim, blocks, k_codes.data_ptr(), v_codes.data_ptr(),
                                  k_steps.data_ptr(), v_steps.data_ptr())
+        self._p = ctypes.addressof(self._c)
 
     @classmethod
     def empty(cls, n_blocks: int, n_kv_heads: int, head_dim: int, device) -> "KvCache":
@@ -380,6 +393,23 @@ class KvBatch:
         self.cu_q, self.kv_len, self.block_table, self.max_q_len = cu_q, kv_len, block_table, int(max_q_len)
         self._c = _KvBatchStruct(ctypes.sizeof(_KvBatchStruct), n, self.max_q_len, block_table.shape[1], cu_q.data_ptr(),
                                  kv_len.data_ptr(), block_table.data_ptr())
+        self._p = ctypes.addressof(self._c)
+
+
+def _by_address(name: str):
+    """The call with its structures passed as addresses, which ctypes converts faster than structure objects."""
+    typed, fn = getattr(lib, name), lib[name]
+    fn.restype = typed.restype
+    fn.argtypes = [ctypes.c_void_p if hasattr(t, "_type_") and hasattr(t, "contents") else t for t in typed.argtypes]
+    return fn
+
+
+_kv_store, _kv_attention = _by_address("tlq_kv_store"), _by_address("tlq_kv_attention")
+
+
+@functools.lru_cache(maxsize=64)
+def _host_ints(values: tuple):
+    return (ctypes.c_int32 * len(values))(*values)
 
 
 def linear_workspace(N: int, C1: int, C2: int, device) -> torch.Tensor:
@@ -402,22 +432,27 @@ def tlq_linear_i8(Xq: torch.Tensor, t: torch.Tensor, Wq: torch.Tensor, u: torch.
                   workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Xq int8 [N,C1] with steps t [N], Wq int8 [C2,C1] with steps u [C2], bias bf16 [C2] or None -> bf16 [N,C2]."""
     N, C1 = Xq.shape
-    C2 = Wq.shape[0]
-    _typed(Xq, torch.int8, (N, C1), "Xq")
-    _typed(Wq, torch.int8, (C2, C1), "Wq")
-    _typed(t, torch.float32, (N,), "t")
-    _typed(u, torch.float32, (C2,), "u")
+    C2, W1 = Wq.shape
+    if (W1 != C1 or Xq.dtype is not _I8 or Wq.dtype is not _I8 or t.dtype is not _F32 or u.dtype is not _F32 or t.ndim != 1
+            or u.ndim != 1 or t.numel() != N or u.numel() != C2 or not Xq.is_contiguous() or not Wq.is_contiguous()
+            or not t.is_contiguous() or not u.is_contiguous()):
+        _typed(Xq, _I8, (N, C1), "Xq")
+        _typed(Wq, _I8, (C2, C1), "Wq")
+        _typed(t, _F32, (N,), "t")
+        _typed(u, _F32, (C2,), "u")
     if bias is not None:
-        _typed(bias, torch.bfloat16, (C2,), "bias")
+        _typed(bias, _BF16, (C2,), "bias")
     if workspace is None:
         workspace = linear_workspace(N, C1, C2, Xq.device)
     if out is None:
-        out = torch.empty((N, C2), dtype=torch.bfloat16, device=Xq.device)
+        out = Xq.new_empty((N, C2), dtype=_BF16)
     else:
-        _typed(out, torch.bfloat16, (N, C2), "out")
-    _check(lib.tlq_linear_i8(Xq.data_ptr(), t.data_ptr(), N, C1, Wq.data_ptr(), u.data_ptr(), C2,
-                             None if bias is None else bias.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                             out.data_ptr(), _stream(stream)), "tlq_linear_i8")
+        _typed(out, _BF16, (N, C2), "out")
+    status = lib.tlq_linear_i8(Xq.data_ptr(), t.data_ptr(), N, C1, Wq.data_ptr(), u.data_ptr(), C2,
+                               None if bias is None else bias.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                               out.data_ptr(), _stream(stream))
+    if status:
+        raise TlqError(status, "tlq_linear_i8")
     return out
 
 
@@ -435,8 +470,8 @@ def tlq_kv_store(qkv: torch.Tensor, n_heads: int, cache: KvCache, batch: KvBatch
         raise ValueError("qkv must be [T, (n_heads + 2 * n_kv_heads) * head_dim]")
     axes, sec, limit = 1, None, 0
     if positions is not None:
-        axes = 1 if positions.dim() == 1 else positions.shape[0]
-        _typed(positions, torch.int32, (T,) if positions.dim() == 1 else (axes, T), "positions")
+        axes = 1 if positions.ndim == 1 else positions.shape[0]
+        _typed(positions, _I32, (T,) if positions.ndim == 1 else (axes, T), "positions")
         if cos_sin is None:
             raise ValueError("positions need cos_sin")
         limit = cos_sin.shape[0]
@@ -444,18 +479,18 @@ def tlq_kv_store(qkv: torch.Tensor, n_heads: int, cache: KvCache, batch: KvBatch
         if sections is not None:
             if len(sections) != axes:
                 raise ValueError("one section for each position axis")
-            sec = (ctypes.c_int32 * axes)(*sections)
-    for w, what in ((q_norm, "q_norm"), (k_norm, "k_norm")):
-        if w is not None:
-            _typed(w, torch.bfloat16, (d,), what)
+            sec = _host_ints(tuple(sections))
+    if q_norm is not None:
+        _typed(q_norm, _BF16, (d,), "q_norm")
+    if k_norm is not None:
+        _typed(k_norm, _BF16, (d,), "k_norm")
     if workspace is None:
         workspace = kv_workspace(cache, n_heads, T, batch)
-    q = torch.empty((T, n_heads, d), dtype=torch.bfloat16, device=qkv.device)
+    q = qkv.new_empty((T, n_heads, d))
     k = v = None
     if want_values:
-        k = torch.empty((T, cache.n_kv_heads, d), dtype=torch.bfloat16, device=qkv.device)
-        v = torch.empty_like(k)
-    _check(lib.tlq_kv_store(qkv.data_ptr(), T, ld, n_heads, cache._c, batch._c,
+        k, v = qkv.new_empty((T, cache.n_kv_heads, d)), qkv.new_empty((T, cache.n_kv_heads, d))
+    _check(_kv_store(qkv.data_ptr(), T, ld, n_heads, cache._p, batch._p,
                             None if positions is None else positions.data_ptr(), axes, sec,
                             None if cos_sin is None else cos_sin.data_ptr(), limit,
                             None if q_norm is None else q_norm.data_ptr(), None if k_norm is None else k_norm.data_ptr(),
@@ -474,9 +509,9 @@ def tlq_kv_attention(q: torch.Tensor, cache: KvCache, batch: KvBatch, scale: flo
     ldq = _rows(q, "q")
     if workspace is None:
         workspace = kv_workspace(cache, n_heads, T, batch)
-    out = torch.empty((T, n_heads, d), dtype=torch.bfloat16, device=q.device)
-    lse = torch.empty((T, n_heads), dtype=torch.float32, device=q.device) if want_lse else None
-    _check(lib.tlq_kv_attention(q.data_ptr(), T, ldq, n_heads, cache._c, batch._c, scale, 1 if causal else 0,
+    out = q.new_empty((T, n_heads, d))
+    lse = q.new_empty((T, n_heads), dtype=_F32) if want_lse else None
+    _check(_kv_attention(q.data_ptr(), T, ldq, n_heads, cache._p, batch._p, scale, 1 if causal else 0,
                                 workspace.data_ptr(), workspace.numel(), out.data_ptr(),
                                 None if lse is None else lse.data_ptr(), _stream(stream)), "tlq_kv_attention")
     return out, lse
