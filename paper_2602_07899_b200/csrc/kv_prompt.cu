@@ -12,6 +12,8 @@
 //   warps 8..11       bring the codes of keys and values from the cache into registers, turn them into f16 and lay them
 //                     out for the tensor core (128-byte swizzle); two stages each
 //   warp 12           issues the products
+//   warp 13           finds the parts of items that this CTA works on and passes them on through a ring (14 and 15 idle:
+//                     registers are shared out by groups of four warps)
 // Work is cut as in the few-row kernel: items (row tiles of a kv head) lie on one line, weighted by their cached tokens,
 // every CTA takes an equal part of it; an item that is cut leaves partial sums, and the CTA that completes it joins them.
 //
@@ -25,7 +27,9 @@ namespace {
 
 constexpr int kTile = 128, kItemRows = 256, kKeys = 128;
 constexpr int kSoftWarps = 8, kLoadWarps = 4;
-constexpr int kThreads = (kSoftWarps + kLoadWarps + 1) * 32;
+constexpr int kThreads = 512;                              // four warpgroups; of the last one a single warp works
+// registers of a thread of each role: 2 x 176 + 112 + 48 = 4 x 128, what the block is launched with
+constexpr int kSoftRegs = 176, kLoadRegs = 112, kIssueRegs = 48;
 constexpr float kShift = 11.f, kGrow = 4.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kStepFloor = 7.8886090522101181e-31f;      // 2^-100, as in kv_attention.cu
@@ -119,6 +123,32 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
         "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
+// The wait for loads of tensor memory, naming 32 of the registers that they fill: no use of those can move before it.
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
+                 "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
+                 "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
+}
+__device__ __forceinline__ float as_f(uint32_t x) { return __uint_as_float(x); }
+template <int N>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+// two 32-bit sums or products in one instruction
+__device__ __forceinline__ void fma2(float& x, float& y, float a, float bx, float by, float c) {
+  asm("{\n\t.reg .b64 p, q, r, s;\n\t"
+      "mov.b64 p, {%2, %2};\n\tmov.b64 q, {%3, %4};\n\tmov.b64 r, {%5, %5};\n\t"
+      "fma.rn.f32x2 s, q, p, r;\n\tmov.b64 {%0, %1}, s;\n\t}"
+      : "=f"(x), "=f"(y) : "f"(a), "f"(bx), "f"(by), "f"(c));
+}
+__device__ __forceinline__ void add2(float& x, float& y, float a, float b) {
+  asm("{\n\t.reg .b64 p, q;\n\t"
+      "mov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\t"
+      "add.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}"
+      : "+f"(x), "+f"(y) : "f"(a), "f"(b));
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // ---------------------------------------------------------------------------------------------- the line of work
@@ -138,12 +168,20 @@ __device__ __forceinline__ Costs costs_of(const KvArgs& a, const PromptArgs& g, 
   return c;
 }
 
-// A part of an item: key tiles [k0, k1) of n.
-struct Segment {
-  int b, h, tile, k0, k1, n;
+// A part of an item: key tiles [k0, k1) of n; k0 < 0: there are no more.
+struct __align__(16) Segment {
+  int b, h, tile, k0;
+  int k1, n, q0, q_len;
   long long at, len;            // the item on the line
-  Request req;
+  int kv, pad[3];
 };
+constexpr int kRing = 4;        // segments in the ring
+
+// The key tiles [k0, k1) of an item (n of them, at `at` of the line) that the part [from, to) of the line holds.
+__device__ __forceinline__ void cut(long long from, long long to, long long at, long long len, int n, int& k0, int& k1) {
+  k0 = from <= at ? 0 : from >= at + len ? n : (int)((long long)n * (from - at) / len);
+  k1 = to >= at + len ? n : to <= at ? 0 : (int)((long long)n * (to - at) / len);
+}
 
 // Walks the items that overlap [x0, x1) of the line.
 struct Walk {
@@ -174,11 +212,6 @@ struct Walk {
     }
     tile = lo;
   }
-  // the part of the current item in [from, to)
-  __device__ __forceinline__ void cut(long long from, long long to, long long at, long long len, int n, int& k0, int& k1) const {
-    k0 = from <= at ? 0 : from >= at + len ? n : (int)((long long)n * (from - at) / len);
-    k1 = to >= at + len ? n : to <= at ? 0 : (int)((long long)n * (to - at) / len);
-  }
   // next part with something to do; false at the end
   __device__ __forceinline__ bool next(const KvArgs& a, const PromptArgs& g, Segment& s) {
     while (true) {
@@ -196,7 +229,7 @@ struct Walk {
       s.len = costs.sum(tile + 1) - costs.sum(tile);
       s.n = key_tiles(a, g);
       cut(x0, x1, s.at, s.len, s.n, s.k0, s.k1);
-      s.b = b; s.h = h; s.tile = tile; s.req = req;
+      s.b = b; s.h = h; s.tile = tile; s.q0 = req.q0; s.q_len = req.q_len; s.kv = req.kv;
       const bool here = s.n == 0 ? s.at >= x0 : s.k0 < s.k1;   // an item without visible keys belongs to whoever has its start
       ++tile;
       if (here) return true;
@@ -215,7 +248,8 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t q_at = base, k_at = q_at + 2 * kQBytes<D>, v_at = k_at + 2 * kKBytes<D>;
-  __shared__ __align__(8) uint64_t bars[16];
+  __shared__ __align__(8) uint64_t bars[16 + 2 * kRing];
+  __shared__ Segment s_ring[kRing];
   __shared__ __align__(16) float4 s_steps[4][2];           // of the two blocks of a key tile: kstep, log2 vstep, 1 / vstep, usable
   __shared__ long long sums[kThreads / 32];
   __shared__ Found found;
@@ -224,7 +258,8 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
   __shared__ int s_abort, s_join[2];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   auto bar = [&](int i) { return ptx::smem_u32(&bars[i]); };
-  // [0,2) q ready, [2,4) k ready, [4,6) k free, [6,8) v ready, [8,10) v free, [10,12) S ready, [12,14) P ready, [14,16) O ready
+  // [0,2) q ready, [2,4) k ready, [4,6) k free, [6,8) v ready, [8,10) v free, [10,12) S ready, [12,14) P ready, [14,16) O ready,
+  // then the ring of segments: ready, free
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(bar(i), 4);
@@ -236,6 +271,10 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       ptx::mbar_init(bar(12 + i), 4);
       ptx::mbar_init(bar(14 + i), 1);
       s_cut[i].len = 0;
+    }
+    for (int i = 0; i < kRing; ++i) {
+      ptx::mbar_init(bar(16 + i), 1);
+      ptx::mbar_init(bar(16 + kRing + i), kSoftWarps + kLoadWarps + 1);
     }
     s_abort = 0;
     ptx::fence_barrier_init();
@@ -263,8 +302,6 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
   const long long x0 = edge(blockIdx.x), x1 = edge(blockIdx.x + 1);
   if (x0 >= x1) return;
   if (!locate_item<kThreads>(a.B, x0, cost_of, sums, &found)) return;
-  Walk walk;
-  walk.start(a, g, found.request, found.rest, x0, x1);
   if (warp == 12) ptx::tmem_alloc(ptx::smem_u32(&s_tmem), 512);
   ptx::tc_fence_before();
   __syncthreads();
@@ -273,9 +310,20 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
   float* const partials = g.split.partials;
   constexpr size_t kPitch = (size_t)kItemRows * (D + 2);   // floats of a partial: maxima, sums, output sums
   auto slot = [&](long long w, int i) { return partials + ((size_t)w * 2 + i) * kPitch; };
-  Segment s;
+  // the next segment, by all lanes of a warp (or the one that issues)
+  int seg = 0;
+  uint32_t seg_phase = 0;
+  auto next_segment = [&](bool& ok) {
+    ok = ptx::mbar_wait(bar(16 + seg), seg_phase, abort_flag);
+    return &s_ring[seg];
+  };
+  auto done_segment = [&]() {                              // its fields have been read
+    ptx::mbar_arrive(bar(16 + kRing + seg));
+    if (++seg == kRing) { seg = 0; seg_phase ^= 1u; }
+  };
 
   if (warp < kSoftWarps) {
+    more_registers<kSoftRegs>();
     // ------------------------------------------------------------------ softmax: a thread is a row
     const int t = warp >> 2, row_in_tile = (warp & 3) * 32 + lane;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -284,16 +332,28 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     uint32_t s_phase = 0, o_phase = 0;
     int step = 0;                                          // key tiles so far, of all segments
     bool ok = true;
-    while (ok && walk.next(a, g, s)) {
+    while (true) {
+      const Segment* from = next_segment(ok);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok) break;
+      struct { int b, h, tile, k0, k1, n, q0, q_len, kv; bool starts; } s = {from->b, from->h, from->tile, from->k0, from->k1,
+                                                               from->n, from->q0, from->q_len, from->kv, from->at >= x0};
+      if (threadIdx.x == 0 && s.k0 >= 0 && (s.k0 > 0 || s.k1 < s.n)) {
+        Cut* c = &s_cut[s.starts ? 1 : 0];
+        c->at = from->at; c->len = from->len; c->b = s.b; c->h = s.h; c->tile = s.tile; c->n = s.n;
+      }
+      __syncwarp();
+      if (lane == 0) done_segment(); else if (++seg == kRing) { seg = 0; seg_phase ^= 1u; }
+      if (s.k0 < 0) break;
       const int row = s.tile * kItemRows + t * kTile + row_in_tile;
-      const long long rows = (long long)s.req.q_len * a.group;
+      const long long rows = (long long)s.q_len * a.group;
       const bool live = row < rows;
-      const int limit = !live ? -1 : g.causal ? min(s.req.kv - s.req.q_len + row / a.group, s.req.kv - 1) : s.req.kv - 1;
-      const int64_t at = live ? (int64_t)(s.req.q0 + row / a.group) * a.n_heads + s.h * a.group + row % a.group : 0;
+      const int limit = !live ? -1 : g.causal ? min(s.kv - s.q_len + row / a.group, s.kv - 1) : s.kv - 1;
+      const int64_t at = live ? (int64_t)(s.q0 + row / a.group) * a.n_heads + s.h * a.group + row % a.group : 0;
       // the row of q: a power of two brings it into the range of f16
       float fac = 0.f, off = 0.f;
       if (s.k0 < s.k1) {
-        const uint16_t* p = g.q + (live ? (int64_t)(s.req.q0 + row / a.group) * g.ldq + (int64_t)(s.h * a.group + row % a.group) * D : 0);
+        const uint16_t* p = g.q + (live ? (int64_t)(s.q0 + row / a.group) * g.ldq + (int64_t)(s.h * a.group + row % a.group) * D : 0);
         uint4 v[D / 8];
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) v[i] = live ? __ldg(reinterpret_cast<const uint4*>(p) + i) : make_uint4(0, 0, 0, 0);
@@ -335,38 +395,46 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
         s_phase ^= 1u;
         ptx::tc_fence_after();
         const float4 w0 = s_steps[step & 3][0], w1 = s_steps[step & 3][1];
-        const float a0 = fac * w0.x, a1 = fac * w1.x;
-        const float b0 = fmaf(-off, a0, w0.y), b1 = fmaf(-off, a1, w1.y);
+        float a0 = fac * w0.x, a1 = fac * w1.x;
+        float b0 = fmaf(-off, a0, w0.y), b1 = fmaf(-off, a1, w1.y);
         const int first = k * kKeys;                       // place of the tile's first key
         const bool masked = __any_sync(0xFFFFFFFFu, first + kKeys - 1 > limit) || w0.w == 0.f || w1.w == 0.f;
-        float top = -INFINITY;
-        if (!masked) {
-          float r0 = -INFINITY, r1 = -INFINITY;
+        uint32_t v[4][32];                                 // the row of S
+        ptx::tmem_ld32(s_col, v[0]);
+        ptx::tmem_ld32(s_col + 32, v[1]);
+        tmem_ld_wait_for(v[0]);
+        tmem_ld_wait_for(v[1]);
+        ptx::tmem_ld32(s_col + 64, v[2]);
+        ptx::tmem_ld32(s_col + 96, v[3]);
+        if (masked) {                                      // t itself, with nothing where there is nothing to see
+          tmem_ld_wait_for(v[2]);
+          tmem_ld_wait_for(v[3]);
+          const int see0 = w0.w == 0.f ? -1 : limit - first, see1 = w1.w == 0.f ? -1 : limit - first;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t v[32];
-            ptx::tmem_ld32(s_col + 32 * c, v);
-            ptx::tmem_ld_wait();
+          for (int c = 0; c < 4; ++c)
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-              if (c < 2) r0 = fmaxf(r0, __uint_as_float(v[j])); else r1 = fmaxf(r1, __uint_as_float(v[j]));
+              const float x = fmaf(as_f(v[c][j]), c < 2 ? a0 : a1, c < 2 ? b0 : b1);
+              v[c][j] = __float_as_uint(32 * c + j <= (c < 2 ? see0 : see1) ? x : -INFINITY);
             }
+          a0 = a1 = 1.f;
+          b0 = b1 = 0.f;
+        }
+        float r[2][4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          if (c == 2) {
+            tmem_ld_wait_for(v[2]);
+            tmem_ld_wait_for(v[3]);
           }
-          top = fmaxf(fmaf(r0, a0, b0), fmaf(r1, a1, b1));
-        } else {
-          const int see0 = w0.w == 0.f ? -1 : min(limit - first, kKeys - 1), see1 = w1.w == 0.f ? -1 : min(limit - first, kKeys - 1);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t v[32];
-            ptx::tmem_ld32(s_col + 32 * c, v);
-            ptx::tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const float x = fmaf(__uint_as_float(v[j]), c < 2 ? a0 : a1, c < 2 ? b0 : b1);
-              top = 32 * c + j <= (c < 2 ? see0 : see1) ? fmaxf(top, x) : top;
-            }
+          for (int j = 0; j < 32; ++j) {
+            float& x = r[c >> 1][j & 3];
+            x = (c & 1) == 0 && j < 4 ? as_f(v[c][j]) : fmaxf(x, as_f(v[c][j]));
           }
         }
+        const float top = fmaxf(fmaf(fmaxf(fmaxf(r[0][0], r[0][1]), fmaxf(r[0][2], r[0][3])), a0, b0),
+                                fmaf(fmaxf(fmaxf(r[1][0], r[1][1]), fmaxf(r[1][2], r[1][3])), a1, b1));
         // a maximum that has grown by more than kGrow: the output sum follows
         const bool grow = top > m + kGrow || (m == -INFINITY && top > -INFINITY);
         if (__any_sync(0xFFFFFFFFu, grow)) {
@@ -376,47 +444,35 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
           l *= corr;
           if (k > s.k0) {
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-              uint32_t v[32];
-              ptx::tmem_ld32(o_col + 32 * c, v);
+            for (int c = 0; c < D / 16; ++c) {
+              uint32_t x[16];
+              ptx::tmem_ld16(o_col + 16 * c, x);
               ptx::tmem_ld_wait();
 #pragma unroll
-              for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * corr);
-              tmem_st32(o_col + 32 * c, v);
+              for (int j = 0; j < 16; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * corr);
+              tmem_st16(o_col + 16 * c, x);
             }
           }
         }
         const float mu = m == -INFINITY ? 0.f : m;
         const float c0 = b0 - mu + kShift, c1 = b1 - mu + kShift;
-        float sum0 = 0.f, sum1 = 0.f;
-        const int see0 = !masked ? kKeys : w0.w == 0.f ? -1 : limit - first, see1 = !masked ? kKeys : w1.w == 0.f ? -1 : limit - first;
+        float sum0[2] = {0.f, 0.f}, sum1[2] = {0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          uint32_t v[32], p[16];
-          ptx::tmem_ld32(s_col + 32 * c, v);
-          ptx::tmem_ld_wait();
-          if (!masked) {
+          uint32_t p[16];
 #pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              const float x = exp2_fast(fmaf(__uint_as_float(v[j]), c < 2 ? a0 : a1, c < 2 ? c0 : c1));
-              const float y = exp2_fast(fmaf(__uint_as_float(v[j + 1]), c < 2 ? a0 : a1, c < 2 ? c0 : c1));
-              if (c < 2) sum0 += x + y; else sum1 += x + y;
-              p[j / 2] = pack_f16(x, y);
-            }
-          } else {
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              float x = exp2_fast(fmaf(__uint_as_float(v[j]), c < 2 ? a0 : a1, c < 2 ? c0 : c1));
-              float y = exp2_fast(fmaf(__uint_as_float(v[j + 1]), c < 2 ? a0 : a1, c < 2 ? c0 : c1));
-              x = 32 * c + j <= (c < 2 ? see0 : see1) ? x : 0.f;
-              y = 32 * c + j + 1 <= (c < 2 ? see0 : see1) ? y : 0.f;
-              if (c < 2) sum0 += x + y; else sum1 += x + y;
-              p[j / 2] = pack_f16(x, y);
-            }
+          for (int j = 0; j < 32; j += 2) {
+            float x, y;
+            fma2(x, y, c < 2 ? a0 : a1, as_f(v[c][j]), as_f(v[c][j + 1]), c < 2 ? c0 : c1);
+            x = exp2_fast(x);
+            y = exp2_fast(y);
+            if (c < 2) add2(sum0[0], sum0[1], x, y); else add2(sum1[0], sum1[1], x, y);
+            p[j / 2] = pack_f16(x, y);
           }
           tmem_st16(s_col + 16 * c, p);                    // over columns that have been read
         }
-        l += (sum0 > 0.f ? sum0 * w0.z : sum0) + (sum1 > 0.f ? sum1 * w1.z : sum1);
+        const float l0 = sum0[0] + sum0[1], l1 = sum1[0] + sum1[1];
+        l += (l0 > 0.f ? l0 * w0.z : l0) + (l1 > 0.f ? l1 * w1.z : l1);
         tmem_st_wait();
         ptx::tc_fence_before();
         __syncwarp();
@@ -435,7 +491,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       }
       const float inv = none ? 0.f : 1.0f / l;
       const int r = t * kTile + row_in_tile;
-      float* part = slot(blockIdx.x, s.at >= x0 ? 1 : 0);
+      float* part = slot(blockIdx.x, s.starts ? 1 : 0);
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
         uint32_t v[32];
@@ -471,14 +527,11 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
         part[r] = m;
         part[kItemRows + r] = l;
       }
-      if (!whole && threadIdx.x == 0) {
-        Cut* c = &s_cut[s.at >= x0 ? 1 : 0];
-        c->at = s.at; c->len = s.len; c->b = s.b; c->h = s.h; c->tile = s.tile; c->n = s.n;
-      }
       ptx::tc_fence_before();
     }
     if (!ok && lane == 0) report_status(a.hdr, TLQ_ERR_TIMEOUT, 230);
   } else if (warp < kSoftWarps + kLoadWarps) {
+    fewer_registers<kLoadRegs>();
     // ------------------------------------------------------------------ codes of keys and values to f16 operands
     const int lw = warp - kSoftWarps, lr = lane & 7, piece = lane >> 3;      // a warp takes 8 rows x 64 bytes at a time
     constexpr int kNum = D / 16;                           // such pieces per warp of a key (or value) tile
@@ -486,19 +539,31 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     bool ok = true;
     int64_t block[2];
     uint4 kr[kNum], vr[kNum];
-    bool more = walk.next(a, g, s);
-    while (more && s.k0 >= s.k1) more = walk.next(a, g, s);
+    struct { int b, h, k0, k1, kv; } s = {0, 0, 0, 0, 0};
+    auto advance = [&]() {                                 // to the next segment with key tiles
+      do {
+        const Segment* from = next_segment(ok);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok) return false;
+        s.b = from->b; s.h = from->h; s.k0 = from->k0; s.k1 = from->k1; s.kv = from->kv;
+        __syncwarp();
+        if (lane == 0) done_segment(); else if (++seg == kRing) { seg = 0; seg_phase ^= 1u; }
+        if (s.k0 < 0) return false;
+      } while (s.k0 >= s.k1);
+      return true;
+    };
+    bool more = advance();
     int k = more ? s.k0 : 0;
     // the blocks of key tile k, and their steps (by two threads)
     int phys[2];
     auto look_up = [&]() {
-      const int n_blocks = (s.req.kv + kKvBlock - 1) / kKvBlock;
+      const int n_blocks = (s.kv + kKvBlock - 1) / kKvBlock;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
         phys[i] = 2 * k + i < n_blocks ? __ldg(a.block_table + (int64_t)s.b * a.max_blocks + 2 * k + i) : -1;
     };
     auto enter = [&](int at_step) {
-      const int n_blocks = (s.req.kv + kKvBlock - 1) / kKvBlock;
+      const int n_blocks = (s.kv + kKvBlock - 1) / kKvBlock;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const bool in = 2 * k + i < n_blocks, bad = phys[i] < 0 || phys[i] >= a.n_blocks;
@@ -536,7 +601,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       int kn = k + 1;
       bool after = true;
       if (kn >= s.k1) {
-        do after = walk.next(a, g, s); while (after && s.k0 >= s.k1);
+        after = advance();
         kn = s.k0;
       }
       k = kn;
@@ -582,7 +647,9 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       }
     }
     if (!ok && lane == 0) report_status(a.hdr, TLQ_ERR_TIMEOUT, 232);
-  } else if (lane == 0) {
+  } else {
+    fewer_registers<kIssueRegs>();
+    if (warp == 12 && lane == 0) {
     // ------------------------------------------------------------------ products
     constexpr uint32_t kIdescS = ptx::make_idesc(1, 0, kTile, kKeys, false);   // f16 x f16 -> f32
     constexpr uint32_t kIdescO = ptx::make_idesc(1, 0, kTile, D, false);
@@ -603,7 +670,12 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       }
       ptx::mma_commit(bar(10 + t));
     };
-    while (ok && walk.next(a, g, s)) {
+    while (true) {
+      const Segment* from = next_segment(ok);
+      if (!ok) break;
+      struct { int k0, k1; } s = {from->k0, from->k1};
+      done_segment();
+      if (s.k0 < 0) break;
       if (s.k0 >= s.k1) continue;
       for (int t = 0; t < 2; ++t) wait(t, q_phase);
       q_phase ^= 1u;
@@ -641,6 +713,25 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       }
     }
     if (!ok) report_status(a.hdr, TLQ_ERR_TIMEOUT, 233);
+    } else if (warp == 13 && lane == 0) {
+      // ---------------------------------------------------------------- segments
+      Walk walk;
+      walk.start(a, g, found.request, found.rest, x0, x1);
+      uint32_t phase = 1;
+      while (true) {
+        Segment s;
+        const bool more = walk.next(a, g, s);
+        if (!more) s.k0 = -1;
+        if (!ptx::mbar_wait(bar(16 + kRing + seg), phase, abort_flag)) {
+          report_status(a.hdr, TLQ_ERR_TIMEOUT, 234);
+          break;
+        }
+        s_ring[seg] = s;
+        ptx::mbar_arrive(bar(16 + seg));
+        if (!more) break;
+        if (++seg == kRing) { seg = 0; phase ^= 1u; }
+      }
+    }
   }
   __syncwarp();
   if (*abort_flag != 0)
@@ -659,7 +750,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     s_join[threadIdx.x] = 0;
     if (c.len > 0) {
       int k0, k1;
-      walk.cut(x0, x1, c.at, c.len, c.n, k0, k1);
+      cut(x0, x1, c.at, c.len, c.n, k0, k1);
       int32_t* counter = g.split.counters + worker_of(c.at);
       __threadfence();                                     // the CTA's partials, which the barrier has ordered before this
       const int before = atomicAdd(counter, k1 - k0);      // key tiles of the item that are done
@@ -685,7 +776,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
       for (long long w = first; w <= final; ++w) {
         int k0, k1;
-        walk.cut(edge(w), edge(w + 1), c.at, c.len, c.n, k0, k1);
+        cut(edge(w), edge(w + 1), c.at, c.len, c.n, k0, k1);
         if (k0 >= k1) continue;
         const float* p = slot(w, c.at >= edge(w) ? 1 : 0);
         const float m = __ldcg(p + r), l = __ldcg(p + kItemRows + r);
