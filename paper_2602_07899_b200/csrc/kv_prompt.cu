@@ -5,15 +5,17 @@
 //
 // A CTA works on 256 rows of one (request, kv head), a row being one query head of one token: two tiles of 128 rows, so
 // that the exponentials of one run while the tensor core works on the other.  Per tile and 128 cached tokens: S = q K^T
-// (tcgen05, f16 x f16 -> f32, tensor memory), one thread per row takes the maximum and the exponentials of its row straight
-// from tensor memory and writes P over S as f16, O += P V with P from tensor memory.  The output sum is rescaled only when
-// the maximum of a row has grown by more than 4 (a factor of 16 in p): p is kept as 2^11 p, so that it fits 16 bits either way.
-//   warps 0..3, 4..7  softmax of tile 0, 1: a thread is a row (and its accumulator lane)
+// (tcgen05, f16 x f16 -> f32, tensor memory), a thread per row takes the maximum and the exponentials of its row from
+// tensor memory and writes P over S as f16, O += P V with P from tensor memory.  The output sum is rescaled only when the
+// maximum of a row has grown by more than 4 (a factor of 16 in p): p is kept as 2^11 p, so that it fits 16 bits either way.
+//   warps 0..3, 4..7  softmax of tile 0, 1: a thread is a row (and its accumulator lane), its 128 scores in registers
 //   warps 8..11       bring the codes of keys and values from the cache into registers, turn them into f16 and lay them
 //                     out for the tensor core (128-byte swizzle); two stages each
 //   warp 12           issues the products
 //   warp 13           finds the parts of items that this CTA works on and passes them on through a ring (14 and 15 idle:
 //                     registers are shared out by groups of four warps)
+// Nothing in the loops may spill: with 200 KB of shared memory in use the first-level cache is too small for local memory,
+// and a few spilled words per step cost more than the step (versions that spilled ran at 850 to 990 us, see below).
 // Work is cut as in the few-row kernel: items (row tiles of a kv head) lie on one line, weighted by their cached tokens,
 // every CTA takes an equal part of it; an item that is cut leaves partial sums, and the CTA that completes it joins them.
 //
@@ -26,10 +28,10 @@ namespace tlq {
 namespace {
 
 constexpr int kTile = 128, kItemRows = 256, kKeys = 128;
-constexpr int kSoftWarps = 8, kLoadWarps = 4;
-constexpr int kThreads = 512;                              // four warpgroups; of the last one a single warp works
-// registers of a thread of each role: 2 x 176 + 112 + 48 = 4 x 128, what the block is launched with
-constexpr int kSoftRegs = 176, kLoadRegs = 112, kIssueRegs = 48;
+constexpr int kSoftWarps = 8, kLoadWarps = 4, kIssueWarp = kSoftWarps + kLoadWarps, kPlanWarp = kIssueWarp + 1;
+constexpr int kThreads = 512;                              // four groups of four warps
+// registers of a thread of each role: 2 x 192 + 80 + 48 = 4 x 128, what the block is launched with
+constexpr int kSoftRegs = 192, kLoadRegs = 80, kIssueRegs = 48, kLaunchRegs = 128;
 constexpr float kShift = 11.f, kGrow = 4.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kStepFloor = 7.8886090522101181e-31f;      // 2^-100, as in kv_attention.cu
@@ -131,6 +133,11 @@ __device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[32]) {
                  "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
                  "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
 }
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
+}
 __device__ __forceinline__ float as_f(uint32_t x) { return __uint_as_float(x); }
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -173,7 +180,7 @@ struct __align__(16) Segment {
   int b, h, tile, k0;
   int k1, n, q0, q_len;
   long long at, len;            // the item on the line
-  int kv, pad[3];
+  int kv, starts, pad[2];       // starts: the item starts in this CTA's part of the line
 };
 constexpr int kRing = 4;        // segments in the ring
 
@@ -229,12 +236,16 @@ struct Walk {
       s.len = costs.sum(tile + 1) - costs.sum(tile);
       s.n = key_tiles(a, g);
       cut(x0, x1, s.at, s.len, s.n, s.k0, s.k1);
-      s.b = b; s.h = h; s.tile = tile; s.q0 = req.q0; s.q_len = req.q_len; s.kv = req.kv;
+      s.b = b; s.h = h; s.tile = tile; s.q0 = req.q0; s.q_len = req.q_len; s.kv = req.kv; s.starts = s.at >= x0 ? 1 : 0;
       const bool here = s.n == 0 ? s.at >= x0 : s.k0 < s.k1;   // an item without visible keys belongs to whoever has its start
       ++tile;
       if (here) return true;
     }
   }
+};
+
+struct Line {                   // the whole line, how many CTAs share it, this CTA's part
+  long long total, workers, x0, x1;
 };
 
 struct Cut {                    // an item of which this CTA has only a part
@@ -254,6 +265,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
   __shared__ long long sums[kThreads / 32];
   __shared__ Found found;
   __shared__ Cut s_cut[2];
+  __shared__ Line s_line;
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort, s_join[2];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -294,22 +306,24 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     total += part;
   }
   if (total == 0) return;
-  // a part is worth joining from some key tiles on
-  const long long workers = max(1LL, min((long long)gridDim.x, total / (64 * kMinTiles)));
-  if (blockIdx.x >= workers) return;
-  auto edge = [&](long long w) { return total * w / workers; };
-  auto worker_of = [&](long long x) { return ((x + 1) * workers - 1) / total; };
-  const long long x0 = edge(blockIdx.x), x1 = edge(blockIdx.x + 1);
-  if (x0 >= x1) return;
-  if (!locate_item<kThreads>(a.B, x0, cost_of, sums, &found)) return;
-  if (warp == 12) ptx::tmem_alloc(ptx::smem_u32(&s_tmem), 512);
+  {
+    // a part is worth joining from some key tiles on
+    const long long workers = max(1LL, min((long long)gridDim.x, total / (64 * kMinTiles)));
+    if (blockIdx.x >= workers) return;
+    const long long x0 = total * blockIdx.x / workers, x1 = total * (blockIdx.x + 1) / workers;
+    if (x0 >= x1) return;
+    if (!locate_item<kThreads>(a.B, x0, cost_of, sums, &found)) return;
+    if (threadIdx.x == 0) {                                // read back where they are needed: the loops have no registers to spare
+      s_line.total = total; s_line.workers = workers; s_line.x0 = x0; s_line.x1 = x1;
+    }
+  }
+  if (warp == kIssueWarp) ptx::tmem_alloc(ptx::smem_u32(&s_tmem), 512);
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = s_tmem;                            // S of tile 0, 1 at columns 0, 128; O at 256, 384
-  float* const partials = g.split.partials;
   constexpr size_t kPitch = (size_t)kItemRows * (D + 2);   // floats of a partial: maxima, sums, output sums
-  auto slot = [&](long long w, int i) { return partials + ((size_t)w * 2 + i) * kPitch; };
+  auto slot = [&](long long w, int i) { return g.split.partials + ((size_t)w * 2 + i) * kPitch; };
   // the next segment, by all lanes of a warp (or the one that issues)
   int seg = 0;
   uint32_t seg_phase = 0;
@@ -326,90 +340,83 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     more_registers<kSoftRegs>();
     // ------------------------------------------------------------------ softmax: a thread is a row
     const int t = warp >> 2, row_in_tile = (warp & 3) * 32 + lane;
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t s_col = tmem + lanes + t * kTile, o_col = tmem + lanes + 256 + t * kTile;
-    const uint32_t q_row = q_at + t * kQBytes<D> + row_in_tile * 128;
+    const uint32_t s_col = tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * kTile, o_col = s_col + 256;   // P over S
     uint32_t s_phase = 0, o_phase = 0;
     int step = 0;                                          // key tiles so far, of all segments
     bool ok = true;
     while (true) {
-      const Segment* from = next_segment(ok);
+      const Segment* s = next_segment(ok);
       ok = __all_sync(0xFFFFFFFFu, ok);
-      if (!ok) break;
-      struct { int b, h, tile, k0, k1, n, q0, q_len, kv; bool starts; } s = {from->b, from->h, from->tile, from->k0, from->k1,
-                                                               from->n, from->q0, from->q_len, from->kv, from->at >= x0};
-      if (threadIdx.x == 0 && s.k0 >= 0 && (s.k0 > 0 || s.k1 < s.n)) {
-        Cut* c = &s_cut[s.starts ? 1 : 0];
-        c->at = from->at; c->len = from->len; c->b = s.b; c->h = s.h; c->tile = s.tile; c->n = s.n;
+      if (!ok || s->k0 < 0) break;
+      const int k0 = s->k0, k1 = s->k1;
+      if (threadIdx.x == 0 && (k0 > 0 || k1 < s->n)) {
+        Cut* c = &s_cut[s->starts];
+        c->at = s->at; c->len = s->len; c->b = s->b; c->h = s->h; c->tile = s->tile; c->n = s->n;
       }
-      __syncwarp();
-      if (lane == 0) done_segment(); else if (++seg == kRing) { seg = 0; seg_phase ^= 1u; }
-      if (s.k0 < 0) break;
-      const int row = s.tile * kItemRows + t * kTile + row_in_tile;
-      const long long rows = (long long)s.q_len * a.group;
-      const bool live = row < rows;
-      const int limit = !live ? -1 : g.causal ? min(s.kv - s.q_len + row / a.group, s.kv - 1) : s.kv - 1;
-      const int64_t at = live ? (int64_t)(s.q0 + row / a.group) * a.n_heads + s.h * a.group + row % a.group : 0;
-      // the row of q: a power of two brings it into the range of f16
+      int limit;
       float fac = 0.f, off = 0.f;
-      if (s.k0 < s.k1) {
-        const uint16_t* p = g.q + (live ? (int64_t)(s.q0 + row / a.group) * g.ldq + (int64_t)(s.h * a.group + row % a.group) * D : 0);
-        uint4 v[D / 8];
+      {
+        // the row of q: a power of two brings it into the range of f16
+        const int row = s->tile * kItemRows + t * kTile + row_in_tile, token = row / a.group;
+        const bool live = token < s->q_len;
+        limit = !live ? -1 : g.causal ? min(s->kv - s->q_len + token, s->kv - 1) : s->kv - 1;
+        if (k0 < k1) {
+          const uint16_t* p = g.q;
+          if (live) p += (int64_t)(s->q0 + token) * g.ldq + (int64_t)(s->h * a.group + row - token * a.group) * D;
+          uint4 v[D / 8];
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) v[i] = live ? __ldg(reinterpret_cast<const uint4*>(p) + i) : make_uint4(0, 0, 0, 0);
-        float top = 0.f;
+          for (int i = 0; i < D / 8; ++i) v[i] = live ? __ldg(reinterpret_cast<const uint4*>(p) + i) : make_uint4(0, 0, 0, 0);
+          float top = 0.f;
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-          float e[8];
-          unpack8(v[i], e);
+          for (int i = 0; i < D / 8; ++i) {
+            float e[8];
+            unpack8(v[i], e);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(e[j]));
-        }
-        const int ex = top > 0.f && top <= 3.4e38f ? ilogbf(top) : 0;
-        const float d0 = ldexpf(1.0f, -(ex / 2)), d1 = ldexpf(1.0f, -(ex - ex / 2));
-        float qs = 0.f;
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-          float e[8];
-          unpack8(v[i], e);
-          uint32_t w[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            w[j] = pack_f16(e[2 * j] * d0 * d1, e[2 * j + 1] * d0 * d1);
-            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
-            qs += y.x + y.y;
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(e[j]));
           }
-          sts128(q_row + (i >> 3) * (kTile * 128) + (((i & 7) ^ (row_in_tile & 7)) << 4), w[0], w[1], w[2], w[3]);
+          const int ex = top > 0.f && top <= 3.4e38f ? ilogbf(top) : 0;
+          const float d0 = ldexpf(1.0f, -(ex / 2)), d1 = ldexpf(1.0f, -(ex - ex / 2));
+          const uint32_t q_row = q_at + t * kQBytes<D> + row_in_tile * 128;
+          float qs = 0.f;
+#pragma unroll
+          for (int i = 0; i < D / 8; ++i) {
+            float e[8];
+            unpack8(v[i], e);
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              w[j] = pack_f16(e[2 * j] * d0 * d1, e[2 * j + 1] * d0 * d1);
+              const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+              qs += y.x + y.y;
+            }
+            sts128(q_row + (i >> 3) * (kTile * 128) + (((i & 7) ^ (row_in_tile & 7)) << 4), w[0], w[1], w[2], w[3]);
+          }
+          fac = ldexpf(g.scale_log2, ex + 24);
+          off = qs * (128.f / kUnit);
+          ptx::fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(bar(t));
         }
-        fac = ldexpf(g.scale_log2, ex + 24);
-        off = qs * (128.f / kUnit);
-        ptx::fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(bar(t));
       }
 
       float m = -INFINITY, l = 0.f;
-      for (int k = s.k0; k < s.k1; ++k, ++step) {
+      for (int k = k0; k < k1; ++k, ++step) {
         ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(10 + t), s_phase, abort_flag));
         if (!ok) break;
         s_phase ^= 1u;
         ptx::tc_fence_after();
+        uint32_t v[4][32];                                 // the row of S
+#pragma unroll
+        for (int c = 0; c < 4; ++c) ptx::tmem_ld32(s_col + 32 * c, v[c]);
         const float4 w0 = s_steps[step & 3][0], w1 = s_steps[step & 3][1];
         float a0 = fac * w0.x, a1 = fac * w1.x;
         float b0 = fmaf(-off, a0, w0.y), b1 = fmaf(-off, a1, w1.y);
-        const int first = k * kKeys;                       // place of the tile's first key
-        const bool masked = __any_sync(0xFFFFFFFFu, first + kKeys - 1 > limit) || w0.w == 0.f || w1.w == 0.f;
-        uint32_t v[4][32];                                 // the row of S
-        ptx::tmem_ld32(s_col, v[0]);
-        ptx::tmem_ld32(s_col + 32, v[1]);
-        tmem_ld_wait_for(v[0]);
-        tmem_ld_wait_for(v[1]);
-        ptx::tmem_ld32(s_col + 64, v[2]);
-        ptx::tmem_ld32(s_col + 96, v[3]);
+        const int see = limit - k * kKeys;                 // last key of the tile that the row sees
+        const bool masked = __any_sync(0xFFFFFFFFu, see < kKeys - 1) || w0.w == 0.f || w1.w == 0.f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld_wait_for(v[c]);
         if (masked) {                                      // t itself, with nothing where there is nothing to see
-          tmem_ld_wait_for(v[2]);
-          tmem_ld_wait_for(v[3]);
-          const int see0 = w0.w == 0.f ? -1 : limit - first, see1 = w1.w == 0.f ? -1 : limit - first;
+          const int see0 = w0.w == 0.f ? -1 : see, see1 = w1.w == 0.f ? -1 : see;
 #pragma unroll
           for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -420,42 +427,40 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
           a0 = a1 = 1.f;
           b0 = b1 = 0.f;
         }
-        float r[2][4];
+        float top;
+        {
+          float r[2][4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          if (c == 2) {
-            tmem_ld_wait_for(v[2]);
-            tmem_ld_wait_for(v[3]);
-          }
+          for (int c = 0; c < 4; ++c)
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            float& x = r[c >> 1][j & 3];
-            x = (c & 1) == 0 && j < 4 ? as_f(v[c][j]) : fmaxf(x, as_f(v[c][j]));
-          }
+            for (int j = 0; j < 32; ++j) {
+              float& x = r[c >> 1][j & 3];
+              x = (c & 1) == 0 && j < 4 ? as_f(v[c][j]) : fmaxf(x, as_f(v[c][j]));
+            }
+          top = fmaxf(fmaf(fmaxf(fmaxf(r[0][0], r[0][1]), fmaxf(r[0][2], r[0][3])), a0, b0),
+                      fmaf(fmaxf(fmaxf(r[1][0], r[1][1]), fmaxf(r[1][2], r[1][3])), a1, b1));
         }
-        const float top = fmaxf(fmaf(fmaxf(fmaxf(r[0][0], r[0][1]), fmaxf(r[0][2], r[0][3])), a0, b0),
-                                fmaf(fmaxf(fmaxf(r[1][0], r[1][1]), fmaxf(r[1][2], r[1][3])), a1, b1));
         // a maximum that has grown by more than kGrow: the output sum follows
-        const bool grow = top > m + kGrow || (m == -INFINITY && top > -INFINITY);
-        if (__any_sync(0xFFFFFFFFu, grow)) {
+        if (__any_sync(0xFFFFFFFFu, top > m + kGrow || (m == -INFINITY && top > -INFINITY))) {
           const float mn = fmaxf(m, top);
           const float corr = mn == -INFINITY ? 1.f : exp2_fast(m - mn);
           m = mn;
           l *= corr;
-          if (k > s.k0) {
-#pragma unroll
+          if (k > k0) {
+#pragma unroll 1
             for (int c = 0; c < D / 16; ++c) {
               uint32_t x[16];
               ptx::tmem_ld16(o_col + 16 * c, x);
-              ptx::tmem_ld_wait();
+              tmem_ld_wait_for(x);
 #pragma unroll
-              for (int j = 0; j < 16; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * corr);
+              for (int j = 0; j < 16; ++j) x[j] = __float_as_uint(as_f(x[j]) * corr);
               tmem_st16(o_col + 16 * c, x);
             }
           }
         }
-        const float mu = m == -INFINITY ? 0.f : m;
-        const float c0 = b0 - mu + kShift, c1 = b1 - mu + kShift;
+        const float shift = kShift - (m == -INFINITY ? 0.f : m);
+        b0 += shift;
+        b1 += shift;
         float sum0[2] = {0.f, 0.f}, sum1[2] = {0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -463,16 +468,16 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
             float x, y;
-            fma2(x, y, c < 2 ? a0 : a1, as_f(v[c][j]), as_f(v[c][j + 1]), c < 2 ? c0 : c1);
+            fma2(x, y, c < 2 ? a0 : a1, as_f(v[c][j]), as_f(v[c][j + 1]), c < 2 ? b0 : b1);
             x = exp2_fast(x);
             y = exp2_fast(y);
             if (c < 2) add2(sum0[0], sum0[1], x, y); else add2(sum1[0], sum1[1], x, y);
             p[j / 2] = pack_f16(x, y);
           }
-          tmem_st16(s_col + 16 * c, p);                    // over columns that have been read
+          tmem_st16(s_col + 16 * c, p);                    // all of S has been read
         }
         const float l0 = sum0[0] + sum0[1], l1 = sum1[0] + sum1[1];
-        l += (l0 > 0.f ? l0 * w0.z : l0) + (l1 > 0.f ? l1 * w1.z : l1);
+        l += (l0 > 0.f ? l0 * s_steps[step & 3][0].z : l0) + (l1 > 0.f ? l1 * s_steps[step & 3][1].z : l1);
         tmem_st_wait();
         ptx::tc_fence_before();
         __syncwarp();
@@ -481,130 +486,134 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       if (!ok) break;
 
       // ---------------------------------------------------------------- leave the item
-      const bool none = m == -INFINITY && l == 0.f;        // a row that sees nothing (a NaN row has a NaN sum)
-      const bool whole = s.k0 == 0 && s.k1 == s.n;
-      if (s.k0 < s.k1) {
+      if (k0 < k1) {
         ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(14 + t), o_phase, abort_flag));
         if (!ok) break;
         o_phase ^= 1u;
         ptx::tc_fence_after();
       }
-      const float inv = none ? 0.f : 1.0f / l;
-      const int r = t * kTile + row_in_tile;
-      float* part = slot(blockIdx.x, s.starts ? 1 : 0);
+      {
+        const bool none = m == -INFINITY && l == 0.f;      // a row that sees nothing (a NaN row has a NaN sum)
+        const bool whole = k0 == 0 && k1 == s->n;
+        const float inv = none ? 0.f : 1.0f / l;
+        const int r = t * kTile + row_in_tile, row = s->tile * kItemRows + r, token = row / a.group;
+        const bool live = token < s->q_len;
+        const int64_t at = (int64_t)(s->q0 + token) * a.n_heads + s->h * a.group + row - token * a.group;
+        float* part = slot(blockIdx.x, s->starts);
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) {
-        uint32_t v[32];
-        if (s.k0 < s.k1) {
-          ptx::tmem_ld32(o_col + 32 * c, v);
-          ptx::tmem_ld_wait();
-        } else {
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t v[32];
+          if (k0 < k1) {
+            ptx::tmem_ld32(o_col + 32 * c, v);
+            tmem_ld_wait_for(v);
+          } else {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = 0u;
-        }
-        if (live && whole) {
-          uint4* to = reinterpret_cast<uint4*>(g.out + at * D + 32 * c);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t y[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const __nv_bfloat162 z = __floats2bfloat162_rn(none ? 0.f : __uint_as_float(v[8 * i + 2 * j]) * inv,
-                                                             none ? 0.f : __uint_as_float(v[8 * i + 2 * j + 1]) * inv);
-              y[j] = *reinterpret_cast<const uint32_t*>(&z);
-            }
-            to[i] = make_uint4(y[0], y[1], y[2], y[3]);
+            for (int j = 0; j < 32; ++j) v[j] = 0u;
           }
-        } else if (live) {
-          uint4* to = reinterpret_cast<uint4*>(part + 2 * kItemRows + (size_t)r * D + 32 * c);
+          if (live && whole) {
+            uint4* to = reinterpret_cast<uint4*>(g.out + at * D + 32 * c);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) to[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            for (int i = 0; i < 4; ++i) {
+              uint32_t y[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const __nv_bfloat162 z = __floats2bfloat162_rn(none ? 0.f : as_f(v[8 * i + 2 * j]) * inv,
+                                                               none ? 0.f : as_f(v[8 * i + 2 * j + 1]) * inv);
+                y[j] = *reinterpret_cast<const uint32_t*>(&z);
+              }
+              to[i] = make_uint4(y[0], y[1], y[2], y[3]);
+            }
+          } else if (live) {
+            uint4* to = reinterpret_cast<uint4*>(part + 2 * kItemRows + (size_t)r * D + 32 * c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) to[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+          }
+          __syncwarp();
         }
-        __syncwarp();
-      }
-      if (live && whole && g.lse != nullptr) g.lse[at] = none ? -INFINITY : kLn2 * (log2f(l) + m - kShift);
-      if (live && !whole) {
-        part[r] = m;
-        part[kItemRows + r] = l;
+        if (live && whole && g.lse != nullptr) g.lse[at] = none ? -INFINITY : kLn2 * (log2f(l) + m - kShift);
+        if (live && !whole) {
+          part[r] = m;
+          part[kItemRows + r] = l;
+        }
       }
       ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) done_segment(); else if (++seg == kRing) { seg = 0; seg_phase ^= 1u; }
     }
     if (!ok && lane == 0) report_status(a.hdr, TLQ_ERR_TIMEOUT, 230);
   } else if (warp < kSoftWarps + kLoadWarps) {
     fewer_registers<kLoadRegs>();
     // ------------------------------------------------------------------ codes of keys and values to f16 operands
-    const int lw = warp - kSoftWarps, lr = lane & 7, piece = lane >> 3;      // a warp takes 8 rows x 64 bytes at a time
-    constexpr int kNum = D / 16;                           // such pieces per warp of a key (or value) tile
-    int step = 0;
+    // A warp takes 8 rows x 64 bytes at a time.  Keys: row group (lw / panels) + i * 4 / panels of 16, the same panel for all
+    // i; values: row group lw + 4 i of a block's D / 8.  Either way the first half of the i is the tile's first block.
+    constexpr int kNum = D / 16, kGroups = 4 / kPanels<D>;   // pieces of a warp; key row groups that the warps take at a time
+    const int lw = warp - kSoftWarps, lr = lane & 7, piece = lane >> 3;
+    const int k_row = (lw / kPanels<D>) * 8 + lr, k_panel = lw % kPanels<D>;
+    const int8_t* const k_from = a.k_codes + k_row * D + k_panel * 64 + piece * 16;
+    const int8_t* const v_from = a.v_codes + (lw * 8 + lr) * kKvBlock + piece * 16;
+    const uint32_t swizzled0 = ((2 * piece) ^ lr) << 4, swizzled1 = ((2 * piece + 1) ^ lr) << 4;
+    const uint32_t k_to = k_at + k_panel * (kKeys * 128) + k_row * 128, v_to = v_at + (lw * 8 + lr) * 128;
+    int step = 0, b = 0, h = 0, k = 0, k1 = 0, n_blocks = 0;
     bool ok = true;
-    int64_t block[2];
     uint4 kr[kNum], vr[kNum];
-    struct { int b, h, k0, k1, kv; } s = {0, 0, 0, 0, 0};
+    int phys[2];
+    float ks = 0.f, vs = 0.f;                              // steps of the block `lane` (lanes 0 and 1 of the first warp)
+    int64_t block[2];                                      // of the tile whose codes are under way, in bytes
+    bool usable[2];
     auto advance = [&]() {                                 // to the next segment with key tiles
-      do {
+      while (true) {
         const Segment* from = next_segment(ok);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) return false;
-        s.b = from->b; s.h = from->h; s.k0 = from->k0; s.k1 = from->k1; s.kv = from->kv;
+        b = from->b; h = from->h; k = from->k0; k1 = from->k1;
+        n_blocks = (from->kv + kKvBlock - 1) / kKvBlock;
         __syncwarp();
         if (lane == 0) done_segment(); else if (++seg == kRing) { seg = 0; seg_phase ^= 1u; }
-        if (s.k0 < 0) return false;
-      } while (s.k0 >= s.k1);
-      return true;
-    };
-    bool more = advance();
-    int k = more ? s.k0 : 0;
-    // the blocks of key tile k, and their steps (by two threads)
-    int phys[2];
-    auto look_up = [&]() {
-      const int n_blocks = (s.kv + kKvBlock - 1) / kKvBlock;
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        phys[i] = 2 * k + i < n_blocks ? __ldg(a.block_table + (int64_t)s.b * a.max_blocks + 2 * k + i) : -1;
-    };
-    auto enter = [&](int at_step) {
-      const int n_blocks = (s.kv + kKvBlock - 1) / kKvBlock;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const bool in = 2 * k + i < n_blocks, bad = phys[i] < 0 || phys[i] >= a.n_blocks;
-        if (in && bad) report_status(a.hdr, TLQ_ERR_SHAPE, 231);
-        block[i] = (int64_t)(bad ? 0 : phys[i]) * a.n_kv + s.h;
-        if (lw == 0 && lane == i) {
-          const float vs = __ldg(a.v_steps + block[i]), v = vs < kStepFloor ? kStepFloor : vs;
-          s_steps[at_step & 3][i] = make_float4(__ldg(a.k_steps + block[i]), log2f(v), 1.0f / v, bad ? 0.f : 1.f);
-        }
+        if (k < 0) return false;
+        if (k < k1) return true;
       }
     };
-    // rows of a key tile: 16 groups of 8 tokens, D / 64 halves; of a value tile: 2 blocks of D / 8 groups of 8 channels
+    auto look_up = [&]() {                                 // the blocks of key tile k
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        phys[i] = 2 * k + i < n_blocks ? __ldg(a.block_table + (int64_t)b * a.max_blocks + 2 * k + i) : -1;
+    };
     auto load_keys = [&]() {
 #pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        usable[i] = phys[i] >= 0 && phys[i] < a.n_blocks;
+        if (!usable[i] && 2 * k + i < n_blocks) report_status(a.hdr, TLQ_ERR_SHAPE, 231);
+        const int64_t at = (int64_t)(usable[i] ? phys[i] : 0) * a.n_kv + h;
+        block[i] = at * (kKvBlock * D);
+        if (lw == 0 && lane == i) {
+          ks = __ldg(a.k_steps + at);
+          vs = __ldg(a.v_steps + at);
+        }
+      }
+#pragma unroll
       for (int i = 0; i < kNum; ++i) {
-        const int idx = lw + 4 * i, r = (idx / kPanels<D>) * 8 + lr, half = idx % kPanels<D>;
-        kr[i] = ld_cache(a.k_codes + block[r >> 6] * (kKvBlock * D) + (r & 63) * D + half * 64 + piece * 16);
+        // rows of the tile from k_row on, kGroups * 8 apart; a block is 64 of them
+        const int row = i * kGroups * 8;
+        kr[i] = ld_cache(k_from + block[row >> 6] + (row & 63) * D);
       }
     };
     auto load_values = [&]() {
 #pragma unroll
-      for (int i = 0; i < kNum; ++i) {
-        const int idx = lw + 4 * i, which = idx / (D / 8), r = (idx % (D / 8)) * 8 + lr;
-        vr[i] = ld_cache(a.v_codes + block[which] * (kKvBlock * D) + r * kKvBlock + piece * 16);
-      }
+      for (int i = 0; i < kNum; ++i) vr[i] = ld_cache(v_from + block[i / (kNum / 2)] + (i % (kNum / 2)) * 32 * kKvBlock);
     };
+    bool more = advance();
     if (more) {
       look_up();
-      enter(0);
       load_keys();
       load_values();
     }
-    while (more && ok) {
+    while (more) {
+      const float my_ks = ks, my_vs = vs;
+      const float my_use = usable[0] && lane == 0 ? 1.f : usable[1] && lane == 1 ? 1.f : 0.f;
       // the tile after this one
-      int kn = k + 1;
       bool after = true;
-      if (kn >= s.k1) {
-        after = advance();
-        kn = s.k0;
-      }
-      k = kn;
+      if (++k >= k1) after = advance();
+      if (!ok) break;
       if (after) look_up();
       const int stage = step & 1;
       const uint32_t parity = ((uint32_t)(step >> 1) & 1u) ^ 1u;
@@ -612,44 +621,43 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       if (!ok) break;
 #pragma unroll
       for (int i = 0; i < kNum; ++i) {
-        const int idx = lw + 4 * i, r = (idx / kPanels<D>) * 8 + lr, half = idx % kPanels<D>;
-        const uint32_t to = k_at + stage * kKBytes<D> + half * (kKeys * 128) + r * 128;
+        const uint32_t to = k_to + stage * kKBytes<D> + i * kGroups * 8 * 128;
         uint32_t x[8];
         keys_to_f16(kr[i].x, x[0], x[1]); keys_to_f16(kr[i].y, x[2], x[3]);
         keys_to_f16(kr[i].z, x[4], x[5]); keys_to_f16(kr[i].w, x[6], x[7]);
-        sts128(to + (((2 * piece) ^ lr) << 4), x[0], x[1], x[2], x[3]);
-        sts128(to + (((2 * piece + 1) ^ lr) << 4), x[4], x[5], x[6], x[7]);
+        sts128(to + swizzled0, x[0], x[1], x[2], x[3]);
+        sts128(to + swizzled1, x[4], x[5], x[6], x[7]);
+      }
+      if (lw == 0 && lane < 2) {
+        const float v = my_vs < kStepFloor ? kStepFloor : my_vs;
+        s_steps[step & 3][lane] = make_float4(my_ks, log2f(v), 1.0f / v, my_use);
       }
       ptx::fence_proxy_async();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(bar(2 + stage));
+      if (after) load_keys();
       ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(8 + stage), parity, abort_flag));
       if (!ok) break;
 #pragma unroll
       for (int i = 0; i < kNum; ++i) {
-        const int idx = lw + 4 * i, which = idx / (D / 8), r = (idx % (D / 8)) * 8 + lr;
-        const uint32_t to = v_at + stage * kVBytes<D> + which * (D * 128) + r * 128;
+        const uint32_t to = v_to + stage * kVBytes<D> + (i / (kNum / 2)) * (D * 128) + (i % (kNum / 2)) * 32 * 128;
         uint32_t x[8];
         values_to_f16(vr[i].x, x[0], x[1]); values_to_f16(vr[i].y, x[2], x[3]);
         values_to_f16(vr[i].z, x[4], x[5]); values_to_f16(vr[i].w, x[6], x[7]);
-        sts128(to + (((2 * piece) ^ lr) << 4), x[0], x[1], x[2], x[3]);
-        sts128(to + (((2 * piece + 1) ^ lr) << 4), x[4], x[5], x[6], x[7]);
+        sts128(to + swizzled0, x[0], x[1], x[2], x[3]);
+        sts128(to + swizzled1, x[4], x[5], x[6], x[7]);
       }
       ptx::fence_proxy_async();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(bar(6 + stage));
+      if (after) load_values();
       ++step;
       more = after;
-      if (more) {
-        enter(step);
-        load_keys();
-        load_values();
-      }
     }
     if (!ok && lane == 0) report_status(a.hdr, TLQ_ERR_TIMEOUT, 232);
   } else {
     fewer_registers<kIssueRegs>();
-    if (warp == 12 && lane == 0) {
+    if (warp == kIssueWarp && lane == 0) {
     // ------------------------------------------------------------------ products
     constexpr uint32_t kIdescS = ptx::make_idesc(1, 0, kTile, kKeys, false);   // f16 x f16 -> f32
     constexpr uint32_t kIdescO = ptx::make_idesc(1, 0, kTile, D, false);
@@ -713,10 +721,10 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       }
     }
     if (!ok) report_status(a.hdr, TLQ_ERR_TIMEOUT, 233);
-    } else if (warp == 13 && lane == 0) {
+    } else if (warp == kPlanWarp && lane == 0) {
       // ---------------------------------------------------------------- segments
       Walk walk;
-      walk.start(a, g, found.request, found.rest, x0, x1);
+      walk.start(a, g, found.request, found.rest, s_line.x0, s_line.x1);
       uint32_t phase = 1;
       while (true) {
         Segment s;
@@ -734,23 +742,28 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     }
   }
   __syncwarp();
+  // the rest is run by all warps: back to what they were launched with
+  if (warp < kSoftWarps) fewer_registers<kLaunchRegs>(); else more_registers<kLaunchRegs>();
   if (*abort_flag != 0)
     for (int i = 0; i < 1000; ++i) __nanosleep(1000);      // products under way end before their memory is given back
   ptx::tc_fence_before();
   __syncthreads();
-  if (warp == 12) {
+  if (warp == kIssueWarp) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc(tmem, 512);
   }
   if (*abort_flag != 0) return;
 
   // ------------------------------------------------------------------ join the CTAs that share an item
+  const long long total_cost = s_line.total, workers = s_line.workers;
+  auto edge = [&](long long w) { return total_cost * w / workers; };
+  auto worker_of = [&](long long x) { return ((x + 1) * workers - 1) / total_cost; };
   if (threadIdx.x < 2) {
     const Cut c = s_cut[threadIdx.x];
     s_join[threadIdx.x] = 0;
     if (c.len > 0) {
       int k0, k1;
-      cut(x0, x1, c.at, c.len, c.n, k0, k1);
+      cut(s_line.x0, s_line.x1, c.at, c.len, c.n, k0, k1);
       int32_t* counter = g.split.counters + worker_of(c.at);
       __threadfence();                                     // the CTA's partials, which the barrier has ordered before this
       const int before = atomicAdd(counter, k1 - k0);      // key tiles of the item that are done
