@@ -3,41 +3,42 @@
 // The formulas are those of kv_attention.cu: scores from (kc + 128) with the 128 sum(q) taken out by a constant of the row,
 // p_j = 2^(t_j - m) with t_j = a (q . kc_j) + log2(vstep), output sums of p vc and sums of p / vstep.
 //
-// A CTA works on 256 rows of one (request, kv head), a row being one query head of one token: two tiles of 128 rows, so
-// that the exponentials of one run while the tensor core works on the other.  Per tile and 128 cached tokens: S = q K^T
-// (tcgen05, f16 x f16 -> f32, tensor memory), a thread per row takes the maximum and the exponentials of its row from
-// tensor memory and writes P over S as f16, O += P V with P from tensor memory.  The output sum is rescaled only when the
-// maximum of a row has grown by more than 4 (a factor of 16 in p): p is kept as 2^11 p, so that it fits 16 bits either way.
-//   warps 0..3, 4..7  softmax of tile 0, 1: a thread is a row (and its accumulator lane), its 128 scores in registers
+// A CTA works on 256 rows of one (request, kv head), a row being one query head of one token: two tiles of 128 rows.  Per
+// tile and cache block (64 keys): S = q K^T (tcgen05, f16 x f16 -> f32, tensor memory), a thread per row takes the maximum
+// and the exponentials of its row from tensor memory and writes P over S as f16, O += P V with P from tensor memory.  S has
+// two buffers per tile: while a row's exponentials of one block are taken, the tensor core finishes P V of the block before
+// and S of the block after it.  The output sum is rescaled only when the maximum of a row has grown by more than 4 (a factor
+// of 16 in p): p is kept as 2^11 p, so that it fits 16 bits either way.
+//   warps 0..3, 4..7  softmax of tile 0, 1: a thread is a row (and its accumulator lane)
 //   warps 8..11       bring the codes of keys and values from the cache into registers, turn them into f16 and lay them
-//                     out for the tensor core (128-byte swizzle); two stages each
-//   warp 12           issues the products
-//   warp 13           finds the parts of items that this CTA works on and passes them on through a ring (14 and 15 idle:
-//                     registers are shared out by groups of four warps)
-// Nothing in the loops may spill: with 200 KB of shared memory in use the first-level cache is too small for local memory,
-// and a few spilled words per step cost more than the step (versions that spilled ran at 850 to 990 us, see below).
+//                     out for the tensor core (128-byte swizzle); four stages each
+//   warps 12, 15      issue the products of tile 0, 1 (one warp for both spends its time waiting: 2500 cycles a block)
+//   warp 13           finds the parts of items that this CTA works on and passes them on through a ring
+//   warp 14           looks up the cache blocks to come and their steps and passes them on through another ring
+// Nothing in the loops may spill: with 200 KB of shared memory in use the first-level cache is too small
+// for local memory, and one reload per step costs as much as a product.
 // Work is cut as in the few-row kernel: items (row tiles of a kv head) lie on one line, weighted by their cached tokens,
 // every CTA takes an equal part of it; an item that is cut leaves partial sums, and the CTA that completes it joins them.
 //
 // Bound: the tensor core (4 D flops per visible pair) and, next to it, the exponential unit: 256 x 128 exponentials at 16
 // per cycle take as long as the products of the same tile.
+#include <type_traits>
+
 #include "serve.cuh"
 #include "umma.cuh"
 
 namespace tlq {
 namespace {
 
-constexpr int kTile = 128, kItemRows = 256, kKeys = 128;
-constexpr int kSoftWarps = 8, kLoadWarps = 4, kIssueWarp = kSoftWarps + kLoadWarps, kPlanWarp = kIssueWarp + 1;
-constexpr int kThreads = 512;                              // four groups of four warps
-// registers of a thread of each role: 2 x 192 + 80 + 48 = 4 x 128, what the block is launched with
-constexpr int kSoftRegs = 192, kLoadRegs = 80, kIssueRegs = 48, kLaunchRegs = 128;
+constexpr int kTile = 128, kItemRows = 256, kKeys = kKvBlock, kStages = 4;
+constexpr int kSoftWarps = 8, kLoadWarps = 4, kIssueWarp = kSoftWarps + kLoadWarps, kPlanWarp = kIssueWarp + 1, kScoutWarp = kIssueWarp + 2;
+constexpr int kThreads = 512;
 constexpr float kShift = 11.f, kGrow = 4.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kStepFloor = 7.8886090522101181e-31f;      // 2^-100, as in kv_attention.cu
 constexpr float kUnit = 16777216.f;                        // 2^24
-constexpr int kMinTiles = 6;                               // key tiles of a CTA's part, at least
-constexpr int kItemCost = 2;                               // what an item costs beside its key tiles, in key tiles
+constexpr int kMinTiles = 12;                              // blocks of a CTA's part, at least
+constexpr int kItemCost = 4;                               // what an item costs beside its blocks, in blocks
 
 struct PromptArgs {
   const uint16_t* q;
@@ -49,6 +50,20 @@ struct PromptArgs {
   KvSplit split;
 };
 
+constexpr int kRing = 4;                                   // segments in the planner's ring
+constexpr int kTileRing = 16;                              // blocks in the scout's ring
+// barriers
+enum : int {
+  kBarQ = 0,                       // [tile] q is laid out
+  kBarS = 2,                       // [tile][buffer] S is complete
+  kBarP = 6,                       // [tile][buffer] P is written
+  kBarFull = 10,                   // [stage] keys and values of a block are laid out
+  kBarFree = kBarFull + kStages,   // [stage] all products of a block have been made
+  kBarSegFull = kBarFree + kStages, kBarSegFree = kBarSegFull + kRing,
+  kBarTileFull = kBarSegFree + kRing, kBarTileFree = kBarTileFull + kTileRing,
+  kBars = kBarTileFree + kTileRing
+};
+
 template <int D>
 constexpr uint32_t kPanels = D / 64;                       // 64 channels of f16 are one row of the swizzle
 template <int D>
@@ -58,7 +73,7 @@ constexpr uint32_t kKBytes = kKeys * D * 2;                // of one stage of ke
 template <int D>
 constexpr uint32_t kVBytes = kKeys * D * 2;                // of one stage of values
 template <int D>
-constexpr size_t kSmem = 1024 + 2 * kQBytes<D> + 2 * kKBytes<D> + 2 * kVBytes<D>;
+constexpr size_t kSmem = 1024 + 2 * kQBytes<D> + kStages * (kKBytes<D> + kVBytes<D>);
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -138,11 +153,13 @@ __device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[16]) {
                : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
                  "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
 }
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }   // one instruction here
 __device__ __forceinline__ float as_f(uint32_t x) { return __uint_as_float(x); }
-template <int N>
-__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N>
-__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+__device__ __forceinline__ bool elect_one() {
+  uint32_t is;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+  return is != 0;
+}
 // two 32-bit sums or products in one instruction
 __device__ __forceinline__ void fma2(float& x, float& y, float a, float bx, float by, float c) {
   asm("{\n\t.reg .b64 p, q, r, s;\n\t"
@@ -157,6 +174,12 @@ __device__ __forceinline__ void add2(float& x, float& y, float a, float b) {
       : "+f"(x), "+f"(y) : "f"(a), "f"(b));
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Scores of keys first .. first + 31 to t, with nothing where there is nothing to see (keys after `see`).
+__device__ __forceinline__ void hide(uint32_t (&v)[32], int first, int see, float a, float b) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(first + j <= see ? fmaf(as_f(v[j]), a, b) : -INFINITY);
+}
 
 // ---------------------------------------------------------------------------------------------- the line of work
 // Item `tile` of a request costs first + tile * more; the first n cost sum(n).
@@ -175,16 +198,15 @@ __device__ __forceinline__ Costs costs_of(const KvArgs& a, const PromptArgs& g, 
   return c;
 }
 
-// A part of an item: key tiles [k0, k1) of n; k0 < 0: there are no more.
+// A part of an item: blocks [k0, k1) of n; k0 < 0: there are no more.
 struct __align__(16) Segment {
   int b, h, tile, k0;
   int k1, n, q0, q_len;
   long long at, len;            // the item on the line
   int kv, starts, pad[2];       // starts: the item starts in this CTA's part of the line
 };
-constexpr int kRing = 4;        // segments in the ring
 
-// The key tiles [k0, k1) of an item (n of them, at `at` of the line) that the part [from, to) of the line holds.
+// The blocks [k0, k1) of an item (n of them, at `at` of the line) that the part [from, to) of the line holds.
 __device__ __forceinline__ void cut(long long from, long long to, long long at, long long len, int n, int& k0, int& k1) {
   k0 = from <= at ? 0 : from >= at + len ? n : (int)((long long)n * (from - at) / len);
   k1 = to >= at + len ? n : to <= at ? 0 : (int)((long long)n * (to - at) / len);
@@ -197,7 +219,7 @@ struct Walk {
   Request req;
   Costs costs;
 
-  __device__ __forceinline__ int key_tiles(const KvArgs& a, const PromptArgs& g) const {
+  __device__ __forceinline__ int blocks_seen(const KvArgs& a, const PromptArgs& g) const {
     const long long rows = (long long)req.q_len * a.group;
     const int row = (int)(min((long long)(tile + 1) * kItemRows, rows) - 1);
     const int last = g.causal ? min(req.kv - req.q_len + row / a.group, req.kv - 1) : req.kv - 1;
@@ -234,7 +256,7 @@ struct Walk {
       s.at = base + costs.sum(tile);
       if (s.at >= x1) return false;
       s.len = costs.sum(tile + 1) - costs.sum(tile);
-      s.n = key_tiles(a, g);
+      s.n = blocks_seen(a, g);
       cut(x0, x1, s.at, s.len, s.n, s.k0, s.k1);
       s.b = b; s.h = h; s.tile = tile; s.q0 = req.q0; s.q_len = req.q_len; s.kv = req.kv; s.starts = s.at >= x0 ? 1 : 0;
       const bool here = s.n == 0 ? s.at >= x0 : s.k0 < s.k1;   // an item without visible keys belongs to whoever has its start
@@ -258,35 +280,39 @@ __global__ void __launch_bounds__(kThreads, 1)
 kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t q_at = base, k_at = q_at + 2 * kQBytes<D>, v_at = k_at + 2 * kKBytes<D>;
-  __shared__ __align__(8) uint64_t bars[16 + 2 * kRing];
+  const uint32_t q_at = base, k_at = q_at + 2 * kQBytes<D>, v_at = k_at + kStages * kKBytes<D>;
+  __shared__ __align__(8) uint64_t bars[kBars];
   __shared__ Segment s_ring[kRing];
-  __shared__ __align__(16) float4 s_steps[4][2];           // of the two blocks of a key tile: kstep, log2 vstep, 1 / vstep, usable
+  __shared__ __align__(16) float4 s_steps[kTileRing];      // of a block: kstep, log2 vstep, 1 / vstep, usable
+  __shared__ int s_block[kTileRing];                       // and where it is (block x kv heads + head)
   __shared__ long long sums[kThreads / 32];
   __shared__ Found found;
   __shared__ Cut s_cut[2];
   __shared__ Line s_line;
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort, s_join[2];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;   // warp: known to be uniform
   auto bar = [&](int i) { return ptx::smem_u32(&bars[i]); };
-  // [0,2) q ready, [2,4) k ready, [4,6) k free, [6,8) v ready, [8,10) v free, [10,12) S ready, [12,14) P ready, [14,16) O ready,
-  // then the ring of segments: ready, free
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      ptx::mbar_init(bar(i), 4);
-      ptx::mbar_init(bar(2 + i), kLoadWarps);
-      ptx::mbar_init(bar(4 + i), 1);
-      ptx::mbar_init(bar(6 + i), kLoadWarps);
-      ptx::mbar_init(bar(8 + i), 1);
-      ptx::mbar_init(bar(10 + i), 1);
-      ptx::mbar_init(bar(12 + i), 4);
-      ptx::mbar_init(bar(14 + i), 1);
+      ptx::mbar_init(bar(kBarQ + i), 4);
       s_cut[i].len = 0;
     }
+    for (int i = 0; i < 4; ++i) {
+      ptx::mbar_init(bar(kBarS + i), 1);
+      ptx::mbar_init(bar(kBarP + i), 4);
+    }
+    for (int i = 0; i < kStages; ++i) {
+      ptx::mbar_init(bar(kBarFull + i), kLoadWarps);
+      ptx::mbar_init(bar(kBarFree + i), 2);
+    }
     for (int i = 0; i < kRing; ++i) {
-      ptx::mbar_init(bar(16 + i), 1);
-      ptx::mbar_init(bar(16 + kRing + i), kSoftWarps + kLoadWarps + 1);
+      ptx::mbar_init(bar(kBarSegFull + i), 1);
+      ptx::mbar_init(bar(kBarSegFree + i), kSoftWarps + 3);
+    }
+    for (int i = 0; i < kTileRing; ++i) {
+      ptx::mbar_init(bar(kBarTileFull + i), 1);
+      ptx::mbar_init(bar(kBarTileFree + i), 1);
     }
     s_abort = 0;
     ptx::fence_barrier_init();
@@ -321,28 +347,93 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
-  const uint32_t tmem = s_tmem;                            // S of tile 0, 1 at columns 0, 128; O at 256, 384
+  const uint32_t tmem = s_tmem;                            // S of tile t, buffer i at column 128 t + 64 i; O at 256 + 128 t
   constexpr size_t kPitch = (size_t)kItemRows * (D + 2);   // floats of a partial: maxima, sums, output sums
   auto slot = [&](long long w, int i) { return g.split.partials + ((size_t)w * 2 + i) * kPitch; };
   // the next segment, by all lanes of a warp (or the one that issues)
   int seg = 0;
   uint32_t seg_phase = 0;
   auto next_segment = [&](bool& ok) {
-    ok = ptx::mbar_wait(bar(16 + seg), seg_phase, abort_flag);
+    ok = ptx::mbar_wait(bar(kBarSegFull + seg), seg_phase, abort_flag);
     return &s_ring[seg];
   };
   auto done_segment = [&]() {                              // its fields have been read
-    ptx::mbar_arrive(bar(16 + kRing + seg));
+    ptx::mbar_arrive(bar(kBarSegFree + seg));
     if (++seg == kRing) { seg = 0; seg_phase ^= 1u; }
   };
 
+  // waits until all products of a block are complete (block number st of this CTA, none before st - kStages open)
+  auto products_of = [&](int st) {
+    return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(kBarFree + st % kStages), (uint32_t)(st / kStages) & 1u, abort_flag)) != 0;
+  };
+
+  // ------------------------------------------------------------------ products of tile T, by a whole warp
+  // All lanes keep step, so that addresses and descriptors stay in uniform registers; one of them issues.
+  auto issue = [&](auto tile_of) {
+    constexpr int T = decltype(tile_of)::value;
+    constexpr uint32_t kIdescS = ptx::make_idesc(1, 0, kTile, kKeys, false);   // f16 x f16 -> f32
+    constexpr uint32_t kIdescO = ptx::make_idesc(1, 0, kTile, D, false);
+    const bool leader = elect_one();
+    int step = 0;                                          // blocks so far, of all segments
+    uint32_t q_phase = 0;
+    bool ok = true;
+    auto wait = [&](int i, uint32_t parity) { ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(i), parity, abort_flag)) != 0; };
+    auto scores = [&](int st) {                            // S of block number st into its buffer
+      if (leader) {
+#pragma unroll
+        for (uint32_t c = 0; c < kPanels<D>; ++c) {
+          const uint64_t x = ptx::smem_desc_sw128(q_at + T * kQBytes<D> + c * (kTile * 128));
+          const uint64_t y = ptx::smem_desc_sw128(k_at + (st % kStages) * kKBytes<D> + c * (kKeys * 128));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mma_f16_ss(tmem + T * kTile + (st & 1) * kKeys, x + 2 * i, y + 2 * i, kIdescS, c > 0 || i > 0);
+        }
+        ptx::mma_commit(bar(kBarS + 2 * T + (st & 1)));
+      }
+      __syncwarp();
+    };
+    while (true) {
+      const Segment* from = next_segment(ok);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok) break;
+      const int k0 = from->k0, k1 = from->k1;
+      __syncwarp();
+      if (lane == 0) done_segment(); else if (++seg == kRing) { seg = 0; seg_phase ^= 1u; }
+      if (k0 < 0) break;
+      if (k0 >= k1) continue;
+      wait(kBarQ + T, q_phase);
+      if (!ok) break;
+      ptx::tc_fence_after();
+      q_phase ^= 1u;
+      for (int st = step; st < step + 2 && st < step + k1 - k0 && ok; ++st) {
+        wait(kBarFull + st % kStages, (uint32_t)(st / kStages) & 1u);
+        if (ok) scores(st);
+      }
+      for (int k = k0; k < k1 && ok; ++k, ++step) {
+        const int stage = step % kStages, ahead = step + 2;
+        if (k + 2 < k1) wait(kBarFull + ahead % kStages, (uint32_t)(ahead / kStages) & 1u);   // long ready, off the chain P -> S
+        if (!ok) break;
+        wait(kBarP + 2 * T + (step & 1), (uint32_t)(step >> 1) & 1u);
+        if (!ok) break;
+        ptx::tc_fence_after();
+        if (leader) {
+          const uint64_t y = ptx::smem_desc_sw128(v_at + stage * kVBytes<D>);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            mma_f16_ts(tmem + 256 + T * kTile, tmem + T * kTile + (step & 1) * kKeys + 8 * i, y + 2 * i, kIdescO, k > k0 || i > 0);
+        }
+        if (k + 2 < k1) scores(ahead);
+        if (leader) ptx::mma_commit(bar(kBarFree + stage));
+        __syncwarp();
+      }
+    }
+    if (!ok && lane == 0) report_status(a.hdr, TLQ_ERR_TIMEOUT, 233);
+  };
+
   if (warp < kSoftWarps) {
-    more_registers<kSoftRegs>();
     // ------------------------------------------------------------------ softmax: a thread is a row
     const int t = warp >> 2, row_in_tile = (warp & 3) * 32 + lane;
     const uint32_t s_col = tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * kTile, o_col = s_col + 256;   // P over S
-    uint32_t s_phase = 0, o_phase = 0;
-    int step = 0;                                          // key tiles so far, of all segments
+    int step = 0;                                          // blocks so far, of all segments
     bool ok = true;
     while (true) {
       const Segment* s = next_segment(ok);
@@ -395,51 +486,45 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
           off = qs * (128.f / kUnit);
           ptx::fence_proxy_async();
           __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(bar(t));
+          if (lane == 0) ptx::mbar_arrive(bar(kBarQ + t));
         }
       }
 
       float m = -INFINITY, l = 0.f;
       for (int k = k0; k < k1; ++k, ++step) {
-        ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(10 + t), s_phase, abort_flag));
+        const int buf = (step & 1) * kKeys;
+        ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(kBarS + 2 * t + (step & 1)), (uint32_t)(step >> 1) & 1u, abort_flag));
         if (!ok) break;
-        s_phase ^= 1u;
         ptx::tc_fence_after();
-        uint32_t v[4][32];                                 // the row of S
-#pragma unroll
-        for (int c = 0; c < 4; ++c) ptx::tmem_ld32(s_col + 32 * c, v[c]);
-        const float4 w0 = s_steps[step & 3][0], w1 = s_steps[step & 3][1];
-        float a0 = fac * w0.x, a1 = fac * w1.x;
-        float b0 = fmaf(-off, a0, w0.y), b1 = fmaf(-off, a1, w1.y);
-        const int see = limit - k * kKeys;                 // last key of the tile that the row sees
-        const bool masked = __any_sync(0xFFFFFFFFu, see < kKeys - 1) || w0.w == 0.f || w1.w == 0.f;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld_wait_for(v[c]);
-        if (masked) {                                      // t itself, with nothing where there is nothing to see
-          const int see0 = w0.w == 0.f ? -1 : see, see1 = w1.w == 0.f ? -1 : see;
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const float x = fmaf(as_f(v[c][j]), c < 2 ? a0 : a1, c < 2 ? b0 : b1);
-              v[c][j] = __float_as_uint(32 * c + j <= (c < 2 ? see0 : see1) ? x : -INFINITY);
-            }
-          a0 = a1 = 1.f;
-          b0 = b1 = 0.f;
+        uint32_t v[2][32];                                 // the row of S
+        ptx::tmem_ld32(s_col + buf, v[0]);
+        ptx::tmem_ld32(s_col + buf + 32, v[1]);
+        const float4 w = s_steps[step % kTileRing];
+        float fa = fac * w.x, fb = fmaf(-off, fa, w.y);
+        const int see = w.w == 0.f ? -1 : limit - k * kKeys;   // last key of the block that the row sees
+        const bool masked = __any_sync(0xFFFFFFFFu, see < kKeys - 1);
+        tmem_ld_wait_for(v[0]);
+        tmem_ld_wait_for(v[1]);
+        if (masked) {
+          hide(v[0], 0, see, fa, fb);
+          hide(v[1], 32, see, fa, fb);
+          fa = 1.f;                                        // the hidden rows are t already
+          fb = 0.f;
         }
-        float top;
-        {
-          float r[2][4];
+        float r[4];
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
+        for (int j = 0; j < 4; ++j) r[j] = max3(as_f(v[0][j]), as_f(v[0][4 + j]), as_f(v[0][8 + j]));
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              float& x = r[c >> 1][j & 3];
-              x = (c & 1) == 0 && j < 4 ? as_f(v[c][j]) : fmaxf(x, as_f(v[c][j]));
-            }
-          top = fmaxf(fmaf(fmaxf(fmaxf(r[0][0], r[0][1]), fmaxf(r[0][2], r[0][3])), a0, b0),
-                      fmaf(fmaxf(fmaxf(r[1][0], r[1][1]), fmaxf(r[1][2], r[1][3])), a1, b1));
-        }
+        for (int j = 12; j < 28; j += 8)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r[i] = max3(r[i], as_f(v[0][j + i]), as_f(v[0][j + 4 + i]));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = max3(r[i], as_f(v[0][28 + i]), as_f(v[1][i]));
+#pragma unroll
+        for (int j = 4; j < 28; j += 8)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r[i] = max3(r[i], as_f(v[1][j + i]), as_f(v[1][j + 4 + i]));
+        const float top = fmaf(fmaxf(max3(r[0], r[1], r[2]), max3(r[3], max3(as_f(v[1][28]), as_f(v[1][29]), as_f(v[1][30])), as_f(v[1][31]))), fa, fb);
         // a maximum that has grown by more than kGrow: the output sum follows
         if (__any_sync(0xFFFFFFFFu, top > m + kGrow || (m == -INFINITY && top > -INFINITY))) {
           const float mn = fmaxf(m, top);
@@ -447,49 +532,49 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
           m = mn;
           l *= corr;
           if (k > k0) {
+            ok = products_of(step - 1);                    // P V of the block before has to be in it
+            if (!ok) break;
+            ptx::tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < D / 16; ++c) {
-              uint32_t x[16];
-              ptx::tmem_ld16(o_col + 16 * c, x);
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t x[32];
+              ptx::tmem_ld32(o_col + 32 * c, x);
               tmem_ld_wait_for(x);
 #pragma unroll
-              for (int j = 0; j < 16; ++j) x[j] = __float_as_uint(as_f(x[j]) * corr);
-              tmem_st16(o_col + 16 * c, x);
+              for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(as_f(x[j]) * corr);
+              tmem_st32(o_col + 32 * c, x);
             }
           }
         }
-        const float shift = kShift - (m == -INFINITY ? 0.f : m);
-        b0 += shift;
-        b1 += shift;
-        float sum0[2] = {0.f, 0.f}, sum1[2] = {0.f, 0.f};
+        fb += kShift - (m == -INFINITY ? 0.f : m);
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 2; ++c) {
           uint32_t p[16];
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
-            float x, y;
-            fma2(x, y, c < 2 ? a0 : a1, as_f(v[c][j]), as_f(v[c][j + 1]), c < 2 ? b0 : b1);
-            x = exp2_fast(x);
+            float y, z;
+            fma2(y, z, fa, as_f(v[c][j]), as_f(v[c][j + 1]), fb);
             y = exp2_fast(y);
-            if (c < 2) add2(sum0[0], sum0[1], x, y); else add2(sum1[0], sum1[1], x, y);
-            p[j / 2] = pack_f16(x, y);
+            z = exp2_fast(z);
+            add2(sum[0], sum[1], y, z);
+            p[j / 2] = pack_f16(y, z);
           }
-          tmem_st16(s_col + 16 * c, p);                    // all of S has been read
+          tmem_st16(s_col + buf + 16 * c, p);              // all of S has been read
         }
-        const float l0 = sum0[0] + sum0[1], l1 = sum1[0] + sum1[1];
-        l += (l0 > 0.f ? l0 * s_steps[step & 3][0].z : l0) + (l1 > 0.f ? l1 * s_steps[step & 3][1].z : l1);
+        const float both = sum[0] + sum[1];
+        l += both > 0.f ? both * w.z : both;
         tmem_st_wait();
         ptx::tc_fence_before();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(bar(12 + t));
+        if (lane == 0) ptx::mbar_arrive(bar(kBarP + 2 * t + (step & 1)));
       }
       if (!ok) break;
 
       // ---------------------------------------------------------------- leave the item
       if (k0 < k1) {
-        ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(14 + t), o_phase, abort_flag));
+        ok = products_of(step - 1);
         if (!ok) break;
-        o_phase ^= 1u;
         ptx::tc_fence_after();
       }
       {
@@ -542,83 +627,48 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     }
     if (!ok && lane == 0) report_status(a.hdr, TLQ_ERR_TIMEOUT, 230);
   } else if (warp < kSoftWarps + kLoadWarps) {
-    fewer_registers<kLoadRegs>();
     // ------------------------------------------------------------------ codes of keys and values to f16 operands
-    // A warp takes 8 rows x 64 bytes at a time.  Keys: row group (lw / panels) + i * 4 / panels of 16, the same panel for all
-    // i; values: row group lw + 4 i of a block's D / 8.  Either way the first half of the i is the tile's first block.
-    constexpr int kNum = D / 16, kGroups = 4 / kPanels<D>;   // pieces of a warp; key row groups that the warps take at a time
+    // A warp takes 8 rows x 64 bytes at a time.  Keys: row group lw / panels + i * 4 / panels of 8, the same panel for all i;
+    // values: row group lw + 4 i of D / 8.
+    constexpr int kNum = D / 32, kGroups = 4 / kPanels<D>;   // pieces of a warp; key row groups that the warps take at a time
     const int lw = warp - kSoftWarps, lr = lane & 7, piece = lane >> 3;
     const int k_row = (lw / kPanels<D>) * 8 + lr, k_panel = lw % kPanels<D>;
     const int8_t* const k_from = a.k_codes + k_row * D + k_panel * 64 + piece * 16;
     const int8_t* const v_from = a.v_codes + (lw * 8 + lr) * kKvBlock + piece * 16;
     const uint32_t swizzled0 = ((2 * piece) ^ lr) << 4, swizzled1 = ((2 * piece + 1) ^ lr) << 4;
     const uint32_t k_to = k_at + k_panel * (kKeys * 128) + k_row * 128, v_to = v_at + (lw * 8 + lr) * 128;
-    int step = 0, b = 0, h = 0, k = 0, k1 = 0, n_blocks = 0;
+    int step = 0;
     bool ok = true;
     uint4 kr[kNum], vr[kNum];
-    int phys[2];
-    float ks = 0.f, vs = 0.f;                              // steps of the block `lane` (lanes 0 and 1 of the first warp)
-    int64_t block[2];                                      // of the tile whose codes are under way, in bytes
-    bool usable[2];
-    auto advance = [&]() {                                 // to the next segment with key tiles
-      while (true) {
-        const Segment* from = next_segment(ok);
-        ok = __all_sync(0xFFFFFFFFu, ok);
-        if (!ok) return false;
-        b = from->b; h = from->h; k = from->k0; k1 = from->k1;
-        n_blocks = (from->kv + kKvBlock - 1) / kKvBlock;
-        __syncwarp();
-        if (lane == 0) done_segment(); else if (++seg == kRing) { seg = 0; seg_phase ^= 1u; }
-        if (k < 0) return false;
-        if (k < k1) return true;
-      }
-    };
-    auto look_up = [&]() {                                 // the blocks of key tile k
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        phys[i] = 2 * k + i < n_blocks ? __ldg(a.block_table + (int64_t)b * a.max_blocks + 2 * k + i) : -1;
+    int64_t block = 0;                                     // whose codes are under way
+    // the next block of the scout's ring; false at the end
+    auto look_up = [&](int at_step) {
+      const int at = at_step % kTileRing;
+      ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(kBarTileFull + at), (uint32_t)(at_step / kTileRing) & 1u, abort_flag));
+      if (!ok) return false;
+      block = (int64_t)s_block[at] * (kKvBlock * D);
+      return block >= 0;
     };
     auto load_keys = [&]() {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        usable[i] = phys[i] >= 0 && phys[i] < a.n_blocks;
-        if (!usable[i] && 2 * k + i < n_blocks) report_status(a.hdr, TLQ_ERR_SHAPE, 231);
-        const int64_t at = (int64_t)(usable[i] ? phys[i] : 0) * a.n_kv + h;
-        block[i] = at * (kKvBlock * D);
-        if (lw == 0 && lane == i) {
-          ks = __ldg(a.k_steps + at);
-          vs = __ldg(a.v_steps + at);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < kNum; ++i) {
-        // rows of the tile from k_row on, kGroups * 8 apart; a block is 64 of them
-        const int row = i * kGroups * 8;
-        kr[i] = ld_cache(k_from + block[row >> 6] + (row & 63) * D);
-      }
+      for (int i = 0; i < kNum; ++i) kr[i] = ld_cache(k_from + block + i * kGroups * 8 * D);
     };
     auto load_values = [&]() {
 #pragma unroll
-      for (int i = 0; i < kNum; ++i) vr[i] = ld_cache(v_from + block[i / (kNum / 2)] + (i % (kNum / 2)) * 32 * kKvBlock);
+      for (int i = 0; i < kNum; ++i) vr[i] = ld_cache(v_from + block + i * 32 * kKvBlock);
     };
-    bool more = advance();
+    bool more = look_up(0);
     if (more) {
-      look_up();
       load_keys();
       load_values();
     }
     while (more) {
-      const float my_ks = ks, my_vs = vs;
-      const float my_use = usable[0] && lane == 0 ? 1.f : usable[1] && lane == 1 ? 1.f : 0.f;
-      // the tile after this one
-      bool after = true;
-      if (++k >= k1) after = advance();
-      if (!ok) break;
-      if (after) look_up();
-      const int stage = step & 1;
-      const uint32_t parity = ((uint32_t)(step >> 1) & 1u) ^ 1u;
-      ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(4 + stage), parity, abort_flag));
-      if (!ok) break;
+      const int stage = step % kStages;
+      if (step >= kStages) {                               // the stage is free, and so is what the scout noted of its block
+        ok = products_of(step - kStages);
+        if (!ok) break;
+        if (lw == 0 && lane == 0) ptx::mbar_arrive(bar(kBarTileFree + (step - kStages) % kTileRing));
+      }
 #pragma unroll
       for (int i = 0; i < kNum; ++i) {
         const uint32_t to = k_to + stage * kKBytes<D> + i * kGroups * 8 * 128;
@@ -628,19 +678,12 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
         sts128(to + swizzled0, x[0], x[1], x[2], x[3]);
         sts128(to + swizzled1, x[4], x[5], x[6], x[7]);
       }
-      if (lw == 0 && lane < 2) {
-        const float v = my_vs < kStepFloor ? kStepFloor : my_vs;
-        s_steps[step & 3][lane] = make_float4(my_ks, log2f(v), 1.0f / v, my_use);
-      }
-      ptx::fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(bar(2 + stage));
-      if (after) load_keys();
-      ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(8 + stage), parity, abort_flag));
+      more = look_up(step + 1);
       if (!ok) break;
+      if (more) load_keys();
 #pragma unroll
       for (int i = 0; i < kNum; ++i) {
-        const uint32_t to = v_to + stage * kVBytes<D> + (i / (kNum / 2)) * (D * 128) + (i % (kNum / 2)) * 32 * 128;
+        const uint32_t to = v_to + stage * kVBytes<D> + i * 32 * 128;
         uint32_t x[8];
         values_to_f16(vr[i].x, x[0], x[1]); values_to_f16(vr[i].y, x[2], x[3]);
         values_to_f16(vr[i].z, x[4], x[5]); values_to_f16(vr[i].w, x[6], x[7]);
@@ -649,78 +692,16 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       }
       ptx::fence_proxy_async();
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(bar(6 + stage));
-      if (after) load_values();
+      if (lane == 0) ptx::mbar_arrive(bar(kBarFull + stage));
+      if (more) load_values();
       ++step;
-      more = after;
     }
     if (!ok && lane == 0) report_status(a.hdr, TLQ_ERR_TIMEOUT, 232);
   } else {
-    fewer_registers<kIssueRegs>();
-    if (warp == kIssueWarp && lane == 0) {
-    // ------------------------------------------------------------------ products
-    constexpr uint32_t kIdescS = ptx::make_idesc(1, 0, kTile, kKeys, false);   // f16 x f16 -> f32
-    constexpr uint32_t kIdescO = ptx::make_idesc(1, 0, kTile, D, false);
-    int step = 0;
-    uint32_t q_phase = 0, p_phase = 0;
-    bool ok = true;
-    auto wait = [&](int i, uint32_t parity) {
-      ok = ok && ptx::mbar_wait(bar(i), parity, abort_flag);
-      ptx::tc_fence_after();
-    };
-    auto scores = [&](int t, int st) {
-#pragma unroll
-      for (uint32_t c = 0; c < kPanels<D>; ++c) {
-        const uint64_t x = ptx::smem_desc_sw128(q_at + t * kQBytes<D> + c * (kTile * 128));
-        const uint64_t y = ptx::smem_desc_sw128(k_at + (st & 1) * kKBytes<D> + c * (kKeys * 128));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mma_f16_ss(tmem + t * kTile, x + 2 * i, y + 2 * i, kIdescS, c > 0 || i > 0);
-      }
-      ptx::mma_commit(bar(10 + t));
-    };
-    while (true) {
-      const Segment* from = next_segment(ok);
-      if (!ok) break;
-      struct { int k0, k1; } s = {from->k0, from->k1};
-      done_segment();
-      if (s.k0 < 0) break;
-      if (s.k0 >= s.k1) continue;
-      for (int t = 0; t < 2; ++t) wait(t, q_phase);
-      q_phase ^= 1u;
-      wait(2 + (step & 1), (uint32_t)(step >> 1) & 1u);
-      if (!ok) break;
-      scores(0, step);
-      scores(1, step);
-      ptx::mma_commit(bar(4 + (step & 1)));
-      for (int k = s.k0; k < s.k1 && ok; ++k, ++step) {
-        const int stage = step & 1;
-        wait(6 + stage, (uint32_t)(step >> 1) & 1u);
-        const bool next = k + 1 < s.k1;
-        for (int t = 0; t < 2 && ok; ++t) {
-          wait(12 + t, p_phase);
-          if (!ok) break;
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const uint64_t y = ptx::smem_desc_sw128(v_at + stage * kVBytes<D> + c * (D * 128));
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              mma_f16_ts(tmem + 256 + t * kTile, tmem + t * kTile + 32 * c + 8 * i, y + 2 * i, kIdescO, k > s.k0 || c > 0 || i > 0);
-          }
-          if (next) {
-            if (t == 0) wait(2 + ((step + 1) & 1), (uint32_t)((step + 1) >> 1) & 1u);
-            if (!ok) break;
-            scores(t, step + 1);
-          } else {
-            ptx::mma_commit(bar(14 + t));
-          }
-        }
-        if (!ok) break;
-        ptx::mma_commit(bar(8 + stage));
-        if (next) ptx::mma_commit(bar(4 + ((step + 1) & 1)));
-        p_phase ^= 1u;
-      }
-    }
-    if (!ok) report_status(a.hdr, TLQ_ERR_TIMEOUT, 233);
+    if (warp == kIssueWarp) {
+      issue(std::integral_constant<int, 0>{});
+    } else if (warp == kIssueWarp + 3) {
+      issue(std::integral_constant<int, 1>{});
     } else if (warp == kPlanWarp && lane == 0) {
       // ---------------------------------------------------------------- segments
       Walk walk;
@@ -730,20 +711,54 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
         Segment s;
         const bool more = walk.next(a, g, s);
         if (!more) s.k0 = -1;
-        if (!ptx::mbar_wait(bar(16 + kRing + seg), phase, abort_flag)) {
+        if (!ptx::mbar_wait(bar(kBarSegFree + seg), phase, abort_flag)) {
           report_status(a.hdr, TLQ_ERR_TIMEOUT, 234);
           break;
         }
         s_ring[seg] = s;
-        ptx::mbar_arrive(bar(16 + seg));
+        ptx::mbar_arrive(bar(kBarSegFull + seg));
         if (!more) break;
         if (++seg == kRing) { seg = 0; phase ^= 1u; }
       }
+    } else if (warp == kScoutWarp) {
+      // ---------------------------------------------------------------- the cache blocks to come, and their steps
+      int step = 0;
+      bool ok = true;
+      while (ok) {
+        const Segment* from = next_segment(ok);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok) break;
+        const int k0 = from->k0, k1 = from->k1, h = from->h;
+        const int32_t* table = a.block_table + (int64_t)from->b * a.max_blocks;
+        __syncwarp();
+        if (lane == 0) done_segment(); else if (++seg == kRing) { seg = 0; seg_phase ^= 1u; }
+        const int last = k0 < 0 ? k0 + 1 : k1;             // the end is passed on as a block that is none
+        for (int k = k0; k < last && ok; k += 32) {
+          const bool in = k0 >= 0 && k + lane < last;      // a lane for each of 32 blocks
+          const int phys = in ? __ldg(table + k + lane) : -1;
+          const bool usable = phys >= 0 && phys < a.n_blocks;
+          if (in && !usable) report_status(a.hdr, TLQ_ERR_SHAPE, 231);
+          const int64_t at = (int64_t)(usable ? phys : 0) * a.n_kv + h;
+          const float ks = __ldg(a.k_steps + at), vs = __ldg(a.v_steps + at), v = vs < kStepFloor ? kStepFloor : vs;
+          const float4 w = make_float4(ks, log2f(v), 1.0f / v, usable ? 1.f : 0.f);
+          for (int j = 0; j < min(32, last - k); ++j, ++step) {
+            const int to = step % kTileRing;
+            ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(kBarTileFree + to), ((uint32_t)(step / kTileRing) & 1u) ^ 1u, abort_flag));
+            if (!ok) break;
+            if (lane == j) {
+              s_steps[to] = w;
+              s_block[to] = k0 < 0 ? -1 : (int)at;
+            }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(bar(kBarTileFull + to));
+          }
+        }
+        if (k0 < 0) break;
+      }
+      if (!ok && lane == 0) report_status(a.hdr, TLQ_ERR_TIMEOUT, 235);
     }
   }
   __syncwarp();
-  // the rest is run by all warps: back to what they were launched with
-  if (warp < kSoftWarps) fewer_registers<kLaunchRegs>(); else more_registers<kLaunchRegs>();
   if (*abort_flag != 0)
     for (int i = 0; i < 1000; ++i) __nanosleep(1000);      // products under way end before their memory is given back
   ptx::tc_fence_before();
@@ -766,7 +781,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       cut(s_line.x0, s_line.x1, c.at, c.len, c.n, k0, k1);
       int32_t* counter = g.split.counters + worker_of(c.at);
       __threadfence();                                     // the CTA's partials, which the barrier has ordered before this
-      const int before = atomicAdd(counter, k1 - k0);      // key tiles of the item that are done
+      const int before = atomicAdd(counter, k1 - k0);      // blocks of the item that are done
       if (before + (k1 - k0) == c.n) {
         *counter = 0;
         s_join[threadIdx.x] = 1;

@@ -12,7 +12,8 @@ constexpr size_t kCounterBytes = kMaxWorkers * sizeof(int32_t);
 int check_cache(const tlq_kv_cache* c) {
   if (c == nullptr || c->struct_size != sizeof(tlq_kv_cache)) return TLQ_ERR_INVALID_ARG;
   if (c->head_dim != 64 && c->head_dim != 128) return TLQ_ERR_UNSUPPORTED;
-  if (c->n_kv_heads < 1 || c->n_kv_heads > 1024 || c->n_blocks < 1) return TLQ_ERR_SHAPE;
+  if (c->n_kv_heads < 1 || c->n_kv_heads > 1024 || c->n_blocks < 1 || (int64_t)c->n_blocks * c->n_kv_heads > 0x7FFFFFFFLL)
+    return TLQ_ERR_SHAPE;
   if (c->k_codes == nullptr || c->v_codes == nullptr || c->k_steps == nullptr || c->v_steps == nullptr)
     return TLQ_ERR_INVALID_ARG;
   if (!aligned16(c->k_codes) || !aligned16(c->v_codes)) return TLQ_ERR_ALIGN;
