@@ -32,13 +32,15 @@ namespace {
 
 constexpr int kTile = 128, kItemRows = 256, kKeys = kKvBlock, kStages = 4;
 constexpr int kSoftWarps = 8, kLoadWarps = 4, kIssueWarp = kSoftWarps + kLoadWarps, kPlanWarp = kIssueWarp + 1, kScoutWarp = kIssueWarp + 2;
-constexpr int kThreads = 512;
+constexpr int kThreads = 512;                              // four groups of four warps
+// registers of a thread of each role: 2 x 176 + 72 + 88 = 4 x 128, what the block is launched with
+constexpr int kSoftRegs = 176, kLoadRegs = 72, kIssueRegs = 88, kLaunchRegs = 128;
 constexpr float kShift = 11.f, kGrow = 4.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kStepFloor = 7.8886090522101181e-31f;      // 2^-100, as in kv_attention.cu
 constexpr float kUnit = 16777216.f;                        // 2^24
 constexpr int kMinTiles = 12;                              // blocks of a CTA's part, at least
-constexpr int kItemCost = 4;                               // what an item costs beside its blocks, in blocks
+constexpr int kItemCost = 12;                              // what an item costs beside its blocks, in blocks
 
 struct PromptArgs {
   const uint16_t* q;
@@ -92,6 +94,11 @@ __device__ __forceinline__ uint4 ld_cache(const int8_t* p) {
 }
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
 }
 // (code + 128) 2^-24 as f16, and exactly the code: see kv_attention.cu
 __device__ __forceinline__ void keys_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
@@ -155,6 +162,16 @@ __device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[16]) {
 }
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }   // one instruction here
 __device__ __forceinline__ float as_f(uint32_t x) { return __uint_as_float(x); }
+// floor(log2 x) of a finite x > 0 (-126 for the smallest), else 0; and 2^n for n in [-126, 127]
+__device__ __forceinline__ int exponent_of(float x) {
+  const int e = (int)(__float_as_uint(x) >> 23);
+  return x == 0.f || e == 255 ? 0 : max(e, 1) - 127;
+}
+__device__ __forceinline__ float power_of_two(int n) { return __uint_as_float((uint32_t)(n + 127) << 23); }
+template <int N>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 __device__ __forceinline__ bool elect_one() {
   uint32_t is;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
@@ -430,9 +447,11 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
   };
 
   if (warp < kSoftWarps) {
+    more_registers<kSoftRegs>();
     // ------------------------------------------------------------------ softmax: a thread is a row
     const int t = warp >> 2, row_in_tile = (warp & 3) * 32 + lane;
     const uint32_t s_col = tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * kTile, o_col = s_col + 256;   // P over S
+    constexpr int kRowLanes = D / 8, kRowsAtOnce = 32 / kRowLanes;       // lanes that hold a row, 16 bytes each
     int step = 0;                                          // blocks so far, of all segments
     bool ok = true;
     while (true) {
@@ -444,50 +463,67 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
         Cut* c = &s_cut[s->starts];
         c->at = s->at; c->len = s->len; c->b = s->b; c->h = s->h; c->tile = s->tile; c->n = s->n;
       }
-      int limit;
+      const int row = s->tile * kItemRows + t * kTile + row_in_tile, token = row / a.group;
+      const bool live = token < s->q_len;
+      const int limit = !live ? -1 : g.causal ? min(s->kv - s->q_len + token, s->kv - 1) : s->kv - 1;
       float fac = 0.f, off = 0.f;
-      {
-        // the row of q: a power of two brings it into the range of f16
-        const int row = s->tile * kItemRows + t * kTile + row_in_tile, token = row / a.group;
-        const bool live = token < s->q_len;
-        limit = !live ? -1 : g.causal ? min(s->kv - s->q_len + token, s->kv - 1) : s->kv - 1;
-        if (k0 < k1) {
-          const uint16_t* p = g.q;
-          if (live) p += (int64_t)(s->q0 + token) * g.ldq + (int64_t)(s->h * a.group + row - token * a.group) * D;
-          uint4 v[D / 8];
+      if (k0 < k1) {
+        // The warp's 32 rows of q, kRowLanes lanes to a row: whole rows come in and go out.  A power of two brings a row into
+        // the range of f16.
+        const int64_t from = live ? (int64_t)(s->q0 + token) * g.ldq + (int64_t)(s->h * a.group + row - token * a.group) * D : -1;
+        uint4 v[D / 8];
 #pragma unroll
-          for (int i = 0; i < D / 8; ++i) v[i] = live ? __ldg(reinterpret_cast<const uint4*>(p) + i) : make_uint4(0, 0, 0, 0);
-          float top = 0.f;
-#pragma unroll
-          for (int i = 0; i < D / 8; ++i) {
-            float e[8];
-            unpack8(v[i], e);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(e[j]));
-          }
-          const int ex = top > 0.f && top <= 3.4e38f ? ilogbf(top) : 0;
-          const float d0 = ldexpf(1.0f, -(ex / 2)), d1 = ldexpf(1.0f, -(ex - ex / 2));
-          const uint32_t q_row = q_at + t * kQBytes<D> + row_in_tile * 128;
-          float qs = 0.f;
-#pragma unroll
-          for (int i = 0; i < D / 8; ++i) {
-            float e[8];
-            unpack8(v[i], e);
-            uint32_t w[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              w[j] = pack_f16(e[2 * j] * d0 * d1, e[2 * j + 1] * d0 * d1);
-              const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
-              qs += y.x + y.y;
-            }
-            sts128(q_row + (i >> 3) * (kTile * 128) + (((i & 7) ^ (row_in_tile & 7)) << 4), w[0], w[1], w[2], w[3]);
-          }
-          fac = ldexpf(g.scale_log2, ex + 24);
-          off = qs * (128.f / kUnit);
-          ptx::fence_proxy_async();
-          __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(bar(kBarQ + t));
+        for (int i = 0; i < D / 8; ++i) {
+          const int64_t p = __shfl_sync(0xFFFFFFFFu, from, i * kRowsAtOnce + lane / kRowLanes);
+          v[i] = p >= 0 ? __ldg(reinterpret_cast<const uint4*>(g.q + p) + lane % kRowLanes) : make_uint4(0, 0, 0, 0);
         }
+        // (all rows advance together: every shuffle of one would otherwise wait for the one before it)
+        float x[D / 8];
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          float e[8];
+          unpack8(v[i], e);
+          x[i] = 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[i] = fmaxf(x[i], fabsf(e[j]));
+        }
+#pragma unroll
+        for (int d = kRowLanes / 2; d > 0; d >>= 1)
+#pragma unroll
+          for (int i = 0; i < D / 8; ++i) x[i] = fmaxf(x[i], __shfl_xor_sync(0xFFFFFFFFu, x[i], d));
+        int ex = 0;
+        const int owner = (lane % kRowsAtOnce) * kRowLanes;   // the lane that has this lane's row, when its turn comes
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          const int r = (warp & 3) * 32 + i * kRowsAtOnce + lane / kRowLanes, piece = lane % kRowLanes;
+          const int y = exponent_of(x[i]), their_y = __shfl_sync(0xFFFFFFFFu, y, owner);
+          if (lane / kRowsAtOnce == i) ex = their_y;
+          const float d0 = power_of_two(-(y / 2)), d1 = power_of_two(-(y - y / 2));
+          float e[8];
+          unpack8(v[i], e);
+          uint32_t w[4];
+          x[i] = 0.f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            w[j] = pack_f16(e[2 * j] * d0 * d1, e[2 * j + 1] * d0 * d1);
+            const float2 z = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+            x[i] += z.x + z.y;
+          }
+          sts128(q_at + t * kQBytes<D> + (piece >> 3) * (kTile * 128) + r * 128 + (((piece & 7) ^ (r & 7)) << 4), w[0], w[1], w[2], w[3]);
+        }
+#pragma unroll
+        for (int d = kRowLanes / 2; d > 0; d >>= 1)
+#pragma unroll
+          for (int i = 0; i < D / 8; ++i) x[i] += __shfl_xor_sync(0xFFFFFFFFu, x[i], d);
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          const float qs = __shfl_sync(0xFFFFFFFFu, x[i], owner);
+          if (lane / kRowsAtOnce == i) off = qs * (128.f / kUnit);
+        }
+        fac = ldexpf(g.scale_log2, ex + 24);
+        ptx::fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(bar(kBarQ + t));
       }
 
       float m = -INFINITY, l = 0.f;
@@ -581,10 +617,11 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
         const bool none = m == -INFINITY && l == 0.f;      // a row that sees nothing (a NaN row has a NaN sum)
         const bool whole = k0 == 0 && k1 == s->n;
         const float inv = none ? 0.f : 1.0f / l;
-        const int r = t * kTile + row_in_tile, row = s->tile * kItemRows + r, token = row / a.group;
-        const bool live = token < s->q_len;
-        const int64_t at = (int64_t)(s->q0 + token) * a.n_heads + s->h * a.group + row - token * a.group;
-        float* part = slot(blockIdx.x, s->starts);
+        const int64_t at = live ? (int64_t)(s->q0 + token) * a.n_heads + s->h * a.group + row - token * a.group : -1;
+        // through the shared memory of the warp's own rows of q, which nobody reads any more, so that whole rows are stored:
+        // all channels as bf16, in the layout of q, or 32 channels at a time as they are (for a partial)
+        const uint32_t mine = q_at + t * kQBytes<D> + (warp & 3) * (32 * 128);
+        float* part = slot(blockIdx.x, s->starts) + 2 * kItemRows + (size_t)(t * kTile + (warp & 3) * 32) * D;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
           uint32_t v[32];
@@ -595,8 +632,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = 0u;
           }
-          if (live && whole) {
-            uint4* to = reinterpret_cast<uint4*>(g.out + at * D + 32 * c);
+          if (whole) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               uint32_t y[4];
@@ -606,19 +642,33 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
                                                                none ? 0.f : as_f(v[8 * i + 2 * j + 1]) * inv);
                 y[j] = *reinterpret_cast<const uint32_t*>(&z);
               }
-              to[i] = make_uint4(y[0], y[1], y[2], y[3]);
+              sts128(mine + (c >> 1) * (kTile * 128) + lane * 128 + (((4 * (c & 1) + i) ^ (lane & 7)) << 4), y[0], y[1], y[2], y[3]);
             }
-          } else if (live) {
-            uint4* to = reinterpret_cast<uint4*>(part + 2 * kItemRows + (size_t)r * D + 32 * c);
+          } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) to[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            for (int i = 0; i < 8; ++i) sts128(mine + lane * 128 + ((i ^ (lane & 7)) << 4), v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int r = 4 * i + (lane >> 3), piece = lane & 7;
+              reinterpret_cast<uint4*>(part + (size_t)r * D + 32 * c)[piece] = lds128(mine + r * 128 + ((piece ^ (r & 7)) << 4));
+            }
           }
           __syncwarp();
         }
-        if (live && whole && g.lse != nullptr) g.lse[at] = none ? -INFINITY : kLn2 * (log2f(l) + m - kShift);
-        if (live && !whole) {
-          part[r] = m;
-          part[kItemRows + r] = l;
+        if (whole) {
+#pragma unroll
+          for (int i = 0; i < D / 8; ++i) {
+            const int r = i * kRowsAtOnce + lane / kRowLanes, piece = lane % kRowLanes;
+            const int64_t to = __shfl_sync(0xFFFFFFFFu, at, r);
+            const uint4 y = lds128(mine + (piece >> 3) * (kTile * 128) + r * 128 + (((piece & 7) ^ (r & 7)) << 4));
+            if (to >= 0) reinterpret_cast<uint4*>(g.out + to * D)[piece] = y;
+          }
+          if (live && g.lse != nullptr) g.lse[at] = none ? -INFINITY : kLn2 * (log2f(l) + m - kShift);
+        } else {
+          float* stats = slot(blockIdx.x, s->starts) + t * kTile + row_in_tile;
+          stats[0] = m;
+          stats[kItemRows] = l;
         }
       }
       ptx::tc_fence_before();
@@ -627,6 +677,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     }
     if (!ok && lane == 0) report_status(a.hdr, TLQ_ERR_TIMEOUT, 230);
   } else if (warp < kSoftWarps + kLoadWarps) {
+    fewer_registers<kLoadRegs>();
     // ------------------------------------------------------------------ codes of keys and values to f16 operands
     // A warp takes 8 rows x 64 bytes at a time.  Keys: row group lw / panels + i * 4 / panels of 8, the same panel for all i;
     // values: row group lw + 4 i of D / 8.
@@ -698,6 +749,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     }
     if (!ok && lane == 0) report_status(a.hdr, TLQ_ERR_TIMEOUT, 232);
   } else {
+    fewer_registers<kIssueRegs>();
     if (warp == kIssueWarp) {
       issue(std::integral_constant<int, 0>{});
     } else if (warp == kIssueWarp + 3) {
@@ -759,6 +811,8 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     }
   }
   __syncwarp();
+  // the rest is run by all warps: back to what they were launched with
+  if (warp < kSoftWarps) fewer_registers<kLaunchRegs>(); else more_registers<kLaunchRegs>();
   if (*abort_flag != 0)
     for (int i = 0; i < 1000; ++i) __nanosleep(1000);      // products under way end before their memory is given back
   ptx::tc_fence_before();
@@ -796,35 +850,72 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     const Request req = load_request(a, c.b);
     const long long rows = (long long)req.q_len * a.group;
     const long long first = worker_of(c.at), final = worker_of(c.at + c.len - 1);
-    for (int e = threadIdx.x; e < kItemRows * (D / 4); e += kThreads) {
-      const int r = e / (D / 4), d = (e % (D / 4)) * 4;
-      const int row = c.tile * kItemRows + r;
-      if (row >= rows) break;
+    // the parts of the CTAs that share the item: number w is at part(w) where it has any blocks
+    auto has = [&](long long w) {
+      int k0, k1;
+      cut(edge(w), edge(w + 1), c.at, c.len, c.n, k0, k1);
+      return k0 < k1;
+    };
+    auto part = [&](long long w) { return (const float*)slot(w, c.at >= edge(w) ? 1 : 0); };
+    // maximum and sum of every row
+    float* const s_m = reinterpret_cast<float*>(smem_raw);
+    float* const s_inv = s_m + kItemRows;
+    if (threadIdx.x < kItemRows) {
+      const int r = threadIdx.x, row = c.tile * kItemRows + r;
       float mm = -INFINITY, den = 0.f;
-      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (long long w = first; w <= final; ++w) {
-        int k0, k1;
-        cut(edge(w), edge(w + 1), c.at, c.len, c.n, k0, k1);
-        if (k0 >= k1) continue;
-        const float* p = slot(w, c.at >= edge(w) ? 1 : 0);
-        const float m = __ldcg(p + r), l = __ldcg(p + kItemRows + r);
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(p + 2 * kItemRows) + e);
-        const float mn = fmaxf(mm, m), mu = mn == -INFINITY ? 0.f : mn;
-        const float f = exp2_fast(mm - mu), h = exp2_fast(m - mu);
-        mm = mn;
-        den = den * f + l * h;
-        sum.x = sum.x * f + v.x * h; sum.y = sum.y * f + v.y * h;
-        sum.z = sum.z * f + v.z * h; sum.w = sum.w * f + v.w * h;
-      }
-      const int64_t at = (int64_t)(req.q0 + row / a.group) * a.n_heads + c.h * a.group + row % a.group;
+#pragma unroll 4
+      for (long long w = first; w <= final; ++w)
+        if (has(w)) mm = fmaxf(mm, __ldcg(part(w) + r));
+      const float mu = mm == -INFINITY ? 0.f : mm;
+#pragma unroll 4
+      for (long long w = first; w <= final; ++w)
+        if (has(w)) den += exp2_fast(__ldcg(part(w) + r) - mu) * __ldcg(part(w) + kItemRows + r);
       const bool none = mm == -INFINITY && den == 0.f;
-      const float inv = none ? 0.f : 1.0f / den;
-      const __nv_bfloat162 y0 = __floats2bfloat162_rn(none ? 0.f : sum.x * inv, none ? 0.f : sum.y * inv);
-      const __nv_bfloat162 y1 = __floats2bfloat162_rn(none ? 0.f : sum.z * inv, none ? 0.f : sum.w * inv);
-      *reinterpret_cast<uint2*>(g.out + at * D + d) =
-          make_uint2(*reinterpret_cast<const uint32_t*>(&y0), *reinterpret_cast<const uint32_t*>(&y1));
-      if (d == 0 && g.lse != nullptr) g.lse[at] = none ? -INFINITY : kLn2 * (log2f(den) + mm - kShift);
+      s_m[r] = mu;
+      s_inv[r] = none ? 0.f : 1.0f / den;
+      if (row < rows && g.lse != nullptr)
+        g.lse[(int64_t)(req.q0 + row / a.group) * a.n_heads + c.h * a.group + row % a.group] =
+            none ? -INFINITY : kLn2 * (log2f(den) + mm - kShift);
     }
+    __syncthreads();
+    constexpr int kEach = 8;                               // pieces of four channels of a thread, whose loads are under way at once
+    for (int e0 = 0; e0 < kItemRows * (D / 4); e0 += kThreads * kEach) {
+      float4 sum[kEach];
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (long long w = first; w <= final; ++w) {
+        if (!has(w)) continue;
+        const float* p = part(w);
+        float4 v[kEach];
+        float f[kEach];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+          const int e = e0 + j * kThreads + (int)threadIdx.x;
+          v[j] = __ldcg(reinterpret_cast<const float4*>(p + 2 * kItemRows) + e);
+          f[j] = __ldcg(p + e / (D / 4));
+        }
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+          const int e = e0 + j * kThreads + (int)threadIdx.x;
+          const float x = exp2_fast(f[j] - s_m[e / (D / 4)]);
+          sum[j].x = fmaf(v[j].x, x, sum[j].x); sum[j].y = fmaf(v[j].y, x, sum[j].y);
+          sum[j].z = fmaf(v[j].z, x, sum[j].z); sum[j].w = fmaf(v[j].w, x, sum[j].w);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        const int e = e0 + j * kThreads + (int)threadIdx.x, r = e / (D / 4), d = (e % (D / 4)) * 4;
+        const int row = c.tile * kItemRows + r;
+        if (row >= rows) continue;
+        const int64_t at = (int64_t)(req.q0 + row / a.group) * a.n_heads + c.h * a.group + row % a.group;
+        const float inv = s_inv[r];
+        const __nv_bfloat162 y0 = __floats2bfloat162_rn(inv == 0.f ? 0.f : sum[j].x * inv, inv == 0.f ? 0.f : sum[j].y * inv);
+        const __nv_bfloat162 y1 = __floats2bfloat162_rn(inv == 0.f ? 0.f : sum[j].z * inv, inv == 0.f ? 0.f : sum[j].w * inv);
+        *reinterpret_cast<uint2*>(g.out + at * D + d) =
+            make_uint2(*reinterpret_cast<const uint32_t*>(&y0), *reinterpret_cast<const uint32_t*>(&y1));
+      }
+    }
+    __syncthreads();
   }
 }
 
