@@ -55,11 +55,14 @@ inline int once_per_device(OncePerDevice& state, F configure) {
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline int have_device() {
+  static bool found = false;             // devices do not come and go while a process runs
+  if (found) return TLQ_OK;
   int n = 0;
   if (cudaGetDeviceCount(&n) != cudaSuccess || n < 1) {
     cudaGetLastError();
     return TLQ_ERR_CUDA;
   }
+  found = true;
   return TLQ_OK;
 }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }

@@ -312,6 +312,7 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
   }
   if (threadIdx.x < 2) s_cta[threadIdx.x].begin = s_cta[threadIdx.x].end = 0;
   if (lane == 0) s_has[warp] = 0;
+  after_previous();
   auto count_units = [&](int b) { return units_of(a, load_request(a, b), kRows, g.max_rows).total; };
   long long total = 0;
   for (int b0 = 0; b0 < a.B; b0 += kThreads) {
@@ -728,8 +729,7 @@ int launch(const KvArgs& a, const AttnArgs& g, cudaStream_t st) {
   const int sms = device_sm_count();
   if (sms <= 0) return TLQ_ERR_CUDA;
   const int grid = sms < kMaxWorkers ? sms : kMaxWorkers;
-  kv_attention_kernel<D, NT><<<grid, kThreads, kRingBytes<D>, st>>>(a, g);
-  return after_launch();
+  return launch_next(kv_attention_kernel<D, NT>, dim3((unsigned)grid), kThreads, kRingBytes<D>, 1, st, a, g);
 }
 
 }  // namespace

@@ -336,6 +336,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
   }
   volatile int* abort_flag = &s_abort;
 
+  after_previous();
   // ---------------------------------------------------------------- this CTA's part of the line
   auto cost_of = [&](int b) {
     const Costs c = costs_of(a, g, load_request(a, b));
@@ -928,8 +929,7 @@ int launch(const KvArgs& a, const PromptArgs& g, cudaStream_t st) {
   if (rc != TLQ_OK) return rc;
   const int sms = device_sm_count();
   if (sms <= 0) return TLQ_ERR_CUDA;
-  kv_prompt_kernel<D><<<sms < kMaxWorkers ? sms : kMaxWorkers, kThreads, kSmem<D>, st>>>(a, g);
-  return after_launch();
+  return launch_next(kv_prompt_kernel<D>, dim3((unsigned)(sms < kMaxWorkers ? sms : kMaxWorkers)), kThreads, kSmem<D>, 1, st, a, g);
 }
 
 }  // namespace

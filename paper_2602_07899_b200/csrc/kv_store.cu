@@ -13,7 +13,7 @@
 //
 // Bound: bytes.  The rows are read once and everything is kept in registers between the maximum and the codes.  One CTA
 // owns a cache block of one head (its tokens lie in one request), because its step needs all of them; the remaining CTAs
-// stream query rows, 64 per CTA.  Values lie channel by token in the cache (what a matrix instruction over tokens
+// stream query rows, four per thread group at once.  Values lie channel by token in the cache (what a matrix instruction over tokens
 // reads), so a CTA turns its 64 x D bytes in shared memory and writes rows of 64 bytes.
 #include "serve.cuh"
 
@@ -42,14 +42,25 @@ struct Row {
   float lo[4], hi[4];
 };
 
+// The same channels as they lie in memory.
+struct Raw {
+  uint2 lo, hi;
+};
 template <int D>
-__device__ __forceinline__ void load_row(Row<D>& r, const uint16_t* p, int l) {
-  const uint2 a = *reinterpret_cast<const uint2*>(p + 4 * l);
-  const uint2 b = *reinterpret_cast<const uint2*>(p + D / 2 + 4 * l);
-  r.lo[0] = __uint_as_float(a.x << 16); r.lo[1] = __uint_as_float(a.x & 0xFFFF0000u);
-  r.lo[2] = __uint_as_float(a.y << 16); r.lo[3] = __uint_as_float(a.y & 0xFFFF0000u);
-  r.hi[0] = __uint_as_float(b.x << 16); r.hi[1] = __uint_as_float(b.x & 0xFFFF0000u);
-  r.hi[2] = __uint_as_float(b.y << 16); r.hi[3] = __uint_as_float(b.y & 0xFFFF0000u);
+__device__ __forceinline__ Raw load_raw(const uint16_t* p, int l) {
+  Raw r;
+  r.lo = __ldg(reinterpret_cast<const uint2*>(p + 4 * l));
+  r.hi = __ldg(reinterpret_cast<const uint2*>(p + D / 2 + 4 * l));
+  return r;
+}
+template <int D>
+__device__ __forceinline__ Row<D> floats(const Raw& w) {
+  Row<D> r;
+  r.lo[0] = __uint_as_float(w.lo.x << 16); r.lo[1] = __uint_as_float(w.lo.x & 0xFFFF0000u);
+  r.lo[2] = __uint_as_float(w.lo.y << 16); r.lo[3] = __uint_as_float(w.lo.y & 0xFFFF0000u);
+  r.hi[0] = __uint_as_float(w.hi.x << 16); r.hi[1] = __uint_as_float(w.hi.x & 0xFFFF0000u);
+  r.hi[2] = __uint_as_float(w.hi.y << 16); r.hi[3] = __uint_as_float(w.hi.y & 0xFFFF0000u);
+  return r;
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
@@ -78,39 +89,46 @@ __device__ __forceinline__ void norm_row(Row<D>& r, const Row<D>& w, float eps) 
   }
 }
 
-template <int D>
-__device__ __forceinline__ void rotate_row(Row<D>& r, const RopeArgs& rope, int64_t T, int64_t token, int l,
-                                           WorkspaceHeader* hdr) {
+// Cosines and sines of the lane's four pairs for one token.
+struct Angles {
   float c[4], s[4];
+};
+template <int D>
+__device__ __forceinline__ Angles load_angles(const RopeArgs& rope, int64_t T, int64_t token, int l, WorkspaceHeader* hdr) {
+  Angles g;
   if (rope.n_axes == 1) {
-    int64_t pos = rope.positions[token];
+    int64_t pos = __ldg(rope.positions + token);
     if (pos < 0 || pos >= rope.n_positions) {
       report_status(hdr, TLQ_ERR_SHAPE, 201);
       pos = 0;
     }
-    const float4 cc = *reinterpret_cast<const float4*>(rope.cos_sin + pos * D + 4 * l);
-    const float4 ss = *reinterpret_cast<const float4*>(rope.cos_sin + pos * D + D / 2 + 4 * l);
-    c[0] = cc.x; c[1] = cc.y; c[2] = cc.z; c[3] = cc.w;
-    s[0] = ss.x; s[1] = ss.y; s[2] = ss.z; s[3] = ss.w;
+    const float4 c = __ldg(reinterpret_cast<const float4*>(rope.cos_sin + pos * D + 4 * l));
+    const float4 s = __ldg(reinterpret_cast<const float4*>(rope.cos_sin + pos * D + D / 2 + 4 * l));
+    g.c[0] = c.x; g.c[1] = c.y; g.c[2] = c.z; g.c[3] = c.w;
+    g.s[0] = s.x; g.s[1] = s.y; g.s[2] = s.z; g.s[3] = s.w;
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int pair = 4 * l + j;
       const int axis = (pair >= rope.pairs_end[0] ? 1 : 0) + (pair >= rope.pairs_end[1] ? 1 : 0);
-      int64_t pos = rope.positions[axis * T + token];
+      int64_t pos = __ldg(rope.positions + axis * T + token);
       if (pos < 0 || pos >= rope.n_positions) {
         report_status(hdr, TLQ_ERR_SHAPE, 201);
         pos = 0;
       }
-      c[j] = rope.cos_sin[pos * D + pair];
-      s[j] = rope.cos_sin[pos * D + D / 2 + pair];
+      g.c[j] = __ldg(rope.cos_sin + pos * D + pair);
+      g.s[j] = __ldg(rope.cos_sin + pos * D + D / 2 + pair);
     }
   }
+  return g;
+}
+template <int D>
+__device__ __forceinline__ void rotate_row(Row<D>& r, const Angles& g) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const float a = r.lo[j], b = r.hi[j];
-    r.lo[j] = a * c[j] - b * s[j];
-    r.hi[j] = b * c[j] + a * s[j];
+    r.lo[j] = a * g.c[j] - b * g.s[j];
+    r.hi[j] = b * g.c[j] + a * g.s[j];
   }
 }
 
@@ -126,35 +144,46 @@ __device__ __forceinline__ int to_code(float x, float step) {
   return (int)fminf(fmaxf(q, -127.f), 127.f) * (q == q ? 1 : 0);
 }
 
+constexpr int kSweepsQ = 4;                          // sweeps of a CTA over query rows whose loads are under way at once
+constexpr int kPitch = kKvBlock + 4;                 // bytes of a channel in `turned`: neighbouring channels in other banks
+
 template <int D>
-__global__ void __launch_bounds__(kStoreThreads)
+__global__ void __launch_bounds__(kStoreThreads, 3)
 kv_store_kernel(const KvArgs a, const StoreArgs g) {
   constexpr int kLanes = D / 8;                      // lanes of a row
   constexpr int kRows = kStoreThreads / kLanes;      // rows of one sweep
   constexpr int kSweeps = kKvBlock / kRows;
   const int l = threadIdx.x % kLanes, row = threadIdx.x / kLanes;
   const bool turn = g.rope.positions != nullptr;
+  after_previous();
 
   if (blockIdx.x >= g.kv_ctas) {
-    // ------------------------------------------------------------------ queries: 64 rows of (token, head)
-    const int64_t first = (int64_t)(blockIdx.x - g.kv_ctas) * kKvBlock;
-    const int64_t rows = a.T * a.n_heads;
+    // ------------------------------------------------------------------ queries: kSweepsQ sweeps over rows of (token, head)
+    const unsigned first = (blockIdx.x - g.kv_ctas) * (unsigned)(kSweepsQ * kRows) + (unsigned)row;
+    const unsigned rows = (unsigned)(a.T * a.n_heads);
     Row<D> w{};
-    if (g.q_norm != nullptr) load_row(w, g.q_norm, l);
-    Row<D> x[kSweeps];
+    if (g.q_norm != nullptr) w = floats<D>(load_raw<D>(g.q_norm, l));
+    Raw x[kSweepsQ];
+    unsigned token[kSweepsQ];
 #pragma unroll
-    for (int i = 0; i < kSweeps; ++i) {
-      const int64_t r = first + i * kRows + row;
-      if (r < rows) load_row(x[i], g.qkv + (r / a.n_heads) * g.ld + (r % a.n_heads) * D, l);
-      else x[i] = Row<D>{};
+    for (int i = 0; i < kSweepsQ; ++i) {
+      const unsigned r = first + (unsigned)(i * kRows);
+      token[i] = r / (unsigned)a.n_heads;
+      if (r < rows) x[i] = load_raw<D>(g.qkv + (int64_t)token[i] * g.ld + (int64_t)(r - token[i] * (unsigned)a.n_heads) * D, l);
+      else x[i] = Raw{};
     }
+    Angles turns{};
 #pragma unroll
-    for (int i = 0; i < kSweeps; ++i) {
-      const int64_t r = first + i * kRows + row;
-      if (g.q_norm != nullptr) norm_row(x[i], w, g.eps);
+    for (int i = 0; i < kSweepsQ; ++i) {
+      const unsigned r = first + (unsigned)(i * kRows);
+      Row<D> y = floats<D>(x[i]);
+      if (g.q_norm != nullptr) norm_row(y, w, g.eps);
       if (r >= rows) continue;
-      if (turn) rotate_row(x[i], g.rope, a.T, r / a.n_heads, l, a.hdr);
-      store_row<D>(g.q_out + r * D, x[i].lo, x[i].hi, l);
+      if (turn) {
+        if (i == 0 || token[i] != token[i - 1]) turns = load_angles<D>(g.rope, a.T, token[i], l, a.hdr);   // heads of a token share them
+        rotate_row(y, turns);
+      }
+      store_row<D>(g.q_out + (int64_t)r * D, y.lo, y.hi, l);
     }
     return;
   }
@@ -163,7 +192,7 @@ kv_store_kernel(const KvArgs a, const StoreArgs g) {
   __shared__ long long sums[kStoreThreads / 32];
   __shared__ Found found;
   __shared__ float tops[2][kStoreThreads / 32];
-  __shared__ __align__(16) int8_t turned[D][kKvBlock];
+  __shared__ __align__(16) int8_t turned[D * kPitch];
   const int h = blockIdx.x % a.n_kv;
   auto blocks_of = [&](int b) -> long long {
     const Request r = load_request(a, b);
@@ -185,33 +214,34 @@ kv_store_kernel(const KvArgs a, const StoreArgs g) {
   const int off0 = p0 - blk * kKvBlock, n_new = p1 - p0;
   const int64_t tok0 = (int64_t)req.q0 + (p0 - begin);
 
+  Raw kraw[kSweeps], vraw[kSweeps];
+#pragma unroll
+  for (int i = 0; i < kSweeps; ++i) {
+    const int n = i * kRows + row;
+    kraw[i] = vraw[i] = Raw{};
+    if (n < n_new) {
+      const uint16_t* p = g.qkv + (tok0 + n) * g.ld + (int64_t)(a.n_heads + h) * D;
+      kraw[i] = load_raw<D>(p, l);
+      vraw[i] = load_raw<D>(p + (int64_t)a.n_kv * D, l);
+    }
+  }
   Row<D> w{};
-  if (g.k_norm != nullptr) load_row(w, g.k_norm, l);
-  Row<D> kx[kSweeps], vx[kSweeps];
+  if (g.k_norm != nullptr) w = floats<D>(load_raw<D>(g.k_norm, l));
+  Row<D> kx[kSweeps];
   float ktop = 0.f, vtop = 0.f;
   bool odd = false;
 #pragma unroll
   for (int i = 0; i < kSweeps; ++i) {
     const int n = i * kRows + row;
-    if (n < n_new) {
-      const uint16_t* p = g.qkv + (tok0 + n) * g.ld + (int64_t)(a.n_heads + h) * D;
-      load_row(kx[i], p, l);
-      load_row(vx[i], p + (int64_t)a.n_kv * D, l);
-    } else {
-      kx[i] = Row<D>{};
-      vx[i] = Row<D>{};
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < kSweeps; ++i) {
-    const int n = i * kRows + row;
+    kx[i] = floats<D>(kraw[i]);
     if (g.k_norm != nullptr) norm_row(kx[i], w, g.eps);
     if (n < n_new) {
-      if (turn) rotate_row(kx[i], g.rope, a.T, tok0 + n, l, a.hdr);
+      if (turn) rotate_row(kx[i], load_angles<D>(g.rope, a.T, tok0 + n, l, a.hdr));
+      const Row<D> v = floats<D>(vraw[i]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         take_max(kx[i].lo[j], ktop, odd); take_max(kx[i].hi[j], ktop, odd);
-        take_max(vx[i].lo[j], vtop, odd); take_max(vx[i].hi[j], vtop, odd);
+        take_max(v.lo[j], vtop, odd); take_max(v.hi[j], vtop, odd);
       }
     }
   }
@@ -260,16 +290,17 @@ kv_store_kernel(const KvArgs a, const StoreArgs g) {
   for (int i = 0; i < kSweeps; ++i) {
     const int n = i * kRows + row;
     if (n >= n_new) break;
+    const Row<D> v = floats<D>(vraw[i]);
     uint32_t lo = 0, hi = 0;
     float klo[4], khi[4], vlo[4], vhi[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int a0 = to_code(kx[i].lo[j], kstep), a1 = to_code(kx[i].hi[j], kstep);
-      const int b0 = to_code(vx[i].lo[j], vstep), b1 = to_code(vx[i].hi[j], vstep);
+      const int b0 = to_code(v.lo[j], vstep), b1 = to_code(v.hi[j], vstep);
       lo |= (uint32_t)(a0 & 255) << (8 * j);
       hi |= (uint32_t)(a1 & 255) << (8 * j);
-      turned[4 * l + j][n] = (int8_t)b0;
-      turned[D / 2 + 4 * l + j][n] = (int8_t)b1;
+      turned[(4 * l + j) * kPitch + n] = (int8_t)b0;
+      turned[(D / 2 + 4 * l + j) * kPitch + n] = (int8_t)b1;
       klo[j] = (float)a0 * kstep; khi[j] = (float)a1 * kstep;
       vlo[j] = (float)b0 * vstep; vhi[j] = (float)b1 * vstep;
     }
@@ -281,12 +312,13 @@ kv_store_kernel(const KvArgs a, const StoreArgs g) {
   }
   __syncthreads();
   if (n_new == kKvBlock) {
-    for (int i = threadIdx.x; i < D * kKvBlock / 16; i += kStoreThreads)
-      reinterpret_cast<uint4*>(vc)[i] = reinterpret_cast<const uint4*>(&turned[0][0])[i];
+    for (int i = threadIdx.x; i < D * kKvBlock / 4; i += kStoreThreads)
+      reinterpret_cast<uint32_t*>(vc)[i] =
+          *reinterpret_cast<const uint32_t*>(turned + (i / (kKvBlock / 4)) * kPitch + (i % (kKvBlock / 4)) * 4);
   } else {
     for (int i = threadIdx.x; i < D * n_new; i += kStoreThreads) {
       const int c = i / n_new, n = i % n_new;
-      vc[c * kKvBlock + off0 + n] = turned[c][n];
+      vc[c * kKvBlock + off0 + n] = turned[c * kPitch + n];
     }
   }
 }
@@ -302,13 +334,12 @@ int launch_kv_store(const uint16_t* qkv, int64_t ld, int head_dim, const KvArgs&
   // n tokens of one request touch at most (n - 1) / 64 + 2 blocks and at most n
   int64_t blocks = a.T / kKvBlock + 2 * (int64_t)a.B;
   if (blocks > a.T) blocks = a.T;
-  const int64_t q_ctas = ceil_div(a.T * a.n_heads, kKvBlock);
+  const int64_t q_ctas = ceil_div(a.T * a.n_heads, (int64_t)kSweepsQ * kStoreThreads / (head_dim / 8));
   if (blocks * a.n_kv + q_ctas > 0x7FFFFFFFLL) return TLQ_ERR_SHAPE;
   g.kv_ctas = (unsigned)(blocks * a.n_kv);
   const unsigned grid = g.kv_ctas + (unsigned)q_ctas;
-  if (head_dim == 128) kv_store_kernel<128><<<grid, kStoreThreads, 0, st>>>(a, g);
-  else kv_store_kernel<64><<<grid, kStoreThreads, 0, st>>>(a, g);
-  return after_launch();
+  return head_dim == 128 ? launch_next(kv_store_kernel<128>, dim3(grid), kStoreThreads, 0, 1, st, a, g)
+                         : launch_next(kv_store_kernel<64>, dim3(grid), kStoreThreads, 0, 1, st, a, g);
 }
 
 }  // namespace tlq

@@ -35,6 +35,7 @@ linear_i8_few_kernel(const int8_t* __restrict__ X, const float* __restrict__ t, 
   __shared__ int s_acc[kWarps][NT * 8][17];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, q = lane & 3;
+  after_previous();
   const int64_t o0 = (int64_t)blockIdx.x * 16, n0 = (int64_t)blockIdx.y * (8 * NT);
   // rows beyond the end read the last one; their results are not stored
   const int8_t* w0 = W + min(o0 + g, C2 - 1) * C1;
@@ -137,6 +138,7 @@ linear_i8_tile_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
   ptx::tc_fence_after();
   const uint32_t tmem = s_tmem;
   volatile int* abort_flag = &s_abort;
+  after_previous();
 
   const int rank = (int)(blockIdx.x % g.splits), tile = (int)(blockIdx.x / g.splits);
   const int mt = tile % g.mtiles, ot = tile / g.mtiles;   // token tiles of the same weights run side by side
@@ -297,22 +299,8 @@ int launch_tiles(const int8_t* Xq, const float* t, const int8_t* Wq, const float
     return cudaFuncSetAttribute(linear_i8_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kStageBudget + 1024));
   });
   if (rc != TLQ_OK) return rc;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(tiles * g.splits));
-  cfg.blockDim = dim3(kTileThreads);
-  cfg.dynamicSmemBytes = smem + 1024;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)g.splits;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, linear_i8_tile_kernel, tmW, tmX, g) != cudaSuccess) {
-    cudaGetLastError();
-    return TLQ_ERR_CUDA;
-  }
-  return after_launch();
+  return launch_next(linear_i8_tile_kernel, dim3((unsigned)(tiles * g.splits)), kTileThreads, smem + 1024, (unsigned)g.splits, st,
+                     tmW, tmX, g);
 }
 
 }  // namespace
@@ -321,12 +309,8 @@ int launch_linear_i8(const int8_t* Xq, const float* t, const int8_t* Wq, const f
                      int64_t C1, int64_t C2, uint16_t* Y, WorkspaceHeader* hdr, cudaStream_t st) {
   if (N > 16) return launch_tiles(Xq, t, Wq, u, bias, N, C1, C2, Y, hdr, st);
   const unsigned rows = (unsigned)ceil_div(C2, 16);
-  if (N <= 8) {
-    linear_i8_few_kernel<1><<<dim3(rows, 1), kThreads, 0, st>>>(Xq, t, Wq, u, bias, N, (int)C1, C2, Y);
-  } else {
-    linear_i8_few_kernel<2><<<dim3(rows, 1), kThreads, 0, st>>>(Xq, t, Wq, u, bias, N, (int)C1, C2, Y);
-  }
-  return after_launch();
+  return N <= 8 ? launch_next(linear_i8_few_kernel<1>, dim3(rows), kThreads, 0, 1, st, Xq, t, Wq, u, bias, N, (int)C1, C2, Y)
+                : launch_next(linear_i8_few_kernel<2>, dim3(rows), kThreads, 0, 1, st, Xq, t, Wq, u, bias, N, (int)C1, C2, Y);
 }
 
 }  // namespace tlq

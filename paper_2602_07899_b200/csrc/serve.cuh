@@ -95,6 +95,38 @@ __device__ __forceinline__ bool locate_item(int B, long long target, F count, lo
   return found->request >= 0;
 }
 
+// ---------------------------------------------------------------------------------------------- launches
+// Kernels of these operators follow one another in every layer, most of them a few microseconds long.  They are launched
+// so that a kernel's blocks may come up while the one before it on the stream still runs (programmatic dependent
+// launch); after_previous() is the first thing that reads or writes memory: it waits until everything earlier on the
+// stream is complete and visible, and then lets the next kernel come up in turn.
+__device__ __forceinline__ void after_previous() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+template <typename... Params, typename... Args>
+inline int launch_next(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, unsigned cluster, cudaStream_t st,
+                       Args... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...) != cudaSuccess) {
+    cudaGetLastError();
+    return TLQ_ERR_CUDA;
+  }
+  return after_launch();
+}
+
 // ---------------------------------------------------------------------------------------------- launchers
 // kv_store.cu
 struct RopeArgs {

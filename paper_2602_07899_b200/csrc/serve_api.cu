@@ -88,7 +88,7 @@ int tlq_kv_store(const void* qkv, int64_t T, int64_t ld, int32_t n_heads, const 
   if (rc == TLQ_OK) rc = check_batch(batch);
   if (rc == TLQ_OK) rc = check_heads(n_heads, cache);
   if (rc != TLQ_OK) return rc;
-  if (T < 0 || T > 0x7FFFFF00LL) return TLQ_ERR_SHAPE;
+  if (T < 0 || T > 0x7FFFFF00LL || T * n_heads > 0x7FFFFF00LL) return TLQ_ERR_SHAPE;
   if (workspace == nullptr) return TLQ_ERR_INVALID_ARG;
   if (T > 0 && (qkv == nullptr || q_out == nullptr)) return TLQ_ERR_INVALID_ARG;
   const int d = cache->head_dim;
