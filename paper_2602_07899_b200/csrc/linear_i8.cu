@@ -1,18 +1,21 @@
 // Y[n,o] = bf16( t[n] u[o] sum_c Xq[n,c] Wq[o,c] + bias[o] ) from kept 8-bit codes.
 //
-// Few tokens: the weights' bytes are the bound (2 N operations per weight byte), and every weight is read once, straight
-// from global memory into the registers of the lane that feeds it to the matrix instruction m16n8k32 (weights on the
-// m side: 16 output channels, tokens on the n side).  Which channel of C1 a matrix index means is free as long as both
-// operands agree, so a lane's operands are whole 16-byte pieces of a row.  A CTA owns 16 output channels and its eight
-// warps share C1; the 32-bit integer partial sums are exact in any order.
+// Few tokens and small weights (linear_i8_few_kernel): latency is the bound.  Weights go straight from global memory into
+// the registers of the lane that feeds them to the matrix instruction m16n8k32 (16 output channels on the m side, tokens on
+// the n side).  Which channel of C1 a matrix index means is free as long as both operands agree, so a lane's operands are
+// whole 16-byte pieces of a row.  A CTA owns 16 output channels and its warps share C1; the 32-bit integer partial sums are
+// exact in any order.  One token, 3584 x 512: 2.7 us with 16 warps to a CTA, 3.2 with 8, 4.7 by the tile kernel.
+//
+// Everything else up to a few hundred tokens (linear_i8_tile_kernel): bound by the weights' bytes, which TMA keeps under way
+// deeper than registers could.  16 tokens, 3584 x 18944 (68 MB): 15.5 us, 18.8 by the few kernel; 1 token, 18944 x 3584:
+// 14.8 us against 17 to 28.
+//
+// Beyond that the persistent kernel of tlq_apply_layer, bound by the tensor core.
 #include "serve.cuh"
 #include "umma.cuh"
 
 namespace tlq {
 namespace {
-
-constexpr int kWarps = 8;
-constexpr int kThreads = kWarps * 32;
 
 __device__ __forceinline__ uint4 ld_weights(const int8_t* p) {
   uint4 v;
@@ -27,11 +30,12 @@ __device__ __forceinline__ void mma_i8(int (&c)[4], uint32_t a0, uint32_t a1, ui
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <int NT>
-__global__ void __launch_bounds__(kThreads)
+template <int NT, int kWarps>
+__global__ void __launch_bounds__(kWarps * 32)
 linear_i8_few_kernel(const int8_t* __restrict__ X, const float* __restrict__ t, const int8_t* __restrict__ W,
                      const float* __restrict__ u, const uint16_t* __restrict__ bias, int64_t N, int C1, int64_t C2,
                      uint16_t* __restrict__ Y) {
+  constexpr int kThreads = kWarps * 32;
   __shared__ int s_acc[kWarps][NT * 8][17];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, q = lane & 3;
@@ -307,10 +311,19 @@ int launch_tiles(const int8_t* Xq, const float* t, const int8_t* Wq, const float
 
 int launch_linear_i8(const int8_t* Xq, const float* t, const int8_t* Wq, const float* u, const uint16_t* bias, int64_t N,
                      int64_t C1, int64_t C2, uint16_t* Y, WorkspaceHeader* hdr, cudaStream_t st) {
-  if (N > 16) return launch_tiles(Xq, t, Wq, u, bias, N, C1, C2, Y, hdr, st);
-  const unsigned rows = (unsigned)ceil_div(C2, 16);
-  return N <= 8 ? launch_next(linear_i8_few_kernel<1>, dim3(rows), kThreads, 0, 1, st, Xq, t, Wq, u, bias, N, (int)C1, C2, Y)
-                : launch_next(linear_i8_few_kernel<2>, dim3(rows), kThreads, 0, 1, st, Xq, t, Wq, u, bias, N, (int)C1, C2, Y);
+  // Few tokens and weights of up to 24 MB: measured, the few kernel is ahead up to 14 MB (1536 x 8960: 4.7 us against 6.1) and
+  // behind from 64 MB on (8192 x 8192: 16.1 against 15.0).
+  if (N > 16 || C1 * C2 > (24 << 20)) return launch_tiles(Xq, t, Wq, u, bias, N, C1, C2, Y, hdr, st);
+  const unsigned ctas = (unsigned)ceil_div(C2, 16);
+  const int sms = device_sm_count();
+  if (sms <= 0) return TLQ_ERR_CUDA;
+  // with no more CTAs than SMs a CTA has an SM to itself and takes twice the warps (1536 x 8960, 560 CTAs: 5.8 us so, 4.7 not)
+  const bool deep = (int)ctas <= sms;
+  auto run = [&](auto kernel, int warps) {
+    return launch_next(kernel, dim3(ctas), warps * 32, 0, 1, st, Xq, t, Wq, u, bias, N, (int)C1, C2, Y);
+  };
+  if (N <= 8) return deep ? run(linear_i8_few_kernel<1, 16>, 16) : run(linear_i8_few_kernel<1, 8>, 8);
+  return deep ? run(linear_i8_few_kernel<2, 16>, 16) : run(linear_i8_few_kernel<2, 8>, 8);
 }
 
 }  // namespace tlq
