@@ -314,21 +314,16 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
   if (lane == 0) s_has[warp] = 0;
   after_previous();
   auto count_units = [&](int b) { return units_of(a, load_request(a, b), kRows, g.max_rows).total; };
-  long long total = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kThreads) {
-    const int b = b0 + (int)threadIdx.x;
-    long long part;
-    block_scan<kThreads>(b < a.B ? count_units(b) : 0, sums, part);
-    total += part;
-  }
-  if (total == 0) return;
   // no more CTAs than give each warp of a CTA a block
-  long long workers = (total + kWarps - 1) / kWarps;
-  if (workers > (long long)gridDim.x) workers = gridDim.x;
-  if ((long long)blockIdx.x >= workers) return;
+  auto workers_of = [&](long long all) { return min((all + kWarps - 1) / kWarps, (long long)gridDim.x); };
+  long long total = 0;
+  if (!plan_items<kThreads>(a.B, count_units,
+                            [&](long long all) { return (long long)blockIdx.x < workers_of(all) ? all * blockIdx.x / workers_of(all) : -1LL; },
+                            sums, &found, total))
+    return;
+  const long long workers = workers_of(total);
   const long long u_begin = total * blockIdx.x / workers, u_end = total * (blockIdx.x + 1) / workers;
   auto worker_of = [&](long long unit) { return ((unit + 1) * workers - 1) / total; };
-  if (!locate_item<kThreads>(a.B, u_begin, count_units, sums, &found)) return;
 
   // ---------------------------------------------------------------- this warp's part of it
   // (with fewer units than warps the first ones get one each: warps with nothing to do are the last ones)

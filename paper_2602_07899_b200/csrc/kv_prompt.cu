@@ -100,6 +100,11 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
   asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
   return v;
 }
+// 16 bytes straight to shared memory (`from` of them from global memory, zeros after that), and the wait for such copies
+__device__ __forceinline__ void copy16(uint32_t to, const void* p, int from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(p), "r"(from) : "memory");
+}
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // (code + 128) 2^-24 as f16, and exactly the code: see kv_attention.cu
 __device__ __forceinline__ void keys_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
   const uint32_t x = w ^ 0x80808080u;
@@ -307,7 +312,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
   __shared__ Cut s_cut[2];
   __shared__ Line s_line;
   __shared__ uint32_t s_tmem;
-  __shared__ int s_abort, s_join[2];
+  __shared__ int s_abort, s_join[2], s_n_parts, s_parts[kMaxWorkers];
   const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;   // warp: known to be uniform
   auto bar = [&](int i) { return ptx::smem_u32(&bars[i]); };
   if (threadIdx.x == 0) {
@@ -342,23 +347,21 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     const Costs c = costs_of(a, g, load_request(a, b));
     return c.sum(c.tiles) * a.n_kv;
   };
-  long long total = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kThreads) {
-    const int b = b0 + (int)threadIdx.x;
-    long long part;
-    block_scan<kThreads>(b < a.B ? cost_of(b) : 0, sums, part);
-    total += part;
-  }
-  if (total == 0) return;
   {
-    // a part is worth joining from some key tiles on
-    const long long workers = max(1LL, min((long long)gridDim.x, total / (64 * kMinTiles)));
-    if (blockIdx.x >= workers) return;
-    const long long x0 = total * blockIdx.x / workers, x1 = total * (blockIdx.x + 1) / workers;
-    if (x0 >= x1) return;
-    if (!locate_item<kThreads>(a.B, x0, cost_of, sums, &found)) return;
+    // a part is worth joining from some blocks on
+    auto workers_of = [&](long long all) { return max(1LL, min((long long)gridDim.x, all / (64 * kMinTiles))); };
+    long long total = 0;
+    if (!plan_items<kThreads>(a.B, cost_of,
+                              [&](long long all) {
+                                const long long n = workers_of(all);
+                                return blockIdx.x < n && all * blockIdx.x / n < all * (blockIdx.x + 1) / n ? all * blockIdx.x / n : -1LL;
+                              },
+                              sums, &found, total))
+      return;
     if (threadIdx.x == 0) {                                // read back where they are needed: the loops have no registers to spare
-      s_line.total = total; s_line.workers = workers; s_line.x0 = x0; s_line.x1 = x1;
+      const long long n = workers_of(total);
+      s_line.total = total; s_line.workers = n;
+      s_line.x0 = total * blockIdx.x / n; s_line.x1 = total * (blockIdx.x + 1) / n;
     }
   }
   if (warp == kIssueWarp) ptx::tmem_alloc(ptx::smem_u32(&s_tmem), 512);
@@ -469,58 +472,47 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       const int limit = !live ? -1 : g.causal ? min(s->kv - s->q_len + token, s->kv - 1) : s->kv - 1;
       float fac = 0.f, off = 0.f;
       if (k0 < k1) {
-        // The warp's 32 rows of q, kRowLanes lanes to a row: whole rows come in and go out.  A power of two brings a row into
-        // the range of f16.
+        // The warp's 32 rows of q come in whole, kRowLanes lanes to a row, straight to their place in shared memory; then every
+        // lane turns its own row into f16 there, after a power of two that brings it into range.  In rolled loops: this is run
+        // once per item, and code that runs once is slower to fetch than to execute.
         const int64_t from = live ? (int64_t)(s->q0 + token) * g.ldq + (int64_t)(s->h * a.group + row - token * a.group) * D : -1;
-        uint4 v[D / 8];
-#pragma unroll
+        const uint32_t tile_at = q_at + t * kQBytes<D>;
+#pragma unroll 1
         for (int i = 0; i < D / 8; ++i) {
-          const int64_t p = __shfl_sync(0xFFFFFFFFu, from, i * kRowsAtOnce + lane / kRowLanes);
-          v[i] = p >= 0 ? __ldg(reinterpret_cast<const uint4*>(g.q + p) + lane % kRowLanes) : make_uint4(0, 0, 0, 0);
+          const int at = i * kRowsAtOnce + lane / kRowLanes, r = (warp & 3) * 32 + at, piece = lane % kRowLanes;
+          const int64_t p = __shfl_sync(0xFFFFFFFFu, from, at);
+          const uint32_t to = tile_at + (piece >> 3) * (kTile * 128) + r * 128 + (((piece & 7) ^ (r & 7)) << 4);
+          copy16(to, p >= 0 ? g.q + p + 8 * piece : g.q, p >= 0 ? 16 : 0);
         }
-        // (all rows advance together: every shuffle of one would otherwise wait for the one before it)
-        float x[D / 8];
-#pragma unroll
+        copy_wait();
+        __syncwarp();
+        const uint32_t mine = tile_at + row_in_tile * 128;
+        float top = 0.f;
+#pragma unroll 2
         for (int i = 0; i < D / 8; ++i) {
           float e[8];
-          unpack8(v[i], e);
-          x[i] = 0.f;
+          unpack8(lds128(mine + (i >> 3) * (kTile * 128) + (((i & 7) ^ (row_in_tile & 7)) << 4)), e);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) x[i] = fmaxf(x[i], fabsf(e[j]));
+          for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(e[j]));
         }
-#pragma unroll
-        for (int d = kRowLanes / 2; d > 0; d >>= 1)
-#pragma unroll
-          for (int i = 0; i < D / 8; ++i) x[i] = fmaxf(x[i], __shfl_xor_sync(0xFFFFFFFFu, x[i], d));
-        int ex = 0;
-        const int owner = (lane % kRowsAtOnce) * kRowLanes;   // the lane that has this lane's row, when its turn comes
-#pragma unroll
+        const int ex = exponent_of(top);
+        const float d0 = power_of_two(-(ex / 2)), d1 = power_of_two(-(ex - ex / 2));
+        float qs = 0.f;
+#pragma unroll 2
         for (int i = 0; i < D / 8; ++i) {
-          const int r = (warp & 3) * 32 + i * kRowsAtOnce + lane / kRowLanes, piece = lane % kRowLanes;
-          const int y = exponent_of(x[i]), their_y = __shfl_sync(0xFFFFFFFFu, y, owner);
-          if (lane / kRowsAtOnce == i) ex = their_y;
-          const float d0 = power_of_two(-(y / 2)), d1 = power_of_two(-(y - y / 2));
+          const uint32_t at = mine + (i >> 3) * (kTile * 128) + (((i & 7) ^ (row_in_tile & 7)) << 4);
           float e[8];
-          unpack8(v[i], e);
+          unpack8(lds128(at), e);
           uint32_t w[4];
-          x[i] = 0.f;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             w[j] = pack_f16(e[2 * j] * d0 * d1, e[2 * j + 1] * d0 * d1);
             const float2 z = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
-            x[i] += z.x + z.y;
+            qs += z.x + z.y;
           }
-          sts128(q_at + t * kQBytes<D> + (piece >> 3) * (kTile * 128) + r * 128 + (((piece & 7) ^ (r & 7)) << 4), w[0], w[1], w[2], w[3]);
+          sts128(at, w[0], w[1], w[2], w[3]);
         }
-#pragma unroll
-        for (int d = kRowLanes / 2; d > 0; d >>= 1)
-#pragma unroll
-          for (int i = 0; i < D / 8; ++i) x[i] += __shfl_xor_sync(0xFFFFFFFFu, x[i], d);
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-          const float qs = __shfl_sync(0xFFFFFFFFu, x[i], owner);
-          if (lane / kRowsAtOnce == i) off = qs * (128.f / kUnit);
-        }
+        off = qs * (128.f / kUnit);
         fac = ldexpf(g.scale_log2, ex + 24);
         ptx::fence_proxy_async();
         __syncwarp();
@@ -623,7 +615,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
         // all channels as bf16, in the layout of q, or 32 channels at a time as they are (for a partial)
         const uint32_t mine = q_at + t * kQBytes<D> + (warp & 3) * (32 * 128);
         float* part = slot(blockIdx.x, s->starts) + 2 * kItemRows + (size_t)(t * kTile + (warp & 3) * 32) * D;
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
           uint32_t v[32];
           if (k0 < k1) {
@@ -649,7 +641,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) sts128(mine + lane * 128 + ((i ^ (lane & 7)) << 4), v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
             __syncwarp();
-#pragma unroll
+#pragma unroll 2
             for (int i = 0; i < 8; ++i) {
               const int r = 4 * i + (lane >> 3), piece = lane & 7;
               reinterpret_cast<uint4*>(part + (size_t)r * D + 32 * c)[piece] = lds128(mine + r * 128 + ((piece ^ (r & 7)) << 4));
@@ -658,7 +650,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
           __syncwarp();
         }
         if (whole) {
-#pragma unroll
+#pragma unroll 2
           for (int i = 0; i < D / 8; ++i) {
             const int r = i * kRowsAtOnce + lane / kRowLanes, piece = lane % kRowLanes;
             const int64_t to = __shfl_sync(0xFFFFFFFFu, at, r);
@@ -851,13 +843,22 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     const Request req = load_request(a, c.b);
     const long long rows = (long long)req.q_len * a.group;
     const long long first = worker_of(c.at), final = worker_of(c.at + c.len - 1);
-    // the parts of the CTAs that share the item: number w is at part(w) where it has any blocks
-    auto has = [&](long long w) {
-      int k0, k1;
-      cut(edge(w), edge(w + 1), c.at, c.len, c.n, k0, k1);
-      return k0 < k1;
-    };
-    auto part = [&](long long w) { return (const float*)slot(w, c.at >= edge(w) ? 1 : 0); };
+    // where the parts of the CTAs that share the item are, in order
+    if (warp == 0) {
+      int n = 0;
+      for (long long w0 = first; w0 <= final; w0 += 32) {
+        const long long w = w0 + lane;
+        int k0 = 0, k1 = 0;
+        if (w <= final) cut(edge(w), edge(w + 1), c.at, c.len, c.n, k0, k1);
+        const uint32_t some = __ballot_sync(0xFFFFFFFFu, k0 < k1);
+        if (k0 < k1) s_parts[n + __popc(some & ((1u << lane) - 1u))] = (int)(2 * w + (c.at >= edge(w) ? 1 : 0));
+        n += __popc(some);
+      }
+      if (lane == 0) s_n_parts = n;
+    }
+    __syncthreads();
+    const int n_parts = s_n_parts;
+    auto part = [&](int i) { return (const float*)(g.split.partials + (size_t)s_parts[i] * kPitch); };
     // maximum and sum of every row
     float* const s_m = reinterpret_cast<float*>(smem_raw);
     float* const s_inv = s_m + kItemRows;
@@ -865,12 +866,10 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       const int r = threadIdx.x, row = c.tile * kItemRows + r;
       float mm = -INFINITY, den = 0.f;
 #pragma unroll 4
-      for (long long w = first; w <= final; ++w)
-        if (has(w)) mm = fmaxf(mm, __ldcg(part(w) + r));
+      for (int i = 0; i < n_parts; ++i) mm = fmaxf(mm, __ldcg(part(i) + r));
       const float mu = mm == -INFINITY ? 0.f : mm;
 #pragma unroll 4
-      for (long long w = first; w <= final; ++w)
-        if (has(w)) den += exp2_fast(__ldcg(part(w) + r) - mu) * __ldcg(part(w) + kItemRows + r);
+      for (int i = 0; i < n_parts; ++i) den += exp2_fast(__ldcg(part(i) + r) - mu) * __ldcg(part(i) + kItemRows + r);
       const bool none = mm == -INFINITY && den == 0.f;
       s_m[r] = mu;
       s_inv[r] = none ? 0.f : 1.0f / den;
@@ -884,9 +883,8 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       float4 sum[kEach];
 #pragma unroll
       for (int j = 0; j < kEach; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (long long w = first; w <= final; ++w) {
-        if (!has(w)) continue;
-        const float* p = part(w);
+      for (int i = 0; i < n_parts; ++i) {
+        const float* p = part(i);
         float4 v[kEach];
         float f[kEach];
 #pragma unroll

@@ -95,6 +95,30 @@ __device__ __forceinline__ bool locate_item(int B, long long target, F count, lo
   return found->request >= 0;
 }
 
+// Both in one: the number of all items, and the item that target_of(total) names (none where that is negative).
+template <int kThreads, typename F, typename G>
+__device__ __forceinline__ bool plan_items(int B, F count, G target_of, long long* sums, Found* found, long long& total) {
+  const int b = (int)threadIdx.x;
+  const long long n = b < B ? count(b) : 0;
+  if (threadIdx.x == 0) found->request = -1;
+  const long long upto = block_scan<kThreads>(n, sums, total);
+  for (int b0 = kThreads; b0 < B; b0 += kThreads) {
+    long long part;
+    block_scan<kThreads>(b0 + b < B ? count(b0 + b) : 0, sums, part);
+    total += part;
+  }
+  if (total == 0) return false;
+  const long long target = target_of(total);
+  if (target < 0) return false;
+  if (B > kThreads) return locate_item<kThreads>(B, target, count, sums, found);
+  if (n > 0 && target >= upto - n && target < upto) {
+    found->request = b;
+    found->rest = target - (upto - n);
+  }
+  __syncthreads();
+  return found->request >= 0;
+}
+
 // ---------------------------------------------------------------------------------------------- launches
 // Kernels of these operators follow one another in every layer, most of them a few microseconds long.  They are launched
 // so that a kernel's blocks may come up while the one before it on the stream still runs (programmatic dependent
