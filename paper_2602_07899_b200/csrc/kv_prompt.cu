@@ -34,7 +34,7 @@ constexpr int kTile = 128, kItemRows = 256, kKeys = kKvBlock, kStages = 4;
 constexpr int kSoftWarps = 8, kLoadWarps = 4, kIssueWarp = kSoftWarps + kLoadWarps, kPlanWarp = kIssueWarp + 1, kScoutWarp = kIssueWarp + 2;
 constexpr int kThreads = 512;                              // four groups of four warps
 // registers of a thread of each role: 2 x 176 + 72 + 88 = 4 x 128, what the block is launched with
-constexpr int kSoftRegs = 176, kLoadRegs = 72, kIssueRegs = 88, kLaunchRegs = 128;
+constexpr int kSoftRegs = 176, kLoadRegs = 72, kIssueRegs = 88;
 constexpr float kShift = 11.f, kGrow = 4.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kStepFloor = 7.8886090522101181e-31f;      // 2^-100, as in kv_attention.cu
@@ -75,7 +75,10 @@ constexpr uint32_t kKBytes = kKeys * D * 2;                // of one stage of ke
 template <int D>
 constexpr uint32_t kVBytes = kKeys * D * 2;                // of one stage of values
 template <int D>
-constexpr size_t kSmem = 1024 + 2 * kQBytes<D> + kStages * (kKBytes<D> + kVBytes<D>);
+constexpr uint32_t kRawBytes = 2 * kKeys * D;              // codes of a block's keys and values
+constexpr int kRaw = 2;                                    // blocks whose codes are under way
+template <int D>
+constexpr size_t kSmem = 1024 + 2 * kQBytes<D> + kStages * (kKBytes<D> + kVBytes<D>) + kRaw * kRawBytes<D>;
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -85,12 +88,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const __half2 v = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ uint4 ld_cache(const int8_t* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
 }
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -105,6 +102,16 @@ __device__ __forceinline__ void copy16(uint32_t to, const void* p, int from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(p), "r"(from) : "memory");
 }
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void copy_mark() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// whether a phase of a barrier is complete, without waiting for it
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t is;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(is) : "r"(bar), "r"(parity) : "memory");
+  return is != 0;
+}
 // (code + 128) 2^-24 as f16, and exactly the code: see kv_attention.cu
 __device__ __forceinline__ void keys_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
   const uint32_t x = w ^ 0x80808080u;
@@ -288,38 +295,35 @@ struct Walk {
   }
 };
 
-struct Line {                   // the whole line, how many CTAs share it, this CTA's part
-  long long total, workers, x0, x1;
-};
-
-struct Cut {                    // an item of which this CTA has only a part
-  long long at, len;
-  int b, h, tile, n;
-};
+constexpr int kJoinRows = 32, kJoinThreads = 256;          // rows of a CTA that joins parts
+template <int D>
+constexpr size_t kPitch = (size_t)kItemRows * (D + 2);     // floats of a partial: maxima, sums, output sums
+template <int D>
+__device__ __forceinline__ float* partial_of(const KvSplit& split, int cta, int i) { return split.partials + ((size_t)cta * 2 + i) * kPitch<D>; }
+template <int D>
+__device__ __forceinline__ PartNote* notes_of(const KvSplit& split) {     // two of every CTA, behind the partials
+  return reinterpret_cast<PartNote*>(split.partials + (size_t)kMaxWorkers * 2 * kPitch<D>);
+}
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t q_at = base, k_at = q_at + 2 * kQBytes<D>, v_at = k_at + kStages * kKBytes<D>;
+  const uint32_t q_at = base, k_at = q_at + 2 * kQBytes<D>, v_at = k_at + kStages * kKBytes<D>, raw_at = v_at + kStages * kVBytes<D>;
   __shared__ __align__(8) uint64_t bars[kBars];
   __shared__ Segment s_ring[kRing];
   __shared__ __align__(16) float4 s_steps[kTileRing];      // of a block: kstep, log2 vstep, 1 / vstep, usable
   __shared__ int s_block[kTileRing];                       // and where it is (block x kv heads + head)
   __shared__ long long sums[kThreads / 32];
   __shared__ Found found;
-  __shared__ Cut s_cut[2];
-  __shared__ Line s_line;
+  __shared__ long long s_from, s_to;                       // this CTA's part of the line
   __shared__ uint32_t s_tmem;
-  __shared__ int s_abort, s_join[2], s_n_parts, s_parts[kMaxWorkers];
+  __shared__ int s_abort;
   const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;   // warp: known to be uniform
   auto bar = [&](int i) { return ptx::smem_u32(&bars[i]); };
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 2; ++i) {
-      ptx::mbar_init(bar(kBarQ + i), 4);
-      s_cut[i].len = 0;
-    }
+    for (int i = 0; i < 2; ++i) ptx::mbar_init(bar(kBarQ + i), 4);
     for (int i = 0; i < 4; ++i) {
       ptx::mbar_init(bar(kBarS + i), 1);
       ptx::mbar_init(bar(kBarP + i), 4);
@@ -342,6 +346,8 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
   volatile int* abort_flag = &s_abort;
 
   after_previous();
+  auto no_parts = [&]() { notes_of<D>(g.split)[2 * blockIdx.x].n = notes_of<D>(g.split)[2 * blockIdx.x + 1].n = 0; };
+  if (threadIdx.x == 0) no_parts();
   // ---------------------------------------------------------------- this CTA's part of the line
   auto cost_of = [&](int b) {
     const Costs c = costs_of(a, g, load_request(a, b));
@@ -360,8 +366,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       return;
     if (threadIdx.x == 0) {                                // read back where they are needed: the loops have no registers to spare
       const long long n = workers_of(total);
-      s_line.total = total; s_line.workers = n;
-      s_line.x0 = total * blockIdx.x / n; s_line.x1 = total * (blockIdx.x + 1) / n;
+      s_from = total * blockIdx.x / n; s_to = total * (blockIdx.x + 1) / n;
     }
   }
   if (warp == kIssueWarp) ptx::tmem_alloc(ptx::smem_u32(&s_tmem), 512);
@@ -369,8 +374,6 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = s_tmem;                            // S of tile t, buffer i at column 128 t + 64 i; O at 256 + 128 t
-  constexpr size_t kPitch = (size_t)kItemRows * (D + 2);   // floats of a partial: maxima, sums, output sums
-  auto slot = [&](long long w, int i) { return g.split.partials + ((size_t)w * 2 + i) * kPitch; };
   // the next segment, by all lanes of a warp (or the one that issues)
   int seg = 0;
   uint32_t seg_phase = 0;
@@ -464,8 +467,9 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       if (!ok || s->k0 < 0) break;
       const int k0 = s->k0, k1 = s->k1;
       if (threadIdx.x == 0 && (k0 > 0 || k1 < s->n)) {
-        Cut* c = &s_cut[s->starts];
-        c->at = s->at; c->len = s->len; c->b = s->b; c->h = s->h; c->tile = s->tile; c->n = s->n;
+        PartNote* note = notes_of<D>(g.split) + 2 * blockIdx.x + s->starts;
+        note->b = s->b; note->h = s->h; note->tile = s->tile; note->q0 = s->q0;
+        note->q_len = s->q_len; note->k0 = k0; note->k1 = k1; note->n = s->n;
       }
       const int row = s->tile * kItemRows + t * kTile + row_in_tile, token = row / a.group;
       const bool live = token < s->q_len;
@@ -614,7 +618,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
         // through the shared memory of the warp's own rows of q, which nobody reads any more, so that whole rows are stored:
         // all channels as bf16, in the layout of q, or 32 channels at a time as they are (for a partial)
         const uint32_t mine = q_at + t * kQBytes<D> + (warp & 3) * (32 * 128);
-        float* part = slot(blockIdx.x, s->starts) + 2 * kItemRows + (size_t)(t * kTile + (warp & 3) * 32) * D;
+        float* part = partial_of<D>(g.split, blockIdx.x, s->starts) + 2 * kItemRows + (size_t)(t * kTile + (warp & 3) * 32) * D;
 #pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
           uint32_t v[32];
@@ -659,7 +663,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
           }
           if (live && g.lse != nullptr) g.lse[at] = none ? -INFINITY : kLn2 * (log2f(l) + m - kShift);
         } else {
-          float* stats = slot(blockIdx.x, s->starts) + t * kTile + row_in_tile;
+          float* stats = partial_of<D>(g.split, blockIdx.x, s->starts) + t * kTile + row_in_tile;
           stats[0] = m;
           stats[kItemRows] = l;
         }
@@ -681,33 +685,44 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     const int8_t* const v_from = a.v_codes + (lw * 8 + lr) * kKvBlock + piece * 16;
     const uint32_t swizzled0 = ((2 * piece) ^ lr) << 4, swizzled1 = ((2 * piece + 1) ^ lr) << 4;
     const uint32_t k_to = k_at + k_panel * (kKeys * 128) + k_row * 128, v_to = v_at + (lw * 8 + lr) * 128;
-    int step = 0;
-    bool ok = true;
-    uint4 kr[kNum], vr[kNum];
-    int64_t block = 0;                                     // whose codes are under way
-    // the next block of the scout's ring; false at the end
-    auto look_up = [&](int at_step) {
-      const int at = at_step % kTileRing;
-      ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(kBarTileFull + at), (uint32_t)(at_step / kTileRing) & 1u, abort_flag));
-      if (!ok) return false;
-      block = (int64_t)s_block[at] * (kKvBlock * D);
-      return block >= 0;
-    };
-    auto load_keys = [&]() {
+    // Codes of the next kRaw blocks are under way to places in shared memory that belong to one thread each, so that no
+    // barrier is needed between their arrival and their use, and no register while they travel.
+    const uint32_t raw = raw_at + (threadIdx.x - kSoftWarps * 32) * 16;
+    constexpr uint32_t kRawStep = kLoadWarps * 32 * 16;
+    int step = 0, fetched = 0;                             // blocks laid out, blocks asked for
+    bool ok = true, more = true;
+    // Asks for the next block of the scout's ring; waits for the ring only when there is nothing to lay out meanwhile, since
+    // the scout may be waiting for what that completes (items in which nobody sees a key have no blocks).
+    auto fetch = [&]() {
+      const int at = fetched % kTileRing;
+      const uint32_t full = bar(kBarTileFull + at), parity = (uint32_t)(fetched / kTileRing) & 1u;
+      if (fetched > step) {
+        if (!__all_sync(0xFFFFFFFFu, mbar_test(full, parity))) return;
+      } else {
+        ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(full, parity, abort_flag));
+        if (!ok) return;
+      }
+      const int64_t block = (int64_t)s_block[at] * (kKvBlock * D);
+      more = block >= 0;
+      if (!more) return;
+      const uint32_t to = raw + fetched % kRaw * kRawBytes<D>;
 #pragma unroll
-      for (int i = 0; i < kNum; ++i) kr[i] = ld_cache(k_from + block + i * kGroups * 8 * D);
-    };
-    auto load_values = [&]() {
+      for (int i = 0; i < kNum; ++i) copy16(to + i * kRawStep, k_from + block + i * kGroups * 8 * D, 16);
 #pragma unroll
-      for (int i = 0; i < kNum; ++i) vr[i] = ld_cache(v_from + block + i * 32 * kKvBlock);
+      for (int i = 0; i < kNum; ++i) copy16(to + (kNum + i) * kRawStep, v_from + block + i * 32 * kKvBlock, 16);
+      copy_mark();
+      ++fetched;
     };
-    bool more = look_up(0);
-    if (more) {
-      load_keys();
-      load_values();
-    }
-    while (more) {
+    while (true) {
+      while (more && ok && fetched - step < kRaw) {
+        const int before = fetched;
+        fetch();
+        if (fetched == before) break;
+      }
+      if (!ok || fetched == step) break;
+      if (fetched - step == kRaw) copy_wait_but<kRaw - 1>(); else copy_wait();
       const int stage = step % kStages;
+      const uint32_t in = raw + step % kRaw * kRawBytes<D>;
       if (step >= kStages) {                               // the stage is free, and so is what the scout noted of its block
         ok = products_of(step - kStages);
         if (!ok) break;
@@ -716,30 +731,29 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
 #pragma unroll
       for (int i = 0; i < kNum; ++i) {
         const uint32_t to = k_to + stage * kKBytes<D> + i * kGroups * 8 * 128;
+        const uint4 y = lds128(in + i * kRawStep);
         uint32_t x[8];
-        keys_to_f16(kr[i].x, x[0], x[1]); keys_to_f16(kr[i].y, x[2], x[3]);
-        keys_to_f16(kr[i].z, x[4], x[5]); keys_to_f16(kr[i].w, x[6], x[7]);
+        keys_to_f16(y.x, x[0], x[1]); keys_to_f16(y.y, x[2], x[3]);
+        keys_to_f16(y.z, x[4], x[5]); keys_to_f16(y.w, x[6], x[7]);
         sts128(to + swizzled0, x[0], x[1], x[2], x[3]);
         sts128(to + swizzled1, x[4], x[5], x[6], x[7]);
       }
-      more = look_up(step + 1);
-      if (!ok) break;
-      if (more) load_keys();
 #pragma unroll
       for (int i = 0; i < kNum; ++i) {
         const uint32_t to = v_to + stage * kVBytes<D> + i * 32 * 128;
+        const uint4 y = lds128(in + (kNum + i) * kRawStep);
         uint32_t x[8];
-        values_to_f16(vr[i].x, x[0], x[1]); values_to_f16(vr[i].y, x[2], x[3]);
-        values_to_f16(vr[i].z, x[4], x[5]); values_to_f16(vr[i].w, x[6], x[7]);
+        values_to_f16(y.x, x[0], x[1]); values_to_f16(y.y, x[2], x[3]);
+        values_to_f16(y.z, x[4], x[5]); values_to_f16(y.w, x[6], x[7]);
         sts128(to + swizzled0, x[0], x[1], x[2], x[3]);
         sts128(to + swizzled1, x[4], x[5], x[6], x[7]);
       }
       ptx::fence_proxy_async();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(bar(kBarFull + stage));
-      if (more) load_values();
       ++step;
     }
+    copy_wait();
     if (!ok && lane == 0) report_status(a.hdr, TLQ_ERR_TIMEOUT, 232);
   } else {
     fewer_registers<kIssueRegs>();
@@ -750,7 +764,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     } else if (warp == kPlanWarp && lane == 0) {
       // ---------------------------------------------------------------- segments
       Walk walk;
-      walk.start(a, g, found.request, found.rest, s_line.x0, s_line.x1);
+      walk.start(a, g, found.request, found.rest, s_from, s_to);
       uint32_t phase = 1;
       while (true) {
         Segment s;
@@ -804,8 +818,6 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     }
   }
   __syncwarp();
-  // the rest is run by all warps: back to what they were launched with
-  if (warp < kSoftWarps) fewer_registers<kLaunchRegs>(); else more_registers<kLaunchRegs>();
   if (*abort_flag != 0)
     for (int i = 0; i < 1000; ++i) __nanosleep(1000);      // products under way end before their memory is given back
   ptx::tc_fence_before();
@@ -814,107 +826,94 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc(tmem, 512);
   }
-  if (*abort_flag != 0) return;
+  if (*abort_flag != 0 && threadIdx.x == 0) no_parts();
+}
 
-  // ------------------------------------------------------------------ join the CTAs that share an item
-  const long long total_cost = s_line.total, workers = s_line.workers;
-  auto edge = [&](long long w) { return total_cost * w / workers; };
-  auto worker_of = [&](long long x) { return ((x + 1) * workers - 1) / total_cost; };
-  if (threadIdx.x < 2) {
-    const Cut c = s_cut[threadIdx.x];
-    s_join[threadIdx.x] = 0;
-    if (c.len > 0) {
-      int k0, k1;
-      cut(s_line.x0, s_line.x1, c.at, c.len, c.n, k0, k1);
-      int32_t* counter = g.split.counters + worker_of(c.at);
-      __threadfence();                                     // the CTA's partials, which the barrier has ordered before this
-      const int before = atomicAdd(counter, k1 - k0);      // blocks of the item that are done
-      if (before + (k1 - k0) == c.n) {
-        *counter = 0;
-        s_join[threadIdx.x] = 1;
-      }
-      __threadfence();
-    }
-  }
-  __syncthreads();
+// Joins the parts of the items that were cut.  CTA (w, y) takes rows 32 y .. 32 y + 31 of the items whose first blocks CTA w of
+// the kernel above had; their other parts are of the CTAs after it.  A kernel of its own, since a single CTA (the last one to
+// finish its part, say) reads parts at 65 GB/s and all of them together from the second-level cache.
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads)
+kv_prompt_join_kernel(const KvArgs a, const PromptArgs g) {
+  __shared__ float s_f[kMaxWorkers][kJoinRows];            // of a part and row: maximum, then the factor of its sums
+  __shared__ float s_inv[kJoinRows];
+  __shared__ int s_parts[kMaxWorkers], s_n;
+  after_previous();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ctas = (int)gridDim.x, row0 = blockIdx.y * kJoinRows;
+  const PartNote* const notes = notes_of<D>(g.split);
   for (int i = 0; i < 2; ++i) {
-    if (!s_join[i]) continue;
-    const Cut c = s_cut[i];
-    const Request req = load_request(a, c.b);
-    const long long rows = (long long)req.q_len * a.group;
-    const long long first = worker_of(c.at), final = worker_of(c.at + c.len - 1);
-    // where the parts of the CTAs that share the item are, in order
-    if (warp == 0) {
-      int n = 0;
-      for (long long w0 = first; w0 <= final; w0 += 32) {
-        const long long w = w0 + lane;
-        int k0 = 0, k1 = 0;
-        if (w <= final) cut(edge(w), edge(w + 1), c.at, c.len, c.n, k0, k1);
-        const uint32_t some = __ballot_sync(0xFFFFFFFFu, k0 < k1);
-        if (k0 < k1) s_parts[n + __popc(some & ((1u << lane) - 1u))] = (int)(2 * w + (c.at >= edge(w) ? 1 : 0));
+    const PartNote mine = notes[2 * blockIdx.x + i];
+    if (mine.n == 0 || mine.k0 != 0) continue;
+    const long long rows = (long long)mine.q_len * a.group - (long long)mine.tile * kItemRows;
+    const int live = (int)min((long long)kJoinRows, rows - row0);
+    if (live <= 0) continue;
+    if (warp == 0) {                                       // the other parts, in order (a CTA whose part has no block left none)
+      int n = 1;
+      bool all = false;
+      if (lane == 0) s_parts[0] = 2 * blockIdx.x + i;
+      for (int w0 = blockIdx.x + 1; w0 < ctas && !all; w0 += 32) {
+        PartNote p{};
+        if (w0 + lane < ctas) p = notes[2 * (w0 + lane)];
+        const bool same = p.n != 0 && p.b == mine.b && p.h == mine.h && p.tile == mine.tile;
+        const uint32_t some = __ballot_sync(0xFFFFFFFFu, same);
+        if (same) s_parts[n + __popc(some & ((1u << lane) - 1u))] = 2 * (w0 + lane);
         n += __popc(some);
+        all = __any_sync(0xFFFFFFFFu, (same && p.k1 == p.n) || (p.n != 0 && !same));
       }
-      if (lane == 0) s_n_parts = n;
+      if (lane == 0) s_n = n;
     }
     __syncthreads();
-    const int n_parts = s_n_parts;
-    auto part = [&](int i) { return (const float*)(g.split.partials + (size_t)s_parts[i] * kPitch); };
-    // maximum and sum of every row
-    float* const s_m = reinterpret_cast<float*>(smem_raw);
-    float* const s_inv = s_m + kItemRows;
-    if (threadIdx.x < kItemRows) {
-      const int r = threadIdx.x, row = c.tile * kItemRows + r;
-      float mm = -INFINITY, den = 0.f;
+    const int n = s_n;
+    auto part = [&](int j) { return (const float*)(g.split.partials + (size_t)s_parts[j] * kPitch<D>); };
+    for (int j = warp; j < n; j += kJoinThreads / 32) s_f[j][lane] = __ldcg(part(j) + row0 + lane);
+    __syncthreads();
+    if (warp == 0) {
+      float m = -INFINITY, den = 0.f;
+      for (int j = 0; j < n; ++j) m = fmaxf(m, s_f[j][lane]);
+      const float mu = m == -INFINITY ? 0.f : m;
 #pragma unroll 4
-      for (int i = 0; i < n_parts; ++i) mm = fmaxf(mm, __ldcg(part(i) + r));
-      const float mu = mm == -INFINITY ? 0.f : mm;
+      for (int j = 0; j < n; ++j) {
+        const float f = exp2_fast(s_f[j][lane] - mu);
+        den = fmaf(f, __ldcg(part(j) + kItemRows + row0 + lane), den);
+        s_f[j][lane] = f;
+      }
+      const bool none = m == -INFINITY && den == 0.f;
+      s_inv[lane] = none ? 0.f : 1.0f / den;
+      const int row = mine.tile * kItemRows + row0 + lane;
+      if (lane < live && g.lse != nullptr)
+        g.lse[(int64_t)(mine.q0 + row / a.group) * a.n_heads + mine.h * a.group + row % a.group] =
+            none ? -INFINITY : kLn2 * (log2f(den) + m - kShift);
+    }
+    __syncthreads();
+    constexpr int kPieces = D / 4, kEach = kJoinRows * kPieces / kJoinThreads;   // four channels each
+    float4 sum[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) sum[e] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-      for (int i = 0; i < n_parts; ++i) den += exp2_fast(__ldcg(part(i) + r) - mu) * __ldcg(part(i) + kItemRows + r);
-      const bool none = mm == -INFINITY && den == 0.f;
-      s_m[r] = mu;
-      s_inv[r] = none ? 0.f : 1.0f / den;
-      if (row < rows && g.lse != nullptr)
-        g.lse[(int64_t)(req.q0 + row / a.group) * a.n_heads + c.h * a.group + row % a.group] =
-            none ? -INFINITY : kLn2 * (log2f(den) + mm - kShift);
-    }
-    __syncthreads();
-    constexpr int kEach = 8;                               // pieces of four channels of a thread, whose loads are under way at once
-    for (int e0 = 0; e0 < kItemRows * (D / 4); e0 += kThreads * kEach) {
-      float4 sum[kEach];
+    for (int j = 0; j < n; ++j) {
+      const float4* from = reinterpret_cast<const float4*>(part(j) + 2 * kItemRows + (size_t)row0 * D);
 #pragma unroll
-      for (int j = 0; j < kEach; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int i = 0; i < n_parts; ++i) {
-        const float* p = part(i);
-        float4 v[kEach];
-        float f[kEach];
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          const int e = e0 + j * kThreads + (int)threadIdx.x;
-          v[j] = __ldcg(reinterpret_cast<const float4*>(p + 2 * kItemRows) + e);
-          f[j] = __ldcg(p + e / (D / 4));
-        }
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          const int e = e0 + j * kThreads + (int)threadIdx.x;
-          const float x = exp2_fast(f[j] - s_m[e / (D / 4)]);
-          sum[j].x = fmaf(v[j].x, x, sum[j].x); sum[j].y = fmaf(v[j].y, x, sum[j].y);
-          sum[j].z = fmaf(v[j].z, x, sum[j].z); sum[j].w = fmaf(v[j].w, x, sum[j].w);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        const int e = e0 + j * kThreads + (int)threadIdx.x, r = e / (D / 4), d = (e % (D / 4)) * 4;
-        const int row = c.tile * kItemRows + r;
-        if (row >= rows) continue;
-        const int64_t at = (int64_t)(req.q0 + row / a.group) * a.n_heads + c.h * a.group + row % a.group;
-        const float inv = s_inv[r];
-        const __nv_bfloat162 y0 = __floats2bfloat162_rn(inv == 0.f ? 0.f : sum[j].x * inv, inv == 0.f ? 0.f : sum[j].y * inv);
-        const __nv_bfloat162 y1 = __floats2bfloat162_rn(inv == 0.f ? 0.f : sum[j].z * inv, inv == 0.f ? 0.f : sum[j].w * inv);
-        *reinterpret_cast<uint2*>(g.out + at * D + d) =
-            make_uint2(*reinterpret_cast<const uint32_t*>(&y0), *reinterpret_cast<const uint32_t*>(&y1));
+      for (int e = 0; e < kEach; ++e) {
+        const int at = e * kJoinThreads + (int)threadIdx.x;
+        const float4 v = __ldcg(from + at);
+        const float f = s_f[j][at / kPieces];
+        sum[e].x = fmaf(v.x, f, sum[e].x); sum[e].y = fmaf(v.y, f, sum[e].y);
+        sum[e].z = fmaf(v.z, f, sum[e].z); sum[e].w = fmaf(v.w, f, sum[e].w);
       }
     }
-    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int at = e * kJoinThreads + (int)threadIdx.x, r = at / kPieces, d = (at % kPieces) * 4;
+      if (r >= live) continue;
+      const int row = mine.tile * kItemRows + row0 + r;
+      const int64_t to = (int64_t)(mine.q0 + row / a.group) * a.n_heads + mine.h * a.group + row % a.group;
+      const float inv = s_inv[r];
+      const __nv_bfloat162 y0 = __floats2bfloat162_rn(inv == 0.f ? 0.f : sum[e].x * inv, inv == 0.f ? 0.f : sum[e].y * inv);
+      const __nv_bfloat162 y1 = __floats2bfloat162_rn(inv == 0.f ? 0.f : sum[e].z * inv, inv == 0.f ? 0.f : sum[e].w * inv);
+      *reinterpret_cast<uint2*>(g.out + to * D + d) =
+          make_uint2(*reinterpret_cast<const uint32_t*>(&y0), *reinterpret_cast<const uint32_t*>(&y1));
+    }
+    __syncthreads();                                       // before the second item's parts take the places of this one's
   }
 }
 
@@ -927,7 +926,10 @@ int launch(const KvArgs& a, const PromptArgs& g, cudaStream_t st) {
   if (rc != TLQ_OK) return rc;
   const int sms = device_sm_count();
   if (sms <= 0) return TLQ_ERR_CUDA;
-  return launch_next(kv_prompt_kernel<D>, dim3((unsigned)(sms < kMaxWorkers ? sms : kMaxWorkers)), kThreads, kSmem<D>, 1, st, a, g);
+  const unsigned ctas = (unsigned)(sms < kMaxWorkers ? sms : kMaxWorkers);
+  const int rp = launch_next(kv_prompt_kernel<D>, dim3(ctas), kThreads, kSmem<D>, 1, st, a, g);
+  if (rp != TLQ_OK) return rp;
+  return launch_next(kv_prompt_join_kernel<D>, dim3(ctas, kItemRows / kJoinRows), kJoinThreads, 0, 1, st, a, g);
 }
 
 }  // namespace

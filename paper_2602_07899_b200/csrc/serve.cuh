@@ -170,9 +170,13 @@ constexpr int kSplitWarps = 8;            // warps of one of them
 constexpr int kMaxRowTile = 16;           // query rows of one work item
 constexpr int kPromptItemRows = 256;      // query rows of one item of the prompt kernel (kv_prompt.cu)
 constexpr int kPromptRows = 64;           // requests with at least this many query rows per kv head go to it
+struct __align__(16) PartNote {           // a part of a row tile's blocks, [k0, k1) of n; n == 0: none
+  int b, h, tile, q0;
+  int q_len, k0, k1, n;
+};
 inline size_t kv_split_floats(int head_dim, int64_t rows) {   // two partials of every warp and of every CTA
   const size_t few = (size_t)kMaxWorkers * 2 * (kSplitWarps + 1) * kMaxRowTile * ((size_t)head_dim + 2);
-  const size_t many = (size_t)kMaxWorkers * 2 * kPromptItemRows * ((size_t)head_dim + 2);
+  const size_t many = (size_t)kMaxWorkers * 2 * (kPromptItemRows * ((size_t)head_dim + 2) + sizeof(PartNote) / sizeof(float));
   return rows >= kPromptRows && many > few ? many : few;
 }
 struct KvSplit {

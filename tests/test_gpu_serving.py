@@ -218,6 +218,11 @@ def test_attention_split_over_the_context(tlq, q_lens, kv_lens):
     check_attention(tlq, make_batch(9, q_lens, kv_lens, 2, 128), 12, 2, 128, True, 10)
 
 
+def test_attention_of_many_rows_before_the_first_key(tlq):
+    """Runs of row tiles without a visible key between tiles that have some, several of both for every CTA."""
+    check_attention(tlq, make_batch(19, [2000] * 20, [70] * 20, 8, 64), 8, 8, 64, True, 13)
+
+
 @pytest.mark.parametrize("q_len", [1, 150])
 def test_attention_with_steps_of_zero_and_of_very_different_size(tlq, q_len):
     """A block of zeros (step 0) still takes part in the softmax; value steps span fourteen powers of ten."""
