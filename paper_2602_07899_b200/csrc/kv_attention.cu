@@ -42,7 +42,7 @@ struct AttnArgs {
   uint16_t* out;
   float* lse;
   float scale_log2;          // scale * log2(e)
-  int causal, max_rows;      // requests with max_rows query rows or more belong to the prompt kernel
+  int causal, prompts;       // prompts: the prompt kernel has run before (and may have had something to do)
   KvSplit split;
 };
 
@@ -313,7 +313,8 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
   if (threadIdx.x < 2) s_cta[threadIdx.x].begin = s_cta[threadIdx.x].end = 0;
   if (lane == 0) s_has[warp] = 0;
   after_previous();
-  auto count_units = [&](int b) { return units_of(a, load_request(a, b), kRows, g.max_rows).total; };
+  const int max_rows = g.prompts && is_prompt_work<kThreads>(a, g.causal, sums) ? kPromptRows : 0x7FFFFFFF;
+  auto count_units = [&](int b) { return units_of(a, load_request(a, b), kRows, max_rows).total; };
   // no more CTAs than give each warp of a CTA a block
   auto workers_of = [&](long long all) { return min((all + kWarps - 1) / kWarps, (long long)gridDim.x); };
   long long total = 0;
@@ -338,7 +339,7 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
 
   if (w_begin < w_end) {
     Walker con;                                            // what is computed now
-    con.max_rows = g.max_rows;
+    con.max_rows = max_rows;
     {
       int b = found.request;
       long long rest = found.rest + (w_begin - u_begin);
@@ -737,9 +738,9 @@ int launch_kv_attention(const uint16_t* q, int64_t ldq, int head_dim, const KvAr
   g.causal = causal;
   g.split = split;
   const int64_t rows = (int64_t)a.group * (a.T < a.max_q_len ? a.T : a.max_q_len);     // of one request, at most
-  g.max_rows = kPromptRows;
-  if (rows >= kPromptRows) {
-    const int rc = launch_kv_prompt(q, ldq, head_dim, a, scale, causal, kPromptRows, out, lse, split, st);
+  g.prompts = rows >= kPromptRows && (double)a.T * a.n_heads * ((double)a.max_blocks * kKvBlock + kRowKeys) >= (double)kPromptPairs;
+  if (g.prompts) {
+    const int rc = launch_kv_prompt(q, ldq, head_dim, a, scale, causal, out, lse, split, st);
     if (rc != TLQ_OK) return rc;
   }
   const bool narrow = rows <= 8;

@@ -35,12 +35,12 @@ constexpr int kSoftWarps = 8, kLoadWarps = 4, kIssueWarp = kSoftWarps + kLoadWar
 constexpr int kThreads = 512;                              // four groups of four warps
 // registers of a thread of each role: 2 x 176 + 72 + 88 = 4 x 128, what the block is launched with
 constexpr int kSoftRegs = 176, kLoadRegs = 72, kIssueRegs = 88;
-constexpr float kShift = 11.f, kGrow = 4.f;
+constexpr float kShift = 11.f, kGrow = 4.9f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kStepFloor = 7.8886090522101181e-31f;      // 2^-100, as in kv_attention.cu
 constexpr float kUnit = 16777216.f;                        // 2^24
-constexpr int kMinTiles = 12;                              // blocks of a CTA's part, at least
-constexpr int kItemCost = 12;                              // what an item costs beside its blocks, in blocks
+constexpr int kMinTiles = 6;                               // blocks of a CTA's part, at least
+constexpr int kItemCost = 8;                               // what an item costs beside its blocks, in blocks
 
 struct PromptArgs {
   const uint16_t* q;
@@ -48,7 +48,7 @@ struct PromptArgs {
   uint16_t* out;
   float* lse;
   float scale_log2;
-  int causal, min_rows;         // requests with fewer rows than this belong to the few-row kernel
+  int causal;
   KvSplit split;
 };
 
@@ -220,7 +220,7 @@ struct Costs {
 __device__ __forceinline__ Costs costs_of(const KvArgs& a, const PromptArgs& g, const Request& r) {
   Costs c;
   const long long rows = (long long)r.q_len * a.group;
-  c.tiles = rows >= g.min_rows ? (int)((rows + kItemRows - 1) / kItemRows) : 0;
+  c.tiles = rows >= kPromptRows ? (int)((rows + kItemRows - 1) / kItemRows) : 0;
   const int seen = g.causal ? min(max(r.kv - r.q_len, 0) + kItemRows / a.group, r.kv) : r.kv;
   c.first = 64LL * (kItemCost + 1) + 64LL * seen / kKeys;
   c.more = g.causal ? 64LL * kItemRows / kKeys / a.group : 0;
@@ -348,6 +348,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
   after_previous();
   auto no_parts = [&]() { notes_of<D>(g.split)[2 * blockIdx.x].n = notes_of<D>(g.split)[2 * blockIdx.x + 1].n = 0; };
   if (threadIdx.x == 0) no_parts();
+  if (!is_prompt_work<kThreads>(a, g.causal, sums)) return;   // left to the few-row kernel
   // ---------------------------------------------------------------- this CTA's part of the line
   auto cost_of = [&](int b) {
     const Costs c = costs_of(a, g, load_request(a, b));
@@ -386,6 +387,9 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     if (++seg == kRing) { seg = 0; seg_phase ^= 1u; }
   };
 
+  auto tile_live = [&](const Segment* s, int t) {          // whether it has rows at all
+    return (long long)s->tile * kItemRows + t * kTile < (long long)s->q_len * a.group;
+  };
   // waits until all products of a block are complete (block number st of this CTA, none before st - kStages open)
   auto products_of = [&](int st) {
     return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(kBarFree + st % kStages), (uint32_t)(st / kStages) & 1u, abort_flag)) != 0;
@@ -398,20 +402,21 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     constexpr uint32_t kIdescS = ptx::make_idesc(1, 0, kTile, kKeys, false);   // f16 x f16 -> f32
     constexpr uint32_t kIdescO = ptx::make_idesc(1, 0, kTile, D, false);
     const bool leader = elect_one();
-    int step = 0;                                          // blocks so far, of all segments
+    int step = 0, passed = 0;                              // blocks so far, of all segments; those without a row of this tile
     uint32_t q_phase = 0;
     bool ok = true;
     auto wait = [&](int i, uint32_t parity) { ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(i), parity, abort_flag)) != 0; };
     auto scores = [&](int st) {                            // S of block number st into its buffer
+      const int buf = (st - passed) & 1;
       if (leader) {
 #pragma unroll
         for (uint32_t c = 0; c < kPanels<D>; ++c) {
           const uint64_t x = ptx::smem_desc_sw128(q_at + T * kQBytes<D> + c * (kTile * 128));
           const uint64_t y = ptx::smem_desc_sw128(k_at + (st % kStages) * kKBytes<D> + c * (kKeys * 128));
 #pragma unroll
-          for (int i = 0; i < 4; ++i) mma_f16_ss(tmem + T * kTile + (st & 1) * kKeys, x + 2 * i, y + 2 * i, kIdescS, c > 0 || i > 0);
+          for (int i = 0; i < 4; ++i) mma_f16_ss(tmem + T * kTile + buf * kKeys, x + 2 * i, y + 2 * i, kIdescS, c > 0 || i > 0);
         }
-        ptx::mma_commit(bar(kBarS + 2 * T + (st & 1)));
+        ptx::mma_commit(bar(kBarS + 2 * T + buf));
       }
       __syncwarp();
     };
@@ -420,10 +425,19 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       ok = __all_sync(0xFFFFFFFFu, ok);
       if (!ok) break;
       const int k0 = from->k0, k1 = from->k1;
+      const bool live = tile_live(from, T);
       __syncwarp();
       if (lane == 0) done_segment(); else if (++seg == kRing) { seg = 0; seg_phase ^= 1u; }
       if (k0 < 0) break;
       if (k0 >= k1) continue;
+      if (!live) {                                         // no rows: the blocks pass
+        for (int k = k0; k < k1 && ok; ++k, ++step, ++passed) {
+          wait(kBarFull + step % kStages, (uint32_t)(step / kStages) & 1u);
+          if (ok && lane == 0) ptx::mbar_arrive(bar(kBarFree + step % kStages));
+        }
+        if (!ok) break;
+        continue;
+      }
       wait(kBarQ + T, q_phase);
       if (!ok) break;
       ptx::tc_fence_after();
@@ -433,17 +447,17 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
         if (ok) scores(st);
       }
       for (int k = k0; k < k1 && ok; ++k, ++step) {
-        const int stage = step % kStages, ahead = step + 2;
+        const int stage = step % kStages, ahead = step + 2, turn = step - passed;
         if (k + 2 < k1) wait(kBarFull + ahead % kStages, (uint32_t)(ahead / kStages) & 1u);   // long ready, off the chain P -> S
         if (!ok) break;
-        wait(kBarP + 2 * T + (step & 1), (uint32_t)(step >> 1) & 1u);
+        wait(kBarP + 2 * T + (turn & 1), (uint32_t)(turn >> 1) & 1u);
         if (!ok) break;
         ptx::tc_fence_after();
         if (leader) {
           const uint64_t y = ptx::smem_desc_sw128(v_at + stage * kVBytes<D>);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            mma_f16_ts(tmem + 256 + T * kTile, tmem + T * kTile + (step & 1) * kKeys + 8 * i, y + 2 * i, kIdescO, k > k0 || i > 0);
+            mma_f16_ts(tmem + 256 + T * kTile, tmem + T * kTile + (turn & 1) * kKeys + 8 * i, y + 2 * i, kIdescO, k > k0 || i > 0);
         }
         if (k + 2 < k1) scores(ahead);
         if (leader) ptx::mma_commit(bar(kBarFree + stage));
@@ -459,7 +473,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
     const int t = warp >> 2, row_in_tile = (warp & 3) * 32 + lane;
     const uint32_t s_col = tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * kTile, o_col = s_col + 256;   // P over S
     constexpr int kRowLanes = D / 8, kRowsAtOnce = 32 / kRowLanes;       // lanes that hold a row, 16 bytes each
-    int step = 0;                                          // blocks so far, of all segments
+    int step = 0, passed = 0;                              // blocks so far, of all segments; those without a row of this tile
     bool ok = true;
     while (true) {
       const Segment* s = next_segment(ok);
@@ -470,6 +484,13 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
         PartNote* note = notes_of<D>(g.split) + 2 * blockIdx.x + s->starts;
         note->b = s->b; note->h = s->h; note->tile = s->tile; note->q0 = s->q0;
         note->q_len = s->q_len; note->k0 = k0; note->k1 = k1; note->n = s->n;
+      }
+      if (!tile_live(s, t)) {
+        step += k1 - k0;
+        passed += k1 - k0;
+        __syncwarp();
+        if (lane == 0) done_segment(); else if (++seg == kRing) { seg = 0; seg_phase ^= 1u; }
+        continue;
       }
       const int row = s->tile * kItemRows + t * kTile + row_in_tile, token = row / a.group;
       const bool live = token < s->q_len;
@@ -525,8 +546,8 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
 
       float m = -INFINITY, l = 0.f;
       for (int k = k0; k < k1; ++k, ++step) {
-        const int buf = (step & 1) * kKeys;
-        ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(kBarS + 2 * t + (step & 1)), (uint32_t)(step >> 1) & 1u, abort_flag));
+        const int turn = step - passed, buf = (turn & 1) * kKeys;
+        ok = __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar(kBarS + 2 * t + (turn & 1)), (uint32_t)(turn >> 1) & 1u, abort_flag));
         if (!ok) break;
         ptx::tc_fence_after();
         uint32_t v[2][32];                                 // the row of S
@@ -600,7 +621,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
         tmem_st_wait();
         ptx::tc_fence_before();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(bar(kBarP + 2 * t + (step & 1)));
+        if (lane == 0) ptx::mbar_arrive(bar(kBarP + 2 * t + (turn & 1)));
       }
       if (!ok) break;
 
@@ -934,13 +955,12 @@ int launch(const KvArgs& a, const PromptArgs& g, cudaStream_t st) {
 
 }  // namespace
 
-int launch_kv_prompt(const uint16_t* q, int64_t ldq, int head_dim, const KvArgs& a, float scale, int causal, int min_rows,
-                     uint16_t* out, float* lse, const KvSplit& split, cudaStream_t st) {
+int launch_kv_prompt(const uint16_t* q, int64_t ldq, int head_dim, const KvArgs& a, float scale, int causal, uint16_t* out,
+                     float* lse, const KvSplit& split, cudaStream_t st) {
   PromptArgs g{};
   g.q = q; g.ldq = ldq; g.out = out; g.lse = lse;
   g.scale_log2 = scale * kLog2e;
   g.causal = causal;
-  g.min_rows = min_rows;
   g.split = split;
   return head_dim == 128 ? launch<128>(a, g, st) : launch<64>(a, g, st);
 }

@@ -119,6 +119,35 @@ __device__ __forceinline__ bool plan_items(int B, F count, G target_of, long lon
   return found->request >= 0;
 }
 
+constexpr int kPromptRows = 64;           // requests with at least this many query rows per kv head go to it ...
+// ... if such requests have this many pairs of a row and a key, every row counted with 256 keys on top (the few-row kernel
+// works on 16 rows at a time and pays for each such item once).  The prompt kernel and its join take 20 to 25 us however
+// little there is to do, the few-row kernel 10, but that one gets no more than 0.25 M pairs done in a us.  Measured, few-row
+// against prompt kernel: 126 rows x 4096 keys x 4 kv heads (2.2 M) 29 : 41 us, 336 x 2000 x 4 (3.0 M) 32 : 37, prompts of 512
+// tokens with 512 rows x 8 (2.1 M) 23 : 26, 3072 x 2 (3.1 M) 45 : 35 and 3584 x 4 (7.3 M) 53 : 35, 800 rows x 1000 x 8 (7.7 M)
+// 35 : 30, 840 x 4096 x 4 (15 M) 70 : 45, 576 rows in 8 requests x 8000 x 8 (38 M) 137 : 105.
+constexpr long long kPromptPairs = 3100000;
+constexpr int kRowKeys = 256;
+
+// Whether the requests of at least kPromptRows rows are the prompt kernel's: their pairs of a row and a key (about half of the
+// new ones where the mask is causal), all counted by both kernels alike.  All threads of the block call it.
+template <int kThreads>
+__device__ __forceinline__ bool is_prompt_work(const KvArgs& a, int causal, long long* sums) {
+  long long all = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+    const int b = b0 + (int)threadIdx.x;
+    long long n = 0, total;
+    if (b < a.B) {
+      const Request r = load_request(a, b);
+      const long long rows = (long long)r.q_len * a.group;
+      if (rows >= kPromptRows) n = rows * ((causal ? max(r.kv - r.q_len / 2, r.kv / 2) : r.kv) + kRowKeys) * a.n_kv;
+    }
+    block_scan<kThreads>(n, sums, total);
+    all += total;
+  }
+  return all >= kPromptPairs;
+}
+
 // ---------------------------------------------------------------------------------------------- launches
 // Kernels of these operators follow one another in every layer, most of them a few microseconds long.  They are launched
 // so that a kernel's blocks may come up while the one before it on the stream still runs (programmatic dependent
@@ -169,7 +198,6 @@ constexpr int kMaxWorkers = 160;          // CTAs that share one call's work (on
 constexpr int kSplitWarps = 8;            // warps of one of them
 constexpr int kMaxRowTile = 16;           // query rows of one work item
 constexpr int kPromptItemRows = 256;      // query rows of one item of the prompt kernel (kv_prompt.cu)
-constexpr int kPromptRows = 64;           // requests with at least this many query rows per kv head go to it
 struct __align__(16) PartNote {           // a part of a row tile's blocks, [k0, k1) of n; n == 0: none
   int b, h, tile, q0;
   int q_len, k0, k1, n;
@@ -183,8 +211,8 @@ struct KvSplit {
   int32_t* counters;          // [kMaxWorkers]
   float* partials;            // kv_split_floats()
 };
-int launch_kv_prompt(const uint16_t* q, int64_t ldq, int head_dim, const KvArgs& a, float scale, int causal, int min_rows,
-                     uint16_t* out, float* lse, const KvSplit& split, cudaStream_t st);
+int launch_kv_prompt(const uint16_t* q, int64_t ldq, int head_dim, const KvArgs& a, float scale, int causal, uint16_t* out,
+                     float* lse, const KvSplit& split, cudaStream_t st);
 int launch_kv_attention(const uint16_t* q, int64_t ldq, int head_dim, const KvArgs& a, float scale, int causal,
                         uint16_t* out, float* lse, const KvSplit& split, cudaStream_t st);
 

@@ -407,6 +407,14 @@ def _by_address(name: str):
 _kv_store, _kv_attention = _by_address("tlq_kv_store"), _by_address("tlq_kv_attention")
 
 
+def _workspace_on(stream, make, *args) -> torch.Tensor:
+    """A workspace for one call, zeroed on the stream that the call runs on."""
+    if stream is None:
+        return make(*args)
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))):
+        return make(*args)
+
+
 @functools.lru_cache(maxsize=64)
 def _host_ints(values: tuple):
     return (ctypes.c_int32 * len(values))(*values)
@@ -443,7 +451,7 @@ def tlq_linear_i8(Xq: torch.Tensor, t: torch.Tensor, Wq: torch.Tensor, u: torch.
     if bias is not None:
         _typed(bias, _BF16, (C2,), "bias")
     if workspace is None:
-        workspace = linear_workspace(N, C1, C2, Xq.device)
+        workspace = _workspace_on(stream, linear_workspace, N, C1, C2, Xq.device)
     if out is None:
         out = Xq.new_empty((N, C2), dtype=_BF16)
     else:
@@ -485,7 +493,7 @@ def tlq_kv_store(qkv: torch.Tensor, n_heads: int, cache: KvCache, batch: KvBatch
     if k_norm is not None:
         _typed(k_norm, _BF16, (d,), "k_norm")
     if workspace is None:
-        workspace = kv_workspace(cache, n_heads, T, batch)
+        workspace = _workspace_on(stream, kv_workspace, cache, n_heads, T, batch)
     q = qkv.new_empty((T, n_heads, d))
     k = v = None
     if want_values:
@@ -508,7 +516,7 @@ def tlq_kv_attention(q: torch.Tensor, cache: KvCache, batch: KvBatch, scale: flo
         raise ValueError("q and the cache differ in head_dim")
     ldq = _rows(q, "q")
     if workspace is None:
-        workspace = kv_workspace(cache, n_heads, T, batch)
+        workspace = _workspace_on(stream, kv_workspace, cache, n_heads, T, batch)
     out = q.new_empty((T, n_heads, d))
     lse = q.new_empty((T, n_heads), dtype=_F32) if want_lse else None
     _check(_kv_attention(q.data_ptr(), T, ldq, n_heads, cache._p, batch._p, scale, 1 if causal else 0,

@@ -192,6 +192,18 @@ def check_attention(tlq, s, heads, hk, d, causal, seed, stride=0):
         assert torch.all(out.cpu()[none] == 0)
 
 
+# A request of this size takes a batch over the 3 M pairs from which requests of many rows have a kernel of their own.
+BIG = (1000, 1400)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads,hk,d", [(12, 2, 128), (7, 1, 128), (8, 8, 64), (14, 2, 64), (5, 1, 64), (32, 1, 128), (4, 4, 128)])
+def test_attention_of_prompts(tlq, heads, hk, d, causal):
+    """Row tiles and blocks that end anywhere, requests on both sides of the limit of rows, some of them empty."""
+    q_lens, kv_lens = [40, 1, 129, 0, BIG[0], 64, 3, 257], [40, 65, 500, 9, BIG[1], 64, 0, 250]
+    check_attention(tlq, make_batch(12, q_lens, kv_lens, hk, d), heads, hk, d, causal, 5)
+
+
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("lens", sorted(LENS))
 @pytest.mark.parametrize("heads,hk,d", HEADS)
@@ -204,6 +216,7 @@ def test_attention(tlq, heads, hk, d, lens, causal):
 def test_attention_of_strided_queries(tlq, heads, hk, d):
     for q_lens, kv_lens in (([1, 1], [90, 200]), ([70, 200], [100, 260])):
         check_attention(tlq, make_batch(2, q_lens, kv_lens, hk, d), heads, hk, d, True, 6, stride=2 * hk * d)
+    check_attention(tlq, make_batch(2, [70, BIG[0]], [100, BIG[1]], hk, d), heads, hk, d, True, 6, stride=2 * hk * d)
 
 
 def test_attention_of_many_requests(tlq):
@@ -223,10 +236,10 @@ def test_attention_of_many_rows_before_the_first_key(tlq):
     check_attention(tlq, make_batch(19, [2000] * 20, [70] * 20, 8, 64), 8, 8, 64, True, 13)
 
 
-@pytest.mark.parametrize("q_len", [1, 150])
-def test_attention_with_steps_of_zero_and_of_very_different_size(tlq, q_len):
+@pytest.mark.parametrize("q_len,big", [(1, False), (150, False), (150, True)])
+def test_attention_with_steps_of_zero_and_of_very_different_size(tlq, q_len, big):
     """A block of zeros (step 0) still takes part in the softmax; value steps span fourteen powers of ten."""
-    s = make_batch(21, [q_len], [64 * 8], 1, 128)
+    s = make_batch(21, [q_len] + [BIG[0]] * big, [64 * 8] + [BIG[1]] * big, 1, 128)
     b = s["table"][0].long()
     s["ks"][b[1]] = 0.0
     s["vs"][b[2]] = 0.0
@@ -236,19 +249,19 @@ def test_attention_with_steps_of_zero_and_of_very_different_size(tlq, q_len):
     check_attention(tlq, s, 7, 1, 128, False, 3)
 
 
-@pytest.mark.parametrize("q_len", [1, 150])
-def test_attention_with_large_and_small_scores(tlq, q_len):
+@pytest.mark.parametrize("q_len,big", [(1, False), (150, False), (150, True)])
+def test_attention_with_large_and_small_scores(tlq, q_len, big):
     """Scores in the hundreds either way: the running maximum moves far from block to block."""
-    s = make_batch(22, [q_len], [64 * 9 + 5], 1, 64)
+    s = make_batch(22, [q_len] + [BIG[0]] * big, [64 * 9 + 5] + [BIG[1]] * big, 1, 64)
     b = s["table"][0].long()
     for i in range(9):
         s["ks"][b[i]] = (0.5, 0.0001, 0.02)[i % 3] * (i + 1)
     check_attention(tlq, s, 4, 1, 64, True, 4)
 
 
-@pytest.mark.parametrize("q_len", [1, 200])
-def test_attention_keeps_non_finite_queries_to_their_rows(tlq, q_len):
-    s = make_batch(31, [q_len, q_len], [400, 300], 2, 128)
+@pytest.mark.parametrize("q_len,big", [(1, False), (200, False), (200, True)])
+def test_attention_keeps_non_finite_queries_to_their_rows(tlq, q_len, big):
+    s = make_batch(31, [q_len, q_len] + [BIG[0]] * big, [400, 300] + [BIG[1]] * big, 2, 128)
     q = torch.randn(s["T"], 12, 128, generator=gen(1)).bfloat16()
     bad = q.clone()
     bad[0, 3, 5] = math.nan
@@ -263,16 +276,32 @@ def test_attention_keeps_non_finite_queries_to_their_rows(tlq, q_len):
     assert torch.isfinite(lse.cpu()[~hit]).all()
 
 
-def test_attention_of_huge_and_tiny_queries(tlq):
+@pytest.mark.parametrize("q_len,kv_len", [(4, 200), BIG])
+def test_attention_of_huge_and_tiny_queries(tlq, q_len, kv_len):
     """Rows far outside of the 16-bit float range of the products: a power of two per row takes care of them."""
-    s = make_batch(33, [4], [200], 1, 128)
+    s = make_batch(33, [q_len], [kv_len], 1, 128)
     s["ks"][:] = s["ks"].nan_to_num(0.01) * 0 + 1e-3
-    q = torch.randn(4, 7, 128, generator=gen(2)).bfloat16()
+    q = torch.randn(q_len, 7, 128, generator=gen(2)).bfloat16()
     cache, batch = on_gpu(tlq, s)
     want, _ = tlq.tlq_kv_attention(q.cuda(), cache, batch, 2.0 ** -3)
     for f in (2.0 ** 40, 2.0 ** -40, 2.0 ** -100):
         got, _ = tlq.tlq_kv_attention((q.float() * f).bfloat16().cuda(), cache, batch, 2.0 ** -3 / f)
         assert torch.equal(got, want)
+
+
+def test_attention_of_prompts_reports_a_block_that_does_not_fit(tlq):
+    s = make_batch(43, [BIG[0], 70], [BIG[1], 130], 1, 64)
+    q = torch.randn(s["T"], 4, 64, generator=gen(3)).bfloat16().cuda()
+    cache, batch = on_gpu(tlq, s)
+    ws = tlq.kv_workspace(cache, 4, s["T"], batch)
+    good, _ = tlq.tlq_kv_attention(q, cache, batch, 0.125, workspace=ws)
+    assert tlq.tlq_read_status(ws) == tlq.OK
+    s["table"][0, 3] = 1 << 30
+    cache, batch = on_gpu(tlq, s)
+    ws = tlq.kv_workspace(cache, 4, s["T"], batch)
+    out, _ = tlq.tlq_kv_attention(q, cache, batch, 0.125, workspace=ws)
+    assert tlq.tlq_read_status(ws) == tlq.ERR_SHAPE
+    assert torch.equal(out[BIG[0]:], good[BIG[0]:]) and torch.isfinite(out.float()).all()
 
 
 def test_attention_reports_metadata_that_does_not_fit(tlq):
@@ -507,3 +536,77 @@ def test_store_then_attention_on_another_stream(tlq):
             most, most_lse = attention_bounds(want, wl, mag, small, weight, d)
             assert torch.all((out.double().cpu() - want).abs() <= most)
             assert torch.all((lse.double().cpu() - wl).abs() <= most_lse)
+
+
+@pytest.mark.parametrize("q_lens,kv_lens", [([1, 5], [300, 200]), (list(BIG[:1]) + [70], list(BIG[1:]) + [100])])
+def test_blocks_beyond_four_gigabytes(tlq, q_lens, kv_lens):
+    """Block numbers whose bytes lie beyond 2^32: the same bits as from a small cache."""
+    hk, d, heads = 8, 128, 16
+    s = make_batch(51, q_lens, kv_lens, hk, d)
+    n_blocks = (1 << 32) // (hk * BLOCK * d) + s["kc"].shape[0]
+    big = tlq.KvCache(*[torch.empty((n_blocks, *s[k].shape[1:]), dtype=s[k].dtype, device="cuda") for k in ("kc", "vc", "ks", "vs")])
+    t = dict(s, table=s["table"] + (n_blocks - s["kc"].shape[0]))
+    qkv = torch.randn(s["T"], (heads + 2 * hk) * d, generator=gen(6)).bfloat16().cuda()
+    results = []
+    for batch_of, cache in ((s, tlq.KvCache(*[s[k].cuda() for k in ("kc", "vc", "ks", "vs")])), (t, big)):
+        for name in ("k_codes", "v_codes", "k_steps", "v_steps"):
+            getattr(cache, name)[-s["kc"].shape[0]:] = s[name[:1] + name[2]].cuda()
+        batch = tlq.KvBatch(s["cu"].cuda(), s["kv"].cuda(), batch_of["table"].cuda(), s["q_max"])
+        ws = tlq.kv_workspace(cache, heads, s["T"], batch)
+        q, _, _ = tlq.tlq_kv_store(qkv, heads, cache, batch, workspace=ws)
+        out, lse = tlq.tlq_kv_attention(q, cache, batch, d ** -0.5, want_lse=True, workspace=ws)
+        assert tlq.tlq_read_status(ws) == tlq.OK
+        tail = [getattr(cache, name)[-s["kc"].shape[0]:].clone() for name in ("k_codes", "v_codes")]
+        results.append([q, out, lse] + tail)
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+def test_step_recorded_as_a_graph(tlq):
+    """Store and attention captured once and replayed with other inputs and lengths in the same places."""
+    hk, d, heads = 2, 128, 12
+    s = make_batch(53, [1, 1], [150, 64], hk, d)
+    lens = [s["kv"].clone(), s["kv"] - 3]
+    inputs = [torch.randn(2, (heads + 2 * hk) * d, generator=gen(7 + i)).bfloat16().cuda() for i in range(2)]
+
+    def fresh():
+        return tlq.KvCache(*[s[k].cuda() for k in ("kc", "vc", "ks", "vs")])
+
+    def step(x, cache, batch, ws):
+        q, _, _ = tlq.tlq_kv_store(x, heads, cache, batch, workspace=ws)
+        return tlq.tlq_kv_attention(q, cache, batch, d ** -0.5, workspace=ws)[0]
+
+    cache, x, kv = fresh(), inputs[0].clone(), lens[0].cuda()
+    batch = tlq.KvBatch(s["cu"].cuda(), kv, s["table"].cuda(), 1)
+    ws = tlq.kv_workspace(cache, heads, 2, batch)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(x, cache, batch, ws)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = step(x, cache, batch, ws)
+    for i in (1, 0, 1):
+        for name, k in (("k_codes", "kc"), ("v_codes", "vc"), ("k_steps", "ks"), ("v_steps", "vs")):
+            getattr(cache, name).copy_(s[k])
+        x.copy_(inputs[i])
+        kv.copy_(lens[i])
+        graph.replay()
+        own = fresh()
+        want = step(inputs[i], own, tlq.KvBatch(s["cu"].cuda(), lens[i].cuda(), s["table"].cuda(), 1), None)
+        assert torch.equal(y, want) and torch.equal(cache.k_codes, own.k_codes) and torch.equal(cache.v_codes, own.v_codes)
+        assert tlq.tlq_read_status(ws) == tlq.OK
+
+
+def test_example_serves_a_calibrated_layer():
+    """Prompts and answers of the example against 32-bit floats.  Rounding to 8 bits is an error of step / sqrt(12); with the
+    largest value of a row at 4 to 8 deviations that is 1 to 2 % of a matrix product's inputs, for each of inputs, weights,
+    keys, values, attention's results and the output weights: 5 % together where they are independent.  10 % is a wrong block."""
+    import importlib.util
+    import pathlib
+    path = pathlib.Path(__file__).resolve().parent.parent / "examples" / "serve_layer.py"
+    spec = importlib.util.spec_from_file_location("serve_layer", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    assert example.main(["--requests", "3", "--prompt", "300", "--steps", "5", "--calibration", "256"]) < 0.10
