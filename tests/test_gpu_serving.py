@@ -600,13 +600,14 @@ def test_step_recorded_as_a_graph(tlq):
 
 
 def test_example_serves_a_calibrated_layer():
-    """Prompts and answers of the example against 32-bit floats.  Rounding to 8 bits is an error of step / sqrt(12); with the
-    largest value of a row at 4 to 8 deviations that is 1 to 2 % of a matrix product's inputs, for each of inputs, weights,
-    keys, values, attention's results and the output weights: 5 % together where they are independent.  10 % is a wrong block."""
+    """Prompts and answers of the example against 32-bit floats on the projections' codes.  Rounding to 8 bits is an error of
+    step / sqrt(12), with the largest of some thousand values at 4 deviations 0.9 %: of the values, of attention's results, and
+    of the keys, where it is multiplied by the scores' deviation (1.2 here, 2 where outliers make it so).  1.7 to 2.5 % where
+    they are independent; 5 % is a wrong block."""
     import importlib.util
     import pathlib
     path = pathlib.Path(__file__).resolve().parent.parent / "examples" / "serve_layer.py"
     spec = importlib.util.spec_from_file_location("serve_layer", path)
     example = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(example)
-    assert example.main(["--requests", "3", "--prompt", "300", "--steps", "5", "--calibration", "256"]) < 0.10
+    assert example.main(["--requests", "3", "--prompt", "300", "--steps", "5", "--calibration", "256"]) < 0.05
