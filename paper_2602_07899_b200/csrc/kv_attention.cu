@@ -738,7 +738,7 @@ int launch_kv_attention(const uint16_t* q, int64_t ldq, int head_dim, const KvAr
   g.causal = causal;
   g.split = split;
   const int64_t rows = (int64_t)a.group * (a.T < a.max_q_len ? a.T : a.max_q_len);     // of one request, at most
-  g.prompts = rows >= kPromptRows && (double)a.T * a.n_heads * ((double)a.max_blocks * kKvBlock + kRowKeys) >= (double)kPromptPairs;
+  g.prompts = rows >= kPromptRows && (double)a.T * a.n_heads * ((double)a.max_blocks * kKvBlock + kRowKeys) >= (double)kPromptPairs * (rows < kFullRows ? 3 : 1);
   if (g.prompts) {
     const int rc = launch_kv_prompt(q, ldq, head_dim, a, scale, causal, out, lse, split, st);
     if (rc != TLQ_OK) return rc;
