@@ -33,7 +33,7 @@ namespace {
 
 constexpr int kWarps = kSplitWarps;
 constexpr int kThreads = kWarps * 32;
-constexpr float kShift = 15.f;            // p is kept as 2^kShift * p in 16 bits
+constexpr float kShift = kFewShift;       // p is kept as 2^kShift * p in 16 bits
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttnArgs {
@@ -104,6 +104,8 @@ __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 
 // Units of a request: row tiles x kv heads x (blocks + kItemUnits); blocks is one for a request without cached tokens, whose
 // rows are empty.  What an item costs beside its blocks (its queries, its result) takes as long as kItemUnits blocks.
 constexpr int kItemUnits = 1;
+// Items of up to kWhole blocks are not cut: the warp that has the unit before their blocks takes them all.
+constexpr int kWhole = 4;
 struct Units {
   int row_tiles, blocks;
   long long total;
@@ -151,134 +153,9 @@ struct Walker {
   }
 };
 
-// An item of which a worker has only a part.
-struct Shared {
-  long long begin, end;        // units of its blocks; begin = end: nothing here
-  int b, h, tile;
-};
-
 // Row of the output that column c of an item belongs to.
 __device__ __forceinline__ int64_t out_row(const KvArgs& a, const Request& r, int h, int row) {
   return (int64_t)(r.q0 + row / a.group) * a.n_heads + h * a.group + row % a.group;
-}
-
-// Writes four channels of one column of a joined item: to the output, or with `to` into another partial.
-template <int D, int NT>
-__device__ __forceinline__ void leave(const KvArgs& a, const AttnArgs& g, const Shared& it, const Request& req, float* to, int e,
-                                      float mm, float den, const float4& sum) {
-  constexpr int kRows = 8 * NT;
-  const int c = e / (D / 4), d = (e % (D / 4)) * 4;
-  if (to != nullptr) {
-    reinterpret_cast<float4*>(to + 2 * kRows)[e] = sum;
-    if (d == 0) {
-      to[c] = mm;
-      to[kRows + c] = den;
-    }
-    return;
-  }
-  const int64_t at = out_row(a, req, it.h, it.tile * kRows + c);
-  const bool none = mm == -INFINITY && den == 0.f;         // a row that sees nothing (a NaN row has den = NaN)
-  const float inv = none ? 0.f : 1.0f / den;
-  const __nv_bfloat162 y0 = __floats2bfloat162_rn(none ? 0.f : sum.x * inv, none ? 0.f : sum.y * inv);
-  const __nv_bfloat162 y1 = __floats2bfloat162_rn(none ? 0.f : sum.z * inv, none ? 0.f : sum.w * inv);
-  *reinterpret_cast<uint2*>(g.out + at * D + d) =
-      make_uint2(*reinterpret_cast<const uint32_t*>(&y0), *reinterpret_cast<const uint32_t*>(&y1));
-  if (d == 0 && g.lse != nullptr) g.lse[at] = none ? -INFINITY : kLn2 * (log2f(den) + mm - kShift);
-}
-
-__device__ __forceinline__ void add_scaled(float4& sum, const float4& v, float f) {
-  sum.x = fmaf(v.x, f, sum.x); sum.y = fmaf(v.y, f, sum.y); sum.z = fmaf(v.z, f, sum.z); sum.w = fmaf(v.w, f, sum.w);
-}
-
-// Joins the partials of up to kWarps warps of this CTA (kRows maxima, kRows sums, kRows x D output sums each; first_part,
-// then `pitch` floats apart from second_part on).  `lanes` threads share the work; all loads of a column are under way at once.
-template <int D, int NT>
-__device__ __forceinline__ void join_warps(const KvArgs& a, const AttnArgs& g, const Shared& it, int count, const float* first_part,
-                                           const float* second_part, size_t pitch, float* to, int lane, int lanes) {
-  constexpr int kRows = 8 * NT;
-  const Request req = load_request(a, it.b);
-  const int n_rows = min(kRows, req.q_len * a.group - it.tile * kRows);
-  for (int e = lane; e < n_rows * (D / 4); e += lanes) {
-    const int c = e / (D / 4);
-    float m[kWarps], l[kWarps];
-    float4 v[kWarps];
-#pragma unroll
-    for (int i = 0; i < kWarps; ++i) {
-      const float* p = i == 0 ? first_part : second_part + (i - 1) * pitch;
-      const bool in = i < count;
-      m[i] = in ? __ldcg(p + c) : -INFINITY;
-      l[i] = in ? __ldcg(p + kRows + c) : 0.f;
-      v[i] = in ? __ldcg(reinterpret_cast<const float4*>(p + 2 * kRows) + e) : make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-    float mm = -INFINITY, den = 0.f;
-#pragma unroll
-    for (int i = 0; i < kWarps; ++i) mm = fmaxf(mm, m[i]);
-    const float mu = mm == -INFINITY ? 0.f : mm;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < kWarps; ++i) {
-      const float f = exp2_fast(m[i] - mu);
-      add_scaled(sum, v[i], f);
-      den = fmaf(l[i], f, den);
-    }
-    leave<D, NT>(a, g, it, req, to, e, mm, den, sum);
-  }
-}
-
-// Joins the partials of `count` CTAs (first_part, then `pitch` floats apart from second_part on) into the output.  All
-// threads of the CTA; `weights` holds kMaxWorkers x kRows floats of shared memory.
-template <int D, int NT>
-__device__ __forceinline__ void join_ctas(const KvArgs& a, const AttnArgs& g, const Shared& it, int count, const float* first_part,
-                                          const float* second_part, size_t pitch, float* weights) {
-  constexpr int kRows = 8 * NT;
-  const Request req = load_request(a, it.b);
-  const int n_rows = min(kRows, req.q_len * a.group - it.tile * kRows);
-  auto part = [&](int i) { return i == 0 ? first_part : second_part + (size_t)(i - 1) * pitch; };
-  constexpr int kBatch = 20;                               // parts whose loads are under way at once
-  __shared__ float s_max[kRows], s_den[kRows];
-  const int lane = threadIdx.x & 31;
-  for (int c = threadIdx.x >> 5; c < kRows; c += kWarps) {
-    float m[kMaxWorkers / 32], l[kMaxWorkers / 32], mm = -INFINITY, den = 0.f;
-#pragma unroll
-    for (int i = 0; i < kMaxWorkers / 32; ++i) {
-      const int k = i * 32 + lane;
-      m[i] = k < count ? __ldcg(part(k) + c) : -INFINITY;
-      l[i] = k < count ? __ldcg(part(k) + kRows + c) : 0.f;
-      mm = fmaxf(mm, m[i]);
-    }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xFFFFFFFFu, mm, d));
-    const float mu = mm == -INFINITY ? 0.f : mm;
-#pragma unroll
-    for (int i = 0; i < kMaxWorkers / 32; ++i) {
-      const int k = i * 32 + lane;
-      const float f = exp2_fast(m[i] - mu);
-      if (k < count) weights[k * kRows + c] = f;
-      den = fmaf(l[i], f, den);
-    }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) den += __shfl_xor_sync(0xFFFFFFFFu, den, d);
-    if (lane == 0) {
-      s_max[c] = mm;
-      s_den[c] = den;
-    }
-  }
-  __syncthreads();
-  for (int e = threadIdx.x; e < n_rows * (D / 4); e += kThreads) {
-    const int c = e / (D / 4);
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i0 = 0; i0 < count; i0 += kBatch) {
-      float4 v[kBatch];
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i)
-        v[i] = i0 + i < count ? __ldcg(reinterpret_cast<const float4*>(part(i0 + i) + 2 * kRows) + e)
-                              : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) add_scaled(sum, v[i], i0 + i < count ? weights[(i0 + i) * kRows + c] : 0.f);
-    }
-    leave<D, NT>(a, g, it, req, nullptr, e, s_max[c], s_den[c], sum);
-  }
-  __syncthreads();                                         // the next item's join may overwrite the weights
 }
 
 template <int D>
@@ -299,8 +176,7 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
   __shared__ __align__(8) uint64_t s_bars[kWarps * kRing];
   __shared__ long long sums[kWarps];
   __shared__ Found found;
-  __shared__ Shared s_first[kWarps], s_last[kWarps], s_cta[2];
-  __shared__ int s_join[2], s_abort, s_has[kWarps];         // s_has: 1 a first part, 2 a last part, 4 the first part does not end here
+  __shared__ int s_abort;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int gr = lane >> 2, tq = lane & 3;
 
@@ -310,9 +186,12 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
     for (int i = 0; i < kRing; ++i) ptx::mbar_init(ptx::smem_u32(&s_bars[warp * kRing + i]), 1);
     ptx::fence_barrier_init();
   }
-  if (threadIdx.x < 2) s_cta[threadIdx.x].begin = s_cta[threadIdx.x].end = 0;
-  if (lane == 0) s_has[warp] = 0;
   after_previous();
+  // the warp's parts: of an item that began before it, of an item that goes on after it
+  const size_t worker = (size_t)blockIdx.x * kWarps + warp;
+  PartNote* const notes = few_notes(g.split, D) + 2 * worker;
+  if (lane < 2) notes[lane].item = -1;
+  __syncwarp();
   const int max_rows = g.prompts && is_prompt_work<kThreads>(a, g.causal, sums) ? kPromptRows : 0x7FFFFFFF;
   auto count_units = [&](int b) { return units_of(a, load_request(a, b), kRows, max_rows).total; };
   // no more CTAs than give each warp of a CTA a block
@@ -324,7 +203,6 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
     return;
   const long long workers = workers_of(total);
   const long long u_begin = total * blockIdx.x / workers, u_end = total * (blockIdx.x + 1) / workers;
-  auto worker_of = [&](long long unit) { return ((unit + 1) * workers - 1) / total; };
 
   // ---------------------------------------------------------------- this warp's part of it
   // (with fewer units than warps the first ones get one each: warps with nothing to do are the last ones)
@@ -333,10 +211,6 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
   const long long w_begin = bound_of(warp), w_end = bound_of(warp + 1);
   const uint32_t ring = ptx::smem_u32(smem) + warp * (kRing * kBytes);
   const uint32_t bars = ptx::smem_u32(&s_bars[warp * kRing]);
-  float* const partials = g.split.partials;
-  auto warp_slot = [&](int w, int i) { return partials + (((size_t)blockIdx.x * kWarps + w) * 2 + i) * kPitch; };
-  auto cta_slot = [&](long long c, int i) { return partials + ((size_t)kMaxWorkers * kWarps * 2 + (size_t)c * 2 + i) * kPitch; };
-
   if (w_begin < w_end) {
     Walker con;                                            // what is computed now
     con.max_rows = max_rows;
@@ -350,8 +224,13 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
       }
       con.start(a, b, rest, kRows);
     }
+    long long unit = w_begin;
+    if (con.un.blocks <= kWhole && con.blk > -kItemUnits) {   // an item that the warp before this one takes
+      unit += con.un.blocks - con.blk;
+      con.next_item(a, kRows);
+    }
     Walker pro = con;                                      // what is copied next
-    long long pro_left = w_end - w_begin;
+    long long pro_left = w_end - unit;
     // steps and first places of the blocks under way
     float q_k[kDeep], q_v[kDeep];
     int q_base[kDeep];
@@ -363,10 +242,11 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
         if (pro.blk < 0) {
           pro_left += pro.blk;
           pro.blk = 0;
+          if (pro.un.blocks <= kWhole) pro_left = max(pro_left, (long long)pro.un.blocks);
         } else if (pro.req.kv > 0) {
           phys = __ldg(a.block_table + (int64_t)pro.b * a.max_blocks + pro.blk);
           return;
-        } else {
+        } else {                                           // one block that is none
           --pro_left;
           pro.next_item(a, kRows);
         }
@@ -416,16 +296,16 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
       if (++take == kRing) { take = 0; phase ^= 1u; }
     };
 
-    long long unit = w_begin;
-    while (true) {
+    while (unit < w_end && ok) {
+      const bool small = con.un.blocks <= kWhole;
       if (con.blk < 0) {
         unit -= con.blk;
         con.blk = 0;
+        if (unit >= w_end && !small) break;
       }
-      if (unit >= w_end || !ok) break;
       const int blk0 = con.blk;
       const long long left = w_end - unit;
-      const int blk1 = con.un.blocks - blk0 <= left ? con.un.blocks : blk0 + (int)left;
+      const int blk1 = small || con.un.blocks - blk0 <= left ? con.un.blocks : blk0 + (int)left;
       const Request req = con.req;
       const int n_rows = min(kRows, req.q_len * a.group - con.tile * kRows);
       const int past = req.kv - req.q_len, row0 = con.tile * kRows;
@@ -630,7 +510,7 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
             if (gr == 0 && g.lse != nullptr) g.lse[at] = none ? -INFINITY : kLn2 * (log2f(l[n][j]) + m[n][j] - kShift);
           }
       } else {
-        float* to = warp_slot(warp, blk0 == 0 ? 1 : 0);
+        float* to = few_partials(g.split) + (2 * worker + (blk0 == 0 ? 1 : 0)) * kPitch;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -647,11 +527,10 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
             }
           }
         if (lane == 0) {
-          Shared* d = blk0 == 0 ? &s_last[warp] : &s_first[warp];
-          d->begin = unit - blk0;
-          d->end = d->begin + con.un.blocks;
-          d->b = con.b; d->h = con.h; d->tile = con.tile;
-          s_has[warp] |= blk0 == 0 ? 2 : blk1 < con.un.blocks ? 5 : 1;
+          PartNote* d = notes + (blk0 == 0 ? 1 : 0);
+          d->item = unit - blk0;
+          d->first = blk0 == 0; d->last = blk1 == con.un.blocks;
+          d->h = con.h; d->tile = con.tile; d->q0 = req.q0; d->q_len = req.q_len;
         }
       }
       unit += blk1 - blk0;
@@ -662,70 +541,19 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
   }
   __syncthreads();
   if (*(volatile int*)&s_abort != 0) {                     // a copy that never came: give those under way time to land
+    if (lane < 2) notes[lane].item = -1;
     for (int i = 0; i < 1000; ++i) __nanosleep(1000);
-    return;
-  }
-
-  // ---------------------------------------------------------------- join the warps of this CTA
-  // An item that is cut starts with the last item of some warp, or began before the CTA (the first of warp 0), and goes on
-  // in the first items of the warps after it.
-  const int has = lane < kWarps ? s_has[lane] : 0;
-  const uint32_t firsts = __ballot_sync(0xFFFFFFFFu, has & 1), lasts = __ballot_sync(0xFFFFFFFFu, has & 2),
-                 thrus = __ballot_sync(0xFFFFFFFFu, has & 4);
-  // one chain: all threads; several: the warp that it begins in (what began before the CTA: warp 0)
-  const int n_chains = __popc(lasts) + (int)(firsts & 1u);
-  for (int i = 0; i < 2; ++i) {
-    const int w = n_chains > 1 ? warp : i == 0 ? 0 : __ffs(lasts) - 1;
-    if (i == 0 ? (w != 0 || !(firsts & 1u)) : (w < 0 || !(lasts >> w & 1u))) continue;
-    int parts = 1;
-    bool on = i != 0 || (thrus & 1u);
-    while (on && w + parts < kWarps && (firsts >> (w + parts) & 1u)) {
-      on = thrus >> (w + parts) & 1u;
-      ++parts;
-    }
-    const Shared it = i ? s_last[w] : s_first[w];
-    const bool inside = it.begin >= u_begin && it.end <= u_end;
-    float* to = inside ? nullptr : cta_slot(blockIdx.x, it.begin >= u_begin ? 1 : 0);
-    const int id = n_chains > 1 ? lane : (int)threadIdx.x;
-    join_warps<D, NT>(a, g, it, parts, warp_slot(w, i), warp_slot(w, 0) + 2 * kPitch, 2 * kPitch, to, id,
-                      n_chains > 1 ? 32 : kThreads);
-    if (!inside && id == 0) s_cta[it.begin >= u_begin ? 1 : 0] = it;
-  }
-  // ---------------------------------------------------------------- join the CTAs that share an item
-  __syncthreads();
-  if (s_cta[0].begin == s_cta[0].end && s_cta[1].begin == s_cta[1].end) return;
-  if (threadIdx.x < 2) {
-    const Shared it = s_cta[threadIdx.x];
-    s_join[threadIdx.x] = 0;
-    if (it.begin < it.end) {
-      const long long first = worker_of(it.begin), final = worker_of(it.end - 1);
-      __threadfence();                                     // the CTA's partials, which the barrier has ordered before this
-      s_join[threadIdx.x] = atomicAdd(g.split.counters + first, 1) == (int)(final - first);
-      if (s_join[threadIdx.x]) g.split.counters[first] = 0;
-      __threadfence();
-    }
-  }
-  __syncthreads();
-  for (int i = 0; i < 2; ++i) {
-    if (!s_join[i]) continue;
-    const Shared it = s_cta[i];
-    const long long first = worker_of(it.begin), final = worker_of(it.end - 1);
-    join_ctas<D, NT>(a, g, it, (int)(final - first) + 1, cta_slot(first, 1), cta_slot(first, 0) + 2 * kPitch, 2 * kPitch,
-                     reinterpret_cast<float*>(smem));
   }
 }
 
 template <int D, int NT>
-int launch(const KvArgs& a, const AttnArgs& g, cudaStream_t st) {
+int launch(const KvArgs& a, const AttnArgs& g, int ctas, cudaStream_t st) {
   static OncePerDevice once;
   const int rc = once_per_device(once, [] {
     return cudaFuncSetAttribute(kv_attention_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes<D>);
   });
   if (rc != TLQ_OK) return rc;
-  const int sms = device_sm_count();
-  if (sms <= 0) return TLQ_ERR_CUDA;
-  const int grid = sms < kMaxWorkers ? sms : kMaxWorkers;
-  return launch_next(kv_attention_kernel<D, NT>, dim3((unsigned)grid), kThreads, kRingBytes<D>, 1, st, a, g);
+  return launch_next(kv_attention_kernel<D, NT>, dim3((unsigned)ctas), kThreads, kRingBytes<D>, 1, st, a, g);
 }
 
 }  // namespace
@@ -737,15 +565,21 @@ int launch_kv_attention(const uint16_t* q, int64_t ldq, int head_dim, const KvAr
   g.scale_log2 = scale * kLog2e;
   g.causal = causal;
   g.split = split;
+  const int sms = device_sm_count();
+  if (sms <= 0) return TLQ_ERR_CUDA;
+  const int ctas = sms < kMaxWorkers ? sms : kMaxWorkers;
   const int64_t rows = (int64_t)a.group * (a.T < a.max_q_len ? a.T : a.max_q_len);     // of one request, at most
-  g.prompts = rows >= kPromptRows && (double)a.T * a.n_heads * ((double)a.max_blocks * kKvBlock + kRowKeys) >= (double)kPromptPairs * (rows < kFullRows ? 3 : 1);
-  if (g.prompts) {
-    const int rc = launch_kv_prompt(q, ldq, head_dim, a, scale, causal, out, lse, split, st);
-    if (rc != TLQ_OK) return rc;
-  }
+  const double most = (double)a.T * a.n_heads * ((double)a.max_blocks * kKvBlock + kRowKeys);
+  g.prompts = rows >= kPromptRows && most >= (double)kPromptPairs * (rows < kFullRows ? 3 : 1);
+  int rc = TLQ_OK;
+  if (g.prompts) rc = launch_kv_prompt(q, ldq, head_dim, a, scale, causal, out, lse, split, ctas, st);
+  if (rc != TLQ_OK) return rc;
   const bool narrow = rows <= 8;
-  if (head_dim == 128) return narrow ? launch<128, 1>(a, g, st) : launch<128, 2>(a, g, st);
-  return narrow ? launch<64, 1>(a, g, st) : launch<64, 2>(a, g, st);
+  if (head_dim == 128) rc = narrow ? launch<128, 1>(a, g, ctas, st) : launch<128, 2>(a, g, ctas, st);
+  else rc = narrow ? launch<64, 1>(a, g, ctas, st) : launch<64, 2>(a, g, ctas, st);
+  if (rc != TLQ_OK) return rc;
+  if (!g.prompts && a.max_blocks <= kWhole) return TLQ_OK;  // nothing was cut
+  return launch_kv_join(head_dim, a, ctas, narrow ? 8 : 16, g.prompts != 0, out, lse, split, st);
 }
 
 }  // namespace tlq

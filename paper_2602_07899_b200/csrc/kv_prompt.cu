@@ -35,7 +35,7 @@ constexpr int kSoftWarps = 8, kLoadWarps = 4, kIssueWarp = kSoftWarps + kLoadWar
 constexpr int kThreads = 512;                              // four groups of four warps
 // registers of a thread of each role: 2 x 176 + 72 + 88 = 4 x 128, what the block is launched with
 constexpr int kSoftRegs = 176, kLoadRegs = 72, kIssueRegs = 88;
-constexpr float kShift = 11.f, kGrow = 4.9f;
+constexpr float kShift = kPromptShift, kGrow = 4.9f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kStepFloor = 7.8886090522101181e-31f;      // 2^-100, as in kv_attention.cu
 constexpr float kUnit = 16777216.f;                        // 2^24
@@ -167,11 +167,6 @@ __device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[32]) {
                  "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
                  "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
 }
-__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[16]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
-                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
-}
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }   // one instruction here
 __device__ __forceinline__ float as_f(uint32_t x) { return __uint_as_float(x); }
 // floor(log2 x) of a finite x > 0 (-126 for the smallest), else 0; and 2^n for n in [-126, 127]
@@ -295,15 +290,10 @@ struct Walk {
   }
 };
 
-constexpr int kJoinRows = 32, kJoinThreads = 256;          // rows of a CTA that joins parts
 template <int D>
 constexpr size_t kPitch = (size_t)kItemRows * (D + 2);     // floats of a partial: maxima, sums, output sums
 template <int D>
-__device__ __forceinline__ float* partial_of(const KvSplit& split, int cta, int i) { return split.partials + ((size_t)cta * 2 + i) * kPitch<D>; }
-template <int D>
-__device__ __forceinline__ PartNote* notes_of(const KvSplit& split) {     // two of every CTA, behind the partials
-  return reinterpret_cast<PartNote*>(split.partials + (size_t)kMaxWorkers * 2 * kPitch<D>);
-}
+__device__ __forceinline__ float* partial_of(const KvSplit& split, int cta, int i) { return prompt_partials(split, D) + ((size_t)cta * 2 + i) * kPitch<D>; }
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -346,7 +336,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
   volatile int* abort_flag = &s_abort;
 
   after_previous();
-  auto no_parts = [&]() { notes_of<D>(g.split)[2 * blockIdx.x].n = notes_of<D>(g.split)[2 * blockIdx.x + 1].n = 0; };
+  auto no_parts = [&]() { prompt_notes(g.split, D)[2 * blockIdx.x].item = prompt_notes(g.split, D)[2 * blockIdx.x + 1].item = -1; };
   if (threadIdx.x == 0) no_parts();
   if (!is_prompt_work<kThreads>(a, g.causal, sums)) return;   // left to the few-row kernel
   // ---------------------------------------------------------------- this CTA's part of the line
@@ -481,9 +471,10 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
       if (!ok || s->k0 < 0) break;
       const int k0 = s->k0, k1 = s->k1;
       if (threadIdx.x == 0 && (k0 > 0 || k1 < s->n)) {
-        PartNote* note = notes_of<D>(g.split) + 2 * blockIdx.x + s->starts;
-        note->b = s->b; note->h = s->h; note->tile = s->tile; note->q0 = s->q0;
-        note->q_len = s->q_len; note->k0 = k0; note->k1 = k1; note->n = s->n;
+        PartNote* note = prompt_notes(g.split, D) + 2 * blockIdx.x + s->starts;
+        note->item = s->at;
+        note->first = k0 == 0; note->last = k1 == s->n;
+        note->h = s->h; note->tile = s->tile; note->q0 = s->q0; note->q_len = s->q_len;
       }
       if (!tile_live(s, t)) {
         step += k1 - k0;
@@ -850,119 +841,26 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
   if (*abort_flag != 0 && threadIdx.x == 0) no_parts();
 }
 
-// Joins the parts of the items that were cut.  CTA (w, y) takes rows 32 y .. 32 y + 31 of the items whose first blocks CTA w of
-// the kernel above had; their other parts are of the CTAs after it.  A kernel of its own, since a single CTA (the last one to
-// finish its part, say) reads parts at 65 GB/s and all of them together from the second-level cache.
 template <int D>
-__global__ void __launch_bounds__(kJoinThreads)
-kv_prompt_join_kernel(const KvArgs a, const PromptArgs g) {
-  __shared__ float s_f[kMaxWorkers][kJoinRows];            // of a part and row: maximum, then the factor of its sums
-  __shared__ float s_inv[kJoinRows];
-  __shared__ int s_parts[kMaxWorkers], s_n;
-  after_previous();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ctas = (int)gridDim.x, row0 = blockIdx.y * kJoinRows;
-  const PartNote* const notes = notes_of<D>(g.split);
-  for (int i = 0; i < 2; ++i) {
-    const PartNote mine = notes[2 * blockIdx.x + i];
-    if (mine.n == 0 || mine.k0 != 0) continue;
-    const long long rows = (long long)mine.q_len * a.group - (long long)mine.tile * kItemRows;
-    const int live = (int)min((long long)kJoinRows, rows - row0);
-    if (live <= 0) continue;
-    if (warp == 0) {                                       // the other parts, in order (a CTA whose part has no block left none)
-      int n = 1;
-      bool all = false;
-      if (lane == 0) s_parts[0] = 2 * blockIdx.x + i;
-      for (int w0 = blockIdx.x + 1; w0 < ctas && !all; w0 += 32) {
-        PartNote p{};
-        if (w0 + lane < ctas) p = notes[2 * (w0 + lane)];
-        const bool same = p.n != 0 && p.b == mine.b && p.h == mine.h && p.tile == mine.tile;
-        const uint32_t some = __ballot_sync(0xFFFFFFFFu, same);
-        if (same) s_parts[n + __popc(some & ((1u << lane) - 1u))] = 2 * (w0 + lane);
-        n += __popc(some);
-        all = __any_sync(0xFFFFFFFFu, (same && p.k1 == p.n) || (p.n != 0 && !same));
-      }
-      if (lane == 0) s_n = n;
-    }
-    __syncthreads();
-    const int n = s_n;
-    auto part = [&](int j) { return (const float*)(g.split.partials + (size_t)s_parts[j] * kPitch<D>); };
-    for (int j = warp; j < n; j += kJoinThreads / 32) s_f[j][lane] = __ldcg(part(j) + row0 + lane);
-    __syncthreads();
-    if (warp == 0) {
-      float m = -INFINITY, den = 0.f;
-      for (int j = 0; j < n; ++j) m = fmaxf(m, s_f[j][lane]);
-      const float mu = m == -INFINITY ? 0.f : m;
-#pragma unroll 4
-      for (int j = 0; j < n; ++j) {
-        const float f = exp2_fast(s_f[j][lane] - mu);
-        den = fmaf(f, __ldcg(part(j) + kItemRows + row0 + lane), den);
-        s_f[j][lane] = f;
-      }
-      const bool none = m == -INFINITY && den == 0.f;
-      s_inv[lane] = none ? 0.f : 1.0f / den;
-      const int row = mine.tile * kItemRows + row0 + lane;
-      if (lane < live && g.lse != nullptr)
-        g.lse[(int64_t)(mine.q0 + row / a.group) * a.n_heads + mine.h * a.group + row % a.group] =
-            none ? -INFINITY : kLn2 * (log2f(den) + m - kShift);
-    }
-    __syncthreads();
-    constexpr int kPieces = D / 4, kEach = kJoinRows * kPieces / kJoinThreads;   // four channels each
-    float4 sum[kEach];
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) sum[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int j = 0; j < n; ++j) {
-      const float4* from = reinterpret_cast<const float4*>(part(j) + 2 * kItemRows + (size_t)row0 * D);
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int at = e * kJoinThreads + (int)threadIdx.x;
-        const float4 v = __ldcg(from + at);
-        const float f = s_f[j][at / kPieces];
-        sum[e].x = fmaf(v.x, f, sum[e].x); sum[e].y = fmaf(v.y, f, sum[e].y);
-        sum[e].z = fmaf(v.z, f, sum[e].z); sum[e].w = fmaf(v.w, f, sum[e].w);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const int at = e * kJoinThreads + (int)threadIdx.x, r = at / kPieces, d = (at % kPieces) * 4;
-      if (r >= live) continue;
-      const int row = mine.tile * kItemRows + row0 + r;
-      const int64_t to = (int64_t)(mine.q0 + row / a.group) * a.n_heads + mine.h * a.group + row % a.group;
-      const float inv = s_inv[r];
-      const __nv_bfloat162 y0 = __floats2bfloat162_rn(inv == 0.f ? 0.f : sum[e].x * inv, inv == 0.f ? 0.f : sum[e].y * inv);
-      const __nv_bfloat162 y1 = __floats2bfloat162_rn(inv == 0.f ? 0.f : sum[e].z * inv, inv == 0.f ? 0.f : sum[e].w * inv);
-      *reinterpret_cast<uint2*>(g.out + to * D + d) =
-          make_uint2(*reinterpret_cast<const uint32_t*>(&y0), *reinterpret_cast<const uint32_t*>(&y1));
-    }
-    __syncthreads();                                       // before the second item's parts take the places of this one's
-  }
-}
-
-template <int D>
-int launch(const KvArgs& a, const PromptArgs& g, cudaStream_t st) {
+int launch(const KvArgs& a, const PromptArgs& g, int ctas, cudaStream_t st) {
   static OncePerDevice once;
   const int rc = once_per_device(once, [] {
     return cudaFuncSetAttribute(kv_prompt_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem<D>);
   });
   if (rc != TLQ_OK) return rc;
-  const int sms = device_sm_count();
-  if (sms <= 0) return TLQ_ERR_CUDA;
-  const unsigned ctas = (unsigned)(sms < kMaxWorkers ? sms : kMaxWorkers);
-  const int rp = launch_next(kv_prompt_kernel<D>, dim3(ctas), kThreads, kSmem<D>, 1, st, a, g);
-  if (rp != TLQ_OK) return rp;
-  return launch_next(kv_prompt_join_kernel<D>, dim3(ctas, kItemRows / kJoinRows), kJoinThreads, 0, 1, st, a, g);
+  return launch_next(kv_prompt_kernel<D>, dim3((unsigned)ctas), kThreads, kSmem<D>, 1, st, a, g);
 }
 
 }  // namespace
 
 int launch_kv_prompt(const uint16_t* q, int64_t ldq, int head_dim, const KvArgs& a, float scale, int causal, uint16_t* out,
-                     float* lse, const KvSplit& split, cudaStream_t st) {
+                     float* lse, const KvSplit& split, int ctas, cudaStream_t st) {
   PromptArgs g{};
   g.q = q; g.ldq = ldq; g.out = out; g.lse = lse;
   g.scale_log2 = scale * kLog2e;
   g.causal = causal;
   g.split = split;
-  return head_dim == 128 ? launch<128>(a, g, st) : launch<64>(a, g, st);
+  return head_dim == 128 ? launch<128>(a, g, ctas, st) : launch<64>(a, g, ctas, st);
 }
 
 }  // namespace tlq

@@ -196,26 +196,42 @@ int launch_kv_store(const uint16_t* qkv, int64_t ld, int head_dim, const KvArgs&
                     const uint16_t* q_norm, const uint16_t* k_norm, float eps, uint16_t* q_out, uint16_t* k_values,
                     uint16_t* v_values, cudaStream_t st);
 
-// kv_attention.cu: workspace of the split over the cache (counters are zero between calls)
+// kv_attention.cu, kv_prompt.cu, kv_join.cu: the split over the cache
 constexpr int kMaxWorkers = 160;          // CTAs that share one call's work (one per SM)
-constexpr int kSplitWarps = 8;            // warps of one of them
-constexpr int kMaxRowTile = 16;           // query rows of one work item
-constexpr int kPromptItemRows = 256;      // query rows of one item of the prompt kernel (kv_prompt.cu)
-struct __align__(16) PartNote {           // a part of a row tile's blocks, [k0, k1) of n; n == 0: none
-  int b, h, tile, q0;
-  int q_len, k0, k1, n;
+constexpr int kSplitWarps = 8;            // warps of one of them in the few-row kernel, each with a part of its own
+constexpr int kMaxRowTile = 16;           // query rows of one of its items (8 or 16)
+constexpr int kPromptItemRows = 256;      // query rows of one item of the prompt kernel
+constexpr int kPromptJoinRows = 32;       // rows of such an item that a CTA joins
+constexpr float kFewShift = 15.f, kPromptShift = 11.f;     // the sums hold 2^shift p
+struct __align__(16) PartNote {           // a part of an item's blocks
+  long long item;             // where the item is on the line of its kernel; negative: there is no part
+  int first, last;            // the part has the item's first, its last blocks
+  int h, tile, q0, q_len;     // kv head, row tile, first row of q and new tokens of the request
 };
-inline size_t kv_split_floats(int head_dim, int64_t rows) {   // two partials of every warp and of every CTA
-  const size_t few = (size_t)kMaxWorkers * 2 * (kSplitWarps + 1) * kMaxRowTile * ((size_t)head_dim + 2);
-  const size_t many = (size_t)kMaxWorkers * 2 * (kPromptItemRows * ((size_t)head_dim + 2) + sizeof(PartNote) / sizeof(float));
-  return rows >= kPromptRows && many > few ? many : few;
+// The workspace after its header: two partials of every worker (a maximum, a sum and D output sums of each row), their notes; of
+// the few-row kernel, then of the prompt kernel.  All of it is written in every call before it is read.
+__host__ __device__ constexpr size_t few_floats(int d) { return (size_t)kMaxWorkers * kSplitWarps * 2 * kMaxRowTile * ((size_t)d + 2); }
+__host__ __device__ constexpr size_t prompt_floats(int d) { return (size_t)kMaxWorkers * 2 * kPromptItemRows * ((size_t)d + 2); }
+constexpr size_t kNoteFloats = sizeof(PartNote) / sizeof(float);
+inline size_t kv_split_floats(int head_dim, int64_t rows) {
+  const size_t few = few_floats(head_dim) + kMaxWorkers * kSplitWarps * 2 * kNoteFloats;
+  return rows < kPromptRows ? few : few + prompt_floats(head_dim) + kMaxWorkers * 2 * kNoteFloats;
 }
 struct KvSplit {
-  int32_t* counters;          // [kMaxWorkers]
-  float* partials;            // kv_split_floats()
+  float* base;                // kv_split_floats()
 };
+__device__ __forceinline__ float* few_partials(const KvSplit& s) { return s.base; }
+__device__ __forceinline__ PartNote* few_notes(const KvSplit& s, int d) { return reinterpret_cast<PartNote*>(s.base + few_floats(d)); }
+__device__ __forceinline__ float* prompt_partials(const KvSplit& s, int d) {
+  return s.base + few_floats(d) + kMaxWorkers * kSplitWarps * 2 * kNoteFloats;
+}
+__device__ __forceinline__ PartNote* prompt_notes(const KvSplit& s, int d) {
+  return reinterpret_cast<PartNote*>(prompt_partials(s, d) + prompt_floats(d));
+}
 int launch_kv_prompt(const uint16_t* q, int64_t ldq, int head_dim, const KvArgs& a, float scale, int causal, uint16_t* out,
-                     float* lse, const KvSplit& split, cudaStream_t st);
+                     float* lse, const KvSplit& split, int ctas, cudaStream_t st);
+int launch_kv_join(int head_dim, const KvArgs& a, int ctas, int few_rows, bool prompts, uint16_t* out, float* lse,
+                   const KvSplit& split, cudaStream_t st);
 int launch_kv_attention(const uint16_t* q, int64_t ldq, int head_dim, const KvArgs& a, float scale, int causal,
                         uint16_t* out, float* lse, const KvSplit& split, cudaStream_t st);
 

@@ -7,7 +7,6 @@ namespace tlq {
 namespace {
 
 constexpr size_t kHeaderBytes = sizeof(WorkspaceHeader);
-constexpr size_t kCounterBytes = kMaxWorkers * sizeof(int32_t);
 
 int check_cache(const tlq_kv_cache* c) {
   if (c == nullptr || c->struct_size != sizeof(tlq_kv_cache)) return TLQ_ERR_INVALID_ARG;
@@ -77,7 +76,7 @@ int tlq_linear_i8(const int8_t* Xq, const float* t, int64_t N, int64_t C1, const
 
 size_t tlq_kv_workspace_bytes(const tlq_kv_cache* cache, const tlq_kv_batch* batch, int32_t n_heads, int64_t T) {
   if (check_cache(cache) != TLQ_OK || check_batch(batch) != TLQ_OK || check_heads(n_heads, cache) != TLQ_OK || T < 0) return 0;
-  return align_up(kHeaderBytes + kCounterBytes + kv_split_floats(cache->head_dim, query_rows(cache, batch, n_heads, T)) * sizeof(float), 256);
+  return align_up(kHeaderBytes + kv_split_floats(cache->head_dim, query_rows(cache, batch, n_heads, T)) * sizeof(float), 256);
 }
 
 int tlq_kv_store(const void* qkv, int64_t T, int64_t ld, int32_t n_heads, const tlq_kv_cache* cache,
@@ -144,8 +143,7 @@ int tlq_kv_attention(const void* q, int64_t T, int64_t ldq, int32_t n_heads, con
   if (rc != TLQ_OK || T == 0) return rc;
   uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
   KvSplit split;
-  split.counters = reinterpret_cast<int32_t*>(ws + kHeaderBytes);
-  split.partials = reinterpret_cast<float*>(ws + kHeaderBytes + kCounterBytes);
+  split.base = reinterpret_cast<float*>(ws + kHeaderBytes);
   return launch_kv_attention(reinterpret_cast<const uint16_t*>(q), ldq, cache->head_dim,
                              make_args(cache, batch, n_heads, T, workspace), scale, causal,
                              reinterpret_cast<uint16_t*>(out), lse, split, reinterpret_cast<cudaStream_t>(stream));
