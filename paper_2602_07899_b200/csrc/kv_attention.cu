@@ -104,8 +104,13 @@ __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 
 // Units of a request: row tiles x kv heads x (blocks + kItemUnits); blocks is one for a request without cached tokens, whose
 // rows are empty.  What an item costs beside its blocks (its queries, its result) takes as long as kItemUnits blocks.
 constexpr int kItemUnits = 1;
-// Items of up to kWhole blocks are not cut: the warp that has the unit before their blocks takes them all.
-constexpr int kWhole = 4;
+// Small items are not cut: the warp that has the unit before their blocks takes them all, and nothing has to be joined.  A
+// single request of 500 tokens (8 blocks) is answered in 12 us cut and in 17 whole; 64 of them, which keep all warps busy
+// either way, in 27 cut and in 24 whole, 64 of 300 tokens in 22 and 14.
+constexpr int kWhole = 4, kWholeBusy = 8;                  // blocks, at most; where there is a unit for every warp
+// The units go to as many CTAs as there are, then to warps that get about this many: every part has to be joined.  One token
+// over 60000 with 2 kv heads 40, 34 and 29 us for 1, 2 and 3, 64 requests of 100 tokens 9.6, 9.6 and 14.8.
+constexpr int kMinUnits = 2;
 struct Units {
   int row_tiles, blocks;
   long long total;
@@ -187,15 +192,10 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
     ptx::fence_barrier_init();
   }
   after_previous();
-  // the warp's parts: of an item that began before it, of an item that goes on after it
-  const size_t worker = (size_t)blockIdx.x * kWarps + warp;
-  PartNote* const notes = few_notes(g.split, D) + 2 * worker;
-  if (lane < 2) notes[lane].item = -1;
-  __syncwarp();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *few_workers(g.split, D) = 0;
   const int max_rows = g.prompts && is_prompt_work<kThreads>(a, g.causal, sums) ? kPromptRows : 0x7FFFFFFF;
   auto count_units = [&](int b) { return units_of(a, load_request(a, b), kRows, max_rows).total; };
-  // no more CTAs than give each warp of a CTA a block
-  auto workers_of = [&](long long all) { return min((all + kWarps - 1) / kWarps, (long long)gridDim.x); };
+  auto workers_of = [&](long long all) { return min(all, (long long)gridDim.x); };
   long long total = 0;
   if (!plan_items<kThreads>(a.B, count_units,
                             [&](long long all) { return (long long)blockIdx.x < workers_of(all) ? all * blockIdx.x / workers_of(all) : -1LL; },
@@ -205,12 +205,19 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
   const long long u_begin = total * blockIdx.x / workers, u_end = total * (blockIdx.x + 1) / workers;
 
   // ---------------------------------------------------------------- this warp's part of it
-  // (with fewer units than warps the first ones get one each: warps with nothing to do are the last ones)
-  const long long n_units = u_end - u_begin;
-  auto bound_of = [&](int w) { return u_begin + (n_units < kWarps ? min((long long)w, n_units) : n_units * w / kWarps); };
+  const int active = (int)min((total + workers * kMinUnits - 1) / (workers * kMinUnits), (long long)kWarps);   // warps of every CTA
+  const int whole = total >= workers * kWarps ? kWholeBusy : kWhole;
+  auto bound_of = [&](int w) { return w >= active ? u_end : u_begin + (u_end - u_begin) * w / active; };
   const long long w_begin = bound_of(warp), w_end = bound_of(warp + 1);
   const uint32_t ring = ptx::smem_u32(smem) + warp * (kRing * kBytes);
   const uint32_t bars = ptx::smem_u32(&s_bars[warp * kRing]);
+  // the warp's parts: of an item that began before it, of an item that goes on after it
+  const size_t worker = (size_t)blockIdx.x * active + warp;
+  PartNote* const notes = few_notes(g.split, D) + 2 * worker;
+  if (warp < active && lane < 2) notes[lane].item = -1;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *few_workers(g.split, D) = (int)workers * active;
+  __syncwarp();
+
   if (w_begin < w_end) {
     Walker con;                                            // what is computed now
     con.max_rows = max_rows;
@@ -225,7 +232,7 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
       con.start(a, b, rest, kRows);
     }
     long long unit = w_begin;
-    if (con.un.blocks <= kWhole && con.blk > -kItemUnits) {   // an item that the warp before this one takes
+    if (con.un.blocks <= whole && con.blk > -kItemUnits) {   // an item that the warp before this one takes
       unit += con.un.blocks - con.blk;
       con.next_item(a, kRows);
     }
@@ -242,7 +249,7 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
         if (pro.blk < 0) {
           pro_left += pro.blk;
           pro.blk = 0;
-          if (pro.un.blocks <= kWhole) pro_left = max(pro_left, (long long)pro.un.blocks);
+          if (pro.un.blocks <= whole) pro_left = max(pro_left, (long long)pro.un.blocks);
         } else if (pro.req.kv > 0) {
           phys = __ldg(a.block_table + (int64_t)pro.b * a.max_blocks + pro.blk);
           return;
@@ -297,7 +304,7 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
     };
 
     while (unit < w_end && ok) {
-      const bool small = con.un.blocks <= kWhole;
+      const bool small = con.un.blocks <= whole;
       if (con.blk < 0) {
         unit -= con.blk;
         con.blk = 0;
@@ -541,7 +548,7 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
   }
   __syncthreads();
   if (*(volatile int*)&s_abort != 0) {                     // a copy that never came: give those under way time to land
-    if (lane < 2) notes[lane].item = -1;
+    if (warp < active && lane < 2) notes[lane].item = -1;
     for (int i = 0; i < 1000; ++i) __nanosleep(1000);
   }
 }

@@ -58,18 +58,21 @@ struct TileShared {                       // of kPromptJoinRows rows of a prompt
   int counts[kThreads / 32];
 };
 
-// Rows row0 .. row1 - 1, one after another, of the items whose first blocks the warps of CTA blockIdx.x had.  Every group of D / 4 threads takes every kGroups-th
-// part; notes, maxima, sums and outputs of kAtOnce parts of a group are asked for together, whether or not they will turn out to be
+// Rows row0 .. row1 - 1, one after another, of the items whose first blocks workers 8 blockIdx.x .. 8 blockIdx.x + 7
+// had.  Every group of D / 4 threads takes every kGroups-th part; notes, maxima, sums and outputs of kAtOnce parts of a group are asked for together, whether or not they will turn out to be
 // the item's: one trip to memory for an item of up to kGroups * kAtOnce parts.
 template <int D, int kItem>
 __device__ __forceinline__ void join_rows(const KvArgs& a, const JoinArgs& g, const float* partials, const PartNote* notes, int row0,
-                                          int row1, float shift, RowShared& s) {
+                                          int row1, int workers, float shift, RowShared& s) {
   constexpr size_t kPitch = (size_t)kItem * (D + 2);
   constexpr int kWide = D / 4, kGroups = kThreads / kWide, kAtOnce = 4;
-  const int t = threadIdx.x, group = t / kWide, piece = t % kWide, workers = (int)gridDim.x * kSplitWarps;
+  const int t = threadIdx.x, group = t / kWide, piece = t % kWide;
   PartNote mine;
   mine.item = -1;
-  if (t < 2 * kSplitWarps) s.notes[t] = mine = load_note(notes + (size_t)blockIdx.x * 2 * kSplitWarps + t);
+  if (t < 2 * kSplitWarps) {
+    if ((int)blockIdx.x * kSplitWarps + t / 2 < workers) mine = load_note(notes + (size_t)blockIdx.x * 2 * kSplitWarps + t);
+    s.notes[t] = mine;
+  }
   if (!__syncthreads_or(mine.item >= 0 && mine.first)) return;
   for (int i = 0; i < 2 * kSplitWarps * (row1 - row0); ++i) {
     const int at = i % (2 * kSplitWarps), r = row0 + i / (2 * kSplitWarps);
@@ -250,7 +253,8 @@ kv_join_kernel(const KvArgs a, const JoinArgs g) {
   constexpr int kRowsEach = kPrompts ? 4 : 1;
   const int y = (int)blockIdx.y - (kPrompts ? kPromptItemRows / kPromptJoinRows : 0);
   if (y >= 0)
-    join_rows<D, kFewRows>(a, g, few_partials(g.split), few_notes(g.split, D), y * kRowsEach, (y + 1) * kRowsEach, kFewShift, s.row);
+    join_rows<D, kFewRows>(a, g, few_partials(g.split), few_notes(g.split, D), y * kRowsEach, (y + 1) * kRowsEach,
+                           __ldcg(few_workers(g.split, D)), kFewShift, s.row);
   else if constexpr (kPrompts)
     join_tile<D>(a, g, prompt_partials(g.split, D), prompt_notes(g.split, D), (int)blockIdx.y * kPromptJoinRows, kPromptShift, s.tile);
 }

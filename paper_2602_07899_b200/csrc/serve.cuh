@@ -213,8 +213,9 @@ struct __align__(16) PartNote {           // a part of an item's blocks
 __host__ __device__ constexpr size_t few_floats(int d) { return (size_t)kMaxWorkers * kSplitWarps * 2 * kMaxRowTile * ((size_t)d + 2); }
 __host__ __device__ constexpr size_t prompt_floats(int d) { return (size_t)kMaxWorkers * 2 * kPromptItemRows * ((size_t)d + 2); }
 constexpr size_t kNoteFloats = sizeof(PartNote) / sizeof(float);
+constexpr size_t kFewNoteFloats = (kMaxWorkers * kSplitWarps * 2 + 1) * kNoteFloats;   // and the number of workers behind them
 inline size_t kv_split_floats(int head_dim, int64_t rows) {
-  const size_t few = few_floats(head_dim) + kMaxWorkers * kSplitWarps * 2 * kNoteFloats;
+  const size_t few = few_floats(head_dim) + kFewNoteFloats;
   return rows < kPromptRows ? few : few + prompt_floats(head_dim) + kMaxWorkers * 2 * kNoteFloats;
 }
 struct KvSplit {
@@ -222,9 +223,10 @@ struct KvSplit {
 };
 __device__ __forceinline__ float* few_partials(const KvSplit& s) { return s.base; }
 __device__ __forceinline__ PartNote* few_notes(const KvSplit& s, int d) { return reinterpret_cast<PartNote*>(s.base + few_floats(d)); }
-__device__ __forceinline__ float* prompt_partials(const KvSplit& s, int d) {
-  return s.base + few_floats(d) + kMaxWorkers * kSplitWarps * 2 * kNoteFloats;
+__device__ __forceinline__ int* few_workers(const KvSplit& s, int d) {
+  return reinterpret_cast<int*>(few_notes(s, d) + kMaxWorkers * kSplitWarps * 2);
 }
+__device__ __forceinline__ float* prompt_partials(const KvSplit& s, int d) { return s.base + few_floats(d) + kFewNoteFloats; }
 __device__ __forceinline__ PartNote* prompt_notes(const KvSplit& s, int d) {
   return reinterpret_cast<PartNote*>(prompt_partials(s, d) + prompt_floats(d));
 }
