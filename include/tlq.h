@@ -258,7 +258,7 @@ int tlq_apply_layer(const void* X, int64_t N, int64_t C1, const void* W, int64_t
  * Serving a calibrated layer (symmetric mode).  What runs the layer that the calls above have calibrated, from the codes
  * that they returned: the 8-bit product, the write of keys and values into an 8-bit cache, and attention over it.  The
  * calls were added without a change to any earlier one.
- *  - Workspaces of these calls are ZEROED ONCE by their owner and then kept: the calls leave their counters at zero.  One
+ *  - Workspaces of these calls are ZEROED ONCE by their owner and then kept: what a call needs of them it writes itself.  One
  *    workspace serves any number of calls on one stream; streams that run at the same time need one each.  The status
  *    word (byte 0, tlq_read_status) is not reset by these calls: it keeps the last error until its owner zeroes the
  *    workspace again.

@@ -1,14 +1,17 @@
 // Joins the parts of attention items that several workers share (kv_attention.cu: warps, kv_prompt.cu: CTAs).
 //
 // A worker walks its part of a line of items and leaves, of an item that is not all its own, the maximum m, the sum l and the
-// output sums o of every row, and a note that says which blocks they cover; an item's parts are those of consecutive workers.
+// output sums o of every row, and a note that says of which item they are; an item's parts are those of consecutive workers.
 // With M = max m_i the row is sum o_i 2^(m_i - M) / sum l_i 2^(m_i - M), in the order of the workers whatever finished first.
 //
-// A kernel of its own, since what is run once costs its fetch: the last arriver of each item joining it inside the kernels
-// above took 15 to 20 us between the last block and the end (two levels, warps and CTAs, of cold code after a loop, and one
-// CTA reading up to 148 parts), this takes 5, most of it the latency of four dependent reads.  Grid: x names the
-// workers whose notes a CTA looks at, y the rows of their items (one row, or 16 of a prompt), so that a single item cut into
-// 148 parts is still read by many SMs.
+// A kernel of its own.  When the last arriver of an item joined it inside the kernels above, 15 to 20 us went by between the
+// last block and the end: two levels (warps, CTAs) of dependent reads, in code that runs once and costs its fetch, while other
+// SMs keep the memory's queues full, and one SM reading all parts of an item.  Bound: latency, three dependent reads for up to
+// 32 parts (1 us each), one more for every 32.  Measured: 32 requests x 2048 keys 31 -> 28 us in all, 9 tokens x 4096 keys
+// 26 -> 20, prompts of 64 tokens over 16384 180 -> 62.
+//
+// Grid: x names the workers whose notes a CTA looks at, y the rows of their items (one row, or 32 of a prompt), so that a single
+// item cut into many parts is still read by many SMs.
 #include "serve.cuh"
 
 namespace tlq {
@@ -58,9 +61,9 @@ struct TileShared {                       // of kPromptJoinRows rows of a prompt
   int counts[kThreads / 32];
 };
 
-// Rows row0 .. row1 - 1, one after another, of the items whose first blocks workers 8 blockIdx.x .. 8 blockIdx.x + 7
-// had.  Every group of D / 4 threads takes every kGroups-th part; notes, maxima, sums and outputs of kAtOnce parts of a group are asked for together, whether or not they will turn out to be
-// the item's: one trip to memory for an item of up to kGroups * kAtOnce parts.
+// Rows row0 .. row1 - 1, one after another, of the items whose first blocks workers 8 blockIdx.x .. 8 blockIdx.x + 7 had.  Every
+// group of D / 4 threads takes every kGroups-th part; notes, maxima, sums and outputs of kAtOnce parts of a group are asked for
+// together, whether or not they will turn out to be the item's: one trip to memory for an item of up to kGroups * kAtOnce parts.
 template <int D, int kItem>
 __device__ __forceinline__ void join_rows(const KvArgs& a, const JoinArgs& g, const float* partials, const PartNote* notes, int row0,
                                           int row1, int workers, float shift, RowShared& s) {
@@ -243,8 +246,8 @@ __device__ __forceinline__ void join_tile(const KvArgs& a, const JoinArgs& g, co
   }
 }
 
-// y: the rows of the few-row kernel's items, kRowsEach to a CTA, then groups of rows of the prompt kernel's.  Where that has run too
-// there are enough CTAs without one for each row, and little for them to do.
+// y: groups of rows of the prompt kernel's items, then the rows of the few-row kernel's, kRowsEach to a CTA: where the prompt
+// kernel has run too there are enough CTAs without one for each row, and little for them to do.
 template <int D, int kFewRows, bool kPrompts>
 __global__ void __launch_bounds__(kThreads)
 kv_join_kernel(const KvArgs a, const JoinArgs g) {

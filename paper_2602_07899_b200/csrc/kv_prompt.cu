@@ -10,18 +10,22 @@
 // and S of the block after it.  The output sum is rescaled only when the maximum of a row has grown by more than 4 (a factor
 // of 16 in p): p is kept as 2^11 p, so that it fits 16 bits either way.
 //   warps 0..3, 4..7  softmax of tile 0, 1: a thread is a row (and its accumulator lane)
-//   warps 8..11       bring the codes of keys and values from the cache into registers, turn them into f16 and lay them
-//                     out for the tensor core (128-byte swizzle); four stages each
+//   warps 8..11       copy the codes of keys and values to shared memory two blocks ahead, turn them into f16 and lay them out
+//                     for the tensor core (128-byte swizzle); four stages
 //   warps 12, 15      issue the products of tile 0, 1 (one warp for both spends its time waiting: 2500 cycles a block)
 //   warp 13           finds the parts of items that this CTA works on and passes them on through a ring
 //   warp 14           looks up the cache blocks to come and their steps and passes them on through another ring
-// Nothing in the loops may spill: with 200 KB of shared memory in use the first-level cache is too small
-// for local memory, and one reload per step costs as much as a product.
-// Work is cut as in the few-row kernel: items (row tiles of a kv head) lie on one line, weighted by their cached tokens,
-// every CTA takes an equal part of it; an item that is cut leaves partial sums, and the CTA that completes it joins them.
+// Nothing in the loops may spill: with 225 KB of shared memory in use the first-level cache is too small for local memory, and
+// one reload per step costs as much as a product.  A tile without rows is passed over.
+// Work is cut as in the few-row kernel: items (row tiles of a kv head) lie on one line, weighted by their cached tokens, every
+// CTA takes an equal part of it; an item that is cut leaves partial sums, which kv_join.cu joins.
 //
-// Bound: the tensor core (4 D flops per visible pair) and, next to it, the exponential unit: 256 x 128 exponentials at 16
-// per cycle take as long as the products of the same tile.
+// Bound: 4 D flops per visible pair on the tensor core.  Measured: 8192 tokens, 28 heads over 4 kv heads 553 to 558 us, 870 TFLOP/s
+// (292 us at the 1646 TFLOP/s of a large bf16 product); the tensor pipe is active 37 % of the time, the exponential unit 39 %.  A
+// block takes about 2200 cycles for 256 rows.  Neither unit bounds it alone: without exponentials 569, without products 488,
+// without fetching codes 521, without all three 298; what remains is the exchange between the roles, and 8 blocks' worth of time
+// around every item.  Tried and slower: taking the exponentials from the maximum of the blocks before while this block's is found
+// (581), the next block's scores loaded before P is handed over (588), two pieces of O rescaled at once (563).
 #include <type_traits>
 
 #include "serve.cuh"
@@ -39,8 +43,8 @@ constexpr float kShift = kPromptShift, kGrow = 4.9f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kStepFloor = 7.8886090522101181e-31f;      // 2^-100, as in kv_attention.cu
 constexpr float kUnit = 16777216.f;                        // 2^24
-constexpr int kMinTiles = 6;                               // blocks of a CTA's part, at least
-constexpr int kItemCost = 8;                               // what an item costs beside its blocks, in blocks
+constexpr int kMinTiles = 6;                               // blocks of a CTA's part, at least (512 tokens x 512: 34 us, 37 with 12)
+constexpr int kItemCost = 8;                               // what an item costs beside its blocks, in blocks (8192 tokens: 555, 564 with 12)
 
 struct PromptArgs {
   const uint16_t* q;

@@ -8,13 +8,15 @@
 // request keeps the larger of its old step and the new tokens' one; when it grows, the older codes follow it,
 // c <- rint(c * old / new).
 //
-// All statistics and products are in 32 bits; the quantizer's division is the IEEE one, so that codes of values (which
-// see no norm) are those of the definition.
+// All statistics and products are in 32 bits; codes are those of the IEEE division (by a reciprocal, and by the
+// division itself where the quotient comes near a tie), so that codes of values, which see no norm, are the definition's.
 //
 // Bound: bytes.  The rows are read once and everything is kept in registers between the maximum and the codes.  One CTA
 // owns a cache block of one head (its tokens lie in one request), because its step needs all of them; the remaining CTAs
-// stream query rows, four per thread group at once.  Values lie channel by token in the cache (what a matrix instruction over tokens
-// reads), so a CTA turns its 64 x D bytes in shared memory and writes rows of 64 bytes.
+// stream query rows, four per thread group at once.  Values lie channel by token in the cache (what a matrix instruction over
+// tokens reads), so a CTA turns its 64 x D bytes in shared memory and writes rows of 64 bytes.  Measured: 16384 tokens, 64 + 8 + 8
+// heads of 128 channels with norms (713 MB) 151 us, 4.7 TB/s, the schedulers busy 60 % of the time with conversions and rotations;
+// 6 ragged prompts (29 MB) 12.4 us; 32 requests of one token 5.4 us, latency.
 #include "serve.cuh"
 
 namespace tlq {
