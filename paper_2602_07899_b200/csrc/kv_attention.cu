@@ -45,6 +45,7 @@ struct AttnArgs {
   float* lse;
   float scale_log2;          // scale * log2(e)
   int causal, prompts;       // prompts: the prompt kernel has run before (and may have had something to do)
+  int whole;                 // items of up to this many blocks are not cut
   KvSplit split;
 };
 
@@ -106,10 +107,11 @@ __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 
 // Units of a request: row tiles x kv heads x (blocks + kItemUnits); blocks is one for a request without cached tokens, whose
 // rows are empty.  What an item costs beside its blocks (its queries, its result) takes as long as kItemUnits blocks.
 constexpr int kItemUnits = 1;
-// Small items are not cut: the warp that has the unit before their blocks takes them all, and nothing has to be joined.  A
-// single request of 500 tokens (8 blocks) is answered in 12 us cut and in 17 whole; 64 of them, which keep all warps busy
-// either way, in 27 cut and in 24 whole, 64 of 300 tokens in 22 and 14.
-constexpr int kWhole = 4, kWholeBusy = 8;                  // blocks, at most; where there is a unit for every warp
+// Small items are not cut: the warp that has the unit before their blocks takes them all, and nothing has to be joined (nor the
+// join launched, where no request can have more blocks: that alone is 5 us).  A single request of 500 tokens (8 blocks) is
+// answered in 12 us cut and in 17 whole; 64 of them, an item or more for every CTA, in 27 cut and in 24 whole, 64 of 300 tokens
+// in 22 and 14.
+constexpr int kWhole = 4, kWholeBusy = 8;                  // blocks, at most; where there may be an item for every CTA
 // The units go to as many CTAs as there are, then to warps that get about this many: every part has to be joined.  One token
 // over 60000 with 2 kv heads 40, 34 and 29 us for 1, 2 and 3, 64 requests of 100 tokens 9.6, 9.6 and 14.8.
 constexpr int kMinUnits = 2;
@@ -208,7 +210,6 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
 
   // ---------------------------------------------------------------- this warp's part of it
   const int active = (int)min((total + workers * kMinUnits - 1) / (workers * kMinUnits), (long long)kWarps);   // warps of every CTA
-  const int whole = total >= workers * kWarps ? kWholeBusy : kWhole;
   auto bound_of = [&](int w) { return w >= active ? u_end : u_begin + (u_end - u_begin) * w / active; };
   const long long w_begin = bound_of(warp), w_end = bound_of(warp + 1);
   const uint32_t ring = ptx::smem_u32(smem) + warp * (kRing * kBytes);
@@ -234,7 +235,7 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
       con.start(a, b, rest, kRows);
     }
     long long unit = w_begin;
-    if (con.un.blocks <= whole && con.blk > -kItemUnits) {   // an item that the warp before this one takes
+    if (con.un.blocks <= g.whole && con.blk > -kItemUnits) {   // an item that the warp before this one takes
       unit += con.un.blocks - con.blk;
       con.next_item(a, kRows);
     }
@@ -251,7 +252,7 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
         if (pro.blk < 0) {
           pro_left += pro.blk;
           pro.blk = 0;
-          if (pro.un.blocks <= whole) pro_left = max(pro_left, (long long)pro.un.blocks);
+          if (pro.un.blocks <= g.whole) pro_left = max(pro_left, (long long)pro.un.blocks);
         } else if (pro.req.kv > 0) {
           phys = __ldg(a.block_table + (int64_t)pro.b * a.max_blocks + pro.blk);
           return;
@@ -306,7 +307,7 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
     };
 
     while (unit < w_end && ok) {
-      const bool small = con.un.blocks <= whole;
+      const bool small = con.un.blocks <= g.whole;
       if (con.blk < 0) {
         unit -= con.blk;
         con.blk = 0;
@@ -580,6 +581,8 @@ int launch_kv_attention(const uint16_t* q, int64_t ldq, int head_dim, const KvAr
   const int64_t rows = (int64_t)a.group * (a.T < a.max_q_len ? a.T : a.max_q_len);     // of one request, at most
   const double most = (double)a.T * a.n_heads * ((double)a.max_blocks * kKvBlock + kRowKeys);
   g.prompts = rows >= kPromptRows && most >= (double)kPromptPairs * (rows < kFullRows ? 3 : 1);
+  const int64_t tiles = a.T * a.group / kMaxRowTile;       // row tiles of all requests, about
+  g.whole = (tiles > a.B ? tiles : a.B) * a.n_kv >= ctas ? kWholeBusy : kWhole;
   int rc = TLQ_OK;
   if (g.prompts) rc = launch_kv_prompt(q, ldq, head_dim, a, scale, causal, out, lse, split, ctas, st);
   if (rc != TLQ_OK) return rc;
@@ -587,7 +590,7 @@ int launch_kv_attention(const uint16_t* q, int64_t ldq, int head_dim, const KvAr
   if (head_dim == 128) rc = narrow ? launch<128, 1>(a, g, ctas, st) : launch<128, 2>(a, g, ctas, st);
   else rc = narrow ? launch<64, 1>(a, g, ctas, st) : launch<64, 2>(a, g, ctas, st);
   if (rc != TLQ_OK) return rc;
-  if (!g.prompts && a.max_blocks <= kWhole) return TLQ_OK;  // nothing was cut
+  if (!g.prompts && a.max_blocks <= g.whole) return TLQ_OK;  // nothing was cut
   return launch_kv_join(head_dim, a, ctas, narrow ? 8 : 16, g.prompts != 0, out, lse, split, st);
 }
 
