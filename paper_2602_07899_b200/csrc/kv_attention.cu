@@ -113,8 +113,9 @@ constexpr int kItemUnits = 1;
 // in 22 and 14.
 constexpr int kWhole = 4, kWholeBusy = 8;                  // blocks, at most; where there may be an item for every CTA
 // The units go to as many CTAs as there are, then to warps that get about this many: every part has to be joined.  One token
-// over 60000 with 2 kv heads 40, 34 and 29 us for 1, 2 and 3, 64 requests of 100 tokens 9.6, 9.6 and 14.8.
-constexpr int kMinUnits = 2;
+// over 60000 with 2 kv heads 37, 31 and 29 us for 2, 3 and 4, over 16384 with 8 25, 22 and 22; 9 tokens over 4096 with 4 kv heads
+// 20, 21 and 23, 16 requests of 700 tokens 16, 19 and 18.
+constexpr int kMinUnits = 3;
 struct Units {
   int row_tiles, blocks;
   long long total;
