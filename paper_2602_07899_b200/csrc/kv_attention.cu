@@ -255,7 +255,7 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
           pro.blk = 0;
           if (pro.un.blocks <= g.whole) pro_left = max(pro_left, (long long)pro.un.blocks);
         } else if (pro.req.kv > 0) {
-          phys = __ldg(a.block_table + (int64_t)pro.b * a.max_blocks + pro.blk);
+          phys = load_near(a.block_table + (int64_t)pro.b * a.max_blocks + pro.blk);
           return;
         } else {                                           // one block that is none
           --pro_left;
@@ -279,8 +279,8 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
       if (bad) report_status(a.hdr, TLQ_ERR_SHAPE, 210);
       const int64_t at = (int64_t)(bad ? 0 : phys) * a.n_kv + pro.h;
       q_base[i] = bad ? 0x7FFFFFFF - kKvBlock : pro.blk * kKvBlock;
-      q_k[i] = __ldg(a.k_steps + at);
-      q_v[i] = __ldg(a.v_steps + at);
+      q_k[i] = load_far(a.k_steps + at);
+      q_v[i] = load_far(a.v_steps + at);
       copy(a.k_codes + at * kBytes);
       v_src = a.v_codes + at * kBytes;
       --pro_left;
@@ -339,7 +339,7 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
               float e[8];
-              unpack8(__ldg(reinterpret_cast<const uint4*>(p + 64 * c + 16 * tq + 8 * i)), e);
+              unpack8(load_near(reinterpret_cast<const uint4*>(p + 64 * c + 16 * tq + 8 * i)), e);
 #pragma unroll
               for (int j = 0; j < 8; ++j) x[c * 16 + i * 8 + j] = e[j];
             }

@@ -33,8 +33,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 __device__ __forceinline__ PartNote load_note(const PartNote* p) {
   union { int4 v[2]; PartNote n; } u;
-  u.v[0] = __ldcg(reinterpret_cast<const int4*>(p));
-  u.v[1] = __ldcg(reinterpret_cast<const int4*>(p) + 1);
+  u.v[0] = load_far(reinterpret_cast<const int4*>(p));
+  u.v[1] = load_far(reinterpret_cast<const int4*>(p) + 1);
   return u.n;
 }
 // which item a part is of, and whether it is the last of it
@@ -44,7 +44,7 @@ struct PartOf {
 };
 __device__ __forceinline__ PartOf load_part_of(const PartNote* p) {
   union { int4 v; PartOf n; } u;
-  u.v = __ldcg(reinterpret_cast<const int4*>(p));
+  u.v = load_far(reinterpret_cast<const int4*>(p));
   return u.n;
 }
 
@@ -93,9 +93,9 @@ __device__ __forceinline__ void join_rows(const KvArgs& a, const JoinArgs& g, co
         const int j = j0 + i * kGroups + group, k = j == 0 ? 2 * w + (at & 1) : 2 * min(w + j, workers - 1);
         const float* from = partials + (size_t)k * kPitch;
         p[i] = load_part_of(notes + k);
-        pm[i] = __ldcg(from + r);
-        pl[i] = __ldcg(from + kItem + r);
-        v[i] = __ldcg(reinterpret_cast<const float4*>(from + 2 * kItem + r * D) + piece);
+        pm[i] = load_far(from + r);
+        pl[i] = load_far(from + kItem + r);
+        v[i] = load_far(reinterpret_cast<const float4*>(from + 2 * kItem + r * D) + piece);
         if (w + j >= workers) p[i].item = -1;
       }
       bool end = w + j0 + kGroups * kAtOnce >= workers;
@@ -191,7 +191,7 @@ __device__ __forceinline__ void join_tile(const KvArgs& a, const JoinArgs& g, co
     // factors of the parts
     float m = -INFINITY;
     for (int j = t / kRows; j < n; j += kThreads / kRows) {
-      const float x = __ldcg(partials + (size_t)s.parts[j] * kPitch + row0 + r);
+      const float x = load_far(partials + (size_t)s.parts[j] * kPitch + row0 + r);
       s.f[j * kRows + r] = x;
       m = fmaxf(m, x);
     }
@@ -201,7 +201,7 @@ __device__ __forceinline__ void join_tile(const KvArgs& a, const JoinArgs& g, co
     for (int j = t / kRows; j < n; j += kThreads / kRows) {
       const float f = exp2_fast(s.f[j * kRows + r] - mu);
       s.f[j * kRows + r] = f;
-      den = fmaf(f, __ldcg(partials + (size_t)s.parts[j] * kPitch + kItem + row0 + r), den);
+      den = fmaf(f, load_far(partials + (size_t)s.parts[j] * kPitch + kItem + row0 + r), den);
     }
     den = over_rows(den, false, 1);                        // (and all factors are written)
     const bool none = m == -INFINITY && den == 0.f;        // a row that sees nothing (a NaN row has a NaN sum)
@@ -223,7 +223,7 @@ __device__ __forceinline__ void join_tile(const KvArgs& a, const JoinArgs& g, co
       const float4* from = reinterpret_cast<const float4*>(partials + (size_t)s.parts[j] * kPitch + 2 * kItem + (size_t)row0 * D) + t;
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
-        const float4 v = __ldcg(from + e * kThreads);
+        const float4 v = load_far(from + e * kThreads);
         const float f = s.f[j * kRows + (e * kThreads + t) / (D / 4)];
         sum[e].x = fmaf(v.x, f, sum[e].x); sum[e].y = fmaf(v.y, f, sum[e].y);
         sum[e].z = fmaf(v.z, f, sum[e].z); sum[e].w = fmaf(v.w, f, sum[e].w);
@@ -257,7 +257,7 @@ kv_join_kernel(const KvArgs a, const JoinArgs g) {
   const int y = (int)blockIdx.y - (kPrompts ? kPromptItemRows / kPromptJoinRows : 0);
   if (y >= 0)
     join_rows<D, kFewRows>(a, g, few_partials(g.split), few_notes(g.split, D), y * kRowsEach, (y + 1) * kRowsEach,
-                           __ldcg(few_workers(g.split, D)), kFewShift, s.row);
+                           load_far(few_workers(g.split, D)), kFewShift, s.row);
   else if constexpr (kPrompts)
     join_tile<D>(a, g, prompt_partials(g.split, D), prompt_notes(g.split, D), (int)blockIdx.y * kPromptJoinRows, kPromptShift, s.tile);
 }

@@ -810,11 +810,11 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
         const int last = k0 < 0 ? k0 + 1 : k1;             // the end is passed on as a block that is none
         for (int k = k0; k < last && ok; k += 32) {
           const bool in = k0 >= 0 && k + lane < last;      // a lane for each of 32 blocks
-          const int phys = in ? __ldg(table + k + lane) : -1;
+          const int phys = in ? load_near(table + k + lane) : -1;
           const bool usable = phys >= 0 && phys < a.n_blocks;
           if (in && !usable) report_status(a.hdr, TLQ_ERR_SHAPE, 231);
           const int64_t at = (int64_t)(usable ? phys : 0) * a.n_kv + h;
-          const float ks = __ldg(a.k_steps + at), vs = __ldg(a.v_steps + at), v = vs < kStepFloor ? kStepFloor : vs;
+          const float ks = load_far(a.k_steps + at), vs = load_far(a.v_steps + at), v = vs < kStepFloor ? kStepFloor : vs;
           const float4 w = make_float4(ks, log2f(v), 1.0f / v, usable ? 1.f : 0.f);
           for (int j = 0; j < min(32, last - k); ++j, ++step) {
             const int to = step % kTileRing;

@@ -52,8 +52,8 @@ struct Raw {
 template <int D>
 __device__ __forceinline__ Raw load_raw(const uint16_t* p, int l) {
   Raw r;
-  r.lo = __ldg(reinterpret_cast<const uint2*>(p + 4 * l));
-  r.hi = __ldg(reinterpret_cast<const uint2*>(p + D / 2 + 4 * l));
+  r.lo = load_near(reinterpret_cast<const uint2*>(p + 4 * l));
+  r.hi = load_near(reinterpret_cast<const uint2*>(p + D / 2 + 4 * l));
   return r;
 }
 template <int D>
@@ -101,7 +101,7 @@ __device__ __forceinline__ Places load_places(const RopeArgs& rope, int64_t T, i
   Places p;
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
-    const int pos = i < rope.n_axes ? __ldg(rope.positions + i * T + token) : 0;
+    const int pos = i < rope.n_axes ? load_near(rope.positions + i * T + token) : 0;
     const bool in = pos >= 0 && (int64_t)pos < rope.n_positions;
     bad = bad || !in;
     p.at[i] = in ? pos : 0;
@@ -121,7 +121,7 @@ __device__ __forceinline__ Angles load_angles(const RopeArgs& rope, const Places
   if (rope.n_axes == 1 || axis == last) {              // one axis for all four
     const int at = rope.n_axes == 1 || axis == 0 ? p.at[0] : axis == 1 ? p.at[1] : p.at[2];
     const float* row = rope.cos_sin + (int64_t)at * D + first;
-    const float4 c = __ldg(reinterpret_cast<const float4*>(row)), s = __ldg(reinterpret_cast<const float4*>(row + D / 2));
+    const float4 c = load_near(reinterpret_cast<const float4*>(row)), s = load_near(reinterpret_cast<const float4*>(row + D / 2));
     g.c[0] = c.x; g.c[1] = c.y; g.c[2] = c.z; g.c[3] = c.w;
     g.s[0] = s.x; g.s[1] = s.y; g.s[2] = s.z; g.s[3] = s.w;
   } else {
@@ -129,8 +129,8 @@ __device__ __forceinline__ Angles load_angles(const RopeArgs& rope, const Places
     for (int j = 0; j < 4; ++j) {
       const int i = (first + j >= rope.pairs_end[0] ? 1 : 0) + (first + j >= rope.pairs_end[1] ? 1 : 0);
       const float* row = rope.cos_sin + (int64_t)(i == 0 ? p.at[0] : i == 1 ? p.at[1] : p.at[2]) * D + first + j;
-      g.c[j] = __ldg(row);
-      g.s[j] = __ldg(row + D / 2);
+      g.c[j] = load_near(row);
+      g.s[j] = load_near(row + D / 2);
     }
   }
   return g;
@@ -183,8 +183,8 @@ kv_store_kernel(const KvArgs a, const StoreArgs g) {
     const unsigned rows = (unsigned)(a.T * a.n_heads);
     uint4 w[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
     if (g.q_norm != nullptr) {
-      w[0] = __ldg(reinterpret_cast<const uint4*>(g.q_norm + 8 * lq));
-      w[1] = __ldg(reinterpret_cast<const uint4*>(g.q_norm + D / 2 + 8 * lq));
+      w[0] = load_near(reinterpret_cast<const uint4*>(g.q_norm + 8 * lq));
+      w[1] = load_near(reinterpret_cast<const uint4*>(g.q_norm + D / 2 + 8 * lq));
     }
     bool bad = false;
     constexpr unsigned kChunk = kSweepsQ * kRowsQ;
@@ -199,8 +199,8 @@ kv_store_kernel(const KvArgs a, const StoreArgs g) {
         x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
         if (r < rows) {
           const uint16_t* p = g.qkv + (int64_t)token[i] * g.ld + (int64_t)(r - token[i] * (unsigned)a.n_heads) * D + 8 * lq;
-          x[i][0] = ld_nc_16(p);
-          x[i][1] = ld_nc_16(p + D / 2);
+          x[i][0] = load_once(p);
+          x[i][1] = load_once(p + D / 2);
         }
       }
       Angles turns[2]{};
@@ -346,7 +346,7 @@ kv_store_kernel(const KvArgs a, const StoreArgs g) {
     tops[1][threadIdx.x >> 5] = vtop;
   }
   const int64_t at = (int64_t)phys * a.n_kv + h;
-  const float kold = off0 > 0 ? a.k_steps[at] : 0.f, vold = off0 > 0 ? a.v_steps[at] : 0.f;
+  const float kold = off0 > 0 ? load_far(a.k_steps + at) : 0.f, vold = off0 > 0 ? load_far(a.v_steps + at) : 0.f;
   __syncthreads();                                   // also: every thread has read the old steps
 #pragma unroll
   for (int i = 0; i < kStoreThreads / 32; ++i) {

@@ -17,12 +17,6 @@
 namespace tlq {
 namespace {
 
-__device__ __forceinline__ uint4 ld_weights(const int8_t* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
 __device__ __forceinline__ void mma_i8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                        uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -32,9 +26,8 @@ __device__ __forceinline__ void mma_i8(int (&c)[4], uint32_t a0, uint32_t a1, ui
 
 template <int NT, int kWarps>
 __global__ void __launch_bounds__(kWarps * 32)
-linear_i8_few_kernel(const int8_t* __restrict__ X, const float* __restrict__ t, const int8_t* __restrict__ W,
-                     const float* __restrict__ u, const uint16_t* __restrict__ bias, int64_t N, int C1, int64_t C2,
-                     uint16_t* __restrict__ Y) {
+linear_i8_few_kernel(const int8_t* X, const float* t, const int8_t* W,
+                     const float* u, const uint16_t* bias, int64_t N, int C1, int64_t C2, uint16_t* Y) {
   constexpr int kThreads = kWarps * 32;
   __shared__ int s_acc[kWarps][NT * 8][17];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -56,10 +49,10 @@ linear_i8_few_kernel(const int8_t* __restrict__ X, const float* __restrict__ t, 
 #pragma unroll 4
   for (int c = (warp * 4 + q) * 16; c - q * 16 < C1; c += kWarps * 64) {
     const bool in = c < C1;                        // C1 is a multiple of 16: a piece is in or out as a whole
-    const uint4 a = in ? ld_weights(w0 + c) : zero, b = in ? ld_weights(w1 + c) : zero;
+    const uint4 a = in ? load_once(w0 + c) : zero, b = in ? load_once(w1 + c) : zero;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const uint4 v = in ? __ldg(reinterpret_cast<const uint4*>(x[n] + c)) : zero;
+      const uint4 v = in ? load_near(reinterpret_cast<const uint4*>(x[n] + c)) : zero;
       mma_i8(acc[n], a.x, b.x, a.y, b.y, v.x, v.y);
       mma_i8(acc[n], a.z, b.z, a.w, b.w, v.z, v.w);
     }
@@ -220,8 +213,8 @@ linear_i8_tile_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     float u[4], b[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      u[j] = o + j < g.C2 ? __ldg(g.u + o + j) : 0.f;
-      b[j] = g.bias != nullptr && o + j < g.C2 ? bf16_bits_to_float(__ldg(g.bias + o + j)) : 0.f;
+      u[j] = o + j < g.C2 ? load_near(g.u + o + j) : 0.f;
+      b[j] = g.bias != nullptr && o + j < g.C2 ? bf16_bits_to_float(g.bias[o + j]) : 0.f;
     }
     const bool whole = (g.C2 & 3) == 0 && o + 4 <= g.C2;  // four channels at an address of 8 bytes
     uint32_t from[kMaxSplits];
@@ -229,7 +222,7 @@ linear_i8_tile_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     for (int r = 0; r < kMaxSplits; ++r) from[r] = g.splits > 1 && r < g.splits ? ptx::map_to_cta(base, (uint32_t)r) : base;
     for (int c = c0 + warp; c < c1; c += kTileThreads / 32) {
       const uint32_t at = (uint32_t)(c * kTileO + 4 * lane) * 4u;
-      const float t = __ldg(g.t + n0 + c);
+      const float t = load_near(g.t + n0 + c);
       int4 s = ld_cluster(from[0] + at);
       if (g.splits > 1) {
         int4 v[kMaxSplits];

@@ -160,6 +160,41 @@ __device__ __forceinline__ void after_previous() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
+// Nothing that a call is given is therefore constant for its kernel's whole life, which begins while the kernel before may still
+// write it: the read-only path (ld.global.nc, which __ldg and const __restrict__ ask for) is not for these kernels.  The loads
+// below are ordinary ones, and volatile, so that none can move before the wait.
+template <typename T>
+__device__ __forceinline__ T load_near(const T* p) {       // may stay in the SM's first-level cache
+  static_assert(sizeof(T) == 4 || sizeof(T) == 8 || sizeof(T) == 16, "");
+  union { T t; uint32_t w[sizeof(T) / 4]; } u;
+  if constexpr (sizeof(T) == 4)
+    asm volatile("ld.global.b32 %0, [%1];" : "=r"(u.w[0]) : "l"(p) : "memory");
+  else if constexpr (sizeof(T) == 8)
+    asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(u.w[0]), "=r"(u.w[1]) : "l"(p) : "memory");
+  else
+    asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(u.w[0]), "=r"(u.w[1]), "=r"(u.w[2]), "=r"(u.w[3]) : "l"(p) : "memory");
+  return u.t;
+}
+// From the second-level cache: partial sums, and the steps of the cache, of which the store's block of one head may have brought its
+// neighbours' into the SM's first-level cache before others wrote those.
+template <typename T>
+__device__ __forceinline__ T load_far(const T* p) {
+  static_assert(sizeof(T) == 4 || sizeof(T) == 16, "");
+  union { T t; uint32_t w[sizeof(T) / 4]; } u;
+  if constexpr (sizeof(T) == 4)
+    asm volatile("ld.global.cg.b32 %0, [%1];" : "=r"(u.w[0]) : "l"(p) : "memory");
+  else
+    asm volatile("ld.global.cg.v4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(u.w[0]), "=r"(u.w[1]), "=r"(u.w[2]), "=r"(u.w[3]) : "l"(p) : "memory");
+  return u.t;
+}
+__device__ __forceinline__ uint4 load_once(const void* p) { // 16 bytes that no other warp of the SM will read
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
 template <typename... Params, typename... Args>
 inline int launch_next(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, unsigned cluster, cudaStream_t st,
                        Args... args) {
