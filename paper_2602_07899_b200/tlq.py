@@ -345,6 +345,22 @@ def _typed(t: torch.Tensor, dtype: torch.dtype, shape, what: str) -> torch.Tenso
     return t
 
 
+def _one_device(what: str, first, *rest) -> int:
+    """Number of the device that all of them lie on (-1: host memory)."""
+    dev = first.get_device()
+    for t in rest:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"{what}: all tensors must lie on one device")
+    return dev
+
+
+def _on_device(what: str, first, *rest) -> None:
+    """The kernels run on the current device, and a pointer to anywhere else is a memory fault there: refused here."""
+    dev = _one_device(what, first, *rest)
+    if dev < 0 or dev != (torch.cuda.current_device() if _raw_device is None else _raw_device()):
+        raise ValueError(f"{what}: tensors must lie on the current CUDA device, got {'host memory' if dev < 0 else f'device {dev}'}")
+
+
 def _rows(t: torch.Tensor, what: str) -> int:
     """Row pitch in elements of a bf16 tensor whose rows are contiguous."""
     if t.dtype is not _BF16:
@@ -369,9 +385,14 @@ class KvCache:
         _typed(v_steps, torch.float32, (blocks, heads), "v_steps")
         self.k_codes, self.v_codes, self.k_steps, self.v_steps = k_codes, v_codes, k_steps, v_steps
         self.n_blocks, self.n_kv_heads, self.head_dim, self.device = blocks, heads, dim, k_codes.device
+        self._device = _one_device("KvCache", k_codes, v_codes, k_steps, v_steps)
         self._c = _KvCacheStruct(ctypes.sizeof(_KvCacheStruct), heads, dim, blocks, k_codes.data_ptr(), v_codes.data_ptr(),
                                  k_steps.data_ptr(), v_steps.data_ptr())
         self._p = ctypes.addressof(self._c)
+
+    def get_device(self) -> int:
+        """As of a tensor: the number of its device, -1 in host memory (which the calls refuse)."""
+        return self._device
 
     @classmethod
     def empty(cls, n_blocks: int, n_kv_heads: int, head_dim: int, device) -> "KvCache":
@@ -391,9 +412,13 @@ class KvBatch:
         _typed(kv_len, torch.int32, (n,), "kv_len")
         _typed(block_table, torch.int32, (n, block_table.shape[-1]), "block_table")
         self.cu_q, self.kv_len, self.block_table, self.max_q_len = cu_q, kv_len, block_table, int(max_q_len)
+        self._device = _one_device("KvBatch", cu_q, kv_len, block_table)
         self._c = _KvBatchStruct(ctypes.sizeof(_KvBatchStruct), n, self.max_q_len, block_table.shape[1], cu_q.data_ptr(),
                                  kv_len.data_ptr(), block_table.data_ptr())
         self._p = ctypes.addressof(self._c)
+
+    def get_device(self) -> int:
+        return self._device
 
 
 def _by_address(name: str):
@@ -450,6 +475,7 @@ def tlq_linear_i8(Xq: torch.Tensor, t: torch.Tensor, Wq: torch.Tensor, u: torch.
         _typed(u, _F32, (C2,), "u")
     if bias is not None:
         _typed(bias, _BF16, (C2,), "bias")
+    _on_device("tlq_linear_i8", Xq, t, Wq, u, bias, workspace, out)
     if workspace is None:
         workspace = _workspace_on(stream, linear_workspace, N, C1, C2, Xq.device)
     if out is None:
@@ -492,6 +518,7 @@ def tlq_kv_store(qkv: torch.Tensor, n_heads: int, cache: KvCache, batch: KvBatch
         _typed(q_norm, _BF16, (d,), "q_norm")
     if k_norm is not None:
         _typed(k_norm, _BF16, (d,), "k_norm")
+    _on_device("tlq_kv_store", qkv, cache, batch, positions, None if positions is None else cos_sin, q_norm, k_norm, workspace)
     if workspace is None:
         workspace = _workspace_on(stream, kv_workspace, cache, n_heads, T, batch)
     q = qkv.new_empty((T, n_heads, d))
@@ -515,6 +542,7 @@ def tlq_kv_attention(q: torch.Tensor, cache: KvCache, batch: KvBatch, scale: flo
     if d != cache.head_dim:
         raise ValueError("q and the cache differ in head_dim")
     ldq = _rows(q, "q")
+    _on_device("tlq_kv_attention", q, cache, batch, workspace)
     if workspace is None:
         workspace = _workspace_on(stream, kv_workspace, cache, n_heads, T, batch)
     out = q.new_empty((T, n_heads, d))
