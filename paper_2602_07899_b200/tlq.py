@@ -361,6 +361,12 @@ def _on_device(what: str, first, *rest) -> None:
         raise ValueError(f"{what}: tensors must lie on the current CUDA device, got {'host memory' if dev < 0 else f'device {dev}'}")
 
 
+def _plain(workspace: Optional[torch.Tensor]) -> None:
+    """Its number of elements is passed on as a number of bytes, which a view that repeats memory does not have."""
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+
+
 def _rows(t: torch.Tensor, what: str) -> int:
     """Row pitch in elements of a bf16 tensor whose rows are contiguous."""
     if t.dtype is not _BF16:
@@ -475,6 +481,7 @@ def tlq_linear_i8(Xq: torch.Tensor, t: torch.Tensor, Wq: torch.Tensor, u: torch.
         _typed(u, _F32, (C2,), "u")
     if bias is not None:
         _typed(bias, _BF16, (C2,), "bias")
+    _plain(workspace)
     _on_device("tlq_linear_i8", Xq, t, Wq, u, bias, workspace, out)
     if workspace is None:
         workspace = _workspace_on(stream, linear_workspace, N, C1, C2, Xq.device)
@@ -518,6 +525,7 @@ def tlq_kv_store(qkv: torch.Tensor, n_heads: int, cache: KvCache, batch: KvBatch
         _typed(q_norm, _BF16, (d,), "q_norm")
     if k_norm is not None:
         _typed(k_norm, _BF16, (d,), "k_norm")
+    _plain(workspace)
     _on_device("tlq_kv_store", qkv, cache, batch, positions, None if positions is None else cos_sin, q_norm, k_norm, workspace)
     if workspace is None:
         workspace = _workspace_on(stream, kv_workspace, cache, n_heads, T, batch)
@@ -542,6 +550,7 @@ def tlq_kv_attention(q: torch.Tensor, cache: KvCache, batch: KvBatch, scale: flo
     if d != cache.head_dim:
         raise ValueError("q and the cache differ in head_dim")
     ldq = _rows(q, "q")
+    _plain(workspace)
     _on_device("tlq_kv_attention", q, cache, batch, workspace)
     if workspace is None:
         workspace = _workspace_on(stream, kv_workspace, cache, n_heads, T, batch)

@@ -66,3 +66,12 @@ def test_caches_and_batches_know_where_they_lie(tlq, monkeypatch, host):
     seen = iter([0, 0, 1])
     with pytest.raises(ValueError, match="device"):
         tlq.KvBatch(batch.cu_q, batch.kv_len, batch.block_table, 1)
+
+
+@pytest.mark.parametrize("name", ["linear", "store", "attention"])
+def test_workspaces_that_are_not_plain_memory_are_refused(tlq, host, name):
+    """The library is told the number of elements as the number of bytes: a view that repeats or skips memory has fewer."""
+    for bad in (torch.zeros(1, dtype=torch.uint8).expand(1 << 20), torch.zeros(1 << 20, dtype=torch.uint8)[::2],
+                torch.zeros(1, 1 << 10, dtype=torch.uint8).expand(1 << 10, -1)):
+        with pytest.raises(ValueError, match="workspace"):
+            calls(tlq)[name](**host[name], workspace=bad)
