@@ -1,0 +1,61 @@
+"""The serving operators where a step, a length or a stream is not what the ordinary case has."""
+import pytest
+import torch
+
+from test_gpu_serving import gen, make_batch, on_gpu
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def tlq():
+    from paper_2602_07899_b200 import tlq as mod
+    return mod
+
+
+def test_steps_that_grow_reach_the_attention_behind_the_store(tlq):
+    """Decoding steps without a pause between the calls against the same with the GPU idle between them: the kernels of one
+    come up while those of the other still write the steps, codes and queries that they read."""
+    hk, d, heads, n = 8, 128, 16, 24
+    s = make_batch(61, [1] * 6, [40, 64, 65, 130, 200, 7], hk, d)
+    s["ks"], s["vs"] = s["ks"].nan_to_num(0.0), s["vs"].nan_to_num(0.0, posinf=0.0)
+    grow = torch.exp2(torch.arange(n) / 3.0)[:, None, None]        # every token is larger than those before: every step grows
+    qkv = (torch.randn(n, 6, (heads + 2 * hk) * d, generator=gen(3)) * grow).bfloat16().cuda()
+
+    def answer(pause):
+        cache, batch = on_gpu(tlq, s)
+        ws = tlq.kv_workspace(cache, heads, 6, batch)
+        outs = []
+        torch.cuda.synchronize()
+        for i in range(n):
+            q, _, _ = tlq.tlq_kv_store(qkv[i], heads, cache, batch, workspace=ws)
+            if pause:
+                torch.cuda.synchronize()
+            outs.append(tlq.tlq_kv_attention(q, cache, batch, d ** -0.5 / 64, want_lse=True, workspace=ws))
+            if pause:
+                torch.cuda.synchronize()
+        assert tlq.tlq_read_status(ws) == tlq.OK
+        return [t for pair in outs for t in pair] + [cache.k_codes, cache.v_codes, cache.k_steps, cache.v_steps]
+
+    want = answer(True)
+    for _ in range(5):
+        assert all(torch.equal(a, b) for a, b in zip(want, answer(False)))
+
+
+def test_tensors_in_host_memory_beside_those_of_the_gpu_are_refused(tlq):
+    s = make_batch(62, [1, 2], [5, 70], 1, 64)
+    cache, batch = on_gpu(tlq, s)
+    q, qkv = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(3, 4 * 64, dtype=torch.bfloat16, device="cuda")
+    pos, ang = torch.zeros(3, dtype=torch.int32), torch.zeros(9, 64)
+    with pytest.raises(ValueError, match="device"):
+        tlq.KvBatch(s["cu"], s["kv"].cuda(), s["table"].cuda(), 2)
+    with pytest.raises(ValueError, match="device"):
+        tlq.tlq_kv_attention(q, cache, tlq.KvBatch(s["cu"], s["kv"], s["table"], 2), 0.1)
+    with pytest.raises(ValueError, match="device"):
+        tlq.tlq_kv_store(qkv, 2, cache, batch, pos, ang.cuda())
+    with pytest.raises(ValueError, match="device"):
+        tlq.tlq_kv_store(qkv, 2, cache, batch, pos.cuda(), ang)
+    x, t, w, u = torch.zeros(2, 32, dtype=torch.int8), torch.zeros(2), torch.zeros(5, 32, dtype=torch.int8), torch.zeros(5)
+    for here in (lambda v: v is not t, lambda v: v is not u, lambda v: v is not w):
+        with pytest.raises(ValueError, match="device"):
+            tlq.tlq_linear_i8(*[v.cuda() if here(v) else v for v in (x, t, w, u)])
