@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_gpu_serving import gen, make_batch, on_gpu
+from test_gpu_serving import gen, linear_close, make_batch, on_gpu
 
 pytestmark = pytest.mark.gpu
 
@@ -59,3 +59,22 @@ def test_tensors_in_host_memory_beside_those_of_the_gpu_are_refused(tlq):
     for here in (lambda v: v is not t, lambda v: v is not u, lambda v: v is not w):
         with pytest.raises(ValueError, match="device"):
             tlq.tlq_linear_i8(*[v.cuda() if here(v) else v for v in (x, t, w, u)])
+
+
+@pytest.mark.parametrize("n,ci,co", [(2048, 1040, 8963), (4100, 208, 2401), (4100, 208, 2396), (700, 48, 13001)])
+def test_linear_of_many_tokens_and_odd_widths(tlq, n, ci, co):
+    """Widths that are no multiple of 8, and sums that end inside a block of channels, in the persistent kernel."""
+    g = gen(n + ci + co)
+    xq = torch.randint(-127, 128, (n, ci), generator=g).to(torch.int8).cuda()
+    wq = torch.randint(-128, 128, (co, ci), generator=g).to(torch.int8).cuda()
+    t, u = (torch.rand(n, generator=g) * 0.05 + 1e-4).cuda(), (torch.rand(co, generator=g) * 0.002 + 1e-6).cuda()
+    b = torch.randn(co, generator=g).bfloat16().cuda()
+    for bias in (b, None):
+        want = (xq.double() @ wq.double().t()) * torch.outer(t.double(), u.double())     # exact: integers below 2^53
+        mag = want.abs()
+        if bias is not None:
+            want, mag = want + bias.double(), mag + bias.double().abs()
+        guarded = torch.full((n * co + 64,), 7.0, dtype=torch.bfloat16, device="cuda")
+        y = tlq.tlq_linear_i8(xq, t, wq, u, bias, out=guarded[:n * co].view(n, co))
+        linear_close(y, want.cpu(), mag.cpu())
+        assert torch.all(guarded[n * co:] == 7.0)
