@@ -1,4 +1,6 @@
 """The serving operators where a step, a length or a stream is not what the ordinary case has."""
+import math
+
 import pytest
 import torch
 
@@ -78,3 +80,24 @@ def test_linear_of_many_tokens_and_odd_widths(tlq, n, ci, co):
         y = tlq.tlq_linear_i8(xq, t, wq, u, bias, out=guarded[:n * co].view(n, co))
         linear_close(y, want.cpu(), mag.cpu())
         assert torch.all(guarded[n * co:] == 7.0)
+
+
+@pytest.mark.parametrize("n,ci,co", [(5, 512, 96), (5, 512, 97), (60, 512, 96), (60, 512, 97), (4100, 208, 2400), (4100, 208, 2401)])
+def test_linear_of_steps_that_are_not_finite(tlq, n, ci, co):
+    """The same pattern of infinities and NaN whichever kernel the size selects; zero sums of an infinite step are NaN."""
+    g = gen(n + co)
+    xq = torch.randint(-127, 128, (n, ci), generator=g).to(torch.int8)
+    wq = torch.randint(-127, 128, (co, ci), generator=g).to(torch.int8)
+    t, u = torch.rand(n, generator=g) + 0.5, torch.rand(co, generator=g) + 0.5
+    xq[1] = 0
+    t[1], t[2], t[n - 1] = math.inf, math.inf, math.nan
+    u[3], u[co - 1], u[co - 2] = math.nan, math.inf, -math.inf
+    acc = xq.cuda().double() @ wq.cuda().double().t()
+    want = (acc * torch.outer(t.cuda().double(), u.cuda().double())).cpu()
+    y = tlq.tlq_linear_i8(xq.cuda(), t.cuda(), wq.cuda(), u.cuda()).double().cpu()
+    assert torch.isnan(want).any() and torch.isinf(want).any()
+    assert torch.equal(torch.isnan(y), torch.isnan(want))
+    odd = torch.isinf(want)
+    assert torch.equal(y[odd], want[odd])
+    fine = torch.isfinite(want)
+    linear_close(y[fine], want[fine], want[fine].abs())
