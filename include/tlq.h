@@ -339,6 +339,7 @@ int tlq_kv_store(const void* qkv, int64_t T, int64_t ld, int32_t n_heads, const 
  *   q [T, n_heads, head_dim] bf16, rows ldq elements apart (a multiple of 8); out [T, n_heads, head_dim] bf16;
  *   lse [T, n_heads] fp32 or NULL: ln sum_j exp(scale * q . k_j).  scale > 0 and finite.
  * A row that sees nothing (no cached token, or a place before the first) gets zeros and lse = -infinity.
+ * Blocks that nothing was written to (codes and steps of zero) are keys and values of zero; value steps below 2^-80 count as 2^-80.
  */
 int tlq_kv_attention(const void* q, int64_t T, int64_t ldq, int32_t n_heads, const tlq_kv_cache* cache,
                      const tlq_kv_batch* batch, float scale, int32_t causal, void* workspace, size_t workspace_bytes,

@@ -99,8 +99,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// Steps below this have a smaller logarithm than the running maximum can carry; values that small count as zero.
-constexpr float kStepFloor = 7.8886090522101181e-31f;      // 2^-100
 
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 

@@ -41,7 +41,6 @@ constexpr int kThreads = 512;                              // four groups of fou
 constexpr int kSoftRegs = 176, kLoadRegs = 72, kIssueRegs = 88;
 constexpr float kShift = kPromptShift, kGrow = 4.9f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kStepFloor = 7.8886090522101181e-31f;      // 2^-100, as in kv_attention.cu
 constexpr float kUnit = 16777216.f;                        // 2^24
 constexpr int kMinTiles = 6;                               // blocks of a CTA's part, at least (512 tokens x 512: 34 us, 37 with 12)
 constexpr int kItemCost = 8;                               // what an item costs beside its blocks, in blocks (8192 tokens: 555, 564 with 12)

@@ -238,6 +238,10 @@ constexpr int kMaxRowTile = 16;           // query rows of one of its items (8 o
 constexpr int kPromptItemRows = 256;      // query rows of one item of the prompt kernel
 constexpr int kPromptJoinRows = 32;       // rows of such an item that a CTA joins
 constexpr float kFewShift = 15.f, kPromptShift = 11.f;     // the sums hold 2^shift p
+// Value steps below this count as this: blocks that nothing was written to have a step of zero (the store's own are 7.9e-8 at least).
+// The sum of p / step over the 2^30 tokens that a table can name stays below 2^(16 + 80 + 30), inside the 32-bit range.
+constexpr float kStepFloor = 8.2718061255302767e-25f;      // 2^-80
+static_assert((long long)(1 << 24) * kKvBlock <= 1ll << 30, "max_blocks is at most 2^24");
 struct __align__(16) PartNote {           // a part of an item's blocks
   long long item;             // where the item is on the line of its kernel; negative: there is no part
   int first, last;            // the part has the item's first, its last blocks

@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_serving import gen, linear_close, make_batch, on_gpu
+from test_gpu_serving import BLOCK, gen, linear_close, make_batch, on_gpu
 
 pytestmark = pytest.mark.gpu
 
@@ -101,3 +101,23 @@ def test_linear_of_steps_that_are_not_finite(tlq, n, ci, co):
     assert torch.equal(y[odd], want[odd])
     fine = torch.isfinite(want)
     linear_close(y[fine], want[fine], want[fine].abs())
+
+
+@pytest.mark.parametrize("q_lens,kv_lens", [([1, 2], [20000, 9]), ([300, 1], [140000, 70])])
+def test_attention_over_an_empty_cache(tlq, q_lens, kv_lens):
+    """Blocks that nothing was written to, as before a warm-up: all scores equal, all values zero.  The logarithm is taken of a sum
+    below 2^112 (its result is exact to 2^-17), and the sums of equal powers of two are exact."""
+    hk, d, heads = 1, 64, 4
+    need = [-(-k // BLOCK) for k in kv_lens]
+    cache = tlq.KvCache.empty(sum(need), hk, d, "cuda")
+    table = torch.zeros(2, max(need), dtype=torch.int32)
+    table[0, :need[0]], table[1, :need[1]] = torch.arange(need[0]), need[0] + torch.arange(need[1])
+    cu = torch.tensor([0, q_lens[0], sum(q_lens)], dtype=torch.int32)
+    batch = tlq.KvBatch(cu.cuda(), torch.tensor(kv_lens, dtype=torch.int32).cuda(), table.cuda(), max(q_lens))
+    q = torch.randn(sum(q_lens), heads, d, generator=gen(1)).bfloat16().cuda()
+    for causal in (True, False):
+        out, lse = tlq.tlq_kv_attention(q, cache, batch, 0.125, causal, want_lse=True)
+        assert torch.all(out == 0)
+        seen = torch.cat([k - n + 1 + torch.arange(n) if causal else torch.full((n,), k) for n, k in zip(q_lens, kv_lens)])
+        want = seen.double().log()[:, None].expand(-1, heads)
+        assert torch.all((lse.double().cpu() - want).abs() <= 2.0 ** -15)
