@@ -277,8 +277,8 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
       if (bad) report_status(a.hdr, TLQ_ERR_SHAPE, 210);
       const int64_t at = (int64_t)(bad ? 0 : phys) * a.n_kv + pro.h;
       q_base[i] = bad ? 0x7FFFFFFF - kKvBlock : pro.blk * kKvBlock;
-      q_k[i] = load_far(a.k_steps + at);
-      q_v[i] = load_far(a.v_steps + at);
+      q_k[i] = load_near(a.k_steps + at);
+      q_v[i] = load_near(a.v_steps + at);
       copy(a.k_codes + at * kBytes);
       v_src = a.v_codes + at * kBytes;
       --pro_left;

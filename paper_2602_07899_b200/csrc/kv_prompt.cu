@@ -813,7 +813,7 @@ kv_prompt_kernel(const KvArgs a, const PromptArgs g) {
           const bool usable = phys >= 0 && phys < a.n_blocks;
           if (in && !usable) report_status(a.hdr, TLQ_ERR_SHAPE, 231);
           const int64_t at = (int64_t)(usable ? phys : 0) * a.n_kv + h;
-          const float ks = load_far(a.k_steps + at), vs = load_far(a.v_steps + at), v = vs < kStepFloor ? kStepFloor : vs;
+          const float ks = load_near(a.k_steps + at), vs = load_near(a.v_steps + at), v = vs < kStepFloor ? kStepFloor : vs;
           const float4 w = make_float4(ks, log2f(v), 1.0f / v, usable ? 1.f : 0.f);
           for (int j = 0; j < min(32, last - k); ++j, ++step) {
             const int to = step % kTileRing;

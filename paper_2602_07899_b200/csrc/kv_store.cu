@@ -346,7 +346,7 @@ kv_store_kernel(const KvArgs a, const StoreArgs g) {
     tops[1][threadIdx.x >> 5] = vtop;
   }
   const int64_t at = (int64_t)phys * a.n_kv + h;
-  const float kold = off0 > 0 ? load_far(a.k_steps + at) : 0.f, vold = off0 > 0 ? load_far(a.v_steps + at) : 0.f;
+  const float kold = off0 > 0 ? load_near(a.k_steps + at) : 0.f, vold = off0 > 0 ? load_near(a.v_steps + at) : 0.f;
   __syncthreads();                                   // also: every thread has read the old steps
 #pragma unroll
   for (int i = 0; i < kStoreThreads / 32; ++i) {
