@@ -262,9 +262,11 @@ int tlq_apply_layer(const void* X, int64_t N, int64_t C1, const void* W, int64_t
  *    workspace serves any number of calls on one stream; streams that run at the same time need one each.  The status
  *    word (byte 0, tlq_read_status) is not reset by these calls: it keeps the last error until its owner zeroes the
  *    workspace again.
- *  - Lengths and block tables are read on the device, so a call never synchronises.  An entry that does not fit (a length
- *    beyond the table, a block outside of the cache, a position outside of the angle table) sets the status word to
- *    TLQ_ERR_SHAPE; what it concerns is left out, and nothing is accessed out of bounds.
+ *  - Lengths and block tables are read on the device, so a call never synchronises.  An entry that does not fit sets the
+ *    status word to TLQ_ERR_SHAPE, and nothing is accessed out of bounds.  A request with a length beyond its table, or with
+ *    more new tokens than max_q_len, is left out whole: nothing of it goes into the cache, and its rows of attention are
+ *    those of a row that sees nothing.  A block outside of the cache is neither read nor written.  A position outside of the
+ *    angle table turns by the angles of position 0.
  *  - T = 0 or N = 0 (nothing to do in this step) is TLQ_OK and launches nothing.
  */
 

@@ -29,8 +29,9 @@ __device__ __forceinline__ void report_status(WorkspaceHeader* hdr, int status, 
   hdr->status = status;
 }
 
-// Lengths of one request, forced into what the call's buffers hold (anything else is reported, and what does not fit
-// is left out), so that no metadata can move an access out of bounds.
+// Lengths of one request, forced into what the call's buffers hold, so that no metadata can move an access out of bounds; anything
+// else is reported.  A request whose cached tokens go beyond its table, or that has more new tokens than the batch allows, is left
+// out whole (as if it had no cached token): with lengths cut to what fits its new tokens would take the places of older ones.
 struct Request {
   int q0, q_len, kv;          // first row of q, new tokens, cached tokens with the new ones
 };
@@ -39,10 +40,10 @@ __device__ __forceinline__ Request load_request(const KvArgs& a, int b) {
   Request r;
   r.q0 = max(0, min(c0, (int)a.T));
   const int end = max(r.q0, min(c1, (int)a.T));
-  r.q_len = min(end - r.q0, a.max_q_len);
-  const long long room = (long long)a.max_blocks * kKvBlock;
-  r.kv = kv < 0 ? 0 : ((long long)kv > room ? (int)room : kv);
-  if (r.q0 != c0 || r.q_len != c1 - c0 || r.kv != kv) report_status(a.hdr, TLQ_ERR_SHAPE, 200);
+  r.q_len = end - r.q0;
+  const bool fits = kv >= 0 && kv <= (long long)a.max_blocks * kKvBlock && r.q_len <= a.max_q_len;
+  r.kv = fits ? kv : 0;
+  if (r.q0 != c0 || end != c1 || !fits) report_status(a.hdr, TLQ_ERR_SHAPE, 200);
   return r;
 }
 

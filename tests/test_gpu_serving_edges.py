@@ -4,7 +4,8 @@ import math
 import pytest
 import torch
 
-from test_gpu_serving import BLOCK, gen, linear_close, make_batch, on_gpu
+import serving_ref as ref
+from test_gpu_serving import BIG, BLOCK, gen, linear_close, make_batch, on_gpu
 
 pytestmark = pytest.mark.gpu
 
@@ -121,3 +122,58 @@ def test_attention_over_an_empty_cache(tlq, q_lens, kv_lens):
         seen = torch.cat([k - n + 1 + torch.arange(n) if causal else torch.full((n,), k) for n, k in zip(q_lens, kv_lens)])
         want = seen.double().log()[:, None].expand(-1, heads)
         assert torch.all((lse.double().cpu() - want).abs() <= 2.0 ** -15)
+
+
+def dirty(*shapes):
+    """Leaves NaN in the memory that the next tensors of these shapes will get."""
+    held = [torch.full(shape, math.nan, dtype=dtype, device="cuda") for shape, dtype in shapes]
+    torch.cuda.synchronize()
+    del held
+
+
+@pytest.mark.parametrize("what", ["length", "negative", "rows"])
+@pytest.mark.parametrize("big", [False, True])
+def test_requests_that_do_not_fit_are_left_out_whole(tlq, what, big):
+    """A length beyond the table, more new tokens than the batch allows: the request's tokens have no place.  None of its
+    blocks is written, its rows are empty, the other requests are unharmed."""
+    hk, d, heads = 2, 64, 6
+    q_lens, kv_lens = [20, 3, 40] + [BIG[0]] * big, [128, 70, 128] + [BIG[1]] * big
+    s = make_batch(64, q_lens, kv_lens, hk, d, pad=0)
+    if what == "length":
+        s["kv"][0] = s["table"].shape[1] * BLOCK + 10
+        s["table"][0] = s["table"][0, 0]
+    elif what == "negative":
+        s["kv"][0] = -5
+    else:
+        s["q_max"], out_of = (BIG[0] - 1, 3) if big else (39, 2)
+    out_of = 0 if what != "rows" else out_of
+    cu = [int(v) for v in s["cu"]]
+    rows = torch.zeros(s["T"], dtype=torch.bool, device="cuda")
+    rows[cu[out_of]:cu[out_of + 1]] = True
+    qkv = torch.randn(s["T"], (heads + 2 * hk) * d, generator=gen(5)).bfloat16().cuda()
+    cache, batch = on_gpu(tlq, s)
+    ws = tlq.kv_workspace(cache, heads, s["T"], batch)
+    q, k, _ = tlq.tlq_kv_store(qkv, heads, cache, batch, want_values=True, workspace=ws)
+    assert tlq.tlq_read_status(ws) == tlq.ERR_SHAPE
+    own = s["table"][out_of, :-(-kv_lens[out_of] // BLOCK)].unique().long()
+    for name in ("kc", "vc", "ks", "vs"):
+        got = getattr(cache, {"kc": "k_codes", "vc": "v_codes", "ks": "k_steps", "vs": "v_steps"}[name]).cpu()
+        assert torch.equal(got[own], s[name][own]), name
+    # the others: as without it
+    fits = dict(s, kv=s["kv"].clone(), q_max=max(q_lens))
+    if what != "rows":
+        fits["kv"][0] = kv_lens[0]
+    good, good_batch = on_gpu(tlq, fits)
+    wq, wk, _ = tlq.tlq_kv_store(qkv, heads, good, good_batch, want_values=True)
+    others = torch.tensor([b for b in range(len(s["ks"])) if b not in own.tolist()])
+    assert torch.equal(cache.k_codes[others], good.k_codes[others]) and torch.equal(cache.v_codes[others], good.v_codes[others])
+    assert torch.equal(q, wq) and torch.equal(k[~rows], wk[~rows])
+    ws.zero_()
+    dirty(((s["T"], heads, d), torch.bfloat16), ((s["T"], heads), torch.float32))
+    out, lse = tlq.tlq_kv_attention(q, cache, batch, 0.125, want_lse=True, workspace=ws)
+    assert tlq.tlq_read_status(ws) == tlq.ERR_SHAPE
+    assert torch.all(out[rows] == 0) and torch.all(lse[rows] == -math.inf)
+    want = ref.attention(q.cpu(), cache.k_codes.cpu(), cache.v_codes.cpu(), cache.k_steps.cpu(), cache.v_steps.cpu(), s["cu"],
+                         torch.where(torch.arange(len(kv_lens)) == out_of, 0, fits["kv"]), s["table"], 0.125, True)[0]
+    err = (out.double().cpu() - want).abs()
+    assert torch.all(err <= 2.0 ** -6 * want.abs().amax())
