@@ -300,7 +300,7 @@ typedef struct {
 
 /* The requests of one step.  Request b owns rows [cu_q[b], cu_q[b+1]) of the call's token tensors (none is allowed); they
  * are the last ones of its kv_len[b] cached tokens, the new ones included.  Token j of its context lies in block
- * block_table[b, j / 64]. */
+ * block_table[b, j / 64].  Rows before cu_q[0] and from cu_q[n_requests] on belong to no request (a batch that is padded). */
 typedef struct {
   uint32_t struct_size; /* sizeof(tlq_kv_batch); checked */
   int32_t n_requests;   /* 1 .. 65535 */
@@ -325,7 +325,7 @@ size_t tlq_kv_workspace_bytes(const tlq_kv_cache* cache, const tlq_kv_batch* bat
  *     up to head_dim / 2; may be NULL for one axis).  n_axes is 1 or 3.
  *   q_out [T, n_heads, head_dim] bf16.
  *   k_values, v_values [T, n_kv_heads, head_dim] bf16 or NULL: the values that the new codes stand for, code * step (what
- *     later steps see; PassAct2 calibration propagates them).
+ *     later steps see; PassAct2 calibration propagates them).  Zeros for a token that has no place in the cache.
  * A block that already holds tokens of its request keeps the larger of its step and the new tokens' one; when it grows, the
  * older codes follow: c <- rint(c * old / new).  Codes saturate at +-127.  Values that are not finite take no part in a
  * step: an infinity saturates, a NaN becomes 0, and the status word is set to TLQ_ERR_NONFINITE.
@@ -340,7 +340,7 @@ int tlq_kv_store(const void* qkv, int64_t T, int64_t ld, int32_t n_heads, const 
  * causal != 0 over those up to the row's own place only.  Query head i reads kv head i / (n_heads / n_kv_heads).
  *   q [T, n_heads, head_dim] bf16, rows ldq elements apart (a multiple of 8); out [T, n_heads, head_dim] bf16;
  *   lse [T, n_heads] fp32 or NULL: ln sum_j exp(scale * q . k_j).  scale > 0 and finite.
- * A row that sees nothing (no cached token, or a place before the first) gets zeros and lse = -infinity.
+ * A row that sees nothing (no cached token, a place before the first, a row of no request) gets zeros and lse = -infinity.
  * Blocks that nothing was written to (codes and steps of zero) are keys and values of zero; value steps below 2^-80 count as 2^-80.
  */
 int tlq_kv_attention(const void* q, int64_t T, int64_t ldq, int32_t n_heads, const tlq_kv_cache* cache,

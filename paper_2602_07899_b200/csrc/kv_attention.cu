@@ -200,10 +200,20 @@ kv_attention_kernel(const KvArgs a, const AttnArgs g) {
   auto count_units = [&](int b) { return units_of(a, load_request(a, b), kRows, max_rows).total; };
   auto workers_of = [&](long long all) { return min(all, (long long)gridDim.x); };
   long long total = 0;
-  if (!plan_items<kThreads>(a.B, count_units,
-                            [&](long long all) { return (long long)blockIdx.x < workers_of(all) ? all * blockIdx.x / workers_of(all) : -1LL; },
-                            sums, &found, total))
-    return;
+  const Padding pad = load_padding(a.cu_q, a.B, a.T);
+  const bool some = plan_items<kThreads>(a.B, count_units,
+                                         [&](long long all) { return (long long)blockIdx.x < workers_of(all) ? all * blockIdx.x / workers_of(all) : -1LL; },
+                                         sums, &found, total);
+  if (pad.before > 0 || pad.after < a.T) {               // rows of no request see nothing
+    const int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x, n = (int64_t)gridDim.x * kThreads, pieces = (int64_t)a.n_heads * D / 8;
+    zero_rows(g.out, 0, pad.before, pieces, t, n);
+    zero_rows(g.out, pad.after, a.T, pieces, t, n);
+    if (g.lse != nullptr) {
+      for (int64_t i = t; i < (int64_t)pad.before * a.n_heads; i += n) g.lse[i] = -INFINITY;
+      for (int64_t i = (int64_t)pad.after * a.n_heads + t; i < a.T * a.n_heads; i += n) g.lse[i] = -INFINITY;
+    }
+  }
+  if (!some) return;
   const long long workers = workers_of(total);
   const long long u_begin = total * blockIdx.x / workers, u_end = total * (blockIdx.x + 1) / workers;
 

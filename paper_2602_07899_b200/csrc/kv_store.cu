@@ -159,6 +159,30 @@ __device__ __forceinline__ int to_code(float x, float step, float inv) {
 }
 
 constexpr int kQueryWaves = 24;                      // CTAs per SM of those that stream queries
+// Values of tokens that have no codes.  Not inlined, and with arguments by value: the loops of the kernel have no registers to spare.
+// Those of one head, tokens [from, from + count):
+template <int D>
+__device__ __noinline__ void no_values(uint16_t* k, uint16_t* v, int n_kv, int h, int64_t from, int count) {
+  for (int i = threadIdx.x; i < count * (D / 8); i += kStoreThreads) {
+    const int64_t at = ((from + i / (D / 8)) * n_kv + h) * (D / 8) + i % (D / 8);
+    if (k != nullptr) reinterpret_cast<uint4*>(k)[at] = make_uint4(0, 0, 0, 0);
+    if (v != nullptr) reinterpret_cast<uint4*>(v)[at] = make_uint4(0, 0, 0, 0);
+  }
+}
+// Those of the rows of no request, by CTAs of their own where values are asked for.  (A look at the padding by those that stream queries,
+// ahead of their rows or behind them, costs the 16384-token prompt 2 to 5 us of 150.)
+constexpr unsigned kPadCtas = 4;
+template <int D>
+__device__ __noinline__ void no_rows(const int32_t* cu_q, int B, int64_t T, uint16_t* k, uint16_t* v, int n_kv) {
+  const Padding pad = load_padding(cu_q, B, T);
+  const int64_t t = (int64_t)(gridDim.x - 1 - blockIdx.x) * kStoreThreads + threadIdx.x, n = (int64_t)kPadCtas * kStoreThreads;
+  for (uint16_t* p : {k, v})
+    if (p != nullptr) {
+      zero_rows(p, 0, pad.before, (int64_t)n_kv * D / 8, t, n);
+      zero_rows(p, pad.after, T, (int64_t)n_kv * D / 8, t, n);
+    }
+}
+
 constexpr int kSweepsQ = 2;                          // sweeps of a CTA over query rows whose loads are under way at once
 constexpr int kPitch = kKvBlock + 4;                 // bytes of a channel in `turned`: neighbouring channels in other banks
 
@@ -171,6 +195,10 @@ kv_store_kernel(const KvArgs a, const StoreArgs g) {
   const int l = threadIdx.x % kLanes, row = threadIdx.x / kLanes;
   const bool turn = g.rope.positions != nullptr;
   after_previous();
+  if (blockIdx.x >= g.kv_ctas + g.q_ctas) {          // padding
+    no_rows<D>(a.cu_q, a.B, a.T, g.k_values, g.v_values, a.n_kv);
+    return;
+  }
 
   // The two kinds are mixed: those of the cache part spend their time in a chain of dependent steps, those of the queries
   // wait for memory.
@@ -267,18 +295,23 @@ kv_store_kernel(const KvArgs a, const StoreArgs g) {
   if (!locate_item<kStoreThreads>(a.B, turn_of / (unsigned)a.n_kv, blocks_of, sums, &found)) return;
   const Request req = load_request(a, found.request);
   const int begin = req.kv - req.q_len;              // place of the request's first new token
-  if (begin < 0 && threadIdx.x == 0) report_status(a.hdr, TLQ_ERR_SHAPE, 202);
+  if (begin < 0 && found.rest == 0) {                // fewer cached tokens than new ones, or a request that is left out
+    if (threadIdx.x == 0) report_status(a.hdr, TLQ_ERR_SHAPE, 202);
+    no_values<D>(g.k_values, g.v_values, a.n_kv, h, req.q0, min(-begin, req.q_len));
+  }
   if (req.kv < 1) return;
   const int blk = max(begin, 0) / kKvBlock + (int)found.rest;
   const int p0 = max(max(begin, 0), blk * kKvBlock); // places [p0, p1) of the new tokens in this block
   const int p1 = min(req.kv, (blk + 1) * kKvBlock);
+  const int n_new = p1 - p0;
+  const int64_t tok0 = (int64_t)req.q0 + (p0 - begin);
   const int phys = a.block_table[(int64_t)found.request * a.max_blocks + blk];
   if (phys < 0 || phys >= a.n_blocks) {
     if (threadIdx.x == 0) report_status(a.hdr, TLQ_ERR_SHAPE, 203);
+    no_values<D>(g.k_values, g.v_values, a.n_kv, h, tok0, n_new);
     return;
   }
-  const int off0 = p0 - blk * kKvBlock, n_new = p1 - p0;
-  const int64_t tok0 = (int64_t)req.q0 + (p0 - begin);
+  const int off0 = p0 - blk * kKvBlock;
 
   Raw kraw[kSweeps], vraw[kSweeps];
 #pragma unroll
@@ -431,15 +464,16 @@ int launch_kv_store(const uint16_t* qkv, int64_t ld, int head_dim, const KvArgs&
   if (sms <= 0) return TLQ_ERR_CUDA;
   int64_t q_ctas = ceil_div(a.T * a.n_heads, (int64_t)kSweepsQ * kStoreThreads / (head_dim / 16));
   if (q_ctas > (int64_t)sms * kQueryWaves) q_ctas = (int64_t)sms * kQueryWaves;
-  if (blocks * a.n_kv + q_ctas > 0x7FFFFFFFLL) return TLQ_ERR_SHAPE;
+  if (blocks * a.n_kv + q_ctas + kPadCtas > 0x7FFFFFFFLL) return TLQ_ERR_SHAPE;
   g.kv_ctas = (unsigned)(blocks * a.n_kv);
   g.q_ctas = (unsigned)q_ctas;
   const unsigned grid = g.kv_ctas + (unsigned)q_ctas;
   // Mixed when the cache part alone is more than the GPU holds at once (16384-token prompt, 64 / 8 heads: 152 us mixed, 171
   // with the cache part first); otherwise its chain is the longest and goes first (six ragged prompts: 12.5 us against 14.1).
   g.period = (int64_t)g.kv_ctas > 3 * (int64_t)sms ? grid / g.kv_ctas : 1;
-  return head_dim == 128 ? launch_next(kv_store_kernel<128>, dim3(grid), kStoreThreads, 0, 1, st, a, g)
-                         : launch_next(kv_store_kernel<64>, dim3(grid), kStoreThreads, 0, 1, st, a, g);
+  const dim3 all(grid + (k_values != nullptr || v_values != nullptr ? kPadCtas : 0u));
+  return head_dim == 128 ? launch_next(kv_store_kernel<128>, all, kStoreThreads, 0, 1, st, a, g)
+                         : launch_next(kv_store_kernel<64>, all, kStoreThreads, 0, 1, st, a, g);
 }
 
 }  // namespace tlq

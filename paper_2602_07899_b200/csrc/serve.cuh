@@ -47,6 +47,21 @@ __device__ __forceinline__ Request load_request(const KvArgs& a, int b) {
   return r;
 }
 
+// Rows of the token tensors that belong to no request: those before the first one's and after the last one's (padding).
+struct Padding {
+  int before, after;          // rows [0, before) and [after, T)
+};
+__device__ __forceinline__ Padding load_padding(const int32_t* cu_q, int B, int64_t T) {
+  Padding p;
+  p.before = max(0, min(cu_q[0], (int)T));
+  p.after = max(p.before, min(cu_q[B], (int)T));
+  return p;
+}
+// Rows [from, to) of `pieces` 16-byte pieces each become zeros; thread number t of n does its share.
+__device__ __forceinline__ void zero_rows(void* p, int64_t from, int64_t to, int64_t pieces, int64_t t, int64_t n) {
+  for (int64_t i = from * pieces + t; i < to * pieces; i += n) reinterpret_cast<uint4*>(p)[i] = make_uint4(0, 0, 0, 0);
+}
+
 // Inclusive scan of one value per thread of a block of kThreads; `sums` is kThreads / 32 words of shared memory.
 template <int kThreads>
 __device__ __forceinline__ long long block_scan(long long v, long long* sums, long long& total) {

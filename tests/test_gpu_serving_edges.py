@@ -131,6 +131,57 @@ def dirty(*shapes):
     del held
 
 
+@pytest.mark.parametrize("big", [False, True])
+@pytest.mark.parametrize("before,after", [(0, 5), (3, 0), (70, 131), (1, 1)])
+def test_rows_of_no_request_are_empty_rows(tlq, before, after, big):
+    """Token tensors padded at either end: attention gives zeros and -infinity there, the store zeros for keys and values."""
+    hk, d, heads = 2, 128, 6
+    q_lens, kv_lens = [1, 40, 0, 3] + [BIG[0]] * big, [90, 300, 64, 3] + [BIG[1]] * big
+    s = make_batch(63, q_lens, kv_lens, hk, d)
+    T = before + s["T"] + after
+    rows = slice(before, before + s["T"])
+    q = torch.randn(T, heads, d, generator=gen(4)).bfloat16().cuda()
+    cache, batch = on_gpu(tlq, s)
+    want, want_lse = tlq.tlq_kv_attention(q[rows], cache, batch, 0.1, want_lse=True)
+    padded = tlq.KvBatch((s["cu"] + before).cuda(), batch.kv_len, batch.block_table, s["q_max"])
+    ws = tlq.kv_workspace(cache, heads, T, padded)
+    dirty(((T, heads, d), torch.bfloat16), ((T, heads), torch.float32))
+    out, lse = tlq.tlq_kv_attention(q, cache, padded, 0.1, want_lse=True, workspace=ws)
+    none = torch.ones(T, dtype=torch.bool, device="cuda")
+    none[rows] = False
+    assert torch.all(out[none] == 0) and torch.all(lse[none] == -math.inf)
+    assert torch.equal(out[rows], want) and torch.equal(lse[rows], want_lse)
+    # the store
+    qkv = torch.randn(T, (heads + 2 * hk) * d, generator=gen(5)).bfloat16().cuda()
+    wq, wk, wv = tlq.tlq_kv_store(qkv[rows], heads, on_gpu(tlq, s)[0], batch, want_values=True)
+    cache = on_gpu(tlq, s)[0]
+    dirty(((T, heads, d), torch.bfloat16), ((T, hk, d), torch.bfloat16), ((T, hk, d), torch.bfloat16))
+    gq, gk, gv = tlq.tlq_kv_store(qkv, heads, cache, padded, want_values=True, workspace=ws)
+    assert torch.equal(gq[rows], wq) and torch.equal(gk[rows], wk) and torch.equal(gv[rows], wv)
+    assert torch.all(gk[none] == 0) and torch.all(gv[none] == 0) and torch.isfinite(gq.float()).all()
+    assert tlq.tlq_read_status(ws) == tlq.OK
+
+
+def test_store_values_of_tokens_without_a_place_are_zeros(tlq):
+    """More new tokens than cached ones (the first have no place), a block outside of the cache, a length beyond the table."""
+    hk, d, heads = 2, 64, 4
+    s = make_batch(66, [5, 70, 3, 9], [2, 100, 10, 9], hk, d, pad=0)
+    s["table"][1, 1] = 1 << 20
+    s["kv"][3] = s["table"].shape[1] * BLOCK + 1
+    gone = torch.zeros(s["T"], dtype=torch.bool, device="cuda")
+    gone[:3] = True                                               # places -3 .. -1
+    gone[5 + 34:5 + 70] = True                                    # places 64 .. 99 of request 1
+    gone[5 + 70 + 3:] = True
+    cache, batch = on_gpu(tlq, s)
+    ws = tlq.kv_workspace(cache, heads, s["T"], batch)
+    qkv = (torch.randn(s["T"], (heads + 2 * hk) * d, generator=gen(5)).abs() + 1).bfloat16().cuda()
+    dirty(((s["T"], heads, d), torch.bfloat16), ((s["T"], hk, d), torch.bfloat16), ((s["T"], hk, d), torch.bfloat16))
+    _, k, v = tlq.tlq_kv_store(qkv, heads, cache, batch, want_values=True, workspace=ws)
+    assert tlq.tlq_read_status(ws) == tlq.ERR_SHAPE
+    for x in (k, v):
+        assert torch.all(x[gone] == 0) and torch.all(x[~gone].float().abs().amax(-1) > 0.5) and torch.isfinite(x.float()).all()
+
+
 @pytest.mark.parametrize("what", ["length", "negative", "rows"])
 @pytest.mark.parametrize("big", [False, True])
 def test_requests_that_do_not_fit_are_left_out_whole(tlq, what, big):
