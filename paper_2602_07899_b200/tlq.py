@@ -331,7 +331,8 @@ def tlq_apply_layer(X: torch.Tensor, W: torch.Tensor, s: Optional[torch.Tensor],
 
 # ----------------------------------------------------------------------------------------------- serving
 # What runs a calibrated layer: see the serving part of include/tlq.h.  These calls never synchronise; read the status
-# word of their workspace with tlq_read_status when a step's results are fetched.
+# word of their workspace with tlq_read_status when a step's results are fetched.  With `stream` given, the results belong to that
+# stream, as if the call had been made with it current.
 
 
 _I8, _I32, _F32, _BF16 = torch.int8, torch.int32, torch.float32, torch.bfloat16
@@ -438,12 +439,13 @@ def _by_address(name: str):
 _kv_store, _kv_attention = _by_address("tlq_kv_store"), _by_address("tlq_kv_attention")
 
 
-def _workspace_on(stream, make, *args) -> torch.Tensor:
-    """A workspace for one call, zeroed on the stream that the call runs on."""
+def _made_on(stream, make, *args, **kw) -> torch.Tensor:
+    """A tensor of one call, made (and a workspace zeroed) on the stream that the call runs on: memory of another stream's pool may still
+    be in use there, and is given away there as soon as it is dropped."""
     if stream is None:
-        return make(*args)
+        return make(*args, **kw)
     with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))):
-        return make(*args)
+        return make(*args, **kw)
 
 
 @functools.lru_cache(maxsize=64)
@@ -484,9 +486,9 @@ def tlq_linear_i8(Xq: torch.Tensor, t: torch.Tensor, Wq: torch.Tensor, u: torch.
     _plain(workspace)
     _on_device("tlq_linear_i8", Xq, t, Wq, u, bias, workspace, out)
     if workspace is None:
-        workspace = _workspace_on(stream, linear_workspace, N, C1, C2, Xq.device)
+        workspace = _made_on(stream, linear_workspace, N, C1, C2, Xq.device)
     if out is None:
-        out = Xq.new_empty((N, C2), dtype=_BF16)
+        out = _made_on(stream, Xq.new_empty, (N, C2), dtype=_BF16)
     else:
         _typed(out, _BF16, (N, C2), "out")
     status = lib.tlq_linear_i8(Xq.data_ptr(), t.data_ptr(), N, C1, Wq.data_ptr(), u.data_ptr(), C2,
@@ -528,11 +530,11 @@ def tlq_kv_store(qkv: torch.Tensor, n_heads: int, cache: KvCache, batch: KvBatch
     _plain(workspace)
     _on_device("tlq_kv_store", qkv, cache, batch, positions, None if positions is None else cos_sin, q_norm, k_norm, workspace)
     if workspace is None:
-        workspace = _workspace_on(stream, kv_workspace, cache, n_heads, T, batch)
-    q = qkv.new_empty((T, n_heads, d))
+        workspace = _made_on(stream, kv_workspace, cache, n_heads, T, batch)
+    q = _made_on(stream, qkv.new_empty, (T, n_heads, d))
     k = v = None
     if want_values:
-        k, v = qkv.new_empty((T, cache.n_kv_heads, d)), qkv.new_empty((T, cache.n_kv_heads, d))
+        k, v = (_made_on(stream, qkv.new_empty, (T, cache.n_kv_heads, d)) for _ in range(2))
     _check(_kv_store(qkv.data_ptr(), T, ld, n_heads, cache._p, batch._p,
                             None if positions is None else positions.data_ptr(), axes, sec,
                             None if cos_sin is None else cos_sin.data_ptr(), limit,
@@ -553,9 +555,9 @@ def tlq_kv_attention(q: torch.Tensor, cache: KvCache, batch: KvBatch, scale: flo
     _plain(workspace)
     _on_device("tlq_kv_attention", q, cache, batch, workspace)
     if workspace is None:
-        workspace = _workspace_on(stream, kv_workspace, cache, n_heads, T, batch)
-    out = q.new_empty((T, n_heads, d))
-    lse = q.new_empty((T, n_heads), dtype=_F32) if want_lse else None
+        workspace = _made_on(stream, kv_workspace, cache, n_heads, T, batch)
+    out = _made_on(stream, q.new_empty, (T, n_heads, d))
+    lse = _made_on(stream, q.new_empty, (T, n_heads), dtype=_F32) if want_lse else None
     _check(_kv_attention(q.data_ptr(), T, ldq, n_heads, cache._p, batch._p, scale, 1 if causal else 0,
                                 workspace.data_ptr(), workspace.numel(), out.data_ptr(),
                                 None if lse is None else lse.data_ptr(), _stream(stream)), "tlq_kv_attention")

@@ -228,3 +228,29 @@ def test_requests_that_do_not_fit_are_left_out_whole(tlq, what, big):
                          torch.where(torch.arange(len(kv_lens)) == out_of, 0, fits["kv"]), s["table"], 0.125, True)[0]
     err = (out.double().cpu() - want).abs()
     assert torch.all(err <= 2.0 ** -6 * want.abs().amax())
+
+
+def pool_of(t):
+    """Stream whose pool the memory of a tensor belongs to."""
+    for seg in torch.cuda.memory_snapshot():
+        if seg["address"] <= t.data_ptr() < seg["address"] + seg["total_size"]:
+            return seg["stream"]
+
+
+def test_results_belong_to_the_stream_that_writes_them(tlq):
+    """Memory from another stream's pool may still be in use there by what was queued before, and is given away again as soon as
+    that stream's owner drops it."""
+    side = torch.cuda.Stream()
+    s = make_batch(65, [1, 70], [90, 100], 2, 64)
+    cache, batch = on_gpu(tlq, s)
+    qkv = torch.randn(s["T"], 10 * 64, generator=gen(1)).bfloat16().cuda()
+    xq, wq = torch.zeros(64, 512, dtype=torch.int8, device="cuda"), torch.zeros(96, 512, dtype=torch.int8, device="cuda")
+    t, u = torch.ones(64, device="cuda"), torch.ones(96, device="cuda")
+    torch.cuda.synchronize()
+    for stream in (side, side.cuda_stream):
+        q, k, v = tlq.tlq_kv_store(qkv, 6, cache, batch, want_values=True, stream=stream)
+        out, lse = tlq.tlq_kv_attention(q, cache, batch, 0.1, want_lse=True, stream=stream)
+        y = tlq.tlq_linear_i8(xq, t, wq, u, stream=stream)
+        side.synchronize()
+        assert [pool_of(r) for r in (q, k, v, out, lse, y)] == [side.cuda_stream] * 6
+    assert pool_of(tlq.tlq_linear_i8(xq, t, wq, u)) == torch.cuda.current_stream().cuda_stream
