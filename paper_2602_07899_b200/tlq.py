@@ -160,13 +160,14 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 # the raw handle of the current stream, without a Stream object (a microsecond per call)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _stream(stream) -> Optional[int]:
+def _stream(stream, dev: Optional[int] = None) -> Optional[int]:
+    """`dev`: number of the current device, where the caller has asked for it."""
     if stream is None:
-        if _raw_stream is not None and _raw_device is not None:
-            return _raw_stream(_raw_device())
+        if _raw_stream is not None:
+            return _raw_stream(_raw_device() if dev is None else dev)
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
@@ -356,16 +357,11 @@ def _one_device(what: str, first, *rest) -> int:
 
 
 def _on_device(what: str, first, *rest) -> None:
-    """The kernels run on the current device, and a pointer to anywhere else is a memory fault there: refused here."""
+    """The kernels run on the current device, and a pointer to anywhere else is a memory fault there: refused here.  (The calls ask
+    what concerns them themselves first, which takes a microsecond less, and come here when something is wrong.)"""
     dev = _one_device(what, first, *rest)
-    if dev < 0 or dev != (torch.cuda.current_device() if _raw_device is None else _raw_device()):
+    if dev < 0 or dev != _raw_device():
         raise ValueError(f"{what}: tensors must lie on the current CUDA device, got {'host memory' if dev < 0 else f'device {dev}'}")
-
-
-def _plain(workspace: Optional[torch.Tensor]) -> None:
-    """Its number of elements is passed on as a number of bytes, which a view that repeats memory does not have."""
-    if workspace is not None and not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous")
 
 
 def _rows(t: torch.Tensor, what: str) -> int:
@@ -474,8 +470,8 @@ def tlq_linear_i8(Xq: torch.Tensor, t: torch.Tensor, Wq: torch.Tensor, u: torch.
     """Xq int8 [N,C1] with steps t [N], Wq int8 [C2,C1] with steps u [C2], bias bf16 [C2] or None -> bf16 [N,C2]."""
     N, C1 = Xq.shape
     C2, W1 = Wq.shape
-    if (W1 != C1 or Xq.dtype is not _I8 or Wq.dtype is not _I8 or t.dtype is not _F32 or u.dtype is not _F32 or t.ndim != 1
-            or u.ndim != 1 or t.numel() != N or u.numel() != C2 or not Xq.is_contiguous() or not Wq.is_contiguous()
+    if (W1 != C1 or Xq.dtype is not _I8 or Wq.dtype is not _I8 or t.dtype is not _F32 or u.dtype is not _F32
+            or t.shape != (N,) or u.shape != (C2,) or not Xq.is_contiguous() or not Wq.is_contiguous()
             or not t.is_contiguous() or not u.is_contiguous()):
         _typed(Xq, _I8, (N, C1), "Xq")
         _typed(Wq, _I8, (C2, C1), "Wq")
@@ -483,17 +479,23 @@ def tlq_linear_i8(Xq: torch.Tensor, t: torch.Tensor, Wq: torch.Tensor, u: torch.
         _typed(u, _F32, (C2,), "u")
     if bias is not None:
         _typed(bias, _BF16, (C2,), "bias")
-    _plain(workspace)
-    _on_device("tlq_linear_i8", Xq, t, Wq, u, bias, workspace, out)
+    # (a workspace's elements count as bytes: a view that repeats memory has fewer)
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    dev = Xq.get_device()
+    if (dev < 0 or dev != _raw_device() or t.get_device() != dev or Wq.get_device() != dev or u.get_device() != dev
+            or bias is not None and bias.get_device() != dev or workspace is not None and workspace.get_device() != dev
+            or out is not None and out.get_device() != dev):
+        _on_device("tlq_linear_i8", Xq, t, Wq, u, bias, workspace, out)
     if workspace is None:
         workspace = _made_on(stream, linear_workspace, N, C1, C2, Xq.device)
     if out is None:
-        out = _made_on(stream, Xq.new_empty, (N, C2), dtype=_BF16)
+        out = Xq.new_empty((N, C2), dtype=_BF16) if stream is None else _made_on(stream, Xq.new_empty, (N, C2), dtype=_BF16)
     else:
         _typed(out, _BF16, (N, C2), "out")
     status = lib.tlq_linear_i8(Xq.data_ptr(), t.data_ptr(), N, C1, Wq.data_ptr(), u.data_ptr(), C2,
                                None if bias is None else bias.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                               out.data_ptr(), _stream(stream))
+                               out.data_ptr(), _stream(stream, dev))
     if status:
         raise TlqError(status, "tlq_linear_i8")
     return out
@@ -527,20 +529,27 @@ def tlq_kv_store(qkv: torch.Tensor, n_heads: int, cache: KvCache, batch: KvBatch
         _typed(q_norm, _BF16, (d,), "q_norm")
     if k_norm is not None:
         _typed(k_norm, _BF16, (d,), "k_norm")
-    _plain(workspace)
-    _on_device("tlq_kv_store", qkv, cache, batch, positions, None if positions is None else cos_sin, q_norm, k_norm, workspace)
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    dev = qkv.get_device()
+    if (dev < 0 or dev != _raw_device() or cache._device != dev or batch._device != dev
+            or positions is not None and (positions.get_device() != dev or cos_sin.get_device() != dev)
+            or q_norm is not None and q_norm.get_device() != dev or k_norm is not None and k_norm.get_device() != dev
+            or workspace is not None and workspace.get_device() != dev):
+        _on_device("tlq_kv_store", qkv, cache, batch, positions, cos_sin, q_norm, k_norm, workspace)
     if workspace is None:
         workspace = _made_on(stream, kv_workspace, cache, n_heads, T, batch)
-    q = _made_on(stream, qkv.new_empty, (T, n_heads, d))
+    empty = qkv.new_empty if stream is None else functools.partial(_made_on, stream, qkv.new_empty)
+    q = empty((T, n_heads, d))
     k = v = None
     if want_values:
-        k, v = (_made_on(stream, qkv.new_empty, (T, cache.n_kv_heads, d)) for _ in range(2))
+        k, v = empty((T, cache.n_kv_heads, d)), empty((T, cache.n_kv_heads, d))
     _check(_kv_store(qkv.data_ptr(), T, ld, n_heads, cache._p, batch._p,
                             None if positions is None else positions.data_ptr(), axes, sec,
                             None if cos_sin is None else cos_sin.data_ptr(), limit,
                             None if q_norm is None else q_norm.data_ptr(), None if k_norm is None else k_norm.data_ptr(),
                             eps, q.data_ptr(), None if k is None else k.data_ptr(), None if v is None else v.data_ptr(),
-                            workspace.data_ptr(), workspace.numel(), _stream(stream)), "tlq_kv_store")
+                            workspace.data_ptr(), workspace.numel(), _stream(stream, dev)), "tlq_kv_store")
     return q, k, v
 
 
@@ -552,15 +561,20 @@ def tlq_kv_attention(q: torch.Tensor, cache: KvCache, batch: KvBatch, scale: flo
     if d != cache.head_dim:
         raise ValueError("q and the cache differ in head_dim")
     ldq = _rows(q, "q")
-    _plain(workspace)
-    _on_device("tlq_kv_attention", q, cache, batch, workspace)
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    dev = q.get_device()
+    if (dev < 0 or dev != _raw_device() or cache._device != dev or batch._device != dev
+            or workspace is not None and workspace.get_device() != dev):
+        _on_device("tlq_kv_attention", q, cache, batch, workspace)
     if workspace is None:
         workspace = _made_on(stream, kv_workspace, cache, n_heads, T, batch)
-    out = _made_on(stream, q.new_empty, (T, n_heads, d))
-    lse = _made_on(stream, q.new_empty, (T, n_heads), dtype=_F32) if want_lse else None
+    empty = q.new_empty if stream is None else functools.partial(_made_on, stream, q.new_empty)
+    out = empty((T, n_heads, d))
+    lse = empty((T, n_heads), dtype=_F32) if want_lse else None
     _check(_kv_attention(q.data_ptr(), T, ldq, n_heads, cache._p, batch._p, scale, 1 if causal else 0,
                                 workspace.data_ptr(), workspace.numel(), out.data_ptr(),
-                                None if lse is None else lse.data_ptr(), _stream(stream)), "tlq_kv_attention")
+                                None if lse is None else lse.data_ptr(), _stream(stream, dev)), "tlq_kv_attention")
     return out, lse
 
 
