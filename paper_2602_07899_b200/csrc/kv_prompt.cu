@@ -7,8 +7,8 @@
 // tile and cache block (64 keys): S = q K^T (tcgen05, f16 x f16 -> f32, tensor memory), a thread per row takes the maximum
 // and the exponentials of its row from tensor memory and writes P over S as f16, O += P V with P from tensor memory.  S has
 // two buffers per tile: while a row's exponentials of one block are taken, the tensor core finishes P V of the block before
-// and S of the block after it.  The output sum is rescaled only when the maximum of a row has grown by more than 4 (a factor
-// of 16 in p): p is kept as 2^11 p, so that it fits 16 bits either way.
+// and S of the block after it.  The output sum is rescaled only when the maximum of a row has grown by more than 4.9 (a
+// factor of 30 in p): p is kept as 2^11 p, and 2^(11 + 4.9) = 61100 still is a 16-bit float (65504 at most).
 //   warps 0..3, 4..7  softmax of tile 0, 1: a thread is a row (and its accumulator lane)
 //   warps 8..11       copy the codes of keys and values to shared memory two blocks ahead, turn them into f16 and lay them out
 //                     for the tensor core (128-byte swizzle); four stages
@@ -40,6 +40,7 @@ constexpr int kThreads = 512;                              // four groups of fou
 // registers of a thread of each role: 2 x 176 + 72 + 88 = 4 x 128, what the block is launched with
 constexpr int kSoftRegs = 176, kLoadRegs = 72, kIssueRegs = 88;
 constexpr float kShift = kPromptShift, kGrow = 4.9f;
+static_assert(kShift + kGrow < 15.99f, "the largest p has to fit a 16-bit float");
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kUnit = 16777216.f;                        // 2^24
 constexpr int kMinTiles = 6;                               // blocks of a CTA's part, at least (512 tokens x 512: 34 us, 37 with 12)

@@ -13,7 +13,7 @@
 //
 // Bound: bytes.  The rows are read once and everything is kept in registers between the maximum and the codes.  One CTA
 // owns a cache block of one head (its tokens lie in one request), because its step needs all of them; the remaining CTAs
-// stream query rows, four per thread group at once.  Values lie channel by token in the cache (what a matrix instruction over
+// stream query rows, two per thread group at once.  Values lie channel by token in the cache (what a matrix instruction over
 // tokens reads), so a CTA turns its 64 x D bytes in shared memory and writes rows of 64 bytes.  Measured: 16384 tokens, 64 + 8 + 8
 // heads of 128 channels with norms (713 MB) 151 us, 4.7 TB/s, the schedulers busy 60 % of the time with conversions and rotations;
 // 6 ragged prompts (29 MB) 12.4 us; 32 requests of one token 5.4 us, latency.
