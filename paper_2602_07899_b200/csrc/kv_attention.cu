@@ -36,7 +36,6 @@ namespace {
 constexpr int kWarps = kSplitWarps;
 constexpr int kThreads = kWarps * 32;
 constexpr float kShift = kFewShift;       // p is kept as 2^kShift * p in 16 bits
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttnArgs {
   const uint16_t* q;
@@ -60,25 +59,6 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
-// Four 8-bit codes to two pairs of f16.  Keys: code + 128 in the lowest byte of a 16-bit float is the (subnormal, exact)
-// number (code + 128) 2^-24.  Values: exactly the code, as 1024 + (code + 128) by byte placement, minus 1152; a sum of
-// p (code + 128) less 128 sum(p) would leave a rounding of 2^-23 x 128 in channels whose own values are small.
-constexpr float kUnit = 16777216.f;       // 2^24
-__device__ __forceinline__ void keys_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  const uint32_t x = w ^ 0x80808080u;
-  lo = __byte_perm(x, 0u, 0x4140);
-  hi = __byte_perm(x, 0u, 0x4342);
-}
-__device__ __forceinline__ void values_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  const uint32_t x = w ^ 0x80808080u;
-  const uint32_t a = __byte_perm(x, 0x64646464u, 0x4140), b = __byte_perm(x, 0x64646464u, 0x4342);
-  const __half2 off = __floats2half2_rn(1152.f, 1152.f);
-  const __half2 ra = __hsub2(*reinterpret_cast<const __half2*>(&a), off);
-  const __half2 rb = __hsub2(*reinterpret_cast<const __half2*>(&b), off);
-  lo = *reinterpret_cast<const uint32_t*>(&ra);
-  hi = *reinterpret_cast<const uint32_t*>(&rb);
-}
-
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                         uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -89,15 +69,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
-}
-__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
-  const __half2 v = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
 }
 
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }

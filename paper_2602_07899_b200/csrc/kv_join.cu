@@ -18,7 +18,6 @@ namespace tlq {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr float kLn2 = 0.6931471805599453f;
 
 struct JoinArgs {
   uint16_t* out;
@@ -26,11 +25,6 @@ struct JoinArgs {
   KvSplit split;
 };
 
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ PartNote load_note(const PartNote* p) {
   union { int4 v[2]; PartNote n; } u;
   u.v[0] = load_far(reinterpret_cast<const int4*>(p));

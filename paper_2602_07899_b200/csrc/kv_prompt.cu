@@ -41,8 +41,6 @@ constexpr int kThreads = 512;                              // four groups of fou
 constexpr int kSoftRegs = 176, kLoadRegs = 72, kIssueRegs = 88;
 constexpr float kShift = kPromptShift, kGrow = 4.9f;
 static_assert(kShift + kGrow < 15.99f, "the largest p has to fit a 16-bit float");
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kUnit = 16777216.f;                        // 2^24
 constexpr int kMinTiles = 6;                               // blocks of a CTA's part, at least (512 tokens x 512: 34 us, 37 with 12)
 constexpr int kItemCost = 8;                               // what an item costs beside its blocks, in blocks (8192 tokens: 555, 564 with 12)
 
@@ -84,15 +82,6 @@ constexpr int kRaw = 2;                                    // blocks whose codes
 template <int D>
 constexpr size_t kSmem = 1024 + 2 * kQBytes<D> + kStages * (kKBytes<D> + kVBytes<D>) + kRaw * kRawBytes<D>;
 
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
-  const __half2 v = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
@@ -116,22 +105,6 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
                : "=r"(is) : "r"(bar), "r"(parity) : "memory");
   return is != 0;
 }
-// (code + 128) 2^-24 as f16, and exactly the code: see kv_attention.cu
-__device__ __forceinline__ void keys_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  const uint32_t x = w ^ 0x80808080u;
-  lo = __byte_perm(x, 0u, 0x4140);
-  hi = __byte_perm(x, 0u, 0x4342);
-}
-__device__ __forceinline__ void values_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  const uint32_t x = w ^ 0x80808080u;
-  const uint32_t a = __byte_perm(x, 0x64646464u, 0x4140), b = __byte_perm(x, 0x64646464u, 0x4342);
-  const __half2 off = __floats2half2_rn(1152.f, 1152.f);
-  const __half2 ra = __hsub2(*reinterpret_cast<const __half2*>(&a), off);
-  const __half2 rb = __hsub2(*reinterpret_cast<const __half2*>(&b), off);
-  lo = *reinterpret_cast<const uint32_t*>(&ra);
-  hi = *reinterpret_cast<const uint32_t*>(&rb);
-}
-
 __device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   ptx::mma_bf16_ss(d, a, b, idesc, accumulate);            // kind::f16 covers both types; the descriptor names f16
 }

@@ -167,6 +167,36 @@ __device__ __forceinline__ bool is_prompt_work(const KvArgs& a, int causal, long
   return all >= kPromptPairs;
 }
 
+// ---------------------------------------------------------------------------------------------- numbers of the attention kernels
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+// Four 8-bit codes to two pairs of f16.  Keys: code + 128 in the lowest byte of a 16-bit float is the (subnormal, exact)
+// number (code + 128) 2^-24.  Values: exactly the code, as 1024 + (code + 128) by byte placement, minus 1152; a sum of
+// p (code + 128) less 128 sum(p) would leave a rounding of 2^-23 x 128 in channels whose own values are small.
+constexpr float kUnit = 16777216.f;       // 2^24
+__device__ __forceinline__ void keys_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  const uint32_t x = w ^ 0x80808080u;
+  lo = __byte_perm(x, 0u, 0x4140);
+  hi = __byte_perm(x, 0u, 0x4342);
+}
+__device__ __forceinline__ void values_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  const uint32_t x = w ^ 0x80808080u;
+  const uint32_t a = __byte_perm(x, 0x64646464u, 0x4140), b = __byte_perm(x, 0x64646464u, 0x4342);
+  const __half2 off = __floats2half2_rn(1152.f, 1152.f);
+  const __half2 ra = __hsub2(*reinterpret_cast<const __half2*>(&a), off);
+  const __half2 rb = __hsub2(*reinterpret_cast<const __half2*>(&b), off);
+  lo = *reinterpret_cast<const uint32_t*>(&ra);
+  hi = *reinterpret_cast<const uint32_t*>(&rb);
+}
+
 // ---------------------------------------------------------------------------------------------- launches
 // Kernels of these operators follow one another in every layer, most of them a few microseconds long.  They are launched
 // so that a kernel's blocks may come up while the one before it on the stream still runs (programmatic dependent
