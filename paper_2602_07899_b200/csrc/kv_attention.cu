@@ -25,8 +25,9 @@
 // Bound: the cache's bytes, 16 KB per block and kv head at 128 channels.  The ring holds 24 KB per warp, 192 KB per SM: at
 // 44 GB/s and about 2 us per SM some 90 KB have to be under way all the time.  Measured: 64 requests of up to 32761 tokens,
 // 4 kv heads (370 MB) 80 us, 57 of them from the first to the last block (6.5 TB/s); one token over 131071 with 8 kv heads
-// (268 MB) 59 us, 42 for the blocks; the rest is the launch, the plan (2 us), the end of the grid and the join.  One token
-// over 100: 8 us.  Items of 16 rows (16 columns) cost twice the matrix work: 320 rows in 8 requests x 8192 keys would take 101.
+// (268 MB) 60 us, 42 for the blocks; the rest is the launch, the plan (2 us), the end of the grid and the join.  One token
+// over 100: 8.4 us.  Items of 16 rows (16 columns) cost twice the matrix work: 8 requests of one token over 8192 keys take 27 us,
+// 8 of 5 tokens (35 rows, three items for each of 4 kv heads) 56.
 #include "serve.cuh"
 #include "umma.cuh"
 
@@ -78,12 +79,12 @@ __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 
 constexpr int kItemUnits = 1;
 // Small items are not cut: the warp that has the unit before their blocks takes them all, and nothing has to be joined (nor the
 // join launched, where no request can have more blocks: that alone is 5 us).  A single request of 500 tokens (8 blocks) is
-// answered in 12 us cut and in 17 whole; 64 of them, an item or more for every CTA, in 27 cut and in 24 whole, 64 of 300 tokens
-// in 22 and 14.
+// answered in 12 us cut and in 17 whole; 64 of them, an item or more for every CTA, in 27 cut and in 25 whole, 64 of 300 tokens
+// in 23 and 14, 64 of 100 in 21 and 10.
 constexpr int kWhole = 4, kWholeBusy = 8;                  // blocks, at most; where there may be an item for every CTA
 // The units go to as many CTAs as there are, then to warps that get about this many: every part has to be joined.  One token
-// over 60000 with 2 kv heads 37, 31 and 29 us for 2, 3 and 4, over 16384 with 8 25, 22 and 22; 9 tokens over 4096 with 4 kv heads
-// 20, 21 and 23, 16 requests of 700 tokens 16, 19 and 18.
+// over 60000 with 2 kv heads 37, 31 and 29 us for 2, 3 and 4, over 16384 with 8 25, 22 and 23; 9 tokens over 4096 with 4 kv heads
+// 20, 21 and 24, 16 requests of 700 tokens 16, 19 and 19, 64 of 500 tokens 25, 25 and 20.
 constexpr int kMinUnits = 3;
 struct Units {
   int row_tiles, blocks;

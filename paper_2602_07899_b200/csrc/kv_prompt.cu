@@ -20,12 +20,13 @@
 // Work is cut as in the few-row kernel: items (row tiles of a kv head) lie on one line, weighted by their cached tokens, every
 // CTA takes an equal part of it; an item that is cut leaves partial sums, which kv_join.cu joins.
 //
-// Bound: 4 D flops per visible pair on the tensor core.  Measured: 8192 tokens, 28 heads over 4 kv heads 553 to 558 us, 870 TFLOP/s
-// (292 us at the 1646 TFLOP/s of a large bf16 product); the tensor pipe is active 37 % of the time, the exponential unit 39 %.  A
-// block takes about 2200 cycles for 256 rows.  Neither unit bounds it alone: without exponentials 569, without products 488,
-// without fetching codes 521, without all three 298; what remains is the exchange between the roles, and 8 blocks' worth of time
-// around every item.  Tried and slower: taking the exponentials from the maximum of the blocks before while this block's is found
-// (581), the next block's scores loaded before P is handed over (588), two pieces of O rescaled at once (563).
+// Bound: 4 D flops per visible pair on the tensor core.  Measured: 8192 tokens, 28 heads over 4 kv heads 558 to 562 us, 860 TFLOP/s
+// (292 us at the 1646 TFLOP/s of a large bf16 product); the tensor pipe is active 42 % of the time, the exponential unit 43 %.  A
+// block takes about 2200 cycles for 256 rows.  Neither unit bounds it: 554 us without exponentials, 548 without products, 543 without
+// both, 519 without the codes' layout too.  What remains is the chain of a block, scores -> maximum -> p -> product, across the
+// barriers between the roles, and 8 blocks' worth of time around every item.  Tried on earlier states of this kernel, and slower:
+// taking the exponentials from the maximum of the blocks before while this block's is found, the next block's scores loaded before
+// P is handed over, two pieces of O rescaled at once.
 #include <type_traits>
 
 #include "serve.cuh"
@@ -41,8 +42,8 @@ constexpr int kThreads = 512;                              // four groups of fou
 constexpr int kSoftRegs = 176, kLoadRegs = 72, kIssueRegs = 88;
 constexpr float kShift = kPromptShift, kGrow = 4.9f;
 static_assert(kShift + kGrow < 15.99f, "the largest p has to fit a 16-bit float");
-constexpr int kMinTiles = 6;                               // blocks of a CTA's part, at least (512 tokens x 512: 34 us, 37 with 12)
-constexpr int kItemCost = 8;                               // what an item costs beside its blocks, in blocks (8192 tokens: 555, 564 with 12)
+constexpr int kMinTiles = 6;                               // blocks of a CTA's part, at least (512 tokens x 512: 38 us, 40 with 12)
+constexpr int kItemCost = 8;                               // what an item costs beside its blocks, in blocks (8192 tokens: 562, 572 with 12)
 
 struct PromptArgs {
   const uint16_t* q;

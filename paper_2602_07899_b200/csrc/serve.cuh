@@ -138,12 +138,15 @@ __device__ __forceinline__ bool plan_items(int B, F count, G target_of, long lon
 constexpr int kPromptRows = 32;           // requests with at least this many query rows per kv head go to it ...
 // ... if such requests have this many pairs of a row and a key, every row counted with 256 keys on top (the few-row kernel
 // works on 16 rows at a time and pays for each such item once), requests of fewer than 64 rows by a third (the prompt kernel
-// works on 128 rows at least).  The prompt kernel and its join take 20 to 25 us however little there is to do, the few-row
-// kernel 10, but that one gets no more than 0.25 M pairs done in a us.  Measured, few-row against prompt kernel:
-// 126 rows x 4096 keys x 4 kv heads (2.2 M) 29 : 41 us, 336 x 2000 x 4 (3.0 M) 32 : 37, prompts of 512 tokens with 512 rows x 8
-// (2.1 M) 23 : 26, 3072 x 2 (3.1 M) 45 : 35 and 3584 x 4 (7.3 M) 53 : 35, 800 rows x 1000 x 8 (7.7 M) 35 : 30, 840 x 4096 x 4
-// (15 M) 70 : 45, 576 rows in 8 requests x 8000 x 8 (38 M) 137 : 105; requests of 32 to 40 rows: 35 x 30000 x 4 (4.2 M) 41 : 54,
-// 128 x 8192 x 8 (8.7 M) 53 : 60, 280 x 8192 x 4 (9.5 M) 64 : 60, 320 x 8192 x 8 (22 M) 101 : 90.
+// works on 128 rows at least).  The prompt kernel and its join take 25 us however little there is to do, the few-row kernel 8 to
+// 12, and 6 more behind a prompt kernel that finds it has nothing to do, but that one gets no more than 0.25 M pairs done in a us.
+// Measured, few-row kernel alone against prompt kernel:
+// 126 rows x 4096 keys x 4 kv heads (2.2 M) 24 : 33 us, 336 x 2000 x 4 (3.0 M) 28 : 38, prompts of 512 tokens with 512 rows x 8
+// (2.1 M) 24 : 27, 3072 x 2 (3.1 M) 24 : 36 and 3584 x 4 (7.3 M) 32 : 38, 800 rows x 1000 x 8 (7.7 M) 51 : 40, 840 x 4096 x 4
+// (15 M) 61 : 47, 576 rows in 8 requests x 8000 x 8 (38 M) 131 : 92; requests of 32 to 40 rows: 35 x 30000 x 4 (4.2 M) 38 : 57,
+// 128 x 8192 x 8 (8.7 M) 44 : 63, 280 x 8192 x 4 (9.5 M) 56 : 64, 320 x 8192 x 8 (22 M) 89 : 94.  (The limits come from when the
+// few-row kernel took 5 to 10 us longer for its joins: the prompts of 512 tokens and the requests of 35 rows are the ones that would
+// gain from a higher one, 800 rows x 1000 x 8 from a lower one.)
 constexpr long long kPromptPairs = 3100000;
 constexpr int kFullRows = 64;
 constexpr int kRowKeys = 256;
