@@ -471,13 +471,13 @@ def tlq_linear_i8(Xq: torch.Tensor, t: torch.Tensor, Wq: torch.Tensor, u: torch.
     N, C1 = Xq.shape
     C2, W1 = Wq.shape
     if (W1 != C1 or Xq.dtype is not _I8 or Wq.dtype is not _I8 or t.dtype is not _F32 or u.dtype is not _F32
-            or t.shape != (N,) or u.shape != (C2,) or not Xq.is_contiguous() or not Wq.is_contiguous()
+            or t.ndim != 1 or u.ndim != 1 or t.numel() != N or u.numel() != C2 or not Xq.is_contiguous() or not Wq.is_contiguous()
             or not t.is_contiguous() or not u.is_contiguous()):
         _typed(Xq, _I8, (N, C1), "Xq")
         _typed(Wq, _I8, (C2, C1), "Wq")
         _typed(t, _F32, (N,), "t")
         _typed(u, _F32, (C2,), "u")
-    if bias is not None:
+    if bias is not None and (bias.dtype is not _BF16 or bias.shape != (C2,) or not bias.is_contiguous()):
         _typed(bias, _BF16, (C2,), "bias")
     # (a workspace's elements count as bytes: a view that repeats memory has fewer)
     if workspace is not None and not workspace.is_contiguous():
@@ -516,18 +516,20 @@ def tlq_kv_store(qkv: torch.Tensor, n_heads: int, cache: KvCache, batch: KvBatch
     axes, sec, limit = 1, None, 0
     if positions is not None:
         axes = 1 if positions.ndim == 1 else positions.shape[0]
-        _typed(positions, _I32, (T,) if positions.ndim == 1 else (axes, T), "positions")
+        if positions.dtype is not _I32 or positions.ndim > 2 or positions.shape[-1] != T or not positions.is_contiguous():
+            _typed(positions, _I32, (T,) if positions.ndim == 1 else (axes, T), "positions")
         if cos_sin is None:
             raise ValueError("positions need cos_sin")
         limit = cos_sin.shape[0]
-        _typed(cos_sin, torch.float32, (limit, d), "cos_sin")
+        if cos_sin.dtype is not _F32 or cos_sin.ndim != 2 or cos_sin.shape[1] != d or not cos_sin.is_contiguous():
+            _typed(cos_sin, _F32, (limit, d), "cos_sin")
         if sections is not None:
             if len(sections) != axes:
                 raise ValueError("one section for each position axis")
             sec = _host_ints(tuple(sections))
-    if q_norm is not None:
+    if q_norm is not None and (q_norm.dtype is not _BF16 or q_norm.shape != (d,) or not q_norm.is_contiguous()):
         _typed(q_norm, _BF16, (d,), "q_norm")
-    if k_norm is not None:
+    if k_norm is not None and (k_norm.dtype is not _BF16 or k_norm.shape != (d,) or not k_norm.is_contiguous()):
         _typed(k_norm, _BF16, (d,), "k_norm")
     if workspace is not None and not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
