@@ -282,6 +282,39 @@ int tlq_linear_i8(const int8_t* Xq, const float* t, int64_t N, int64_t C1, const
                   const void* bias, void* workspace, size_t workspace_bytes, void* Y, void* stream);
 
 /*
+ * The same product with what follows it in a layer, before the one rounding to bf16:
+ *   z[n,o] = t[n] u[o] sum_c Xq[n,c] Wq[o,c] + bias[o];   Y[n,o] = act(z[n,o]) + residual[n,o],
+ * or, with gated != 0 (C2 even): Y[n,j] = act(z[n,2j]) z[n,2j+1] + residual[n,j], Y [N, C2/2]: rows 2j and 2j+1 of Wq, u and bias are
+ * channel j of the gate and of the up projection.
+ *   residual bf16 or NULL, rows ldr elements apart (any pitch); it may be Y itself (then ldr is Y's width), not overlap it otherwise.
+ *   Everything else, and the workspace, as in tlq_linear_i8.
+ */
+#define TLQ_ACT_NONE 0
+#define TLQ_ACT_SILU 1      /* z / (1 + e^-z) */
+#define TLQ_ACT_GELU 2      /* z times the normal distribution's integral up to z */
+#define TLQ_ACT_GELU_TANH 3 /* 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */
+int tlq_linear_i8_act(const int8_t* Xq, const float* t, int64_t N, int64_t C1, const int8_t* Wq, const float* u, int64_t C2,
+                      const void* bias, int32_t act, int32_t gated, const void* residual, int64_t ldr, void* workspace,
+                      size_t workspace_bytes, void* Y, void* stream);
+
+/*
+ * The residual's addition, the root-mean-square norm and the activation quantizer (Sec. 2.2, first two equations) in one pass:
+ *   h = bf16(x + residual) (x without one);   y = h / sqrt(mean_c h^2 + eps) * w;   v = y / s;
+ *   steps[n] = max(max_c |v|, 1e-5) / (2^(a_bits-1) - 1);   codes = rint(v / steps[n]).
+ *   x [N,C], residual [N,C] or NULL: bf16, rows ldx and ldr elements apart (multiples of 8); w [C] bf16 or NULL (ones);
+ *   s [C] bf16 or NULL: the scale that the search found for the product that follows (ones); eps > 0.  C a multiple of 16, to 32768.
+ *   cfg: symmetric mode, a_bits; not read without codes.
+ * Outputs, NULL where not wanted: h_out [N,C] bf16, rows ldh apart (may be x or residual themselves, with their pitch); codes [N,C] int8
+ * with steps [N] fp32; values [N,C] bf16: the values that the codes stand for, codes * steps, as the product sees them; y_out [N,C]
+ * bf16: y before the quantizer.  Codes or y_out are wanted, codes and steps come together, values and s belong to codes.
+ * Outputs lie over no input but as said, nor over one another.
+ * A row with a value that is not finite is not a number: y and values NaN, codes 0 and steps NaN, so that a product of it is NaN.
+ */
+int tlq_norm_quantize(const void* x, int64_t N, int64_t C, int64_t ldx, const void* residual, int64_t ldr, const void* w, float eps,
+                      const void* s, const tlq_config* cfg, void* h_out, int64_t ldh, int8_t* codes, float* steps, void* values,
+                      void* y_out, void* stream);
+
+/*
  * The 8-bit cache of one layer.  A block holds TLQ_KV_BLOCK tokens of one request.  Keys and values are int8 codes with
  * one step per block and kv head (the quantizer of Sec. 2.2 with n = 8: step = max|.| / 127, floor 1e-5 on the maximum).
  * Keys lie token by channel, values channel by token.
@@ -346,6 +379,45 @@ int tlq_kv_store(const void* qkv, int64_t T, int64_t ld, int32_t n_heads, const 
 int tlq_kv_attention(const void* q, int64_t T, int64_t ldq, int32_t n_heads, const tlq_kv_cache* cache,
                      const tlq_kv_batch* batch, float scale, int32_t causal, void* workspace, size_t workspace_bytes,
                      void* out, float* lse, void* stream);
+
+/*
+ * ------------------------------------------------------------------------------------------------------------------
+ * Scoring a model by its logits: what a calibrated model answers with, and how far it is from the full-precision one.
+ *  - logits [N,V] bf16 or fp32 (dtype: TLQ_DTYPE_*), rows ld elements apart (any pitch and alignment of whole elements), read once from
+ *    memory.  1 <= V <= 2^24.  `scale` (one over the temperature) multiplies the logits, 2^-16 <= scale <= 2^16.
+ *  - Logits below -2^100 count as masked, like -infinity: probability 0.  A row with a NaN or +infinity has no distribution: its numbers
+ *    are NaN, its alternatives -1.
+ *  - N = 0 is TLQ_OK and launches nothing.  The calls use no workspace; results do not depend on timing.
+ */
+#define TLQ_MAX_TOP 128
+
+/*
+ * Log probabilities of given tokens:  lse[n] = ln sum_v exp(scale logits[n,v]);  logp[n] = scale logits[n,ids[n]] - lse[n];
+ *   entropy[n] = - sum_v p_v ln p_v;  top_ids [N,K]: the K largest logits of a row, largest first, the lower index first among equals;
+ *   top_logp [N,K] their log probabilities.
+ *   ids [N] int32 or NULL; a negative one is no token (a padded row): logp 0.  One of V or more has no logit: logp NaN.
+ *   logp [N] fp32 (with ids), entropy, lse [N] fp32 or NULL, K 0 .. TLQ_MAX_TOP; top_ids int32 and top_logp fp32 (with K > 0).
+ * A row with fewer than K logits (V < K) is filled up with -1 and -infinity.  A row in which everything is masked has lse -infinity,
+ * entropy 0, and -infinity for every log probability.
+ */
+int tlq_token_logprobs(const void* logits, int dtype, int64_t N, int64_t V, int64_t ld, float scale, const int32_t* ids, int32_t K,
+                       float* logp, float* entropy, float* lse, int32_t* top_ids, float* top_logp, void* stream);
+
+/*
+ * Distillation from a teacher's top logits, forward and backward in one call:
+ *   p = softmax over the row's K teacher logits (scale * top_logits[n,k]),  q = softmax over V of scale * logits[n,v],
+ *   loss[n] = weights[n] sum_k p_k (ln p_k - ln q_{top_ids[n,k]}),
+ *   grad[n,v] = d loss[n] / d logits[n,v] = weights[n] scale (q_v - sum_{k: top_ids[n,k] = v} p_k).
+ *   top_ids [N,K] int32, top_logits [N,K] fp32 (logits, or log probabilities as tlq_token_logprobs returns them: the softmax removes
+ *   any constant); 1 <= K <= TLQ_MAX_TOP.  A token may stand in several places.  A negative id is an empty place; a row without a teacher
+ *   (empty places or logits of -infinity only) has loss 0 and gradient 0.  An id of V or more makes its row NaN.
+ *   weights [N] fp32 or NULL (ones): the gradient that arrives at the row's loss.  A row of weight 0 gives zeros, whatever else it holds.
+ *   loss [N] fp32; grad [N,V] of the logits' type, rows ldg apart, or NULL (the loss alone).  grad may be the logits themselves (same
+ *   pitch), not overlap them otherwise.
+ * A row whose logits are all masked has an infinite loss and gradient 0.  grad as [1,N,V] is what tlq_token_importance takes.
+ */
+int tlq_distill_loss(const void* logits, int dtype, int64_t N, int64_t V, int64_t ld, float scale, const int32_t* top_ids,
+                     const float* top_logits, int32_t K, const float* weights, float* loss, void* grad, int64_t ldg, void* stream);
 
 /* Synchronise `stream` and return the device status word of `workspace` (TLQ_OK, TLQ_ERR_TIMEOUT,
  * TLQ_ERR_NONFINITE) or TLQ_ERR_CUDA if the stream reports an error. */

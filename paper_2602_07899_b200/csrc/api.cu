@@ -499,7 +499,7 @@ int tlq_apply_layer(const void* X, int64_t N, int64_t C1, const void* W, int64_t
     if (codes != nullptr) TLQ_CUDA_TRY(cudaMemcpyAsync(codes, L.Wq, (size_t)C2 * C1, cudaMemcpyDeviceToDevice, st));
     if (steps != nullptr)
       TLQ_CUDA_TRY(cudaMemcpyAsync(steps, L.u, (size_t)C2 * sizeof(float), cudaMemcpyDeviceToDevice, st));
-    rc = launch_apply_gemm_i8(L.Xq, L.Wq, L.t, L.u, bb, N, C1, C2, reinterpret_cast<uint16_t*>(Yq), L.hdr, st);
+    rc = launch_apply_gemm_i8(L.Xq, L.Wq, L.t, L.u, bb, N, C1, C2, nullptr, reinterpret_cast<uint16_t*>(Yq), L.hdr, st);
   }
   if (rc != TLQ_OK) return rc;
   if (L.guards.n > 0) rc = launch_canary_check(workspace, L.guards, L.hdr, st);

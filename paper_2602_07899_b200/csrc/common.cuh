@@ -65,6 +65,12 @@ inline int have_device() {
   found = true;
   return TLQ_OK;
 }
+// Bytes from the first to the last element of N rows of `width` elements that begin `ld` elements apart.
+inline int64_t row_bytes(int64_t N, int64_t width, int64_t ld, int64_t size) { return N < 1 ? 0 : ((N - 1) * ld + width) * size; }
+inline bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+  return a != nullptr && b != nullptr && p < q + (uintptr_t)b_bytes && q < p + (uintptr_t)a_bytes;
+}
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
@@ -332,8 +338,10 @@ int launch_search_gemm_i8(const uint16_t* X, const uint16_t* W, const int8_t* Xq
 int launch_search_gemm_dual_bf16(const uint16_t* Xq, const uint16_t* Xfp, const uint16_t* W, const uint16_t* dW,
                                  const float* w_imp, const GemmPlan& plan, float* partials, float* ptab,
                                  WorkspaceHeader* hdr, cudaStream_t st);
-// Apply: Yq[N,C2] = t[n] * u[o] * (Xq Wq^T) (+bias), bf16 out
+// Apply: Yq[N,C2] = t[n] * u[o] * (Xq Wq^T) (+bias), bf16 out; with `epi` what epilogue.cuh makes of it
+struct Epilogue;
 int launch_apply_gemm_i8(const int8_t* Xq, const int8_t* Wq, const float* t, const float* u, const uint16_t* bias,
-                         int64_t N, int64_t C1, int64_t C2, uint16_t* Yq, WorkspaceHeader* hdr, cudaStream_t st);
+                         int64_t N, int64_t C1, int64_t C2, const Epilogue* epi, uint16_t* Yq, WorkspaceHeader* hdr,
+                         cudaStream_t st);
 
 }  // namespace tlq

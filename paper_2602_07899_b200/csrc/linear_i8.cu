@@ -24,10 +24,10 @@ __device__ __forceinline__ void mma_i8(int (&c)[4], uint32_t a0, uint32_t a1, ui
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <int NT, int kWarps>
+template <int NT, int kWarps, bool kEpi>
 __global__ void __launch_bounds__(kWarps * 32)
-linear_i8_few_kernel(const int8_t* X, const float* t, const int8_t* W,
-                     const float* u, const uint16_t* bias, int64_t N, int C1, int64_t C2, uint16_t* Y) {
+linear_i8_few_kernel(const int8_t* X, const float* t, const int8_t* W, const float* u, const uint16_t* bias, int64_t N, int C1,
+                     int64_t C2, const Epilogue epi, uint16_t* Y) {
   constexpr int kThreads = kWarps * 32;
   __shared__ int s_acc[kWarps][NT * 8][17];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -62,15 +62,33 @@ linear_i8_few_kernel(const int8_t* X, const float* t, const int8_t* W,
 #pragma unroll
     for (int j = 0; j < 4; ++j) s_acc[warp][n * 8 + 2 * q + (j & 1)][g + (j >> 1) * 8] = acc[n][j];
   __syncthreads();
-  for (int e = threadIdx.x; e < NT * 8 * 16; e += kThreads) {
-    const int r = e & 15, n = e >> 4;
-    if (n0 + n >= N || o0 + r >= C2) continue;
+  auto product = [&](int n, int r) {
     int sum = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) sum += s_acc[w][n][r];
     float y = (float)sum * (t[n0 + n] * u[o0 + r]);
     if (bias != nullptr) y += bf16_bits_to_float(bias[o0 + r]);
-    const __nv_bfloat16 v = __float2bfloat16_rn(y);
+    return y;
+  };
+  if constexpr (kEpi) {
+    const int pair = epi.gated ? 1 : 0;                       // C2 is even then: both rows of a pair are there
+    const int64_t width = C2 >> pair;
+    for (int e = threadIdx.x; e < NT * 8 * (16 >> pair); e += kThreads) {
+      const int r = (e & ((16 >> pair) - 1)) << pair, n = e >> (4 - pair);
+      if (n0 + n >= N || o0 + r >= C2) continue;
+      float y = activate(epi.act, product(n, r));
+      if (pair) y *= product(n, r + 1);
+      const int64_t o = (o0 + r) >> pair;
+      if (epi.residual != nullptr) y += bf16_bits_to_float(epi.residual[(n0 + n) * epi.ldr + o]);
+      const __nv_bfloat16 v = __float2bfloat16_rn(y);
+      Y[(n0 + n) * width + o] = *reinterpret_cast<const uint16_t*>(&v);
+    }
+    return;
+  }
+  for (int e = threadIdx.x; e < NT * 8 * 16; e += kThreads) {
+    const int r = e & 15, n = e >> 4;
+    if (n0 + n >= N || o0 + r >= C2) continue;
+    const __nv_bfloat16 v = __float2bfloat16_rn(product(n, r));
     Y[(n0 + n) * C2 + o0 + r] = *reinterpret_cast<const uint16_t*>(&v);
   }
 }
@@ -97,6 +115,8 @@ struct TileArgs {
   int64_t N, C2;
   int num_kb, tile_n, stages, mtiles, splits;
   uint32_t tmem_cols;
+  Epilogue epi;
+  bool even;                  // of a result with an epilogue: two channels lie at an address of 4 bytes, in Y and in the residual
 };
 
 __device__ __forceinline__ int4 ld_cluster(uint32_t addr) {
@@ -106,6 +126,7 @@ __device__ __forceinline__ int4 ld_cluster(uint32_t addr) {
 }
 __device__ __forceinline__ void add(int4& a, const int4& b) { a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w; }
 
+template <bool kEpi>
 __global__ void __launch_bounds__(kTileThreads, 1)
 linear_i8_tile_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const TileArgs g) {
   extern __shared__ uint8_t smem_raw[];
@@ -233,6 +254,43 @@ linear_i8_tile_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
       }
       const float y0 = fmaf((float)s.x, t * u[0], b[0]), y1 = fmaf((float)s.y, t * u[1], b[1]);
       const float y2 = fmaf((float)s.z, t * u[2], b[2]), y3 = fmaf((float)s.w, t * u[3], b[3]);
+      if constexpr (kEpi) {
+        // channels o .. o + 3, or o / 2 and o / 2 + 1 of pairs (C2 is even then)
+        const int64_t width = g.epi.gated ? g.C2 >> 1 : g.C2, at = g.epi.gated ? o >> 1 : o;
+        const int count = (int)max((int64_t)0, min((int64_t)(g.epi.gated ? 2 : 4), width - at));
+        float v[4] = {activate(g.epi.act, y0), 0.f, activate(g.epi.act, y2), 0.f};
+        if (g.epi.gated) {
+          v[0] *= y1;
+          v[1] = v[2] * y3;
+        } else {
+          v[1] = activate(g.epi.act, y1);
+          v[3] = activate(g.epi.act, y3);
+        }
+        uint16_t* out = g.Y + (n0 + c) * width + at;
+        const uint16_t* res = g.epi.residual == nullptr ? nullptr : g.epi.residual + (n0 + c) * g.epi.ldr + at;
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+          if (j >= count) continue;
+          if (g.even) {                                      // (width is even, so that both are there)
+            if (res != nullptr) {
+              const uint32_t r = load_near(reinterpret_cast<const uint32_t*>(res + j));
+              v[j] += bf16_bits_to_float(r & 0xFFFFu);
+              v[j + 1] += bf16_bits_to_float(r >> 16);
+            }
+            const __nv_bfloat162 p = __floats2bfloat162_rn(v[j], v[j + 1]);
+            *reinterpret_cast<uint32_t*>(out + j) = *reinterpret_cast<const uint32_t*>(&p);
+          } else {
+#pragma unroll
+            for (int k = j; k < j + 2; ++k) {
+              if (k >= count) continue;
+              if (res != nullptr) v[k] += bf16_bits_to_float(res[k]);
+              const __nv_bfloat16 p = __float2bfloat16_rn(v[k]);
+              out[k] = *reinterpret_cast<const uint16_t*>(&p);
+            }
+          }
+        }
+        continue;
+      }
       const __nv_bfloat162 p0 = __floats2bfloat162_rn(y0, y1), p1 = __floats2bfloat162_rn(y2, y3);
       const uint2 w = make_uint2(*reinterpret_cast<const uint32_t*>(&p0), *reinterpret_cast<const uint32_t*>(&p1));
       uint16_t* y = g.Y + (n0 + c) * g.C2 + o;
@@ -265,8 +323,16 @@ bool map_codes(CUtensorMap* tm, const int8_t* p, int64_t rows, int64_t cols, uin
   return encode_tensor_map(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, p, dims, pitch, box);
 }
 
+template <bool kEpi>
+int configure_tiles() {
+  static OncePerDevice once;
+  return once_per_device(once, [] {
+    return cudaFuncSetAttribute(linear_i8_tile_kernel<kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kStageBudget + 1024));
+  });
+}
+
 int launch_tiles(const int8_t* Xq, const float* t, const int8_t* Wq, const float* u, const uint16_t* bias, int64_t N, int64_t C1,
-                 int64_t C2, uint16_t* Y, WorkspaceHeader* hdr, cudaStream_t st) {
+                 int64_t C2, const Epilogue* epi, uint16_t* Y, WorkspaceHeader* hdr, cudaStream_t st) {
   const int sms = device_sm_count();
   if (sms <= 0) return TLQ_ERR_CUDA;
   TileArgs g{};
@@ -277,7 +343,7 @@ int launch_tiles(const int8_t* Xq, const float* t, const int8_t* Wq, const float
   const bool narrow = g.tile_n <= 64;
   const int64_t slots = narrow ? 2 * sms : sms, tiles = mtiles * otiles;
   // more tiles than that: the persistent kernel of tlq_apply_layer, which writes one tile while it sums the next
-  if (tiles > slots) return launch_apply_gemm_i8(Xq, Wq, t, u, bias, N, C1, C2, Y, hdr, st);
+  if (tiles > slots) return launch_apply_gemm_i8(Xq, Wq, t, u, bias, N, C1, C2, epi, Y, hdr, st);
   g.mtiles = (int)mtiles;
   g.num_kb = (int)ceil_div(C1, kTileK);
   const uint32_t stage_bytes = kWBytes + (uint32_t)g.tile_n * kTileK;
@@ -291,32 +357,39 @@ int launch_tiles(const int8_t* Xq, const float* t, const int8_t* Wq, const float
   if (!map_codes(&tmW, Wq, C2, C1, kTileO) || !map_codes(&tmX, Xq, N, C1, (uint32_t)g.tile_n)) return TLQ_ERR_CUDA;
   size_t smem = (size_t)g.stages * stage_bytes;
   if (smem < (size_t)g.tile_n * kTileO * 4) smem = (size_t)g.tile_n * kTileO * 4;
-  static OncePerDevice once;
-  const int rc = once_per_device(once, [] {
-    return cudaFuncSetAttribute(linear_i8_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kStageBudget + 1024));
-  });
+  if (epi != nullptr) {
+    g.epi = *epi;
+    const int64_t width = epi->gated ? C2 / 2 : C2;
+    g.even = (width & 1) == 0 && (epi->residual == nullptr || ((epi->ldr & 1) == 0 && (reinterpret_cast<uintptr_t>(epi->residual) & 3u) == 0));
+  }
+  const int rc = epi != nullptr ? configure_tiles<true>() : configure_tiles<false>();
   if (rc != TLQ_OK) return rc;
-  return launch_next(linear_i8_tile_kernel, dim3((unsigned)(tiles * g.splits)), kTileThreads, smem + 1024, (unsigned)g.splits, st,
-                     tmW, tmX, g);
+  return launch_next(epi != nullptr ? linear_i8_tile_kernel<true> : linear_i8_tile_kernel<false>, dim3((unsigned)(tiles * g.splits)),
+                     kTileThreads, smem + 1024, (unsigned)g.splits, st, tmW, tmX, g);
 }
 
 }  // namespace
 
 int launch_linear_i8(const int8_t* Xq, const float* t, const int8_t* Wq, const float* u, const uint16_t* bias, int64_t N,
-                     int64_t C1, int64_t C2, uint16_t* Y, WorkspaceHeader* hdr, cudaStream_t st) {
+                     int64_t C1, int64_t C2, const Epilogue* epi, uint16_t* Y, WorkspaceHeader* hdr, cudaStream_t st) {
   // Few tokens and weights of up to 24 MB: measured, the few kernel is ahead up to 14 MB (1536 x 8960: 4.7 us against 6.1) and
   // behind from 64 MB on (8192 x 8192: 16.1 against 15.0).
-  if (N > 16 || C1 * C2 > (24 << 20)) return launch_tiles(Xq, t, Wq, u, bias, N, C1, C2, Y, hdr, st);
+  if (N > 16 || C1 * C2 > (24 << 20)) return launch_tiles(Xq, t, Wq, u, bias, N, C1, C2, epi, Y, hdr, st);
   const unsigned ctas = (unsigned)ceil_div(C2, 16);
   const int sms = device_sm_count();
   if (sms <= 0) return TLQ_ERR_CUDA;
   // with no more CTAs than SMs a CTA has an SM to itself and takes twice the warps (1536 x 8960, 560 CTAs: 5.8 us so, 4.7 not)
   const bool deep = (int)ctas <= sms;
+  const Epilogue e = epi != nullptr ? *epi : Epilogue{};
   auto run = [&](auto kernel, int warps) {
-    return launch_next(kernel, dim3(ctas), warps * 32, 0, 1, st, Xq, t, Wq, u, bias, N, (int)C1, C2, Y);
+    return launch_next(kernel, dim3(ctas), warps * 32, 0, 1, st, Xq, t, Wq, u, bias, N, (int)C1, C2, e, Y);
   };
-  if (N <= 8) return deep ? run(linear_i8_few_kernel<1, 16>, 16) : run(linear_i8_few_kernel<1, 8>, 8);
-  return deep ? run(linear_i8_few_kernel<2, 16>, 16) : run(linear_i8_few_kernel<2, 8>, 8);
+  if (epi != nullptr) {
+    if (N <= 8) return deep ? run(linear_i8_few_kernel<1, 16, true>, 16) : run(linear_i8_few_kernel<1, 8, true>, 8);
+    return deep ? run(linear_i8_few_kernel<2, 16, true>, 16) : run(linear_i8_few_kernel<2, 8, true>, 8);
+  }
+  if (N <= 8) return deep ? run(linear_i8_few_kernel<1, 16, false>, 16) : run(linear_i8_few_kernel<1, 8, false>, 8);
+  return deep ? run(linear_i8_few_kernel<2, 16, false>, 16) : run(linear_i8_few_kernel<2, 8, false>, 8);
 }
 
 }  // namespace tlq

@@ -19,6 +19,7 @@
 //   warps 2..9  epilogue: two warps per tensor-memory lane quarter, 128 columns each
 // The same kernel serves tlq_apply_layer for W8A8 (a single int8 pass, bf16 store of t*u*acc + bias).
 #include "common.cuh"
+#include "epilogue.cuh"
 #include "umma.cuh"
 
 namespace tlq {
@@ -59,6 +60,8 @@ struct I8Args {
   const uint16_t* bias;    // apply
   uint16_t* yq;            // apply
   WorkspaceHeader* hdr;
+  Epilogue epi;            // apply with an epilogue
+  bool whole8;             // ... whose results and residual lie in rows of whole 16-byte pieces
 };
 
 __device__ __forceinline__ void report_timeout(WorkspaceHeader* hdr, int where) {
@@ -73,6 +76,7 @@ __device__ __forceinline__ void report_timeout(WorkspaceHeader* hdr, int where) 
 //          part is accumulated once per tile by two bf16 passes into one accumulator (X_fp W^T, then X_q W^T
 //          with the negate bit) and kept in registers; every candidate adds its bf16 pass X_q dW_k^T to it.
 //          Tensor maps: tmX = X_fp, tmW = W, tmXq = X_q (bf16, 3-D with a single slice), tmWq = dW (bf16, 3-D).
+// kMode 3: apply with activation, gate and residual (epilogue.cuh) before the rounding
 template <int kMode>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_w8a8_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW,
@@ -90,7 +94,7 @@ gemm_w8a8_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr bool kApply = kMode == 1;
+  constexpr bool kApply = kMode == 1 || kMode == 3;
   constexpr bool kDual = kMode == 2;
 
   if (threadIdx.x == 0) {
@@ -308,6 +312,65 @@ gemm_w8a8_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
           for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, off);
           if (lane == 0)
             args.partials[(int64_t)k * args.otiles * args.mtiles * 8 + ((int64_t)ot * args.mtiles + mt) * 8 + ew] = v;
+        } else if constexpr (kMode == 3) {
+          const int pair = args.epi.gated ? 1 : 0;             // C2 is even then: both rows of a pair are there
+          const int64_t width = args.C2 >> pair;
+#pragma unroll 1
+          for (int c = 0; c < 8; ++c) {
+            uint32_t r[16];
+            __syncwarp();
+            ptx::tmem_ld16(taddr + c * 16, r);
+            ptx::tmem_ld_wait();
+            const int64_t col = col_base + c * 16;
+            if (n >= n_tokens || col >= args.C2) continue;
+            float v[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const int64_t o = min(col + j, args.C2 - 1);     // (columns beyond the end are not stored)
+              v[j] = (float)(int)r[j] * (tn * __ldg(u_row + o));
+              if (args.bias != nullptr) v[j] += bf16_bits_to_float(args.bias[o]);
+            }
+            if (pair) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] = activate(args.epi.act, v[2 * j]) * v[2 * j + 1];
+            } else {
+#pragma unroll
+              for (int j = 0; j < 16; ++j) v[j] = activate(args.epi.act, v[j]);
+            }
+            const int64_t at = col >> pair;
+            uint16_t* out = args.yq + n * width + at;
+            const uint16_t* res = args.epi.residual == nullptr ? nullptr : args.epi.residual + n * args.epi.ldr + at;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {                      // eight channels at a time, the second eight where rows are not paired
+              if (p == 1 && pair) continue;
+              if (at + p * 8 >= width) continue;
+              if (args.whole8) {
+                float f[8];
+                if (res != nullptr) {
+                  unpack8(*reinterpret_cast<const uint4*>(res + p * 8), f);
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) v[p * 8 + j] += f[j];
+                }
+                uint32_t o[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  const __nv_bfloat162 b = __floats2bfloat162_rn(v[p * 8 + 2 * j], v[p * 8 + 2 * j + 1]);
+                  o[j] = *reinterpret_cast<const uint32_t*>(&b);
+                }
+                *reinterpret_cast<uint4*>(out + p * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+              } else {
+#pragma unroll
+                for (int j = p * 8; j < p * 8 + 8; ++j) {
+                  if (at + j >= width) continue;
+                  const __nv_bfloat16 b = __float2bfloat16_rn(res != nullptr ? v[j] + bf16_bits_to_float(res[j]) : v[j]);
+                  out[j] = *reinterpret_cast<const uint16_t*>(&b);
+                }
+              }
+            }
+          }
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(tempty_bar(acc));
         } else {
           const bool even = (args.C2 & 7) == 0;
 #pragma unroll 1
@@ -437,10 +500,11 @@ int launch_search_gemm_i8(const uint16_t* X, const uint16_t* W, const int8_t* Xq
 }
 
 int launch_apply_gemm_i8(const int8_t* Xq, const int8_t* Wq, const float* t, const float* u, const uint16_t* bias,
-                         int64_t N, int64_t C1, int64_t C2, uint16_t* Yq, WorkspaceHeader* hdr, cudaStream_t st) {
+                         int64_t N, int64_t C1, int64_t C2, const Epilogue* epi, uint16_t* Yq, WorkspaceHeader* hdr,
+                         cudaStream_t st) {
   CUtensorMap tmXq, tmWq;
   if (!map_i8_3d(&tmXq, Xq, N, C1, 1, BM) || !map_i8_3d(&tmWq, Wq, C2, C1, 1, BN)) return TLQ_ERR_CUDA;
-  int rc = configure_kernel<1>();
+  int rc = epi != nullptr ? configure_kernel<3>() : configure_kernel<1>();
   if (rc != TLQ_OK) return rc;
   GemmPlan plan = plan_search_gemm_i8(N, C1, C2, 1);
   I8Args a{};
@@ -456,6 +520,13 @@ int launch_apply_gemm_i8(const int8_t* Xq, const int8_t* Wq, const float* t, con
   if (sms <= 0) return TLQ_ERR_CUDA;
   const unsigned grid = (unsigned)(a.num_tiles < sms ? a.num_tiles : sms);
   a.raster = make_raster(plan.mtiles, plan.otiles, sms, plan.N * plan.C1, BM);
+  if (epi != nullptr) {
+    a.epi = *epi;
+    const int64_t width = epi->gated ? C2 / 2 : C2;
+    a.whole8 = (width & 7) == 0 && (epi->residual == nullptr || ((epi->ldr & 7) == 0 && aligned16(epi->residual)));
+    gemm_w8a8_kernel<3><<<grid, kThreads, kSmemBytes, st>>>(tmXq, tmWq, tmXq, tmWq, a);
+    return after_launch();
+  }
   gemm_w8a8_kernel<1><<<grid, kThreads, kSmemBytes, st>>>(tmXq, tmWq, tmXq, tmWq, a);
   return after_launch();
 }

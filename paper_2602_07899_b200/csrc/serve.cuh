@@ -1,9 +1,11 @@
-// Shared declarations of the serving operators: the 8-bit product, the key-value store and attention over the cache.
+// Shared declarations of the serving operators: the norm, the 8-bit product, the key-value store and attention over the cache; and
+// of those that score a model by its logits.
 #pragma once
 
 #include <cuda_fp16.h>
 
 #include "common.cuh"
+#include "epilogue.cuh"
 
 namespace tlq {
 
@@ -326,8 +328,19 @@ int launch_kv_join(int head_dim, const KvArgs& a, int ctas, int few_rows, bool p
 int launch_kv_attention(const uint16_t* q, int64_t ldq, int head_dim, const KvArgs& a, float scale, int causal,
                         uint16_t* out, float* lse, const KvSplit& split, cudaStream_t st);
 
-// linear_i8.cu
+// linear_i8.cu; `epi`: what happens to the products before they are rounded, or null for nothing
 int launch_linear_i8(const int8_t* Xq, const float* t, const int8_t* Wq, const float* u, const uint16_t* bias, int64_t N,
-                     int64_t C1, int64_t C2, uint16_t* Y, WorkspaceHeader* hdr, cudaStream_t st);
+                     int64_t C1, int64_t C2, const Epilogue* epi, uint16_t* Y, WorkspaceHeader* hdr, cudaStream_t st);
+
+// norm.cu
+int launch_norm_quantize(const uint16_t* x, int64_t N, int64_t C, int64_t ldx, const uint16_t* r, int64_t ldr, const uint16_t* w,
+                         float eps, const uint16_t* s, int a_bits, uint16_t* h, int64_t ldh, int8_t* codes, float* steps,
+                         uint16_t* values, uint16_t* y, cudaStream_t st);
+
+// logits.cu
+int launch_token_logprobs(const void* logits, int f32, int64_t N, int64_t V, int64_t ld, float scale, const int32_t* ids, int K,
+                          float* logp, float* entropy, float* lse, int32_t* top_ids, float* top_logp, cudaStream_t st);
+int launch_distill_loss(const void* logits, int f32, int64_t N, int64_t V, int64_t ld, float scale, const int32_t* top_ids,
+                        const float* top_logits, int K, const float* weights, float* loss, void* grad, int64_t ldg, cudaStream_t st);
 
 }  // namespace tlq

@@ -70,8 +70,124 @@ int tlq_linear_i8(const int8_t* Xq, const float* t, int64_t N, int64_t C1, const
   if (workspace_bytes < need) return TLQ_ERR_WORKSPACE;
   int rc = have_device();
   if (rc != TLQ_OK || N == 0) return rc;
-  return launch_linear_i8(Xq, t, Wq, u, reinterpret_cast<const uint16_t*>(bias), N, C1, C2, reinterpret_cast<uint16_t*>(Y),
+  return launch_linear_i8(Xq, t, Wq, u, reinterpret_cast<const uint16_t*>(bias), N, C1, C2, nullptr,
+                          reinterpret_cast<uint16_t*>(Y), reinterpret_cast<WorkspaceHeader*>(workspace),
+                          reinterpret_cast<cudaStream_t>(stream));
+}
+
+int tlq_linear_i8_act(const int8_t* Xq, const float* t, int64_t N, int64_t C1, const int8_t* Wq, const float* u, int64_t C2,
+                      const void* bias, int32_t act, int32_t gated, const void* residual, int64_t ldr, void* workspace,
+                      size_t workspace_bytes, void* Y, void* stream) {
+  const size_t need = tlq_linear_i8_workspace_bytes(N, C1, C2);
+  if (need == 0) return TLQ_ERR_SHAPE;
+  if (act < TLQ_ACT_NONE || act > TLQ_ACT_GELU_TANH) return TLQ_ERR_INVALID_ARG;
+  if (gated != 0 && (C2 & 1) != 0) return TLQ_ERR_SHAPE;
+  const int64_t width = gated != 0 ? C2 / 2 : C2;
+  if (Wq == nullptr || u == nullptr || workspace == nullptr) return TLQ_ERR_INVALID_ARG;
+  if (N > 0 && (Xq == nullptr || t == nullptr || Y == nullptr)) return TLQ_ERR_INVALID_ARG;
+  if (residual != nullptr && (ldr < width || ldr > (1LL << 40))) return TLQ_ERR_SHAPE;
+  if (!aligned16(Xq) || !aligned16(Wq) || !aligned16(workspace) || !aligned16(Y)) return TLQ_ERR_ALIGN;
+  // the residual's rows may be the result's own (each element is read by the thread that writes it), but not lie across them
+  if (residual != nullptr && overlap(residual, row_bytes(N, width, ldr, 2), Y, row_bytes(N, width, width, 2)) &&
+      !(residual == Y && ldr == width))
+    return TLQ_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return TLQ_ERR_WORKSPACE;
+  int rc = have_device();
+  if (rc != TLQ_OK || N == 0) return rc;
+  Epilogue e{};
+  e.act = act;
+  e.gated = gated != 0;
+  e.residual = reinterpret_cast<const uint16_t*>(residual);
+  e.ldr = ldr;
+  return launch_linear_i8(Xq, t, Wq, u, reinterpret_cast<const uint16_t*>(bias), N, C1, C2, &e, reinterpret_cast<uint16_t*>(Y),
                           reinterpret_cast<WorkspaceHeader*>(workspace), reinterpret_cast<cudaStream_t>(stream));
+}
+
+int tlq_norm_quantize(const void* x, int64_t N, int64_t C, int64_t ldx, const void* residual, int64_t ldr, const void* w, float eps,
+                      const void* s, const tlq_config* cfg, void* h_out, int64_t ldh, int8_t* codes, float* steps, void* values,
+                      void* y_out, void* stream) {
+  if (N < 0 || N > 0x7FFFFF00LL || C < 16 || (C % 16) != 0 || C > 32768) return TLQ_ERR_SHAPE;
+  if (codes != nullptr) {
+    if (cfg == nullptr || cfg->struct_size != sizeof(tlq_config)) return TLQ_ERR_INVALID_ARG;
+    if (cfg->mode != TLQ_W8A8_SYM || cfg->a_bits < 2 || cfg->a_bits > 8) return TLQ_ERR_UNSUPPORTED;
+    if (steps == nullptr) return TLQ_ERR_INVALID_ARG;
+  } else if (N > 0 && (steps != nullptr || values != nullptr || s != nullptr)) {
+    return TLQ_ERR_INVALID_ARG;           // (buffers of no rows may be NULL)
+  }
+  if (!(eps > 0.0f) || isinf(eps)) return TLQ_ERR_INVALID_ARG;
+  if (N > 0 && (x == nullptr || (codes == nullptr && y_out == nullptr))) return TLQ_ERR_INVALID_ARG;
+  const int64_t most = 1LL << 40;
+  if (ldx < C || ldx > most || (ldx % 8) != 0) return TLQ_ERR_SHAPE;
+  if (residual != nullptr && (ldr < C || ldr > most || (ldr % 8) != 0)) return TLQ_ERR_SHAPE;
+  if (h_out != nullptr && (ldh < C || ldh > most || (ldh % 8) != 0)) return TLQ_ERR_SHAPE;
+  if (!aligned16(x) || !aligned16(residual) || !aligned16(w) || !aligned16(s) || !aligned16(h_out) || !aligned16(codes) ||
+      !aligned16(values) || !aligned16(y_out))
+    return TLQ_ERR_ALIGN;
+  const int64_t flat = N * C;
+  const struct { const void* p; int64_t bytes; int64_t ld; } in[4] = {{x, row_bytes(N, C, ldx, 2), ldx}, {residual, row_bytes(N, C, ldr, 2), ldr},
+                                                                      {w, C * 2, 0}, {s, C * 2, 0}};
+  const struct { const void* p; int64_t bytes; int64_t ld; } out[5] = {{h_out, row_bytes(N, C, ldh, 2), ldh}, {codes, flat, -1},
+                                                                       {steps, N * 4, -1}, {values, flat * 2, -1}, {y_out, flat * 2, -1}};
+  for (int i = 0; i < 5; ++i) {
+    // the sum may go where x or the residual lie (each element is read by the thread that writes it); nothing else may lie over an input
+    for (int j = 0; j < 4; ++j)
+      if (overlap(out[i].p, out[i].bytes, in[j].p, in[j].bytes) && !(out[i].p == in[j].p && out[i].ld == in[j].ld)) return TLQ_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i].p, out[i].bytes, out[j].p, out[j].bytes)) return TLQ_ERR_INVALID_ARG;
+  }
+  int rc = have_device();
+  if (rc != TLQ_OK || N == 0) return rc;
+  return launch_norm_quantize(reinterpret_cast<const uint16_t*>(x), N, C, ldx, reinterpret_cast<const uint16_t*>(residual), ldr,
+                              reinterpret_cast<const uint16_t*>(w), eps, reinterpret_cast<const uint16_t*>(s),
+                              codes != nullptr ? cfg->a_bits : 8, reinterpret_cast<uint16_t*>(h_out), ldh, codes, steps,
+                              reinterpret_cast<uint16_t*>(values), reinterpret_cast<uint16_t*>(y_out),
+                              reinterpret_cast<cudaStream_t>(stream));
+}
+
+static int check_logits(const void* logits, int dtype, int64_t N, int64_t V, int64_t ld, float scale, int32_t K) {
+  if (dtype != TLQ_DTYPE_BF16 && dtype != TLQ_DTYPE_F32) return TLQ_ERR_INVALID_ARG;
+  if (N < 0 || N > 0x0FFFFFFFLL || V < 1 || V > (1LL << 24) || ld < V || ld > (1LL << 32) || K < 0 || K > TLQ_MAX_TOP) return TLQ_ERR_SHAPE;
+  if (!(scale >= 1.52587890625e-05f && scale <= 65536.0f)) return TLQ_ERR_INVALID_ARG;
+  if (N > 0 && logits == nullptr) return TLQ_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(logits) & (dtype == TLQ_DTYPE_F32 ? 3u : 1u)) != 0) return TLQ_ERR_ALIGN;
+  return TLQ_OK;
+}
+
+int tlq_token_logprobs(const void* logits, int dtype, int64_t N, int64_t V, int64_t ld, float scale, const int32_t* ids, int32_t K,
+                       float* logp, float* entropy, float* lse, int32_t* top_ids, float* top_logp, void* stream) {
+  int rc = check_logits(logits, dtype, N, V, ld, scale, K);
+  if (rc != TLQ_OK) return rc;
+  if (N > 0) {              // (buffers of no rows may be NULL)
+    if ((ids == nullptr) != (logp == nullptr) || (K > 0) != (top_ids != nullptr) || (K > 0) != (top_logp != nullptr)) return TLQ_ERR_INVALID_ARG;
+    if (logp == nullptr && entropy == nullptr && lse == nullptr && K == 0) return TLQ_ERR_INVALID_ARG;
+  }
+  rc = have_device();
+  if (rc != TLQ_OK || N == 0) return rc;
+  return launch_token_logprobs(logits, dtype == TLQ_DTYPE_F32, N, V, ld, scale, ids, K, logp, entropy, lse, top_ids, top_logp,
+                               reinterpret_cast<cudaStream_t>(stream));
+}
+
+int tlq_distill_loss(const void* logits, int dtype, int64_t N, int64_t V, int64_t ld, float scale, const int32_t* top_ids,
+                     const float* top_logits, int32_t K, const float* weights, float* loss, void* grad, int64_t ldg, void* stream) {
+  int rc = check_logits(logits, dtype, N, V, ld, scale, K);
+  if (rc != TLQ_OK) return rc;
+  if (K < 1) return TLQ_ERR_SHAPE;
+  if (N > 0 && (top_ids == nullptr || top_logits == nullptr || loss == nullptr)) return TLQ_ERR_INVALID_ARG;
+  if (grad != nullptr) {
+    const int64_t size = dtype == TLQ_DTYPE_F32 ? 4 : 2;
+    if (ldg < V || ldg > (1LL << 32)) return TLQ_ERR_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(grad) & (uintptr_t)(size - 1)) != 0) return TLQ_ERR_ALIGN;
+    // the gradient may be written over the logits (each is read by the thread that writes it), but not across them, nor over the rest
+    const int64_t bytes = row_bytes(N, V, ldg, size);
+    if (overlap(grad, bytes, logits, row_bytes(N, V, ld, size)) && !(grad == logits && ldg == ld)) return TLQ_ERR_INVALID_ARG;
+    if (overlap(grad, bytes, top_ids, N * K * 4) || overlap(grad, bytes, top_logits, N * K * 4) || overlap(grad, bytes, weights, N * 4) ||
+        overlap(grad, bytes, loss, N * 4))
+      return TLQ_ERR_INVALID_ARG;
+  }
+  rc = have_device();
+  if (rc != TLQ_OK || N == 0) return rc;
+  return launch_distill_loss(logits, dtype == TLQ_DTYPE_F32, N, V, ld, scale, top_ids, top_logits, K, weights, loss, grad, ldg,
+                             reinterpret_cast<cudaStream_t>(stream));
 }
 
 size_t tlq_kv_workspace_bytes(const tlq_kv_cache* cache, const tlq_kv_batch* batch, int32_t n_heads, int64_t T) {

@@ -34,7 +34,7 @@ EXPORTS = (
     "tlq_apply_layer_workspace_bytes", "tlq_apply_layer", "tlq_read_status", "tlq_stage_timing_enable",
     "tlq_stage_timing_drain", "tlq_kernel_launch_count", "tlq_selftest_bounded_wait", "tlq_debug_tile_walk", "tlq_debug_resident_walk", "tlq_l2_partition_info", "tlq_debug_canary_offsets",
     "tlq_debug_check_canaries", "tlq_linear_i8_workspace_bytes", "tlq_linear_i8", "tlq_kv_workspace_bytes", "tlq_kv_store",
-    "tlq_kv_attention",
+    "tlq_kv_attention", "tlq_linear_i8_act", "tlq_norm_quantize", "tlq_token_logprobs", "tlq_distill_loss",
 )
 
 
@@ -63,6 +63,8 @@ class _KvBatchStruct(ctypes.Structure):
 
 
 KV_BLOCK = 64                 # tokens of one cache block
+ACT_NONE, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3
+MAX_TOP = 128                 # alternatives of a token, or teacher's logits of a row
 
 FLAG_SKIP_ZERO_WEIGHT_TOKENS = 1
 FLAG_GEMM_CTA_PAIRS = 2
@@ -137,6 +139,15 @@ def _load() -> ctypes.CDLL:
                                  ctypes.c_float, vp, vp, vp, vp, sz, vp]
     lib.tlq_kv_attention.restype = i32
     lib.tlq_kv_attention.argtypes = [vp, i64, i64, i32, kvp, kbp, ctypes.c_float, i32, vp, sz, vp, vp, vp]
+    f32 = ctypes.c_float
+    lib.tlq_linear_i8_act.restype = i32
+    lib.tlq_linear_i8_act.argtypes = [vp, vp, i64, i64, vp, vp, i64, vp, i32, i32, vp, i64, vp, sz, vp, vp]
+    lib.tlq_norm_quantize.restype = i32
+    lib.tlq_norm_quantize.argtypes = [vp, i64, i64, i64, vp, i64, vp, f32, vp, cfgp, vp, i64, vp, vp, vp, vp, vp]
+    lib.tlq_token_logprobs.restype = i32
+    lib.tlq_token_logprobs.argtypes = [vp, i32, i64, i64, i64, f32, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.tlq_distill_loss.restype = i32
+    lib.tlq_distill_loss.argtypes = [vp, i32, i64, i64, i64, f32, vp, vp, i32, vp, vp, vp, i64, vp]
     for fn in ("tlq_token_importance", "tlq_scale_candidates", "tlq_scale_candidates_noalloc", "tlq_quantize_weights", "tlq_pack_codes4", "tlq_quantize_activations", "tlq_scale_search_layer",
                "tlq_apply_layer", "tlq_read_status", "tlq_stage_timing_enable", "tlq_stage_timing_drain"):
         getattr(lib, fn).restype = i32
@@ -578,6 +589,195 @@ def tlq_kv_attention(q: torch.Tensor, cache: KvCache, batch: KvBatch, scale: flo
                                 workspace.data_ptr(), workspace.numel(), out.data_ptr(),
                                 None if lse is None else lse.data_ptr(), _stream(stream, dev)), "tlq_kv_attention")
     return out, lse
+
+
+def _empty_on(like: torch.Tensor, stream):
+    return like.new_empty if stream is None else functools.partial(_made_on, stream, like.new_empty)
+
+
+def tlq_linear_i8_act(Xq: torch.Tensor, t: torch.Tensor, Wq: torch.Tensor, u: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                      act: int = ACT_NONE, gated: bool = False, residual: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """tlq_linear_i8 with act (ACT_*), gate and residual before the rounding -> bf16 [N, C2], or [N, C2 / 2] with `gated`, where rows
+    2j and 2j + 1 of Wq, u and bias make channel j (gated_rows lays them out).  residual bf16 of the result's shape (rows may be
+    strided); it may be `out` itself.  Workspace as of tlq_linear_i8."""
+    N, C1 = Xq.shape
+    C2 = Wq.shape[0]
+    width = C2 // 2 if gated else C2
+    if (Wq.shape[1] != C1 or Xq.dtype is not _I8 or Wq.dtype is not _I8 or t.dtype is not _F32 or u.dtype is not _F32
+            or t.ndim != 1 or u.ndim != 1 or t.numel() != N or u.numel() != C2 or not Xq.is_contiguous() or not Wq.is_contiguous()
+            or not t.is_contiguous() or not u.is_contiguous()):
+        _typed(Xq, _I8, (N, C1), "Xq")
+        _typed(Wq, _I8, (C2, C1), "Wq")
+        _typed(t, _F32, (N,), "t")
+        _typed(u, _F32, (C2,), "u")
+    if bias is not None and (bias.dtype is not _BF16 or bias.shape != (C2,) or not bias.is_contiguous()):
+        _typed(bias, _BF16, (C2,), "bias")
+    ldr = 0
+    if residual is not None:
+        ldr = _rows(residual, "residual")
+        if residual.shape != (N, width):
+            raise ValueError(f"residual must have the result's shape {(N, width)}, got {tuple(residual.shape)}")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    dev = Xq.get_device()
+    if (dev < 0 or dev != _raw_device() or t.get_device() != dev or Wq.get_device() != dev or u.get_device() != dev
+            or bias is not None and bias.get_device() != dev or residual is not None and residual.get_device() != dev
+            or workspace is not None and workspace.get_device() != dev or out is not None and out.get_device() != dev):
+        _on_device("tlq_linear_i8_act", Xq, t, Wq, u, bias, residual, workspace, out)
+    if workspace is None:
+        workspace = _made_on(stream, linear_workspace, N, C1, C2, Xq.device)
+    if out is None:
+        out = _empty_on(Xq, stream)((N, width), dtype=_BF16)
+    else:
+        _typed(out, _BF16, (N, width), "out")
+    status = lib.tlq_linear_i8_act(Xq.data_ptr(), t.data_ptr(), N, C1, Wq.data_ptr(), u.data_ptr(), C2,
+                                   None if bias is None else bias.data_ptr(), act, 1 if gated else 0,
+                                   None if residual is None else residual.data_ptr(), ldr, workspace.data_ptr(), workspace.numel(),
+                                   out.data_ptr(), _stream(stream, dev))
+    if status:
+        raise TlqError(status, "tlq_linear_i8_act")
+    return out
+
+
+def gated_rows(gate: torch.Tensor, up: torch.Tensor) -> torch.Tensor:
+    """Rows of a gate and an up projection (codes, steps or biases) in the order that tlq_linear_i8_act takes: 2j gate, 2j + 1 up."""
+    if gate.shape != up.shape or gate.dtype is not up.dtype:
+        raise ValueError("gate and up must have one shape and type")
+    return torch.stack((gate, up), 1).flatten(0, 1)
+
+
+def tlq_norm_quantize(x: torch.Tensor, w: Optional[torch.Tensor], cfg: Optional[Config] = None, residual: Optional[torch.Tensor] = None,
+                      s: Optional[torch.Tensor] = None, eps: float = 1e-6, want_codes: bool = True, want_values: bool = False,
+                      want_y: bool = False, h: Optional[torch.Tensor] = None, stream=None):
+    """x bf16 [N,C], residual bf16 [N,C] or None (rows of both may be strided), w bf16 [C] or None, s bf16 [C] or None ->
+    dict(h, codes, steps, values, y): the sum x + residual (x itself without one), int8 codes [N,C] with steps [N] of its norm times
+    w / s, with want_values the values they stand for (bf16), with want_y the norm times w (bf16).  `h`: where the sum goes (x and
+    residual are allowed).  cfg: symmetric mode, 8 bits by default."""
+    N, C = x.shape
+    ldx = _rows(x, "x")
+    ldr = ldh = 0
+    if residual is not None:
+        ldr = _rows(residual, "residual")
+        if residual.shape != x.shape:
+            raise ValueError("x and residual must have one shape")
+    if w is not None and (w.dtype is not _BF16 or w.shape != (C,) or not w.is_contiguous()):
+        _typed(w, _BF16, (C,), "w")
+    if s is not None and (s.dtype is not _BF16 or s.shape != (C,) or not s.is_contiguous()):
+        _typed(s, _BF16, (C,), "s")
+    if not want_codes and (want_values or s is not None):
+        raise ValueError("values and s belong to codes")
+    dev = x.get_device()
+    if (dev < 0 or dev != _raw_device() or residual is not None and residual.get_device() != dev or w is not None and w.get_device() != dev
+            or s is not None and s.get_device() != dev or h is not None and h.get_device() != dev):
+        _on_device("tlq_norm_quantize", x, residual, w, s, h)
+    empty = _empty_on(x, stream)
+    if h is not None:
+        ldh = _rows(h, "h")
+        if h.shape != x.shape:
+            raise ValueError("h must have the shape of x")
+    elif residual is not None:
+        h, ldh = empty((N, C)), C
+    codes = steps = values = y = None
+    if want_codes:
+        codes, steps = empty((N, C), dtype=_I8), empty((N,), dtype=_F32)
+        if cfg is None:
+            cfg = _default_cfg()
+    if want_values:
+        values = empty((N, C))
+    if want_y:
+        y = empty((N, C))
+    ptr = lambda v: None if v is None else v.data_ptr()  # noqa: E731
+    status = _norm_quantize(x.data_ptr(), N, C, ldx, ptr(residual), ldr, ptr(w), eps, ptr(s), None if cfg is None else ctypes.addressof(cfg),
+                            ptr(h), ldh, ptr(codes), ptr(steps), ptr(values), ptr(y), _stream(stream, dev))
+    if status:
+        raise TlqError(status, "tlq_norm_quantize")
+    return dict(h=x if h is None else h, codes=codes, steps=steps, values=values, y=y)
+
+
+@functools.lru_cache(maxsize=1)
+def _default_cfg() -> Config:
+    return config(W8A8_SYM)
+
+
+_norm_quantize = _by_address("tlq_norm_quantize")
+
+
+# ----------------------------------------------------------------------------------------------- scoring
+# A model by its logits: see the scoring part of include/tlq.h.
+
+def _logits(t: torch.Tensor, what: str):
+    """Type number and row pitch of logits [N,V]."""
+    if t.dtype is not _BF16 and t.dtype is not _F32:
+        raise ValueError(f"{what} must be torch.bfloat16 or torch.float32, got {t.dtype}")
+    if t.ndim != 2 or t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what} must be [N,V] with the logits of a row one after another")
+    return (DTYPE_F32 if t.dtype is _F32 else DTYPE_BF16), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def tlq_token_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, top_k: int = 0, scale: float = 1.0,
+                       want_entropy: bool = False, want_lse: bool = False, stream=None):
+    """logits bf16 or float32 [N,V] (rows may be strided), ids int32 [N] or None (negative: no token) -> dict(logp, entropy, lse: float32 [N],
+    top_ids int32 [N,K], top_logp float32 [N,K]), None where not asked for: log probabilities of the given tokens under
+    softmax(scale * logits), its entropy and normaliser, and the top_k largest logits, largest first."""
+    kind, ld = _logits(logits, "logits")
+    N, V = logits.shape
+    if ids is not None and (ids.dtype is not _I32 or ids.shape != (N,) or not ids.is_contiguous()):
+        _typed(ids, _I32, (N,), "ids")
+    if not 0 <= top_k <= MAX_TOP:
+        raise ValueError(f"top_k must be 0 to {MAX_TOP}")
+    dev = logits.get_device()
+    if dev < 0 or dev != _raw_device() or ids is not None and ids.get_device() != dev:
+        _on_device("tlq_token_logprobs", logits, ids)
+    empty = _empty_on(logits, stream)
+    logp = None if ids is None else empty((N,), dtype=_F32)
+    entropy = empty((N,), dtype=_F32) if want_entropy else None
+    lse = empty((N,), dtype=_F32) if want_lse else None
+    top_ids = top_logp = None
+    if top_k:
+        top_ids, top_logp = empty((N, top_k), dtype=_I32), empty((N, top_k), dtype=_F32)
+    ptr = lambda v: None if v is None else v.data_ptr()  # noqa: E731
+    status = lib.tlq_token_logprobs(logits.data_ptr(), kind, N, V, ld, scale, ptr(ids), top_k, ptr(logp), ptr(entropy), ptr(lse),
+                                    ptr(top_ids), ptr(top_logp), _stream(stream, dev))
+    if status:
+        raise TlqError(status, "tlq_token_logprobs")
+    return dict(logp=logp, entropy=entropy, lse=lse, top_ids=top_ids, top_logp=top_logp)
+
+
+def tlq_distill_loss(logits: torch.Tensor, top_ids: torch.Tensor, top_logits: torch.Tensor, weights: Optional[torch.Tensor] = None,
+                     scale: float = 1.0, want_grad: bool = True, grad: Optional[torch.Tensor] = None, stream=None):
+    """logits bf16 or float32 [N,V] (rows may be strided), a teacher's top_ids int32 [N,K] (negative: empty place) and top_logits float32
+    [N,K], weights float32 [N] or None -> (loss float32 [N], grad of the logits' type [N,V] or None): weights times the divergence of
+    softmax(scale * logits) from the teacher's softmax over its K places, and the gradient of that by the logits.  `grad`: where it goes
+    (the logits themselves are allowed)."""
+    kind, ld = _logits(logits, "logits")
+    N, V = logits.shape
+    K = top_ids.shape[-1]
+    if top_ids.dtype is not _I32 or top_ids.shape != (N, K) or not top_ids.is_contiguous():
+        _typed(top_ids, _I32, (N, K), "top_ids")
+    if top_logits.dtype is not _F32 or top_logits.shape != (N, K) or not top_logits.is_contiguous():
+        _typed(top_logits, _F32, (N, K), "top_logits")
+    if weights is not None and (weights.dtype is not _F32 or weights.shape != (N,) or not weights.is_contiguous()):
+        _typed(weights, _F32, (N,), "weights")
+    dev = logits.get_device()
+    if (dev < 0 or dev != _raw_device() or top_ids.get_device() != dev or top_logits.get_device() != dev
+            or weights is not None and weights.get_device() != dev or grad is not None and grad.get_device() != dev):
+        _on_device("tlq_distill_loss", logits, top_ids, top_logits, weights, grad)
+    empty = _empty_on(logits, stream)
+    ldg = V
+    if grad is not None:
+        if grad.dtype is not logits.dtype or grad.shape != logits.shape:
+            raise ValueError("grad must have the type and shape of the logits")
+        ldg = _logits(grad, "grad")[1]
+    elif want_grad:
+        grad = empty((N, V))
+    loss = empty((N,), dtype=_F32)
+    status = lib.tlq_distill_loss(logits.data_ptr(), kind, N, V, ld, scale, top_ids.data_ptr(), top_logits.data_ptr(), K,
+                                  None if weights is None else weights.data_ptr(), loss.data_ptr(), None if grad is None else grad.data_ptr(),
+                                  ldg, _stream(stream, dev))
+    if status:
+        raise TlqError(status, "tlq_distill_loss")
+    return loss, grad
 
 
 def tlq_read_status(workspace: torch.Tensor, stream=None) -> int:
