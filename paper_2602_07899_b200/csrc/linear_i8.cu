@@ -76,12 +76,13 @@ linear_i8_few_kernel(const int8_t* X, const float* t, const int8_t* W, const flo
     for (int e = threadIdx.x; e < NT * 8 * (16 >> pair); e += kThreads) {
       const int r = (e & ((16 >> pair) - 1)) << pair, n = e >> (4 - pair);
       if (n0 + n >= N || o0 + r >= C2) continue;
-      float y = activate(epi.act, product(n, r));
-      if (pair) y *= product(n, r + 1);
+      float v[2] = {product(n, r), pair ? product(n, r + 1) : 0.f};
+      activate_all(epi.act, pair != 0, v);
+      float y = v[0];
       const int64_t o = (o0 + r) >> pair;
       if (epi.residual != nullptr) y += bf16_bits_to_float(epi.residual[(n0 + n) * epi.ldr + o]);
-      const __nv_bfloat16 v = __float2bfloat16_rn(y);
-      Y[(n0 + n) * width + o] = *reinterpret_cast<const uint16_t*>(&v);
+      const __nv_bfloat16 b = __float2bfloat16_rn(y);
+      Y[(n0 + n) * width + o] = *reinterpret_cast<const uint16_t*>(&b);
     }
     return;
   }
@@ -258,14 +259,8 @@ linear_i8_tile_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
         // channels o .. o + 3, or o / 2 and o / 2 + 1 of pairs (C2 is even then)
         const int64_t width = g.epi.gated ? g.C2 >> 1 : g.C2, at = g.epi.gated ? o >> 1 : o;
         const int count = (int)max((int64_t)0, min((int64_t)(g.epi.gated ? 2 : 4), width - at));
-        float v[4] = {activate(g.epi.act, y0), 0.f, activate(g.epi.act, y2), 0.f};
-        if (g.epi.gated) {
-          v[0] *= y1;
-          v[1] = v[2] * y3;
-        } else {
-          v[1] = activate(g.epi.act, y1);
-          v[3] = activate(g.epi.act, y3);
-        }
+        float v[4] = {y0, y1, y2, y3};
+        activate_all(g.epi.act, g.epi.gated != 0, v);
         uint16_t* out = g.Y + (n0 + c) * width + at;
         const uint16_t* res = g.epi.residual == nullptr ? nullptr : g.epi.residual + (n0 + c) * g.epi.ldr + at;
 #pragma unroll

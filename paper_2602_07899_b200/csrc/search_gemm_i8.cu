@@ -38,6 +38,8 @@ constexpr uint32_t kBBytes = BN * 128;
 constexpr uint32_t kStageBytes = kABytes + kBBytes;
 constexpr uint32_t kTmemCols = 512;
 constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + 256;
+constexpr uint32_t kEpiFloats = 2 * 128;  // steps and biases of an epilogue warp's columns, where there is an activation to apply
+constexpr size_t kSmemBytesEpi = kSmemBytes + kEpiWarps * kEpiFloats * sizeof(float);
 
 constexpr uint32_t kIdescBf16 = ptx::make_idesc(1, 1, BM, BN, false);   // bf16 x bf16 -> f32
 constexpr uint32_t kIdescBf16NegB = ptx::make_idesc(1, 1, BM, BN, true);
@@ -244,6 +246,15 @@ gemm_w8a8_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
       raster.decode(tile, mt, ot);
       const int64_t n = (int64_t)mt * BM + row_in_tile;
       const int64_t col_base = (int64_t)ot * BN + half * 128;
+      [[maybe_unused]] float* const steps = reinterpret_cast<float*>(smem_gen + kStages * kStageBytes + 256) + ew * kEpiFloats;
+      if constexpr (kMode == 3) {                 // read once for the tile; the warp's lanes all want the same ones at a time
+        for (int j = lane; j < 128; j += 32) {
+          const bool in = col_base + j < args.C2;
+          steps[j] = in ? args.u[col_base + j] : 0.f;
+          steps[128 + j] = in && args.bias != nullptr ? bf16_bits_to_float(args.bias[col_base + j]) : 0.f;
+        }
+        __syncwarp();
+      }
       for (int pass = 0; pass < passes; ++pass, ++it) {
         const int acc = (int)(it & 1);
         const uint32_t acc_phase = (uint32_t)((it >> 1) & 1);
@@ -325,18 +336,14 @@ gemm_w8a8_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
             if (n >= n_tokens || col >= args.C2) continue;
             float v[16];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const int64_t o = min(col + j, args.C2 - 1);     // (columns beyond the end are not stored)
-              v[j] = (float)(int)r[j] * (tn * __ldg(u_row + o));
-              if (args.bias != nullptr) v[j] += bf16_bits_to_float(args.bias[o]);
+            for (int j = 0; j < 16; j += 4) {
+              const float4 u = *reinterpret_cast<const float4*>(steps + c * 16 + j), b = *reinterpret_cast<const float4*>(steps + 128 + c * 16 + j);
+              v[j] = __fadd_rn(__fmul_rn((float)(int)r[j], tn * u.x), b.x);
+              v[j + 1] = __fadd_rn(__fmul_rn((float)(int)r[j + 1], tn * u.y), b.y);
+              v[j + 2] = __fadd_rn(__fmul_rn((float)(int)r[j + 2], tn * u.z), b.z);
+              v[j + 3] = __fadd_rn(__fmul_rn((float)(int)r[j + 3], tn * u.w), b.w);
             }
-            if (pair) {
-#pragma unroll
-              for (int j = 0; j < 8; ++j) v[j] = activate(args.epi.act, v[2 * j]) * v[2 * j + 1];
-            } else {
-#pragma unroll
-              for (int j = 0; j < 16; ++j) v[j] = activate(args.epi.act, v[j]);
-            }
+            activate_all(args.epi.act, pair != 0, v);
             const int64_t at = col >> pair;
             uint16_t* out = args.yq + n * width + at;
             const uint16_t* res = args.epi.residual == nullptr ? nullptr : args.epi.residual + n * args.epi.ldr + at;
@@ -437,7 +444,8 @@ template <int kMode>
 int configure_kernel() {
   static OncePerDevice once;
   return once_per_device(once, [] {
-    return cudaFuncSetAttribute(gemm_w8a8_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
+    return cudaFuncSetAttribute(gemm_w8a8_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                (int)(kMode == 3 ? kSmemBytesEpi : kSmemBytes));
   });
 }
 
@@ -524,7 +532,7 @@ int launch_apply_gemm_i8(const int8_t* Xq, const int8_t* Wq, const float* t, con
     a.epi = *epi;
     const int64_t width = epi->gated ? C2 / 2 : C2;
     a.whole8 = (width & 7) == 0 && (epi->residual == nullptr || ((epi->ldr & 7) == 0 && aligned16(epi->residual)));
-    gemm_w8a8_kernel<3><<<grid, kThreads, kSmemBytes, st>>>(tmXq, tmWq, tmXq, tmWq, a);
+    gemm_w8a8_kernel<3><<<grid, kThreads, kSmemBytesEpi, st>>>(tmXq, tmWq, tmXq, tmWq, a);
     return after_launch();
   }
   gemm_w8a8_kernel<1><<<grid, kThreads, kSmemBytes, st>>>(tmXq, tmWq, tmXq, tmWq, a);
