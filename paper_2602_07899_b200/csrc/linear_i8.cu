@@ -117,7 +117,7 @@ struct TileArgs {
   int num_kb, tile_n, stages, mtiles, splits;
   uint32_t tmem_cols;
   Epilogue epi;
-  bool even;                  // of a result with an epilogue: two channels lie at an address of 4 bytes, in Y and in the residual
+  int piece;                  // ... whose results and residual lie in rows of whole pieces of 4, 2 or 1 channels
 };
 
 __device__ __forceinline__ int4 ld_cluster(uint32_t addr) {
@@ -242,6 +242,67 @@ linear_i8_tile_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     uint32_t from[kMaxSplits];
 #pragma unroll
     for (int r = 0; r < kMaxSplits; ++r) from[r] = g.splits > 1 && r < g.splits ? ptx::map_to_cta(base, (uint32_t)r) : base;
+    if constexpr (kEpi) {
+      // channels o .. o + 3, or o / 2 and o / 2 + 1 of pairs (C2 is even then)
+      const bool gated = g.epi.gated != 0;
+      const int64_t width = gated ? g.C2 >> 1 : g.C2, to = gated ? o >> 1 : o;
+      const int count = (int)max((int64_t)0, min((int64_t)(gated ? 2 : 4), width - to));
+      auto finish = [&](int c, const int4& s, float t) {
+        float v[4] = {fmaf((float)s.x, t * u[0], b[0]), fmaf((float)s.y, t * u[1], b[1]), fmaf((float)s.z, t * u[2], b[2]),
+                      fmaf((float)s.w, t * u[3], b[3])};
+        activate_all(g.epi.act, gated, v);
+        uint16_t* out = g.Y + (n0 + c) * width + to;
+        const uint16_t* res = g.epi.residual == nullptr ? nullptr : g.epi.residual + (n0 + c) * g.epi.ldr + to;
+        if (count > 0 && g.piece >= (gated ? 2 : 4)) {       // all of them at an address that is a multiple of their size
+          uint2 r = make_uint2(0u, 0u);
+          if (res != nullptr && gated) r.x = load_near(reinterpret_cast<const uint32_t*>(res));
+          if (res != nullptr && !gated) r = load_near(reinterpret_cast<const uint2*>(res));
+          if (res != nullptr) {
+            v[0] += bf16_bits_to_float(r.x & 0xFFFFu); v[1] += bf16_bits_to_float(r.x >> 16);
+            v[2] += bf16_bits_to_float(r.y & 0xFFFFu); v[3] += bf16_bits_to_float(r.y >> 16);
+          }
+          const __nv_bfloat162 p0 = __floats2bfloat162_rn(v[0], v[1]), p1 = __floats2bfloat162_rn(v[2], v[3]);
+          r = make_uint2(*reinterpret_cast<const uint32_t*>(&p0), *reinterpret_cast<const uint32_t*>(&p1));
+          if (gated) *reinterpret_cast<uint32_t*>(out) = r.x;
+          else *reinterpret_cast<uint2*>(out) = r;
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (k >= count) continue;
+            if (res != nullptr) v[k] += bf16_bits_to_float(res[k]);
+            const __nv_bfloat16 p = __float2bfloat16_rn(v[k]);
+            out[k] = *reinterpret_cast<const uint16_t*>(&p);
+          }
+        }
+      };
+      constexpr int kStep = kTileThreads / 32;
+      if (g.splits == 1) {                                   // many tokens to a warp: four of them under way
+        for (int c = c0 + warp; c < c1; c += 4 * kStep) {
+          int4 s[4];
+          float t[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int at = min(c + k * kStep, c1 - 1);
+            t[k] = load_near(g.t + n0 + at);
+            s[k] = ld_cluster(base + (uint32_t)(at * kTileO + 4 * lane) * 4u);
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (c + k * kStep < c1) finish(c + k * kStep, s[k], t[k]);
+        }
+      } else {
+        for (int c = c0 + warp; c < c1; c += kStep) {
+          const uint32_t at = (uint32_t)(c * kTileO + 4 * lane) * 4u;
+          const float t = load_near(g.t + n0 + c);
+          int4 v[kMaxSplits];
+#pragma unroll
+          for (int r = 0; r < kMaxSplits; ++r) v[r] = r < g.splits ? ld_cluster(from[r] + at) : make_int4(0, 0, 0, 0);
+#pragma unroll
+          for (int r = 1; r < kMaxSplits; ++r) add(v[0], v[r]);
+          finish(c, v[0], t);
+        }
+      }
+    } else
     for (int c = c0 + warp; c < c1; c += kTileThreads / 32) {
       const uint32_t at = (uint32_t)(c * kTileO + 4 * lane) * 4u;
       const float t = load_near(g.t + n0 + c);
@@ -255,37 +316,6 @@ linear_i8_tile_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
       }
       const float y0 = fmaf((float)s.x, t * u[0], b[0]), y1 = fmaf((float)s.y, t * u[1], b[1]);
       const float y2 = fmaf((float)s.z, t * u[2], b[2]), y3 = fmaf((float)s.w, t * u[3], b[3]);
-      if constexpr (kEpi) {
-        // channels o .. o + 3, or o / 2 and o / 2 + 1 of pairs (C2 is even then)
-        const int64_t width = g.epi.gated ? g.C2 >> 1 : g.C2, at = g.epi.gated ? o >> 1 : o;
-        const int count = (int)max((int64_t)0, min((int64_t)(g.epi.gated ? 2 : 4), width - at));
-        float v[4] = {y0, y1, y2, y3};
-        activate_all(g.epi.act, g.epi.gated != 0, v);
-        uint16_t* out = g.Y + (n0 + c) * width + at;
-        const uint16_t* res = g.epi.residual == nullptr ? nullptr : g.epi.residual + (n0 + c) * g.epi.ldr + at;
-#pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-          if (j >= count) continue;
-          if (g.even) {                                      // (width is even, so that both are there)
-            if (res != nullptr) {
-              const uint32_t r = load_near(reinterpret_cast<const uint32_t*>(res + j));
-              v[j] += bf16_bits_to_float(r & 0xFFFFu);
-              v[j + 1] += bf16_bits_to_float(r >> 16);
-            }
-            const __nv_bfloat162 p = __floats2bfloat162_rn(v[j], v[j + 1]);
-            *reinterpret_cast<uint32_t*>(out + j) = *reinterpret_cast<const uint32_t*>(&p);
-          } else {
-#pragma unroll
-            for (int k = j; k < j + 2; ++k) {
-              if (k >= count) continue;
-              if (res != nullptr) v[k] += bf16_bits_to_float(res[k]);
-              const __nv_bfloat16 p = __float2bfloat16_rn(v[k]);
-              out[k] = *reinterpret_cast<const uint16_t*>(&p);
-            }
-          }
-        }
-        continue;
-      }
       const __nv_bfloat162 p0 = __floats2bfloat162_rn(y0, y1), p1 = __floats2bfloat162_rn(y2, y3);
       const uint2 w = make_uint2(*reinterpret_cast<const uint32_t*>(&p0), *reinterpret_cast<const uint32_t*>(&p1));
       uint16_t* y = g.Y + (n0 + c) * g.C2 + o;
@@ -355,7 +385,10 @@ int launch_tiles(const int8_t* Xq, const float* t, const int8_t* Wq, const float
   if (epi != nullptr) {
     g.epi = *epi;
     const int64_t width = epi->gated ? C2 / 2 : C2;
-    g.even = (width & 1) == 0 && (epi->residual == nullptr || ((epi->ldr & 1) == 0 && (reinterpret_cast<uintptr_t>(epi->residual) & 3u) == 0));
+    auto pieces = [&](int64_t n) {
+      return width % n == 0 && (epi->residual == nullptr || (epi->ldr % n == 0 && (reinterpret_cast<uintptr_t>(epi->residual) & (uintptr_t)(2 * n - 1)) == 0));
+    };
+    g.piece = pieces(4) ? 4 : pieces(2) ? 2 : 1;
   }
   const int rc = epi != nullptr ? configure_tiles<true>() : configure_tiles<false>();
   if (rc != TLQ_OK) return rc;

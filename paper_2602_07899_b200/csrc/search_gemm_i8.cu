@@ -63,12 +63,53 @@ struct I8Args {
   uint16_t* yq;            // apply
   WorkspaceHeader* hdr;
   Epilogue epi;            // apply with an epilogue
-  bool whole8;             // ... whose results and residual lie in rows of whole 16-byte pieces
+  int piece;               // ... whose results and residual lie in rows of whole pieces of 16, 8 or 1 channels
 };
 
 __device__ __forceinline__ void report_timeout(WorkspaceHeader* hdr, int where) {
   hdr->where = where;
   hdr->status = TLQ_ERR_TIMEOUT;
+}
+
+// The first `count` of 16 channels of a row, with what is added to them, as bf16.  `piece`: 16, 8 or 1 of them lie at an address that is a
+// multiple of their size (a row then has whole pieces only).
+__device__ __forceinline__ void store16(const float (&f)[16], uint16_t* out, const uint16_t* res, int64_t count, int piece) {
+  if (count <= 0) return;
+  uint32_t w[8];
+  if (piece == 1) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      if (j >= count) continue;
+      const __nv_bfloat16 b = __float2bfloat16_rn(res != nullptr ? f[j] + bf16_bits_to_float(res[j]) : f[j]);
+      out[j] = *reinterpret_cast<const uint16_t*>(&b);
+    }
+    return;
+  }
+  if (res != nullptr) {
+    if (piece == 16) {
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(res) : "memory");
+    } else {
+      const uint4 lo = *reinterpret_cast<const uint4*>(res), hi = count > 8 ? *reinterpret_cast<const uint4*>(res + 8) : make_uint4(0, 0, 0, 0);
+      w[0] = lo.x; w[1] = lo.y; w[2] = lo.z; w[3] = lo.w; w[4] = hi.x; w[5] = hi.y; w[6] = hi.z; w[7] = hi.w;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = 0;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const __nv_bfloat162 b = res == nullptr ? __floats2bfloat162_rn(f[2 * j], f[2 * j + 1])
+                                            : __floats2bfloat162_rn(f[2 * j] + bf16_bits_to_float(w[j] & 0xFFFFu), f[2 * j + 1] + bf16_bits_to_float(w[j] >> 16));
+    w[j] = *reinterpret_cast<const uint32_t*>(&b);
+  }
+  if (piece == 16) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(out), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+  } else {
+    *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
+    if (count > 8) *reinterpret_cast<uint4*>(out + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+  }
 }
 
 // kMode 0: W8A8-style search (one bf16 pass for the full-precision tile, then K int8 passes)
@@ -327,17 +368,17 @@ gemm_w8a8_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
           const int pair = args.epi.gated ? 1 : 0;             // C2 is even then: both rows of a pair are there
           const int64_t width = args.C2 >> pair;
 #pragma unroll 1
-          for (int c = 0; c < 8; ++c) {
-            uint32_t r[16];
+          for (int c = 0; c < 4; ++c) {
+            uint32_t r[32];
             __syncwarp();
-            ptx::tmem_ld16(taddr + c * 16, r);
+            ptx::tmem_ld32(taddr + c * 32, r);
             ptx::tmem_ld_wait();
-            const int64_t col = col_base + c * 16;
+            const int64_t col = col_base + c * 32;
             if (n >= n_tokens || col >= args.C2) continue;
-            float v[16];
+            float v[32];
 #pragma unroll
-            for (int j = 0; j < 16; j += 4) {
-              const float4 u = *reinterpret_cast<const float4*>(steps + c * 16 + j), b = *reinterpret_cast<const float4*>(steps + 128 + c * 16 + j);
+            for (int j = 0; j < 32; j += 4) {
+              const float4 u = *reinterpret_cast<const float4*>(steps + c * 32 + j), b = *reinterpret_cast<const float4*>(steps + 128 + c * 32 + j);
               v[j] = __fadd_rn(__fmul_rn((float)(int)r[j], tn * u.x), b.x);
               v[j + 1] = __fadd_rn(__fmul_rn((float)(int)r[j + 1], tn * u.y), b.y);
               v[j + 2] = __fadd_rn(__fmul_rn((float)(int)r[j + 2], tn * u.z), b.z);
@@ -347,33 +388,9 @@ gemm_w8a8_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
             const int64_t at = col >> pair;
             uint16_t* out = args.yq + n * width + at;
             const uint16_t* res = args.epi.residual == nullptr ? nullptr : args.epi.residual + n * args.epi.ldr + at;
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {                      // eight channels at a time, the second eight where rows are not paired
-              if (p == 1 && pair) continue;
-              if (at + p * 8 >= width) continue;
-              if (args.whole8) {
-                float f[8];
-                if (res != nullptr) {
-                  unpack8(*reinterpret_cast<const uint4*>(res + p * 8), f);
-#pragma unroll
-                  for (int j = 0; j < 8; ++j) v[p * 8 + j] += f[j];
-                }
-                uint32_t o[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  const __nv_bfloat162 b = __floats2bfloat162_rn(v[p * 8 + 2 * j], v[p * 8 + 2 * j + 1]);
-                  o[j] = *reinterpret_cast<const uint32_t*>(&b);
-                }
-                *reinterpret_cast<uint4*>(out + p * 8) = make_uint4(o[0], o[1], o[2], o[3]);
-              } else {
-#pragma unroll
-                for (int j = p * 8; j < p * 8 + 8; ++j) {
-                  if (at + j >= width) continue;
-                  const __nv_bfloat16 b = __float2bfloat16_rn(res != nullptr ? v[j] + bf16_bits_to_float(res[j]) : v[j]);
-                  out[j] = *reinterpret_cast<const uint16_t*>(&b);
-                }
-              }
-            }
+            // 16 channels at a time, the second 16 where rows are not paired: a whole sector of 32 bytes for a thread, whose row is its own
+            store16(*reinterpret_cast<const float(*)[16]>(v), out, res, width - at, args.piece);
+            if (!pair) store16(*reinterpret_cast<const float(*)[16]>(v + 16), out + 16, res == nullptr ? nullptr : res + 16, width - at - 16, args.piece);
           }
           ptx::tc_fence_before();
           __syncwarp();
@@ -531,7 +548,12 @@ int launch_apply_gemm_i8(const int8_t* Xq, const int8_t* Wq, const float* t, con
   if (epi != nullptr) {
     a.epi = *epi;
     const int64_t width = epi->gated ? C2 / 2 : C2;
-    a.whole8 = (width & 7) == 0 && (epi->residual == nullptr || ((epi->ldr & 7) == 0 && aligned16(epi->residual)));
+    auto whole = [&](int64_t n) {
+      const uintptr_t low = (uintptr_t)(2 * n - 1);
+      return width % n == 0 && (reinterpret_cast<uintptr_t>(Yq) & low) == 0 &&
+             (epi->residual == nullptr || (epi->ldr % n == 0 && (reinterpret_cast<uintptr_t>(epi->residual) & low) == 0));
+    };
+    a.piece = whole(16) ? 16 : whole(8) ? 8 : 1;
     gemm_w8a8_kernel<3><<<grid, kThreads, kSmemBytesEpi, st>>>(tmXq, tmWq, tmXq, tmWq, a);
     return after_launch();
   }
