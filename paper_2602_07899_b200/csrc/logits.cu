@@ -5,13 +5,17 @@
 //   lse = ln2 (m' + log2 S),  ln p_v = ln2 (d_v - log2 S),  entropy = ln S - ln2 T / S,
 //   grad_v = w scale (2^d_v / S - sum of the teacher's p at v).
 //
-// Maximum and sums run along in one pass (each thread with a maximum of its own, looked at once for a batch of loads), so that the
-// row is read from memory once; the loss then takes K logits of it.  The gradient reads the row a second time, from the second-level
-// cache: the rows under way at one time are kept to what stays there by giving a row to a cluster of CTAs.  The largest K: at the end of
-// the pass every thread knows the largest logit it has seen; the K-th largest of these is a bound below which nothing is wanted, and
-// only the threads above it look through their logits again.  Bound by memory; the exponentials take 3/4 of that time (16 bits).
+// Maximum and sums run along in one pass (each thread with a maximum of its own, looked at once for a batch of vectors), so that a row is
+// read from memory once.  Bound by memory; the exponentials take 3/4 of that time (16 bits).
+//  - Every warp has slots of shared memory of its own, into which it has pieces of the rows copied ahead of time, the next row's too, so
+//    that the memory has work while the CTA joins its sums, looks for the largest or writes; no warp waits for another but at a row's end.
+//  - The gradient needs the row a second time, and gets it from the second-level cache: a CTA has an SM to itself, and rows are shared by
+//    the CTAs of a cluster where those under way at one time would not stay there.  Both times come through the same slots.
+//  - The largest K: every thread notes the largest of each run of its vectors.  The K-th largest of what the threads have seen is a bound
+//    below which nothing is wanted, and only the runs that reach it are looked through again: little more than K of them.
 //
-// Rows may begin at any element: vectors of 16 bytes lie on the memory's own grid, those at a row's ends are read element by element.
+// Rows may begin at any element: vectors of 16 bytes lie on the memory's own grid, and what belongs to a neighbour is masked.  (16 bytes
+// at a multiple of 16 that hold an element of the row lie in the row's own memory page.)
 #include <type_traits>
 
 #include "serve.cuh"
@@ -22,8 +26,13 @@ namespace {
 
 constexpr int kMaxCluster = 8;
 constexpr int kMaxTop = TLQ_MAX_TOP;
-constexpr int kBatch = 4;                 // vectors of a thread under way at a time
-constexpr int kCandidates = 2048;         // logits that may be among the largest, as keys
+constexpr int kBatch = 4;                 // vectors that a thread works on at a time
+// Rows over 16 KB: CTAs of 256 threads, four to an SM, or of 256 to 1024 for the gradient; a warp has slots of kBatch vectors for each lane.
+constexpr int kShort = 128, kLong = 256;
+constexpr int kSlotsOnce = 3, kSlotsTop = 2;
+// Runs of batches of a thread that have a maximum of their own, and logits that may be among the largest (those of eight lists at least).
+__host__ __device__ constexpr int runs_of(int threads) { return threads == kShort ? 4 : 16; }
+constexpr int kCandidates = kMaxCluster * kMaxTop;
 constexpr float kMasked = -1.2676506002282294e30f;       // -2^100: logits from here down have probability 0
 constexpr uint32_t kMaskedPair = 0xF180F180u;            // the same, twice in bf16
 
@@ -41,6 +50,11 @@ __device__ __forceinline__ float2 halves(f32x2 v) {
 __device__ __forceinline__ f32x2 padd(f32x2 a, f32x2 b) {
   f32x2 r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 pmul(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
 __device__ __forceinline__ f32x2 pfma(f32x2 a, f32x2 b, f32x2 c) {
@@ -78,10 +92,11 @@ struct Elem<uint16_t> {
   __device__ static uint4 clamp(const uint4& v) {
     return make_uint4(max_bf16x2(v.x, kMaskedPair), max_bf16x2(v.y, kMaskedPair), max_bf16x2(v.z, kMaskedPair), max_bf16x2(v.w, kMaskedPair));
   }
-  __device__ static float largest(const uint4 (&v)[kBatch]) {
+  template <int n>
+  __device__ static float largest(const uint4 (&v)[n]) {
     uint32_t m = max_bf16x2(max_bf16x2(v[0].x, v[0].y), max_bf16x2(v[0].z, v[0].w));
 #pragma unroll
-    for (int u = 1; u < kBatch; ++u) m = max_bf16x2(m, max_bf16x2(max_bf16x2(v[u].x, v[u].y), max_bf16x2(v[u].z, v[u].w)));
+    for (int u = 1; u < n; ++u) m = max_bf16x2(m, max_bf16x2(max_bf16x2(v[u].x, v[u].y), max_bf16x2(v[u].z, v[u].w)));
     return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
   }
   __device__ static void pairs(const uint4& v, f32x2 (&x)[kPairs]) {
@@ -90,15 +105,17 @@ struct Elem<uint16_t> {
     for (int i = 0; i < 4; ++i) x[i] = pair_of(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
   }
   __device__ static uint32_t masked() { return kMaskedPair; }
-  __device__ static uint4 pack(const float (&f)[kVec]) {
+  __device__ static uint4 pack(const f32x2 (&x)[kPairs]) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+      const float2 f = halves(x[i]);
+      const __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
       w[i] = *reinterpret_cast<const uint32_t*>(&b);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
+  __device__ static void put_into(uint16_t* p, const uint4& v, int j) { *p = (uint16_t)((&v.x)[j >> 1] >> (j & 1) * 16); }
   __device__ static void put(uint4& v, int j, float f) {
     const uint32_t bits = __float_as_uint(f) >> 16;
     uint32_t* w = &v.x + (j >> 1);
@@ -114,10 +131,11 @@ struct Elem<float> {
     auto c = [](uint32_t w) { return __float_as_uint(max_nan(__uint_as_float(w), kMasked)); };
     return make_uint4(c(v.x), c(v.y), c(v.z), c(v.w));
   }
-  __device__ static float largest(const uint4 (&v)[kBatch]) {
+  template <int n>
+  __device__ static float largest(const uint4 (&v)[n]) {
     float m = kMasked;
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u)
+    for (int u = 0; u < n; ++u)
       m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(v[u].x), __uint_as_float(v[u].y)), fmaxf(__uint_as_float(v[u].z), __uint_as_float(v[u].w))));
     return m;
   }
@@ -126,9 +144,11 @@ struct Elem<float> {
     x[1] = pair_of(__uint_as_float(v.z), __uint_as_float(v.w));
   }
   __device__ static uint32_t masked() { return __float_as_uint(kMasked); }
-  __device__ static uint4 pack(const float (&f)[kVec]) {
-    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  __device__ static uint4 pack(const f32x2 (&x)[kPairs]) {
+    const float2 a = halves(x[0]), b = halves(x[1]);
+    return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
   }
+  __device__ static void put_into(float* p, const uint4& v, int j) { *p = __uint_as_float((&v.x)[j]); }
   __device__ static void put(uint4& v, int j, float f) { (&v.x)[j] = __float_as_uint(f); }
 };
 
@@ -146,15 +166,127 @@ struct Row {
   __device__ int first(int i) const { return i * Elem<T>::kVec - off; }
   __device__ bool whole(int i) const { return first(i) >= 0 && first(i) + Elem<T>::kVec <= V; }
   __device__ uint4 none() const { return make_uint4(Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked()); }
-  __device__ uint4 load(int i) const {
-    if (whole(i)) return load_once(z + first(i));
-    uint4 v = none();
+  // A piece from vector p on has no end of the row in it.
+  __device__ bool inside(int p) const { return first(p) >= 0 && p + 32 * kBatch < hi; }
+  // Vector i as it came, with what does not belong to the row masked.
+  __device__ uint4 own(uint4 v, int i) const {
+    if (!whole(i)) {
 #pragma unroll
-    for (int j = 0; j < Elem<T>::kVec; ++j)
-      if (first(i) + j >= 0 && first(i) + j < V) Elem<T>::put(v, j, Elem<T>::load(z + first(i) + j));
+      for (int j = 0; j < Elem<T>::kVec; ++j)
+        if (first(i) + j < 0 || first(i) + j >= V) Elem<T>::put(v, j, kMasked);
+    }
     return v;
   }
+  __device__ uint4 load(int i) const { return own(load_once(z + first(i)), i); }
 };
+
+struct Rows {                 // of one CTA: first, first + step, ...
+  const void* z;
+  int64_t ld, first, step, N;
+  int V, rank, ctas;
+  const float* weights;       // rows of weight 0 are not read, or null
+};
+// A warp's pieces of 32 kBatch vectors, row after row, in slots of its own: of each part of a row every (warps)th piece; with kAgain every row
+// a second time before the next.
+constexpr int kPiece = 32 * kBatch;
+constexpr uint32_t kPieceBytes = kPiece * 16;
+template <typename T, int kThreads, int kSlots, bool kAgain>
+struct Pieces {
+  const Rows& r;
+  int64_t n;                  // what comes next: `left` vectors from src on, of row n
+  const T* src;
+  int left;
+  bool second;
+  float w, w_next;            // (read a row ahead)
+  int slot;                   // what is read next
+  uint32_t data, bar, phase;  // ... this lane's first vector of it, its barrier, how often it was read
+
+  __device__ Pieces(const Rows& rows, const void* smem, uint64_t* barriers, int* abort)
+      : r(rows), n(r.first), left(0), second(false), w(1.f), w_next(1.f), slot(0), phase(0) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    data = ptx::smem_u32(smem) + (uint32_t)(warp * kSlots) * kPieceBytes + lane * 16u;
+    bar = ptx::smem_u32(barriers + warp * kSlots);
+    if (lane == 0) {
+      for (int k = 0; k < kSlots; ++k) ptx::mbar_init(bar + 8u * k, 1);
+      ptx::fence_barrier_init();
+    }
+    if (threadIdx.x == 0) *abort = 0;
+    __syncthreads();
+    if (r.weights != nullptr) {
+      w = load_near(r.weights + n);
+      if (n + r.step < r.N) w_next = load_near(r.weights + n + r.step);
+    }
+    begin();
+#pragma unroll
+    for (int k = 0; k < kSlots; ++k) fill(data + k * kPieceBytes, bar + 8u * k);
+  }
+  __device__ void begin() {
+    const Row<T> row(reinterpret_cast<const T*>(r.z), n, r.ld, r.V, r.rank, r.ctas);
+    const int first = row.lo + (int)(threadIdx.x >> 5) * kPiece;
+    src = row.z + row.first(first);
+    left = w == 0.f ? 0 : row.hi - first;
+  }
+  // On to the row that comes next, or to the same one again; false where there is none.
+  __device__ bool go_on() {
+    do {
+      if (n >= r.N) return false;
+      if (kAgain && !second && w != 0.f) {
+        second = true;
+      } else {
+        second = false;
+        n += r.step;
+        if (n >= r.N) return false;
+        if (r.weights != nullptr) {
+          w = w_next;
+          if (n + r.step < r.N) w_next = load_near(r.weights + n + r.step);
+        }
+      }
+      begin();
+    } while (left <= 0);
+    return true;
+  }
+  // The next piece into a slot; nothing where there is none.
+  __device__ void fill(uint32_t to, uint32_t to_bar) {
+    if (left <= 0 && !go_on()) return;
+    if ((threadIdx.x & 31) == 0) {
+      const uint32_t bytes = (uint32_t)min(kPiece, left) * 16u;
+      ptx::mbar_expect_tx(to_bar, bytes);
+      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                   ::"r"(to), "l"(src), "r"(bytes), "r"(to_bar) : "memory");
+    }
+    src += kThreads * kBatch * Elem<T>::kVec;
+    left -= kThreads * kBatch;
+  }
+  // The lane's vectors of the piece that is read next, whose slot then takes another one; false when it did not come within the limit of
+  // a wait, which no correct run reaches.  (A load from shared memory that is still on its way may be overtaken by a copy into the same
+  // place: the fence waits for it.)
+  __device__ bool next(uint4 (&v)[kBatch], int* abort) {
+    const bool ok = ptx::mbar_try_wait(bar, phase) || ptx::mbar_wait(bar, phase, abort);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[u].x), "=r"(v[u].y), "=r"(v[u].z), "=r"(v[u].w)
+                   : "r"(data + u * 512u) : "memory");
+    ptx::fence_proxy_async();
+    __syncwarp();
+    fill(data, bar);
+    data += kPieceBytes;
+    bar += 8u;
+    if (++slot == kSlots) {
+      slot = 0;
+      phase ^= 1u;
+      data -= kSlots * kPieceBytes;
+      bar -= 8u * kSlots;
+    }
+    return ok;
+  }
+};
+// Where a thread's vectors of a row are: the first of its batch number b, and how far apart those of a batch are.
+template <int kThreads>
+__device__ __forceinline__ int first_vector(int lo, int b) {
+  return lo + b * kThreads * kBatch + (kThreads == kShort ? (int)threadIdx.x : (int)(threadIdx.x >> 5) * 32 * kBatch + (int)(threadIdx.x & 31));
+}
+template <int kThreads>
+__device__ __forceinline__ constexpr int vector_step() { return kThreads == kShort ? kShort : 32; }
 
 // ---------------------------------------------------------------------------------------------- maximum and sums
 struct Stat {
@@ -181,9 +313,9 @@ __device__ __forceinline__ Stat merge_warp(const Stat& a, float c2) {
   return r;
 }
 
-struct RowShared {
-  Stat warps[16];
-  float cta[4];               // what the other CTAs of the cluster read
+struct RowShared {            // of two rows in turn: a warp may be a row ahead of one that still reads
+  Stat warps[2][32];
+  float cta[2][4];            // what the other CTAs of the cluster read
 };
 __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
   float v;
@@ -191,36 +323,31 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
   return v;
 }
 
-// Maximum and sums of the whole row, the same in every thread of every CTA of it; `mine`: the largest logit of this thread's vectors.
-template <typename T, bool kEntropy, int kThreads>
-__device__ __forceinline__ Stat row_stat(const Row<T>& row, float c2, int ctas, RowShared& sh, float& mine) {
-  constexpr int kWarps = kThreads / 32, kPairs = Elem<T>::kPairs;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  Stat a = empty_stat(c2);
-  const f32x2 cc = pair_of(c2, c2);
-  f32x2 s = pair_of(0.f, 0.f), t = s;
-  for (int i0 = row.lo + (int)threadIdx.x; i0 < row.hi; i0 += kBatch * kThreads) {
-    uint4 v[kBatch];
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) v[u] = i0 + u * kThreads < row.hi ? row.load(i0 + u * kThreads) : row.none();
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) v[u] = Elem<T>::clamp(v[u]);
-    const float m = fmaxf(a.m, Elem<T>::largest(v));          // (a NaN passes by here and shows in the sum)
-    if (m > a.m) {
-      const float mc = m * c2, d = a.mc - mc, f = exp2_fast(d);
+// A thread's own maximum and sums as its vectors come.
+template <typename T, bool kEntropy>
+struct Running {
+  float c2, m, mc;
+  f32x2 cc, s, t;
+  __device__ explicit Running(float c2_) : c2(c2_), m(kMasked), mc(kMasked * c2_), cc(pair_of(c2_, c2_)), s(pair_of(0.f, 0.f)), t(s) {}
+  // Returns the vectors' largest.
+  template <int n>
+  __device__ float add(const uint4 (&v)[n]) {
+    const float largest = Elem<T>::largest(v), top = fmaxf(m, largest);        // (a NaN passes by here and shows in the sum)
+    if (top > m) {
+      const float c = top * c2, d = mc - c, f = exp2_fast(d);
       const float2 s2 = halves(s), t2 = halves(t);
       if (kEntropy) t = pair_of(f * fmaf(s2.x, d, t2.x), f * fmaf(s2.y, d, t2.y));
       s = pair_of(s2.x * f, s2.y * f);
-      a.m = m;
-      a.mc = mc;
+      m = top;
+      mc = c;
     }
-    const f32x2 minus = pair_of(-a.mc, -a.mc);
+    const f32x2 minus = pair_of(-mc, -mc);
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      f32x2 x[kPairs];
+    for (int u = 0; u < n; ++u) {
+      f32x2 x[Elem<T>::kPairs];
       Elem<T>::pairs(v[u], x);
 #pragma unroll
-      for (int j = 0; j < kPairs; ++j) {
+      for (int j = 0; j < Elem<T>::kPairs; ++j) {
         const f32x2 d = pfma(x[j], cc, minus);
         const float2 d2 = halves(d);
         const f32x2 e = pair_of(exp2_fast(d2.x), exp2_fast(d2.y));
@@ -228,23 +355,50 @@ __device__ __forceinline__ Stat row_stat(const Row<T>& row, float c2, int ctas, 
         if (kEntropy) t = pfma(e, d, t);
       }
     }
+    return largest;
   }
-  mine = a.m;
-  a.s = halves(s).x + halves(s).y;
-  a.t = halves(t).x + halves(t).y;
+  __device__ Stat stat() const { return Stat{m, mc, halves(s).x + halves(s).y, halves(t).x + halves(t).y}; }
+};
+
+// A batch of vectors from i on, from the warp's slot or from memory, with what is not the row's masked, and with kClamp no value below the
+// mask's (which the entropy's terms 0 x -infinity need; without them the sums take any).
+template <typename T, int kThreads, bool kClamp, typename P, typename R>
+__device__ __forceinline__ void read_batch(const Row<T>& row, int i, P& pieces, int* abort, uint4 (&v)[kBatch], R& run) {
+  constexpr int kStep = vector_step<kThreads>();
+  if constexpr (kThreads != kShort) {
+    if (!pieces.next(v, abort)) run.s = pair_of(NAN, NAN);
+    if (!row.inside(i - (int)(threadIdx.x & 31))) {
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) v[u] = i + u * kStep < row.hi ? row.own(v[u], i + u * kStep) : row.none();
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) v[u] = i + u * kStep < row.hi ? row.load(i + u * kStep) : row.none();
+  }
+  if (kClamp) {
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) v[u] = Elem<T>::clamp(v[u]);
+  }
+}
+
+// Maximum and sums of the whole row from those of the threads, the same in every thread of every CTA of it.
+template <int kThreads>
+__device__ __forceinline__ Stat join_row(Stat a, float c2, int ctas, RowShared& sh, int parity) {
+  constexpr int kWarps = kThreads / 32;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   a = merge_warp(a, c2);
-  if (lane == 0) sh.warps[warp] = a;
+  if (lane == 0) sh.warps[parity][warp] = a;
   __syncthreads();
-  a = merge_warp(lane < kWarps ? sh.warps[lane] : empty_stat(c2), c2);
+  a = merge_warp(lane < kWarps ? sh.warps[parity][lane] : empty_stat(c2), c2);
   if (ctas > 1) {
     if (threadIdx.x == 0) {
-      sh.cta[0] = a.m; sh.cta[1] = a.mc; sh.cta[2] = a.s; sh.cta[3] = a.t;
+      sh.cta[parity][0] = a.m; sh.cta[parity][1] = a.mc; sh.cta[parity][2] = a.s; sh.cta[parity][3] = a.t;
     }
     __syncwarp();
     ptx::cluster_sync_all();
     a = empty_stat(c2);
     if (lane < ctas) {
-      const uint32_t from = ptx::map_to_cta(ptx::smem_u32(sh.cta), (uint32_t)lane);
+      const uint32_t from = ptx::map_to_cta(ptx::smem_u32(sh.cta[parity]), (uint32_t)lane);
       a.m = ld_cluster_f32(from); a.mc = ld_cluster_f32(from + 4); a.s = ld_cluster_f32(from + 8); a.t = ld_cluster_f32(from + 12);
     }
     __syncwarp();
@@ -264,17 +418,23 @@ __device__ __forceinline__ unsigned long long key_of(float x, int index) {
   return ((unsigned long long)in_order(x) << 32) | (0xFFFFFFFFu - (uint32_t)index);
 }
 
+template <int kThreads>
 struct TopShared {
-  unsigned long long keys[kCandidates];
+  static constexpr int kRuns = runs_of(kThreads);
+  union {
+    unsigned long long keys[kCandidates];
+    uint16_t runs[kRuns][kThreads];       // upper half of the order of the largest logit of each thread's runs, until they are listed
+  };
   unsigned long long top[kMaxTop];        // of this CTA's part, largest first
   unsigned long long all[kMaxTop];        // of the row
-  uint16_t threads[512];
-  int n_keys, n_threads;
+  uint32_t bounds[kThreads / 32];
+  uint16_t listed[kCandidates];           // runs that reach the bound: run kThreads + thread
+  int n_keys, n_listed;
 };
 
 // The K-th largest of the first n keys (n >= K).
 template <int kThreads>
-__device__ unsigned long long kth_key(const TopShared& sh, int n, int K) {
+__device__ unsigned long long kth_key(const TopShared<kThreads>& sh, int n, int K) {
   unsigned long long bound = 0;
   for (int bit = 63; bit >= 0; --bit) {
     const unsigned long long next = bound | (1ull << bit);
@@ -285,43 +445,67 @@ __device__ unsigned long long kth_key(const TopShared& sh, int n, int K) {
   return bound;
 }
 
-// The largest K of this CTA's part of the row into sh.top.  `mine`: the largest logit of this thread's vectors.
+// The largest K of this CTA's part of the row into sh.top.  `mine`: the largest logit of this thread's vectors; a run is `batches` batches.
 template <typename T, int kThreads>
-__device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine, TopShared& sh) {
+__device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine, int runs, int batches, TopShared<kThreads>& sh) {
   const int tid = threadIdx.x;
-  const bool any = row.lo + tid < row.hi;
-  const uint32_t own = any ? in_order(mine) : 0u;
-  // a bound that K threads at least reach (none where fewer have anything; the part is small then); the 16 lower bits of a bf16 say nothing
+  const bool any = first_vector<kThreads>(row.lo, 0) < row.hi;
+  const uint32_t own = any ? in_order(mine) >> 16 : 0u;
+  // A bound that K threads at least reach: in every warp its share of them does, found by bisection among the lanes.  (None where fewer have
+  // anything; the part is small then.)
+  const int vectors = row.hi - row.lo, here = __popc(__ballot_sync(0xFFFFFFFFu, any));
+  const int active = kThreads == kShort ? min(kThreads, vectors) : min(kThreads / 32, vectors / kPiece) * 32 + min(32, vectors % kPiece) * (vectors < kThreads * kBatch);
+  const int share = max(1, (K * here + active - 1) / max(active, 1));
   uint32_t bound = 0;
-  for (int bit = 31; bit >= (sizeof(T) == 2 ? 16 : 0); --bit) {
+  for (int bit = 15; bit >= 0; --bit) {
     const uint32_t next = bound | (1u << bit);
-    if (__syncthreads_count(own >= next) >= K) bound = next;
+    if (__popc(__ballot_sync(0xFFFFFFFFu, own >= next)) >= share) bound = next;
   }
-  if (tid == 0) sh.n_threads = 0;
+  if ((tid & 31) == 0) sh.bounds[tid >> 5] = bound;
+  if (tid == 0) sh.n_listed = 0;
   if (tid < K) sh.top[tid] = 0;
   __syncthreads();
-  if (any && own >= bound) sh.threads[atomicAdd(&sh.n_threads, 1)] = (uint16_t)tid;
+#pragma unroll
+  for (int k = 0; k < kThreads / 32; ++k) bound = min(bound, sh.bounds[k]);
+  if (any && own >= bound) {
+    uint32_t x[TopShared<kThreads>::kRuns];
+#pragma unroll
+    for (int r = 0; r < TopShared<kThreads>::kRuns; ++r) x[r] = sh.runs[r][tid];
+#pragma unroll
+    for (int r = 0; r < TopShared<kThreads>::kRuns; ++r)
+      if (r < runs && x[r] >= bound) {
+        const int at = atomicAdd(&sh.n_listed, 1);
+        if (at < kCandidates) sh.listed[at] = (uint16_t)(r * kThreads + tid);
+      }
+  }
+  if (tid == 0) sh.n_keys = 0;
   __syncthreads();
-  const int listed = sh.n_threads, columns = (row.hi - row.lo + kThreads - 1) / kThreads;
-  unsigned long long least = (unsigned long long)bound << 32;
+  // all of them where there are more than the list holds (equal logits in every run)
+  const bool all = sh.n_listed > kCandidates;
+  const int total = (all ? runs * kThreads : sh.n_listed) * batches;
+  unsigned long long least = (unsigned long long)bound << 48;
   int n;
   while (true) {
-    if (tid == 0) sh.n_keys = 0;
-    __syncthreads();
-    for (int k = tid; k < listed * columns; k += kThreads) {
-      const int i = row.lo + sh.threads[k % listed] + k / listed * kThreads;
-      if (i >= row.hi) continue;
-      const uint4 v = Elem<T>::clamp(row.load(i));
-      f32x2 x[Elem<T>::kPairs];
-      Elem<T>::pairs(v, x);
+    for (int k = tid; k < total; k += kThreads) {
+      const int e = batches == 1 ? k : k / batches, which = all ? e : sh.listed[e], t = which % kThreads;
+      const int i = row.lo + (which / kThreads * batches + k - e * batches) * kThreads * kBatch + (kThreads == kShort ? t : (t >> 5) * kPiece + (t & 31));
+      uint4 v[kBatch];
 #pragma unroll
-      for (int j = 0; j < Elem<T>::kVec; ++j) {
-        const float2 h = halves(x[j >> 1]);
-        const int e = row.first(i) + j;
-        const unsigned long long key = key_of((j & 1) ? h.y : h.x, e);
-        if (key >= least && e >= 0 && e < row.V) {
-          const int at = atomicAdd(&sh.n_keys, 1);
-          if (at < kCandidates) sh.keys[at] = key;
+      for (int u = 0; u < kBatch; ++u)
+        v[u] = i + u * vector_step<kThreads>() < row.hi ? load_once(row.z + row.first(i + u * vector_step<kThreads>())) : row.none();
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        f32x2 x[Elem<T>::kPairs];
+        Elem<T>::pairs(Elem<T>::clamp(v[u]), x);
+#pragma unroll
+        for (int j = 0; j < Elem<T>::kVec; ++j) {
+          const float2 h = halves(x[j >> 1]);
+          const int at = row.first(i + u * vector_step<kThreads>()) + j;
+          const unsigned long long key = key_of((j & 1) ? h.y : h.x, at);
+          if (key >= least && at >= 0 && at < row.V && i + u * vector_step<kThreads>() < row.hi) {
+            const int to = atomicAdd(&sh.n_keys, 1);
+            if (to < kCandidates) sh.keys[to] = key;
+          }
         }
       }
     }
@@ -330,13 +514,16 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
     if (n <= kCandidates) break;
     least = kth_key<kThreads>(sh, kCandidates, K);            // more than there is room for: a higher bound, from those there was room for
     __syncthreads();
+    if (tid == 0) sh.n_keys = 0;
+    __syncthreads();
   }
   // each key's place is the number of larger ones; with many of them only the largest K are placed
-  if (n > kThreads / 2 && n > K) least = kth_key<kThreads>(sh, n, K);
+  if (n > 512 && n > K) least = kth_key<kThreads>(sh, n, K);
   for (int i = tid; i < n; i += kThreads) {
     const unsigned long long key = sh.keys[i];
     if (key < least) continue;
     int place = 0;
+#pragma unroll 4
     for (int j = 0; j < n; ++j) place += sh.keys[j] > key;
     if (place < K) sh.top[place] = key;
   }
@@ -345,7 +532,7 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
 
 // The row's from its CTAs' lists, into sh.all of the first CTA.
 template <int kThreads>
-__device__ __forceinline__ void join_tops(int K, int ctas, int rank, TopShared& sh) {
+__device__ __forceinline__ void join_tops(int K, int ctas, int rank, TopShared<kThreads>& sh) {
   ptx::cluster_sync_all();
   if (rank == 0) {
     for (int i = threadIdx.x; i < ctas * K; i += kThreads) {
@@ -376,8 +563,8 @@ __device__ __forceinline__ void join_tops(int K, int ctas, int rank, TopShared& 
 // ---------------------------------------------------------------------------------------------- log probabilities
 struct LogprobArgs {
   const void* z;
-  int64_t ld;
-  int V, ctas, K;
+  int64_t N, ld;
+  int V, ctas, K, batches;    // batches of a run
   float c2;                   // scale log2(e)
   const int32_t* ids;
   float* logp;
@@ -394,53 +581,83 @@ __device__ __forceinline__ float log_p(float x, const Stat& a, float c2, float l
   return kLn2 * (fmaf(x, c2, -a.mc) - log2_s);
 }
 
+// Long rows come through slots, short ones straight from memory.
 template <typename T, bool kEntropy, bool kTop, int kThreads>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
 logprobs_kernel(const LogprobArgs g) {
+  constexpr bool kSlots = kThreads != kShort;
+  extern __shared__ __align__(128) uint8_t slots[];
   __shared__ RowShared sh;
-  __shared__ typename std::conditional<kTop, TopShared, int>::type top;
+  __shared__ typename std::conditional<kTop, TopShared<kThreads>, int>::type top;
+  __shared__ uint64_t barriers[kSlots ? kSlotsOnce * kThreads / 32 : 1];
+  __shared__ int abort;
   after_previous();
   const int rank = (int)(blockIdx.x % (unsigned)g.ctas);
-  const int64_t n = blockIdx.x / (unsigned)g.ctas;
-  const Row<T> row(reinterpret_cast<const T*>(g.z), n, g.ld, g.V, rank, g.ctas);
-  int id = -1;
-  float z_id = 0.f;
-  if (rank == 0 && threadIdx.x == 0 && g.ids != nullptr) {
-    id = load_near(g.ids + n);
-    if (id >= 0 && id < g.V) z_id = Elem<T>::load(row.z + id);
-  }
-  float mine;
-  const Stat a = row_stat<T, kEntropy, kThreads>(row, g.c2, g.ctas, sh, mine);
-  const float log2_s = log2f(a.s);
-  if (rank == 0 && threadIdx.x == 0) {
-    const bool none = a.m <= kMasked && !isnan(a.s);
-    if (g.ids != nullptr) g.logp[n] = id < 0 ? 0.f : id >= g.V ? NAN : log_p(z_id, a, g.c2, log2_s);
-    if (g.lse != nullptr) g.lse[n] = none ? -INFINITY : isnan(a.s) ? NAN : kLn2 * (a.mc + log2_s);
-    if (kEntropy) g.entropy[n] = none ? 0.f : kLn2 * (log2_s - a.t / a.s);
-  }
-  if constexpr (kTop) {
-    const bool bad = isnan(a.s);                              // (the same in all CTAs of the row)
-    if (!bad) {
-      top_of_part<T, kThreads>(row, g.K, mine, top);
-      if (g.ctas > 1) join_tops<kThreads>(g.K, g.ctas, rank, top);
+  const Rows rows{g.z, g.ld, blockIdx.x / (unsigned)g.ctas, gridDim.x / (unsigned)g.ctas, g.N, g.V, rank, g.ctas, nullptr};
+  typename std::conditional<kSlots, Pieces<T, kThreads, kTop ? kSlotsTop : kSlotsOnce, false>, int>::type pieces = [&] {
+    if constexpr (kSlots) return Pieces<T, kThreads, kTop ? kSlotsTop : kSlotsOnce, false>(rows, slots, barriers, &abort);
+    else return 0;
+  }();
+  int parity = 0;
+  for (int64_t n = rows.first; n < g.N; n += rows.step, parity ^= 1) {
+    const Row<T> row(reinterpret_cast<const T*>(g.z), n, g.ld, g.V, rank, g.ctas);
+    int id = -1;
+    float z_id = 0.f;
+    if (rank == 0 && threadIdx.x == 0 && g.ids != nullptr) {
+      id = load_near(g.ids + n);
+      if (id >= 0 && id < g.V) z_id = Elem<T>::load(row.z + id);
     }
-    if (rank == 0 && (int)threadIdx.x < g.K) {
-      const unsigned long long key = bad ? 0 : g.ctas > 1 ? top.all[threadIdx.x] : top.top[threadIdx.x];
-      const int64_t at = n * g.K + threadIdx.x;
-      g.top_ids[at] = key == 0 ? -1 : (int)(0xFFFFFFFFu - (uint32_t)key);
-      g.top_logp[at] = bad ? NAN : key == 0 ? -INFINITY : log_p(of_order((uint32_t)(key >> 32)), a, g.c2, log2_s);
+    Running<T, kEntropy> run(g.c2);
+    float run_top = kMasked;
+    int batch = 0;
+    for (int i = first_vector<kThreads>(row.lo, 0); i - (kSlots ? (int)(threadIdx.x & 31) : (int)threadIdx.x) < row.hi; i += kBatch * kThreads, ++batch) {
+      uint4 v[kBatch];
+      read_batch<T, kThreads, kEntropy>(row, i, pieces, &abort, v, run);
+      const float largest = run.add(v);
+      if constexpr (kTop) {
+        run_top = fmaxf(run_top, largest);
+        if ((batch + 1) % g.batches == 0) {
+          top.runs[batch / g.batches][threadIdx.x] = (uint16_t)(in_order(run_top) >> 16);
+          run_top = kMasked;
+        }
+      }
+    }
+    if constexpr (kTop)
+      if (batch % g.batches != 0) top.runs[batch / g.batches][threadIdx.x] = (uint16_t)(in_order(run_top) >> 16);
+    const Stat a = join_row<kThreads>(run.stat(), g.c2, g.ctas, sh, parity);
+    const float log2_s = log2f(a.s);
+    if (rank == 0 && threadIdx.x == 0) {
+      const bool none = a.m <= kMasked && !isnan(a.s);
+      if (g.ids != nullptr) g.logp[n] = id < 0 ? 0.f : id >= g.V ? NAN : log_p(z_id, a, g.c2, log2_s);
+      if (g.lse != nullptr) g.lse[n] = none ? -INFINITY : isnan(a.s) ? NAN : kLn2 * (a.mc + log2_s);
+      if (kEntropy) g.entropy[n] = none ? 0.f : kLn2 * (log2_s - a.t / a.s);
+    }
+    if constexpr (kTop) {
+      const bool bad = isnan(a.s);                            // (the same in all CTAs of the row)
+      if (!bad) {
+        top_of_part<T, kThreads>(row, g.K, run.m, (batch + g.batches - 1) / g.batches, g.batches, top);
+        if (g.ctas > 1) join_tops<kThreads>(g.K, g.ctas, rank, top);
+      }
+      if (rank == 0 && (int)threadIdx.x < g.K) {
+        const unsigned long long key = bad ? 0 : g.ctas > 1 ? top.all[threadIdx.x] : top.top[threadIdx.x];
+        const int64_t to = n * g.K + threadIdx.x;
+        g.top_ids[to] = key == 0 ? -1 : (int)(0xFFFFFFFFu - (uint32_t)key);
+        g.top_logp[to] = bad ? NAN : key == 0 ? -INFINITY : log_p(of_order((uint32_t)(key >> 32)), a, g.c2, log2_s);
+      }
     }
   }
   if (g.ctas > 1) {
     __syncwarp();
     ptx::cluster_sync_all();                                  // nobody leaves while its shared memory is read
   }
+  if (kSlots && *reinterpret_cast<volatile int*>(&abort) != 0)
+    for (int i = 0; i < 1000; ++i) __nanosleep(1000);         // copies under way land before the shared memory is given back
 }
 
 // ---------------------------------------------------------------------------------------------- distillation
 struct DistillArgs {
   const void* z;
-  int64_t ld;
+  int64_t N, ld;
   int V, ctas, K;
   float c2, scale;
   const int32_t* ids;
@@ -451,201 +668,310 @@ struct DistillArgs {
   int64_t ldg;
 };
 
-struct DistillShared {
-  int id[kMaxTop];
-  float t[kMaxTop], z[kMaxTop], p[kMaxTop];
-  float loss;
-  int teacher;                // 0: the row has none, 1: it has, 2: an id outside of the vocabulary
+struct DistillShared {        // of two rows in turn
+  int id[2][kMaxTop];
+  float t[2][kMaxTop], z[2][kMaxTop], p[2][kMaxTop];
+  uint32_t flags[2][kMaxTop / 32];  // of each warp's places: 1 there is a teacher, 2 an id outside of the vocabulary
 };
+
+// p = softmax over the places, and the row's loss: by one warp, a lane has every 32nd place.
+__device__ __forceinline__ float teacher_loss(const DistillArgs& g, const Stat& a, DistillShared& d, int parity) {
+  constexpr int kPer = kMaxTop / 32;
+  const int lane = threadIdx.x & 31;
+  float x[kPer], top = kMasked;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int i = lane + 32 * k;
+    x[k] = i < g.K ? d.t[parity][i] : kMasked;
+    top = fmaxf(top, x[k]);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+  const float tc = top * g.c2;
+  float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) sum += x[k] <= kMasked ? 0.f : exp2_fast(fmaf(x[k], g.c2, -tc));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+  const float logs = log2f(a.s) - log2f(sum);
+  float loss = 0.f;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int i = lane + 32 * k;
+    if (i >= g.K) continue;
+    const float dt = fmaf(x[k], g.c2, -tc), p = x[k] <= kMasked ? 0.f : __fdiv_rn(exp2_fast(dt), sum);
+    d.p[parity][i] = p;
+    if (p == 0.f) continue;
+    const float z = d.z[parity][i];
+    loss += z <= kMasked ? INFINITY : p * ((dt - fmaf(z, g.c2, -a.mc)) + logs);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xFFFFFFFFu, loss, o);
+  return kLn2 * loss;
+}
 
 template <typename T, bool kGrad, int kThreads>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
 distill_kernel(const DistillArgs g) {
-  constexpr int kVec = Elem<T>::kVec;
+  constexpr bool kSlots = kThreads != kShort;
+  constexpr int kVec = Elem<T>::kVec, kStep = vector_step<kThreads>();
+  extern __shared__ __align__(128) uint8_t slots[];
   __shared__ RowShared sh;
   __shared__ DistillShared d;
+  __shared__ uint64_t barriers[kSlots ? kSlotsOnce * kThreads / 32 : 1];
+  __shared__ int abort;
   after_previous();
-  const int tid = threadIdx.x, lane = tid & 31;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = (int)(blockIdx.x % (unsigned)g.ctas);
-  const int64_t n = blockIdx.x / (unsigned)g.ctas;
-  const Row<T> row(reinterpret_cast<const T*>(g.z), n, g.ld, g.V, rank, g.ctas);
-  T* grad = kGrad ? reinterpret_cast<T*>(g.grad) + n * g.ldg : nullptr;
-  const bool aligned = kGrad && ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(row.z)) & 15u) == 0;
-  auto store = [&](int i, const float (&f)[kVec]) {
-    if (aligned && row.whole(i)) {
-      *reinterpret_cast<uint4*>(grad + row.first(i)) = Elem<T>::pack(f);
-    } else {
+  const Rows rows{g.z, g.ld, blockIdx.x / (unsigned)g.ctas, gridDim.x / (unsigned)g.ctas, g.N, g.V, rank, g.ctas, g.weights};
+  typename std::conditional<kSlots, Pieces<T, kThreads, kSlotsOnce, kGrad>, int>::type pieces = [&] {
+    if constexpr (kSlots) return Pieces<T, kThreads, kSlotsOnce, kGrad>(rows, slots, barriers, &abort);
+    else return 0;
+  }();
+  int parity = 0;
+  float w = g.weights != nullptr ? load_near(g.weights + rows.first) : 1.f, w_next = 1.f;
+  for (int64_t n = rows.first; n < g.N; n += rows.step, w = w_next) {
+    if (g.weights != nullptr && n + rows.step < g.N) w_next = load_near(g.weights + n + rows.step);
+    const Row<T> row(reinterpret_cast<const T*>(g.z), n, g.ld, g.V, rank, g.ctas);
+    T* grad = kGrad ? reinterpret_cast<T*>(g.grad) + n * g.ldg : nullptr;
+    const bool aligned = kGrad && ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(row.z)) & 15u) == 0;
+    auto store = [&](int i, const uint4& y) {
+      if (aligned && row.whole(i)) {
+        *reinterpret_cast<uint4*>(grad + row.first(i)) = y;
+      } else {
 #pragma unroll
-      for (int j = 0; j < kVec; ++j)
-        if (row.first(i) + j >= 0 && row.first(i) + j < row.V) Elem<T>::store(grad + row.first(i) + j, f[j]);
+        for (int j = 0; j < kVec; ++j)
+          if (row.first(i) + j >= 0 && row.first(i) + j < row.V) Elem<T>::put_into(grad + row.first(i) + j, y, j);
+      }
+    };
+    auto store_zeros = [&]() {
+      for (int i = row.lo + tid; i < row.hi; i += kThreads) store(i, make_uint4(0, 0, 0, 0));
+    };
+    if (w == 0.f) {                                           // the same for all CTAs of the row, which is not read
+      if (rank == 0 && tid == 0) g.loss[n] = 0.f;
+      if (kGrad) store_zeros();
+      continue;
     }
-  };
-  auto store_zeros = [&]() {
-    float f[kVec];
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) f[j] = 0.f;
-    for (int i = row.lo + tid; i < row.hi; i += kThreads) store(i, f);
-  };
-  const float w = g.weights != nullptr ? load_near(g.weights + n) : 1.f;
-  if (w == 0.f) {                                             // the same for all CTAs of the row
-    if (rank == 0 && tid == 0) g.loss[n] = 0.f;
-    if (kGrad) store_zeros();
-    return;
-  }
-  // the teacher's places, and the student's logits there: read before a gradient may be written over them
-  if (tid < g.K) {
-    const int id = load_near(g.ids + n * g.K + tid);
-    d.id[tid] = id;
-    d.t[tid] = load_near(g.top + n * g.K + tid);
-    d.z[tid] = id >= 0 && id < g.V ? Elem<T>::load(row.z + id) : kMasked;
-  }
-  float mine;
-  const Stat a = row_stat<T, false, kThreads>(row, g.c2, g.ctas, sh, mine);
-  if (tid < 32) {
-    // p = softmax over the places: a lane has every 32nd
-    constexpr int kPer = kMaxTop / 32;
-    const float log2_s = log2f(a.s);
-    float x[kPer], top = kMasked;
-    bool outside = false;
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const int i = lane + 32 * k, id = i < g.K ? d.id[i] : -1;
-      outside |= id >= g.V;
-      x[k] = id >= 0 ? max_nan(d.t[i], kMasked) : kMasked;
-      top = fmaxf(top, x[k]);
+    int id = -1;
+    float teacher = kMasked, z_id = kMasked;
+    if (tid < g.K) {
+      id = load_near(g.ids + n * g.K + tid);
+      teacher = load_near(g.top + n * g.K + tid);
     }
-    bool any = false;
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) any |= !(x[k] <= kMasked);  // (a NaN counts)
-    const int teacher = __any_sync(0xFFFFFFFFu, outside) ? 2 : __any_sync(0xFFFFFFFFu, any) ? 1 : 0;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    const float tc = top * g.c2;
-    float sum = 0.f;
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) sum += x[k] <= kMasked ? 0.f : exp2_fast(fmaf(x[k], g.c2, -tc));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-    const float log2_t = log2f(sum);
-    float loss = 0.f;
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const int i = lane + 32 * k;
-      if (i >= g.K) continue;
-      const float dt = fmaf(x[k], g.c2, -tc), p = x[k] <= kMasked ? 0.f : __fdiv_rn(exp2_fast(dt), sum);
-      d.p[i] = p;
-      if (p == 0.f) continue;
-      const float z = d.z[i];
-      loss += z <= kMasked ? INFINITY : p * ((dt - fmaf(z, g.c2, -a.mc)) + (log2_s - log2_t));
+    Running<T, false> run(g.c2);
+    const int i0 = first_vector<kThreads>(row.lo, 0), lead = kSlots ? lane : tid;
+    for (int i = i0; i - lead < row.hi; i += kBatch * kThreads) {
+      uint4 v[kBatch];
+      read_batch<T, kThreads, false>(row, i, pieces, &abort, v, run);
+      run.add(v);
+      // the student's logits at the teacher's places: read before a gradient may be written over them
+      if (i == i0 && tid < g.K && id >= 0 && id < g.V) z_id = Elem<T>::load(row.z + id);
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xFFFFFFFFu, loss, o);
-    if (lane == 0) {
-      d.teacher = teacher;
-      if (rank == 0) g.loss[n] = teacher == 0 ? 0.f : teacher == 2 || isnan(a.s) ? NAN : w * (kLn2 * loss);
+    if (i0 - lead >= row.hi && tid < g.K && id >= 0 && id < g.V) z_id = Elem<T>::load(row.z + id);
+    if (tid < g.K) {
+      d.id[parity][tid] = id;
+      d.t[parity][tid] = id >= 0 ? max_nan(teacher, kMasked) : kMasked;
+      d.z[parity][tid] = max_nan(z_id, kMasked);
     }
-  }
-  if constexpr (kGrad) {
-    __syncthreads();
-    const bool bad = d.teacher == 2 || isnan(a.s);
-    if (d.teacher == 0 || (!bad && a.m <= kMasked)) {
-      store_zeros();
-    } else {
-      const float gp = w * g.scale, gq = bad ? NAN : gp / a.s;
+    const bool there = tid < g.K && id >= 0;
+    const uint32_t flags = (__any_sync(0xFFFFFFFFu, there && !(teacher <= kMasked)) ? 1u : 0u) | (__any_sync(0xFFFFFFFFu, there && id >= g.V) ? 2u : 0u);
+    if (lane == 0 && warp < kMaxTop / 32) d.flags[parity][warp] = flags;
+    const Stat a = join_row<kThreads>(run.stat(), g.c2, g.ctas, sh, parity);
+    uint32_t all = 0;
+#pragma unroll
+    for (int k = 0; k < kMaxTop / 32; ++k) all |= d.flags[parity][k];
+    const bool bad = isnan(a.s) || (all & 2u) != 0;           // (an id outside of the vocabulary, or a row that is no number)
+    const bool none = all == 0;                               // no teacher
+    if (warp == 0 && !none) {
+      const float loss = teacher_loss(g, a, d, parity);
+      if (rank == 0 && lane == 0) g.loss[n] = bad ? NAN : w * loss;
+    }
+    if (none && rank == 0 && tid == 0) g.loss[n] = 0.f;
+    if constexpr (kGrad) {
+      const bool zeros = none || (!bad && a.m <= kMasked);
+      const float gp = zeros ? 0.f : w * g.scale;
+      const float gq = zeros ? 0.f : bad ? NAN : gp / a.s;
+      bool late = false;                                      // (a copy that did not come in time: the row is no number)
       const f32x2 cc = pair_of(g.c2, g.c2), minus = pair_of(-a.mc, -a.mc);
-      for (int i0 = row.lo + tid; i0 < row.hi; i0 += kBatch * kThreads) {
+      const f32x2 scale2 = pair_of(gq, gq);
+      const uint32_t keep = zeros ? 0u : 0xFFFFFFFFu;
+      uint4* const out = reinterpret_cast<uint4*>(grad - row.off);      // vector 0, where the gradient lies as the logits do
+      for (int i = i0; i - lead < row.hi; i += kBatch * kThreads) {
         uint4 v[kBatch];
+        if constexpr (kSlots) {
+          if (!pieces.next(v, &abort)) late = true;
+        } else {
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) v[u] = i0 + u * kThreads < row.hi ? row.load(i0 + u * kThreads) : row.none();
+          for (int u = 0; u < kBatch; ++u) v[u] = i + u * kStep < row.hi ? row.load(i + u * kStep) : row.none();
+        }
+        const bool inside = kSlots && aligned && row.inside(i - lane);
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-          if (i0 + u * kThreads >= row.hi) continue;
           f32x2 x[Elem<T>::kPairs];
-          Elem<T>::pairs(Elem<T>::clamp(v[u]), x);
-          float f[kVec];
+          Elem<T>::pairs(v[u], x);
 #pragma unroll
-          for (int j = 0; j < Elem<T>::kPairs; ++j) {
-            const float2 e = halves(pfma(x[j], cc, minus));
-            f[2 * j] = exp2_fast(e.x) * gq;
-            f[2 * j + 1] = exp2_fast(e.y) * gq;
+          for (int q = 0; q < Elem<T>::kPairs; ++q) {
+            const float2 e = halves(pfma(x[q], cc, minus));
+            x[q] = pmul(pair_of(exp2_fast(e.x), exp2_fast(e.y)), scale2);
           }
-          store(i0 + u * kThreads, f);
+          uint4 y = Elem<T>::pack(x);
+          y.x &= keep; y.y &= keep; y.z &= keep; y.w &= keep;
+          if (inside) out[i + u * kStep] = y;
+          else if (i + u * kStep < row.hi) store(i + u * kStep, y);
         }
       }
       __syncthreads();
       // the teacher's places of this CTA's part, after the barrier: each with all of its p, in the order of the places
-      if (tid < g.K && d.id[tid] >= 0 && d.id[tid] < g.V) {
-        const int id = d.id[tid], i = (id + row.off) / kVec;
+      if (!zeros && tid < g.K && id >= 0 && id < g.V) {
+        const int i = (id + row.off) / kVec;
         if (i >= row.lo && i < row.hi) {
           float p = 0.f;
-          for (int k = 0; k < g.K; ++k) p += d.id[k] == id ? d.p[k] : 0.f;
-          Elem<T>::store(grad + id, exp2_fast(fmaf(max_nan(d.z[tid], kMasked), g.c2, -a.mc)) * gq - gp * p);
+          for (int k = 0; k < g.K; ++k) p += d.id[parity][k] == id ? d.p[parity][k] : 0.f;
+          Elem<T>::store(grad + id, exp2_fast(fmaf(d.z[parity][tid], g.c2, -a.mc)) * gq - gp * p);
         }
       }
+      if (late && rank == 0) g.loss[n] = NAN;
     }
+    parity ^= 1;
   }
   if (g.ctas > 1) {
     __syncwarp();
     ptx::cluster_sync_all();                                  // nobody leaves while its shared memory is read
   }
+  if (kSlots && *reinterpret_cast<volatile int*>(&abort) != 0)
+    for (int i = 0; i < 1000; ++i) __nanosleep(1000);         // copies under way land before the shared memory is given back
 }
 
 // ---------------------------------------------------------------------------------------------- launches
-// CTAs of 128 threads for rows of up to 32 KB, of which an SM runs eight at a time, of 512 for longer ones, two at a time.  Rows that
-// are too few for all SMs are shared by the CTAs of a cluster, as long as each thread has a vector; and with `again` (the row is read
-// a second time) so that the rows under way at one time take no more than a third of the second-level cache.
-constexpr int64_t kShortRow = 32 << 10, kRowsUnderWay = 40 << 20;
+constexpr int64_t kShortRow = 16 << 10;      // bytes of rows for CTAs of kShort threads
+constexpr int64_t kRowsUnderWay = 48 << 20;  // bytes of rows that are to be found again in the second-level cache
+
 struct Plan {
-  int threads, ctas;
+  int ctas;                   // of a row
+  int64_t rows;               // under way at a time
 };
-Plan plan_rows(int64_t N, int64_t V, int64_t size, bool again, int sms) {
+// CTAs of a cluster share a row where rows are too few for all SMs, or do not go up evenly in those that can be under way, or where those
+// are not to be more than the second-level cache keeps (`again`).  The time of a row's part is estimated by its bytes at the share of the
+// memory's rate that a CTA has, and 2 us (3 with others) around it.
+template <typename F>
+int plan_rows(int64_t N, int64_t row /* vectors, at most */, int threads, bool again, Plan& p, F clusters) {
+  double best = 0;
+  p.ctas = 0;
+  for (int c = 1; c <= kMaxCluster; c *= 2) {
+    const int64_t part = ceil_div(row, c);
+    if (c > 1 && part < threads * kBatch) break;
+    const int64_t slots = clusters(c);
+    if (slots < 1) continue;
+    const int64_t rows = N < slots ? N : slots;
+    const double us = (double)ceil_div(N, slots) * ((double)part * 16 * (again ? 2 : 1) / (43.0 * threads) + (c > 1 ? 3.0 : 2.0));
+    const bool fits = rows * row * 16 <= kRowsUnderWay;
+    if (p.ctas == 0 || us < 0.97 * best || (again && fits && p.rows * row * 16 > kRowsUnderWay)) {
+      best = us;
+      p.ctas = c;
+      p.rows = rows;
+    }
+  }
+  return p.ctas == 0 ? TLQ_ERR_CUDA : TLQ_OK;
+}
+// Vectors that rows have at most: one more where they do not begin on the vectors' grid.
+int64_t row_vectors(const void* z, int64_t N, int64_t V, int64_t ld, int64_t size) {
+  return ceil_div(V * size, 16) + (aligned16(z) && (N == 1 || ld * size % 16 == 0) ? 0 : 1);
+}
+
+// Clusters of `c` CTAs that a device runs at a time (asked once for each kernel, size and device).
+struct Resident {
+  int count[kMaxDevices][4] = {};
+};
+template <typename Kernel>
+int64_t resident_clusters(Kernel kernel, Resident& known, int threads, size_t smem, int c) {
+  const int dev = current_device_index(), k = c == 1 ? 0 : c == 2 ? 1 : c == 4 ? 2 : 3;
+  if (dev < 0) return 0;
+  int& n = known.count[dev][k];
+  if (n == 0) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return 0;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(c * 1024));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)c;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      n = 0;
+    }
+  }
+  return n;
+}
+
+template <typename T, bool kEntropy, bool kTop, int kThreads>
+int run_logprobs(LogprobArgs g, cudaStream_t st) {
+  static Resident known;
+  constexpr size_t smem = kThreads != kShort ? (size_t)(kTop ? kSlotsTop : kSlotsOnce) * kBatch * kThreads * 16 : 0;
+  auto kernel = logprobs_kernel<T, kEntropy, kTop, kThreads>;
+  const int64_t vectors = row_vectors(g.z, g.N, g.V, g.ld, sizeof(T));
   Plan p;
-  p.threads = V * size <= kShortRow ? 128 : 512;
-  p.ctas = 1;
-  const int64_t slots = (int64_t)sms * (1024 / p.threads), row = V * size;
-  auto wanted = [&] {
-    return N * p.ctas * 2 <= slots || (again && (N * p.ctas < slots ? N : slots / p.ctas) * row > kRowsUnderWay);
-  };
-  while (p.ctas < kMaxCluster && row >= (int64_t)2 * p.ctas * p.threads * 16 && wanted()) p.ctas *= 2;
-  return p;
+  const int rc = plan_rows(g.N, vectors, kThreads, false, p, [&](int c) { return resident_clusters(kernel, known, kThreads, smem, c); });
+  if (rc != TLQ_OK) return rc;
+  g.ctas = p.ctas;
+  g.batches = (int)ceil_div(ceil_div(ceil_div(vectors, p.ctas), (int64_t)kBatch * kThreads), runs_of(kThreads));
+  return launch_next(kernel, dim3((unsigned)(p.rows * p.ctas)), kThreads, smem, (unsigned)p.ctas, st, g);
+}
+
+template <typename T, bool kGrad, int kThreads>
+int run_distill(DistillArgs g, cudaStream_t st) {
+  static Resident known;
+  constexpr size_t smem = kThreads != kShort ? (size_t)kSlotsOnce * kBatch * kThreads * 16 : 0;
+  auto kernel = distill_kernel<T, kGrad, kThreads>;
+  Plan p;
+  const int rc = plan_rows(g.N, row_vectors(g.z, g.N, g.V, g.ld, sizeof(T)), kThreads, kGrad, p,
+                           [&](int c) { return resident_clusters(kernel, known, kThreads, smem, c); });
+  if (rc != TLQ_OK) return rc;
+  g.ctas = p.ctas;
+  return launch_next(kernel, dim3((unsigned)(p.rows * p.ctas)), kThreads, smem, (unsigned)p.ctas, st, g);
 }
 
 }  // namespace
 
 int launch_token_logprobs(const void* logits, int f32, int64_t N, int64_t V, int64_t ld, float scale, const int32_t* ids, int K,
                           float* logp, float* entropy, float* lse, int32_t* top_ids, float* top_logp, cudaStream_t st) {
-  const int sms = device_sm_count();
-  if (sms <= 0) return TLQ_ERR_CUDA;
-  const Plan p = plan_rows(N, V, f32 ? 4 : 2, false, sms);
   LogprobArgs g{};
-  g.z = logits; g.ld = ld; g.V = (int)V; g.ctas = p.ctas; g.K = K; g.c2 = scale * kLog2e;
+  g.z = logits; g.N = N; g.ld = ld; g.V = (int)V; g.K = K; g.c2 = scale * kLog2e;
   g.ids = ids; g.logp = logp; g.entropy = entropy; g.lse = lse; g.top_ids = top_ids; g.top_logp = top_logp;
-  auto run = [&](auto kernel) { return launch_next(kernel, dim3((unsigned)(N * p.ctas)), p.threads, 0, (unsigned)p.ctas, st, g); };
   auto of_type = [&](auto type, auto threads) {
     using T = decltype(type);
     constexpr int kThreads = decltype(threads)::value;
-    if (entropy != nullptr) return K > 0 ? run(logprobs_kernel<T, true, true, kThreads>) : run(logprobs_kernel<T, true, false, kThreads>);
-    return K > 0 ? run(logprobs_kernel<T, false, true, kThreads>) : run(logprobs_kernel<T, false, false, kThreads>);
+    if (entropy != nullptr) return K > 0 ? run_logprobs<T, true, true, kThreads>(g, st) : run_logprobs<T, true, false, kThreads>(g, st);
+    return K > 0 ? run_logprobs<T, false, true, kThreads>(g, st) : run_logprobs<T, false, false, kThreads>(g, st);
   };
-  const std::integral_constant<int, 128> few;
-  const std::integral_constant<int, 512> many;
-  if (f32) return p.threads == 128 ? of_type(0.f, few) : of_type(0.f, many);
-  return p.threads == 128 ? of_type((uint16_t)0, few) : of_type((uint16_t)0, many);
+  const std::integral_constant<int, kShort> few;
+  const std::integral_constant<int, kLong> many;
+  const bool is_short = V * (f32 ? 4 : 2) <= kShortRow;
+  if (f32) return is_short ? of_type(0.f, few) : of_type(0.f, many);
+  return is_short ? of_type((uint16_t)0, few) : of_type((uint16_t)0, many);
 }
 
 int launch_distill_loss(const void* logits, int f32, int64_t N, int64_t V, int64_t ld, float scale, const int32_t* top_ids,
                         const float* top_logits, int K, const float* weights, float* loss, void* grad, int64_t ldg, cudaStream_t st) {
   const int sms = device_sm_count();
   if (sms <= 0) return TLQ_ERR_CUDA;
-  const Plan p = plan_rows(N, V, f32 ? 4 : 2, grad != nullptr, sms);
   DistillArgs g{};
-  g.z = logits; g.ld = ld; g.V = (int)V; g.ctas = p.ctas; g.K = K; g.c2 = scale * kLog2e; g.scale = scale;
+  g.z = logits; g.N = N; g.ld = ld; g.V = (int)V; g.K = K; g.c2 = scale * kLog2e; g.scale = scale;
   g.ids = top_ids; g.top = top_logits; g.weights = weights; g.loss = loss; g.grad = grad; g.ldg = ldg;
-  auto run = [&](auto kernel) { return launch_next(kernel, dim3((unsigned)(N * p.ctas)), p.threads, 0, (unsigned)p.ctas, st, g); };
   auto of_type = [&](auto type) {
     using T = decltype(type);
-    if (grad != nullptr) return p.threads == 128 ? run(distill_kernel<T, true, 128>) : run(distill_kernel<T, true, 512>);
-    return p.threads == 128 ? run(distill_kernel<T, false, 128>) : run(distill_kernel<T, false, 512>);
+    const bool is_short = V * (int64_t)sizeof(T) <= kShortRow;
+    if (grad != nullptr) {
+      if (is_short) return run_distill<T, true, kShort>(g, st);
+      // the smallest CTAs whose rows under way stay in the second-level cache
+      const int64_t row = V * (int64_t)sizeof(T), most = kRowsUnderWay / row;
+      return N <= most || 4 * sms <= most ? run_distill<T, true, 256>(g, st)
+                                          : 2 * sms <= most ? run_distill<T, true, 512>(g, st) : run_distill<T, true, 1024>(g, st);
+    }
+    return is_short ? run_distill<T, false, kShort>(g, st) : run_distill<T, false, kLong>(g, st);
   };
   return f32 ? of_type(0.f) : of_type((uint16_t)0);
 }
