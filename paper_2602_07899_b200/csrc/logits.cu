@@ -486,6 +486,7 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
   unsigned long long least = (unsigned long long)bound << 48;
   int n;
   while (true) {
+    const float least_z = least >> 32 == 0 ? -INFINITY : of_order((uint32_t)(least >> 32));
     for (int k = tid; k < total; k += kThreads) {
       const int e = batches == 1 ? k : k / batches, which = all ? e : sh.listed[e], t = which % kThreads;
       const int i = row.lo + (which / kThreads * batches + k - e * batches) * kThreads * kBatch + (kThreads == kShort ? t : (t >> 5) * kPiece + (t & 31));
@@ -500,8 +501,10 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
 #pragma unroll
         for (int j = 0; j < Elem<T>::kVec; ++j) {
           const float2 h = halves(x[j >> 1]);
+          const float z = (j & 1) ? h.y : h.x;
+          if (z < least_z) continue;
           const int at = row.first(i + u * vector_step<kThreads>()) + j;
-          const unsigned long long key = key_of((j & 1) ? h.y : h.x, at);
+          const unsigned long long key = key_of(z, at);
           if (key >= least && at >= 0 && at < row.V && i + u * vector_step<kThreads>() < row.hi) {
             const int to = atomicAdd(&sh.n_keys, 1);
             if (to < kCandidates) sh.keys[to] = key;
@@ -608,22 +611,23 @@ logprobs_kernel(const LogprobArgs g) {
       if (id >= 0 && id < g.V) z_id = Elem<T>::load(row.z + id);
     }
     Running<T, kEntropy> run(g.c2);
-    float run_top = kMasked;
-    int batch = 0;
-    for (int i = first_vector<kThreads>(row.lo, 0); i - (kSlots ? (int)(threadIdx.x & 31) : (int)threadIdx.x) < row.hi; i += kBatch * kThreads, ++batch) {
+    float run_top = kMasked;                                  // of the batches of a run
+    int runs = 0, run_left = g.batches;
+    for (int i = first_vector<kThreads>(row.lo, 0); i - (kSlots ? (int)(threadIdx.x & 31) : (int)threadIdx.x) < row.hi; i += kBatch * kThreads) {
       uint4 v[kBatch];
       read_batch<T, kThreads, kEntropy>(row, i, pieces, &abort, v, run);
       const float largest = run.add(v);
       if constexpr (kTop) {
         run_top = fmaxf(run_top, largest);
-        if ((batch + 1) % g.batches == 0) {
-          top.runs[batch / g.batches][threadIdx.x] = (uint16_t)(in_order(run_top) >> 16);
+        if (--run_left == 0) {
+          top.runs[runs++][threadIdx.x] = (uint16_t)(in_order(run_top) >> 16);
           run_top = kMasked;
+          run_left = g.batches;
         }
       }
     }
     if constexpr (kTop)
-      if (batch % g.batches != 0) top.runs[batch / g.batches][threadIdx.x] = (uint16_t)(in_order(run_top) >> 16);
+      if (run_left != g.batches) top.runs[runs++][threadIdx.x] = (uint16_t)(in_order(run_top) >> 16);
     const Stat a = join_row<kThreads>(run.stat(), g.c2, g.ctas, sh, parity);
     const float log2_s = log2f(a.s);
     if (rank == 0 && threadIdx.x == 0) {
@@ -635,7 +639,7 @@ logprobs_kernel(const LogprobArgs g) {
     if constexpr (kTop) {
       const bool bad = isnan(a.s);                            // (the same in all CTAs of the row)
       if (!bad) {
-        top_of_part<T, kThreads>(row, g.K, run.m, (batch + g.batches - 1) / g.batches, g.batches, top);
+        top_of_part<T, kThreads>(row, g.K, run.m, runs, g.batches, top);
         if (g.ctas > 1) join_tops<kThreads>(g.K, g.ctas, rank, top);
       }
       if (rank == 0 && (int)threadIdx.x < g.K) {
