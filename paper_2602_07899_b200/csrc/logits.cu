@@ -445,21 +445,58 @@ __device__ unsigned long long kth_key(const TopShared<kThreads>& sh, int n, int 
   return bound;
 }
 
+// The largest K of n keys to their places, largest first: 32 at a time are put in order by a warp; a key's place is then the number of larger
+// ones in every such list.
+template <int kThreads>
+__device__ __forceinline__ void place_keys(unsigned long long* keys, int n, int K, unsigned long long* places) {
+  const int tid = threadIdx.x, lane = tid & 31, lists = (n + 31) / 32;
+  for (int l = tid >> 5; l < lists; l += kThreads / 32) {
+    unsigned long long key = l * 32 + lane < n ? keys[l * 32 + lane] : 0;
+#pragma unroll
+    for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+      for (int step = size >> 1; step > 0; step >>= 1) {
+        const unsigned long long other = __shfl_xor_sync(0xFFFFFFFFu, key, step);
+        key = ((lane & step) == 0) == ((lane & size) == 0) ? max(key, other) : min(key, other);
+      }
+    keys[l * 32 + lane] = key;
+  }
+  __syncthreads();
+  for (int i = tid; i < lists * 32; i += kThreads) {
+    const unsigned long long key = keys[i];
+    int place = i & 31;
+    if (key == 0 || place >= K) continue;
+    for (int l = 0; l < lists; ++l) {
+      if (l == i >> 5) continue;
+      int above = 0;
+#pragma unroll
+      for (int step = 16; step > 0; step >>= 1)
+        if (keys[l * 32 + above + step - 1] > key) above += step;
+      above += keys[l * 32 + above] > key;                    // (31 at most before this)
+      place += above;
+      if (place >= K) break;
+    }
+    if (place < K) places[place] = key;
+  }
+}
+
 // The largest K of this CTA's part of the row into sh.top.  `mine`: the largest logit of this thread's vectors; a run is `batches` batches.
 template <typename T, int kThreads>
 __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine, int runs, int batches, TopShared<kThreads>& sh) {
   const int tid = threadIdx.x;
   const bool any = first_vector<kThreads>(row.lo, 0) < row.hi;
   const uint32_t own = any ? in_order(mine) >> 16 : 0u;
-  // A bound that K threads at least reach: in every warp its share of them does, found by bisection among the lanes.  (None where fewer have
+  // A bound that K threads at least reach: in every warp its share of them does.  (None where fewer have
   // anything; the part is small then.)
   const int vectors = row.hi - row.lo, here = __popc(__ballot_sync(0xFFFFFFFFu, any));
   const int active = kThreads == kShort ? min(kThreads, vectors) : min(kThreads / 32, vectors / kPiece) * 32 + min(32, vectors % kPiece) * (vectors < kThreads * kBatch);
   const int share = max(1, (K * here + active - 1) / max(active, 1));
-  uint32_t bound = 0;
-  for (int bit = 15; bit >= 0; --bit) {
-    const uint32_t next = bound | (1u << bit);
-    if (__popc(__ballot_sync(0xFFFFFFFFu, own >= next)) >= share) bound = next;
+  uint32_t bound = 0, rest = own;
+  for (int have = 0; have < share;) {                         // the largest that is left, and with it all lanes that have it
+    bound = __reduce_max_sync(0xFFFFFFFFu, rest);
+    if (bound == 0) break;
+    have += __popc(__ballot_sync(0xFFFFFFFFu, rest == bound));
+    rest = rest == bound ? 0u : rest;
   }
   if ((tid & 31) == 0) sh.bounds[tid >> 5] = bound;
   if (tid == 0) sh.n_listed = 0;
@@ -468,15 +505,14 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
 #pragma unroll
   for (int k = 0; k < kThreads / 32; ++k) bound = min(bound, sh.bounds[k]);
   if (any && own >= bound) {
-    uint32_t x[TopShared<kThreads>::kRuns];
+    uint32_t hit = 0;
 #pragma unroll
-    for (int r = 0; r < TopShared<kThreads>::kRuns; ++r) x[r] = sh.runs[r][tid];
-#pragma unroll
-    for (int r = 0; r < TopShared<kThreads>::kRuns; ++r)
-      if (r < runs && x[r] >= bound) {
-        const int at = atomicAdd(&sh.n_listed, 1);
-        if (at < kCandidates) sh.listed[at] = (uint16_t)(r * kThreads + tid);
-      }
+    for (int r = 0; r < TopShared<kThreads>::kRuns; ++r) hit |= sh.runs[r][tid] >= bound ? 1u << r : 0u;
+    hit &= (1u << runs) - 1u;
+    for (; hit != 0; hit &= hit - 1) {
+      const int at = atomicAdd(&sh.n_listed, 1);
+      if (at < kCandidates) sh.listed[at] = (uint16_t)((__ffs(hit) - 1) * kThreads + tid);
+    }
   }
   if (tid == 0) sh.n_keys = 0;
   __syncthreads();
@@ -494,6 +530,7 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
 #pragma unroll
       for (int u = 0; u < kBatch; ++u)
         v[u] = i + u * vector_step<kThreads>() < row.hi ? load_once(row.z + row.first(i + u * vector_step<kThreads>())) : row.none();
+      uint32_t hit = 0;                                       // of the batch's elements, in the vectors' order
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
         f32x2 x[Elem<T>::kPairs];
@@ -501,15 +538,16 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
 #pragma unroll
         for (int j = 0; j < Elem<T>::kVec; ++j) {
           const float2 h = halves(x[j >> 1]);
-          const float z = (j & 1) ? h.y : h.x;
-          if (z < least_z) continue;
-          const int at = row.first(i + u * vector_step<kThreads>()) + j;
-          const unsigned long long key = key_of(z, at);
-          if (key >= least && at >= 0 && at < row.V && i + u * vector_step<kThreads>() < row.hi) {
-            const int to = atomicAdd(&sh.n_keys, 1);
-            if (to < kCandidates) sh.keys[to] = key;
-          }
+          hit |= ((j & 1) ? h.y : h.x) < least_z ? 0u : 1u << (u * Elem<T>::kVec + j);
         }
+      }
+      for (; hit != 0; hit &= hit - 1) {
+        const int bit = __ffs(hit) - 1, from = i + bit / Elem<T>::kVec * vector_step<kThreads>(), at = row.first(from) + bit % Elem<T>::kVec;
+        if (at < 0 || at >= row.V || from >= row.hi) continue;
+        const unsigned long long key = key_of(max_nan(Elem<T>::load(row.z + at), kMasked), at);
+        if (key < least) continue;
+        const int to = atomicAdd(&sh.n_keys, 1);
+        if (to < kCandidates) sh.keys[to] = key;
       }
     }
     __syncthreads();
@@ -520,16 +558,7 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
     if (tid == 0) sh.n_keys = 0;
     __syncthreads();
   }
-  // each key's place is the number of larger ones; with many of them only the largest K are placed
-  if (n > 512 && n > K) least = kth_key<kThreads>(sh, n, K);
-  for (int i = tid; i < n; i += kThreads) {
-    const unsigned long long key = sh.keys[i];
-    if (key < least) continue;
-    int place = 0;
-#pragma unroll 4
-    for (int j = 0; j < n; ++j) place += sh.keys[j] > key;
-    if (place < K) sh.top[place] = key;
-  }
+  place_keys<kThreads>(sh.keys, n, K, sh.top);
   __syncthreads();
 }
 
@@ -546,19 +575,7 @@ __device__ __forceinline__ void join_tops(int K, int ctas, int rank, TopShared<k
     }
     if (threadIdx.x < K) sh.all[threadIdx.x] = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < ctas * K; i += kThreads) {
-      const unsigned long long key = sh.keys[i];
-      if (key == 0) continue;
-      int place = i % K;                                      // larger ones in its own list, and in the others
-      for (int r = 0; r < ctas; ++r) {
-        if (r == i / K) continue;
-        int above = 0;
-        for (int step = kMaxTop; step > 0; step >>= 1)
-          if (above + step <= K && sh.keys[r * K + above + step - 1] > key) above += step;
-        place += above;
-      }
-      if (place < K) sh.all[place] = key;
-    }
+    place_keys<kThreads>(sh.keys, ctas * K, K, sh.all);
     __syncthreads();
   }
 }
