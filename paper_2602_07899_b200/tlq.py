@@ -628,7 +628,7 @@ def tlq_linear_i8_act(Xq: torch.Tensor, t: torch.Tensor, Wq: torch.Tensor, u: to
     if workspace is None:
         workspace = _made_on(stream, linear_workspace, N, C1, C2, Xq.device)
     if out is None:
-        out = _empty_on(Xq, stream)((N, width), dtype=_BF16)
+        out = _empty_on(Xq, stream)(N, width, dtype=_BF16)
     else:
         _typed(out, _BF16, (N, width), "out")
     status = lib.tlq_linear_i8_act(Xq.data_ptr(), t.data_ptr(), N, C1, Wq.data_ptr(), u.data_ptr(), C2,
@@ -671,25 +671,29 @@ def tlq_norm_quantize(x: torch.Tensor, w: Optional[torch.Tensor], cfg: Optional[
     if (dev < 0 or dev != _raw_device() or residual is not None and residual.get_device() != dev or w is not None and w.get_device() != dev
             or s is not None and s.get_device() != dev or h is not None and h.get_device() != dev):
         _on_device("tlq_norm_quantize", x, residual, w, s, h)
-    empty = _empty_on(x, stream)
+    # (a tensor like another one is made in two thirds of the time of one of given sizes)
+    like, empty = (torch.empty_like, x.new_empty) if stream is None else (functools.partial(_made_on, stream, torch.empty_like),
+                                                                          functools.partial(_made_on, stream, x.new_empty))
     if h is not None:
         ldh = _rows(h, "h")
         if h.shape != x.shape:
             raise ValueError("h must have the shape of x")
     elif residual is not None:
-        h, ldh = empty((N, C)), C
+        h, ldh = like(x), C
     codes = steps = values = y = None
     if want_codes:
-        codes, steps = empty((N, C), dtype=_I8), empty((N,), dtype=_F32)
+        codes, steps = like(x, dtype=_I8), empty(N, dtype=_F32)
         if cfg is None:
             cfg = _default_cfg()
-    if want_values:
-        values = empty((N, C))
+        if want_values:
+            values = like(x)
     if want_y:
-        y = empty((N, C))
-    ptr = lambda v: None if v is None else v.data_ptr()  # noqa: E731
-    status = _norm_quantize(x.data_ptr(), N, C, ldx, ptr(residual), ldr, ptr(w), eps, ptr(s), None if cfg is None else ctypes.addressof(cfg),
-                            ptr(h), ldh, ptr(codes), ptr(steps), ptr(values), ptr(y), _stream(stream, dev))
+        y = like(x)
+    status = _norm_quantize(x.data_ptr(), N, C, ldx, None if residual is None else residual.data_ptr(), ldr,
+                            None if w is None else w.data_ptr(), eps, None if s is None else s.data_ptr(),
+                            None if cfg is None else ctypes.addressof(cfg), None if h is None else h.data_ptr(), ldh,
+                            None if codes is None else codes.data_ptr(), None if steps is None else steps.data_ptr(),
+                            None if values is None else values.data_ptr(), None if y is None else y.data_ptr(), _stream(stream, dev))
     if status:
         raise TlqError(status, "tlq_norm_quantize")
     return dict(h=x if h is None else h, codes=codes, steps=steps, values=values, y=y)
@@ -729,16 +733,23 @@ def tlq_token_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor] = None,
     dev = logits.get_device()
     if dev < 0 or dev != _raw_device() or ids is not None and ids.get_device() != dev:
         _on_device("tlq_token_logprobs", logits, ids)
-    empty = _empty_on(logits, stream)
-    logp = None if ids is None else empty((N,), dtype=_F32)
-    entropy = empty((N,), dtype=_F32) if want_entropy else None
-    lse = empty((N,), dtype=_F32) if want_lse else None
-    top_ids = top_logp = None
+    like, empty = (torch.empty_like, logits.new_empty) if stream is None else (functools.partial(_made_on, stream, torch.empty_like),
+                                                                               functools.partial(_made_on, stream, logits.new_empty))
+    logp = entropy = lse = top_ids = top_logp = None
+    if ids is not None:
+        logp = like(ids, dtype=_F32)
+    if want_entropy:
+        entropy = empty(N, dtype=_F32) if logp is None else like(logp)
+    if want_lse:
+        one = entropy if logp is None else logp
+        lse = empty(N, dtype=_F32) if one is None else like(one)
     if top_k:
-        top_ids, top_logp = empty((N, top_k), dtype=_I32), empty((N, top_k), dtype=_F32)
-    ptr = lambda v: None if v is None else v.data_ptr()  # noqa: E731
-    status = lib.tlq_token_logprobs(logits.data_ptr(), kind, N, V, ld, scale, ptr(ids), top_k, ptr(logp), ptr(entropy), ptr(lse),
-                                    ptr(top_ids), ptr(top_logp), _stream(stream, dev))
+        top_ids = empty(N, top_k, dtype=_I32)
+        top_logp = like(top_ids, dtype=_F32)
+    status = lib.tlq_token_logprobs(logits.data_ptr(), kind, N, V, ld, scale, None if ids is None else ids.data_ptr(), top_k,
+                                    None if logp is None else logp.data_ptr(), None if entropy is None else entropy.data_ptr(),
+                                    None if lse is None else lse.data_ptr(), None if top_ids is None else top_ids.data_ptr(),
+                                    None if top_logp is None else top_logp.data_ptr(), _stream(stream, dev))
     if status:
         raise TlqError(status, "tlq_token_logprobs")
     return dict(logp=logp, entropy=entropy, lse=lse, top_ids=top_ids, top_logp=top_logp)
@@ -770,8 +781,8 @@ def tlq_distill_loss(logits: torch.Tensor, top_ids: torch.Tensor, top_logits: to
             raise ValueError("grad must have the type and shape of the logits")
         ldg = _logits(grad, "grad")[1]
     elif want_grad:
-        grad = empty((N, V))
-    loss = empty((N,), dtype=_F32)
+        grad = empty(N, V)
+    loss = empty(N, dtype=_F32)
     status = lib.tlq_distill_loss(logits.data_ptr(), kind, N, V, ld, scale, top_ids.data_ptr(), top_logits.data_ptr(), K,
                                   None if weights is None else weights.data_ptr(), loss.data_ptr(), None if grad is None else grad.data_ptr(),
                                   ldg, _stream(stream, dev))
