@@ -49,7 +49,7 @@ __device__ __forceinline__ uint4 ld_shared(uint32_t addr) {
 }
 
 // Thread t has pieces t, t + kThreads, ... of a row.
-template <int kPieces, int kThreads, int kCtas>
+template <int kPieces, int kThreads, int kCtas, bool kKeep>
 __global__ void __launch_bounds__(kThreads, kCtas)
 norm_quantize_kernel(const NormArgs a) {
   constexpr int kWarps = kThreads / 32;
@@ -75,19 +75,28 @@ norm_quantize_kernel(const NormArgs a) {
   };
   after_previous();
   fetch();
-  float g[kPieces][8];
+  // w / s of a piece; kept in registers for all rows where there is room for them, else made anew from the first-level cache
+  auto gains = [&](int p, float (&f)[8]) {
 #pragma unroll
-  for (int p = 0; p < kPieces; ++p) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) g[p][j] = 1.f;
-    if (in[p] && a.w != nullptr) unpack8(load_near(reinterpret_cast<const uint4*>(a.w) + p * kThreads + tid), g[p]);
+    for (int j = 0; j < 8; ++j) f[j] = 1.f;
+    if (in[p] && a.w != nullptr) unpack8(load_near(reinterpret_cast<const uint4*>(a.w) + p * kThreads + tid), f);
     if (in[p] && a.s != nullptr) {
       float s[8];
       unpack8(load_near(reinterpret_cast<const uint4*>(a.s) + p * kThreads + tid), s);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) g[p][j] *= __frcp_rn(s[j]);
+      for (int j = 0; j < 8; ++j) f[j] *= kKeep ? __frcp_rn(s[j]) : __fdividef(1.f, s[j]);
     }
+  };
+  float kept[kKeep ? kPieces : 1][8];
+  if (kKeep) {
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) gains(p, kept[kKeep ? p : 0]);
   }
+  auto gain = [&](int p, float (&f)[8]) {
+    if (!kKeep) return gains(p, f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = kept[kKeep ? p : 0][j];
+  };
   int64_t flat = n * a.pieces + tid;                          // this thread's first piece in the outputs without a pitch
   for (int parity = 0; n < a.N; n += gridDim.x, flat += (int64_t)gridDim.x * a.pieces, parity ^= 1) {
     uint4 h[kPieces];
@@ -116,12 +125,13 @@ norm_quantize_kernel(const NormArgs a) {
       float sum = 0.f, most = 0.f;
 #pragma unroll
       for (int p = 0; p < kPieces; ++p) {
-        float u[8];
+        float u[8], g[8];
         unpack8(h[p], u);
+        gain(p, g);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           sum = fmaf(u[j], u[j], sum);
-          most = max_nan(most, fabsf(u[j] * g[p][j]));
+          most = max_nan(most, fabsf(u[j] * g[j]));
         }
       }
 #pragma unroll
@@ -197,12 +207,13 @@ norm_quantize_kernel(const NormArgs a) {
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
       if (!in[p]) continue;
-      float u[8];
+      float u[8], g[8];
       unpack8(h[p], u);
+      gain(p, g);
       uint32_t c[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float q = fmaf(u[j] * g[p][j], k, kRoundMagic);
+        const float q = fmaf(u[j] * g[j], k, kRoundMagic);
         c[j] = __float_as_uint(q);
         u[j] = (q - kRoundMagic) * step;
       }
@@ -221,7 +232,7 @@ int run_norm(const NormArgs& a, cudaStream_t st) {
   constexpr size_t smem = 2 * kPieces * kThreads * 16;
   static OncePerDevice once;
   static int resident[kMaxDevices] = {};
-  auto kernel = norm_quantize_kernel<kPieces, kThreads, kCtas>;
+  auto kernel = norm_quantize_kernel<kPieces, kThreads, kCtas, (kPieces * kThreads <= 2048)>;
   const int dev = current_device_index(), sms = device_sm_count();
   const int rc = once_per_device(once, [&] {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -262,7 +273,7 @@ int launch_norm_quantize(const uint16_t* x, int64_t N, int64_t C, int64_t ldx, c
     if (pieces <= 512) return run_norm<2, 256, 4>(a, st);
     if (pieces <= 1024) return run_norm<2, 512, 2>(a, st);
   }
-  return pieces <= 2048 ? run_norm<4, 512, 1>(a, st) : run_norm<8, 512, 1>(a, st);
+  return pieces <= 2048 ? run_norm<4, 512, 1>(a, st) : run_norm<4, 1024, 1>(a, st);
 }
 
 }  // namespace tlq
