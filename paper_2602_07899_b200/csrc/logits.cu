@@ -29,7 +29,7 @@ constexpr int kMaxTop = TLQ_MAX_TOP;
 constexpr int kBatch = 4;                 // vectors that a thread works on at a time
 // Rows over 16 KB: CTAs of 256 threads, four to an SM, or of 256 to 1024 for the gradient; a warp has slots of kBatch vectors for each lane.
 constexpr int kShort = 128, kLong = 256;
-constexpr int kSlotsOnce = 3, kSlotsTop = 2;
+constexpr int kSlotsOnce = 2, kSlotsTwice = 3;
 // Runs of batches of a thread that have a maximum of their own, and logits that may be among the largest (those of eight lists at least).
 __host__ __device__ constexpr int runs_of(int threads) { return threads == kShort ? 4 : 16; }
 constexpr int kCandidates = kMaxCluster * kMaxTop;
@@ -104,6 +104,7 @@ struct Elem<uint16_t> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = pair_of(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
   }
+  __device__ static void mask(uint32_t addr) { asm volatile("st.shared.b16 [%0], %1;" ::"r"(addr), "h"((uint16_t)kMaskedPair) : "memory"); }
   __device__ static uint32_t masked() { return kMaskedPair; }
   __device__ static uint4 pack(const f32x2 (&x)[kPairs]) {
     uint32_t w[4];
@@ -143,6 +144,7 @@ struct Elem<float> {
     x[0] = pair_of(__uint_as_float(v.x), __uint_as_float(v.y));
     x[1] = pair_of(__uint_as_float(v.z), __uint_as_float(v.w));
   }
+  __device__ static void mask(uint32_t addr) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(kMasked) : "memory"); }
   __device__ static uint32_t masked() { return __float_as_uint(kMasked); }
   __device__ static uint4 pack(const f32x2 (&x)[kPairs]) {
     const float2 a = halves(x[0]), b = halves(x[1]);
@@ -260,8 +262,18 @@ struct Pieces {
   // The lane's vectors of the piece that is read next, whose slot then takes another one; false when it did not come within the limit of
   // a wait, which no correct run reaches.  (A load from shared memory that is still on its way may be overtaken by a copy into the same
   // place: the fence waits for it.)
-  __device__ bool next(uint4 (&v)[kBatch], int* abort) {
+  // With `row`, what is not the row's is masked: in its place in shared memory, so that the pieces inside of a row, which are almost all, are
+  // not held up by it.
+  __device__ bool next(uint4 (&v)[kBatch], int* abort, const Row<T>* row, int i) {
     const bool ok = ptx::mbar_try_wait(bar, phase) || ptx::mbar_wait(bar, phase, abort);
+    if (row != nullptr && !row->inside(i - (int)(threadIdx.x & 31))) {
+      for (int u = 0; u < kBatch; ++u) {
+        const int k = i + u * 32;
+        if (k < row->hi && row->whole(k)) continue;
+        for (int j = 0; j < Elem<T>::kVec; ++j)
+          if (k >= row->hi || row->first(k) + j < 0 || row->first(k) + j >= row->V) Elem<T>::mask(data + u * 512u + j * (uint32_t)sizeof(T));
+      }
+    }
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
       asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[u].x), "=r"(v[u].y), "=r"(v[u].z), "=r"(v[u].w)
@@ -366,11 +378,7 @@ template <typename T, int kThreads, bool kClamp, typename P, typename R>
 __device__ __forceinline__ void read_batch(const Row<T>& row, int i, P& pieces, int* abort, uint4 (&v)[kBatch], R& run) {
   constexpr int kStep = vector_step<kThreads>();
   if constexpr (kThreads != kShort) {
-    if (!pieces.next(v, abort)) run.s = pair_of(NAN, NAN);
-    if (!row.inside(i - (int)(threadIdx.x & 31))) {
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) v[u] = i + u * kStep < row.hi ? row.own(v[u], i + u * kStep) : row.none();
-    }
+    if (!pieces.next(v, abort, &row, i)) run.s = pair_of(NAN, NAN);
   } else {
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) v[u] = i + u * kStep < row.hi ? row.load(i + u * kStep) : row.none();
@@ -614,8 +622,8 @@ logprobs_kernel(const LogprobArgs g) {
   after_previous();
   const int rank = (int)(blockIdx.x % (unsigned)g.ctas);
   const Rows rows{g.z, g.ld, blockIdx.x / (unsigned)g.ctas, gridDim.x / (unsigned)g.ctas, g.N, g.V, rank, g.ctas, nullptr};
-  typename std::conditional<kSlots, Pieces<T, kThreads, kTop ? kSlotsTop : kSlotsOnce, false>, int>::type pieces = [&] {
-    if constexpr (kSlots) return Pieces<T, kThreads, kTop ? kSlotsTop : kSlotsOnce, false>(rows, slots, barriers, &abort);
+  typename std::conditional<kSlots, Pieces<T, kThreads, kSlotsOnce, false>, int>::type pieces = [&] {
+    if constexpr (kSlots) return Pieces<T, kThreads, kSlotsOnce, false>(rows, slots, barriers, &abort);
     else return 0;
   }();
   int parity = 0;
@@ -735,18 +743,18 @@ template <typename T, bool kGrad, int kThreads>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
 distill_kernel(const DistillArgs g) {
   constexpr bool kSlots = kThreads != kShort;
-  constexpr int kVec = Elem<T>::kVec, kStep = vector_step<kThreads>();
+  constexpr int kVec = Elem<T>::kVec, kStep = vector_step<kThreads>(), kSlotsRow = kGrad ? kSlotsTwice : kSlotsOnce;
   extern __shared__ __align__(128) uint8_t slots[];
   __shared__ RowShared sh;
   __shared__ DistillShared d;
-  __shared__ uint64_t barriers[kSlots ? kSlotsOnce * kThreads / 32 : 1];
+  __shared__ uint64_t barriers[kSlots ? kSlotsRow * kThreads / 32 : 1];
   __shared__ int abort;
   after_previous();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = (int)(blockIdx.x % (unsigned)g.ctas);
   const Rows rows{g.z, g.ld, blockIdx.x / (unsigned)g.ctas, gridDim.x / (unsigned)g.ctas, g.N, g.V, rank, g.ctas, g.weights};
-  typename std::conditional<kSlots, Pieces<T, kThreads, kSlotsOnce, kGrad>, int>::type pieces = [&] {
-    if constexpr (kSlots) return Pieces<T, kThreads, kSlotsOnce, kGrad>(rows, slots, barriers, &abort);
+  typename std::conditional<kSlots, Pieces<T, kThreads, kSlotsRow, kGrad>, int>::type pieces = [&] {
+    if constexpr (kSlots) return Pieces<T, kThreads, kSlotsRow, kGrad>(rows, slots, barriers, &abort);
     else return 0;
   }();
   int parity = 0;
@@ -820,7 +828,7 @@ distill_kernel(const DistillArgs g) {
       for (int i = i0; i - lead < row.hi; i += kBatch * kThreads) {
         uint4 v[kBatch];
         if constexpr (kSlots) {
-          if (!pieces.next(v, &abort)) late = true;
+          if (!pieces.next(v, &abort, nullptr, 0)) late = true;
         } else {
 #pragma unroll
           for (int u = 0; u < kBatch; ++u) v[u] = i + u * kStep < row.hi ? row.load(i + u * kStep) : row.none();
@@ -931,7 +939,7 @@ int64_t resident_clusters(Kernel kernel, Resident& known, int threads, size_t sm
 template <typename T, bool kEntropy, bool kTop, int kThreads>
 int run_logprobs(LogprobArgs g, cudaStream_t st) {
   static Resident known;
-  constexpr size_t smem = kThreads != kShort ? (size_t)(kTop ? kSlotsTop : kSlotsOnce) * kBatch * kThreads * 16 : 0;
+  constexpr size_t smem = kThreads != kShort ? (size_t)kSlotsOnce * kBatch * kThreads * 16 : 0;
   auto kernel = logprobs_kernel<T, kEntropy, kTop, kThreads>;
   const int64_t vectors = row_vectors(g.z, g.N, g.V, g.ld, sizeof(T));
   Plan p;
@@ -945,7 +953,7 @@ int run_logprobs(LogprobArgs g, cudaStream_t st) {
 template <typename T, bool kGrad, int kThreads>
 int run_distill(DistillArgs g, cudaStream_t st) {
   static Resident known;
-  constexpr size_t smem = kThreads != kShort ? (size_t)kSlotsOnce * kBatch * kThreads * 16 : 0;
+  constexpr size_t smem = kThreads != kShort ? (size_t)(kGrad ? kSlotsTwice : kSlotsOnce) * kBatch * kThreads * 16 : 0;
   auto kernel = distill_kernel<T, kGrad, kThreads>;
   Plan p;
   const int rc = plan_rows(g.N, row_vectors(g.z, g.N, g.V, g.ld, sizeof(T)), kThreads, kGrad, p,
