@@ -30,9 +30,10 @@ constexpr int kBatch = 4;                 // vectors that a thread works on at a
 // Rows over 16 KB: CTAs of 256 threads, four to an SM, or of 256 to 1024 for the gradient; a warp has slots of kBatch vectors for each lane.
 constexpr int kShort = 128, kLong = 256;
 constexpr int kSlotsOnce = 2, kSlotsTwice = 3;
-// Runs of batches of a thread that have a maximum of their own, and logits that may be among the largest (those of eight lists at least).
-__host__ __device__ constexpr int runs_of(int threads) { return threads == kShort ? 4 : 16; }
-constexpr int kCandidates = kMaxCluster * kMaxTop;
+constexpr int kRuns = 16;                 // runs of batches of a thread that have a maximum of their own
+constexpr int kCandidates = kMaxCluster * kMaxTop;       // logits that may be among the largest: those of eight lists at least
+constexpr int64_t kShortRow = 16 << 10;   // bytes of rows that CTAs of kShort threads read straight from memory
+constexpr int kShortVectors = kShortRow / 16 + 1;
 constexpr float kMasked = -1.2676506002282294e30f;       // -2^100: logits from here down have probability 0
 constexpr uint32_t kMaskedPair = 0xF180F180u;            // the same, twice in bf16
 
@@ -84,6 +85,7 @@ struct Elem<uint16_t> {
     asm volatile("ld.global.b16 %0, [%1];" : "=h"(v) : "l"(p) : "memory");
     return bf16_bits_to_float(v);
   }
+  __device__ static float get(uint16_t v) { return bf16_bits_to_float(v); }
   __device__ static void store(uint16_t* p, float f) {
     const __nv_bfloat16 v = __float2bfloat16_rn(f);
     *p = *reinterpret_cast<const uint16_t*>(&v);
@@ -127,6 +129,7 @@ template <>
 struct Elem<float> {
   static constexpr int kVec = 4, kPairs = 2;
   __device__ static float load(const float* p) { return load_near(p); }
+  __device__ static float get(float v) { return v; }
   __device__ static void store(float* p, float f) { *p = f; }
   __device__ static uint4 clamp(const uint4& v) {
     auto c = [](uint32_t w) { return __float_as_uint(max_nan(__uint_as_float(w), kMasked)); };
@@ -428,15 +431,16 @@ __device__ __forceinline__ unsigned long long key_of(float x, int index) {
 
 template <int kThreads>
 struct TopShared {
-  static constexpr int kRuns = runs_of(kThreads);
+  static constexpr bool kShortRows = kThreads == kShort;
   union {
     unsigned long long keys[kCandidates];
-    uint16_t runs[kRuns][kThreads];       // upper half of the order of the largest logit of each thread's runs, until they are listed
+    uint16_t runs[kShortRows ? 1 : kRuns][kThreads];     // upper half of the order of the largest logit of each thread's runs, until they are listed
   };
   unsigned long long top[kMaxTop];        // of this CTA's part, largest first
-  unsigned long long all[kMaxTop];        // of the row
+  unsigned long long all[kShortRows ? 1 : kMaxTop];      // of the row
   uint32_t bounds[kThreads / 32];
-  uint16_t listed[kCandidates];           // runs that reach the bound: run kThreads + thread
+  uint4 row[kShortRows ? kShortVectors : 1];             // a short row
+  uint16_t listed[kShortRows ? 1 : kCandidates];         // runs that reach the bound: run kThreads + thread
   int n_keys, n_listed;
 };
 
@@ -488,6 +492,18 @@ __device__ __forceinline__ void place_keys(unsigned long long* keys, int n, int 
   }
 }
 
+// A bound that `share` lanes at least reach: the largest that is left, and with it all lanes that have it, until there are enough.
+__device__ __forceinline__ uint32_t bound_of_lanes(uint32_t own, int share) {
+  uint32_t bound = 0;
+  for (int have = 0; have < share;) {
+    bound = __reduce_max_sync(0xFFFFFFFFu, own);
+    if (bound == 0) break;
+    have += __popc(__ballot_sync(0xFFFFFFFFu, own == bound));
+    own = own == bound ? 0u : own;
+  }
+  return bound;
+}
+
 // The largest K of this CTA's part of the row into sh.top.  `mine`: the largest logit of this thread's vectors; a run is `batches` batches.
 template <typename T, int kThreads>
 __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine, int runs, int batches, TopShared<kThreads>& sh) {
@@ -497,15 +513,9 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
   // A bound that K threads at least reach: in every warp its share of them does.  (None where fewer have
   // anything; the part is small then.)
   const int vectors = row.hi - row.lo, here = __popc(__ballot_sync(0xFFFFFFFFu, any));
-  const int active = kThreads == kShort ? min(kThreads, vectors) : min(kThreads / 32, vectors / kPiece) * 32 + min(32, vectors % kPiece) * (vectors < kThreads * kBatch);
+  const int active = min(kThreads / 32, vectors / kPiece) * 32 + min(32, vectors % kPiece) * (vectors < kThreads * kBatch);
   const int share = max(1, (K * here + active - 1) / max(active, 1));
-  uint32_t bound = 0, rest = own;
-  for (int have = 0; have < share;) {                         // the largest that is left, and with it all lanes that have it
-    bound = __reduce_max_sync(0xFFFFFFFFu, rest);
-    if (bound == 0) break;
-    have += __popc(__ballot_sync(0xFFFFFFFFu, rest == bound));
-    rest = rest == bound ? 0u : rest;
-  }
+  uint32_t bound = bound_of_lanes(own, share);
   if ((tid & 31) == 0) sh.bounds[tid >> 5] = bound;
   if (tid == 0) sh.n_listed = 0;
   if (tid < K) sh.top[tid] = 0;
@@ -515,7 +525,7 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
   if (any && own >= bound) {
     uint32_t hit = 0;
 #pragma unroll
-    for (int r = 0; r < TopShared<kThreads>::kRuns; ++r) hit |= sh.runs[r][tid] >= bound ? 1u << r : 0u;
+    for (int r = 0; r < kRuns; ++r) hit |= sh.runs[r][tid] >= bound ? 1u << r : 0u;
     hit &= (1u << runs) - 1u;
     for (; hit != 0; hit &= hit - 1) {
       const int at = atomicAdd(&sh.n_listed, 1);
@@ -567,6 +577,91 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
     __syncthreads();
   }
   place_keys<kThreads>(sh.keys, n, K, sh.top);
+  __syncthreads();
+}
+
+// The same of a short row, which the threads have left in sh.row.  What counts for the bound are the largest of the threads, or where there
+// are hardly more of them than K those of the vectors, or else the elements: in every warp its share of them reaches its bound.
+template <typename T>
+__device__ __forceinline__ void top_of_short_row(const Row<T>& row, int K, float mine, TopShared<kShort>& sh) {
+  constexpr int kVec = Elem<T>::kVec, kMine = (kShortVectors + kShort - 1) / kShort, kUnits = kMine > 2 * kVec ? kMine : 2 * kVec;
+  static_assert(2 * kMaxTop <= 2 * kShort, "elements of two vectors of each thread at most");
+  const int tid = threadIdx.x, vectors = row.hi - row.lo, active = min(vectors, kShort);
+  uint32_t bound = 0;
+  int units = __popc(__ballot_sync(0xFFFFFFFFu, tid < vectors));     // of the warp
+  if (4 * K <= 3 * active) {
+    bound = bound_of_lanes(tid < vectors ? in_order(mine) >> 16 : 0u, max(1, (K * units + active - 1) / active));
+  } else {
+    const bool fine = vectors < 2 * K;
+    uint32_t unit[kUnits];
+    units = 0;
+#pragma unroll
+    for (int q = 0; q < kUnits; ++q) unit[q] = 0;
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+      if (j * kShort >= vectors) continue;
+      const bool in = j * kShort + tid < vectors;
+      units += __popc(__ballot_sync(0xFFFFFFFFu, in));
+      f32x2 x[Elem<T>::kPairs];
+      Elem<T>::pairs(in ? sh.row[j * kShort + tid] : row.none(), x);
+      float most = kMasked;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const float2 h = halves(x[e >> 1]);
+        const float z = (e & 1) ? h.y : h.x;
+        most = fmaxf(most, z);
+        if (fine && j < 2) unit[j < 2 ? j * kVec + e : 0] = in ? in_order(z) >> 16 : 0u;
+      }
+      if (!fine) unit[j] = in ? in_order(most) >> 16 : 0u;
+    }
+    const int share = max(1, (K * units + vectors - 1) / vectors), rows = (vectors + kShort - 1) / kShort, count = fine ? min(2, rows) * kVec : rows;
+    for (int bit = 15; bit >= 0; --bit) {
+      const uint32_t next = bound | (1u << bit);
+      int reach = 0;
+#pragma unroll
+      for (int q = 0; q < kUnits; ++q)
+        if (q < count) reach += __popc(__ballot_sync(0xFFFFFFFFu, unit[q] >= next));
+      if (reach >= share) bound = next;
+    }
+  }
+  if ((tid & 31) == 0) sh.bounds[tid >> 5] = units > 0 ? bound : 0xFFFFu;     // (a warp without any has no say)
+  if (tid == 0) sh.n_keys = 0;
+  if (tid < K) sh.top[tid] = 0;
+  __syncthreads();
+  bound = 0xFFFFu;
+#pragma unroll
+  for (int k = 0; k < kShort / 32; ++k) bound = min(bound, sh.bounds[k]);
+  unsigned long long least = (unsigned long long)bound << 48;
+  int n;
+  while (true) {
+    const float least_z = least >> 32 == 0 ? -INFINITY : of_order((uint32_t)(least >> 32));
+    for (int j = tid; j < vectors; j += kShort) {
+      f32x2 x[Elem<T>::kPairs];
+      Elem<T>::pairs(sh.row[j], x);
+      uint32_t hit = 0;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const float2 h = halves(x[e >> 1]);
+        hit |= ((e & 1) ? h.y : h.x) < least_z ? 0u : 1u << e;
+      }
+      for (; hit != 0; hit &= hit - 1) {
+        const int e = __ffs(hit) - 1, at = row.first(row.lo + j) + e;
+        if (at < 0 || at >= row.V) continue;
+        const unsigned long long key = key_of(Elem<T>::get(reinterpret_cast<const T*>(sh.row + j)[e]), at);
+        if (key < least) continue;
+        const int to = atomicAdd(&sh.n_keys, 1);
+        if (to < kCandidates) sh.keys[to] = key;
+      }
+    }
+    __syncthreads();
+    n = sh.n_keys;
+    if (n <= kCandidates) break;
+    least = kth_key<kShort>(sh, kCandidates, K);
+    __syncthreads();
+    if (tid == 0) sh.n_keys = 0;
+    __syncthreads();
+  }
+  place_keys<kShort>(sh.keys, n, K, sh.top);
   __syncthreads();
 }
 
@@ -642,7 +737,7 @@ logprobs_kernel(const LogprobArgs g) {
       uint4 v[kBatch];
       read_batch<T, kThreads, kEntropy>(row, i, pieces, &abort, v, run);
       const float largest = run.add(v);
-      if constexpr (kTop) {
+      if constexpr (kTop && kSlots) {
         run_top = fmaxf(run_top, largest);
         if (--run_left == 0) {
           top.runs[runs++][threadIdx.x] = (uint16_t)(in_order(run_top) >> 16);
@@ -650,8 +745,13 @@ logprobs_kernel(const LogprobArgs g) {
           run_left = g.batches;
         }
       }
+      if constexpr (kTop && !kSlots) {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+          if (i + u * kThreads < row.hi) top.row[i + u * kThreads - row.lo] = kEntropy ? v[u] : Elem<T>::clamp(v[u]);
+      }
     }
-    if constexpr (kTop)
+    if constexpr (kTop && kSlots)
       if (run_left != g.batches) top.runs[runs++][threadIdx.x] = (uint16_t)(in_order(run_top) >> 16);
     const Stat a = join_row<kThreads>(run.stat(), g.c2, g.ctas, sh, parity);
     const float log2_s = log2f(a.s);
@@ -664,11 +764,13 @@ logprobs_kernel(const LogprobArgs g) {
     if constexpr (kTop) {
       const bool bad = isnan(a.s);                            // (the same in all CTAs of the row)
       if (!bad) {
-        top_of_part<T, kThreads>(row, g.K, run.m, runs, g.batches, top);
-        if (g.ctas > 1) join_tops<kThreads>(g.K, g.ctas, rank, top);
+        if constexpr (kSlots) top_of_part<T, kThreads>(row, g.K, run.m, runs, g.batches, top);
+        else top_of_short_row<T>(row, g.K, run.m, top);
+        if constexpr (kSlots)
+          if (g.ctas > 1) join_tops<kThreads>(g.K, g.ctas, rank, top);
       }
       if (rank == 0 && (int)threadIdx.x < g.K) {
-        const unsigned long long key = bad ? 0 : g.ctas > 1 ? top.all[threadIdx.x] : top.top[threadIdx.x];
+        const unsigned long long key = bad ? 0 : kSlots && g.ctas > 1 ? top.all[kSlots ? threadIdx.x : 0] : top.top[threadIdx.x];
         const int64_t to = n * g.K + threadIdx.x;
         g.top_ids[to] = key == 0 ? -1 : (int)(0xFFFFFFFFu - (uint32_t)key);
         g.top_logp[to] = bad ? NAN : key == 0 ? -INFINITY : log_p(of_order((uint32_t)(key >> 32)), a, g.c2, log2_s);
@@ -872,7 +974,6 @@ distill_kernel(const DistillArgs g) {
 }
 
 // ---------------------------------------------------------------------------------------------- launches
-constexpr int64_t kShortRow = 16 << 10;      // bytes of rows for CTAs of kShort threads
 constexpr int64_t kRowsUnderWay = 48 << 20;  // bytes of rows that are to be found again in the second-level cache
 
 struct Plan {
@@ -888,7 +989,7 @@ int plan_rows(int64_t N, int64_t row /* vectors, at most */, int threads, bool a
   p.ctas = 0;
   for (int c = 1; c <= kMaxCluster; c *= 2) {
     const int64_t part = ceil_div(row, c);
-    if (c > 1 && part < threads * kBatch) break;
+    if (c > 1 && (threads < kLong || part < threads * kBatch)) break;
     const int64_t slots = clusters(c);
     if (slots < 1) continue;
     const int64_t rows = N < slots ? N : slots;
@@ -946,7 +1047,7 @@ int run_logprobs(LogprobArgs g, cudaStream_t st) {
   const int rc = plan_rows(g.N, vectors, kThreads, false, p, [&](int c) { return resident_clusters(kernel, known, kThreads, smem, c); });
   if (rc != TLQ_OK) return rc;
   g.ctas = p.ctas;
-  g.batches = (int)ceil_div(ceil_div(ceil_div(vectors, p.ctas), (int64_t)kBatch * kThreads), runs_of(kThreads));
+  g.batches = (int)ceil_div(ceil_div(ceil_div(vectors, p.ctas), (int64_t)kBatch * kThreads), kRuns);
   return launch_next(kernel, dim3((unsigned)(p.rows * p.ctas)), kThreads, smem, (unsigned)p.ctas, st, g);
 }
 
