@@ -18,6 +18,7 @@
 // at a multiple of 16 that hold an element of the row lie in the row's own memory page.)
 #include <type_traits>
 
+#include "pairs.cuh"
 #include "serve.cuh"
 #include "umma.cuh"
 
@@ -37,32 +38,7 @@ constexpr int kShortVectors = kShortRow / 16 + 1;
 constexpr float kMasked = -1.2676506002282294e30f;       // -2^100: logits from here down have probability 0
 constexpr uint32_t kMaskedPair = 0xF180F180u;            // the same, twice in bf16
 
-using f32x2 = unsigned long long;
-__device__ __forceinline__ f32x2 pair_of(float lo, float hi) {
-  f32x2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ float2 halves(f32x2 v) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-  return r;
-}
-__device__ __forceinline__ f32x2 padd(f32x2 a, f32x2 b) {
-  f32x2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ f32x2 pmul(f32x2 a, f32x2 b) {
-  f32x2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ f32x2 pfma(f32x2 a, f32x2 b, f32x2 c) {
-  f32x2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
+using f32x2 = pair2;
 __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {   // (a NaN stays one)
   uint32_t r;
   asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));

@@ -63,7 +63,7 @@ struct I8Args {
   uint16_t* yq;            // apply
   WorkspaceHeader* hdr;
   Epilogue epi;            // apply with an epilogue
-  int piece;               // ... whose results and residual lie in rows of whole pieces of 16, 8 or 1 channels
+  int piece;               // ... whose results and residual lie in rows of whole pieces of 16, 8, 4, 2 or 1 channels
 };
 
 __device__ __forceinline__ void report_timeout(WorkspaceHeader* hdr, int where) {
@@ -71,11 +71,44 @@ __device__ __forceinline__ void report_timeout(WorkspaceHeader* hdr, int where) 
   hdr->status = TLQ_ERR_TIMEOUT;
 }
 
-// The first `count` of 16 channels of a row, with what is added to them, as bf16.  `piece`: 16, 8 or 1 of them lie at an address that is a
-// multiple of their size (a row then has whole pieces only).
+// The first `count` of 16 channels of a row, with what is added to them, as bf16.  `piece`: 16, 8, 4, 2 or 1 of them lie at an address that is
+// a multiple of their size (a row then has whole pieces only).
 __device__ __forceinline__ void store16(const float (&f)[16], uint16_t* out, const uint16_t* res, int64_t count, int piece) {
   if (count <= 0) return;
   uint32_t w[8];
+  if (piece == 4 || piece == 2) {
+    uint32_t r[8];
+#pragma unroll
+    for (int j = 0; j < 16; j += 4) {
+      r[j / 2] = r[j / 2 + 1] = 0;
+      if (res == nullptr || j >= count) continue;
+      if (piece == 4) {
+        const uint2 v = *reinterpret_cast<const uint2*>(res + j);
+        r[j / 2] = v.x; r[j / 2 + 1] = v.y;
+      } else {
+        r[j / 2] = *reinterpret_cast<const uint32_t*>(res + j);
+        if (j + 2 < count) r[j / 2 + 1] = *reinterpret_cast<const uint32_t*>(res + j + 2);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 16; j += 4) {
+      if (j >= count) continue;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const float x = res == nullptr ? f[j + 2 * k] : f[j + 2 * k] + bf16_bits_to_float(r[j / 2 + k] & 0xFFFFu);
+        const float y = res == nullptr ? f[j + 2 * k + 1] : f[j + 2 * k + 1] + bf16_bits_to_float(r[j / 2 + k] >> 16);
+        const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
+        w[j / 2 + k] = *reinterpret_cast<const uint32_t*>(&b);
+      }
+      if (piece == 4) {
+        *reinterpret_cast<uint2*>(out + j) = make_uint2(w[j / 2], w[j / 2 + 1]);
+      } else {
+        *reinterpret_cast<uint32_t*>(out + j) = w[j / 2];
+        if (j + 2 < count) *reinterpret_cast<uint32_t*>(out + j + 2) = w[j / 2 + 1];
+      }
+    }
+    return;
+  }
   if (piece == 1) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
@@ -379,10 +412,9 @@ gemm_w8a8_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
 #pragma unroll
             for (int j = 0; j < 32; j += 4) {
               const float4 u = *reinterpret_cast<const float4*>(steps + c * 32 + j), b = *reinterpret_cast<const float4*>(steps + 128 + c * 32 + j);
-              v[j] = __fadd_rn(__fmul_rn((float)(int)r[j], tn * u.x), b.x);
-              v[j + 1] = __fadd_rn(__fmul_rn((float)(int)r[j + 1], tn * u.y), b.y);
-              v[j + 2] = __fadd_rn(__fmul_rn((float)(int)r[j + 2], tn * u.z), b.z);
-              v[j + 3] = __fadd_rn(__fmul_rn((float)(int)r[j + 3], tn * u.w), b.w);
+              const float2 lo = halves(pfma(pair_of((float)(int)r[j], (float)(int)r[j + 1]), pmul(both(tn), pair_of(u.x, u.y)), pair_of(b.x, b.y)));
+              const float2 hi = halves(pfma(pair_of((float)(int)r[j + 2], (float)(int)r[j + 3]), pmul(both(tn), pair_of(u.z, u.w)), pair_of(b.z, b.w)));
+              v[j] = lo.x; v[j + 1] = lo.y; v[j + 2] = hi.x; v[j + 3] = hi.y;
             }
             activate_all(args.epi.act, pair != 0, v);
             const int64_t at = col >> pair;
@@ -553,7 +585,7 @@ int launch_apply_gemm_i8(const int8_t* Xq, const int8_t* Wq, const float* t, con
       return width % n == 0 && (reinterpret_cast<uintptr_t>(Yq) & low) == 0 &&
              (epi->residual == nullptr || (epi->ldr % n == 0 && (reinterpret_cast<uintptr_t>(epi->residual) & low) == 0));
     };
-    a.piece = whole(16) ? 16 : whole(8) ? 8 : 1;
+    a.piece = whole(16) ? 16 : whole(8) ? 8 : whole(4) ? 4 : whole(2) ? 2 : 1;
     gemm_w8a8_kernel<3><<<grid, kThreads, kSmemBytesEpi, st>>>(tmXq, tmWq, tmXq, tmWq, a);
     return after_launch();
   }
