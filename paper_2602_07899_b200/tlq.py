@@ -654,29 +654,35 @@ def tlq_norm_quantize(x: torch.Tensor, w: Optional[torch.Tensor], cfg: Optional[
     dict(h, codes, steps, values, y): the sum x + residual (x itself without one), int8 codes [N,C] with steps [N] of its norm times
     w / s, with want_values the values they stand for (bf16), with want_y the norm times w (bf16).  `h`: where the sum goes (x and
     residual are allowed).  cfg: symmetric mode, 8 bits by default."""
-    N, C = x.shape
-    ldx = _rows(x, "x")
+    shape = x.shape
+    N, C = shape
+    ldx = C if x.dtype is _BF16 and x.is_contiguous() else _rows(x, "x")
     ldr = ldh = 0
+    dev = x.get_device()
+    here = dev >= 0 and dev == _raw_device()
     if residual is not None:
-        ldr = _rows(residual, "residual")
-        if residual.shape != x.shape:
+        ldr = C if residual.dtype is _BF16 and residual.is_contiguous() else _rows(residual, "residual")
+        if residual.shape != shape:
             raise ValueError("x and residual must have one shape")
-    if w is not None and (w.dtype is not _BF16 or w.shape != (C,) or not w.is_contiguous()):
-        _typed(w, _BF16, (C,), "w")
-    if s is not None and (s.dtype is not _BF16 or s.shape != (C,) or not s.is_contiguous()):
-        _typed(s, _BF16, (C,), "s")
+        here = here and residual.get_device() == dev
+    if w is not None:
+        if w.dtype is not _BF16 or w.ndim != 1 or w.numel() != C or not w.is_contiguous():
+            _typed(w, _BF16, (C,), "w")
+        here = here and w.get_device() == dev
+    if s is not None:
+        if s.dtype is not _BF16 or s.ndim != 1 or s.numel() != C or not s.is_contiguous():
+            _typed(s, _BF16, (C,), "s")
+        here = here and s.get_device() == dev
     if not want_codes and (want_values or s is not None):
         raise ValueError("values and s belong to codes")
-    dev = x.get_device()
-    if (dev < 0 or dev != _raw_device() or residual is not None and residual.get_device() != dev or w is not None and w.get_device() != dev
-            or s is not None and s.get_device() != dev or h is not None and h.get_device() != dev):
+    if not here or h is not None and h.get_device() != dev:
         _on_device("tlq_norm_quantize", x, residual, w, s, h)
     # (a tensor like another one is made in two thirds of the time of one of given sizes)
     like, empty = (torch.empty_like, x.new_empty) if stream is None else (functools.partial(_made_on, stream, torch.empty_like),
                                                                           functools.partial(_made_on, stream, x.new_empty))
     if h is not None:
         ldh = _rows(h, "h")
-        if h.shape != x.shape:
+        if h.shape != shape:
             raise ValueError("h must have the shape of x")
     elif residual is not None:
         h, ldh = like(x), C
@@ -714,6 +720,8 @@ def _logits(t: torch.Tensor, what: str):
     """Type number and row pitch of logits [N,V]."""
     if t.dtype is not _BF16 and t.dtype is not _F32:
         raise ValueError(f"{what} must be torch.bfloat16 or torch.float32, got {t.dtype}")
+    if t.ndim == 2 and t.is_contiguous():
+        return (DTYPE_F32 if t.dtype is _F32 else DTYPE_BF16), t.shape[1]
     if t.ndim != 2 or t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{what} must be [N,V] with the logits of a row one after another")
     return (DTYPE_F32 if t.dtype is _F32 else DTYPE_BF16), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
@@ -726,11 +734,11 @@ def tlq_token_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor] = None,
     softmax(scale * logits), its entropy and normaliser, and the top_k largest logits, largest first."""
     kind, ld = _logits(logits, "logits")
     N, V = logits.shape
-    if ids is not None and (ids.dtype is not _I32 or ids.shape != (N,) or not ids.is_contiguous()):
+    dev = logits.get_device()
+    if ids is not None and (ids.dtype is not _I32 or ids.ndim != 1 or ids.numel() != N or not ids.is_contiguous()):
         _typed(ids, _I32, (N,), "ids")
     if not 0 <= top_k <= MAX_TOP:
         raise ValueError(f"top_k must be 0 to {MAX_TOP}")
-    dev = logits.get_device()
     if dev < 0 or dev != _raw_device() or ids is not None and ids.get_device() != dev:
         _on_device("tlq_token_logprobs", logits, ids)
     like, empty = (torch.empty_like, logits.new_empty) if stream is None else (functools.partial(_made_on, stream, torch.empty_like),
