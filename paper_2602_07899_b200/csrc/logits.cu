@@ -193,11 +193,17 @@ struct Pieces {
     }
     if (threadIdx.x == 0) *abort = 0;
     __syncthreads();
+    begin();
     if (r.weights != nullptr) {
+      // whether the first row counts is a trip to memory away: its first pieces are sent for meanwhile, as far as the second-level cache
+      const int there = left - lane * kThreads * kBatch;
+      if (lane < kSlots && there > 0)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;"
+                     ::"l"(src + lane * kThreads * kBatch * Elem<T>::kVec), "r"((uint32_t)min(kPiece, there) * 16u) : "memory");
       w = load_near(r.weights + n);
       if (n + r.step < r.N) w_next = load_near(r.weights + n + r.step);
+      if (w == 0.f) left = 0;
     }
-    begin();
 #pragma unroll
     for (int k = 0; k < kSlots; ++k) fill(data + k * kPieceBytes, bar + 8u * k);
   }
