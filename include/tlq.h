@@ -385,8 +385,8 @@ int tlq_kv_attention(const void* q, int64_t T, int64_t ldq, int32_t n_heads, con
  * Scoring a model by its logits: what a calibrated model answers with, and how far it is from the full-precision one.
  *  - logits [N,V] bf16 or fp32 (dtype: TLQ_DTYPE_*), rows ld elements apart (any pitch and alignment of whole elements), read once from
  *    memory.  1 <= V <= 2^24.  `scale` (one over the temperature) multiplies the logits, 2^-16 <= scale <= 2^16.
- *  - Logits below -2^100 count as masked, like -infinity: probability 0.  A row with a NaN or +infinity has no distribution: its numbers
- *    are NaN, its alternatives -1.
+ *  - Logits of -2^100 and below count as masked, like -infinity: probability 0.  A row with a NaN or +infinity, or whose largest logit
+ *    leaves the 32-bit range when multiplied by scale, has no distribution: its numbers are NaN, its alternatives -1.
  *  - N = 0 is TLQ_OK and launches nothing.  The calls use no workspace; results do not depend on timing.
  */
 #define TLQ_MAX_TOP 128
@@ -410,7 +410,8 @@ int tlq_token_logprobs(const void* logits, int dtype, int64_t N, int64_t V, int6
  *   grad[n,v] = d loss[n] / d logits[n,v] = weights[n] scale (q_v - sum_{k: top_ids[n,k] = v} p_k).
  *   top_ids [N,K] int32, top_logits [N,K] fp32 (logits, or log probabilities as tlq_token_logprobs returns them: the softmax removes
  *   any constant); 1 <= K <= TLQ_MAX_TOP.  A token may stand in several places.  A negative id is an empty place; a row without a teacher
- *   (empty places or logits of -infinity only) has loss 0 and gradient 0.  An id of V or more makes its row NaN.
+ *   (empty places or logits of -infinity only) has loss 0 and gradient 0.  An id of V or more makes its row NaN; a teacher's logit that is
+ *   NaN or +infinity the row's loss, and its gradient at the places.
  *   weights [N] fp32 or NULL (ones): the gradient that arrives at the row's loss.  A row of weight 0 gives zeros, whatever else it holds.
  *   loss [N] fp32; grad [N,V] of the logits' type, rows ldg apart, or NULL (the loss alone).  grad may be the logits themselves (same
  *   pitch), not overlap them otherwise.

@@ -1,8 +1,8 @@
 // A model's logits, read once: log probabilities of given tokens with entropy and the largest alternatives, and the distillation loss
 // on a teacher's top logits with its gradient.
 //
-//   d_v = scale log2(e) z_v - m',  S = sum 2^d_v,  T = sum 2^d_v d_v   (m': the largest of scale log2(e) z_v, rounded)
-//   lse = ln2 (m' + log2 S),  ln p_v = ln2 (d_v - log2 S),  entropy = ln S - ln2 T / S,
+//   d_v = scale log2(e) (z_v - m),  S = sum 2^d_v,  T = sum 2^d_v d_v   (m: the largest z_v)
+//   lse = scale m + ln S,  ln p_v = ln2 (d_v - log2 S),  entropy = ln S - ln2 T / S,
 //   grad_v = w scale (2^d_v / S - sum of the teacher's p at v).
 //
 // Maximum and sums run along in one pass (each thread with a maximum of its own, looked at once for a batch of vectors), so that a row is
@@ -30,7 +30,7 @@ constexpr int kMaxTop = TLQ_MAX_TOP;
 constexpr int kBatch = 4;                 // vectors that a thread works on at a time
 // Rows over 16 KB: CTAs of 256 threads, four to an SM, or of 256 to 1024 for the gradient; a warp has slots of kBatch vectors for each lane.
 constexpr int kShort = 128, kLong = 256;
-constexpr int kSlotsOnce = 2, kSlotsTwice = 3;
+constexpr int kSlotsOnce = 2, kSlotsTwice = 3;            // (the latter for CTAs of 1024 threads: 405 us against 412; of 256 and 512 two are better)
 constexpr int kRuns = 16;                 // runs of batches of a thread that have a maximum of their own
 constexpr int kCandidates = kMaxCluster * kMaxTop;       // logits that may be among the largest: those of eight lists at least
 constexpr int64_t kShortRow = 16 << 10;   // bytes of rows that CTAs of kShort threads read straight from memory
@@ -286,11 +286,21 @@ template <int kThreads>
 __device__ __forceinline__ constexpr int vector_step() { return kThreads == kShort ? kShort : 32; }
 
 // ---------------------------------------------------------------------------------------------- maximum and sums
+// The factor of a logit's distance from the row's largest, m, to the exponent of 2: c2 = scale log2(e).  d = fma(z, c2, -mc) with mc = m c2 rounded
+// is off by that rounding, the same for all logits of the row, which drops out of everything as long as 2^d stays in range: up to
+// |m c2| = 2^31, where it is 64.  Beyond, any other logit is 2^-24 m away from m, over 64 in the exponent, and counts nothing; with
+// a power of 2 for the factor m c is exact, and d is 0 for m itself.
+__device__ __forceinline__ float factor(float m, float c2) {
+  return fabsf(m * c2) < 2147483648.f ? c2 : __uint_as_float(__float_as_uint(c2) & 0xFF800000u);
+}
+constexpr float kFar = -16384.f;          // 2^kFar is 0, and no product with it leaves the range
 struct Stat {
-  float m, mc;                // the largest logit, and that times scale log2(e), rounded
+  float m, mc;                // the largest logit, and that times its factor, rounded
   float s, t;                 // sums of 2^d and of 2^d d
 };
-__device__ __forceinline__ Stat empty_stat(float c2) { return Stat{kMasked, kMasked * c2, 0.f, 0.f}; }
+__device__ __forceinline__ Stat empty_stat(float c2) { return Stat{kMasked, kMasked * factor(kMasked, c2), 0.f, 0.f}; }
+// log2 of the sum of 2^((z - m) c2): without the rounding of mc.
+__device__ __forceinline__ float log2_sum(const Stat& a, float c2) { return log2f(a.s) - fmaf(a.m, factor(a.m, c2), -a.mc); }
 
 // Over the lanes of a warp, in a fixed order; every lane gets the same.
 __device__ __forceinline__ Stat merge_warp(const Stat& a, float c2) {
@@ -298,10 +308,10 @@ __device__ __forceinline__ Stat merge_warp(const Stat& a, float c2) {
   r.m = a.m;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) r.m = fmaxf(r.m, __shfl_xor_sync(0xFFFFFFFFu, r.m, o));
-  r.mc = r.m * c2;
-  const float d = a.mc - r.mc, f = exp2_fast(d);
+  r.mc = r.m * factor(r.m, c2);
+  const float d = fmaxf(a.mc - r.mc, kFar), f = exp2_fast(d);
   r.s = a.s * f;
-  r.t = f * fmaf(a.s, d, a.t);
+  r.t = fmaf(r.s, d, a.t * f);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     r.s += __shfl_xor_sync(0xFFFFFFFFu, r.s, o);
@@ -325,16 +335,20 @@ template <typename T, bool kEntropy>
 struct Running {
   float c2, m, mc;
   f32x2 cc, s, t;
-  __device__ explicit Running(float c2_) : c2(c2_), m(kMasked), mc(kMasked * c2_), cc(pair_of(c2_, c2_)), s(pair_of(0.f, 0.f)), t(s) {}
+  __device__ explicit Running(float c2_) : c2(c2_), m(kMasked), s(pair_of(0.f, 0.f)), t(s) {
+    const float c = factor(m, c2);
+    mc = m * c;
+    cc = pair_of(c, c);
+  }
   // Returns the vectors' largest.
   template <int n>
   __device__ float add(const uint4 (&v)[n]) {
     const float largest = Elem<T>::largest(v), top = fmaxf(m, largest);        // (a NaN passes by here and shows in the sum)
     if (top > m) {
-      const float c = top * c2, d = mc - c, f = exp2_fast(d);
-      const float2 s2 = halves(s), t2 = halves(t);
-      if (kEntropy) t = pair_of(f * fmaf(s2.x, d, t2.x), f * fmaf(s2.y, d, t2.y));
-      s = pair_of(s2.x * f, s2.y * f);
+      const float of_top = factor(top, c2), c = top * of_top, d = fmaxf(mc - c, kFar), f = exp2_fast(d);
+      cc = pair_of(of_top, of_top);
+      s = pmul(s, pair_of(f, f));
+      if (kEntropy) t = pfma(s, pair_of(d, d), pmul(t, pair_of(f, f)));
       m = top;
       mc = c;
     }
@@ -670,7 +684,7 @@ struct LogprobArgs {
   const void* z;
   int64_t N, ld;
   int V, ctas, K, batches;    // batches of a run
-  float c2;                   // scale log2(e)
+  float c2, scale;            // c2 = scale log2(e)
   const int32_t* ids;
   float* logp;
   float* entropy;
@@ -683,7 +697,7 @@ struct LogprobArgs {
 __device__ __forceinline__ float log_p(float x, const Stat& a, float c2, float log2_s) {
   if (isnan(a.s)) return NAN;
   if (!(x > kMasked)) return isnan(x) ? NAN : -INFINITY;
-  return kLn2 * (fmaf(x, c2, -a.mc) - log2_s);
+  return kLn2 * ((x - a.m) * c2 - log2_s);
 }
 
 // Long rows come through slots, short ones straight from memory.
@@ -736,12 +750,12 @@ logprobs_kernel(const LogprobArgs g) {
     if constexpr (kTop && kSlots)
       if (run_left != g.batches) top.runs[runs++][threadIdx.x] = (uint16_t)(in_order(run_top) >> 16);
     const Stat a = join_row<kThreads>(run.stat(), g.c2, g.ctas, sh, parity);
-    const float log2_s = log2f(a.s);
+    const float log2_s = log2_sum(a, g.c2);
     if (rank == 0 && threadIdx.x == 0) {
       const bool none = a.m <= kMasked && !isnan(a.s);
       if (g.ids != nullptr) g.logp[n] = id < 0 ? 0.f : id >= g.V ? NAN : log_p(z_id, a, g.c2, log2_s);
-      if (g.lse != nullptr) g.lse[n] = none ? -INFINITY : isnan(a.s) ? NAN : kLn2 * (a.mc + log2_s);
-      if (kEntropy) g.entropy[n] = none ? 0.f : kLn2 * (log2_s - a.t / a.s);
+      if (g.lse != nullptr) g.lse[n] = none ? -INFINITY : isnan(a.s) ? NAN : fmaf(a.m, g.scale, kLn2 * log2_s);
+      if (kEntropy) g.entropy[n] = none ? 0.f : kLn2 * (log2f(a.s) - a.t / a.s);     // (with the rounding of mc in both)
     }
     if constexpr (kTop) {
       const bool bad = isnan(a.s);                            // (the same in all CTAs of the row)
@@ -800,23 +814,22 @@ __device__ __forceinline__ float teacher_loss(const DistillArgs& g, const Stat& 
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-  const float tc = top * g.c2;
   float sum = 0.f;
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) sum += x[k] <= kMasked ? 0.f : exp2_fast(fmaf(x[k], g.c2, -tc));
+  for (int k = 0; k < kPer; ++k) sum += x[k] <= kMasked ? 0.f : exp2_fast((x[k] - top) * g.c2);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-  const float logs = log2f(a.s) - log2f(sum);
+  const float logs = log2_sum(a, g.c2) - log2f(sum);
   float loss = 0.f;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const int i = lane + 32 * k;
     if (i >= g.K) continue;
-    const float dt = fmaf(x[k], g.c2, -tc), p = x[k] <= kMasked ? 0.f : __fdiv_rn(exp2_fast(dt), sum);
+    const float dt = (x[k] - top) * g.c2, p = x[k] <= kMasked ? 0.f : __fdiv_rn(exp2_fast(dt), sum);
     d.p[parity][i] = p;
     if (p == 0.f) continue;
     const float z = d.z[parity][i];
-    loss += z <= kMasked ? INFINITY : p * ((dt - fmaf(z, g.c2, -a.mc)) + logs);
+    loss += z <= kMasked ? INFINITY : p * ((dt - (z - a.m) * g.c2) + logs);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xFFFFFFFFu, loss, o);
@@ -827,7 +840,7 @@ template <typename T, bool kGrad, int kThreads>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
 distill_kernel(const DistillArgs g) {
   constexpr bool kSlots = kThreads != kShort;
-  constexpr int kVec = Elem<T>::kVec, kStep = vector_step<kThreads>(), kSlotsRow = kGrad ? kSlotsTwice : kSlotsOnce;
+  constexpr int kVec = Elem<T>::kVec, kStep = vector_step<kThreads>(), kSlotsRow = kThreads == 1024 ? kSlotsTwice : kSlotsOnce;
   extern __shared__ __align__(128) uint8_t slots[];
   __shared__ RowShared sh;
   __shared__ DistillShared d;
@@ -905,7 +918,8 @@ distill_kernel(const DistillArgs g) {
       const float gp = zeros ? 0.f : w * g.scale;
       const float gq = zeros ? 0.f : bad ? NAN : gp / a.s;
       bool late = false;                                      // (a copy that did not come in time: the row is no number)
-      const f32x2 cc = pair_of(g.c2, g.c2), minus = pair_of(-a.mc, -a.mc);
+      const float c = factor(a.m, g.c2);
+      const f32x2 cc = pair_of(c, c), minus = pair_of(-a.mc, -a.mc);
       const f32x2 scale2 = pair_of(gq, gq);
       const uint32_t keep = zeros ? 0u : 0xFFFFFFFFu;
       uint4* const out = reinterpret_cast<uint4*>(grad - row.off);      // vector 0, where the gradient lies as the logits do
@@ -940,7 +954,7 @@ distill_kernel(const DistillArgs g) {
         if (i >= row.lo && i < row.hi) {
           float p = 0.f;
           for (int k = 0; k < g.K; ++k) p += d.id[parity][k] == id ? d.p[parity][k] : 0.f;
-          Elem<T>::store(grad + id, exp2_fast(fmaf(d.z[parity][tid], g.c2, -a.mc)) * gq - gp * p);
+          Elem<T>::store(grad + id, exp2_fast(fmaf(d.z[parity][tid], c, -a.mc)) * gq - gp * p);
         }
       }
       if (late && rank == 0) g.loss[n] = NAN;
@@ -1036,7 +1050,7 @@ int run_logprobs(LogprobArgs g, cudaStream_t st) {
 template <typename T, bool kGrad, int kThreads>
 int run_distill(DistillArgs g, cudaStream_t st) {
   static Resident known;
-  constexpr size_t smem = kThreads != kShort ? (size_t)(kGrad ? kSlotsTwice : kSlotsOnce) * kBatch * kThreads * 16 : 0;
+  constexpr size_t smem = kThreads != kShort ? (size_t)(kThreads == 1024 ? kSlotsTwice : kSlotsOnce) * kBatch * kThreads * 16 : 0;
   auto kernel = distill_kernel<T, kGrad, kThreads>;
   Plan p;
   const int rc = plan_rows(g.N, row_vectors(g.z, g.N, g.V, g.ld, sizeof(T)), kThreads, kGrad, p,
@@ -1051,7 +1065,7 @@ int run_distill(DistillArgs g, cudaStream_t st) {
 int launch_token_logprobs(const void* logits, int f32, int64_t N, int64_t V, int64_t ld, float scale, const int32_t* ids, int K,
                           float* logp, float* entropy, float* lse, int32_t* top_ids, float* top_logp, cudaStream_t st) {
   LogprobArgs g{};
-  g.z = logits; g.N = N; g.ld = ld; g.V = (int)V; g.K = K; g.c2 = scale * kLog2e;
+  g.z = logits; g.N = N; g.ld = ld; g.V = (int)V; g.K = K; g.c2 = scale * kLog2e; g.scale = scale;
   g.ids = ids; g.logp = logp; g.entropy = entropy; g.lse = lse; g.top_ids = top_ids; g.top_logp = top_logp;
   auto of_type = [&](auto type, auto threads) {
     using T = decltype(type);

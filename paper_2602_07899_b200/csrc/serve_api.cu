@@ -160,6 +160,9 @@ int tlq_token_logprobs(const void* logits, int dtype, int64_t N, int64_t V, int6
   if (N > 0) {              // (buffers of no rows may be NULL)
     if ((ids == nullptr) != (logp == nullptr) || (K > 0) != (top_ids != nullptr) || (K > 0) != (top_logp != nullptr)) return TLQ_ERR_INVALID_ARG;
     if (logp == nullptr && entropy == nullptr && lse == nullptr && K == 0) return TLQ_ERR_INVALID_ARG;
+    const struct { const void* p; int64_t bytes; } out[5] = {{logp, N * 4}, {entropy, N * 4}, {lse, N * 4}, {top_ids, N * K * 4}, {top_logp, N * K * 4}};
+    for (const auto& o : out)
+      if (overlap(o.p, o.bytes, logits, row_bytes(N, V, ld, dtype == TLQ_DTYPE_F32 ? 4 : 2)) || overlap(o.p, o.bytes, ids, N * 4)) return TLQ_ERR_INVALID_ARG;
   }
   rc = have_device();
   if (rc != TLQ_OK || N == 0) return rc;
@@ -173,6 +176,9 @@ int tlq_distill_loss(const void* logits, int dtype, int64_t N, int64_t V, int64_
   if (rc != TLQ_OK) return rc;
   if (K < 1) return TLQ_ERR_SHAPE;
   if (N > 0 && (top_ids == nullptr || top_logits == nullptr || loss == nullptr)) return TLQ_ERR_INVALID_ARG;
+  if (overlap(loss, N * 4, logits, row_bytes(N, V, ld, dtype == TLQ_DTYPE_F32 ? 4 : 2)) || overlap(loss, N * 4, top_ids, N * K * 4) ||
+      overlap(loss, N * 4, top_logits, N * K * 4) || overlap(loss, N * 4, weights, N * 4))
+    return TLQ_ERR_INVALID_ARG;
   if (grad != nullptr) {
     const int64_t size = dtype == TLQ_DTYPE_F32 ? 4 : 2;
     if (ldg < V || ldg > (1LL << 32)) return TLQ_ERR_SHAPE;

@@ -78,20 +78,21 @@ def test_product_refusals(tlq, addr):
 
 
 def test_logprobs_refusals(tlq, addr):
-    a = addr
+    a, o = addr, addr + 8192
 
-    def call(z=a, dt=0, n=4, v=100, ld=100, scale=1.0, ids=None, k=0, logp=None, ent=None, lse=a, tid=None, tlp=None):
+    def call(z=a, dt=0, n=4, v=100, ld=100, scale=1.0, ids=None, k=0, logp=None, ent=None, lse=o, tid=None, tlp=None):
         return tlq.lib.tlq_token_logprobs(z, dt, n, v, ld, scale, ids, k, logp, ent, lse, tid, tlp, None)
 
-    for bad in (dict(n=-1), dict(v=0), dict(v=(1 << 24) + 1, ld=1 << 25), dict(ld=99), dict(ld=0), dict(ld=1 << 33), dict(k=-1), dict(k=129, tid=a, tlp=a),
+    for bad in (dict(n=-1), dict(v=0), dict(v=(1 << 24) + 1, ld=1 << 25), dict(ld=99), dict(ld=0), dict(ld=1 << 33), dict(k=-1), dict(k=129, tid=o, tlp=o),
                 dict(n=1 << 28)):
         assert call(**bad) == tlq.ERR_SHAPE, bad
     for bad in (dict(z=None), dict(dt=2), dict(dt=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=NAN), dict(scale=INF), dict(scale=2.0 ** 17),
-                dict(scale=2.0 ** -17), dict(lse=None), dict(ids=a), dict(logp=a), dict(k=3), dict(k=3, tid=a), dict(tid=a, tlp=a)):
+                dict(scale=2.0 ** -17), dict(lse=None), dict(ids=a), dict(logp=a), dict(k=3), dict(k=3, tid=o), dict(tid=o, tlp=o), dict(lse=a), dict(lse=a + 700),
+                dict(ids=o, logp=o + 8), dict(k=3, tid=a + 8, tlp=o)):
         assert call(**bad) == tlq.ERR_INVALID_ARG, bad
     for bad in (dict(z=a + 1), dict(z=a + 2, dt=1)):
         assert call(**bad) == tlq.ERR_ALIGN, bad
-    for fine in (dict(), dict(z=a + 2), dict(z=a + 4, dt=1), dict(k=128, tid=a, tlp=a), dict(ids=a, logp=a, lse=None), dict(scale=2.0 ** -16), dict(scale=2.0 ** 16)):
+    for fine in (dict(), dict(z=a + 2), dict(z=a + 4, dt=1), dict(k=128, tid=o, tlp=o), dict(ids=a, logp=o, lse=None), dict(scale=2.0 ** -16), dict(scale=2.0 ** 16)):
         no_device(tlq, lambda: call(**fine))
 
 
@@ -105,7 +106,7 @@ def test_distill_refusals(tlq, addr):
         assert call(**bad) == tlq.ERR_SHAPE, bad
     for bad in (dict(z=None), dict(dt=3), dict(scale=0.0), dict(scale=NAN), dict(ids=None), dict(top=None), dict(loss=None), dict(grad=a + 2, ldg=100),
                 dict(grad=a, ldg=104), dict(grad=a + 200, ldg=100), dict(grad=a + 8192, ldg=100), dict(grad=a + 12288, ldg=100),
-                dict(grad=a + 4096, ldg=100, w=a + 4200)):
+                dict(grad=a + 4096, ldg=100, w=a + 4200), dict(loss=a), dict(loss=a + 8192), dict(w=a + 12288)):
         assert call(**bad) == tlq.ERR_INVALID_ARG, bad
     for bad in (dict(z=a + 1), dict(grad=a + 4097, ldg=100), dict(dt=1, grad=a + 4098, ldg=100)):
         assert call(**bad) == tlq.ERR_ALIGN, bad
