@@ -1,4 +1,4 @@
-"""Scale search of a layer's linears whose inputs live in (pinned) host memory.
+"""Scale search of a layer's linears whose inputs live in (pinned) host memory, and the importance of tokens from a teacher.
 
 The searches themselves are the library's kernels (`tlq_scale_search_layer`); what this module adds is
 plumbing only: per-linear staging buffers on the device, a side stream for the host-to-device copies,
@@ -106,3 +106,27 @@ class HostLayerSearch:
         st = tlq.tlq_read_status(self.workspace)
         if st != tlq.OK:
             raise tlq.TlqError(st, "HostLayerSearch")
+
+
+def importance_from_teacher(logits: torch.Tensor, top_ids: torch.Tensor, top_logits: torch.Tensor, weights: Optional[torch.Tensor] = None,
+                            scale: float = 1.0, norm_kind: int = tlq.NORM_L2, top_frac: float = 0.5
+                            ) -> Tuple[torch.Tensor, Optional[torch.Tensor], torch.Tensor]:
+    """How much each calibration token says about what quantization changed at the model's output: the norm of the distillation loss's
+    gradient by the token's logits (gradient-derived importance, paper Sec. 3.1.2, with the full-precision model's answers in the place of
+    labels).
+
+    logits [N,V] (bf16 or float32) of the quantized model, top_ids and top_logits [N,K] the full-precision model's alternatives
+    (tlq_token_logprobs' top_ids and top_logp), weights float32 [N] or None.  -> (importance float32 [N], mask of the top_frac most
+    important tokens or None, loss float32 [N]).  V may be any: the gradient's rows are laid out in whole 16-byte pieces.
+    """
+    n, v = logits.shape
+    wide = -(-v // 8) * 8
+    if wide == v:
+        loss, grad = tlq.tlq_distill_loss(logits, top_ids, top_logits, weights, scale)
+    else:       # (zeros behind a row add nothing to its norm)
+        grad = torch.zeros((n, wide), dtype=logits.dtype, device=logits.device)
+        loss, _ = tlq.tlq_distill_loss(logits, top_ids, top_logits, weights, scale, grad=grad[:, :v])
+    imp, mask = tlq.tlq_token_importance(grad[None], norm_kind, top_frac)
+    if norm_kind == tlq.NORM_MEAN_ABS and wide != v:
+        imp *= wide / v
+    return imp, mask, loss

@@ -514,3 +514,19 @@ def test_from_a_teachers_alternatives_to_the_importance_of_tokens(tlq):
     # these weights go where the calibration takes the importance of tokens
     best_scale = tlq.tlq_scale_search_layer(first["y"], head, imp, cfg)
     assert 0 <= int(best_scale.best_idx) < cfg.n_grid
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("v", [1000, 4093])
+def test_importance_from_a_teacher(tlq, v, dtype):
+    from paper_2602_07899_b200 import calibrate
+    n = 60
+    z = logits_of(n, v, dtype)
+    ids, top = teacher_of(z, 20)
+    w = weights_of(n)
+    loss, grad = tlq.tlq_distill_loss(z, ids, top, w)
+    for kind, norm in ((tlq.NORM_L2, grad.double().norm(dim=1)), (tlq.NORM_MEAN_ABS, grad.double().abs().mean(1))):
+        imp, mask, got = calibrate.importance_from_teacher(z, ids, top, w, norm_kind=kind)
+        assert torch.equal(got, loss) and int(mask.sum()) == n // 2
+        assert torch.all((imp.double() - norm).abs() <= 1e-5 * norm)          # (an fp32 result of fp64 sums of fp32 parts)
+        assert float(imp[mask.bool()].min()) >= float(imp[~mask.bool()].max())
