@@ -387,7 +387,8 @@ int tlq_kv_attention(const void* q, int64_t T, int64_t ldq, int32_t n_heads, con
  *    memory.  1 <= V <= 2^24.  `scale` (one over the temperature) multiplies the logits, 2^-16 <= scale <= 2^16.
  *  - Logits of -2^100 and below count as masked, like -infinity: probability 0.  A row with a NaN or +infinity, or whose largest logit
  *    leaves the 32-bit range when multiplied by scale, has no distribution: its numbers are NaN, its alternatives -1.
- *  - N = 0 is TLQ_OK and launches nothing.  The calls use no workspace; results do not depend on timing.
+ *  - N = 0 is TLQ_OK and launches nothing.  The calls use no workspace; results do not depend on timing.  Outputs lie over no input but
+ *    as said, nor over one another.
  */
 #define TLQ_MAX_TOP 128
 

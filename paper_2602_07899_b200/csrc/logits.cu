@@ -836,7 +836,43 @@ __device__ __forceinline__ float teacher_loss(const DistillArgs& g, const Stat& 
   return kLn2 * loss;
 }
 
-template <typename T, bool kGrad, int kThreads>
+// A lane's vector of 32 that follow one another, to an address off the grid: the elements before the grid's next line go with the lane before, and
+// the next lane's first ones come here.  `beyond`: what lane 0 gives to lane 31, where there is `more`.  The first vector's first elements
+// (`begin`) and the last one's last ones are written one by one.
+// (2048 x 131072 with an odd pitch of the gradient: 842 us with all elements one by one, 293 so, 200 where the grids agree.)
+template <typename T>
+__device__ __forceinline__ void store_off_grid(T* to, const uint4& y, const uint4& beyond, bool begin, bool more) {
+  constexpr int kVec = Elem<T>::kVec;
+  const int lane = threadIdx.x & 31, ahead = kVec - (int)((reinterpret_cast<uintptr_t>(to) & 15u) / sizeof(T));    // elements before the next line
+  const bool give = lane == 0 && more;
+  uint32_t w[8] = {y.x, y.y, y.z, y.w};
+  w[4] = __shfl_sync(0xFFFFFFFFu, give ? beyond.x : y.x, (lane + 1) & 31);
+  w[5] = __shfl_sync(0xFFFFFFFFu, give ? beyond.y : y.y, (lane + 1) & 31);
+  w[6] = __shfl_sync(0xFFFFFFFFu, give ? beyond.z : y.z, (lane + 1) & 31);
+  w[7] = __shfl_sync(0xFFFFFFFFu, give ? beyond.w : y.w, (lane + 1) & 31);
+  const int words = ahead * (int)sizeof(T) / 4;
+#pragma unroll
+  for (int j = 0; j < 6; ++j) w[j] = (words & 2) ? w[j + 2] : w[j];
+#pragma unroll
+  for (int j = 0; j < 5; ++j) w[j] = (words & 1) ? w[j + 1] : w[j];
+  const uint32_t bits = sizeof(T) == 2 && (ahead & 1) ? 16u : 0u;
+  if (lane < 31 || more) {
+    *reinterpret_cast<uint4*>(to + ahead) = make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits),
+                                                       __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+  } else {
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+      if (j >= ahead) Elem<T>::put_into(to + j, y, j);
+  }
+  if (lane == 0 && begin) {
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+      if (j < ahead) Elem<T>::put_into(to + j, y, j);
+  }
+}
+
+// kShift: the gradient's rows do not all lie as the logits' do on the memory's grid.
+template <typename T, bool kGrad, int kThreads, bool kShift>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
 distill_kernel(const DistillArgs g) {
   constexpr bool kSlots = kThreads != kShort;
@@ -860,7 +896,7 @@ distill_kernel(const DistillArgs g) {
     if (g.weights != nullptr && n + rows.step < g.N) w_next = load_near(g.weights + n + rows.step);
     const Row<T> row(reinterpret_cast<const T*>(g.z), n, g.ld, g.V, rank, g.ctas);
     T* grad = kGrad ? reinterpret_cast<T*>(g.grad) + n * g.ldg : nullptr;
-    const bool aligned = kGrad && ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(row.z)) & 15u) == 0;
+    const bool aligned = kGrad && (!kShift || ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(row.z)) & 15u) == 0);
     auto store = [&](int i, const uint4& y) {
       if (aligned && row.whole(i)) {
         *reinterpret_cast<uint4*>(grad + row.first(i)) = y;
@@ -870,8 +906,13 @@ distill_kernel(const DistillArgs g) {
           if (row.first(i) + j >= 0 && row.first(i) + j < row.V) Elem<T>::put_into(grad + row.first(i) + j, y, j);
       }
     };
-    auto store_zeros = [&]() {
-      for (int i = row.lo + tid; i < row.hi; i += kThreads) store(i, make_uint4(0, 0, 0, 0));
+    auto store_zeros = [&]() {                                // of this CTA's part: on the gradient's own grid, and one by one at its ends
+      T* const from = grad + max(0, row.first(row.lo)), * const to = grad + min(g.V, row.first(row.hi));
+      const int lead_in = (int)((0u - (uint32_t)reinterpret_cast<uintptr_t>(from)) & 15u) / (int)sizeof(T), all = (int)(to - from);
+      const int body = all > lead_in ? (all - lead_in) / kVec : 0, rest = min(all, lead_in) + body * kVec;
+      for (int i = tid; i < body; i += kThreads) *reinterpret_cast<uint4*>(from + lead_in + i * kVec) = make_uint4(0, 0, 0, 0);
+      if (tid < min(all, lead_in)) Elem<T>::store(from + tid, 0.f);
+      if (tid < all - rest) Elem<T>::store(from + rest + tid, 0.f);
     };
     if (w == 0.f) {                                           // the same for all CTAs of the row, which is not read
       if (rank == 0 && tid == 0) g.loss[n] = 0.f;
@@ -931,7 +972,7 @@ distill_kernel(const DistillArgs g) {
 #pragma unroll
           for (int u = 0; u < kBatch; ++u) v[u] = i + u * kStep < row.hi ? row.load(i + u * kStep) : row.none();
         }
-        const bool inside = kSlots && aligned && row.inside(i - lane);
+        const bool piece = kSlots && row.inside(i - lane), inside = aligned && piece;
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
           f32x2 x[Elem<T>::kPairs];
@@ -943,8 +984,21 @@ distill_kernel(const DistillArgs g) {
           }
           uint4 y = Elem<T>::pack(x);
           y.x &= keep; y.y &= keep; y.z &= keep; y.w &= keep;
-          if (inside) out[i + u * kStep] = y;
+          if constexpr (kShift) v[u] = y;
+          else if (inside) out[i + u * kStep] = y;
           else if (i + u * kStep < row.hi) store(i + u * kStep, y);
+        }
+        if constexpr (kShift) {
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u) {
+            const int k = i + u * kStep;
+            if (!aligned && (piece || __all_sync(0xFFFFFFFFu, k < row.hi && row.whole(k)))) {
+              const bool joined = piece && u + 1 < kBatch;    // (the lanes' next vectors follow those of lane 31)
+              store_off_grid<T>(grad + row.first(k), v[u], v[u + 1 < kBatch ? u + 1 : u], !piece || u == 0, joined);
+            } else if (k < row.hi) {
+              store(k, v[u]);
+            }
+          }
         }
       }
       __syncthreads();
@@ -970,6 +1024,9 @@ distill_kernel(const DistillArgs g) {
 }
 
 // ---------------------------------------------------------------------------------------------- launches
+// Rows of 32-bit logits of which nothing is kept in shared memory are short to half of that (4096 x 4000 with 16 KB: log probabilities
+// 26.6 us as short rows, 21.2 as long ones, gradient 61 and 40; 2000 with 8 KB: no difference; of 16 bits, 8000: 21.2 and 25.8, 43 and 44).
+constexpr int64_t short_row(int f32) { return f32 ? kShortRow / 2 : kShortRow; }
 constexpr int64_t kRowsUnderWay = 48 << 20;  // bytes of rows that are to be found again in the second-level cache
 
 struct Plan {
@@ -1047,11 +1104,11 @@ int run_logprobs(LogprobArgs g, cudaStream_t st) {
   return launch_next(kernel, dim3((unsigned)(p.rows * p.ctas)), kThreads, smem, (unsigned)p.ctas, st, g);
 }
 
-template <typename T, bool kGrad, int kThreads>
+template <typename T, bool kGrad, int kThreads, bool kShift>
 int run_distill(DistillArgs g, cudaStream_t st) {
   static Resident known;
   constexpr size_t smem = kThreads != kShort ? (size_t)(kThreads == 1024 ? kSlotsTwice : kSlotsOnce) * kBatch * kThreads * 16 : 0;
-  auto kernel = distill_kernel<T, kGrad, kThreads>;
+  auto kernel = distill_kernel<T, kGrad, kThreads, kShift>;
   Plan p;
   const int rc = plan_rows(g.N, row_vectors(g.z, g.N, g.V, g.ld, sizeof(T)), kThreads, kGrad, p,
                            [&](int c) { return resident_clusters(kernel, known, kThreads, smem, c); });
@@ -1075,7 +1132,7 @@ int launch_token_logprobs(const void* logits, int f32, int64_t N, int64_t V, int
   };
   const std::integral_constant<int, kShort> few;
   const std::integral_constant<int, kLong> many;
-  const bool is_short = V * (f32 ? 4 : 2) <= kShortRow;
+  const bool is_short = V * (f32 ? 4 : 2) <= (K > 0 ? kShortRow : short_row(f32));
   if (f32) return is_short ? of_type(0.f, few) : of_type(0.f, many);
   return is_short ? of_type((uint16_t)0, few) : of_type((uint16_t)0, many);
 }
@@ -1087,17 +1144,22 @@ int launch_distill_loss(const void* logits, int f32, int64_t N, int64_t V, int64
   DistillArgs g{};
   g.z = logits; g.N = N; g.ld = ld; g.V = (int)V; g.K = K; g.c2 = scale * kLog2e; g.scale = scale;
   g.ids = top_ids; g.top = top_logits; g.weights = weights; g.loss = loss; g.grad = grad; g.ldg = ldg;
+  const bool is_short = V * (f32 ? 4 : 2) <= short_row(f32);
+  auto with_grad = [&](auto type, auto off_grid) {
+    using T = decltype(type);
+    constexpr bool kShift = decltype(off_grid)::value;
+    if (is_short) return run_distill<T, true, kShort, kShift>(g, st);
+    // the smallest CTAs whose rows under way stay in the second-level cache
+    const int64_t row = V * (int64_t)sizeof(T), most = kRowsUnderWay / row;
+    return N <= most || 4 * sms <= most ? run_distill<T, true, 256, kShift>(g, st)
+                                        : 2 * sms <= most ? run_distill<T, true, 512, kShift>(g, st) : run_distill<T, true, 1024, kShift>(g, st);
+  };
   auto of_type = [&](auto type) {
     using T = decltype(type);
-    const bool is_short = V * (int64_t)sizeof(T) <= kShortRow;
-    if (grad != nullptr) {
-      if (is_short) return run_distill<T, true, kShort>(g, st);
-      // the smallest CTAs whose rows under way stay in the second-level cache
-      const int64_t row = V * (int64_t)sizeof(T), most = kRowsUnderWay / row;
-      return N <= most || 4 * sms <= most ? run_distill<T, true, 256>(g, st)
-                                          : 2 * sms <= most ? run_distill<T, true, 512>(g, st) : run_distill<T, true, 1024>(g, st);
-    }
-    return is_short ? run_distill<T, false, kShort>(g, st) : run_distill<T, false, kLong>(g, st);
+    if (grad == nullptr) return is_short ? run_distill<T, false, kShort, false>(g, st) : run_distill<T, false, kLong, false>(g, st);
+    const bool alike = ((reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(grad)) & 15u) == 0 &&
+                       (N == 1 || (ld - ldg) * (int64_t)sizeof(T) % 16 == 0);
+    return alike ? with_grad(type, std::false_type()) : with_grad(type, std::true_type());
   };
   return f32 ? of_type(0.f) : of_type((uint16_t)0);
 }

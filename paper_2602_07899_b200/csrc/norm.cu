@@ -203,7 +203,7 @@ norm_quantize_kernel(const NormArgs a) {
       if (tid == 0) a.steps[n] = NAN;
       continue;
     }
-    const float step = fmaxf(largest, TLQ_RANGE_FLOOR) * a.inv_qpos, k = __fdividef(root, step);
+    const float step = fmaxf(largest, TLQ_RANGE_FLOOR) * a.inv_qpos, k = __fdiv_rn(root, step);
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
       if (!in[p]) continue;

@@ -161,8 +161,12 @@ int tlq_token_logprobs(const void* logits, int dtype, int64_t N, int64_t V, int6
     if ((ids == nullptr) != (logp == nullptr) || (K > 0) != (top_ids != nullptr) || (K > 0) != (top_logp != nullptr)) return TLQ_ERR_INVALID_ARG;
     if (logp == nullptr && entropy == nullptr && lse == nullptr && K == 0) return TLQ_ERR_INVALID_ARG;
     const struct { const void* p; int64_t bytes; } out[5] = {{logp, N * 4}, {entropy, N * 4}, {lse, N * 4}, {top_ids, N * K * 4}, {top_logp, N * K * 4}};
-    for (const auto& o : out)
-      if (overlap(o.p, o.bytes, logits, row_bytes(N, V, ld, dtype == TLQ_DTYPE_F32 ? 4 : 2)) || overlap(o.p, o.bytes, ids, N * 4)) return TLQ_ERR_INVALID_ARG;
+    for (int i = 0; i < 5; ++i) {
+      if (overlap(out[i].p, out[i].bytes, logits, row_bytes(N, V, ld, dtype == TLQ_DTYPE_F32 ? 4 : 2)) || overlap(out[i].p, out[i].bytes, ids, N * 4))
+        return TLQ_ERR_INVALID_ARG;
+      for (int j = 0; j < i; ++j)
+        if (overlap(out[i].p, out[i].bytes, out[j].p, out[j].bytes)) return TLQ_ERR_INVALID_ARG;
+    }
   }
   rc = have_device();
   if (rc != TLQ_OK || N == 0) return rc;

@@ -615,9 +615,9 @@ def tlq_linear_i8_act(Xq: torch.Tensor, t: torch.Tensor, Wq: torch.Tensor, u: to
         _typed(bias, _BF16, (C2,), "bias")
     ldr = 0
     if residual is not None:
-        ldr = _rows(residual, "residual")
         if residual.shape != (N, width):
             raise ValueError(f"residual must have the result's shape {(N, width)}, got {tuple(residual.shape)}")
+        ldr = _rows(residual, "residual")
     if workspace is not None and not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
     dev = Xq.get_device()
@@ -661,9 +661,9 @@ def tlq_norm_quantize(x: torch.Tensor, w: Optional[torch.Tensor], cfg: Optional[
     dev = x.get_device()
     here = dev >= 0 and dev == _raw_device()
     if residual is not None:
-        ldr = C if residual.dtype is _BF16 and residual.is_contiguous() else _rows(residual, "residual")
         if residual.shape != shape:
             raise ValueError("x and residual must have one shape")
+        ldr = C if residual.dtype is _BF16 and residual.is_contiguous() else _rows(residual, "residual")
         here = here and residual.get_device() == dev
     if w is not None:
         if w.dtype is not _BF16 or w.ndim != 1 or w.numel() != C or not w.is_contiguous():
@@ -681,9 +681,9 @@ def tlq_norm_quantize(x: torch.Tensor, w: Optional[torch.Tensor], cfg: Optional[
     like, empty = (torch.empty_like, x.new_empty) if stream is None else (functools.partial(_made_on, stream, torch.empty_like),
                                                                           functools.partial(_made_on, stream, x.new_empty))
     if h is not None:
-        ldh = _rows(h, "h")
         if h.shape != shape:
             raise ValueError("h must have the shape of x")
+        ldh = _rows(h, "h")
     elif residual is not None:
         h, ldh = like(x), C
     codes = steps = values = y = None

@@ -330,6 +330,25 @@ def test_distill_of_strided_rows_at_any_alignment_and_in_place(tlq, v, pitch, dt
         wide.fill_(5.0)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,v,pitch,start", [(6, 1, 3, 1), (6, 5, 9, 2), (40, 77, 80, 3), (700, 1000, 1001, 1), (5, 4090, 4099, 6), (5, 8193, 8200, 0),
+                                             (700, 20011, 20012, 5), (600, 65537, 65544, 0), (3, 262147, 262150, 7)])
+def test_distill_gradient_that_lies_elsewhere_on_the_grid_than_the_logits(tlq, n, v, pitch, start, dtype):
+    """Rows of the gradient at all offsets from those of the logits: the same gradient bit for bit, and nothing beside it touched."""
+    z = logits_of(n, v, dtype)
+    ids, top = teacher_of(z, min(v, 7))
+    w = weights_of(n)
+    w[1::3] = 0.0
+    loss, want = tlq.tlq_distill_loss(z, ids, top, w)
+    buf = torch.full((n * pitch + 16,), 7.0, dtype=dtype, device="cuda")
+    grad = buf[start:start + n * pitch].view(n, pitch)[:, :v]
+    again, _ = tlq.tlq_distill_loss(z, ids, top, w, grad=grad)
+    assert torch.equal(again, loss) and torch.equal(grad, want)
+    rest = torch.ones_like(buf, dtype=torch.bool)
+    rest[start:start + n * pitch].view(n, pitch)[:, :v] = False
+    assert torch.all(buf[rest] == 7)
+
+
 def test_distill_in_place_with_a_row_over_several_ctas(tlq):
     for n, v, dtype in ((1, 262147, F32), (5, 131072, BF16), (300, 131072, BF16)):
         z = logits_of(n, v, dtype)

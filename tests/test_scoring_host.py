@@ -88,11 +88,12 @@ def test_logprobs_refusals(tlq, addr):
         assert call(**bad) == tlq.ERR_SHAPE, bad
     for bad in (dict(z=None), dict(dt=2), dict(dt=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=NAN), dict(scale=INF), dict(scale=2.0 ** 17),
                 dict(scale=2.0 ** -17), dict(lse=None), dict(ids=a), dict(logp=a), dict(k=3), dict(k=3, tid=o), dict(tid=o, tlp=o), dict(lse=a), dict(lse=a + 700),
-                dict(ids=o, logp=o + 8), dict(k=3, tid=a + 8, tlp=o)):
+                dict(ids=o, logp=o + 8), dict(k=3, tid=a + 8, tlp=o + 4096), dict(ent=o), dict(ent=o + 12), dict(k=3, tid=o + 4096, tlp=o + 4140),
+                dict(k=3, tid=o + 8, tlp=o + 4096)):
         assert call(**bad) == tlq.ERR_INVALID_ARG, bad
     for bad in (dict(z=a + 1), dict(z=a + 2, dt=1)):
         assert call(**bad) == tlq.ERR_ALIGN, bad
-    for fine in (dict(), dict(z=a + 2), dict(z=a + 4, dt=1), dict(k=128, tid=o, tlp=o), dict(ids=a, logp=o, lse=None), dict(scale=2.0 ** -16), dict(scale=2.0 ** 16)):
+    for fine in (dict(), dict(z=a + 2), dict(z=a + 4, dt=1), dict(k=128, tid=o + 4096, tlp=o + 8192), dict(ids=a, logp=o, lse=None), dict(scale=2.0 ** -16), dict(scale=2.0 ** 16)):
         no_device(tlq, lambda: call(**fine))
 
 
@@ -137,10 +138,10 @@ def test_binding_refuses_wrong_types_and_layouts(tlq, host):
     x = host["norm"]["x"]
     wrong = {
         "norm": (dict(x=x.float()), dict(x=x.t()), dict(residual=x[:1]), dict(residual=x.half()), dict(w=torch.zeros(31, dtype=BF16)),
-                 dict(w=torch.zeros(32)), dict(s=torch.zeros(64, dtype=BF16)[::2]), dict(want_codes=False, want_values=True), dict(h=x[:1]),
+                 dict(w=torch.zeros(32)), dict(s=torch.zeros(64, dtype=BF16)[::2]), dict(want_codes=False, want_values=True), dict(h=x[:1]), dict(residual=x[0]), dict(h=x[0]),
                  dict(want_codes=False, want_y=True, s=x[0]), dict(h=x.float())),
         "product": (dict(Xq=x), dict(t=torch.zeros(3)), dict(u=torch.zeros(7)), dict(Wq=torch.zeros(8, 16, dtype=I8)), dict(bias=torch.zeros(8)),
-                    dict(residual=torch.zeros(2, 8)), dict(residual=torch.zeros(2, 4, dtype=BF16)), dict(gated=True, residual=torch.zeros(2, 8, dtype=BF16)),
+                    dict(residual=torch.zeros(2, 8)), dict(residual=torch.zeros(8, dtype=BF16)), dict(residual=torch.zeros(2, 4, dtype=BF16)), dict(gated=True, residual=torch.zeros(2, 8, dtype=BF16)),
                     dict(residual=torch.zeros(2, 16, dtype=BF16)[:, ::2]), dict(workspace=torch.zeros(1, dtype=torch.uint8).expand(1 << 12))),
         "logprobs": (dict(logits=x.half()), dict(logits=x[0]), dict(logits=x.t()), dict(ids=torch.zeros(2)), dict(ids=torch.zeros(3, dtype=I32)),
                      dict(ids=torch.zeros(4, dtype=I32)[::2]), dict(top_k=129), dict(top_k=-1)),
