@@ -40,7 +40,7 @@ __device__ __forceinline__ pair2 both(float x) { return pair_of(x, x); }
 //  GELU          max(z, 0) - |z| tail(|z|), with the normal distribution's integral from a on, tail(a) = t P(t) e^(-a^2/2), t = 1 / (1 + 0.398 a),
 //                which turns all of a >= 0 into (0, 1].  P is a fit of lowest relative error to the quotient of both sides: off by
 //                2^-13.4 at most, a sixteenth of the rounding of the result to 8 bits.
-// (1025 tokens, 1280 -> 5120 with GELU: 52 us with CUDA's erfc, one at a time; 18.9 so; 16.4 without an activation.)
+// (1025 tokens, 1280 -> 5120 with GELU: 52 us with CUDA's erfc, one at a time; 19 so; 15.5 without an activation.)
 template <int kAct>
 __device__ __forceinline__ pair2 activate(pair2 z) {
   if constexpr (kAct == TLQ_ACT_SILU) return pmul(z, one_over(padd(both(1.f), exp2_of(pmul(z, both(-1.4426950408889634f))))));
