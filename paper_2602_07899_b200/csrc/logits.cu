@@ -32,7 +32,7 @@ constexpr int kBatch = 4;                 // vectors that a thread works on at a
 // Rows over 16 KB: CTAs of 256 threads, four to an SM, or of 256 to 1024 for the gradient; a warp has slots of kBatch vectors for each lane.
 constexpr int kShort = 128, kLong = 256;
 constexpr int kSlotsOnce = 2, kSlotsTwice = 3;            // (the latter for CTAs of 1024 threads: 405 us against 412; of 256 and 512 two are better)
-constexpr int kRuns = 16;                 // runs of batches of a thread that have a maximum of their own
+constexpr int kRuns = 16;                 // a thread's batches b, b + kRuns, ... are a run, which has a maximum of its own
 constexpr int kCandidates = kMaxCluster * kMaxTop;       // logits that may be among the largest: those of eight lists at least
 constexpr int64_t kShortRow = 16 << 10;   // bytes of rows that CTAs of kShort threads read straight from memory
 constexpr int kShortVectors = kShortRow / 16 + 1;
@@ -50,6 +50,11 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
+// All ones in the halves of a that are no less than those of b, as bf16; b of the upper half of a float, twice.
+__device__ __forceinline__ uint32_t at_least(uint32_t a, uint32_t b) {
+  return __hge2_mask(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+}
+__device__ __forceinline__ uint32_t reach_word(float least) { return (__float_as_uint(least) >> 16) * 0x10001u; }
 
 // ---------------------------------------------------------------------------------------------- elements and rows
 template <typename T>
@@ -83,6 +88,21 @@ struct Elem<uint16_t> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = pair_of(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
   }
+  // A bit for each element that is no less than `least`, and which element (of all in v) a bit stands for.
+  template <int n>
+  __device__ static uint32_t reach(const uint4 (&v)[n], float least) {
+    const uint32_t b = reach_word(least);
+    uint32_t hit = 0;
+#pragma unroll
+    for (int u = 0; u < n; ++u) {
+      hit |= at_least(v[u].x, b) & (0x10001u << (4 * u));
+      hit |= at_least(v[u].y, b) & (0x10001u << (4 * u + 1));
+      hit |= at_least(v[u].z, b) & (0x10001u << (4 * u + 2));
+      hit |= at_least(v[u].w, b) & (0x10001u << (4 * u + 3));
+    }
+    return hit;
+  }
+  __device__ static int element(int bit) { return 2 * (bit & 15) + (bit >> 4); }
   __device__ static void mask(uint32_t addr) { asm volatile("st.shared.b16 [%0], %1;" ::"r"(addr), "h"((uint16_t)kMaskedPair) : "memory"); }
   __device__ static uint32_t masked() { return kMaskedPair; }
   __device__ static uint4 pack(const f32x2 (&x)[kPairs]) {
@@ -124,6 +144,19 @@ struct Elem<float> {
     x[0] = pair_of(__uint_as_float(v.x), __uint_as_float(v.y));
     x[1] = pair_of(__uint_as_float(v.z), __uint_as_float(v.w));
   }
+  template <int n>
+  __device__ static uint32_t reach(const uint4 (&v)[n], float least) {
+    uint32_t hit = 0;
+#pragma unroll
+    for (int u = 0; u < n; ++u) {
+      hit |= __uint_as_float(v[u].x) >= least ? 1u << (4 * u) : 0u;
+      hit |= __uint_as_float(v[u].y) >= least ? 2u << (4 * u) : 0u;
+      hit |= __uint_as_float(v[u].z) >= least ? 4u << (4 * u) : 0u;
+      hit |= __uint_as_float(v[u].w) >= least ? 8u << (4 * u) : 0u;
+    }
+    return hit;
+  }
+  __device__ static int element(int bit) { return bit; }
   __device__ static void mask(uint32_t addr) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(kMasked) : "memory"); }
   __device__ static uint32_t masked() { return __float_as_uint(kMasked); }
   __device__ static uint4 pack(const f32x2 (&x)[kPairs]) {
@@ -422,6 +455,8 @@ __device__ __forceinline__ uint32_t in_order(float x) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float of_order(uint32_t o) { return __uint_as_float((o & 0x80000000u) ? o & 0x7FFFFFFFu : ~o); }
+// What a logit has to reach to come as far in the order; of masked logits all do.
+__device__ __forceinline__ float least_of(uint32_t order) { return order <= in_order(kMasked) ? -INFINITY : of_order(order); }
 __device__ __forceinline__ unsigned long long key_of(float x, int index) {
   return ((unsigned long long)in_order(x) << 32) | (0xFFFFFFFFu - (uint32_t)index);
 }
@@ -431,7 +466,7 @@ struct TopShared {
   static constexpr bool kShortRows = kThreads == kShort;
   union {
     unsigned long long keys[kCandidates];
-    uint16_t runs[kShortRows ? 1 : kRuns][kThreads];     // upper half of the order of the largest logit of each thread's runs, until they are listed
+    uint32_t runs[kShortRows ? 1 : kRuns / 2][kThreads]; // upper halves of the largest logit of each thread's runs 2 j and 2 j + 1, until they are listed
   };
   unsigned long long top[kMaxTop];        // of this CTA's part, largest first
   unsigned long long all[kShortRows ? 1 : kMaxTop];      // of the row
@@ -501,7 +536,7 @@ __device__ __forceinline__ uint32_t bound_of_lanes(uint32_t own, int share) {
   return bound;
 }
 
-// The largest K of this CTA's part of the row into sh.top.  `mine`: the largest logit of this thread's vectors; a run is `batches` batches.
+// The largest K of this CTA's part of the row into sh.top.  `mine`: the largest logit of this thread's vectors; a run has up to `batches` batches.
 template <typename T, int kThreads>
 __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine, int runs, int batches, TopShared<kThreads>& sh) {
   const int tid = threadIdx.x;
@@ -520,13 +555,14 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
 #pragma unroll
   for (int k = 0; k < kThreads / 32; ++k) bound = min(bound, sh.bounds[k]);
   if (any && own >= bound) {
-    uint32_t hit = 0;
+    const uint32_t least = reach_word(least_of(bound << 16));
+    uint32_t hit = 0;                                         // run 2 j: bit j, 2 j + 1: bit 16 + j
 #pragma unroll
-    for (int r = 0; r < kRuns; ++r) hit |= sh.runs[r][tid] >= bound ? 1u << r : 0u;
-    hit &= (1u << runs) - 1u;
+    for (int j = 0; j < kRuns / 2; ++j) hit |= at_least(sh.runs[j][tid], least) & (0x10001u << j);
+    hit &= ((1u << (runs + 1) / 2) - 1u) | (((1u << runs / 2) - 1u) << 16);
     for (; hit != 0; hit &= hit - 1) {
       const int at = atomicAdd(&sh.n_listed, 1);
-      if (at < kCandidates) sh.listed[at] = (uint16_t)((__ffs(hit) - 1) * kThreads + tid);
+      if (at < kCandidates) sh.listed[at] = (uint16_t)((((__ffs(hit) - 1) & 15) * 2 + ((__ffs(hit) - 1) >> 4)) * kThreads + tid);
     }
   }
   if (tid == 0) sh.n_keys = 0;
@@ -537,27 +573,16 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
   unsigned long long least = (unsigned long long)bound << 48;
   int n;
   while (true) {
-    const float least_z = least >> 32 == 0 ? -INFINITY : of_order((uint32_t)(least >> 32));
+    const float least_z = least_of((uint32_t)(least >> 32));
     for (int k = tid; k < total; k += kThreads) {
-      const int e = batches == 1 ? k : k / batches, which = all ? e : sh.listed[e], t = which % kThreads;
-      const int i = row.lo + (which / kThreads * batches + k - e * batches) * kThreads * kBatch + (kThreads == kShort ? t : (t >> 5) * kPiece + (t & 31));
+      const int entry = batches == 1 ? k : k / batches, which = all ? entry : sh.listed[entry], t = which % kThreads;
+      const int i = row.lo + (which / kThreads + (k - entry * batches) * kRuns) * kThreads * kBatch + (kThreads == kShort ? t : (t >> 5) * kPiece + (t & 31));
       uint4 v[kBatch];
 #pragma unroll
       for (int u = 0; u < kBatch; ++u)
         v[u] = i + u * vector_step<kThreads>() < row.hi ? load_once(row.z + row.first(i + u * vector_step<kThreads>())) : row.none();
-      uint32_t hit = 0;                                       // of the batch's elements, in the vectors' order
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        f32x2 x[Elem<T>::kPairs];
-        Elem<T>::pairs(Elem<T>::clamp(v[u]), x);
-#pragma unroll
-        for (int j = 0; j < Elem<T>::kVec; ++j) {
-          const float2 h = halves(x[j >> 1]);
-          hit |= ((j & 1) ? h.y : h.x) < least_z ? 0u : 1u << (u * Elem<T>::kVec + j);
-        }
-      }
-      for (; hit != 0; hit &= hit - 1) {
-        const int bit = __ffs(hit) - 1, from = i + bit / Elem<T>::kVec * vector_step<kThreads>(), at = row.first(from) + bit % Elem<T>::kVec;
+      for (uint32_t hit = Elem<T>::reach(v, least_z); hit != 0; hit &= hit - 1) {
+        const int e = Elem<T>::element(__ffs(hit) - 1), from = i + e / Elem<T>::kVec * vector_step<kThreads>(), at = row.first(from) + e % Elem<T>::kVec;
         if (at < 0 || at >= row.V || from >= row.hi) continue;
         const unsigned long long key = key_of(max_nan(Elem<T>::load(row.z + at), kMasked), at);
         if (key < least) continue;
@@ -631,18 +656,11 @@ __device__ __forceinline__ void top_of_short_row(const Row<T>& row, int K, float
   unsigned long long least = (unsigned long long)bound << 48;
   int n;
   while (true) {
-    const float least_z = least >> 32 == 0 ? -INFINITY : of_order((uint32_t)(least >> 32));
+    const float least_z = least_of((uint32_t)(least >> 32));
     for (int j = tid; j < vectors; j += kShort) {
-      f32x2 x[Elem<T>::kPairs];
-      Elem<T>::pairs(sh.row[j], x);
-      uint32_t hit = 0;
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const float2 h = halves(x[e >> 1]);
-        hit |= ((e & 1) ? h.y : h.x) < least_z ? 0u : 1u << e;
-      }
-      for (; hit != 0; hit &= hit - 1) {
-        const int e = __ffs(hit) - 1, at = row.first(row.lo + j) + e;
+      const uint4 v[1] = {sh.row[j]};
+      for (uint32_t hit = Elem<T>::reach(v, least_z); hit != 0; hit &= hit - 1) {
+        const int e = Elem<T>::element(__ffs(hit) - 1), at = row.first(row.lo + j) + e;
         if (at < 0 || at >= row.V) continue;
         const unsigned long long key = key_of(Elem<T>::get(reinterpret_cast<const T*>(sh.row + j)[e]), at);
         if (key < least) continue;
@@ -728,19 +746,17 @@ logprobs_kernel(const LogprobArgs g) {
       if (id >= 0 && id < g.V) z_id = Elem<T>::load(row.z + id);
     }
     Running<T, kEntropy> run(g.c2);
-    float run_top = kMasked;                                  // of the batches of a run
-    int runs = 0, run_left = g.batches;
+    int batch = 0;
     for (int i = first_vector<kThreads>(row.lo, 0); i - (kSlots ? (int)(threadIdx.x & 31) : (int)threadIdx.x) < row.hi; i += kBatch * kThreads) {
       uint4 v[kBatch];
       read_batch<T, kThreads, kEntropy>(row, i, pieces, &abort, v, run);
       const float largest = run.add(v);
       if constexpr (kTop && kSlots) {
-        run_top = fmaxf(run_top, largest);
-        if (--run_left == 0) {
-          top.runs[runs++][threadIdx.x] = (uint16_t)(in_order(run_top) >> 16);
-          run_top = kMasked;
-          run_left = g.batches;
-        }
+        uint16_t* const at = reinterpret_cast<uint16_t*>(&top.runs[batch / 2 % (kRuns / 2)][threadIdx.x]) + batch % 2;
+        float most = kEntropy ? largest : fmaxf(largest, kMasked);
+        if (batch >= kRuns) most = fmaxf(most, bf16_bits_to_float(*at));
+        *at = (uint16_t)(__float_as_uint(most) >> 16);
+        ++batch;
       }
       if constexpr (kTop && !kSlots) {
 #pragma unroll
@@ -748,8 +764,6 @@ logprobs_kernel(const LogprobArgs g) {
           if (i + u * kThreads < row.hi) top.row[i + u * kThreads - row.lo] = kEntropy ? v[u] : Elem<T>::clamp(v[u]);
       }
     }
-    if constexpr (kTop && kSlots)
-      if (run_left != g.batches) top.runs[runs++][threadIdx.x] = (uint16_t)(in_order(run_top) >> 16);
     const Stat a = join_row<kThreads>(run.stat(), g.c2, g.ctas, sh, parity);
     const float log2_s = log2_sum(a, g.c2);
     if (rank == 0 && threadIdx.x == 0) {
@@ -761,7 +775,7 @@ logprobs_kernel(const LogprobArgs g) {
     if constexpr (kTop) {
       const bool bad = isnan(a.s);                            // (the same in all CTAs of the row)
       if (!bad) {
-        if constexpr (kSlots) top_of_part<T, kThreads>(row, g.K, run.m, runs, g.batches, top);
+        if constexpr (kSlots) top_of_part<T, kThreads>(row, g.K, run.m, min(batch, kRuns), g.batches, top);
         else top_of_short_row<T>(row, g.K, run.m, top);
         if constexpr (kSlots)
           if (g.ctas > 1) join_tops<kThreads>(g.K, g.ctas, rank, top);
