@@ -103,6 +103,7 @@ struct Elem<uint16_t> {
     return hit;
   }
   __device__ static int element(int bit) { return 2 * (bit & 15) + (bit >> 4); }
+  __device__ static float value(uint32_t word, int bit) { return __uint_as_float(bit < 16 ? word << 16 : word & 0xFFFF0000u); }
   __device__ static void mask(uint32_t addr) { asm volatile("st.shared.b16 [%0], %1;" ::"r"(addr), "h"((uint16_t)kMaskedPair) : "memory"); }
   __device__ static uint32_t masked() { return kMaskedPair; }
   __device__ static uint4 pack(const f32x2 (&x)[kPairs]) {
@@ -157,6 +158,7 @@ struct Elem<float> {
     return hit;
   }
   __device__ static int element(int bit) { return bit; }
+  __device__ static float value(uint32_t word, int) { return __uint_as_float(word); }
   __device__ static void mask(uint32_t addr) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(kMasked) : "memory"); }
   __device__ static uint32_t masked() { return __float_as_uint(kMasked); }
   __device__ static uint4 pack(const f32x2 (&x)[kPairs]) {
@@ -524,6 +526,13 @@ __device__ __forceinline__ void place_keys(unsigned long long* keys, int n, int 
   }
 }
 
+// Word `i` of four vectors, without a detour through memory.
+__device__ __forceinline__ uint32_t word_of(const uint4 (&v)[4], int i) {
+  auto pick = [](bool second, const uint4& a, const uint4& b) { return make_uint4(second ? b.x : a.x, second ? b.y : a.y, second ? b.z : a.z, second ? b.w : a.w); };
+  const uint4 w = pick(i & 8, pick(i & 4, v[0], v[1]), pick(i & 4, v[2], v[3]));
+  return (i & 2) ? ((i & 1) ? w.w : w.z) : ((i & 1) ? w.y : w.x);
+}
+
 // A bound that `share` lanes at least reach: the largest that is left, and with it all lanes that have it, until there are enough.
 __device__ __forceinline__ uint32_t bound_of_lanes(uint32_t own, int share) {
   uint32_t bound = 0;
@@ -582,9 +591,9 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
       for (int u = 0; u < kBatch; ++u)
         v[u] = i + u * vector_step<kThreads>() < row.hi ? load_once(row.z + row.first(i + u * vector_step<kThreads>())) : row.none();
       for (uint32_t hit = Elem<T>::reach(v, least_z); hit != 0; hit &= hit - 1) {
-        const int e = Elem<T>::element(__ffs(hit) - 1), from = i + e / Elem<T>::kVec * vector_step<kThreads>(), at = row.first(from) + e % Elem<T>::kVec;
+        const int bit = __ffs(hit) - 1, e = Elem<T>::element(bit), from = i + e / Elem<T>::kVec * vector_step<kThreads>(), at = row.first(from) + e % Elem<T>::kVec;
         if (at < 0 || at >= row.V || from >= row.hi) continue;
-        const unsigned long long key = key_of(max_nan(Elem<T>::load(row.z + at), kMasked), at);
+        const unsigned long long key = key_of(fmaxf(Elem<T>::value(word_of(v, bit & 15), bit), kMasked), at);
         if (key < least) continue;
         const int to = atomicAdd(&sh.n_keys, 1);
         if (to < kCandidates) sh.keys[to] = key;
