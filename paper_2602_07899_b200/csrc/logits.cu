@@ -1053,29 +1053,39 @@ distill_kernel(const DistillArgs g) {
 constexpr int64_t short_row(int f32) { return f32 ? kShortRow / 2 : kShortRow; }
 constexpr int64_t kRowsUnderWay = 48 << 20;  // bytes of rows that are to be found again in the second-level cache
 
+constexpr double kRateSm = 43e3, kRateThread = 117;     // bytes in a us
 struct Plan {
   int ctas;                   // of a row
   int64_t rows;               // under way at a time
+  size_t smem;
 };
 // CTAs of a cluster share a row where rows are too few for all SMs, or do not go up evenly in those that can be under way, or where those
-// are not to be more than the second-level cache keeps (`again`).  The time of a row's part is estimated by its bytes at the share of the
-// memory's rate that a CTA has, and 2 us (3 with others) around it.
+// are not to be more than the second-level cache keeps (`again`).  `clusters(c, k)`: how many of c CTAs run at a time with k CTAs to an SM; k is
+// no larger than all rows need, or some SMs would get four CTAs and others one (300 x 131072: 21.5 us with 3, 26.7 with room for 4).
+// The time of a row's part is estimated by its bytes at the rate that a CTA has, alone or beside others on its SM, and what is around it: 2 us,
+// joining with others 1.6 to 2.2, and 0.8 more for their alternatives (1 x 131072 with 1, 2, 4, 8 CTAs: 10.9, 7.8, 5.7, 4.7 us, with 20
+// alternatives 14.8, 12.7, 10.7, 10.1; 140 x 50001 with 20: 10.4, 12.1, 13.8).
 template <typename F>
-int plan_rows(int64_t N, int64_t row /* vectors, at most */, int threads, bool again, Plan& p, F clusters) {
+int plan_rows(int64_t N, int64_t row /* vectors, at most */, int threads, bool again, bool tops, Plan& p, int& to_sm, F clusters) {
   double best = 0;
   p.ctas = 0;
   for (int c = 1; c <= kMaxCluster; c *= 2) {
     const int64_t part = ceil_div(row, c);
     if (c > 1 && (threads < kLong || part < threads * kBatch)) break;
-    const int64_t slots = clusters(c);
-    if (slots < 1) continue;
-    const int64_t rows = N < slots ? N : slots;
-    const double us = (double)ceil_div(N, slots) * ((double)part * 16 * (again ? 2 : 1) / (43.0 * threads) + (c > 1 ? 3.0 : 2.0));
-    const bool fits = rows * row * 16 <= kRowsUnderWay;
-    if (p.ctas == 0 || us < 0.97 * best || (again && fits && p.rows * row * 16 > kRowsUnderWay)) {
-      best = us;
-      p.ctas = c;
-      p.rows = rows;
+    for (int k = 1; k <= 1024 / threads; ++k) {
+      const int64_t slots = clusters(c, k);
+      if (slots < 1) continue;
+      const int64_t rows = N < slots ? N : slots;
+      const double rate = fmin(kRateSm / k, kRateThread * threads), around = 2.0 + (c > 1 ? (tops ? 2.2 : 1.4) + 0.1 * c : 0.0);
+      const double us = (double)ceil_div(N, slots) * ((double)part * 16 * (again ? 2 : 1) / rate + around);
+      const bool fits = rows * row * 16 <= kRowsUnderWay;
+      if (p.ctas == 0 || us < 0.97 * best || (again && fits && p.rows * row * 16 > kRowsUnderWay)) {
+        best = us;
+        p.ctas = c;
+        p.rows = rows;
+        to_sm = k;
+      }
+      if (slots >= N) break;
     }
   }
   return p.ctas == 0 ? TLQ_ERR_CUDA : TLQ_OK;
@@ -1085,33 +1095,51 @@ int64_t row_vectors(const void* z, int64_t N, int64_t V, int64_t ld, int64_t siz
   return ceil_div(V * size, 16) + (aligned16(z) && (N == 1 || ld * size % 16 == 0) ? 0 : 1);
 }
 
-// Clusters of `c` CTAs that a device runs at a time (asked once for each kernel, size and device).
+// What is asked once for each kernel and device: its shared memory, and the clusters of c CTAs that run at a time with k to an SM.
 struct Resident {
-  int count[kMaxDevices][4] = {};
+  size_t fixed[kMaxDevices] = {};
+  int count[kMaxDevices][4][8] = {};
 };
-template <typename Kernel>
-int64_t resident_clusters(Kernel kernel, Resident& known, int threads, size_t smem, int c) {
-  const int dev = current_device_index(), k = c == 1 ? 0 : c == 2 ? 1 : c == 4 ? 2 : 3;
-  if (dev < 0) return 0;
-  int& n = known.count[dev][k];
-  if (n == 0) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return 0;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(c * 1024));
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = smem;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)c;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
-      cudaGetLastError();
-      n = 0;
-    }
+constexpr size_t kSharedOfSm = 228 << 10, kSharedOfCta = 1 << 10;         // (the latter is the system's)
+template <int kThreads, typename Kernel>
+int plan_launch(Kernel kernel, Resident& known, size_t smem, int64_t N, int64_t row, bool again, bool tops, Plan& p) {
+  constexpr int kMost = 1024 / kThreads;
+  const int dev = current_device_index();
+  if (dev < 0) return TLQ_ERR_CUDA;
+  if (known.fixed[dev] == 0) {
+    cudaFuncAttributes attr;
+    TLQ_CUDA_TRY(cudaFuncGetAttributes(&attr, kernel));
+    TLQ_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(smem > kSharedOfSm / 2 + 1024 ? smem : kSharedOfSm / 2 + 1024)));
+    known.fixed[dev] = attr.sharedSizeBytes + kSharedOfCta;
   }
-  return n;
+  const size_t fixed = known.fixed[dev];
+  auto with = [&](int k) {    // shared memory of which k + 1 CTAs have no room on an SM
+    const size_t wanted = align_up(kSharedOfSm / (k + 1) + 1, 128);
+    return k >= kMost || wanted < fixed + smem ? smem : wanted - fixed;
+  };
+  int to_sm = kMost;
+  const int rc = plan_rows(N, row, kThreads, again, tops, p, to_sm, [&](int c, int k) -> int64_t {
+    int& n = known.count[dev][c == 1 ? 0 : c == 2 ? 1 : c == 4 ? 2 : 3][k - 1];
+    if (n == 0) {
+      cudaLaunchConfig_t cfg{};
+      cfg.gridDim = dim3((unsigned)(c * 1024));
+      cfg.blockDim = dim3((unsigned)kThreads);
+      cfg.dynamicSmemBytes = with(k);
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = (unsigned)c;
+      attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+      cfg.attrs = attr;
+      cfg.numAttrs = 1;
+      if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        n = 0;
+      }
+    }
+    return n;
+  });
+  p.smem = with(to_sm);
+  return rc;
 }
 
 template <typename T, bool kEntropy, bool kTop, int kThreads>
@@ -1121,11 +1149,11 @@ int run_logprobs(LogprobArgs g, cudaStream_t st) {
   auto kernel = logprobs_kernel<T, kEntropy, kTop, kThreads>;
   const int64_t vectors = row_vectors(g.z, g.N, g.V, g.ld, sizeof(T));
   Plan p;
-  const int rc = plan_rows(g.N, vectors, kThreads, false, p, [&](int c) { return resident_clusters(kernel, known, kThreads, smem, c); });
+  const int rc = plan_launch<kThreads>(kernel, known, smem, g.N, vectors, false, kTop, p);
   if (rc != TLQ_OK) return rc;
   g.ctas = p.ctas;
   g.batches = (int)ceil_div(ceil_div(ceil_div(vectors, p.ctas), (int64_t)kBatch * kThreads), kRuns);
-  return launch_next(kernel, dim3((unsigned)(p.rows * p.ctas)), kThreads, smem, (unsigned)p.ctas, st, g);
+  return launch_next(kernel, dim3((unsigned)(p.rows * p.ctas)), kThreads, p.smem, (unsigned)p.ctas, st, g);
 }
 
 template <typename T, bool kGrad, int kThreads, bool kShift>
@@ -1134,11 +1162,10 @@ int run_distill(DistillArgs g, cudaStream_t st) {
   constexpr size_t smem = kThreads != kShort ? (size_t)(kThreads == 1024 ? kSlotsTwice : kSlotsOnce) * kBatch * kThreads * 16 : 0;
   auto kernel = distill_kernel<T, kGrad, kThreads, kShift>;
   Plan p;
-  const int rc = plan_rows(g.N, row_vectors(g.z, g.N, g.V, g.ld, sizeof(T)), kThreads, kGrad, p,
-                           [&](int c) { return resident_clusters(kernel, known, kThreads, smem, c); });
+  const int rc = plan_launch<kThreads>(kernel, known, smem, g.N, row_vectors(g.z, g.N, g.V, g.ld, sizeof(T)), kGrad, false, p);
   if (rc != TLQ_OK) return rc;
   g.ctas = p.ctas;
-  return launch_next(kernel, dim3((unsigned)(p.rows * p.ctas)), kThreads, smem, (unsigned)p.ctas, st, g);
+  return launch_next(kernel, dim3((unsigned)(p.rows * p.ctas)), kThreads, p.smem, (unsigned)p.ctas, st, g);
 }
 
 }  // namespace
