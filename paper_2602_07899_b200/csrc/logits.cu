@@ -457,8 +457,9 @@ __device__ __forceinline__ uint32_t in_order(float x) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float of_order(uint32_t o) { return __uint_as_float((o & 0x80000000u) ? o & 0x7FFFFFFFu : ~o); }
-// What a logit has to reach to come as far in the order; of masked logits all do.
-__device__ __forceinline__ float least_of(uint32_t order) { return order <= in_order(kMasked) ? -INFINITY : of_order(order); }
+// A bound, in the order of logits, that none masked reaches, and the logit that stands there.
+__device__ __forceinline__ uint32_t above_mask(uint32_t order) { return max(order, in_order(kMasked) + 1u); }
+__device__ __forceinline__ float least_of(uint32_t order) { return of_order(above_mask(order)); }
 __device__ __forceinline__ unsigned long long key_of(float x, int index) {
   return ((unsigned long long)in_order(x) << 32) | (0xFFFFFFFFu - (uint32_t)index);
 }
@@ -579,7 +580,13 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
   // all of them where there are more than the list holds (equal logits in every run)
   const bool all = sh.n_listed > kCandidates;
   const int total = (all ? runs * kThreads : sh.n_listed) * batches;
-  unsigned long long least = (unsigned long long)bound << 48;
+  unsigned long long least = (unsigned long long)above_mask(bound << 16) << 32;
+  // Where the bound is no higher than the mask, fewer than K may be above it: the part's first masked logits are wanted then, which
+  // are among its first K.
+  if (bound << 16 <= in_order(kMasked) && tid < K) {
+    const int at = max(0, row.first(row.lo)) + tid;
+    if (at < min(row.V, row.first(row.hi)) && !(Elem<T>::load(row.z + at) > kMasked)) sh.keys[atomicAdd(&sh.n_keys, 1)] = key_of(kMasked, at);
+  }
   int n;
   while (true) {
     const float least_z = least_of((uint32_t)(least >> 32));
@@ -597,6 +604,7 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
         if (key < least) continue;
         const int to = atomicAdd(&sh.n_keys, 1);
         if (to < kCandidates) sh.keys[to] = key;
+        else k = total;                                       // (no room: enough has been seen)
       }
     }
     __syncthreads();
@@ -662,7 +670,11 @@ __device__ __forceinline__ void top_of_short_row(const Row<T>& row, int K, float
   bound = 0xFFFFu;
 #pragma unroll
   for (int k = 0; k < kShort / 32; ++k) bound = min(bound, sh.bounds[k]);
-  unsigned long long least = (unsigned long long)bound << 48;
+  unsigned long long least = (unsigned long long)above_mask(bound << 16) << 32;
+  if (bound << 16 <= in_order(kMasked) && tid < min(K, row.V)) {       // the first masked ones, as above
+    const int e = tid + row.off;
+    if (!(Elem<T>::get(reinterpret_cast<const T*>(sh.row)[e]) > kMasked)) sh.keys[atomicAdd(&sh.n_keys, 1)] = key_of(kMasked, tid);
+  }
   int n;
   while (true) {
     const float least_z = least_of((uint32_t)(least >> 32));
@@ -675,6 +687,7 @@ __device__ __forceinline__ void top_of_short_row(const Row<T>& row, int K, float
         if (key < least) continue;
         const int to = atomicAdd(&sh.n_keys, 1);
         if (to < kCandidates) sh.keys[to] = key;
+        else j = vectors;
       }
     }
     __syncthreads();

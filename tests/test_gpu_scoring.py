@@ -153,6 +153,26 @@ def test_alternatives_of_equal_logits_come_by_index(tlq, v, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,v", [(13, 300), (13, 8000), (13, 131072), (700, 20011), (1, 262147)])
+def test_alternatives_of_rows_with_few_or_crowded_tokens(tlq, n, v, dtype):
+    """All masked but some, side by side or strewn about: those come first, then the first of the masked ones."""
+    g = gen(v)
+    z = torch.randn(n, v, generator=g, device="cuda").to(dtype)
+    index = torch.arange(v, device="cuda")
+    allowed = torch.zeros(n, v, dtype=torch.bool, device="cuda")
+    for i, count in enumerate((0, 1, 5, 19, 20, 21, 63, 64, 65, 128, 129, 1000, 2000)):
+        for j in range(i, n, 13):
+            count = min(count, v)
+            start = (0, v - count, (v - count) // 2 + 3)[j % 3] if count < v - 8 else 0
+            allowed[j] = (index >= start) & (index < start + count)
+            if j % 4 == 3:
+                allowed[j] = allowed[j, torch.randperm(v, generator=g, device="cuda")]
+    z = torch.where(allowed, z, torch.tensor(-math.inf if v % 2 else -1e38, dtype=dtype, device="cuda"))
+    for k in (1, 20, 64, 128):
+        check_logprobs(tlq, z, None, k)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("v", [5000, 131072])
 def test_alternatives_in_orders_that_defeat_a_bound(tlq, v, dtype):
     """Rising and falling rows, and rows whose large logits all belong to a few threads: more of them than there is room for."""
