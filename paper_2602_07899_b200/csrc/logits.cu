@@ -464,6 +464,17 @@ __device__ __forceinline__ unsigned long long key_of(float x, int index) {
   return ((unsigned long long)in_order(x) << 32) | (0xFFFFFFFFu - (uint32_t)index);
 }
 
+// What logits have to reach for a key of `least` or more: that key's logit up to its index, a larger one behind it.
+template <typename T>
+struct KeyBound {
+  float least, larger;
+  int last;
+  __device__ explicit KeyBound(unsigned long long key)
+      : least(least_of((uint32_t)(key >> 32))), larger(least_of((uint32_t)(key >> 32) + (sizeof(T) == 2 ? 0x10000u : 1u))),
+        last((int)min(0xFFFFFFFFu - (uint32_t)key, 0x7FFFFFFFu)) {}
+  __device__ float from(int index) const { return index > last ? larger : least; }
+};
+
 template <int kThreads>
 struct TopShared {
   static constexpr bool kShortRows = kThreads == kShort;
@@ -589,7 +600,7 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
   }
   int n;
   while (true) {
-    const float least_z = least_of((uint32_t)(least >> 32));
+    const KeyBound<T> above(least);
     for (int k = tid; k < total; k += kThreads) {
       const int entry = batches == 1 ? k : k / batches, which = all ? entry : sh.listed[entry], t = which % kThreads;
       const int i = row.lo + (which / kThreads + (k - entry * batches) * kRuns) * kThreads * kBatch + (kThreads == kShort ? t : (t >> 5) * kPiece + (t & 31));
@@ -597,14 +608,14 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, int K, float mine
 #pragma unroll
       for (int u = 0; u < kBatch; ++u)
         v[u] = i + u * vector_step<kThreads>() < row.hi ? load_once(row.z + row.first(i + u * vector_step<kThreads>())) : row.none();
-      for (uint32_t hit = Elem<T>::reach(v, least_z); hit != 0; hit &= hit - 1) {
+      for (uint32_t hit = Elem<T>::reach(v, above.from(row.first(i))); hit != 0; hit &= hit - 1) {
         const int bit = __ffs(hit) - 1, e = Elem<T>::element(bit), from = i + e / Elem<T>::kVec * vector_step<kThreads>(), at = row.first(from) + e % Elem<T>::kVec;
         if (at < 0 || at >= row.V || from >= row.hi) continue;
         const unsigned long long key = key_of(fmaxf(Elem<T>::value(word_of(v, bit & 15), bit), kMasked), at);
         if (key < least) continue;
         const int to = atomicAdd(&sh.n_keys, 1);
         if (to < kCandidates) sh.keys[to] = key;
-        else k = total;                                       // (no room: enough has been seen)
+        else k = total, hit = 1;                              // (no room: enough has been seen)
       }
     }
     __syncthreads();
@@ -677,17 +688,17 @@ __device__ __forceinline__ void top_of_short_row(const Row<T>& row, int K, float
   }
   int n;
   while (true) {
-    const float least_z = least_of((uint32_t)(least >> 32));
+    const KeyBound<T> above(least);
     for (int j = tid; j < vectors; j += kShort) {
       const uint4 v[1] = {sh.row[j]};
-      for (uint32_t hit = Elem<T>::reach(v, least_z); hit != 0; hit &= hit - 1) {
+      for (uint32_t hit = Elem<T>::reach(v, above.from(row.first(row.lo + j))); hit != 0; hit &= hit - 1) {
         const int e = Elem<T>::element(__ffs(hit) - 1), at = row.first(row.lo + j) + e;
         if (at < 0 || at >= row.V) continue;
         const unsigned long long key = key_of(Elem<T>::get(reinterpret_cast<const T*>(sh.row + j)[e]), at);
         if (key < least) continue;
         const int to = atomicAdd(&sh.n_keys, 1);
         if (to < kCandidates) sh.keys[to] = key;
-        else j = vectors;
+        else j = vectors, hit = 1;
       }
     }
     __syncthreads();
