@@ -204,7 +204,7 @@ norm_quantize_kernel(const NormArgs a) {
       if (tid == 0) a.steps[n] = NAN;
       continue;
     }
-    const float step = fmaxf(largest, TLQ_RANGE_FLOOR) * a.inv_qpos, k = __fdiv_rn(root, step);
+    const float step = fmaxf(largest, TLQ_RANGE_FLOOR) * a.inv_qpos, k = __fdividef(root * 0.0625f, step * 0.0625f);   // (of a divisor over 2^126 it would make 0)
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
       if (!in[p]) continue;

@@ -324,3 +324,15 @@ def test_norm_gate_down_and_residual_in_a_row(tlq, n):
     y = h / (h.square().mean(1, keepdim=True) + 1e-6).sqrt() * w.double()
     m = activate(y @ gate.double().t(), 1) * (y @ up.double().t())
     assert float((out.double() - h - m @ down.double().t()).norm() / (m @ down.double().t()).norm()) < 0.075
+
+
+@pytest.mark.parametrize("c", [128, 3584])
+@pytest.mark.parametrize("bits", [2, 8])
+def test_norm_of_steps_near_the_end_of_the_range(tlq, c, bits):
+    g = gen(c)
+    x, w = torch.randn(5, c, generator=g).clamp(-2, 2), torch.full((c,), 2.0 ** 126)
+    x[:, 7] = 2.0
+    x, w = bf(x), bf(w)
+    out = tlq.tlq_norm_quantize(x, w, tlq.config(tlq.W8A8_SYM, a_bits=bits), want_values=True)
+    check_norm(tlq, out, x, None, w, None, bits=bits)
+    assert int(out["codes"].abs().max()) == 2 ** (bits - 1) - 1
