@@ -326,6 +326,8 @@ __device__ __forceinline__ constexpr int vector_step() { return kThreads == kSho
 // is off by that rounding, the same for all logits of the row, which drops out of everything as long as 2^d stays in range: up to
 // |m c2| = 2^31, where it is 64.  Beyond, any other logit is 2^-24 m away from m, over 64 in the exponent, and counts nothing; with
 // a power of 2 for the factor m c is exact, and d is 0 for m itself.
+// Sums with largest logits on both sides of that border have no common factor, and need none: they are 2^-24 2^31 apart at least, so that the
+// one of the smaller logit counts nothing.
 __device__ __forceinline__ float factor(float m, float c2) {
   return fabsf(m * c2) < 2147483648.f ? c2 : __uint_as_float(__float_as_uint(c2) & 0xFF800000u);
 }
@@ -344,8 +346,9 @@ __device__ __forceinline__ Stat merge_warp(const Stat& a, float c2) {
   r.m = a.m;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) r.m = fmaxf(r.m, __shfl_xor_sync(0xFFFFFFFFu, r.m, o));
-  r.mc = r.m * factor(r.m, c2);
-  const float d = fmaxf(a.mc - r.mc, kFar), f = exp2_fast(d);
+  const float c = factor(r.m, c2);
+  r.mc = r.m * c;
+  const float d = c == factor(a.m, c2) ? fmaxf(a.mc - r.mc, kFar) : kFar, f = exp2_fast(d);
   r.s = a.s * f;
   r.t = fmaf(r.s, d, a.t * f);
 #pragma unroll
@@ -381,7 +384,7 @@ struct Running {
   __device__ float add(const uint4 (&v)[n]) {
     const float largest = Elem<T>::largest(v), top = fmaxf(m, largest);        // (a NaN passes by here and shows in the sum)
     if (top > m) {
-      const float of_top = factor(top, c2), c = top * of_top, d = fmaxf(mc - c, kFar), f = exp2_fast(d);
+      const float of_top = factor(top, c2), c = top * of_top, d = of_top == halves(cc).x ? fmaxf(mc - c, kFar) : kFar, f = exp2_fast(d);
       cc = pair_of(of_top, of_top);
       s = pmul(s, pair_of(f, f));
       if (kEntropy) t = pfma(s, pair_of(d, d), pmul(t, pair_of(f, f)));
