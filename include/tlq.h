@@ -409,10 +409,12 @@ int tlq_token_logprobs(const void* logits, int dtype, int64_t N, int64_t V, int6
  *   p = softmax over the row's K teacher logits (scale * top_logits[n,k]),  q = softmax over V of scale * logits[n,v],
  *   loss[n] = weights[n] sum_k p_k (ln p_k - ln q_{top_ids[n,k]}),
  *   grad[n,v] = d loss[n] / d logits[n,v] = weights[n] scale (q_v - sum_{k: top_ids[n,k] = v} p_k).
- *   top_ids [N,K] int32, top_logits [N,K] fp32 (logits, or log probabilities as tlq_token_logprobs returns them: the softmax removes
- *   any constant); 1 <= K <= TLQ_MAX_TOP.  A token may stand in several places.  A negative id is an empty place; a row without a teacher
- *   (empty places or logits of -infinity only) has loss 0 and gradient 0.  An id of V or more makes its row NaN; a teacher's logit that is
- *   NaN or +infinity the row's loss, and its gradient at the places.
+ *   top_ids [N,K] int32, top_logits [N,K] fp32; 1 <= K <= TLQ_MAX_TOP.  Logits, or log probabilities as tlq_token_logprobs returns them
+ *   at scale 1, which are the logits less a constant that the softmax removes.  Those of another scale have it in them already, and
+ *   this call multiplies by its own: a temperature belongs into this call alone.
+ *   A token may stand in several places.  A negative id is an empty place; a row without a teacher (empty places or logits of -infinity
+ *   only) has loss 0 and gradient 0.  An id of V or more makes its row NaN; a teacher's logit that is NaN or +infinity the row's loss,
+ *   and its gradient at the places.
  *   weights [N] fp32 or NULL (ones): the gradient that arrives at the row's loss.  A row of weight 0 gives zeros, whatever else it holds.
  *   loss [N] fp32; grad [N,V] of the logits' type, rows ldg apart, or NULL (the loss alone).  grad may be the logits themselves (same
  *   pitch), not overlap them otherwise.

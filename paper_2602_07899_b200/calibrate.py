@@ -116,8 +116,9 @@ def importance_from_teacher(logits: torch.Tensor, top_ids: torch.Tensor, top_log
     labels).
 
     logits [N,V] (bf16 or float32) of the quantized model, top_ids and top_logits [N,K] the full-precision model's alternatives
-    (tlq_token_logprobs' top_ids and top_logp), weights float32 [N] or None.  -> (importance float32 [N], mask of the top_frac most
-    important tokens or None, loss float32 [N]).  V may be any: the gradient's rows are laid out in whole 16-byte pieces.
+    (tlq_token_logprobs' top_ids and top_logp at scale 1; `scale` is applied here, to both models), weights float32 [N] or None.
+    -> (importance float32 [N], mask of the top_frac most important tokens or None, loss float32 [N]).  V may be any: the gradient's
+    rows are laid out in whole 16-byte pieces.
     """
     n, v = logits.shape
     wide = -(-v // 8) * 8

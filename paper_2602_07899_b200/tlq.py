@@ -767,8 +767,9 @@ def tlq_distill_loss(logits: torch.Tensor, top_ids: torch.Tensor, top_logits: to
                      scale: float = 1.0, want_grad: bool = True, grad: Optional[torch.Tensor] = None, stream=None):
     """logits bf16 or float32 [N,V] (rows may be strided), a teacher's top_ids int32 [N,K] (negative: empty place) and top_logits float32
     [N,K], weights float32 [N] or None -> (loss float32 [N], grad of the logits' type [N,V] or None): weights times the divergence of
-    softmax(scale * logits) from the teacher's softmax over its K places, and the gradient of that by the logits.  `grad`: where it goes
-    (the logits themselves are allowed)."""
+    softmax(scale * logits) from the teacher's softmax(scale * top_logits) over its K places, and the gradient of that by the logits.
+    top_logits may be tlq_token_logprobs' top_logp of scale 1 (of another scale they have it in them already: a temperature belongs
+    here alone).  `grad`: where it goes (the logits themselves are allowed)."""
     kind, ld = _logits(logits, "logits")
     N, V = logits.shape
     K = top_ids.shape[-1]
