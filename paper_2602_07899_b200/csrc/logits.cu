@@ -748,11 +748,12 @@ struct LogprobArgs {
   float* top_logp;
 };
 
-// ln p of a logit; nothing is left of a row whose largest logit is masked.
-__device__ __forceinline__ float log_p(float x, const Stat& a, float c2, float log2_s) {
+// ln p of a logit; nothing is left of a row whose largest logit is masked.  (Not by way of log2 p, which may leave the range where ln p does
+// not.)
+__device__ __forceinline__ float log_p(float x, const Stat& a, float scale, float ln_s) {
   if (isnan(a.s)) return NAN;
   if (!(x > kMasked)) return isnan(x) ? NAN : -INFINITY;
-  return kLn2 * ((x - a.m) * c2 - log2_s);
+  return fmaf(x - a.m, scale, -ln_s);
 }
 
 // Long rows come through slots, short ones straight from memory.
@@ -801,11 +802,11 @@ logprobs_kernel(const LogprobArgs g) {
       }
     }
     const Stat a = join_row<kThreads>(run.stat(), g.c2, g.ctas, sh, parity);
-    const float log2_s = log2_sum(a, g.c2);
+    const float ln_s = kLn2 * log2_sum(a, g.c2);
     if (rank == 0 && threadIdx.x == 0) {
       const bool none = a.m <= kMasked && !isnan(a.s);
-      if (g.ids != nullptr) g.logp[n] = id < 0 ? 0.f : id >= g.V ? NAN : log_p(z_id, a, g.c2, log2_s);
-      if (g.lse != nullptr) g.lse[n] = none ? -INFINITY : isnan(a.s) ? NAN : fmaf(a.m, g.scale, kLn2 * log2_s);
+      if (g.ids != nullptr) g.logp[n] = id < 0 ? 0.f : id >= g.V ? NAN : log_p(z_id, a, g.scale, ln_s);
+      if (g.lse != nullptr) g.lse[n] = none ? -INFINITY : isnan(a.s) ? NAN : fmaf(a.m, g.scale, ln_s);
       if (kEntropy) g.entropy[n] = none ? 0.f : kLn2 * (log2f(a.s) - a.t / a.s);     // (with the rounding of mc in both)
     }
     if constexpr (kTop) {
@@ -820,7 +821,7 @@ logprobs_kernel(const LogprobArgs g) {
         const unsigned long long key = bad ? 0 : kSlots && g.ctas > 1 ? top.all[kSlots ? threadIdx.x : 0] : top.top[threadIdx.x];
         const int64_t to = n * g.K + threadIdx.x;
         g.top_ids[to] = key == 0 ? -1 : (int)(0xFFFFFFFFu - (uint32_t)key);
-        g.top_logp[to] = bad ? NAN : key == 0 ? -INFINITY : log_p(of_order((uint32_t)(key >> 32)), a, g.c2, log2_s);
+        g.top_logp[to] = bad ? NAN : key == 0 ? -INFINITY : log_p(of_order((uint32_t)(key >> 32)), a, g.scale, ln_s);
       }
     }
   }
@@ -870,21 +871,21 @@ __device__ __forceinline__ float teacher_loss(const DistillArgs& g, const Stat& 
   for (int k = 0; k < kPer; ++k) sum += x[k] <= kMasked ? 0.f : exp2_fast((x[k] - top) * g.c2);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-  const float logs = log2_sum(a, g.c2) - log2f(sum);
+  const float logs = kLn2 * (log2_sum(a, g.c2) - log2f(sum));
   float loss = 0.f;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const int i = lane + 32 * k;
     if (i >= g.K) continue;
-    const float dt = (x[k] - top) * g.c2, p = x[k] <= kMasked ? 0.f : __fdiv_rn(exp2_fast(dt), sum);
+    const float p = x[k] <= kMasked ? 0.f : __fdiv_rn(exp2_fast((x[k] - top) * g.c2), sum);
     d.p[parity][i] = p;
     if (p == 0.f) continue;
     const float z = d.z[parity][i];
-    loss += z <= kMasked ? INFINITY : p * ((dt - (z - a.m) * g.c2) + logs);
+    loss += z <= kMasked ? INFINITY : p * fmaf((x[k] - top) - (z - a.m), g.scale, logs);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xFFFFFFFFu, loss, o);
-  return kLn2 * loss;
+  return loss;
 }
 
 // A lane's vector of 32 that follow one another, to an address off the grid: the elements before the grid's next line go with the lane before, and
