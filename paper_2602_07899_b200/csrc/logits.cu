@@ -322,33 +322,44 @@ template <int kThreads>
 __device__ __forceinline__ constexpr int vector_step() { return kThreads == kShort ? kShort : 32; }
 
 // ---------------------------------------------------------------------------------------------- maximum and sums
-// The factor of a logit's distance from the row's largest, m, to the exponent of 2: c2 = scale log2(e).  d = fma(z, c2, -mc) with mc = m c2 rounded
+// The factor of a logit's distance from the row's largest, m, to the exponent of 2: c = scale log2(e).  d = fma(z, c, -mc) with mc = m c rounded
 // is off by that rounding, the same for all logits of the row, which drops out of everything as long as 2^d stays in range: up to
-// |m c2| = 2^31, where it is 64.  Beyond, any other logit is 2^-24 m away from m, over 64 in the exponent, and counts nothing; with
-// a power of 2 for the factor m c is exact, and d is 0 for m itself.
-// Sums with largest logits on both sides of that border have no common factor, and need none: they are 2^-24 2^31 apart at least, so that the
-// one of the smaller logit counts nothing.
-__device__ __forceinline__ float factor(float m, float c2) {
-  return fabsf(m * c2) < 2147483648.f ? c2 : __uint_as_float(__float_as_uint(c2) & 0xFF800000u);
+// |m c| = 2^31, where it is 64.  Beyond, any other logit is 2^-24 m away from m, over 64 in the exponent, and counts nothing; with
+// the power of 2 under c for the factor m c is exact, and d is 0 for m itself.  (Half of that where m c would leave the 32-bit range, which
+// scale m does not.)
+// Sums whose largest logits have different factors have no common one, and need none: the logits are 2^-24 2^31 apart at least, so
+// that the sum of the smaller one counts nothing.
+struct Factors {
+  float near, far;            // c, and the power of 2 under it
+};
+Factors factors_of(float scale) {
+  const float c = scale * kLog2e;
+  int e;
+  frexpf(c, &e);              // c = [0.5, 1) 2^e
+  return Factors{c, ldexpf(1.f, e - 1)};
+}
+__device__ __forceinline__ bool is_near(float m, const Factors& f) { return fabsf(m * f.near) < 2147483648.f; }
+__device__ __forceinline__ float factor(float m, const Factors& f) {
+  return is_near(m, f) ? f.near : m * f.far < INFINITY ? f.far : 0.5f * f.far;
 }
 constexpr float kFar = -16384.f;          // 2^kFar is 0, and no product with it leaves the range
 struct Stat {
   float m, mc;                // the largest logit, and that times its factor, rounded
   float s, t;                 // sums of 2^d and of 2^d d
 };
-__device__ __forceinline__ Stat empty_stat(float c2) { return Stat{kMasked, kMasked * factor(kMasked, c2), 0.f, 0.f}; }
-// log2 of the sum of 2^((z - m) c2): without the rounding of mc.
-__device__ __forceinline__ float log2_sum(const Stat& a, float c2) { return log2f(a.s) - fmaf(a.m, factor(a.m, c2), -a.mc); }
+__device__ __forceinline__ Stat empty_stat(const Factors& f) { return Stat{kMasked, kMasked * f.far, 0.f, 0.f}; }
+// log2 of the sum of 2^((z - m) c): without the rounding of mc.
+__device__ __forceinline__ float log2_sum(const Stat& a, const Factors& f) { return log2f(a.s) - fmaf(a.m, factor(a.m, f), -a.mc); }
 
 // Over the lanes of a warp, in a fixed order; every lane gets the same.
-__device__ __forceinline__ Stat merge_warp(const Stat& a, float c2) {
+__device__ __forceinline__ Stat merge_warp(const Stat& a, const Factors& of) {
   Stat r;
   r.m = a.m;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) r.m = fmaxf(r.m, __shfl_xor_sync(0xFFFFFFFFu, r.m, o));
-  const float c = factor(r.m, c2);
+  const float c = factor(r.m, of);
   r.mc = r.m * c;
-  const float d = c == factor(a.m, c2) ? fmaxf(a.mc - r.mc, kFar) : kFar, f = exp2_fast(d);
+  const float d = c == factor(a.m, of) ? fmaxf(a.mc - r.mc, kFar) : kFar, f = exp2_fast(d);
   r.s = a.s * f;
   r.t = fmaf(r.s, d, a.t * f);
 #pragma unroll
@@ -372,19 +383,16 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
 // A thread's own maximum and sums as its vectors come.
 template <typename T, bool kEntropy>
 struct Running {
-  float c2, m, mc;
+  const Factors& of;
+  float m, mc;
   f32x2 cc, s, t;
-  __device__ explicit Running(float c2_) : c2(c2_), m(kMasked), s(pair_of(0.f, 0.f)), t(s) {
-    const float c = factor(m, c2);
-    mc = m * c;
-    cc = pair_of(c, c);
-  }
+  __device__ explicit Running(const Factors& f) : of(f), m(kMasked), mc(kMasked * f.far), cc(pair_of(f.far, f.far)), s(pair_of(0.f, 0.f)), t(s) {}
   // Returns the vectors' largest.
   template <int n>
   __device__ float add(const uint4 (&v)[n]) {
     const float largest = Elem<T>::largest(v), top = fmaxf(m, largest);        // (a NaN passes by here and shows in the sum)
     if (top > m) {
-      const float of_top = factor(top, c2), c = top * of_top, d = of_top == halves(cc).x ? fmaxf(mc - c, kFar) : kFar, f = exp2_fast(d);
+      const float of_top = factor(top, of), c = top * of_top, d = of_top == halves(cc).x ? fmaxf(mc - c, kFar) : kFar, f = exp2_fast(d);
       cc = pair_of(of_top, of_top);
       s = pmul(s, pair_of(f, f));
       if (kEntropy) t = pfma(s, pair_of(d, d), pmul(t, pair_of(f, f)));
@@ -427,29 +435,31 @@ __device__ __forceinline__ void read_batch(const Row<T>& row, int i, P& pieces, 
   }
 }
 
-// Maximum and sums of the whole row from those of the threads, the same in every thread of every CTA of it.
+// Maximum and sums of the whole row from those of the threads, the same in every thread of every CTA of it.  The sum is no number where the
+// row has no distribution: where it has a NaN or +infinity, or its largest logit leaves the range when multiplied by scale.
 template <int kThreads>
-__device__ __forceinline__ Stat join_row(Stat a, float c2, int ctas, RowShared& sh, int parity) {
+__device__ __forceinline__ Stat join_row(Stat a, const Factors& f, float scale, int ctas, RowShared& sh, int parity) {
   constexpr int kWarps = kThreads / 32;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  a = merge_warp(a, c2);
+  a = merge_warp(a, f);
   if (lane == 0) sh.warps[parity][warp] = a;
   __syncthreads();
-  a = merge_warp(lane < kWarps ? sh.warps[parity][lane] : empty_stat(c2), c2);
+  a = merge_warp(lane < kWarps ? sh.warps[parity][lane] : empty_stat(f), f);
   if (ctas > 1) {
     if (threadIdx.x == 0) {
       sh.cta[parity][0] = a.m; sh.cta[parity][1] = a.mc; sh.cta[parity][2] = a.s; sh.cta[parity][3] = a.t;
     }
     __syncwarp();
     ptx::cluster_sync_all();
-    a = empty_stat(c2);
+    a = empty_stat(f);
     if (lane < ctas) {
       const uint32_t from = ptx::map_to_cta(ptx::smem_u32(sh.cta[parity]), (uint32_t)lane);
       a.m = ld_cluster_f32(from); a.mc = ld_cluster_f32(from + 4); a.s = ld_cluster_f32(from + 8); a.t = ld_cluster_f32(from + 12);
     }
     __syncwarp();
-    a = merge_warp(a, c2);
+    a = merge_warp(a, f);
   }
+  if (!(a.m * scale < INFINITY)) a.s = NAN;
   return a;
 }
 
@@ -739,7 +749,8 @@ struct LogprobArgs {
   const void* z;
   int64_t N, ld;
   int V, ctas, K, batches;    // batches of a run
-  float c2, scale;            // c2 = scale log2(e)
+  float scale;
+  Factors f;
   const int32_t* ids;
   float* logp;
   float* entropy;
@@ -782,7 +793,7 @@ logprobs_kernel(const LogprobArgs g) {
       id = load_near(g.ids + n);
       if (id >= 0 && id < g.V) z_id = Elem<T>::load(row.z + id);
     }
-    Running<T, kEntropy> run(g.c2);
+    Running<T, kEntropy> run(g.f);
     int batch = 0;
     for (int i = first_vector<kThreads>(row.lo, 0); i - (kSlots ? (int)(threadIdx.x & 31) : (int)threadIdx.x) < row.hi; i += kBatch * kThreads) {
       uint4 v[kBatch];
@@ -801,13 +812,14 @@ logprobs_kernel(const LogprobArgs g) {
           if (i + u * kThreads < row.hi) top.row[i + u * kThreads - row.lo] = kEntropy ? v[u] : Elem<T>::clamp(v[u]);
       }
     }
-    const Stat a = join_row<kThreads>(run.stat(), g.c2, g.ctas, sh, parity);
-    const float ln_s = kLn2 * log2_sum(a, g.c2);
+    const Stat a = join_row<kThreads>(run.stat(), g.f, g.scale, g.ctas, sh, parity);
+    const float ln_s = kLn2 * log2_sum(a, g.f);
     if (rank == 0 && threadIdx.x == 0) {
       const bool none = a.m <= kMasked && !isnan(a.s);
       if (g.ids != nullptr) g.logp[n] = id < 0 ? 0.f : id >= g.V ? NAN : log_p(z_id, a, g.scale, ln_s);
       if (g.lse != nullptr) g.lse[n] = none ? -INFINITY : isnan(a.s) ? NAN : fmaf(a.m, g.scale, ln_s);
-      if (kEntropy) g.entropy[n] = none ? 0.f : kLn2 * (log2f(a.s) - a.t / a.s);     // (with the rounding of mc in both)
+      // (with the rounding of mc in both; where there is none t is 0, but for terms 0 x -infinity where d itself leaves the range)
+      if (kEntropy) g.entropy[n] = none ? 0.f : kLn2 * (log2f(a.s) - (is_near(a.m, g.f) ? a.t / a.s : 0.f));
     }
     if constexpr (kTop) {
       const bool bad = isnan(a.s);                            // (the same in all CTAs of the row)
@@ -838,7 +850,8 @@ struct DistillArgs {
   const void* z;
   int64_t N, ld;
   int V, ctas, K;
-  float c2, scale;
+  float scale;
+  Factors f;
   const int32_t* ids;
   const float* top;
   const float* weights;
@@ -868,16 +881,16 @@ __device__ __forceinline__ float teacher_loss(const DistillArgs& g, const Stat& 
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
   float sum = 0.f;
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) sum += x[k] <= kMasked ? 0.f : exp2_fast((x[k] - top) * g.c2);
+  for (int k = 0; k < kPer; ++k) sum += x[k] <= kMasked ? 0.f : exp2_fast((x[k] - top) * g.f.near);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-  const float logs = kLn2 * (log2_sum(a, g.c2) - log2f(sum));
+  const float logs = kLn2 * (log2_sum(a, g.f) - log2f(sum));
   float loss = 0.f;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const int i = lane + 32 * k;
     if (i >= g.K) continue;
-    const float p = x[k] <= kMasked ? 0.f : __fdiv_rn(exp2_fast((x[k] - top) * g.c2), sum);
+    const float p = x[k] <= kMasked ? 0.f : __fdiv_rn(exp2_fast((x[k] - top) * g.f.near), sum);
     d.p[parity][i] = p;
     if (p == 0.f) continue;
     const float z = d.z[parity][i];
@@ -977,7 +990,7 @@ distill_kernel(const DistillArgs g) {
       id = load_near(g.ids + n * g.K + tid);
       teacher = load_near(g.top + n * g.K + tid);
     }
-    Running<T, false> run(g.c2);
+    Running<T, false> run(g.f);
     const int i0 = first_vector<kThreads>(row.lo, 0), lead = kSlots ? lane : tid;
     for (int i = i0; i - lead < row.hi; i += kBatch * kThreads) {
       uint4 v[kBatch];
@@ -995,7 +1008,7 @@ distill_kernel(const DistillArgs g) {
     const bool there = tid < g.K && id >= 0;
     const uint32_t flags = (__any_sync(0xFFFFFFFFu, there && !(teacher <= kMasked)) ? 1u : 0u) | (__any_sync(0xFFFFFFFFu, there && id >= g.V) ? 2u : 0u);
     if (lane == 0 && warp < kMaxTop / 32) d.flags[parity][warp] = flags;
-    const Stat a = join_row<kThreads>(run.stat(), g.c2, g.ctas, sh, parity);
+    const Stat a = join_row<kThreads>(run.stat(), g.f, g.scale, g.ctas, sh, parity);
     uint32_t all = 0;
 #pragma unroll
     for (int k = 0; k < kMaxTop / 32; ++k) all |= d.flags[parity][k];
@@ -1011,7 +1024,7 @@ distill_kernel(const DistillArgs g) {
       const float gp = zeros ? 0.f : w * g.scale;
       const float gq = zeros ? 0.f : bad ? NAN : gp / a.s;
       bool late = false;                                      // (a copy that did not come in time: the row is no number)
-      const float c = factor(a.m, g.c2);
+      const float c = factor(a.m, g.f);
       const f32x2 cc = pair_of(c, c), minus = pair_of(-a.mc, -a.mc);
       const f32x2 scale2 = pair_of(gq, gq);
       const uint32_t keep = zeros ? 0u : 0xFFFFFFFFu;
@@ -1201,7 +1214,7 @@ int run_distill(DistillArgs g, cudaStream_t st) {
 int launch_token_logprobs(const void* logits, int f32, int64_t N, int64_t V, int64_t ld, float scale, const int32_t* ids, int K,
                           float* logp, float* entropy, float* lse, int32_t* top_ids, float* top_logp, cudaStream_t st) {
   LogprobArgs g{};
-  g.z = logits; g.N = N; g.ld = ld; g.V = (int)V; g.K = K; g.c2 = scale * kLog2e; g.scale = scale;
+  g.z = logits; g.N = N; g.ld = ld; g.V = (int)V; g.K = K; g.f = factors_of(scale); g.scale = scale;
   g.ids = ids; g.logp = logp; g.entropy = entropy; g.lse = lse; g.top_ids = top_ids; g.top_logp = top_logp;
   auto of_type = [&](auto type, auto threads) {
     using T = decltype(type);
@@ -1221,7 +1234,7 @@ int launch_distill_loss(const void* logits, int f32, int64_t N, int64_t V, int64
   const int sms = device_sm_count();
   if (sms <= 0) return TLQ_ERR_CUDA;
   DistillArgs g{};
-  g.z = logits; g.N = N; g.ld = ld; g.V = (int)V; g.K = K; g.c2 = scale * kLog2e; g.scale = scale;
+  g.z = logits; g.N = N; g.ld = ld; g.V = (int)V; g.K = K; g.f = factors_of(scale); g.scale = scale;
   g.ids = top_ids; g.top = top_logits; g.weights = weights; g.loss = loss; g.grad = grad; g.ldg = ldg;
   const bool is_short = V * (f32 ? 4 : 2) <= short_row(f32);
   auto with_grad = [&](auto type, auto off_grid) {
