@@ -324,23 +324,25 @@ __device__ __forceinline__ constexpr int vector_step() { return kThreads == kSho
 // ---------------------------------------------------------------------------------------------- maximum and sums
 // The factor of a logit's distance from the row's largest, m, to the exponent of 2: c = scale log2(e).  d = fma(z, c, -mc) with mc = m c rounded
 // is off by that rounding, the same for all logits of the row, which drops out of everything as long as 2^d stays in range: up to
-// |m c| = 2^31, where it is 64.  Beyond, any other logit is 2^-24 m away from m, over 64 in the exponent, and counts nothing; with
-// the power of 2 under c for the factor m c is exact, and d is 0 for m itself.  (Half of that where m c would leave the 32-bit range, which
+// |m c| = 2^31, where it is 64.  Beyond, any other logit is 2^-24 m away from m, over 128 in the exponent, and counts nothing; with
+// the power of 2 above c for the factor m c is exact, and d is 0 for m itself.  (A quarter of that where m c would leave the 32-bit range, which
 // scale m does not.)
-// Sums whose largest logits have different factors have no common one, and need none: the logits are 2^-24 2^31 apart at least, so
-// that the sum of the smaller one counts nothing.
+// Sums whose largest logits have different factors are joined with the larger one's: their logits are 2^-24 2^31 apart at least, so that the
+// sum of the smaller one, rounded by 64 or not, counts nothing.
 struct Factors {
-  float near, far;            // c, and the power of 2 under it
+  float near, far;            // c, and the power of 2 above it
 };
 Factors factors_of(float scale) {
   const float c = scale * kLog2e;
   int e;
   frexpf(c, &e);              // c = [0.5, 1) 2^e
-  return Factors{c, ldexpf(1.f, e - 1)};
+  return Factors{c, ldexpf(1.f, e)};
 }
 __device__ __forceinline__ bool is_near(float m, const Factors& f) { return fabsf(m * f.near) < 2147483648.f; }
 __device__ __forceinline__ float factor(float m, const Factors& f) {
-  return is_near(m, f) ? f.near : m * f.far < INFINITY ? f.far : 0.5f * f.far;
+  float c = f.near;
+  if (__builtin_expect(!is_near(m, f), 0)) c = m * f.far < INFINITY ? f.far : 0.25f * f.far;
+  return c;
 }
 constexpr float kFar = -16384.f;          // 2^kFar is 0, and no product with it leaves the range
 struct Stat {
@@ -358,8 +360,8 @@ __device__ __forceinline__ Stat merge_warp(const Stat& a, const Factors& of) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) r.m = fmaxf(r.m, __shfl_xor_sync(0xFFFFFFFFu, r.m, o));
   const float c = factor(r.m, of);
-  r.mc = r.m * c;
-  const float d = c == factor(a.m, of) ? fmaxf(a.mc - r.mc, kFar) : kFar, f = exp2_fast(d);
+  r.mc = __fmul_rn(r.m, c);               // (rounded as it is everywhere else, not within the difference)
+  const float d = fmaxf(__fmul_rn(a.m, c) - r.mc, kFar), f = exp2_fast(d);
   r.s = a.s * f;
   r.t = fmaf(r.s, d, a.t * f);
 #pragma unroll
@@ -392,7 +394,7 @@ struct Running {
   __device__ float add(const uint4 (&v)[n]) {
     const float largest = Elem<T>::largest(v), top = fmaxf(m, largest);        // (a NaN passes by here and shows in the sum)
     if (top > m) {
-      const float of_top = factor(top, of), c = top * of_top, d = of_top == halves(cc).x ? fmaxf(mc - c, kFar) : kFar, f = exp2_fast(d);
+      const float of_top = factor(top, of), c = __fmul_rn(top, of_top), d = fmaxf(__fmul_rn(m, of_top) - c, kFar), f = exp2_fast(d);
       cc = pair_of(of_top, of_top);
       s = pmul(s, pair_of(f, f));
       if (kEntropy) t = pfma(s, pair_of(d, d), pmul(t, pair_of(f, f)));
