@@ -287,6 +287,8 @@ int tlq_linear_i8(const int8_t* Xq, const float* t, int64_t N, int64_t C1, const
  * or, with gated != 0 (C2 even): Y[n,j] = act(z[n,2j]) z[n,2j+1] + residual[n,j], Y [N, C2/2]: rows 2j and 2j+1 of Wq, u and bias are
  * channel j of the gate and of the up projection.
  *   residual bf16 or NULL, rows ldr elements apart (any pitch); it may be Y itself (then ldr is Y's width), not overlap it otherwise.
+ *   z beyond the 32-bit range is infinite (as with a bias that is): act(+infinity) is +infinity, act(-infinity) NaN, as the activation's
+ *   -infinity times 0.
  *   Everything else, and the workspace, as in tlq_linear_i8.
  */
 #define TLQ_ACT_NONE 0
