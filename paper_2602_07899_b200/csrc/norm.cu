@@ -85,7 +85,7 @@ norm_quantize_kernel(const NormArgs a) {
       float s[8];
       unpack8(load_near(reinterpret_cast<const uint4*>(a.s) + p * kThreads + tid), s);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] *= kKeep ? __frcp_rn(s[j]) : __fdividef(1.f, s[j]);
+      for (int j = 0; j < 8; ++j) f[j] = kKeep ? f[j] * __frcp_rn(s[j]) : __fdividef(f[j] * 0.25f, s[j] * 0.25f);    // (by a divisor over 2^126 it would make 0)
     }
   };
   float kept[kKeep ? kPieces : 1][8];
