@@ -310,7 +310,8 @@ int tlq_linear_i8_act(const int8_t* Xq, const float* t, int64_t N, int64_t C1, c
  * with steps [N] fp32; values [N,C] bf16: the values that the codes stand for, codes * steps, as the product sees them; y_out [N,C]
  * bf16: y before the quantizer.  Codes or y_out are wanted, codes and steps come together, values and s belong to codes.
  * Outputs lie over no input but as said, nor over one another.
- * A row with a value that is not finite is not a number: y and values NaN, codes 0 and steps NaN, so that a product of it is NaN.
+ * A row with a value that is not finite is not a number: y and values NaN, codes 0 and steps NaN, so that a product of it is NaN.  So are
+ * the codes of a row of which a v leaves the 32-bit range (|h w / s| may), or w / s does.
  */
 int tlq_norm_quantize(const void* x, int64_t N, int64_t C, int64_t ldx, const void* residual, int64_t ldr, const void* w, float eps,
                       const void* s, const tlq_config* cfg, void* h_out, int64_t ldh, int8_t* codes, float* steps, void* values,

@@ -52,7 +52,7 @@ __device__ __forceinline__ uint4 ld_shared(uint32_t addr) {
 // Thread t has pieces t, t + kThreads, ... of a row.
 template <int kPieces, int kThreads, int kCtas, bool kKeep>
 __global__ void __launch_bounds__(kThreads, kCtas)
-norm_quantize_kernel(const NormArgs a) {
+norm_quantize_kernel(const __grid_constant__ NormArgs a) {
   constexpr int kWarps = kThreads / 32;
   extern __shared__ __align__(16) uint8_t ahead[];           // the next row's pieces of x, then of r
   __shared__ float2 s_part[2][kWarps];                       // of each warp, of two rows in turn
@@ -154,6 +154,18 @@ norm_quantize_kernel(const NormArgs a) {
         }
       }
     };
+    auto once_more = [&](float power) {        // with h times a power of 2
+      __syncthreads();
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p) {
+        float u[8];
+        unpack8(h[p], u);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] *= power;
+        h[p] = pack8(u);
+      }
+      sums();
+    };
     sums();
     if (n + gridDim.x < a.N) {                 // the next row (behind the sum over the CTA, which needs all of this one)
       x += (int64_t)gridDim.x * a.ldx / 8;
@@ -162,22 +174,13 @@ norm_quantize_kernel(const NormArgs a) {
     }
     float eps = a.eps;
     if (!(total < INFINITY)) {                 // squares beyond the 32-bit range (or a row that is not finite): once more with h 2^-96,
-      __syncthreads();                         // where the sum of 32768 squares of the largest number is 2^79
-#pragma unroll
-      for (int p = 0; p < kPieces; ++p) {
-        float u[8];
-        unpack8(h[p], u);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) u[j] *= 1.2621774483536189e-29f;
-        h[p] = pack8(u);
-      }
+      once_more(1.2621774483536189e-29f);      // where the sum of 32768 squares of the largest number is 2^79
       eps = 0.f;                               // (nothing beside such squares)
-      sums();
     }
 #pragma unroll
     for (int p = 0; p < kPieces; ++p)          // (nothing of it is kept unpacked, which would take twice the registers)
       asm volatile("" : "+r"(h[p].x), "+r"(h[p].y), "+r"(h[p].z), "+r"(h[p].w));
-    const float root = total < INFINITY ? rsqrtf(fmaf(total, a.inv_c, eps)) : NAN;
+    float root = total < INFINITY ? rsqrtf(fmaf(total, a.inv_c, eps)) : NAN;
     if (a.y != nullptr) {
 #pragma unroll
       for (int p = 0; p < kPieces; ++p) {
@@ -193,8 +196,13 @@ norm_quantize_kernel(const NormArgs a) {
       }
     }
     if (a.codes == nullptr) continue;
+    if (top == INFINITY && root < INFINITY) {  // |h g| beyond the 32-bit range, which |v| may be in: with h times the power of 2 in the root, where
+      const float power = __uint_as_float(__float_as_uint(root) & 0x7F800000u);      // no |h| is above the square root of the row's length
+      once_more(power);                        // (what gets lost below rounds to 0)
+      root /= power;
+    }
     const float largest = top * root;
-    if (!(largest < INFINITY)) {               // not a number, or w / s is none
+    if (!(largest < INFINITY)) {               // not a number, or v or w / s leaves the range
 #pragma unroll
       for (int p = 0; p < kPieces; ++p) {
         if (!in[p]) continue;
