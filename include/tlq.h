@@ -304,7 +304,8 @@ int tlq_linear_i8_act(const int8_t* Xq, const float* t, int64_t N, int64_t C1, c
  *   h = bf16(x + residual) (x without one);   y = h / sqrt(mean_c h^2 + eps) * w;   v = y / s;
  *   steps[n] = max(max_c |v|, 1e-5) / (2^(a_bits-1) - 1);   codes = rint(v / steps[n]).
  *   x [N,C], residual [N,C] or NULL: bf16, rows ldx and ldr elements apart (multiples of 8); w [C] bf16 or NULL (ones);
- *   s [C] bf16 or NULL: the scale that the search found for the product that follows (ones); eps > 0.  C a multiple of 16, to 32768.
+ *   s [C] bf16 or NULL: the scale that the search found for the product that follows (ones); eps a normal number above 0.  C a multiple of
+ *   16, to 32768.
  *   cfg: symmetric mode, a_bits; not read without codes.
  * Outputs, NULL where not wanted: h_out [N,C] bf16, rows ldh apart (may be x or residual themselves, with their pitch); codes [N,C] int8
  * with steps [N] fp32; values [N,C] bf16: the values that the codes stand for, codes * steps, as the product sees them; y_out [N,C]

@@ -114,7 +114,7 @@ int tlq_norm_quantize(const void* x, int64_t N, int64_t C, int64_t ldx, const vo
   } else if (N > 0 && (steps != nullptr || values != nullptr || s != nullptr)) {
     return TLQ_ERR_INVALID_ARG;           // (buffers of no rows may be NULL)
   }
-  if (!(eps > 0.0f) || isinf(eps)) return TLQ_ERR_INVALID_ARG;
+  if (!(eps >= 1.17549435e-38f) || isinf(eps)) return TLQ_ERR_INVALID_ARG;     // (beside a smaller one squares would count that 32 bits do not hold)
   if (N > 0 && (x == nullptr || (codes == nullptr && y_out == nullptr))) return TLQ_ERR_INVALID_ARG;
   const int64_t most = 1LL << 40;
   if (ldx < C || ldx > most || (ldx % 8) != 0) return TLQ_ERR_SHAPE;
