@@ -1025,16 +1025,15 @@ distill_kernel(const DistillArgs g) {
       const bool zeros = none || (!bad && a.m <= kMasked);
       const float gp = zeros ? 0.f : w * g.scale;
       const float gq = zeros ? 0.f : bad ? NAN : gp / a.s;
-      bool late = false;                                      // (a copy that did not come in time: the row is no number)
       const float c = factor(a.m, g.f);
       const f32x2 cc = pair_of(c, c), minus = pair_of(-a.mc, -a.mc);
-      const f32x2 scale2 = pair_of(gq, gq);
+      f32x2 scale2 = pair_of(gq, gq);
       const uint32_t keep = zeros ? 0u : 0xFFFFFFFFu;
       uint4* const out = reinterpret_cast<uint4*>(grad - row.off);      // vector 0, where the gradient lies as the logits do
       for (int i = i0; i - lead < row.hi; i += kBatch * kThreads) {
         uint4 v[kBatch];
         if constexpr (kSlots) {
-          if (!pieces.next(v, &abort, nullptr, 0)) late = true;
+          if (!pieces.next(v, &abort, nullptr, 0)) scale2 = pair_of(NAN, NAN);       // (a copy that did not come in time)
         } else {
 #pragma unroll
           for (int u = 0; u < kBatch; ++u) v[u] = i + u * kStep < row.hi ? row.load(i + u * kStep) : row.none();
@@ -1078,7 +1077,7 @@ distill_kernel(const DistillArgs g) {
           Elem<T>::store(grad + id, exp2_fast(fmaf(d.z[parity][tid], c, -a.mc)) * gq - gp * p);
         }
       }
-      if (late && rank == 0) g.loss[n] = NAN;
+      if (kSlots && !zeros && isnan(halves(scale2).x)) g.loss[n] = NAN;  // (a row that is no number, or part of it came late)
     }
     parity ^= 1;
   }
