@@ -310,7 +310,8 @@ int tlq_linear_i8_act(const int8_t* Xq, const float* t, int64_t N, int64_t C1, c
  * Outputs, NULL where not wanted: h_out [N,C] bf16, rows ldh apart (may be x or residual themselves, with their pitch); codes [N,C] int8
  * with steps [N] fp32; values [N,C] bf16: the values that the codes stand for, codes * steps, as the product sees them; y_out [N,C]
  * bf16: y before the quantizer.  Codes or y_out are wanted, codes and steps come together, values and s belong to codes.
- * Outputs lie over no input but as said, nor over one another.
+ * Outputs lie over no input but as said, nor over one another.  Rows of one pitch may be columns of one buffer; of others all memory from
+ * the first to the last row counts.
  * A row with a value that is not finite is not a number: y and values NaN, codes 0 and steps NaN, so that a product of it is NaN.  So are
  * the codes of a row of which a v leaves the 32-bit range (|h w / s| may), or w / s does.
  */
@@ -392,7 +393,8 @@ int tlq_kv_attention(const void* q, int64_t T, int64_t ldq, int32_t n_heads, con
  *  - Logits of -2^100 and below count as masked, like -infinity: probability 0.  A row with a NaN or +infinity, or whose largest logit
  *    leaves the 32-bit range when multiplied by scale, has no distribution: its numbers are NaN, its alternatives -1.
  *  - N = 0 is TLQ_OK and launches nothing.  The calls use no workspace; results do not depend on timing.  Outputs lie over no input but
- *    as said, nor over one another.
+ *    as said, nor over one another (logits and gradient of one pitch may be columns of one buffer; of others all memory from the first to
+ *    the last row counts).
  */
 #define TLQ_MAX_TOP 128
 

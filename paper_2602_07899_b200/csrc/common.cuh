@@ -65,12 +65,26 @@ inline int have_device() {
   found = true;
   return TLQ_OK;
 }
-// Bytes from the first to the last element of N rows of `width` elements that begin `ld` elements apart.
-inline int64_t row_bytes(int64_t N, int64_t width, int64_t ld, int64_t size) { return N < 1 ? 0 : ((N - 1) * ld + width) * size; }
-inline bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
-  const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
-  return a != nullptr && b != nullptr && p < q + (uintptr_t)b_bytes && q < p + (uintptr_t)a_bytes;
+// N rows of `bytes` each that begin `pitch` bytes apart.
+struct Rows2D {
+  const void* p;
+  int64_t N, bytes, pitch;
+};
+inline Rows2D rows_of(const void* p, int64_t N, int64_t width, int64_t ld, int64_t size) {
+  return Rows2D{p, N, width * size, N > 1 ? ld * size : width * size};
 }
+inline Rows2D flat_of(const void* p, int64_t bytes) { return Rows2D{p, bytes > 0 ? 1 : 0, bytes, bytes}; }
+// Whether they lie over one another.  Rows of one pitch may be columns of one buffer; of others, all memory from the first to the last row counts.
+inline bool overlap(const Rows2D& a, const Rows2D& b) {
+  if (a.p == nullptr || b.p == nullptr || a.N < 1 || b.N < 1) return false;
+  using wide = unsigned __int128;                  // (no row count times a pitch leaves it)
+  const wide p = reinterpret_cast<uintptr_t>(a.p), q = reinterpret_cast<uintptr_t>(b.p);
+  if (p >= q + (wide)(b.N - 1) * (wide)b.pitch + (wide)b.bytes || q >= p + (wide)(a.N - 1) * (wide)a.pitch + (wide)a.bytes) return false;
+  if (a.N == 1 || b.N == 1 || a.pitch != b.pitch) return true;
+  const wide pitch = (wide)a.pitch, from_a = q >= p ? (q - p) % pitch : (pitch - (p - q) % pitch) % pitch;      // of b's rows, from a's before them
+  return from_a < (wide)a.bytes || from_a + (wide)b.bytes > pitch;
+}
+inline bool same_rows(const Rows2D& a, const Rows2D& b) { return a.p == b.p && a.N == b.N && a.bytes == b.bytes && a.pitch == b.pitch; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 

@@ -88,9 +88,8 @@ int tlq_linear_i8_act(const int8_t* Xq, const float* t, int64_t N, int64_t C1, c
   if (residual != nullptr && (ldr < width || ldr > (1LL << 40))) return TLQ_ERR_SHAPE;
   if (!aligned16(Xq) || !aligned16(Wq) || !aligned16(workspace) || !aligned16(Y)) return TLQ_ERR_ALIGN;
   // the residual's rows may be the result's own (each element is read by the thread that writes it), but not lie across them
-  if (residual != nullptr && overlap(residual, row_bytes(N, width, ldr, 2), Y, row_bytes(N, width, width, 2)) &&
-      !(residual == Y && ldr == width))
-    return TLQ_ERR_INVALID_ARG;
+  const Rows2D out = rows_of(Y, N, width, width, 2), added = rows_of(residual, N, width, ldr, 2);
+  if (overlap(added, out) && !same_rows(added, out)) return TLQ_ERR_INVALID_ARG;
   if (workspace_bytes < need) return TLQ_ERR_WORKSPACE;
   int rc = have_device();
   if (rc != TLQ_OK || N == 0) return rc;
@@ -123,17 +122,14 @@ int tlq_norm_quantize(const void* x, int64_t N, int64_t C, int64_t ldx, const vo
   if (!aligned16(x) || !aligned16(residual) || !aligned16(w) || !aligned16(s) || !aligned16(h_out) || !aligned16(codes) ||
       !aligned16(values) || !aligned16(y_out))
     return TLQ_ERR_ALIGN;
-  const int64_t flat = N * C;
-  const struct { const void* p; int64_t bytes; int64_t ld; } in[4] = {{x, row_bytes(N, C, ldx, 2), ldx}, {residual, row_bytes(N, C, ldr, 2), ldr},
-                                                                      {w, C * 2, 0}, {s, C * 2, 0}};
-  const struct { const void* p; int64_t bytes; int64_t ld; } out[5] = {{h_out, row_bytes(N, C, ldh, 2), ldh}, {codes, flat, -1},
-                                                                       {steps, N * 4, -1}, {values, flat * 2, -1}, {y_out, flat * 2, -1}};
+  const Rows2D in[4] = {rows_of(x, N, C, ldx, 2), rows_of(residual, N, C, ldr, 2), flat_of(w, C * 2), flat_of(s, C * 2)};
+  const Rows2D out[5] = {rows_of(h_out, N, C, ldh, 2), flat_of(codes, N * C), flat_of(steps, N * 4), flat_of(values, N * C * 2), flat_of(y_out, N * C * 2)};
   for (int i = 0; i < 5; ++i) {
     // the sum may go where x or the residual lie (each element is read by the thread that writes it); nothing else may lie over an input
     for (int j = 0; j < 4; ++j)
-      if (overlap(out[i].p, out[i].bytes, in[j].p, in[j].bytes) && !(out[i].p == in[j].p && out[i].ld == in[j].ld)) return TLQ_ERR_INVALID_ARG;
+      if (overlap(out[i], in[j]) && !(i == 0 && j < 2 && same_rows(out[i], in[j]))) return TLQ_ERR_INVALID_ARG;
     for (int j = 0; j < i; ++j)
-      if (overlap(out[i].p, out[i].bytes, out[j].p, out[j].bytes)) return TLQ_ERR_INVALID_ARG;
+      if (overlap(out[i], out[j])) return TLQ_ERR_INVALID_ARG;
   }
   int rc = have_device();
   if (rc != TLQ_OK || N == 0) return rc;
@@ -160,12 +156,12 @@ int tlq_token_logprobs(const void* logits, int dtype, int64_t N, int64_t V, int6
   if (N > 0) {              // (buffers of no rows may be NULL)
     if ((ids == nullptr) != (logp == nullptr) || (K > 0) != (top_ids != nullptr) || (K > 0) != (top_logp != nullptr)) return TLQ_ERR_INVALID_ARG;
     if (logp == nullptr && entropy == nullptr && lse == nullptr && K == 0) return TLQ_ERR_INVALID_ARG;
-    const struct { const void* p; int64_t bytes; } out[5] = {{logp, N * 4}, {entropy, N * 4}, {lse, N * 4}, {top_ids, N * K * 4}, {top_logp, N * K * 4}};
+    const Rows2D in[2] = {rows_of(logits, N, V, ld, dtype == TLQ_DTYPE_F32 ? 4 : 2), flat_of(ids, N * 4)};
+    const Rows2D out[5] = {flat_of(logp, N * 4), flat_of(entropy, N * 4), flat_of(lse, N * 4), flat_of(top_ids, N * K * 4), flat_of(top_logp, N * K * 4)};
     for (int i = 0; i < 5; ++i) {
-      if (overlap(out[i].p, out[i].bytes, logits, row_bytes(N, V, ld, dtype == TLQ_DTYPE_F32 ? 4 : 2)) || overlap(out[i].p, out[i].bytes, ids, N * 4))
-        return TLQ_ERR_INVALID_ARG;
+      if (overlap(out[i], in[0]) || overlap(out[i], in[1])) return TLQ_ERR_INVALID_ARG;
       for (int j = 0; j < i; ++j)
-        if (overlap(out[i].p, out[i].bytes, out[j].p, out[j].bytes)) return TLQ_ERR_INVALID_ARG;
+        if (overlap(out[i], out[j])) return TLQ_ERR_INVALID_ARG;
     }
   }
   rc = have_device();
@@ -180,19 +176,18 @@ int tlq_distill_loss(const void* logits, int dtype, int64_t N, int64_t V, int64_
   if (rc != TLQ_OK) return rc;
   if (K < 1) return TLQ_ERR_SHAPE;
   if (N > 0 && (top_ids == nullptr || top_logits == nullptr || loss == nullptr)) return TLQ_ERR_INVALID_ARG;
-  if (overlap(loss, N * 4, logits, row_bytes(N, V, ld, dtype == TLQ_DTYPE_F32 ? 4 : 2)) || overlap(loss, N * 4, top_ids, N * K * 4) ||
-      overlap(loss, N * 4, top_logits, N * K * 4) || overlap(loss, N * 4, weights, N * 4))
-    return TLQ_ERR_INVALID_ARG;
+  const int64_t size = dtype == TLQ_DTYPE_F32 ? 4 : 2;
+  const Rows2D in[4] = {rows_of(logits, N, V, ld, size), flat_of(top_ids, N * K * 4), flat_of(top_logits, N * K * 4), flat_of(weights, N * 4)};
+  const Rows2D losses = flat_of(loss, N * 4), gradient = rows_of(grad, N, V, ldg, size);
+  for (int j = 0; j < 4; ++j)
+    if (overlap(losses, in[j])) return TLQ_ERR_INVALID_ARG;
   if (grad != nullptr) {
-    const int64_t size = dtype == TLQ_DTYPE_F32 ? 4 : 2;
     if (ldg < V || ldg > (1LL << 32)) return TLQ_ERR_SHAPE;
     if ((reinterpret_cast<uintptr_t>(grad) & (uintptr_t)(size - 1)) != 0) return TLQ_ERR_ALIGN;
     // the gradient may be written over the logits (each is read by the thread that writes it), but not across them, nor over the rest
-    const int64_t bytes = row_bytes(N, V, ldg, size);
-    if (overlap(grad, bytes, logits, row_bytes(N, V, ld, size)) && !(grad == logits && ldg == ld)) return TLQ_ERR_INVALID_ARG;
-    if (overlap(grad, bytes, top_ids, N * K * 4) || overlap(grad, bytes, top_logits, N * K * 4) || overlap(grad, bytes, weights, N * 4) ||
-        overlap(grad, bytes, loss, N * 4))
-      return TLQ_ERR_INVALID_ARG;
+    for (int j = 0; j < 4; ++j)
+      if (overlap(gradient, in[j]) && !(j == 0 && same_rows(gradient, in[0]))) return TLQ_ERR_INVALID_ARG;
+    if (overlap(gradient, losses)) return TLQ_ERR_INVALID_ARG;
   }
   rc = have_device();
   if (rc != TLQ_OK || N == 0) return rc;
