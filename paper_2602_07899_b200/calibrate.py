@@ -112,8 +112,9 @@ def importance_from_teacher(logits: torch.Tensor, top_ids: torch.Tensor, top_log
                             scale: float = 1.0, norm_kind: int = tlq.NORM_L2, top_frac: float = 0.5
                             ) -> Tuple[torch.Tensor, Optional[torch.Tensor], torch.Tensor]:
     """How much each calibration token says about what quantization changed at the model's output: the norm of the distillation loss's
-    gradient by the token's logits (gradient-derived importance, paper Sec. 3.1.2, with the full-precision model's answers in the place of
-    labels).
+    gradient by the token's logits.  It stands in for the gradient-derived importance of paper Sec. 3.1.2, which is the norm of a loss's
+    gradient by the input of the layer that is calibrated: this one needs no labels and no backward pass through the model, and is the same
+    for all layers.
 
     logits [N,V] (bf16 or float32) of the quantized model, top_ids and top_logits [N,K] the full-precision model's alternatives
     (tlq_token_logprobs' top_ids and top_logp at scale 1; `scale` is applied here, to both models), weights float32 [N] or None.
@@ -125,7 +126,8 @@ def importance_from_teacher(logits: torch.Tensor, top_ids: torch.Tensor, top_log
     if wide == v:
         loss, grad = tlq.tlq_distill_loss(logits, top_ids, top_logits, weights, scale)
     else:       # (zeros behind a row add nothing to its norm)
-        grad = torch.zeros((n, wide), dtype=logits.dtype, device=logits.device)
+        grad = torch.empty((n, wide), dtype=logits.dtype, device=logits.device)
+        grad[:, v:] = 0
         loss, _ = tlq.tlq_distill_loss(logits, top_ids, top_logits, weights, scale, grad=grad[:, :v])
     imp, mask = tlq.tlq_token_importance(grad[None], norm_kind, top_frac)
     if norm_kind == tlq.NORM_MEAN_ABS and wide != v:
