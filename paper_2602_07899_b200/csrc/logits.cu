@@ -7,7 +7,7 @@
 //
 // Maximum and sums run along in one pass (each thread with a maximum of its own, looked at once for a batch of vectors), so that a row is
 // read from memory once.  Bound by memory; the exponentials take 3/4 of that time (16 bits).  4096 x 131072 of 16 bits, which a copy's rate
-// reads in 166 us: log probabilities 174, with 64 alternatives 227, the distillation loss 174, with the gradient (333) 403.
+// reads in 166 us: log probabilities 177, with 64 alternatives 226, the distillation loss 175, with the gradient (333) 405.
 //  - Every warp has slots of shared memory of its own, into which it has pieces of the rows copied ahead of time, the next row's too, so
 //    that the memory has work while the CTA joins its sums, looks for the largest or writes; no warp waits for another but at a row's end.
 //  - The gradient needs the row a second time, and gets it from the second-level cache: a CTA has an SM to itself, and rows are shared by

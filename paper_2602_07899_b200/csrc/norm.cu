@@ -4,8 +4,9 @@
 // between the sums and the codes, and the factors g = w / s of its channels in 32 bits for all rows of the CTA.  The largest |v| is the
 // largest |h g| times the root, so that one sum over the CTA gives both; code = rint(h g k) with k = root / step.  The row after the one in
 // registers is on its way into shared memory, into places of the thread's own: no barrier, and the memory has work while the CTA sums and
-// rounds.  Bound by memory for many rows (8192 x 8192 with all but y: 102 us, 92 % of the copy rate; 4096 x 3584 24), by one trip to memory
-// and the sum over the CTA for a few (1 x 3584: 2.4 us).
+// rounds.  Bound by memory for many rows (8192 x 8192 with all but y: 98 us, 95 % of the copy rate; 4096 x 3584 24), by one trip to memory
+// and the sum over the CTA for a few (1 x 3584: 2.3 us).  With its arguments as __grid_constant__ the compiler
+// needs 8 to 16 registers less where they are not held to 64 (8192 x 8192 102 us without, 98 so).
 #include "serve.cuh"
 
 namespace tlq {
@@ -85,7 +86,8 @@ norm_quantize_kernel(const __grid_constant__ NormArgs a) {
       float s[8];
       unpack8(load_near(reinterpret_cast<const uint4*>(a.s) + p * kThreads + tid), s);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = kKeep ? f[j] * __frcp_rn(s[j]) : __fdividef(f[j] * 0.25f, s[j] * 0.25f);    // (by a divisor over 2^126 it would make 0)
+      for (int j = 0; j < 8; ++j)              // (by a divisor over 2^126 __fdividef would make 0)
+        f[j] = kKeep ? f[j] * __frcp_rn(s[j]) : __fdividef(f[j] * 0.25f, s[j] * 0.25f);
     }
   };
   float kept[kKeep ? kPieces : 1][8];
@@ -196,9 +198,10 @@ norm_quantize_kernel(const __grid_constant__ NormArgs a) {
       }
     }
     if (a.codes == nullptr) continue;
-    if (top == INFINITY && root < INFINITY) {  // |h g| beyond the 32-bit range, which |v| may be in: with h times the power of 2 in the root, where
-      const float power = __uint_as_float(__float_as_uint(root) & 0x7F800000u);      // no |h| is above the square root of the row's length
-      once_more(power);                        // (what gets lost below rounds to 0)
+    if (top == INFINITY && root < INFINITY) {  // |h g| beyond the 32-bit range, which |v| may be in: once more with h times the power of 2 in
+      // the root, where no |h| is above the square root of the row's length (what gets lost below rounds to 0)
+      const float power = __uint_as_float(__float_as_uint(root) & 0x7F800000u);
+      once_more(power);
       root /= power;
     }
     const float largest = top * root;
@@ -212,7 +215,7 @@ norm_quantize_kernel(const __grid_constant__ NormArgs a) {
       if (tid == 0) a.steps[n] = NAN;
       continue;
     }
-    const float step = fmaxf(largest, TLQ_RANGE_FLOOR) * a.inv_qpos, k = __fdividef(root * 0.0625f, step * 0.0625f);   // (of a divisor over 2^126 it would make 0)
+    const float step = fmaxf(largest, TLQ_RANGE_FLOOR) * a.inv_qpos, k = __fdividef(root * 0.0625f, step * 0.0625f);   // (the same)
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
       if (!in[p]) continue;
@@ -276,7 +279,7 @@ int launch_norm_quantize(const uint16_t* x, int64_t N, int64_t C, int64_t ldx, c
     if (pieces <= 1024) return run_norm<2, 512, 1>(a, st);
   } else {                                     // many rows: two pieces to a thread, so that a sum over the CTA serves more bytes (four do
     if (pieces <= 32) return run_norm<1, 32, 1>(a, st);      // not fit into the registers of three CTAs of 256: 8192 x 8192 104 us with two
-    if (pieces <= 64) return run_norm<2, 32, 1>(a, st);      // of them, 141 with spills, 102 so)
+    if (pieces <= 64) return run_norm<2, 32, 1>(a, st);      // of them, 141 with spills, 102 so, then)
     if (pieces <= 128) return run_norm<2, 64, 16>(a, st);
     if (pieces <= 256) return run_norm<2, 128, 8>(a, st);
     if (pieces <= 512) return run_norm<2, 256, 4>(a, st);

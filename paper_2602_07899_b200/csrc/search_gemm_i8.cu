@@ -153,7 +153,7 @@ __device__ __forceinline__ void store16(const float (&f)[16], uint16_t* out, con
 //          with the negate bit) and kept in registers; every candidate adds its bf16 pass X_q dW_k^T to it.
 //          Tensor maps: tmX = X_fp, tmW = W, tmXq = X_q (bf16, 3-D with a single slice), tmWq = dW (bf16, 3-D).
 // kMode 3: apply with activation, gate and residual (epilogue.cuh) before the rounding.  8192 tokens, 3584 -> 18944: 384 to 403 us without
-//          an activation, 387 to 435 with GELU, 354 to 402 gated; the tensor core at the power limit (333 at its measured rate)
+//          an activation, 389 to 443 with GELU, 354 to 402 gated; the tensor core at the power limit (333 at its measured rate)
 template <int kMode>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_w8a8_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW,
