@@ -62,3 +62,26 @@ def test_rows_that_leave_the_range_have_none(tlq, v, dtype, scale, top):  # noqa
     assert torch.isfinite(loss[1::2]).all() and torch.isfinite(grad[1::2].float()).all()
     alone, _ = tlq.tlq_distill_loss(both, ids, teacher, None, scale, want_grad=False)
     assert torch.isnan(alone[::2]).all() and torch.isfinite(alone[1::2]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("v", [9, 1000, 16391, 131072])
+@pytest.mark.parametrize("scale", [1.0, 1.3, 2.0 ** 16])
+def test_rows_in_the_last_powers_of_two_of_the_range(tlq, v, dtype, scale):  # noqa: F811
+    """Logits on both sides of where a power of 2 above scale log2(e) times them leaves the range, in every order."""
+    exact = torch.tensor(scale, dtype=F32).item()
+    a, b, c = (torch.tensor(f * 2.0 ** 128 / exact, dtype=dtype).item() for f in (0.3, 0.6, 0.98))
+    i = torch.arange(v, device="cuda")
+    z = torch.empty(10, v, dtype=torch.float64, device="cuda")
+    z[0], z[1], z[2], z[3], z[4] = a, a, b, b, c
+    z[0, v - 1], z[1, ::5], z[2, v // 2], z[3, 1::3] = b, c, c, a
+    z[5] = torch.where(i < v // 2, a, c)
+    z[6] = torch.where(i < v // 2, c, a)
+    z[7] = (0.1 + 0.85 * i.double() / v) * 2.0 ** 128 / exact
+    z[8] = z[7].flip(0)
+    z[9] = -1
+    z[9, v // 3] = c
+    z = z.to(dtype)
+    check_logprobs(tlq, z, some_ids(10, v), 5, exact)
+    ids, _ = teacher_of(z / 4, 4)
+    check_distill(tlq, z, ids, torch.zeros(10, 4, device="cuda"), None, exact)
